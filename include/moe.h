@@ -169,6 +169,81 @@ moe_status moe_layer_forward(moe_ctx* ctx, const void* x, const void* router_pac
                              const float* bias, const void* packed, int32_t T, void* out,
                              int32_t* counts_out, void* stream);
 
+/* ---- operators around the experts' weights: training them, and serving them in 4 bits --------------------------
+ *
+ * These calls need no context.  Pointers are device memory unless marked "host"; matrices are row-major with rows
+ * `ld*` values apart (a multiple of 8 bf16 or 4 fp32 values, at most 2^21), every base pointer 16-byte aligned.
+ * Widths (K, N, f) are multiples of 8 (K of 32 for 4-bit values), at most 2^17; E <= 256.  A call only launches
+ * kernels on `stream`.  Tensors without rows may be NULL.
+ *
+ * Rows grouped by expert lie as moe_permute leaves them: expert e has rows [offsets[e], offsets[e+1]), offsets [E+1] is
+ * read on the device, n_rows_cap (<= 2^24) is the host's bound on offsets[E] and sizes the launch.  Rows from offsets[E] on are
+ * neither read nor written.  Offsets that do not ascend or pass the bound never lead out of [0, n_rows_cap). */
+
+typedef enum { MOE_BF16 = 0, MOE_F32 = 1 } moe_type;
+
+/* y[r, :] = x[r, :] . W[e] for the rows r of every expert e: bf16 operands, fp32 sums, bf16 results rounded once.
+ * W is [E, K, N] (transpose_w == 0; the layout of W1, W3 and W2) or [E, N, K] (transpose_w != 0: x times W[e]^T).  The
+ * gradient of x is this call on the gradient of y with transpose_w the other way round.
+ * x [n_rows_cap, K], y [n_rows_cap, N]. */
+moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t transpose_w, const int32_t* offsets,
+                            int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y, int64_t ldy, void* stream);
+
+/* Gradient of the weights: dw[e] = sum over the rows r of expert e of x[r, :]^T dy[r, :]  (fp32 sums in a fixed order).
+ * dw [E, K, N] of `type` (moe_type); experts without rows get zeros.  accumulate != 0 (fp32 only): added to what dw
+ * holds, experts without rows are left alone. */
+moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets,
+                                  int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* dw, int32_t type,
+                                  int32_t accumulate, void* stream);
+
+/* h = silu(g) * u with g = gu[:, :f], u = gu[:, f:2f] (bf16).  n_rows: NULL, or the number of rows there are on the device
+ * (e.g. offsets + E), at most n_rows_cap; later rows are left alone.  gu [n_rows_cap, 2f], h [n_rows_cap, f]. */
+moe_status moe_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int32_t n_rows_cap, int32_t f, void* h,
+                      int64_t ldh, void* stream);
+
+/* Gradient of moe_swiglu: dgu[:, :f] = dh u s(g) (1 + g (1 - s(g))), dgu[:, f:] = dh g s(g), s the logistic function.
+ * h NULL, or the rows of moe_swiglu formed again (a program then need not keep them).  dgu may be gu itself. */
+moe_status moe_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int64_t ldgu, const int32_t* n_rows,
+                               int32_t n_rows_cap, int32_t f, void* dgu, int64_t lddgu, void* h, int64_t ldh, void* stream);
+
+/* Global norm of n gradients: norm[0] = sqrt(sum over tensors and values of g^2), squares added in 64 bits in a fixed order.
+ * grads, counts, types: host arrays [n] of device pointers (aligned to their values), numbers of values and moe_type;
+ * norm [1] fp32.  workspace: moe_grad_norm_workspace_bytes(n) bytes, 8-byte aligned, used until the call's work is done.
+ * The host arrays are read before the call returns. */
+size_t moe_grad_norm_workspace_bytes(int32_t n);
+moe_status moe_grad_norm(const void* const* grads /* host */, const int64_t* counts /* host */, const int32_t* types /* host */,
+                         int32_t n, void* workspace, size_t workspace_bytes, float* norm, void* stream);
+
+/* The same norm, and outs[i] = scale * grads[i] with scale = min(1, max_norm / (norm + 1e-6)), of grads[i]'s type.  outs[i] is
+ * grads[i] itself (in place: nothing is written where the scale is 1) or memory of its own.  A norm that is not a number
+ * makes every value one; an infinite one gives 0 * g. */
+moe_status moe_clip_grad_norm(const void* const* grads /* host */, void* const* outs /* host */, const int64_t* counts /* host */,
+                              const int32_t* types /* host */, int32_t n, float max_norm, void* workspace, size_t workspace_bytes,
+                              float* norm, void* stream);
+
+/* Microscaled 4-bit floating point: blocks of 32 neighbouring values of a row share a scale 2^e,
+ *   e = max(floor(log2(largest magnitude)) - 2, -127);  a value is 2^e times one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign,
+ *   the nearest one, ties to the even code, at most 6.
+ * values [rows, K/2]: two codes a byte, the lower index in the lower half (sign bit, then the magnitude's number 0..7);
+ * scales [rows, moe_mxfp4_scale_cols(K)]: e + 127; 0 in blocks of zeros and behind the last block (the products rely on it),
+ * 255 in a block that holds an infinity or a NaN: the whole block then stands for NaN. */
+int32_t moe_mxfp4_scale_cols(int32_t K); /* K / 32 up to the next multiple of 16; 0: K is not supported */
+moe_status moe_mxfp4_quantize(const void* x, int32_t type, int64_t ldx, const int32_t* n_rows, int32_t n_rows_cap, int32_t K,
+                              void* values, void* scales, void* stream); /* n_rows as in moe_swiglu */
+
+/* Weights W [E, K, N] bf16, once at load time: values [E, N, K/2], scales [E, N, scale_cols(K)], blocks along K. */
+moe_status moe_mxfp4_quantize_weights(const void* w, int32_t E, int32_t K, int32_t N, void* values, void* scales, void* stream);
+
+/* The values that rows of codes and scales stand for, in bf16 (exact). */
+moe_status moe_mxfp4_dequantize(const void* values, const void* scales, int64_t rows, int32_t K, void* x, int64_t ldx,
+                                void* stream);
+
+/* y[r, :] = x[r, :] . W[e]^T on such operands: exact products, fp32 sums, bf16 results rounded once.
+ * x_values [n_rows_cap, K/2], x_scales [n_rows_cap, scale_cols(K)], w_values [E, N, K/2], w_scales [E, N, scale_cols(K)]. */
+moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, const void* w_values, const void* w_scales,
+                                  const int32_t* offsets, int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y,
+                                  int64_t ldy, void* stream);
+
 /* ---- introspection --------------------------------------------------------------------------- */
 
 /* Mean milliseconds of each stage over the moe_layer_forward calls made since the previous

@@ -16,4 +16,14 @@ from .binding import (  # noqa: F401
     moe_measure_mfma_rate,
     moe_measure_hbm_read_rate,
     moe_permute_noalloc,
+    moe_grouped_gemm,
+    moe_grouped_gemm_wgrad,
+    moe_swiglu,
+    moe_swiglu_backward,
+    moe_grad_norm,
+    moe_clip_grad_norm,
+    moe_mxfp4_quantize,
+    moe_mxfp4_quantize_weights,
+    moe_mxfp4_dequantize,
+    moe_mxfp4_grouped_gemm,
 )

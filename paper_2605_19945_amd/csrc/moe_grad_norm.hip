@@ -1,0 +1,227 @@
+// Global norm of a list of gradients, and their clipped copy (or clipping in place):
+//   norm = sqrt(sum over tensors and values of g^2),  scale = min(1, max_norm / (norm + 1e-6)),  out = scale * g.
+// Memory bounds both: the norm reads every value once, clipping reads it again and writes it.  The tensors of a launch
+// are cut into parts of equal length that a bounded number of workgroups go through; each workgroup leaves one partial
+// sum, and whoever needs the norm adds the partial sums in the order of their places, so the result does not depend on
+// which workgroup ran when.  Squares are added in 64 bits: gradients whose squares pass the range of 32 bits still have a
+// norm, and the additions stay below the time of the reads (one 64-bit fused multiply-add a value).
+// The clipping launches go through the parts from the last to the first: what the norm has read last is still in the
+// 256 MB last-level cache.
+#include "moe_ops.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPart = 16384;  // values of a part: 64 a lane
+
+struct GradList {
+    const void* grad[GRAD_LIST];
+    void* out[GRAD_LIST];
+    int64_t count[GRAD_LIST];
+    int32_t first_part[GRAD_LIST + 1];  // parts of the tensors before this one
+    uint32_t f32[GRAD_LIST / 32];
+    int n;
+};
+static_assert(sizeof(GradList) < 4000, "kernel arguments");
+
+static __device__ inline int tensor_of(const GradList& l, int part) {
+    int lo = 0, hi = l.n;  // first_part[lo] <= part < first_part[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (l.first_part[mid] <= part) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Sum over the workgroup in a fixed order, in every thread.
+static __device__ inline double block_sum(double v, double* lds) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double s = 0;
+    for (int w = 0; w < kThreads / 64; ++w) s += lds[w];
+    __syncthreads();
+    return s;
+}
+
+template <typename T> struct Words;
+template <> struct Words<float> {
+    static constexpr int PER = 4;  // values of 16 bytes
+    static __device__ inline void open(const u32x4_t& w, float* v) {
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
+    }
+    static __device__ inline u32x4_t close(const float* v) {
+        u32x4_t w;
+        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(v[j]);
+        return w;
+    }
+    static __device__ inline float get(const float* p) { return *p; }
+    static __device__ inline void put(float* p, float v) { *p = v; }
+};
+template <> struct Words<uint16_t> {
+    static constexpr int PER = 8;
+    static __device__ inline void open(const u32x4_t& w, float* v) {
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    }
+    static __device__ inline u32x4_t close(const float* v) {
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        u32x4_t w;
+        for (int j = 0; j < 4; ++j) {
+            const bf16x2_t p = {(__bf16)v[2 * j], (__bf16)v[2 * j + 1]};
+            w[j] = __builtin_bit_cast(uint32_t, p);
+        }
+        return w;
+    }
+    static __device__ inline float get(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+    static __device__ inline void put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+};
+
+// Values [from, to) of a tensor: its 16-byte words between the first and last aligned address, and the values before
+// and behind them one by one.
+template <typename T> static __device__ inline double sum_part(const T* g, int64_t from, int64_t to) {
+    constexpr int PER = Words<T>::PER;
+    double s = 0;
+    const int64_t skew = ((uintptr_t)(g + from) & 15) / sizeof(T);
+    const int64_t a = min(to, from + (skew ? PER - skew : 0)), b = a + (to - a) / PER * PER;
+    for (int64_t i = from + threadIdx.x; i < a; i += kThreads) s += (double)Words<T>::get(g + i) * Words<T>::get(g + i);
+    for (int64_t i = a + threadIdx.x * PER; i < b; i += kThreads * PER) {
+        float v[PER];
+        Words<T>::open(*(const u32x4_t*)(g + i), v);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) s = fma((double)v[j], (double)v[j], s);
+    }
+    for (int64_t i = b + threadIdx.x; i < to; i += kThreads) s += (double)Words<T>::get(g + i) * Words<T>::get(g + i);
+    return s;
+}
+
+template <typename T> static __device__ inline void scale_part(const T* g, T* o, int64_t from, int64_t to, float scale) {
+    constexpr int PER = Words<T>::PER;
+    const int64_t skew = ((uintptr_t)(g + from) & 15) / sizeof(T);
+    const bool alike = (((uintptr_t)g ^ (uintptr_t)o) & 15) == 0;
+    const int64_t a = alike ? min(to, from + (skew ? PER - skew : 0)) : to, b = a + (to - a) / PER * PER;
+    for (int64_t i = from + threadIdx.x; i < a; i += kThreads) Words<T>::put(o + i, Words<T>::get(g + i) * scale);
+    for (int64_t i = a + threadIdx.x * PER; i < b; i += kThreads * PER) {
+        float v[PER];
+        Words<T>::open(*(const u32x4_t*)(g + i), v);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] *= scale;
+        *(u32x4_t*)(o + i) = Words<T>::close(v);
+    }
+    for (int64_t i = b + threadIdx.x; i < to; i += kThreads) Words<T>::put(o + i, Words<T>::get(g + i) * scale);
+}
+
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradList l, double* partials) {
+    __shared__ double lds[kThreads / 64];
+    double s = 0;
+    for (int part = blockIdx.x; part < l.first_part[l.n]; part += gridDim.x) {
+        const int t = tensor_of(l, part);
+        const int64_t from = (int64_t)(part - l.first_part[t]) * kPart, to = min(from + kPart, l.count[t]);
+        if (l.f32[t >> 5] >> (t & 31) & 1) s += sum_part((const float*)l.grad[t], from, to);
+        else s += sum_part((const uint16_t*)l.grad[t], from, to);
+    }
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) partials[blockIdx.x] = s;
+}
+
+static __device__ inline double sum_partials(const double* partials, int n, double* lds) {
+    double s = 0;
+    for (int i = threadIdx.x; i < n; i += kThreads) s += partials[i];
+    return block_sum(s, lds);
+}
+
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* partials, int n, float* norm) {
+    __shared__ double lds[kThreads / 64];
+    const double s = sum_partials(partials, n, lds);
+    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+__global__ __launch_bounds__(kThreads) void clip_kernel(GradList l, const double* partials, int n_partials, float max_norm, float* norm) {
+    __shared__ double lds[kThreads / 64];
+    const double total = sqrt(sum_partials(partials, n_partials, lds));
+    if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+    const double ratio = (double)max_norm / (total + 1e-6);
+    const float scale = ratio > 1.0 ? 1.f : (float)ratio;  // (a NaN stays one)
+    const int parts = l.first_part[l.n];
+    for (int p = blockIdx.x; p < parts; p += gridDim.x) {
+        const int part = parts - 1 - p, t = tensor_of(l, part);
+        if (scale == 1.f && l.grad[t] == l.out[t]) continue;
+        const int64_t from = (int64_t)(part - l.first_part[t]) * kPart, to = min(from + kPart, l.count[t]);
+        if (l.f32[t >> 5] >> (t & 31) & 1) scale_part((const float*)l.grad[t], (float*)l.out[t], from, to, scale);
+        else scale_part((const uint16_t*)l.grad[t], (uint16_t*)l.out[t], from, to, scale);
+    }
+}
+
+// Tensors [first, first + n) as kernel arguments; returns their parts.
+int fill(GradList* l, const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int first, int n) {
+    int parts = 0;
+    l->n = n;
+    for (int i = 0; i < GRAD_LIST / 32; ++i) l->f32[i] = 0;
+    for (int i = 0; i < n; ++i) {
+        l->grad[i] = grads[first + i];
+        l->out[i] = outs != nullptr ? outs[first + i] : nullptr;
+        l->count[i] = counts[first + i];
+        if (f32[first + i]) l->f32[i >> 5] |= 1u << (i & 31);
+        l->first_part[i] = parts;
+        parts += (int)((counts[first + i] + kPart - 1) / kPart);
+    }
+    l->first_part[n] = parts;
+    return parts;
+}
+
+int blocks_of(int parts) { return parts < GRAD_BLOCKS ? (parts > 0 ? parts : 1) : GRAD_BLOCKS; }
+
+hipError_t launch_squares(const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, int* n_partials,
+                          hipStream_t st) {
+    *n_partials = 0;
+    for (int first = 0; first < n; first += GRAD_LIST) {
+        GradList l;
+        const int blocks = blocks_of(fill(&l, grads, nullptr, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
+        grad_squares_kernel<<<blocks, kThreads, 0, st>>>(l, partials + *n_partials);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        *n_partials += blocks;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t grad_norm_workspace(int64_t n_tensors) {
+    const int64_t lists = (n_tensors + GRAD_LIST - 1) / GRAD_LIST;
+    return (size_t)(lists > 0 ? lists : 1) * GRAD_BLOCKS * sizeof(double);
+}
+
+hipError_t launch_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, float* norm,
+                            hipStream_t st) {
+    int np = 0;
+    const hipError_t e = launch_squares(grads, counts, f32, n, partials, &np, st);
+    if (e != hipSuccess) return e;
+    grad_norm_kernel<<<1, kThreads, 0, st>>>(partials, np, norm);
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_grads(const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int n, float max_norm,
+                             double* partials, float* norm, hipStream_t st) {
+    int np = 0;
+    hipError_t e = launch_squares(grads, counts, f32, n, partials, &np, st);
+    if (e != hipSuccess) return e;
+    if (n == 0) {
+        grad_norm_kernel<<<1, kThreads, 0, st>>>(partials, 0, norm);
+        return hipGetLastError();
+    }
+    const int lists = (n + GRAD_LIST - 1) / GRAD_LIST;
+    for (int i = lists - 1; i >= 0; --i) {
+        GradList l;
+        const int first = i * GRAD_LIST;
+        const int blocks = blocks_of(fill(&l, grads, outs, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
+        clip_kernel<<<blocks, kThreads, 0, st>>>(l, partials, np, max_norm, i == lists - 1 ? norm : nullptr);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}

@@ -1,0 +1,118 @@
+// SwiGLU between the experts' two products, and its gradient: h = g s(g) u with s the logistic function,
+// dg = dh u s (1 + g (1 - s)), du = dh g s.  One pass, every value read and written once: 6 bytes a value of h forward,
+// 10 backward (12 where h is formed again), so memory bounds it.  A lane takes 8 neighbouring columns (16 bytes an access)
+// of one row; the arithmetic is in 32 bits and every result is rounded to bf16 once.
+#include "moe_ops.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Row8 { float v[8]; };
+
+static __device__ inline Row8 load8(const uint16_t* p) {
+    const u32x4_t w = *(const u32x4_t*)p;
+    Row8 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        r.v[2 * j] = __uint_as_float(w[j] << 16);
+        r.v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+    return r;
+}
+
+static __device__ inline void store8(uint16_t* p, const Row8& r) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    u32x4_t w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bf16x2_t v = {(__bf16)r.v[2 * j], (__bf16)r.v[2 * j + 1]};
+        w[j] = __builtin_bit_cast(uint32_t, v);
+    }
+    *(u32x4_t*)p = w;
+}
+
+// With e = exp(-|g|) in (0, 1]: 1 / (1 + e) for g >= 0, e / (1 + e) below, which keeps its digits down to the smallest numbers
+static __device__ inline float logistic(float g) {
+    const float e = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e);
+    return g >= 0.f ? r : e * r;
+}
+
+// (row, first column) of chunk i of `chunks` a row; chunk numbers pass 32 bits only for outputs past 64 GB
+static __device__ inline void place(uint64_t i, uint32_t chunks, int64_t* row, int* col) {
+    if (i >> 32) {
+        *row = i / chunks;
+        *col = (int)(i - *row * chunks) * 8;
+    } else {
+        const uint32_t r = (uint32_t)i / chunks;
+        *row = r;
+        *col = (int)((uint32_t)i - r * chunks) * 8;
+    }
+}
+
+static __device__ inline uint64_t live_chunks(const int32_t* n_rows, int rows, int f) {
+    const int n = n_rows != nullptr ? min(max(*n_rows, 0), rows) : rows;
+    return (uint64_t)n * (f / 8);
+}
+
+__global__ __launch_bounds__(kThreads) void swiglu_kernel(const uint16_t* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f,
+                                                          uint16_t* h, int64_t ldh) {
+    const uint64_t total = live_chunks(n_rows, rows, f);
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kThreads) {
+        int64_t row;
+        int col;
+        place(i, f / 8, &row, &col);
+        const uint16_t* p = gu + row * ldgu + col;
+        const Row8 g = load8(p), u = load8(p + f);
+        Row8 o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o.v[j] = g.v[j] * logistic(g.v[j]) * u.v[j];
+        store8(h + row * ldh + col, o);
+    }
+}
+
+template <bool WITH_H>
+__global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* gu, int64_t ldgu,
+                                                                   const int32_t* n_rows, int rows, int f, uint16_t* dgu, int64_t lddgu,
+                                                                   uint16_t* h, int64_t ldh) {
+    const uint64_t total = live_chunks(n_rows, rows, f);
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kThreads) {
+        int64_t row;
+        int col;
+        place(i, f / 8, &row, &col);
+        const uint16_t* p = gu + row * ldgu + col;
+        const Row8 g = load8(p), u = load8(p + f), d = load8(dh + row * lddh + col);
+        Row8 dg, du, o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = logistic(g.v[j]), gs = g.v[j] * s;
+            dg.v[j] = d.v[j] * u.v[j] * (s + gs * (1.f - s));
+            du.v[j] = d.v[j] * gs;
+            o.v[j] = gs * u.v[j];
+        }
+        uint16_t* q = dgu + row * lddgu + col;
+        store8(q, dg);
+        store8(q + f, du);
+        if (WITH_H) store8(h + row * ldh + col, o);
+    }
+}
+
+int blocks_of(int rows, int f) {
+    const int64_t want = ((int64_t)rows * (f / 8) + kThreads - 1) / kThreads;
+    return (int)(want < 8192 ? want : 8192);
+}
+
+}  // namespace
+
+hipError_t launch_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f, void* h, int64_t ldh, hipStream_t st) {
+    swiglu_kernel<<<blocks_of(rows, f), kThreads, 0, st>>>((const uint16_t*)gu, ldgu, n_rows, rows, f, (uint16_t*)h, ldh);
+    return hipGetLastError();
+}
+
+hipError_t launch_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f,
+                                  void* dgu, int64_t lddgu, void* h, int64_t ldh, hipStream_t st) {
+    auto kernel = h != nullptr ? swiglu_backward_kernel<true> : swiglu_backward_kernel<false>;
+    kernel<<<blocks_of(rows, f), kThreads, 0, st>>>((const uint16_t*)dh, lddh, (const uint16_t*)gu, ldgu, n_rows, rows, f, (uint16_t*)dgu,
+                                                    lddgu, (uint16_t*)h, ldh);
+    return hipGetLastError();
+}

@@ -1,0 +1,506 @@
+"""The operators around the experts' weights against plain computations in 64 bits (torch float64 / numpy on the CPU).
+
+Bounds.  Products of small whole numbers have sums that 32 bits hold exactly, in any order: results are then the
+exact ones, rounded once to the output's type, and are compared by equality.  Elsewhere a sum of n products in 32 bits is off by at
+most n 2^-23 times the sum of their magnitudes (2^-24 a rounded addition, twice that where one is cut), and a rounding to
+bf16 by 2^-9 of the value."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_19945_amd as moe
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+
+
+def whole(shape, lo, hi, seed, dtype=BF16):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(lo, hi + 1, shape, generator=g).to(dtype)
+
+
+def normal(shape, seed, std=1.0, dtype=BF16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g, dtype=F32) * std).to(dtype)
+
+
+def offsets_of(rows):
+    return torch.tensor(np.concatenate([[0], np.cumsum(rows)]), dtype=torch.int32)
+
+
+def ref_gemm(x, w, off, transpose_w):
+    out = torch.zeros(x.shape[0], w.shape[1] if transpose_w else w.shape[2], dtype=F64)
+    for e in range(w.shape[0]):
+        a, b = int(off[e]), int(off[e + 1])
+        out[a:b] = x[a:b].double() @ (w[e].double().t() if transpose_w else w[e].double())
+    return out
+
+
+def ref_wgrad(x, dy, off):
+    return torch.stack([x[int(a):int(b)].double().t() @ dy[int(a):int(b)].double() for a, b in zip(off, off[1:])])
+
+
+# rows of the experts, K, N
+SHAPES = [
+    ([1], 8, 8),
+    ([1], 64, 64),
+    ([0, 1, 0], 128, 256),
+    ([2, 0, 0, 3], 72, 40),                 # widths that end inside a K step and inside a tile
+    ([5, 16, 17, 0, 31, 33], 200, 136),
+    ([64, 1, 63], 1032, 264),
+    ([7, 300, 0, 129, 128], 328, 520),
+    ([255, 257, 256], 136, 1288),
+    ([0, 0, 4000, 1], 264, 24),             # one expert has nearly everything
+    ([1200, 0, 900, 801], 192, 6152),       # enough work for the largest tiles, ragged
+    ([3] * 256, 64, 72),                    # as many experts as there may be
+    ([2], 4104, 1544),                      # one token, long reduction
+    ([40, 9], 2056, 2064),
+    ([520, 530], 8, 4096),                  # shortest reduction
+]
+
+
+@pytest.mark.parametrize("rows,K,N", SHAPES)
+@pytest.mark.parametrize("transpose_w", [False, True])
+def test_grouped_gemm_whole_numbers_exactly(rows, K, N, transpose_w):
+    off = offsets_of(rows)
+    x = whole((int(off[-1]), K), -2, 2, 1)
+    w = whole((len(rows), N, K) if transpose_w else (len(rows), K, N), -2, 2, 2)
+    got = moe.moe_grouped_gemm(x.cuda(), w.cuda(), off.cuda(), transpose_w=transpose_w)
+    assert got.dtype == BF16 and torch.equal(got.cpu(), ref_gemm(x, w, off, transpose_w).to(BF16))
+
+
+@pytest.mark.parametrize("rows,K,N", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_grouped_wgrad_whole_numbers_exactly(rows, K, N, dtype):
+    off = offsets_of(rows)
+    x, dy = whole((int(off[-1]), K), -2, 2, 3), whole((int(off[-1]), N), -2, 2, 4)
+    got = moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda(), dtype=dtype)
+    assert got.dtype == dtype and torch.equal(got.cpu(), ref_wgrad(x, dy, off).to(dtype))
+
+
+@pytest.mark.parametrize("rows,K,N", [([3, 0, 250], 136, 264), ([700, 900], 320, 2064)])
+def test_grouped_wgrad_accumulates_and_leaves_empty_experts_alone(rows, K, N):
+    off = offsets_of(rows)
+    x, dy = whole((int(off[-1]), K), -2, 2, 5), whole((int(off[-1]), N), -2, 2, 6)
+    old = whole((len(rows), K, N), -100, 100, 7, F32)
+    out = old.clone().cuda()
+    got = moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda(), out=out, accumulate=True)
+    assert got is out and torch.equal(out.cpu(), (ref_wgrad(x, dy, off) + old).to(F32))
+
+
+@pytest.mark.parametrize("rows,K,N", [([200, 0, 57], 512, 320), ([1500, 1000], 1024, 4096), ([1], 4096, 512), ([17, 3], 14336, 256)])
+def test_grouped_products_of_gaussians_within_their_rounding(rows, K, N):
+    off = offsets_of(rows)
+    n = int(off[-1])
+    x, w, dy = normal((n, K), 8), normal((len(rows), K, N), 9, 0.02), normal((n, N), 10, 0.1)
+    cases = [
+        (moe.moe_grouped_gemm(x.cuda(), w.cuda(), off.cuda()), ref_gemm(x, w, off, False), ref_gemm(x.abs(), w.abs(), off, False), K),
+        (moe.moe_grouped_gemm(dy.cuda(), w.cuda(), off.cuda(), transpose_w=True), ref_gemm(dy, w, off, True),
+         ref_gemm(dy.abs(), w.abs(), off, True), N),
+        (moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda()), ref_wgrad(x, dy, off), ref_wgrad(x.abs(), dy.abs(), off), n),
+    ]
+    for got, ref, size, terms in cases:
+        rounding = 2.0 ** -8 if got.dtype == BF16 else 2.0 ** -24
+        bound = rounding * 1.01 * ref.abs() + terms * 2.0 ** -23 * size + 1e-37
+        assert ((got.cpu().double() - ref).abs() <= bound).all()
+
+
+def test_grouped_gradients_are_those_of_the_product():
+    """The product is linear in x and in w: its difference along a direction is the gradient times that direction,
+    exactly, on whole numbers."""
+    rows, K, N = [33, 0, 90], 72, 104
+    off = offsets_of(rows)
+    n = int(off[-1])
+    x, v, w, u, dy = (whole(s, -2, 2, 20 + i) for i, s in enumerate([(n, K), (n, K), (3, K, N), (3, K, N), (n, N)]))
+
+    def loss(a, b):
+        y = moe.moe_grouped_gemm(a.cuda(), b.cuda(), off.cuda()).cpu().double()
+        return (y * dy.double()).sum()
+
+    dx = moe.moe_grouped_gemm(dy.cuda(), w.cuda(), off.cuda(), transpose_w=True).cpu().double()
+    dw = moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda()).cpu().double()
+    for got, a1, b1, a0, b0, grad, way in [("dx", x + v, w, x, w, dx, v), ("dw", x, w + u, x, w, dw, u)]:
+        y1, y0 = ref_gemm(a1, b1, off, False), ref_gemm(a0, b0, off, False)
+        # each of the two sums is off by its rows' roundings to bf16 alone, and dx by its own
+        slack = 2.0 ** -8 * float(((y1.abs() + y0.abs()) * dy.double().abs()).sum() + (grad.abs() * way.double().abs()).sum())
+        assert abs(float(loss(a1, b1) - loss(a0, b0) - (grad * way.double()).sum())) <= slack, got
+        exact = ((y1 - y0) * dy.double()).sum()
+        assert abs(float(exact - (grad * way.double()).sum())) <= 2.0 ** -8 * float((grad.abs() * way.double().abs()).sum()), got
+
+
+def test_grouped_rows_strides_and_what_lies_behind_them():
+    """Views into wider rows; NaN between the rows' ends, behind the last row and in the weights of an expert without rows
+    reach nothing; rows behind offsets[E] and columns beside the view stay as they are."""
+    rows, K, N, extra = [70, 0, 45], 136, 200, 30
+    off = offsets_of(rows)
+    n = int(off[-1])
+    xs = torch.full((n + extra, K + 24), float("nan"), dtype=BF16)
+    xs[:n, :K] = whole((n, K), -2, 2, 30)
+    w = whole((3, K, N), -2, 2, 31)
+    w[1] = float("nan")
+    ys = torch.full((n + extra, N + 16), 7.0, dtype=BF16)
+    xg, yg = xs.cuda(), ys.cuda()
+    ref = ref_gemm(xs[:n, :K], torch.where(torch.isnan(w), torch.zeros_like(w), w), off, False).to(BF16)
+    out = moe.moe_grouped_gemm(xg[:, :K], w.cuda(), off.cuda(), out=yg[:, 8:8 + N])
+    assert out.data_ptr() == yg[:, 8:].data_ptr()
+    want = ys.clone()
+    want[:n, 8:8 + N] = ref
+    assert torch.equal(yg.cpu(), want)
+    # the transposed kind, and the weight gradient from the same views
+    wt = w.transpose(1, 2).contiguous()
+    yg = ys.cuda()
+    moe.moe_grouped_gemm(xg[:, :K], wt.cuda(), off.cuda(), transpose_w=True, out=yg[:, 8:8 + N])
+    assert torch.equal(yg.cpu(), want)
+    dys = torch.full((n + extra, N + 8), float("nan"), dtype=BF16)
+    dys[:n, :N] = whole((n, N), -2, 2, 32)
+    dw = moe.moe_grouped_gemm_wgrad(xg[:, :K], dys.cuda()[:, :N], off.cuda())
+    assert torch.equal(dw.cpu(), ref_wgrad(xs[:n, :K], dys[:n, :N], off).to(F32))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_grouped_non_finite_rows_stay_with_their_expert(bad):
+    rows, K, N = [37, 50, 3], 104, 144
+    off = offsets_of(rows)
+    x, w, dy = whole((90, K), -2, 2, 40), whole((3, K, N), 1, 2, 41), whole((90, N), 1, 2, 42)
+    x[36] = bad  # the last row of expert 0, beside the first of expert 1
+    x[87] = bad
+    got = moe.moe_grouped_gemm(x.cuda(), w.cuda(), off.cuda()).cpu()
+    ref = ref_gemm(x, w, off, False)
+    keep = [i for i in range(90) if i not in (36, 87)]
+    assert torch.equal(got[keep], ref[keep].to(BF16)) and not torch.isfinite(got[[36, 87]]).any()
+    dw = moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda()).cpu()
+    assert torch.equal(dw[1], ref_wgrad(x, dy, off)[1].to(F32)) and not torch.isfinite(dw[[0, 2]]).any()
+
+
+def test_grouped_offsets_out_of_order_stay_inside_the_bound():
+    """Offsets that pass the number of rows, descend or are negative: whatever is computed, nothing is read or written outside."""
+    K, N, cap = 64, 72, 40
+    x, w = whole((cap, K), -2, 2, 50).cuda(), whole((4, K, N), -2, 2, 51).cuda()
+    guard = torch.full((cap + 64, N), 5.0, dtype=BF16, device="cuda")
+    for off in ([0, 10, 30, 50, 90], [0, 30, 20, 40, 40], [-5, 10, 20, 30, 40], [0, 0, 0, 0, 2 ** 31 - 1]):
+        o = torch.tensor(off, dtype=torch.int32).cuda()
+        moe.moe_grouped_gemm(x, w, o, out=guard[32:32 + cap])
+        dw = moe.moe_grouped_gemm_wgrad(x, x, o)
+        assert (guard[:32] == 5).all() and (guard[32 + cap:] == 5).all() and torch.isfinite(dw).all()
+        inside = torch.tensor(off).clamp(0, cap)
+        ref = ref_wgrad(x.cpu(), x.cpu(), torch.maximum(inside, torch.cummax(inside * 0, 0).values))
+        for e in range(4):
+            if inside[e + 1] >= inside[e]:
+                assert torch.equal(dw[e].cpu(), ref[e].to(F32))
+
+
+def test_grouped_no_rows_at_all():
+    off = torch.zeros(4, dtype=torch.int32).cuda()
+    x, w, dy = torch.empty(0, 64, dtype=BF16).cuda(), whole((3, 64, 40), -2, 2, 60).cuda(), torch.empty(0, 40, dtype=BF16).cuda()
+    assert moe.moe_grouped_gemm(x, w, off).shape == (0, 40)
+    assert (moe.moe_grouped_gemm_wgrad(x, dy, off) == 0).all()
+    some = whole((5, 64), -2, 2, 61).cuda()  # a bound, but no rows
+    assert (moe.moe_grouped_gemm_wgrad(some, whole((5, 40), -2, 2, 62).cuda(), off) == 0).all()
+
+
+# ---- SwiGLU ----------------------------------------------------------------------------------------------
+def ref_swiglu(dh, gu):
+    f = dh.shape[1]
+    g, u, d = gu[:, :f].double(), gu[:, f:].double(), dh.double()
+    s = torch.sigmoid(g)
+    return g * s * u, torch.cat([d * u * s * (1 + g * (1 - s)), d * g * s], 1)
+
+
+@pytest.mark.parametrize("rows,f", [(1, 8), (1, 14336), (3, 72), (616, 768), (257, 1352), (2049, 520)])
+def test_swiglu_and_its_gradient(rows, f):
+    gu, dh = normal((rows, 2 * f), 70, 3.0), normal((rows, f), 71)
+    gu[0, :8] = torch.tensor([0.0, -0.0, 100.0, -100.0, 1e30, -1e30, 88.0, -88.0], dtype=BF16)
+    h, dgu = ref_swiglu(dh, gu)
+    got = moe.moe_swiglu(gu.cuda()).cpu().double()
+    again = torch.empty(rows, f, dtype=BF16, device="cuda")
+    dgot = moe.moe_swiglu_backward(dh.cuda(), gu.cuda(), h=again).cpu().double()
+    # the arithmetic in 32 bits, about ten roundings of 2^-24 and an exponential good to 2^-21; the bracket 1 + g (1 - s)
+    # cancels around g = -1.28, so its error counts against the size of its terms
+    small = 2.0 ** -19
+    assert ((got - h).abs() <= (2.0 ** -8 * 1.01 + small) * h.abs() + 1e-37).all()
+    d = dh.double().abs()
+    g, u = gu[:, :f].double(), gu[:, f:].double()
+    s = torch.sigmoid(g)
+    terms = torch.cat([d * u.abs() * s * (1 + g.abs() * (1 - s)), d * (g * s).abs()], 1)
+    assert ((dgot - dgu).abs() <= 2.0 ** -8 * 1.01 * dgu.abs() + small * terms + 1e-37).all()
+    assert torch.equal(again.cpu().double(), got)
+
+
+def test_swiglu_gradient_against_differences():
+    gu, dh = normal((4, 64), 72).double(), normal((4, 32), 73).double()
+    got = moe.moe_swiglu_backward(dh.to(BF16).cuda(), gu.to(BF16).cuda()).cpu().double()
+    h = 1e-5
+    for r, c in [(0, 0), (1, 17), (2, 31), (3, 32), (0, 63), (2, 40)]:
+        up, down = gu.clone(), gu.clone()
+        up[r, c] += h
+        down[r, c] -= h
+        slope = float(((ref_swiglu(dh, up)[0] - ref_swiglu(dh, down)[0]) * dh).sum() / (2 * h))
+        assert abs(float(got[r, c]) - slope) <= 2.0 ** -8 * abs(slope) + 1e-5
+
+
+def test_swiglu_views_in_place_and_rows_that_are_not_there():
+    rows, f = 50, 136
+    wide = normal((rows, 2 * f + 40), 74)
+    dh = normal((rows, f), 75)
+    off = torch.tensor([0, 12, 31], dtype=torch.int32)
+    gu = wide[:, 16:16 + 2 * f]
+    h, dgu = ref_swiglu(dh, gu)
+    out = torch.full((rows, f + 8), 3.0, dtype=BF16, device="cuda")
+    moe.moe_swiglu(wide.cuda()[:, 16:16 + 2 * f], offsets=off.cuda(), out=out[:, :f])
+    assert ((out[:31, :f].cpu().double() - h[:31]).abs() <= 2.0 ** -8 * h[:31].abs()).all()
+    assert (out[31:] == 3).all() and (out[:, f:] == 3).all()
+    buf = wide.cuda()
+    view = buf[:, 16:16 + 2 * f]
+    moe.moe_swiglu_backward(dh.cuda(), view, offsets=off.cuda(), out=view)  # over gu itself
+    assert torch.equal(buf[31:].cpu(), wide[31:]) and torch.equal(buf[:, :16].cpu(), wide[:, :16])
+    assert torch.equal(view[:31].cpu(), moe.moe_swiglu_backward(dh.cuda(), wide.cuda()[:, 16:16 + 2 * f]).cpu()[:31])
+    for n in (0, -3, 1000):  # no rows, a count that is none, a count past the bound
+        out.fill_(3.0)
+        moe.moe_swiglu(wide.cuda()[:, 16:16 + 2 * f], offsets=torch.tensor([n], dtype=torch.int32).cuda(), out=out[:, :f])
+        assert bool((out[:, :f] == 3).all()) == (n <= 0) and (out[:, f:] == 3).all()
+
+
+# ---- norms of gradients ----------------------------------------------------------------------------------
+def grads_of(kind):
+    if kind == "one":
+        return [normal((1,), 80, dtype=F32)]
+    if kind == "ragged":  # views that begin anywhere, both types, empty ones among them
+        flat, half = normal((40000,), 81, dtype=F32), normal((70000,), 82)
+        return [flat[1:8], flat[9:9], flat[10:16395], half[3:4], half[5:33000], half[33001:33001], half[33002:70000], flat[16395:40000]]
+    if kind == "many":    # more tensors than one launch takes
+        flat = normal((300 * 37,), 83, dtype=F32)
+        return [flat[37 * i:37 * i + 1 + i % 37] for i in range(300)]
+    return [normal((3, 1000, 333), 84, 1e-3, F32), normal((2000, 1001), 85, 5e-3), normal((7,), 86, dtype=F32)]
+
+
+def on_gpu(grads):
+    """On the GPU, at the same distance from a 16-byte boundary as here."""
+    out = []
+    for g in grads:
+        skip = g.storage_offset() % 8
+        buf = torch.zeros(g.numel() + skip, dtype=g.dtype, device="cuda")
+        buf[skip:] = g.reshape(-1).cuda()
+        out.append(buf[skip:].view(g.shape))
+    return out
+
+
+@pytest.mark.parametrize("kind", ["one", "ragged", "many", "large"])
+@pytest.mark.parametrize("share", [0.25, 4.0])
+def test_clip_grad_norm(kind, share):
+    grads = grads_of(kind)
+    norm = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    scale = min(1.0, float(np.float32(share * norm)) / (norm + 1e-6))
+    dev = on_gpu(grads)
+    assert abs(float(moe.moe_grad_norm(dev)) - norm) <= 2.0 ** -23 * norm
+    out = [torch.full_like(g, 9.0) for g in dev]
+    got = moe.moe_clip_grad_norm(dev, share * norm, out=out)
+    assert abs(float(got) - norm) <= 2.0 ** -23 * norm and got.dim() == 0
+    for g, d, o in zip(grads, dev, out):
+        assert torch.equal(d.cpu(), g)
+        rounding = 2.0 ** -8 * 1.01 if g.dtype == BF16 else 2.0 ** -23
+        assert ((o.cpu().double() - g.double() * scale).abs() <= rounding * g.double().abs() * scale + 1e-38).all()
+    assert float(moe.moe_clip_grad_norm(dev, share * norm)) == float(got)
+    for d, o, g in zip(dev, out, grads):
+        assert torch.equal(d, o)                      # in place: the same values
+        assert share < 1 or torch.equal(d.cpu(), g)   # nothing to clip: untouched
+
+
+def test_clip_into_memory_aligned_otherwise():
+    g = normal((5000,), 87).cuda()
+    out = torch.zeros(5003, dtype=BF16, device="cuda")
+    moe.moe_clip_grad_norm([g], 1.0, out=[out[3:]])
+    want = torch.zeros(5000, dtype=BF16, device="cuda")
+    moe.moe_clip_grad_norm([g], 1.0, out=[want])
+    assert torch.equal(out[3:], want) and (out[:3] == 0).all()
+
+
+def test_grad_norm_of_extreme_values_and_of_none():
+    big = torch.full((1000,), 1e30, dtype=F32, device="cuda")   # squares pass the range of 32 bits
+    assert abs(float(moe.moe_grad_norm([big])) / (1e30 * math.sqrt(1000)) - 1) < 1e-6
+    moe.moe_clip_grad_norm([big], 1.0)
+    assert abs(float(moe.moe_grad_norm([big])) - 1) < 1e-6
+    tiny = torch.full((1000,), 1e-30, dtype=F32, device="cuda")
+    assert abs(float(moe.moe_grad_norm([tiny])) / (1e-30 * math.sqrt(1000)) - 1) < 1e-6
+    huge = torch.full((1000,), 3e38, dtype=F32, device="cuda")
+    assert math.isinf(float(moe.moe_grad_norm([huge])))         # the norm itself is past 32 bits
+    assert float(moe.moe_grad_norm([])) == 0 and float(moe.moe_clip_grad_norm([], 1.0)) == 0
+    zeros = torch.zeros(100, dtype=BF16, device="cuda")
+    assert float(moe.moe_clip_grad_norm([zeros], 0.0)) == 0 and (zeros == 0).all()
+    for bad, left in ((float("nan"), float("nan")), (float("inf"), 0.0)):
+        g = torch.ones(64, dtype=F32, device="cuda")
+        g[5] = bad
+        n = float(moe.moe_clip_grad_norm([g], 1.0))
+        assert math.isnan(n) if math.isnan(bad) else math.isinf(n)
+        assert math.isnan(float(g[5])) and (math.isnan(float(g[0])) if math.isnan(left) else float(g[0]) == 0)
+
+
+def test_grad_norm_gives_the_same_bits_every_time():
+    grads = on_gpu(grads_of("large"))
+    assert len({float(moe.moe_grad_norm(grads)) for _ in range(20)}) == 1
+
+
+# ---- 4-bit values ----------------------------------------------------------------------------------------
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def ref_quantize(x):
+    """Rows of float64 -> (codes [n, K], scale bytes [n, K / 32]) by a search for the nearest magnitude, ties to the even one."""
+    b = x.reshape(x.shape[0], -1, 32)
+    bad = ~np.isfinite(b).all(-1)
+    b = np.where(bad[..., None], 0.0, b)
+    top = np.abs(b).max(-1)
+    e = np.where(top > 0, np.maximum(np.floor(np.log2(np.where(top > 0, top, 1))) - 2, -127), -127)
+    away = np.abs(np.abs(b)[..., None] * 2.0 ** -e[..., None, None] - GRID)
+    away[..., 1::2] += 1e-12  # of two at the same distance the even one
+    code = away.argmin(-1) + 8 * np.signbit(b)
+    code = np.where(bad[..., None], 0, code)
+    return code.reshape(x.shape).astype(np.uint8), np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def unpack(values):
+    v = values.cpu().numpy()
+    return np.stack([v & 15, v >> 4], -1).reshape(*v.shape[:-1], -1)
+
+
+def values_of(codes, scales):
+    m = np.concatenate([GRID, -GRID])[codes].reshape(*codes.shape[:-1], -1, 32)
+    unit = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return (m * unit[..., None]).reshape(codes.shape)
+
+
+def special_rows(K, dtype):
+    """Rows whose blocks try the rounding: ties, values under the smallest scale, zeros, infinities, NaN."""
+    x = normal((12, K), 90, dtype=F32)
+    x[0] = 0
+    x[1, :32] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 7.5, 6.5, 0.24, 0.26, 1.0, 4.5, 5.5, 2.25] * 2)
+    x[2] *= 2.0 ** -126
+    x[3] *= 2.0 ** 120
+    x[4, 5] = float("inf")
+    x[5, K - 1] = float("nan")
+    x[6, 3] = -float("inf")
+    x[7, :32] = 0
+    x[7, 4] = -5.0
+    x[8] *= 1e-39
+    x[9, :32] = -0.0
+    x[10, :32] = torch.arange(32) * 2.0 ** -133
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("rows,K", [(12, 32), (12, 96), (12, 512), (12, 544), (300, 2048), (1, 14336)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_mxfp4_quantize_exactly(rows, K, dtype):
+    x = special_rows(K, dtype) if rows == 12 else normal((rows, K), 91, dtype=dtype)
+    code, byte = ref_quantize(x.double().numpy())
+    values, scales = moe.moe_mxfp4_quantize(x.cuda())
+    assert values.shape == (rows, K // 2) and scales.shape == (rows, -(-K // 512) * 16)
+    got = scales.cpu().numpy()
+    assert (got[:, :K // 32] == byte).all() and (got[:, K // 32:] == 0).all()
+    assert (unpack(values) == code).all()
+    back = moe.moe_mxfp4_dequantize(values, scales).cpu().double().numpy()
+    np.testing.assert_array_equal(back, values_of(code, byte))
+
+
+def test_mxfp4_quantize_views_and_rows_that_are_not_there():
+    wide = normal((40, 200), 92)
+    off = torch.tensor([0, 3, 17], dtype=torch.int32).cuda()
+    values, scales = moe.moe_mxfp4_quantize(wide.cuda()[:, 8:8 + 160], offsets=off)
+    code, byte = ref_quantize(wide[:17, 8:168].double().numpy())
+    assert (unpack(values)[:17] == code).all() and (scales.cpu().numpy()[:17, :5] == byte).all()
+
+
+@pytest.mark.parametrize("E,K,N", [(1, 32, 8), (3, 96, 40), (2, 544, 136), (4, 256, 200), (1, 2048, 1032)])
+def test_mxfp4_quantize_weights_exactly(E, K, N):
+    w = normal((E, K, N), 93, 0.02)
+    w[0, :32, 0] = 0
+    w[0, 3, 1] = float("inf")
+    values, scales = moe.moe_mxfp4_quantize_weights(w.cuda())
+    assert values.shape == (E, N, K // 2) and scales.shape == (E, N, -(-K // 512) * 16)
+    for e in range(E):
+        code, byte = ref_quantize(w[e].t().double().numpy())
+        assert (unpack(values[e]) == code).all() and (scales[e].cpu().numpy()[:, :K // 32] == byte).all()
+        assert (scales[e].cpu().numpy()[:, K // 32:] == 0).all()
+
+
+def test_mxfp4_dequantize_every_code_under_every_scale():
+    codes = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
+    values = torch.tensor(codes[:, 0::2] | codes[:, 1::2] << 4).cuda()
+    scales = torch.zeros(256, 16, dtype=torch.uint8)
+    scales[:, 0] = torch.arange(256)
+    got = moe.moe_mxfp4_dequantize(values, scales.cuda()).cpu()
+    want = torch.tensor(values_of(codes, np.arange(256, dtype=np.uint8)[:, None]))
+    want = torch.where(want.abs() > 3.39e38, torch.sign(want) * float("inf"), want)  # past bf16
+    np.testing.assert_array_equal(got.double().numpy(), want.numpy())
+
+
+MX_SHAPES = [([1], 32, 8), ([0, 3, 0], 96, 40), ([5, 17, 0, 33], 544, 136), ([64, 1, 130], 1056, 264), ([300, 0, 257], 288, 520),
+             ([1200, 0, 900, 801], 320, 6152), ([2] * 256, 64, 72), ([1], 14336, 512), ([9, 40], 4096, 1032)]
+
+
+@pytest.mark.parametrize("rows,K,N", MX_SHAPES)
+def test_mxfp4_grouped_gemm(rows, K, N):
+    off, E = offsets_of(rows), len(rows)
+    n = int(off[-1])
+    x, w = normal((n, K), 94), normal((E, K, N), 95, 0.02)
+    x *= torch.tensor([1.0, 100.0, 1e-3])[torch.arange(n) % 3][:, None].to(BF16)  # scales that differ from row to row
+    xq, xs = moe.moe_mxfp4_quantize(x.cuda())
+    wq, ws = moe.moe_mxfp4_quantize_weights(w.cuda())
+    got = moe.moe_mxfp4_grouped_gemm(xq, xs, wq, ws, off.cuda()).cpu().double()
+    xv = torch.tensor(values_of(unpack(xq), xs.cpu().numpy()[:, :K // 32]))
+    wv = torch.tensor(values_of(unpack(wq), ws.cpu().numpy()[:, :, :K // 32]))
+    ref = ref_gemm(xv, wv, off, True)
+    bound = 2.0 ** -8 * 1.01 * ref.abs() + K * 2.0 ** -23 * ref_gemm(xv.abs(), wv.abs(), off, True) + 1e-37
+    assert ((got - ref).abs() <= bound).all()
+
+
+def test_mxfp4_grouped_gemm_not_a_number_and_rows_that_are_not_there():
+    rows, K, N = [37, 0, 12], 96, 72
+    off = offsets_of(rows)
+    x, w = normal((60, K), 96), normal((3, K, N), 97)
+    x[36, 40] = float("inf")
+    xq, xs = moe.moe_mxfp4_quantize(x.cuda())
+    xs[49:] = 255  # rows behind the last one
+    wq, ws = moe.moe_mxfp4_quantize_weights(w.cuda())
+    ws[1] = 255    # weights of the expert without rows
+    out = torch.full((60, N + 8), 5.0, dtype=BF16, device="cuda")
+    moe.moe_mxfp4_grouped_gemm(xq, xs, wq, ws, off.cuda(), out=out[:, :N])
+    got = out.cpu()
+    assert torch.isnan(got[36, :N]).all() and torch.isfinite(got[:36]).all() and torch.isfinite(got[37:49]).all()
+    assert (got[49:] == 5).all() and (got[:, N:] == 5).all()
+
+
+# ---- streams and graphs ----------------------------------------------------------------------------------
+def small_step(x, w, off):
+    gu = moe.moe_grouped_gemm(x, w, off)
+    h = moe.moe_swiglu(gu)
+    dgu = moe.moe_swiglu_backward(h, gu)
+    dw = moe.moe_grouped_gemm_wgrad(x, dgu, off)
+    dx = moe.moe_grouped_gemm(dgu, w, off, transpose_w=True)
+    norm = moe.moe_clip_grad_norm([dw], 1.0)
+    xq, xs = moe.moe_mxfp4_quantize(dx)
+    wq, ws = moe.moe_mxfp4_quantize_weights(w)
+    return [gu, h, dgu, dw, dx, norm, moe.moe_mxfp4_grouped_gemm(xq, xs, wq, ws, off)]
+
+
+def test_operators_on_another_stream_and_in_a_graph():
+    off = offsets_of([20, 0, 130]).cuda()
+    x, w = normal((150, 128), 98).cuda(), normal((3, 128, 192), 99, 0.1).cuda()
+    want = [t.clone() for t in small_step(x, w, off)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = small_step(x, w, off)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = small_step(x, w, off)
+    for i in range(4):
+        x.copy_(normal((150, 128), 200 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = small_step(x, w, off)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager)), i
