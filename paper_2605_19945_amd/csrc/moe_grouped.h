@@ -150,6 +150,15 @@ static __device__ inline bool find_weight_tile(const GroupedArgs& g, int mt, int
     return true;
 }
 
+// 16-byte chunk c of a row lies at chunk c ^ swizzle(row) of its LDS row, so that the lanes that read together fall on
+// different banks.  LAY_MN: rows 0-3 and 8-11, two neighbouring chunks.  LAY_K: a 16-byte read serves lanes 0-3, 12-15 and 20-27 together,
+// so rows 0-3 and 12-15 of one chunk (swizzles 0 to 3) and rows 4-11 of a second one (4 to 7): whichever two chunks of an even distance
+// below 4 or neighbouring ones those are, the two sets stay apart (no conflicts counted for either format).
+static __device__ inline int swizzle_k(int row) {
+    const int t = row >> 1;
+    return (t & 1) | (t >> 1 & 2) | ((t ^ t << 1) & 4);
+}
+
 // One operand's share of a wave: NL loads of 1 KiB a K step.
 template <int LAY, int B, int NL> struct Loader {
     static constexpr int ROW = LAY == LAY_K ? 128 : 2 * B;  // bytes of a row in LDS
@@ -183,28 +192,27 @@ template <int LAY, int B, int NL> struct Loader {
             if (LAY == LAY_MN && c * 16 >= (int)width) offset[j] = OUT_OF_RANGE;
         }
     }
-    // 16-byte chunk c of a row lies at chunk c ^ swizzle(row) of its LDS row: the lanes that read together then fall on
-    // different banks (LAY_K: 16 rows, one chunk; LAY_MN: rows 0-3 and 8-11, two neighbouring chunks)
-    static __device__ inline int swizzle(int row) {
-        return LAY == LAY_K ? (row >> 1) & 7 : 2 * ((row & 3) + 4 * ((row >> 3) & 1));
-    }
+    static __device__ inline int swizzle(int row) { return LAY == LAY_K ? swizzle_k(row) : 2 * ((row & 3) + 4 * ((row >> 3) & 1)); }
     __device__ inline u32x4_t desc() const {
-        if (LAY == LAY_K) return make_desc(base, rows > 0 && (int)width > 0 ? (rows - 1) * ld + width : 0);
+        if (LAY == LAY_K) return make_desc(base, rows > 0 ? (rows - 1) * ld + width : 0);
         return make_desc(base, rows > 0 ? (min(rows, 64) - 1) * ld + width : 0);
     }
-    __device__ inline void issue(const u32x4_t& d, uint32_t to, int j, int wave) const {
-        uint32_t o = offset[j];
-        if (LAY == LAY_K && (int)width < 128) {  // the last K step of a row that ends inside it
-            const int p = (wave * NL + j) * 1024 + (threadIdx.x & 63) * 16;
-            const int c = ((p % ROW) / 16) ^ swizzle(p / ROW);
-            if (c * 16 >= (int)width) o = OUT_OF_RANGE;
-        }
-        load_to_lds(to + (wave * NL + j) * 1024, o, d);
-    }
+    __device__ inline void issue(const u32x4_t& d, uint32_t to, int j, int wave) const { load_to_lds(to + (wave * NL + j) * 1024, offset[j], d); }
     __device__ inline void next() {
         base += step;
         if (LAY == LAY_K) width -= 128;
         else rows -= 64;
+    }
+    // before the last K step, of a row that may end inside it
+    __device__ inline void cut(int wave) {
+        if (LAY == LAY_K && width < 128) {
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const int p = (wave * NL + j) * 1024 + (threadIdx.x & 63) * 16;
+                const int c = ((p % ROW) / 16) ^ swizzle(p / ROW);
+                if (c * 16 >= (int)width) offset[j] = OUT_OF_RANGE;
+            }
+        }
     }
 };
 
@@ -221,7 +229,7 @@ template <int FMT, int LAY, int B> struct Reader {
             for (int h = 0; h < 2; ++h) {
                 // 4-bit values: a lane's two blocks of 32 are neighbours, in both operands alike
                 const int c = FMT == FMT_MX4 ? 2 * q + h : 4 * h + q;
-                at[h] = (first + i) * 128 + ((c ^ ((i >> 1) & 7)) * 16);
+                at[h] = (first + i) * 128 + ((c ^ swizzle_k(i)) * 16);
             }
         } else {
             cl = (8 * q + (i >> 2)) * (2 * B) + (i & 1) * 8;
@@ -253,19 +261,14 @@ static __device__ inline uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, v);
 }
 
-template <int FMT> static __device__ inline f32x4_t multiply(const s16x8_t& b, const s16x8_t& a, f32x4_t c, int sb, int sa, Int<0>) {
+// One matrix instruction on fragments of 16 columns (b) and 16 rows (a); 4-bit ones take their blocks' scales from byte
+// SB of sb and byte SA of sa.
+template <int FMT, int SB, int SA> static __device__ inline f32x4_t multiply(const s16x8_t& b, const s16x8_t& a, f32x4_t c, int sb, int sa) {
     if constexpr (FMT == FMT_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b), __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
     typedef int i32x4_t __attribute__((ext_vector_type(4)));
     const i32x4_t x = __builtin_bit_cast(i32x4_t, b), y = __builtin_bit_cast(i32x4_t, a);
     const i32x8_t u = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, v = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, c, 4, 4, 0, sb, 0, sa);
-}
-template <int FMT> static __device__ inline f32x4_t multiply(const s16x8_t& b, const s16x8_t& a, f32x4_t c, int sb, int sa, Int<1>) {
-    if constexpr (FMT == FMT_BF16) return multiply<FMT>(b, a, c, sb, sa, Int<0>{});
-    typedef int i32x4_t __attribute__((ext_vector_type(4)));
-    const i32x4_t x = __builtin_bit_cast(i32x4_t, b), y = __builtin_bit_cast(i32x4_t, a);
-    const i32x8_t u = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, v = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, c, 4, 4, 1, sb, 1, sa);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, c, 4, 4, SB, sb, SA, sa);
 }
 
 // Stores a wave's FM x FN fragments.  The weights are the first operand of the matrix instruction, so a lane has 4
@@ -329,13 +332,13 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     else lb.init(WEIGHTS ? g.b + (int64_t)t.lo * g.ldb + (int64_t)t.n0 * 2 : wb + (int64_t)t.n0 * 2, g.ldb, ncols, red, wave);
     const int steps = (red + (MX ? 127 : 63)) / (MX ? 128 : 64);
 
-    auto issue = [&](int kt) {
-        const int s = kt & 1;
-        const u32x4_t da = la.desc(), db = lb.desc();
-        repeat<NLA>([&](auto j) { la.issue(da, lds_addr(lds_a) + s * BM * 128, j.value, wave); });
-        repeat<NLB>([&](auto j) { lb.issue(db, lds_addr(lds_b) + s * BN * 128, j.value, wave); });
+    // The loads of a stage, one at a time: begin(kt), load(kt, 0 .. NLA + NLB - 1), end().
+    u32x4_t da, db;
+    auto begin = [&](int kt) {
+        da = la.desc();
+        db = lb.desc();
         if constexpr (MX) {
-            if (s == 0) repeat<NS>([&](auto j) {
+            if ((kt & 1) == 0) repeat<NS>([&](auto j) {
                 const int part = wave * NS + j.value;  // 64 rows of a, or of b behind them
                 const bool of_b = part * 64 >= BM;
                 const int row = part * 64 - (of_b ? BM : 0), have = min((of_b ? ncols : mrows) - row, 64);
@@ -344,6 +347,18 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
                 load_to_lds(lds_addr(lds_s) + ((kt >> 1) & 1) * (BM + BN) * 16 + part * 1024, (threadIdx.x & 63) * g.scale_ld, d);
             });
         }
+    };
+    auto load = [&](int kt, auto j) {
+        if constexpr (j.value < NLA) la.issue(da, lds_addr(lds_a) + (kt & 1) * BM * 128, j.value, wave);
+        else lb.issue(db, lds_addr(lds_b) + (kt & 1) * BN * 128, j.value - NLA, wave);
+    };
+    auto cut = [&]() {
+        la.cut(wave);
+        lb.cut(wave);
+    };
+    auto issue = [&](int kt) {
+        begin(kt);
+        repeat<NLA + NLB>([&](auto j) { load(kt, j); });
         la.next();
         lb.next();
     };
@@ -359,32 +374,85 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     ra.init(wm * FM * 16);
     rb.init(wn * FN * 16);
 
-    if (steps > 0) issue(0);
-    for (int kt = 0; kt < steps; ++kt) {
+    // A K step is four phases of FM / 2 x FN products: (first half of the reduction, upper rows), (first, lower), (second,
+    // upper), (second, lower).  The fragments of a phase are read during the one before it.  Before the last phase of a step the
+    // next stage is published: by then every wave holds all it needs of this one, whose memory takes the stage after next.
+    s16x8_t fa[2][FM / 2], fb[2][FN];
+    int sa[FM / 2], sb[FN / 2];  // scale bytes of two fragments each: (first half, second half) of both
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    const char* ts0 = lds_s + ((threadIdx.x >> 4) & 3) * 2 + (threadIdx.x & 15) * 16;
+    auto read_scale = [&](auto i, int kt) {  // pair i of the wave's rows, then of its columns
+        const char* ts = ts0 + ((kt >> 1) & 1) * (BM + BN) * 16 + (kt & 1) * 8;
+        const uint16_t* r = (const uint16_t*)(i.value < FM / 2 ? ts + (wm * FM + 2 * i.value) * 256 : ts + BM * 16 + (wn * FN + 2 * i.value - FM) * 256);
+        return __builtin_bit_cast(int, u16x2_t{r[0], r[128]});
+    };
+    // WITH: the last phase of a step also asks for the stage after next.
+    auto phase = [&](auto p, auto with, int kt) {
+        constexpr int P = p.value, H = P >> 1, U = P & 1, NP = (P + 1) & 3, NH = NP >> 1, NU = NP & 1, NL = NLA + NLB;
+        constexpr int READS = FM / 2 + (NU == 0 ? FN : 0), PROD = FM / 2 * FN;
+        const int ns = (P == 3 ? kt + 1 : kt) & 1;
+        const char* ta = lds_a + ns * BM * 128;
+        const char* tb = lds_b + ns * BN * 128;
+        int na[FM / 2], nb[FN / 2];
+        if constexpr (P == 3) {
+            wait_loads<0>();
+            block_barrier();
+            if constexpr (with.value) begin(kt + 2);
+        }
+        repeat<PROD>([&](auto i) {
+            constexpr int I = i.value, m = I / FN, n = I % FN, M = U * FM / 2 + m;
+            acc[M][n] = multiply<FMT, H + 2 * (n & 1), H + 2 * (M & 1)>(fb[H][n], fa[U][m], acc[M][n], sb[n / 2], sa[M / 2]);
+            // the next phase's fragments in the first places, the columns' before the rows' as the products need them
+            if constexpr (I < READS) {
+                if constexpr (I < READS - FM / 2) fb[NH][I] = rb.template get<I, NH>(tb);
+                else fa[NU][I - (READS - FM / 2)] = ra.template get<NU * FM / 2 + I - (READS - FM / 2), NH>(ta);
+            }
+            if constexpr (P == 3 && with.value) repeat<(I + 1) * NL / PROD - I * NL / PROD>([&](auto j) { load(kt + 2, Int<I * NL / PROD + j.value>{}); });
+            if constexpr (P == 3 && MX) {
+                constexpr int NSC = (FM + FN) / 2, s0 = I * NSC / PROD, s1 = (I + 1) * NSC / PROD;
+                if constexpr (s1 > s0) {
+                    if constexpr (s0 < FM / 2) na[s0] = read_scale(Int<s0>{}, kt + 1);
+                    else nb[s0 - FM / 2] = read_scale(Int<s0>{}, kt + 1);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (P == 3) {
+            if constexpr (with.value) {
+                la.next();
+                lb.next();
+            }
+            if constexpr (MX) {
+                repeat<FM / 2>([&](auto f) { sa[f.value] = na[f.value]; });
+                repeat<FN / 2>([&](auto f) { sb[f.value] = nb[f.value]; });
+            }
+        }
+    };
+    auto step = [&](auto with, int kt) {
+        phase(Int<0>{}, with, kt);
+        phase(Int<1>{}, with, kt);
+        phase(Int<2>{}, with, kt);
+        phase(Int<3>{}, with, kt);
+    };
+    if (steps > 0) {
+        if (steps == 1) cut();
+        issue(0);
+        if (steps == 2) cut();
         wait_loads<0>();
         block_barrier();
-        if (kt + 1 < steps) issue(kt + 1);
-        const char* ta = lds_a + (kt & 1) * BM * 128;
-        const char* tb = lds_b + (kt & 1) * BN * 128;
-        int sa[FM], sb[FN];
+        if (steps > 1) issue(1);
         if constexpr (MX) {
-            const char* ts = lds_s + ((kt >> 1) & 1) * (BM + BN) * 16 + (kt & 1) * 8 + ((threadIdx.x >> 4) & 3) * 2 + (threadIdx.x & 15) * 16;
-            repeat<FM>([&](auto f) { sa[f.value] = *(const uint16_t*)(ts + (wm * FM + f.value) * 256); });
-            repeat<FN>([&](auto f) { sb[f.value] = *(const uint16_t*)(ts + BM * 16 + (wn * FN + f.value) * 256); });
-        } else {
-            repeat<FM>([&](auto f) { sa[f.value] = 0; });
-            repeat<FN>([&](auto f) { sb[f.value] = 0; });
+            repeat<FM / 2>([&](auto f) { sa[f.value] = read_scale(f, 0); });
+            repeat<FN / 2>([&](auto f) { sb[f.value] = read_scale(Int<FM / 2 + f.value>{}, 0); });
         }
-        repeat<2>([&](auto h) {
-            s16x8_t fa[FM], fb[FN];
-            repeat<FM>([&](auto f) { fa[f.value] = ra.template get<f.value, h.value>(ta); });
-            repeat<FN>([&](auto f) { fb[f.value] = rb.template get<f.value, h.value>(tb); });
-            repeat<FM>([&](auto m) {
-                repeat<FN>([&](auto n) {
-                    acc[m.value][n.value] = multiply<FMT>(fb[n.value], fa[m.value], acc[m.value][n.value], sb[n.value], sa[m.value], h);
-                });
-            });
-        });
+        repeat<FN>([&](auto f) { fb[0][f.value] = rb.template get<f.value, 0>(lds_b); });
+        repeat<FM / 2>([&](auto f) { fa[0][f.value] = ra.template get<f.value, 0>(lds_a); });
+        int kt = 0;
+        for (; kt + 2 < steps; ++kt) {
+            if (kt + 3 == steps) cut();
+            step(Int<1>{}, kt);
+        }
+        for (; kt < steps; ++kt) step(Int<0>{}, kt);
     }
 
     const int m = t.m0 + wm * FM * 16, n = t.n0 + wn * FN * 16;
