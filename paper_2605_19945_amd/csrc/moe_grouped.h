@@ -41,12 +41,12 @@ constexpr uint32_t OUT_OF_RANGE = 0x80000000u;  // an offset behind the end of e
 
 static __device__ inline uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(const lds_char*)p; }
 
-static __device__ inline u32x4_t make_desc(const char* base, uint32_t bytes) {
+static __device__ inline u32x4_t make_desc(const char* base, int bytes) {
     const uint64_t p = (uint64_t)base;
     u32x4_t d;
     d[0] = __builtin_amdgcn_readfirstlane((uint32_t)p);
     d[1] = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32) & 0xffffu);
-    d[2] = __builtin_amdgcn_readfirstlane(bytes);
+    d[2] = __builtin_amdgcn_readfirstlane(max(bytes, 0));
     d[3] = 0x00027000u;
     return d;
 }
@@ -80,18 +80,61 @@ static __device__ inline void place_in_band(int t, int mt, int nt, int* m, int* 
     *m = 8 * band + r - *n * h;
 }
 
-// The tile of workgroup `bid` of a product over ragged rows: each XCD (bid % 8) takes one stretch of the list of all
-// tiles, which follows from the offsets alone; every wave finds its entry by itself (4 experts a lane).  False: no tile.
-template <int BM> static __device__ inline bool find_row_tile(const GroupedArgs& g, int nt, int bid, int bn, GroupedTile* out) {
-    const int lane = threadIdx.x & 63;
-    int cnt[4], sum = 0;
+// The list of all tiles, expert by expert, follows from the offsets alone; each XCD (workgroup number % 8) takes one stretch of
+// it, and its workgroups go through that side by side.  Every workgroup builds what it needs of the list in LDS.
+struct TileList {
+    int lo[256], n[256];  // first row and rows of every expert
+    int first[257];       // row tiles before the expert (products over ragged rows)
+    int begin, end;       // this XCD's stretch
+    int height;           // rows of a tile (products over ragged rows)
+};
+
+// Cost of a tile of a weight gradient beside its K steps, in K steps: its stores.
+constexpr int TILE_COST = 6;
+// Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside.
+constexpr int QUARTER_COST = 5, STEP_COST = 7;
+
+// By one wave.  WEIGHTS: every expert has `per` tiles, which cost what it has rows, and the stretches are of equal cost; otherwise a tile
+// costs the same everywhere.
+template <bool WEIGHTS, int BM> static __device__ inline void make_list(const GroupedArgs& g, int per, TileList* l) {
+    const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
+    int rows[4], c[4], sum = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int e = 4 * lane + j;
-        int lo = 0, n = 0;
-        if (e < g.E) expert_rows(g.offsets, e, g.rows_cap, &lo, &n);
-        cnt[j] = (n + BM - 1) / BM;
-        sum += cnt[j];
+        int lo = 0;
+        rows[j] = 0;
+        if (e < g.E) expert_rows(g.offsets, e, g.rows_cap, &lo, &rows[j]);
+        l->lo[e] = lo;
+        l->n[e] = rows[j];
+    }
+    int height = BM;
+    if (!WEIGHTS) {
+        // Quarters of BM in the height that leaves the least to the busiest workgroup.  A step of a tile takes QUARTER_COST for every
+        // quarter and STEP_COST beside.
+        int best = 0x7fffffff;
+#pragma unroll
+        for (int quarters = 4; quarters > 0; --quarters) {
+            const int h = BM / 4 * quarters;
+            int tiles = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tiles += (rows[j] + h - 1) / h;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d);
+            const int64_t rounds = ((int64_t)tiles * per + gridDim.x - 1) / gridDim.x;
+            const int cost = (int)min(rounds * (STEP_COST + QUARTER_COST * quarters), (int64_t)0x7ffffffe);
+            if (cost < best) {
+                best = cost;
+                height = h;
+            }
+        }
+        height = __builtin_amdgcn_readfirstlane(height);
+        if (lane == 0) l->height = height;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        c[j] = WEIGHTS ? (4 * lane + j < g.E ? (rows[j] + 63) / 64 + TILE_COST : 0) : (rows[j] + height - 1) / height;
+        sum += c[j];
     }
     int incl = sum;
 #pragma unroll
@@ -99,55 +142,62 @@ template <int BM> static __device__ inline bool find_row_tile(const GroupedArgs&
         const int o = __shfl_up(incl, d);
         if (lane >= d) incl += o;
     }
-    const int mts = __builtin_amdgcn_readlane(incl, 63);
-    const int64_t total = (int64_t)mts * nt;
-    const int xcd = bid & 7, idx = bid >> 3;
-    const int64_t base = total >> 3, rem = total & 7;
-    if (idx >= base + (xcd < rem ? 1 : 0)) return false;
-    const int64_t t = xcd * base + (xcd < rem ? xcd : rem) + idx;
-    const int tm = (int)(t / nt);  // row tiles of earlier experts are all of theirs times nt
-    const uint64_t past = __ballot(incl > tm);
-    if (past == 0) return false;
-    const int src = __builtin_ctzll(past);
-    int before = __builtin_amdgcn_readlane(incl - sum, src), e = 4 * src, mt = 0;
+    const int all = __builtin_amdgcn_readlane(incl, 63);
+    int before = incl - sum;
+    const int64_t total = (int64_t)all * per;
+    // the first tile at or behind position `at` of the total cost (of expert e: at = per * before + tile * c)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = __builtin_amdgcn_readlane(cnt[j], src);
-        if (mt == 0) {
-            if (tm < before + c) {
-                mt = c;
-                e = 4 * src + j;
-            } else {
-                before += c;
+    for (int k = 0; k < 2; ++k) {
+        const int64_t at = total * (xcd + k) / 8;
+        if (!WEIGHTS) {
+            if (lane == 0) (k ? l->end : l->begin) = (int)at;
+        } else if (xcd + k == 8) {
+            if (lane == 0) l->end = g.E * per;
+        } else {
+            int b = before;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t from = (int64_t)b * per, to = from + (int64_t)c[j] * per;
+                if (c[j] > 0 && at >= from && at < to) (k ? l->end : l->begin) = (4 * lane + j) * per + (int)((at - from + c[j] - 1) / c[j]);
+                b += c[j];
             }
         }
     }
-    int m, n;
-    place_in_band((int)(t - (int64_t)before * nt), mt, nt, &m, &n);
-    out->e = e;
-    expert_rows(g.offsets, e, g.rows_cap, &out->lo, &out->n);
-    out->lo = __builtin_amdgcn_readfirstlane(out->lo);
-    out->n = __builtin_amdgcn_readfirstlane(out->n);
-    out->m0 = m * BM;
-    out->n0 = n * bn;
-    return true;
+    if (!WEIGHTS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            l->first[4 * lane + j] = before;
+            before += c[j];
+        }
+        if (lane == 63) l->first[256] = before;
+    }
 }
 
-// The tile of workgroup `bid` of a weight gradient: every expert has mt x nt tiles, and each XCD takes an eighth of
-// every expert's, because an expert's tiles cost what it has rows.
-static __device__ inline bool find_weight_tile(const GroupedArgs& g, int mt, int nt, int bid, int bm, int bn, GroupedTile* out) {
-    const int per = mt * nt, px = (per + 7) / 8, xcd = bid & 7, idx = bid >> 3;
-    const int e = idx / px, t = xcd * px + idx % px;
-    if (e >= g.E || t >= per) return false;
-    int m, n;
-    place_in_band(t, mt, nt, &m, &n);
-    out->e = e;
-    expert_rows(g.offsets, e, g.rows_cap, &out->lo, &out->n);
-    out->lo = __builtin_amdgcn_readfirstlane(out->lo);
-    out->n = __builtin_amdgcn_readfirstlane(out->n);
-    out->m0 = m * bm;
-    out->n0 = n * bn;
-    return true;
+template <bool WEIGHTS, int BN>
+static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileList& l, int height, int mt, int nt, int t) {
+    GroupedTile out;
+    int e, m, n, r;
+    if (WEIGHTS) {
+        e = __builtin_amdgcn_readfirstlane(t / (mt * nt));
+        r = t - e * mt * nt;
+    } else {
+        const int tm = __builtin_amdgcn_readfirstlane(t / nt);  // an expert's tiles are its row tiles times nt
+        const uint64_t past = __ballot(l.first[4 * (threadIdx.x & 63) + 4] > tm);
+        e = 4 * __builtin_ctzll(past);
+        e += (l.first[e + 1] <= tm) + (l.first[e + 2] <= tm) + (l.first[e + 3] <= tm);
+        e = __builtin_amdgcn_readfirstlane(e);
+        r = t - l.first[e] * nt;
+        mt = l.first[e + 1] - l.first[e];
+    }
+    r = __builtin_amdgcn_readfirstlane(r);
+    mt = __builtin_amdgcn_readfirstlane(mt);
+    place_in_band(r, mt, nt, &m, &n);
+    out.e = e;
+    out.lo = __builtin_amdgcn_readfirstlane(l.lo[e]);
+    out.n = __builtin_amdgcn_readfirstlane(l.n[e]);
+    out.m0 = __builtin_amdgcn_readfirstlane(m) * height;
+    out.n0 = __builtin_amdgcn_readfirstlane(n) * BN;
+    return out;
 }
 
 // 16-byte chunk c of a row lies at chunk c ^ swizzle(row) of its LDS row, so that the lanes that read together fall on
@@ -159,12 +209,18 @@ static __device__ inline int swizzle_k(int row) {
     return (t & 1) | (t >> 1 & 2) | ((t ^ t << 1) & 4);
 }
 
+// Rows of 64 columns lie two to a turn of the banks.
+template <int B> static __device__ inline int swizzle_mn(int row) {
+    return B == 64 ? (row & 2) | (row >> 1 & 4) : 2 * ((row & 3) + (row >> 1 & 4));
+}
+
 // One operand's share of a wave: NL loads of 1 KiB a K step.
 template <int LAY, int B, int NL> struct Loader {
     static constexpr int ROW = LAY == LAY_K ? 128 : 2 * B;  // bytes of a row in LDS
     const char* base;
     int64_t step;        // bytes to the next K step
-    uint32_t ld, width;  // bytes between rows; bytes of the last row that belong to the operand
+    uint32_t ld;         // bytes between rows
+    int width;           // bytes of the last row that belong to the operand
     int rows;            // LAY_K: valid rows of the tile; LAY_MN: rows (k) left from this step on
     uint32_t offset[NL];
 
@@ -181,7 +237,7 @@ template <int LAY, int B, int NL> struct Loader {
         } else {
             step = 64 * ld_;
             rows = k;
-            width = 2 * min(valid, B);
+            width = 2 * max(min(valid, B), 0);  // (none in the lower half of a low tile)
         }
 #pragma unroll
         for (int j = 0; j < NL; ++j) {
@@ -189,14 +245,15 @@ template <int LAY, int B, int NL> struct Loader {
             const int row = p / ROW, chunk = (p % ROW) / 16;
             const int c = chunk ^ swizzle(row);
             offset[j] = row * ld + c * 16;
-            if (LAY == LAY_MN && c * 16 >= (int)width) offset[j] = OUT_OF_RANGE;
+            if (LAY == LAY_MN && c * 16 >= width) offset[j] = OUT_OF_RANGE;
         }
     }
-    static __device__ inline int swizzle(int row) { return LAY == LAY_K ? swizzle_k(row) : 2 * ((row & 3) + 4 * ((row >> 3) & 1)); }
+    static __device__ inline int swizzle(int row) { return LAY == LAY_K ? swizzle_k(row) : swizzle_mn<B>(row); }
     __device__ inline u32x4_t desc() const {
-        if (LAY == LAY_K) return make_desc(base, rows > 0 ? (rows - 1) * ld + width : 0);
-        return make_desc(base, rows > 0 ? (min(rows, 64) - 1) * ld + width : 0);
+        if (LAY == LAY_K) return make_desc(base, rows > 0 && width > 0 ? (rows - 1) * (int)ld + width : 0);
+        return make_desc(base, rows > 0 && width > 0 ? (min(rows, 64) - 1) * (int)ld + width : 0);
     }
+    __device__ inline void stop() { rows = 0; }  // later stages read zeros
     __device__ inline void issue(const u32x4_t& d, uint32_t to, int j, int wave) const { load_to_lds(to + (wave * NL + j) * 1024, offset[j], d); }
     __device__ inline void next() {
         base += step;
@@ -210,7 +267,7 @@ template <int LAY, int B, int NL> struct Loader {
             for (int j = 0; j < NL; ++j) {
                 const int p = (wave * NL + j) * 1024 + (threadIdx.x & 63) * 16;
                 const int c = ((p % ROW) / 16) ^ swizzle(p / ROW);
-                if (c * 16 >= (int)width) offset[j] = OUT_OF_RANGE;
+                if (c * 16 >= width) offset[j] = OUT_OF_RANGE;
             }
         }
     }
@@ -234,7 +291,7 @@ template <int FMT, int LAY, int B> struct Reader {
         } else {
             cl = (8 * q + (i >> 2)) * (2 * B) + (i & 1) * 8;
             ch = first / 8 + ((i & 3) >> 1);
-            sw = 2 * ((i >> 2) + 4 * (q & 1));
+            sw = swizzle_mn<B>(8 * q + (i >> 2));
         }
     }
     template <int F, int H> __device__ inline s16x8_t get(const char* tile) const {
@@ -274,11 +331,11 @@ template <int FMT, int SB, int SA> static __device__ inline f32x4_t multiply(con
 // Stores a wave's FM x FN fragments.  The weights are the first operand of the matrix instruction, so a lane has 4
 // neighbouring columns of one row; two fragments change halves between neighbouring rows of 16 lanes, and every lane
 // then stores 8 bf16 columns (16 bytes) of one row.
-template <int OUT, int FM, int FN>
+template <int OUT, int FM, int FN, int FAR>
 static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], void* c, int64_t ldc, int rows, int cols) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     repeat<FM>([&](auto mf) {
-        const int row = mf.value * 16 + i;
+        const int row = mf.value / (FM / 2) * FAR + mf.value % (FM / 2) * 16 + i;
         if constexpr (OUT == OUT_BF16) {
             repeat<FN / 2>([&](auto p) {
                 const f32x4_t u = acc[mf.value][2 * p.value], v = acc[mf.value][2 * p.value + 1];
@@ -304,159 +361,216 @@ static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], void* c, 
     });
 }
 
+// Persistent: a workgroup goes through its tiles as one stream of K steps.  The stages of the next tile's first two steps are
+// asked for during the last two of this one, so only the first tile waits for memory, and a tile's stores leave under the next one's
+// products.
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
-    constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, NLA = BM / 8 / NW, NLB = BN / 8 / NW;
+    constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;
     constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4;
-    constexpr int NS = (BM + BN) / 64 / NW;  // loads of scales a wave, every second K step
+    constexpr int HALF = BM / 2, GROUP = HALF / WM;  // a wave has GROUP rows of each half of the tile: rows that are missing spare every wave alike
+    constexpr int NS = (BM + BN) / 64 / NW;          // loads of scales a wave, every second K step
     static_assert(!MX || NS * 64 * NW == BM + BN, "scale loads");
-    __shared__ __attribute__((aligned(1024))) char lds_a[2 * BM * 128];
-    __shared__ __attribute__((aligned(1024))) char lds_b[2 * BN * 128];
+    __shared__ __attribute__((aligned(1024))) char lds_a[2][2][HALF * 128];  // [half of the rows][slot]
+    __shared__ __attribute__((aligned(1024))) char lds_b[2][BN * 128];
     __shared__ __attribute__((aligned(1024))) char lds_s[MX ? 2 * (BM + BN) * 16 : 16];
+    __shared__ TileList list;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    GroupedTile t;
-    if (WEIGHTS ? !find_weight_tile(g, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, blockIdx.x, BM, BN, &t)
-                : !find_row_tile<BM>(g, (g.N + BN - 1) / BN, blockIdx.x, BN, &t))
-        return;
-    const int mrows = WEIGHTS ? g.M - t.m0 : t.n - t.m0, ncols = g.N - t.n0;
-    if (OUT == OUT_F32_ADD && t.n == 0) return;
+    const int mt = (g.M + BM - 1) / BM, nt = (g.N + BN - 1) / BN;
+    if (wave == 0) make_list<WEIGHTS, BM>(g, WEIGHTS ? mt * nt : nt, &list);
+    block_barrier();
+    const int height = WEIGHTS ? BM : __builtin_amdgcn_readfirstlane(list.height);
+    int at = __builtin_amdgcn_readfirstlane(list.begin) + (blockIdx.x >> 3);
+    const int last = __builtin_amdgcn_readfirstlane(list.end);
+    if (at >= last) return;
 
-    Loader<LA, BM, NLA> la;
+    // ---- the stages: a cursor that runs two steps ahead of the products
+    Loader<LA, HALF, NLA> la[2];
     Loader<LB, BN, NLB> lb;
-    const char* wb = g.b + t.e * g.b_expert;
-    const int red = LA == LAY_K ? g.kbytes / (MX ? 1 : 2) : t.n;  // reduction: values (bytes of 4-bit values)
-    if constexpr (LA == LAY_K) la.init(g.a + (int64_t)(t.lo + t.m0) * g.lda, g.lda, mrows, g.kbytes, wave);
-    else la.init(g.a + (int64_t)t.lo * g.lda + (int64_t)t.m0 * 2, g.lda, mrows, red, wave);
-    if constexpr (LB == LAY_K) lb.init(wb + (int64_t)t.n0 * g.ldb, g.ldb, ncols, g.kbytes, wave);
-    else lb.init(WEIGHTS ? g.b + (int64_t)t.lo * g.ldb + (int64_t)t.n0 * 2 : wb + (int64_t)t.n0 * 2, g.ldb, ncols, red, wave);
-    const int steps = (red + (MX ? 127 : 63)) / (MX ? 128 : 64);
-
-    // The loads of a stage, one at a time: begin(kt), load(kt, 0 .. NLA + NLB - 1), end().
-    u32x4_t da, db;
-    auto begin = [&](int kt) {
-        da = la.desc();
-        db = lb.desc();
-        if constexpr (MX) {
-            if ((kt & 1) == 0) repeat<NS>([&](auto j) {
-                const int part = wave * NS + j.value;  // 64 rows of a, or of b behind them
-                const bool of_b = part * 64 >= BM;
-                const int row = part * 64 - (of_b ? BM : 0), have = min((of_b ? ncols : mrows) - row, 64);
-                const uint8_t* p = of_b ? g.sb + ((int64_t)t.e * g.N + t.n0 + row) * g.scale_ld : g.sa + (int64_t)(t.lo + t.m0 + row) * g.scale_ld;
-                const u32x4_t d = make_desc((const char*)p + kt * 8, have > 0 ? (have - 1) * g.scale_ld + 16 : 0);
-                load_to_lds(lds_addr(lds_s) + ((kt >> 1) & 1) * (BM + BN) * 16 + part * 1024, (threadIdx.x & 63) * g.scale_ld, d);
+    GroupedTile lt;
+    int ls = 0, lsteps = 0, lpair = 0;  // its tile, step in it, steps of it; which half of lds_s the last scales went to
+    auto steps_of = [&](const GroupedTile& t) {  // at least two: a step that is not there reads zeros
+        const int red = LA == LAY_K ? g.kbytes / (MX ? 1 : 2) : t.n;
+        return max(2, (red + (MX ? 127 : 63)) / (MX ? 128 : 64));
+    };
+    auto start = [&](const GroupedTile& t) {
+        const int mrows = WEIGHTS ? g.M - t.m0 : min(t.n - t.m0, height), ncols = g.N - t.n0;
+        const char* wb = g.b + t.e * g.b_expert;
+        repeat<2>([&](auto u) {
+            constexpr int R = u.value * HALF;
+            if constexpr (LA == LAY_K) la[u.value].init(g.a + (int64_t)(t.lo + t.m0 + R) * g.lda, g.lda, mrows - R, g.kbytes, wave);
+            else la[u.value].init(g.a + (int64_t)t.lo * g.lda + (int64_t)(t.m0 + R) * 2, g.lda, mrows - R, t.n, wave);
+        });
+        if constexpr (LB == LAY_K) lb.init(wb + (int64_t)t.n0 * g.ldb, g.ldb, ncols, g.kbytes, wave);
+        else lb.init(WEIGHTS ? g.b + (int64_t)t.lo * g.ldb + (int64_t)t.n0 * 2 : wb + (int64_t)t.n0 * 2, g.ldb, ncols, WEIGHTS ? t.n : g.kbytes / 2, wave);
+        lt = t;
+        ls = 0;
+        lsteps = steps_of(t);
+    };
+    // The loads of a stage in two parts, 0: upper rows, columns and scales; 1: lower rows.  begin(part), load_scales(), load(part, slot, 0 ..),
+    // end(part).
+    u32x4_t da[2], db;
+    auto begin = [&](auto part) {
+        if (LA == LAY_K) la[part.value].cut(wave);
+        da[part.value] = la[part.value].desc();
+        if constexpr (part.value == 0) {
+            if (LB == LAY_K) lb.cut(wave);
+            db = lb.desc();
+        }
+    };
+    auto load_scales = [&]() {
+        if ((ls & 1) == 0) {
+            lpair ^= 1;
+            const int mrows = lt.n - lt.m0, ncols = g.N - lt.n0;
+            repeat<NS>([&](auto j) {
+                const int rows64 = wave * NS + j.value;  // 64 rows of a, or of b behind them
+                const bool of_b = rows64 * 64 >= BM;
+                const int row = rows64 * 64 - (of_b ? BM : 0), have = min((of_b ? ncols : mrows) - row, 64);
+                const uint8_t* p = of_b ? g.sb + ((int64_t)lt.e * g.N + lt.n0 + row) * g.scale_ld : g.sa + (int64_t)(lt.lo + lt.m0 + row) * g.scale_ld;
+                const u32x4_t d = make_desc((const char*)p + ls * 8, have > 0 && ls * 8 < g.scale_ld ? (have - 1) * g.scale_ld + 16 : 0);
+                load_to_lds(lds_addr(lds_s) + lpair * (BM + BN) * 16 + rows64 * 1024, (threadIdx.x & 63) * g.scale_ld, d);
             });
         }
     };
-    auto load = [&](int kt, auto j) {
-        if constexpr (j.value < NLA) la.issue(da, lds_addr(lds_a) + (kt & 1) * BM * 128, j.value, wave);
-        else lb.issue(db, lds_addr(lds_b) + (kt & 1) * BN * 128, j.value - NLA, wave);
+    auto load = [&](auto part, int slot, auto j) {
+        if constexpr (j.value < NLA) la[part.value].issue(da[part.value], lds_addr(lds_a[part.value][0]) + slot * HALF * 128, j.value, wave);
+        else lb.issue(db, lds_addr(lds_b[0]) + slot * BN * 128, j.value - NLA, wave);
     };
-    auto cut = [&]() {
-        la.cut(wave);
-        lb.cut(wave);
-    };
-    auto issue = [&](int kt) {
-        begin(kt);
-        repeat<NLA + NLB>([&](auto j) { load(kt, j); });
-        la.next();
-        lb.next();
+    auto end = [&](auto part) {
+        la[part.value].next();
+        if constexpr (part.value == 0) lb.next();
+        else ++ls;
     };
 
-    f32x4_t acc[FM][FN];
+    f32x4_t acc[2 * FH][FN];
+    auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+        for (int i = 0; i < 2 * FH; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    };
     const int wm = wave / WN, wn = wave % WN;
-    Reader<FMT, LA, BM> ra;
+    Reader<FMT, LA, HALF> ra;
     Reader<FMT, LB, BN> rb;
-    ra.init(wm * FM * 16);
+    ra.init(wm * GROUP);
     rb.init(wn * FN * 16);
 
-    // A K step is four phases of FM / 2 x FN products: (first half of the reduction, upper rows), (first, lower), (second,
-    // upper), (second, lower).  The fragments of a phase are read during the one before it.  Before the last phase of a step the
-    // next stage is published: by then every wave holds all it needs of this one, whose memory takes the stage after next.
-    s16x8_t fa[2][FM / 2], fb[2][FN];
-    int sa[FM / 2], sb[FN / 2];  // scale bytes of two fragments each: (first half, second half) of both
+    // A K step is four phases of FH x FN products: (upper rows, first half of the reduction), (upper, second), (lower, first),
+    // (lower, second).  The fragments of a phase are read during the one before it, those of the columns once for both halves of the
+    // rows.  So the upper rows and the columns of a stage are free before phase 1 and the lower rows before phase 3; the stage after
+    // next is asked for there (three loads a wave and phase, what the compute unit's one memory pipe takes meanwhile) and has a step and
+    // a quarter to arrive.
+    s16x8_t fa[2][FH], fb[2][FN];
+    int sa[FH], sb[FN / 2];  // scale bytes of two fragments each: (first half, second half) of both
+    int slot = 0, pair = 1;  // of the step at hand: its slot in lds_a and lds_b, its half of lds_s
     typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
-    const char* ts0 = lds_s + ((threadIdx.x >> 4) & 3) * 2 + (threadIdx.x & 15) * 16;
-    auto read_scale = [&](auto i, int kt) {  // pair i of the wave's rows, then of its columns
-        const char* ts = ts0 + ((kt >> 1) & 1) * (BM + BN) * 16 + (kt & 1) * 8;
-        const uint16_t* r = (const uint16_t*)(i.value < FM / 2 ? ts + (wm * FM + 2 * i.value) * 256 : ts + BM * 16 + (wn * FN + 2 * i.value - FM) * 256);
+    auto read_scale = [&](auto i, int pr, int odd) {  // pair i of the wave's rows, then of its columns
+        constexpr int I = i.value, ROW = 2 * I / FH * HALF + 2 * I % FH * 16;
+        const char* ts = lds_s + pr * (BM + BN) * 16 + odd * 8 + ((threadIdx.x >> 4) & 3) * 2 + (threadIdx.x & 15) * 16;
+        const uint16_t* r = (const uint16_t*)(I < FH ? ts + (wm * GROUP + ROW) * 16 : ts + BM * 16 + (wn * FN + 2 * (I - FH)) * 256);
         return __builtin_bit_cast(int, u16x2_t{r[0], r[128]});
     };
-    // WITH: the last phase of a step also asks for the stage after next.
-    auto phase = [&](auto p, auto with, int kt) {
-        constexpr int P = p.value, H = P >> 1, U = P & 1, NP = (P + 1) & 3, NH = NP >> 1, NU = NP & 1, NL = NLA + NLB;
-        constexpr int READS = FM / 2 + (NU == 0 ? FN : 0), PROD = FM / 2 * FN;
-        const int ns = (P == 3 ? kt + 1 : kt) & 1;
-        const char* ta = lds_a + ns * BM * 128;
-        const char* tb = lds_b + ns * BN * 128;
-        int na[FM / 2], nb[FN / 2];
-        if constexpr (P == 3) {
-            wait_loads<0>();
+    int live = 2;  // halves in which this wave has rows
+    auto phase = [&](auto p, int odd) {  // odd: of the next step, in its tile
+        constexpr int P = p.value, U = P >> 1, H = P & 1, NP = (P + 1) & 3, NU = NP >> 1, NH = NP & 1;
+        constexpr bool NEWB = NP < 2;  // the next phase's columns are read as well
+        constexpr int READS = FH + (NEWB ? FN : 0), PROD = FH * FN, ALL = NLA + NLB;
+        constexpr int PART = P == 3, FIRST = P == 2 ? ALL / 2 : 0, NL = P == 1 ? ALL / 2 : P == 2 ? ALL - ALL / 2 : P == 3 ? NLA : 0;
+        const int from = P == 3 ? slot ^ 1 : slot;
+        const char* ta = lds_a[NU][0] + from * HALF * 128;
+        const char* tb = lds_b[0] + from * BN * 128;
+        int na[FH], nb[FN / 2];
+        if constexpr (H == 1) {
+            wait_loads<2 * NLA + NLB>();
             block_barrier();
-            if constexpr (with.value) begin(kt + 2);
+            if constexpr (MX && P == 1) load_scales();
+            if (MX && P == 3 && !odd) pair ^= 1;
         }
-        repeat<PROD>([&](auto i) {
-            constexpr int I = i.value, m = I / FN, n = I % FN, M = U * FM / 2 + m;
-            acc[M][n] = multiply<FMT, H + 2 * (n & 1), H + 2 * (M & 1)>(fb[H][n], fa[U][m], acc[M][n], sb[n / 2], sa[M / 2]);
-            // the next phase's fragments in the first places, the columns' before the rows' as the products need them
+        // what goes on beside product I: the next phase's fragments in the first places, the columns' before the rows' as the
+        // products need them; the loads of a stage; the next step's scales
+        auto beside = [&](auto i) {
+            constexpr int I = i.value;
             if constexpr (I < READS) {
-                if constexpr (I < READS - FM / 2) fb[NH][I] = rb.template get<I, NH>(tb);
-                else fa[NU][I - (READS - FM / 2)] = ra.template get<NU * FM / 2 + I - (READS - FM / 2), NH>(ta);
+                if constexpr (I < READS - FH) fb[NH][I] = rb.template get<I, NH>(tb);
+                else fa[NH][I - (READS - FH)] = ra.template get<I - (READS - FH), NH>(ta);
             }
-            if constexpr (P == 3 && with.value) repeat<(I + 1) * NL / PROD - I * NL / PROD>([&](auto j) { load(kt + 2, Int<I * NL / PROD + j.value>{}); });
+            if constexpr (NL > 0) repeat<(I + 1) * NL / PROD - I * NL / PROD>([&](auto j) { load(Int<PART>{}, slot, Int<FIRST + I * NL / PROD + j.value>{}); });
+            if constexpr (H == 0 && I == PROD / 2) begin(Int<U>{});  // what the next phase asks for
             if constexpr (P == 3 && MX) {
-                constexpr int NSC = (FM + FN) / 2, s0 = I * NSC / PROD, s1 = (I + 1) * NSC / PROD;
+                constexpr int NSC = FH + FN / 2, s0 = I * NSC / PROD, s1 = (I + 1) * NSC / PROD;
                 if constexpr (s1 > s0) {
-                    if constexpr (s0 < FM / 2) na[s0] = read_scale(Int<s0>{}, kt + 1);
-                    else nb[s0 - FM / 2] = read_scale(Int<s0>{}, kt + 1);
+                    if constexpr (s0 < FH) na[s0] = read_scale(Int<s0>{}, pair, odd);
+                    else nb[s0 - FH] = read_scale(Int<s0>{}, pair, odd);
                 }
             }
-            __builtin_amdgcn_sched_barrier(0);
-        });
+        };
+        if (live > U) {
+            repeat<PROD>([&](auto i) {
+                constexpr int m = i.value / FN, n = i.value % FN, M = U * FH + m;
+                acc[M][n] = multiply<FMT, H + 2 * (n & 1), H + 2 * (M & 1)>(fb[H][n], fa[H][m], acc[M][n], sb[n / 2], sa[M / 2]);
+                beside(i);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        } else {
+            repeat<PROD>(beside);
+        }
+        if constexpr (P >= 2) end(Int<P - 2>{});
         if constexpr (P == 3) {
-            if constexpr (with.value) {
-                la.next();
-                lb.next();
-            }
             if constexpr (MX) {
-                repeat<FM / 2>([&](auto f) { sa[f.value] = na[f.value]; });
+                repeat<FH>([&](auto f) { sa[f.value] = na[f.value]; });
                 repeat<FN / 2>([&](auto f) { sb[f.value] = nb[f.value]; });
             }
+            slot ^= 1;
         }
     };
-    auto step = [&](auto with, int kt) {
-        phase(Int<0>{}, with, kt);
-        phase(Int<1>{}, with, kt);
-        phase(Int<2>{}, with, kt);
-        phase(Int<3>{}, with, kt);
-    };
-    if (steps > 0) {
-        if (steps == 1) cut();
-        issue(0);
-        if (steps == 2) cut();
-        wait_loads<0>();
-        block_barrier();
-        if (steps > 1) issue(1);
-        if constexpr (MX) {
-            repeat<FM / 2>([&](auto f) { sa[f.value] = read_scale(f, 0); });
-            repeat<FN / 2>([&](auto f) { sb[f.value] = read_scale(Int<FM / 2 + f.value>{}, 0); });
-        }
-        repeat<FN>([&](auto f) { fb[0][f.value] = rb.template get<f.value, 0>(lds_b); });
-        repeat<FM / 2>([&](auto f) { fa[0][f.value] = ra.template get<f.value, 0>(lds_a); });
-        int kt = 0;
-        for (; kt + 2 < steps; ++kt) {
-            if (kt + 3 == steps) cut();
-            step(Int<1>{}, kt);
-        }
-        for (; kt < steps; ++kt) step(Int<0>{}, kt);
-    }
 
-    const int m = t.m0 + wm * FM * 16, n = t.n0 + wn * FN * 16;
-    const int64_t row = WEIGHTS ? (int64_t)t.e * g.M + m : (int64_t)t.lo + m;
-    const int esize = OUT == OUT_BF16 ? 2 : 4;
-    store_tile<OUT, FM, FN>(acc, (char*)g.c + (row * g.ldc + n) * esize, g.ldc, (WEIGHTS ? g.M : t.n) - m, g.N - n);
+    start(find_tile<WEIGHTS, BN>(g, list, WEIGHTS ? BM : height, mt, nt, at));
+    repeat<2>([&](auto s) {
+        repeat<2>([&](auto part) {
+            begin(part);
+            if constexpr (MX && part.value == 0) load_scales();
+            repeat<NLA + (part.value == 0 ? NLB : 0)>([&](auto j) { load(part, s.value, j); });
+            end(part);
+        });
+    });
+    clear();
+    wait_loads<3 * NLA + NLB>();
+    block_barrier();
+    if constexpr (MX) {
+        repeat<FH>([&](auto f) { sa[f.value] = read_scale(f, 1, 0); });
+        repeat<FN / 2>([&](auto f) { sb[f.value] = read_scale(Int<FH + f.value>{}, 1, 0); });
+    }
+    repeat<FN>([&](auto f) { fb[0][f.value] = rb.template get<f.value, 0>(lds_b[0]); });
+    repeat<FH>([&](auto f) { fa[0][f.value] = ra.template get<f.value, 0>(lds_a[0][0]); });
+    for (;;) {
+        const GroupedTile t = lt;
+        const int mrows = WEIGHTS ? g.M - t.m0 : min(t.n - t.m0, height);
+        live = (mrows > wm * GROUP) + (mrows > HALF + wm * GROUP);
+        int left = lsteps;
+        for (int kt = 0; left > 0; ++kt, --left) {
+            asm volatile("" : "+s"(left));  // one loop body: the compiler would peel the last steps
+            if (left == 2) {                // from here on the loads are the next tile's
+                at += gridDim.x >> 3;
+                if (at < last) {
+                    start(find_tile<WEIGHTS, BN>(g, list, WEIGHTS ? BM : height, mt, nt, at));
+                } else {
+                    la[0].stop();
+                    la[1].stop();
+                    lb.stop();
+                    ls = 1;  // (no scales either)
+                }
+            }
+            const int odd = left == 1 ? 0 : (kt + 1) & 1;
+            repeat<4>([&](auto p) { phase(p, odd); });
+        }
+        const int m = t.m0 + wm * GROUP, n = t.n0 + wn * FN * 16;
+        const int64_t row = WEIGHTS ? (int64_t)t.e * g.M + m : (int64_t)t.lo + m;
+        constexpr int esize = OUT == OUT_BF16 ? 2 : 4;
+        if (!(OUT == OUT_F32_ADD && t.n == 0))
+            store_tile<OUT, 2 * FH, FN, HALF>(acc, (char*)g.c + (row * g.ldc + n) * esize, g.ldc, mrows - wm * GROUP, g.N - n);
+        if (at >= last) break;
+        clear();
+    }
+    wait_loads<0>();  // nothing may arrive in LDS after the workgroup has left it
 }

@@ -4,15 +4,10 @@
 
 namespace {
 
-// Row tiles there can be: every full one, and one more for every expert that has rows.
-int64_t row_tiles(int rows_cap, int E, int bm) { return rows_cap / bm + (rows_cap < E ? rows_cap : E); }
-
+// One workgroup a compute unit (two where two fit), in eights so that every XCD has as many.
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN> hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
-    const int64_t nt = (g.N + BN - 1) / BN;
-    int64_t blocks;
-    if (LA == LAY_MN) blocks = (((int64_t)(g.M + BM - 1) / BM * nt + 7) / 8) * 8 * g.E;
-    else blocks = (row_tiles(g.rows_cap, g.E, BM) * nt + 7) / 8 * 8;
-    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN><<<(int)blocks, WM * WN * 64, 0, st>>>(g);
+    constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
+    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN><<<blocks, WM * WN * 64, 0, st>>>(g);
     return hipGetLastError();
 }
 

@@ -5,9 +5,8 @@
 namespace {
 
 template <int BM, int BN, int WM, int WN> hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
-    const int64_t tiles = (int64_t)g.rows_cap / BM + (g.rows_cap < g.E ? g.rows_cap : g.E), nt = (g.N + BN - 1) / BN;
-    const int64_t blocks = (tiles * nt + 7) / 8 * 8;
-    grouped_tile_kernel<FMT_MX4, LAY_K, LAY_K, OUT_BF16, BM, BN, WM, WN><<<(int)blocks, WM * WN * 64, 0, st>>>(g);
+    constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
+    grouped_tile_kernel<FMT_MX4, LAY_K, LAY_K, OUT_BF16, BM, BN, WM, WN><<<blocks, WM * WN * 64, 0, st>>>(g);
     return hipGetLastError();
 }
 
