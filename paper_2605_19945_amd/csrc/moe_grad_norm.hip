@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPart = 16384;  // values of a part: 64 a lane
+constexpr int kPart = 16384, kSmallPart = 2048;  // values of a part: 64 a lane, 8 where there are few
 
 struct GradList {
     const void* grad[GRAD_LIST];
@@ -20,7 +20,7 @@ struct GradList {
     int64_t count[GRAD_LIST];
     int32_t first_part[GRAD_LIST + 1];  // parts of the tensors before this one
     uint32_t f32[GRAD_LIST / 32];
-    int n;
+    int n, part;                        // tensors; values of a part
 };
 static_assert(sizeof(GradList) < 4000, "kernel arguments");
 
@@ -81,48 +81,75 @@ template <> struct Words<uint16_t> {
     static __device__ inline void put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
 };
 
+static __device__ inline double square(float v) { return (double)v * (double)v; }
+
 // Values [from, to) of a tensor: its 16-byte words between the first and last aligned address, and the values before
 // and behind them one by one.
-template <typename T> static __device__ inline double sum_part(const T* g, int64_t from, int64_t to) {
+template <bool NT> static __device__ inline u32x4_t load_word(const void* p) {
+    return NT ? __builtin_nontemporal_load((const u32x4_t*)p) : *(const u32x4_t*)p;
+}
+
+template <bool NT, typename T> static __device__ inline double sum_part(const T* g, int64_t from, int64_t to) {
     constexpr int PER = Words<T>::PER;
     double s = 0;
     const int64_t skew = ((uintptr_t)(g + from) & 15) / sizeof(T);
     const int64_t a = min(to, from + (skew ? PER - skew : 0)), b = a + (to - a) / PER * PER;
-    for (int64_t i = from + threadIdx.x; i < a; i += kThreads) s += (double)Words<T>::get(g + i) * Words<T>::get(g + i);
-    for (int64_t i = a + threadIdx.x * PER; i < b; i += kThreads * PER) {
+    for (int64_t j = from + threadIdx.x; j < a; j += kThreads) s += square(Words<T>::get(g + j));
+    auto add = [&](const u32x4_t& w) {
         float v[PER];
-        Words<T>::open(*(const u32x4_t*)(g + i), v);
+        Words<T>::open(w, v);
 #pragma unroll
         for (int j = 0; j < PER; ++j) s = fma((double)v[j], (double)v[j], s);
+    };
+    int64_t i = a + threadIdx.x * PER;
+    for (; i + 3 * kThreads * PER < b; i += 4 * kThreads * PER) {  // four words on their way
+        u32x4_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = load_word<NT>(g + i + k * kThreads * PER);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(w[k]);
     }
-    for (int64_t i = b + threadIdx.x; i < to; i += kThreads) s += (double)Words<T>::get(g + i) * Words<T>::get(g + i);
+    for (; i < b; i += kThreads * PER) add(load_word<NT>(g + i));
+    for (int64_t j = b + threadIdx.x; j < to; j += kThreads) s += square(Words<T>::get(g + j));
     return s;
 }
 
-template <typename T> static __device__ inline void scale_part(const T* g, T* o, int64_t from, int64_t to, float scale) {
+template <bool NT, typename T> static __device__ inline void scale_part(const T* g, T* o, int64_t from, int64_t to, float scale) {
     constexpr int PER = Words<T>::PER;
     const int64_t skew = ((uintptr_t)(g + from) & 15) / sizeof(T);
     const bool alike = (((uintptr_t)g ^ (uintptr_t)o) & 15) == 0;
     const int64_t a = alike ? min(to, from + (skew ? PER - skew : 0)) : to, b = a + (to - a) / PER * PER;
-    for (int64_t i = from + threadIdx.x; i < a; i += kThreads) Words<T>::put(o + i, Words<T>::get(g + i) * scale);
-    for (int64_t i = a + threadIdx.x * PER; i < b; i += kThreads * PER) {
+    for (int64_t j = from + threadIdx.x; j < a; j += kThreads) Words<T>::put(o + j, Words<T>::get(g + j) * scale);
+    auto put = [&](int64_t i, const u32x4_t& w) {
         float v[PER];
-        Words<T>::open(*(const u32x4_t*)(g + i), v);
+        Words<T>::open(w, v);
 #pragma unroll
         for (int j = 0; j < PER; ++j) v[j] *= scale;
-        *(u32x4_t*)(o + i) = Words<T>::close(v);
+        const u32x4_t out = Words<T>::close(v);
+        if (NT) __builtin_nontemporal_store(out, (u32x4_t*)(o + i));
+        else *(u32x4_t*)(o + i) = out;
+    };
+    int64_t i = a + threadIdx.x * PER;
+    for (; i + 3 * kThreads * PER < b; i += 4 * kThreads * PER) {
+        u32x4_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = load_word<NT>(g + i + k * kThreads * PER);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) put(i + k * kThreads * PER, w[k]);
     }
-    for (int64_t i = b + threadIdx.x; i < to; i += kThreads) Words<T>::put(o + i, Words<T>::get(g + i) * scale);
+    for (; i < b; i += kThreads * PER) put(i, load_word<NT>(g + i));
+    for (int64_t j = b + threadIdx.x; j < to; j += kThreads) Words<T>::put(o + j, Words<T>::get(g + j) * scale);
 }
 
+template <bool NT>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradList l, double* partials) {
     __shared__ double lds[kThreads / 64];
     double s = 0;
     for (int part = blockIdx.x; part < l.first_part[l.n]; part += gridDim.x) {
         const int t = tensor_of(l, part);
-        const int64_t from = (int64_t)(part - l.first_part[t]) * kPart, to = min(from + kPart, l.count[t]);
-        if (l.f32[t >> 5] >> (t & 31) & 1) s += sum_part((const float*)l.grad[t], from, to);
-        else s += sum_part((const uint16_t*)l.grad[t], from, to);
+        const int64_t from = (int64_t)(part - l.first_part[t]) * l.part, to = min(from + l.part, l.count[t]);
+        if (l.f32[t >> 5] >> (t & 31) & 1) s += sum_part<NT>((const float*)l.grad[t], from, to);
+        else s += sum_part<NT>((const uint16_t*)l.grad[t], from, to);
     }
     s = block_sum(s, lds);
     if (threadIdx.x == 0) partials[blockIdx.x] = s;
@@ -140,6 +167,7 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* parti
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+template <bool NT>
 __global__ __launch_bounds__(kThreads) void clip_kernel(GradList l, const double* partials, int n_partials, float max_norm, float* norm) {
     __shared__ double lds[kThreads / 64];
     const double total = sqrt(sum_partials(partials, n_partials, lds));
@@ -150,16 +178,29 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(GradList l, const double
     for (int p = blockIdx.x; p < parts; p += gridDim.x) {
         const int part = parts - 1 - p, t = tensor_of(l, part);
         if (scale == 1.f && l.grad[t] == l.out[t]) continue;
-        const int64_t from = (int64_t)(part - l.first_part[t]) * kPart, to = min(from + kPart, l.count[t]);
-        if (l.f32[t >> 5] >> (t & 31) & 1) scale_part((const float*)l.grad[t], (float*)l.out[t], from, to, scale);
-        else scale_part((const uint16_t*)l.grad[t], (uint16_t*)l.out[t], from, to, scale);
+        const int64_t from = (int64_t)(part - l.first_part[t]) * l.part, to = min(from + l.part, l.count[t]);
+        if (l.f32[t >> 5] >> (t & 31) & 1) scale_part<NT>((const float*)l.grad[t], (float*)l.out[t], from, to, scale);
+        else scale_part<NT>((const uint16_t*)l.grad[t], (uint16_t*)l.out[t], from, to, scale);
     }
 }
 
+// How a list is gone through: the length of a part (the small one while every compute unit still gets several), and whether the
+// accesses carry the non-temporal hint (where the last-level cache does not hold the list from one pass to the next).
+struct Way { int part; bool nt; };
+Way way_of(const int64_t* counts, const int32_t* f32, int n) {
+    int64_t values = 0, bytes = 0;
+    for (int i = 0; i < n; ++i) {
+        values += counts[i];
+        bytes += counts[i] * (f32[i] ? 4 : 2);
+    }
+    return {values < (int64_t)GRAD_BLOCKS * kPart ? kSmallPart : kPart, bytes > (int64_t)256 << 20};
+}
+
 // Tensors [first, first + n) as kernel arguments; returns their parts.
-int fill(GradList* l, const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int first, int n) {
+int fill(GradList* l, const Way& way, const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int first, int n) {
     int parts = 0;
     l->n = n;
+    l->part = way.part;
     for (int i = 0; i < GRAD_LIST / 32; ++i) l->f32[i] = 0;
     for (int i = 0; i < n; ++i) {
         l->grad[i] = grads[first + i];
@@ -167,7 +208,7 @@ int fill(GradList* l, const void* const* grads, void* const* outs, const int64_t
         l->count[i] = counts[first + i];
         if (f32[first + i]) l->f32[i >> 5] |= 1u << (i & 31);
         l->first_part[i] = parts;
-        parts += (int)((counts[first + i] + kPart - 1) / kPart);
+        parts += (int)((counts[first + i] + way.part - 1) / way.part);
     }
     l->first_part[n] = parts;
     return parts;
@@ -175,13 +216,14 @@ int fill(GradList* l, const void* const* grads, void* const* outs, const int64_t
 
 int blocks_of(int parts) { return parts < GRAD_BLOCKS ? (parts > 0 ? parts : 1) : GRAD_BLOCKS; }
 
-hipError_t launch_squares(const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, int* n_partials,
+hipError_t launch_squares(const Way& way, const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, int* n_partials,
                           hipStream_t st) {
     *n_partials = 0;
     for (int first = 0; first < n; first += GRAD_LIST) {
         GradList l;
-        const int blocks = blocks_of(fill(&l, grads, nullptr, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
-        grad_squares_kernel<<<blocks, kThreads, 0, st>>>(l, partials + *n_partials);
+        const int blocks = blocks_of(fill(&l, way, grads, nullptr, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
+        auto kernel = way.nt ? grad_squares_kernel<true> : grad_squares_kernel<false>;
+        kernel<<<blocks, kThreads, 0, st>>>(l, partials + *n_partials);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         *n_partials += blocks;
@@ -198,8 +240,9 @@ size_t grad_norm_workspace(int64_t n_tensors) {
 
 hipError_t launch_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, float* norm,
                             hipStream_t st) {
+    const Way way = way_of(counts, f32, n);
     int np = 0;
-    const hipError_t e = launch_squares(grads, counts, f32, n, partials, &np, st);
+    const hipError_t e = launch_squares(way, grads, counts, f32, n, partials, &np, st);
     if (e != hipSuccess) return e;
     grad_norm_kernel<<<1, kThreads, 0, st>>>(partials, np, norm);
     return hipGetLastError();
@@ -207,8 +250,9 @@ hipError_t launch_grad_norm(const void* const* grads, const int64_t* counts, con
 
 hipError_t launch_clip_grads(const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int n, float max_norm,
                              double* partials, float* norm, hipStream_t st) {
+    const Way way = way_of(counts, f32, n);
     int np = 0;
-    hipError_t e = launch_squares(grads, counts, f32, n, partials, &np, st);
+    hipError_t e = launch_squares(way, grads, counts, f32, n, partials, &np, st);
     if (e != hipSuccess) return e;
     if (n == 0) {
         grad_norm_kernel<<<1, kThreads, 0, st>>>(partials, 0, norm);
@@ -218,8 +262,9 @@ hipError_t launch_clip_grads(const void* const* grads, void* const* outs, const 
     for (int i = lists - 1; i >= 0; --i) {
         GradList l;
         const int first = i * GRAD_LIST;
-        const int blocks = blocks_of(fill(&l, grads, outs, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
-        clip_kernel<<<blocks, kThreads, 0, st>>>(l, partials, np, max_norm, i == lists - 1 ? norm : nullptr);
+        const int blocks = blocks_of(fill(&l, way, grads, outs, counts, f32, first, n - first < GRAD_LIST ? n - first : GRAD_LIST));
+        auto kernel = way.nt ? clip_kernel<true> : clip_kernel<false>;
+        kernel<<<blocks, kThreads, 0, st>>>(l, partials, np, max_norm, i == lists - 1 ? norm : nullptr);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

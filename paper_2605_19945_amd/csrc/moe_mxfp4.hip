@@ -95,7 +95,7 @@ __global__ __launch_bounds__(512) void mx_quantize_weights_kernel(const uint16_t
         const uint32_t* p = (const uint32_t*)(w + ((int64_t)e * K + blk * 32) * N + n);
         uint32_t in[32];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) in[k] = p[(int64_t)k * (N / 2)];
+        for (int k = 0; k < 32; ++k) in[k] = __builtin_nontemporal_load(p + (int64_t)k * (N / 2));  // read once
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             uint32_t top = 0;

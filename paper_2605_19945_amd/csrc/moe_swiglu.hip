@@ -10,8 +10,12 @@ constexpr int kThreads = 256;
 
 struct Row8 { float v[8]; };
 
-static __device__ inline Row8 load8(const uint16_t* p) {
-    const u32x4_t w = *(const u32x4_t*)p;
+// NT: the non-temporal hint, for tensors that no cache holds until their next use
+template <bool NT> static __device__ inline u32x4_t load8(const uint16_t* p) {
+    return NT ? __builtin_nontemporal_load((const u32x4_t*)p) : *(const u32x4_t*)p;
+}
+
+static __device__ inline Row8 open8(const u32x4_t& w) {
     Row8 r;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -21,7 +25,7 @@ static __device__ inline Row8 load8(const uint16_t* p) {
     return r;
 }
 
-static __device__ inline void store8(uint16_t* p, const Row8& r) {
+template <bool NT> static __device__ inline void store8(uint16_t* p, const Row8& r) {
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     u32x4_t w;
 #pragma unroll
@@ -29,7 +33,8 @@ static __device__ inline void store8(uint16_t* p, const Row8& r) {
         const bf16x2_t v = {(__bf16)r.v[2 * j], (__bf16)r.v[2 * j + 1]};
         w[j] = __builtin_bit_cast(uint32_t, v);
     }
-    *(u32x4_t*)p = w;
+    if (NT) __builtin_nontemporal_store(w, (u32x4_t*)p);
+    else *(u32x4_t*)p = w;
 }
 
 // With e = exp(-|g|) in (0, 1]: 1 / (1 + e) for g >= 0, e / (1 + e) below, which keeps its digits down to the smallest numbers
@@ -55,6 +60,7 @@ static __device__ inline uint64_t live_chunks(const int32_t* n_rows, int rows, i
     return (uint64_t)n * (f / 8);
 }
 
+template <bool NT>
 __global__ __launch_bounds__(kThreads) void swiglu_kernel(const uint16_t* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f,
                                                           uint16_t* h, int64_t ldh) {
     const uint64_t total = live_chunks(n_rows, rows, f);
@@ -63,15 +69,16 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const uint16_t* gu, in
         int col;
         place(i, f / 8, &row, &col);
         const uint16_t* p = gu + row * ldgu + col;
-        const Row8 g = load8(p), u = load8(p + f);
+        const u32x4_t gw = load8<NT>(p), uw = load8<NT>(p + f);
+        const Row8 g = open8(gw), u = open8(uw);
         Row8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o.v[j] = g.v[j] * logistic(g.v[j]) * u.v[j];
-        store8(h + row * ldh + col, o);
+        store8<NT>(h + row * ldh + col, o);
     }
 }
 
-template <bool WITH_H>
+template <bool WITH_H, bool NT>
 __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* gu, int64_t ldgu,
                                                                    const int32_t* n_rows, int rows, int f, uint16_t* dgu, int64_t lddgu,
                                                                    uint16_t* h, int64_t ldh) {
@@ -81,7 +88,8 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const uint16_
         int col;
         place(i, f / 8, &row, &col);
         const uint16_t* p = gu + row * ldgu + col;
-        const Row8 g = load8(p), u = load8(p + f), d = load8(dh + row * lddh + col);
+        const u32x4_t gw = load8<NT>(p), uw = load8<NT>(p + f), dw = load8<NT>(dh + row * lddh + col);
+        const Row8 g = open8(gw), u = open8(uw), d = open8(dw);
         Row8 dg, du, o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -91,9 +99,9 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const uint16_
             o.v[j] = gs * u.v[j];
         }
         uint16_t* q = dgu + row * lddgu + col;
-        store8(q, dg);
-        store8(q + f, du);
-        if (WITH_H) store8(h + row * ldh + col, o);
+        store8<NT>(q, dg);
+        store8<NT>(q + f, du);
+        if (WITH_H) store8<NT>(h + row * ldh + col, o);
     }
 }
 
@@ -102,16 +110,22 @@ int blocks_of(int rows, int f) {
     return (int)(want < 8192 ? want : 8192);
 }
 
+// Outputs past 128 MB are gone from the 256 MB last-level cache before they are read again
+bool streams(int rows, int f) { return (int64_t)rows * f * 2 > (int64_t)128 << 20; }
+
 }  // namespace
 
 hipError_t launch_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f, void* h, int64_t ldh, hipStream_t st) {
-    swiglu_kernel<<<blocks_of(rows, f), kThreads, 0, st>>>((const uint16_t*)gu, ldgu, n_rows, rows, f, (uint16_t*)h, ldh);
+    auto kernel = streams(rows, f) ? swiglu_kernel<true> : swiglu_kernel<false>;
+    kernel<<<blocks_of(rows, f), kThreads, 0, st>>>((const uint16_t*)gu, ldgu, n_rows, rows, f, (uint16_t*)h, ldh);
     return hipGetLastError();
 }
 
 hipError_t launch_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f,
                                   void* dgu, int64_t lddgu, void* h, int64_t ldh, hipStream_t st) {
-    auto kernel = h != nullptr ? swiglu_backward_kernel<true> : swiglu_backward_kernel<false>;
+    const bool nt = streams(rows, f);
+    auto kernel = h != nullptr ? (nt ? swiglu_backward_kernel<true, true> : swiglu_backward_kernel<true, false>)
+                               : (nt ? swiglu_backward_kernel<false, true> : swiglu_backward_kernel<false, false>);
     kernel<<<blocks_of(rows, f), kThreads, 0, st>>>((const uint16_t*)dh, lddh, (const uint16_t*)gu, ldgu, n_rows, rows, f, (uint16_t*)dgu,
                                                     lddgu, (uint16_t*)h, ldh);
     return hipGetLastError();
