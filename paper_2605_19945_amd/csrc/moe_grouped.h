@@ -53,8 +53,10 @@ static __device__ inline u32x4_t make_desc(const char* base, int bytes) {
 
 // 16 bytes a lane from memory to LDS at `to` + 16 * lane.  Inline asm, so that the compiler does not wait for it at the
 // next LDS read; it has no output registers.
-static __device__ inline void load_to_lds(uint32_t to, uint32_t offset, const u32x4_t& desc) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(desc) : "memory");
+// NT: with the non-temporal hint, for weights that one workgroup reads once.
+template <bool NT = false> static __device__ inline void load_to_lds(uint32_t to, uint32_t offset, const u32x4_t& desc) {
+    if (NT) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(offset), "s"(desc) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(desc) : "memory");
 }
 template <int N> static __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 static __device__ inline void block_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -79,6 +81,63 @@ static __device__ inline void place_in_band(int t, int mt, int nt, int* m, int* 
     *n = r / h;
     *m = 8 * band + r - *n * h;
 }
+
+// The list of the row tiles (BM rows) of all experts times nt column tiles, kept by every wave in its registers, 4 experts a lane;
+// each XCD (workgroup number % 8) takes one stretch [begin, end) of it.
+template <int BM> struct RowTiles {
+    int lo[4], n[4], cnt[4], before, upto;  // row tiles before the lane's experts, and with them
+    int nt, begin, end;
+
+    __device__ inline void init(const GroupedArgs& g, int nt_) {
+        const int lane = threadIdx.x & 63;
+        nt = nt_;
+        before = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 4 * lane + j;
+            lo[j] = n[j] = 0;
+            if (e < g.E) expert_rows(g.offsets, e, g.rows_cap, &lo[j], &n[j]);
+            cnt[j] = (n[j] + BM - 1) / BM;
+            before -= cnt[j];
+        }
+        upto = -before;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        before += upto;
+        const int64_t total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nt;
+        const int xcd = blockIdx.x & 7;
+        begin = (int)(total * xcd / 8);
+        end = (int)(total * (xcd + 1) / 8);
+    }
+    __device__ inline GroupedTile find(int t, int bn) const {
+        GroupedTile out = {};
+        const int tm = __builtin_amdgcn_readfirstlane(t / nt);  // an expert's tiles are its row tiles times nt
+        const int src = __builtin_ctzll(__ballot(upto > tm));
+        int b = __builtin_amdgcn_readlane(before, src), mt = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = __builtin_amdgcn_readlane(cnt[j], src);
+            if (mt == 0) {
+                if (tm < b + c) {
+                    mt = c;
+                    out.e = 4 * src + j;
+                    out.lo = __builtin_amdgcn_readlane(lo[j], src);
+                    out.n = __builtin_amdgcn_readlane(n[j], src);
+                } else {
+                    b += c;
+                }
+            }
+        }
+        int m, c;
+        place_in_band(t - b * nt, mt, nt, &m, &c);
+        out.m0 = __builtin_amdgcn_readfirstlane(m) * BM;
+        out.n0 = __builtin_amdgcn_readfirstlane(c) * bn;
+        return out;
+    }
+};
 
 // The list of all tiles, expert by expert, follows from the offsets alone; each XCD (workgroup number % 8) takes one stretch of
 // it, and its workgroups go through that side by side.  Every workgroup builds what it needs of the list in LDS.
@@ -204,7 +263,12 @@ static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileL
 // different banks.  LAY_MN: rows 0-3 and 8-11, two neighbouring chunks.  LAY_K: a 16-byte read serves lanes 0-3, 12-15 and 20-27 together,
 // so rows 0-3 and 12-15 of one chunk (swizzles 0 to 3) and rows 4-11 of a second one (4 to 7): whichever two chunks of an even distance
 // below 4 or neighbouring ones those are, the two sets stay apart (no conflicts counted for either format).
-static __device__ inline int swizzle_k(int row) {
+// Rows of 64 bytes lie four to a turn of the banks, so the four rows that share a place in it need a chunk each.
+template <int SPAN> static __device__ inline int swizzle_k(int row) {
+    if (SPAN == 64) {
+        const int t = row >> 2;
+        return (t << 1 & 2) ^ (t & 2) ^ (t >> 1 & 1);  // 0, 2, 3, 1 for t = 0 .. 3
+    }
     const int t = row >> 1;
     return (t & 1) | (t >> 1 & 2) | ((t ^ t << 1) & 4);
 }
@@ -214,9 +278,9 @@ template <int B> static __device__ inline int swizzle_mn(int row) {
     return B == 64 ? (row & 2) | (row >> 1 & 4) : 2 * ((row & 3) + (row >> 1 & 4));
 }
 
-// One operand's share of a wave: NL loads of 1 KiB a K step.
-template <int LAY, int B, int NL> struct Loader {
-    static constexpr int ROW = LAY == LAY_K ? 128 : 2 * B;  // bytes of a row in LDS
+// One operand's share of a wave: NL loads of 1 KiB a stage.  A stage is SPAN bytes of LAY_K rows or SPAN / 2 LAY_MN rows.
+template <int LAY, int B, int NL, int SPAN = 128> struct Loader {
+    static constexpr int ROW = LAY == LAY_K ? SPAN : 2 * B;  // bytes of a row in LDS
     const char* base;
     int64_t step;        // bytes to the next K step
     uint32_t ld;         // bytes between rows
@@ -231,11 +295,11 @@ template <int LAY, int B, int NL> struct Loader {
         base = first;
         ld = (uint32_t)ld_;
         if (LAY == LAY_K) {
-            step = 128;
+            step = SPAN;
             rows = min(valid, B);
             width = k;
         } else {
-            step = 64 * ld_;
+            step = SPAN / 2 * ld_;
             rows = k;
             width = 2 * max(min(valid, B), 0);  // (none in the lower half of a low tile)
         }
@@ -248,21 +312,21 @@ template <int LAY, int B, int NL> struct Loader {
             if (LAY == LAY_MN && c * 16 >= width) offset[j] = OUT_OF_RANGE;
         }
     }
-    static __device__ inline int swizzle(int row) { return LAY == LAY_K ? swizzle_k(row) : swizzle_mn<B>(row); }
+    static __device__ inline int swizzle(int row) { return LAY == LAY_K ? swizzle_k<SPAN>(row) : swizzle_mn<B>(row); }
     __device__ inline u32x4_t desc() const {
         if (LAY == LAY_K) return make_desc(base, rows > 0 && width > 0 ? (rows - 1) * (int)ld + width : 0);
-        return make_desc(base, rows > 0 && width > 0 ? (min(rows, 64) - 1) * (int)ld + width : 0);
+        return make_desc(base, rows > 0 && width > 0 ? (min(rows, SPAN / 2) - 1) * (int)ld + width : 0);
     }
     __device__ inline void stop() { rows = 0; }  // later stages read zeros
-    __device__ inline void issue(const u32x4_t& d, uint32_t to, int j, int wave) const { load_to_lds(to + (wave * NL + j) * 1024, offset[j], d); }
-    __device__ inline void next() {
-        base += step;
-        if (LAY == LAY_K) width -= 128;
-        else rows -= 64;
+    template <bool NT = false> __device__ inline void issue(const u32x4_t& d, uint32_t to, int j, int wave) const { load_to_lds<NT>(to + (wave * NL + j) * 1024, offset[j], d); }
+    __device__ inline void next(int stages = 1) {
+        base += step * stages;
+        if (LAY == LAY_K) width -= SPAN * stages;
+        else rows -= SPAN / 2 * stages;
     }
     // before the last K step, of a row that may end inside it
     __device__ inline void cut(int wave) {
-        if (LAY == LAY_K && width < 128) {
+        if (LAY == LAY_K && width < SPAN) {
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
                 const int p = (wave * NL + j) * 1024 + (threadIdx.x & 63) * 16;
@@ -274,7 +338,7 @@ template <int LAY, int B, int NL> struct Loader {
 };
 
 // Reads of one operand's fragments (16 rows or columns by the values of one matrix instruction).
-template <int FMT, int LAY, int B> struct Reader {
+template <int FMT, int LAY, int B, int SPAN = 128> struct Reader {
     uint32_t at[2];   // LAY_K: lane address for the first and second half of a K step
     uint32_t cl, ch;  // LAY_MN: lane address without its column chunk; the chunk of fragment 0 before the swizzle
     uint32_t sw;
@@ -286,7 +350,7 @@ template <int FMT, int LAY, int B> struct Reader {
             for (int h = 0; h < 2; ++h) {
                 // 4-bit values: a lane's two blocks of 32 are neighbours, in both operands alike
                 const int c = FMT == FMT_MX4 ? 2 * q + h : 4 * h + q;
-                at[h] = (first + i) * 128 + ((c ^ swizzle_k(i)) * 16);
+                at[h] = (first + i) * SPAN + ((c ^ swizzle_k<SPAN>(i)) * 16);
             }
         } else {
             cl = (8 * q + (i >> 2)) * (2 * B) + (i & 1) * 8;
@@ -295,7 +359,7 @@ template <int FMT, int LAY, int B> struct Reader {
         }
     }
     template <int F, int H> __device__ inline s16x8_t get(const char* tile) const {
-        if (LAY == LAY_K) return *(const s16x8_t*)(tile + at[H] + F * 2048);
+        if (LAY == LAY_K) return *(const s16x8_t*)(tile + at[H] + F * 16 * SPAN);
         const uint32_t o = cl + (((ch + 2 * F) ^ sw) * 16);
         typedef __attribute__((address_space(3))) s16x4_t lds4;
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + o + H * 64 * B));

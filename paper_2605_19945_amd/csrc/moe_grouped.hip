@@ -1,5 +1,5 @@
 // Launches of the matrix products grouped by expert.
-#include "moe_grouped.h"
+#include "moe_grouped_stream.h"
 #include "moe_ops.h"
 
 namespace {
@@ -40,6 +40,7 @@ hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool t
     g.rows_cap = rows_cap;
     g.N = N;
     g.kbytes = K * 2;
+    if (few_rows(rows_cap, E)) return transpose_w ? launch_stream<FMT_BF16, LAY_K>(g, st) : launch_stream<FMT_BF16, LAY_MN>(g, st);
     const bool large = large_tiles(g, false);
     if (transpose_w)
         return large ? launch_tiles<FMT_BF16, LAY_K, LAY_K, OUT_BF16, 256, 256, 2, 4>(g, st)

@@ -1,5 +1,5 @@
 // Launches of the matrix product grouped by expert on microscaled 4-bit operands.
-#include "moe_grouped.h"
+#include "moe_grouped_stream.h"
 #include "moe_ops.h"
 
 namespace {
@@ -29,6 +29,7 @@ hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, con
     g.N = N;
     g.kbytes = K / 2;
     g.scale_ld = mx_scale_cols(K);
+    if (few_rows(rows_cap, E)) return launch_stream<FMT_MX4, LAY_K>(g, st);
     if (rows_cap / E >= 192 && (int64_t)rows_cap / 256 * ((N + 255) / 256) >= 256) return launch_tiles<256, 256, 2, 4>(g, st);
     return launch_tiles<128, 128, 2, 2>(g, st);
 }
