@@ -182,19 +182,26 @@ moe_status moe_layer_forward(moe_ctx* ctx, const void* x, const void* router_pac
 
 typedef enum { MOE_BF16 = 0, MOE_F32 = 1 } moe_type;
 
+/* The grouped products take a workspace of at least the bytes that their *_workspace_bytes functions give for the same sizes (0: it may be
+ * NULL): partial sums where a long reduction of few tiles is cut into ranges.  16-byte aligned, used until the call's work is
+ * done; calls that may overlap need one each. */
+
 /* y[r, :] = x[r, :] . W[e] for the rows r of every expert e: bf16 operands, fp32 sums, bf16 results rounded once.
  * W is [E, K, N] (transpose_w == 0; the layout of W1, W3 and W2) or [E, N, K] (transpose_w != 0: x times W[e]^T).  The
  * gradient of x is this call on the gradient of y with transpose_w the other way round.
  * x [n_rows_cap, K], y [n_rows_cap, N]. */
+size_t moe_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, int32_t transpose_w);
 moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t transpose_w, const int32_t* offsets,
-                            int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y, int64_t ldy, void* stream);
+                            int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y, int64_t ldy, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* Gradient of the weights: dw[e] = sum over the rows r of expert e of x[r, :]^T dy[r, :]  (fp32 sums in a fixed order).
  * dw [E, K, N] of `type` (moe_type); experts without rows get zeros.  accumulate != 0 (fp32 only): added to what dw
  * holds, experts without rows are left alone. */
+size_t moe_grouped_gemm_wgrad_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N);
 moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets,
                                   int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* dw, int32_t type,
-                                  int32_t accumulate, void* stream);
+                                  int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /* h = silu(g) * u with g = gu[:, :f], u = gu[:, f:2f] (bf16).  n_rows: NULL, or the number of rows there are on the device
  * (e.g. offsets + E), at most n_rows_cap; later rows are left alone.  gu [n_rows_cap, 2f], h [n_rows_cap, f]. */
@@ -240,9 +247,10 @@ moe_status moe_mxfp4_dequantize(const void* values, const void* scales, int64_t 
 
 /* y[r, :] = x[r, :] . W[e]^T on such operands: exact products, fp32 sums, bf16 results rounded once.
  * x_values [n_rows_cap, K/2], x_scales [n_rows_cap, scale_cols(K)], w_values [E, N, K/2], w_scales [E, N, scale_cols(K)]. */
+size_t moe_mxfp4_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N);
 moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, const void* w_values, const void* w_scales,
                                   const int32_t* offsets, int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y,
-                                  int64_t ldy, void* stream);
+                                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- introspection --------------------------------------------------------------------------- */
 

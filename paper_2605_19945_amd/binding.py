@@ -5,7 +5,9 @@ PyTorch is used for device memory and streams: tensors are passed as raw device 
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import functools
 import os
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -72,8 +74,10 @@ _SIGNATURES = {
     "moe_ffn_refused_flag": (C.c_int, [_VP, C.POINTER(_VP)]),
     "moe_tile_rows": (_I32, [_VP]),
     "moe_set_tile_class": (C.c_int, [_VP, _I32]),
-    "moe_grouped_gemm": (C.c_int, [_VP, _I64, _VP, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _I64, _VP]),
-    "moe_grouped_gemm_wgrad": (C.c_int, [_VP, _I64, _VP, _I64, _VP, _I32, _I32, _I32, _I32, _VP, _I32, _I32, _VP]),
+    "moe_grouped_gemm_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32]),
+    "moe_grouped_gemm": (C.c_int, [_VP, _I64, _VP, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _SZ, _VP]),
+    "moe_grouped_gemm_wgrad_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
+    "moe_grouped_gemm_wgrad": (C.c_int, [_VP, _I64, _VP, _I64, _VP, _I32, _I32, _I32, _I32, _VP, _I32, _I32, _VP, _SZ, _VP]),
     "moe_swiglu": (C.c_int, [_VP, _I64, _VP, _I32, _I32, _VP, _I64, _VP]),
     "moe_swiglu_backward": (C.c_int, [_VP, _I64, _VP, _I64, _VP, _I32, _I32, _VP, _I64, _VP, _I64, _VP]),
     "moe_grad_norm_workspace_bytes": (_SZ, [_I32]),
@@ -83,7 +87,8 @@ _SIGNATURES = {
     "moe_mxfp4_quantize": (C.c_int, [_VP, _I32, _I64, _VP, _I32, _I32, _VP, _VP, _VP]),
     "moe_mxfp4_quantize_weights": (C.c_int, [_VP, _I32, _I32, _I32, _VP, _VP, _VP]),
     "moe_mxfp4_dequantize": (C.c_int, [_VP, _VP, _I64, _I32, _VP, _I64, _VP]),
-    "moe_mxfp4_grouped_gemm": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I32, _I32, _I32, _I32, _VP, _I64, _VP]),
+    "moe_mxfp4_grouped_gemm_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
+    "moe_mxfp4_grouped_gemm": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _SZ, _VP]),
     "moe_layer_intermediates": (C.c_int, [_VP, C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP)]),
 }
 
@@ -297,24 +302,28 @@ def moe_permute_noalloc(x, topk_idx, E, e_lo=0, E_local=-1, xp=None, offsets=Non
 
 
 # ---- operators around the experts' weights (no context) -----------------------------------------------
-# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.
+# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.  Small calls are bound by
+# this code (a call takes 5 to 6 us, half of it the launch), so the checks are plain comparisons.
 def _refuse(what, why):
     raise MoEError(1, f"{what}: {why}")
 
 
-def _check_tensors(what, *tensors):
-    for t in tensors:
-        if t.get_device() < 0:
-            _refuse(what, "tensors have to be on the GPU")
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t.get_device() != dev:
-            _refuse(what, f"tensors have to be on the current device, cuda:{dev}")
+def _launch_device(what, t, *others):
+    """The device of all these tensors, which has to be the current one."""
+    dev = t.get_device()
+    if dev < 0:
+        _refuse(what, "tensors have to be on the GPU")
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            _refuse(what, "tensors have to be on one device")
+    if torch._C._cuda_getDevice() != dev:
+        _refuse(what, f"tensors have to be on the current device, cuda:{torch._C._cuda_getDevice()}")
+    return dev
 
 
 def _rows(what, name, t, dtype, width=None):
     """Values between two rows of the matrix t, whose own values are contiguous."""
-    if t.dtype != dtype or t.dim() != 2:
+    if t.dtype is not dtype or t.dim() != 2:
         _refuse(what, f"{name} has to be a matrix of {dtype}")
     rows, w = t.shape
     if width is not None and w != width:
@@ -326,13 +335,30 @@ def _rows(what, name, t, dtype, width=None):
 
 
 def _whole(what, name, t, dtype, shape):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _refuse(what, f"{name} has to be a contiguous tensor of {dtype}, {tuple(shape)}")
 
 
 def _groups(what, offsets, E):
-    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] != E + 1 or not offsets.is_contiguous():
+    if offsets.dtype is not torch.int32 or offsets.shape != (E + 1,) or not offsets.is_contiguous():
         _refuse(what, f"offsets has to be a contiguous vector of {E + 1} int32")
+
+
+def _live(what, offsets):
+    """Address of the number of rows that there are, the last of the offsets (None: all rows)."""
+    if offsets is None:
+        return None
+    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous():
+        _refuse(what, "offsets has to be a contiguous vector of int32")
+    return offsets.data_ptr() + 4 * (offsets.shape[0] - 1)
+
+
+def _out_rows(what, name, out, rows, width):
+    """Values between the rows of the output `out`, bf16 [rows, width]."""
+    ld = _rows(what, name, out, torch.bfloat16, width)
+    if out.shape[0] != rows:
+        _refuse(what, f"{name} has to have {rows} rows")
+    return ld
 
 
 def _done(st, what):
@@ -340,215 +366,239 @@ def _done(st, what):
         raise MoEError(st, what)
 
 
-def _live(what, offsets):
-    """Address of the number of rows that there are, the last of the offsets (None: all rows)."""
-    if offsets is None:
-        return None
-    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous():
-        _refuse(what, "offsets has to be a contiguous vector of int32")
-    return offsets.data_ptr() + 4 * (offsets.shape[0] - 1)
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name, *sizes):
+    """What a call of these sizes needs (it follows from them alone)."""
+    return getattr(load_library(), name)(*sizes)
 
 
-def _like_rows(what, name, out, t, rows, width, dtype=None):
-    """The output `out`, or a new one on t's device, and the values between its rows."""
-    dtype = dtype or torch.bfloat16
-    if out is None:
-        return torch.empty((rows, width), dtype=dtype, device=t.device), width
-    ld = _rows(what, name, out, dtype, width)
-    if out.shape[0] != rows:
-        _refuse(what, f"{name} has to have {rows} rows")
-    return out, ld
+def _workspace(t, name, *sizes):
+    """(workspace or None, its address, its bytes) for a call on t's device."""
+    n = _workspace_bytes(name, *sizes)
+    if n == 0:
+        return None, None, 0
+    ws = t.new_empty(n, dtype=torch.uint8)
+    return ws, ws.data_ptr(), n
 
 
 def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
     """y[r] = x[r] @ w[e] (transpose_w: @ w[e].T) for the rows r of every expert e.  x [rows, K] bf16; w [E, K, N]
     (transpose_w: [E, N, K]) bf16; offsets [E + 1] int32.  Rows from offsets[E] on are left as they are."""
-    lib, what = load_library(), "moe_grouped_gemm"
-    if w.dim() != 3:
-        _refuse(what, "w has to have three dimensions")
+    lib, what = _lib or load_library(), "moe_grouped_gemm"
+    if w.dim() != 3 or w.dtype is not torch.bfloat16 or not w.is_contiguous():
+        _refuse(what, "w has to be a contiguous tensor of bfloat16 with three dimensions")
     E, K, N = w.shape
     if transpose_w:
         K, N = N, K
-    _whole(what, "w", w, torch.bfloat16, w.shape)
     ldx = _rows(what, "x", x, torch.bfloat16, K)
+    rows = x.shape[0]
     _groups(what, offsets, E)
-    out, ldy = _like_rows(what, "out", out, x, x.shape[0], N)
-    _check_tensors(what, x, w, offsets, out)
-    _done(lib.moe_grouped_gemm(x.data_ptr(), ldx, w.data_ptr(), 1 if transpose_w else 0, offsets.data_ptr(), x.shape[0], E, K, N,
-                               out.data_ptr(), ldy, _stream()), what)
+    dev = _launch_device(what, x, w, offsets, out)
+    if out is None:
+        out, ldy = x.new_empty((rows, N)), N
+    else:
+        ldy = _out_rows(what, "out", out, rows, N)
+    t = 1 if transpose_w else 0
+    ws, at, n = _workspace(x, "moe_grouped_gemm_workspace_bytes", rows, E, K, N, t)
+    st = lib.moe_grouped_gemm(x.data_ptr(), ldx, w.data_ptr(), t, offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n,
+                              torch._C._cuda_getCurrentRawStream(dev))
+    _done(st, what)
     return out
 
 
 def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=False):
     """dw[e] = x[r].T @ dy[r] summed over the rows r of expert e: [E, K, N] of `dtype` (fp32, the default, or bf16).
     accumulate: add to `out` (fp32)."""
-    lib, what = load_library(), "moe_grouped_gemm_wgrad"
+    lib, what = _lib or load_library(), "moe_grouped_gemm_wgrad"
     ldx, lddy = _rows(what, "x", x, torch.bfloat16), _rows(what, "dy", dy, torch.bfloat16)
-    if x.shape[0] != dy.shape[0]:
+    rows, K = x.shape
+    if dy.shape[0] != rows:
         _refuse(what, "x and dy have to have as many rows")
-    E, K, N = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, x.shape[1], dy.shape[1]
+    E, N = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, dy.shape[1]
     _groups(what, offsets, E)
+    if out is not None:
+        if out.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and out.dtype is not dtype):
+            _refuse(what, "out has to be of dtype, float32 or bfloat16")
+        _whole(what, "out", out, out.dtype, (E, K, N))
+    elif accumulate:
+        _refuse(what, "accumulate needs out")
+    elif dtype not in (None, torch.float32, torch.bfloat16):
+        _refuse(what, "dtype has to be float32 or bfloat16")
+    dev = _launch_device(what, x, dy, offsets, out)
     if out is None:
-        if accumulate:
-            _refuse(what, "accumulate needs out")
-        dtype = dtype or torch.float32
-        if dtype not in (torch.float32, torch.bfloat16):
-            _refuse(what, "dtype has to be float32 or bfloat16")
-        _check_tensors(what, x)
-        out = torch.empty((max(E, 0), K, N), dtype=dtype, device=x.device)
-    elif out.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and out.dtype != dtype):
-        _refuse(what, "out has to be of dtype, float32 or bfloat16")
-    _whole(what, "out", out, out.dtype, (E, K, N))
-    _check_tensors(what, x, dy, offsets, out)
-    _done(lib.moe_grouped_gemm_wgrad(x.data_ptr(), ldx, dy.data_ptr(), lddy, offsets.data_ptr(), x.shape[0], E, K, N, out.data_ptr(),
-                                     1 if out.dtype == torch.float32 else 0, 1 if accumulate else 0, _stream()), what)
+        out = x.new_empty((max(E, 0), K, N), dtype=dtype or torch.float32)
+    ws, at, n = _workspace(x, "moe_grouped_gemm_wgrad_workspace_bytes", rows, E, K, N)
+    st = lib.moe_grouped_gemm_wgrad(x.data_ptr(), ldx, dy.data_ptr(), lddy, offsets.data_ptr(), rows, E, K, N, out.data_ptr(),
+                                    1 if out.dtype is torch.float32 else 0, 1 if accumulate else 0, at, n,
+                                    torch._C._cuda_getCurrentRawStream(dev))
+    _done(st, what)
     return out
 
 
 def moe_swiglu(gu, offsets=None, out=None):
     """silu(gu[:, :f]) * gu[:, f:] (bf16).  offsets: rows from its last value on are left as they are."""
-    lib, what = load_library(), "moe_swiglu"
+    lib, what = _lib or load_library(), "moe_swiglu"
     ldgu, live = _rows(what, "gu", gu, torch.bfloat16), _live(what, offsets)
-    rows, f = gu.shape[0], gu.shape[1] // 2
-    if gu.shape[1] % 2:
+    rows, f2 = gu.shape
+    if f2 % 2:
         _refuse(what, "gu has to have an even number of columns")
-    out, ldh = _like_rows(what, "out", out, gu, rows, f)
-    _check_tensors(what, gu, out, *(() if offsets is None else (offsets,)))
-    _done(lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), ldh, _stream()), what)
+    f = f2 // 2
+    dev = _launch_device(what, gu, offsets, out)
+    if out is None:
+        out, ldh = gu.new_empty((rows, f)), f
+    else:
+        ldh = _out_rows(what, "out", out, rows, f)
+    _done(lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), ldh, torch._C._cuda_getCurrentRawStream(dev)), what)
     return out
 
 
 def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     """The gradient of gu [rows, 2f] from that of moe_swiglu's result.  h: a matrix [rows, f] that gets that result
     again.  out may be gu itself."""
-    lib, what = load_library(), "moe_swiglu_backward"
+    lib, what = _lib or load_library(), "moe_swiglu_backward"
     lddh, live = _rows(what, "dh", dh, torch.bfloat16), _live(what, offsets)
     rows, f = dh.shape
     ldgu = _rows(what, "gu", gu, torch.bfloat16, 2 * f)
     if gu.shape[0] != rows:
         _refuse(what, "dh and gu have to have as many rows")
-    out, lddgu = _like_rows(what, "out", out, gu, rows, 2 * f)
-    ldh = f
-    if h is not None:
-        h, ldh = _like_rows(what, "h", h, gu, rows, f)
-    _check_tensors(what, dh, gu, out, *(t for t in (offsets, h) if t is not None))
+    ldh = f if h is None else _out_rows(what, "h", h, rows, f)
+    dev = _launch_device(what, dh, gu, offsets, out, h)
+    if out is None:
+        out, lddgu = gu.new_empty((rows, 2 * f)), 2 * f
+    else:
+        lddgu = _out_rows(what, "out", out, rows, 2 * f)
     _done(lib.moe_swiglu_backward(dh.data_ptr(), lddh, gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), lddgu, _ptr(h), ldh,
-                                  _stream()), what)
+                                  torch._C._cuda_getCurrentRawStream(dev)), what)
     return out
 
 
 def _grad_list(what, tensors):
+    """Host arrays of the addresses, sizes and types of a list of gradients."""
     f32, bf16 = torch.float32, torch.bfloat16
-    for t in tensors:
-        if (t.dtype != f32 and t.dtype != bf16) or not t.is_contiguous():
-            _refuse(what, "gradients have to be contiguous tensors of float32 or bfloat16")
+    types = [t.dtype for t in tensors]
+    if not all(t is f32 or t is bf16 for t in types) or not all([t.is_contiguous() for t in tensors]):
+        _refuse(what, "gradients have to be contiguous tensors of float32 or bfloat16")
     n = len(tensors)
-    return ((_VP * n)(*[t.data_ptr() for t in tensors]), (_I64 * n)(*[t.numel() for t in tensors]),
-            (_I32 * n)(*[t.dtype == f32 for t in tensors]))
+    return (array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", [t.numel() for t in tensors]),
+            array.array("i", [t is f32 for t in types]))
 
 
-def _norm_of(what, tensors, call):
-    _check_tensors(what, *tensors)
-    n = load_library().moe_grad_norm_workspace_bytes(len(tensors))
-    dev = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
-    ws = torch.empty(n + 8, dtype=torch.uint8, device=dev)  # the norm lies behind the workspace
-    _done(call(ws.data_ptr(), n, ws.data_ptr() + n, _stream()), what)
-    return ws[n:n + 4].view(torch.float32)[0]
+def _norm_of(what, tensors, others, call):
+    if tensors:
+        devices = {t.get_device() for t in tensors} | {t.get_device() for t in others}
+        dev = _launch_device(what, tensors[0])
+        if len(devices) > 1:
+            _refuse(what, "tensors have to be on one device")
+    else:
+        dev = torch.cuda.current_device()
+    n = _workspace_bytes("moe_grad_norm_workspace_bytes", len(tensors))
+    ws = torch.empty(n // 4 + 1, dtype=torch.float32, device=torch.device("cuda", dev))  # the norm lies behind the workspace
+    at = ws.data_ptr()
+    _done(call(at, n, at + n, torch._C._cuda_getCurrentRawStream(dev)), what)
+    return ws[n // 4]
 
 
 def moe_grad_norm(grads):
     """Norm over all values of a list of gradients (float32 or bfloat16), as a tensor on the GPU."""
-    lib, what = load_library(), "moe_grad_norm"
+    lib, what = _lib or load_library(), "moe_grad_norm"
     grads = list(grads)
     ptrs, counts, types = _grad_list(what, grads)
-    return _norm_of(what, grads, lambda ws, n, norm, st: lib.moe_grad_norm(ptrs, counts, types, len(grads), ws, n, norm, st))
+    a = [v.buffer_info()[0] for v in (ptrs, counts, types)]
+    return _norm_of(what, grads, (), lambda ws, n, norm, st: lib.moe_grad_norm(*a, len(grads), ws, n, norm, st))
 
 
 def moe_clip_grad_norm(grads, max_norm, out=None):
     """Scales the gradients by min(1, max_norm / (norm + 1e-6)) in place, or into the tensors of `out` (of the same
     types and sizes, overlapping nothing).  Returns the norm before, as a tensor on the GPU."""
-    lib, what = load_library(), "moe_clip_grad_norm"
+    lib, what = _lib or load_library(), "moe_clip_grad_norm"
     grads = list(grads)
     ptrs, counts, types = _grad_list(what, grads)
-    outs = ptrs
-    if out is not None:
-        out = list(out)
+    outs, out = ptrs, () if out is None else list(out)
+    if out:
         outs, n_out, out_types = _grad_list(what, out)
-        if list(n_out) != list(counts) or list(out_types) != list(types):
+        if n_out != counts or out_types != types:
             _refuse(what, "out has to hold as many tensors of the same types and sizes")
-        _check_tensors(what, *out)
-    return _norm_of(what, grads, lambda ws, n, norm, st: lib.moe_clip_grad_norm(ptrs, outs, counts, types, len(grads), max_norm, ws, n,
-                                                                               norm, st))
+    a = [v.buffer_info()[0] for v in (ptrs, outs, counts, types)]
+    return _norm_of(what, grads, out, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
 
 
-def _mx_pair(what, lead, K, device):
-    cols = load_library().moe_mxfp4_scale_cols(K)
+def _mx_pair(what, t, lead, K):
+    cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
     if cols == 0:
         raise MoEError(2, what)
-    return (torch.empty((*lead, K // 2), dtype=torch.uint8, device=device), torch.empty((*lead, cols), dtype=torch.uint8, device=device))
+    return t.new_empty((*lead, K // 2), dtype=torch.uint8), t.new_empty((*lead, cols), dtype=torch.uint8)
 
 
 def moe_mxfp4_quantize(x, offsets=None):
     """Rows [n, K] (bf16 or fp32) -> (values [n, K / 2], scales [n, S]), uint8.  offsets: rows from its last value on
     are not quantised."""
-    lib, what = load_library(), "moe_mxfp4_quantize"
-    ldx, live = _rows(what, "x", x, torch.float32 if x.dtype == torch.float32 else torch.bfloat16), _live(what, offsets)
-    _check_tensors(what, x, *(() if offsets is None else (offsets,)))
-    values, scales = _mx_pair(what, (x.shape[0],), x.shape[1], x.device)
-    _done(lib.moe_mxfp4_quantize(x.data_ptr(), 1 if x.dtype == torch.float32 else 0, ldx, live, x.shape[0], x.shape[1],
-                                 values.data_ptr(), scales.data_ptr(), _stream()), what)
+    lib, what = _lib or load_library(), "moe_mxfp4_quantize"
+    f32 = x.dtype is torch.float32
+    ldx, live = _rows(what, "x", x, torch.float32 if f32 else torch.bfloat16), _live(what, offsets)
+    rows, K = x.shape
+    dev = _launch_device(what, x, offsets)
+    values, scales = _mx_pair(what, x, (rows,), K)
+    _done(lib.moe_mxfp4_quantize(x.data_ptr(), 1 if f32 else 0, ldx, live, rows, K, values.data_ptr(), scales.data_ptr(),
+                                 torch._C._cuda_getCurrentRawStream(dev)), what)
     return values, scales
 
 
 def moe_mxfp4_quantize_weights(w):
     """Weights [E, K, N] (bf16) -> (values [E, N, K / 2], scales [E, N, S]), uint8, blocks along K."""
-    lib, what = load_library(), "moe_mxfp4_quantize_weights"
-    if w.dim() != 3:
-        _refuse(what, "w has to have three dimensions")
+    lib, what = _lib or load_library(), "moe_mxfp4_quantize_weights"
+    if w.dim() != 3 or w.dtype is not torch.bfloat16 or not w.is_contiguous():
+        _refuse(what, "w has to be a contiguous tensor of bfloat16 with three dimensions")
     E, K, N = w.shape
-    _whole(what, "w", w, torch.bfloat16, w.shape)
-    _check_tensors(what, w)
-    values, scales = _mx_pair(what, (E, N), K, w.device)
-    _done(lib.moe_mxfp4_quantize_weights(w.data_ptr(), E, K, N, values.data_ptr(), scales.data_ptr(), _stream()), what)
+    dev = _launch_device(what, w)
+    values, scales = _mx_pair(what, w, (E, N), K)
+    _done(lib.moe_mxfp4_quantize_weights(w.data_ptr(), E, K, N, values.data_ptr(), scales.data_ptr(),
+                                         torch._C._cuda_getCurrentRawStream(dev)), what)
     return values, scales
 
 
 def _mx_check(what, name, values, scales):
     """K of a pair of codes and scales."""
-    if values.dim() < 2 or values.dtype != torch.uint8 or not values.is_contiguous():
+    if values.dim() < 2 or values.dtype is not torch.uint8 or not values.is_contiguous():
         _refuse(what, f"the values of {name} have to be a contiguous tensor of uint8")
     K = 2 * values.shape[-1]
-    cols = load_library().moe_mxfp4_scale_cols(K)
+    cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
     if cols == 0:
         raise MoEError(2, what)
-    _whole(what, f"scales of {name}", scales, torch.uint8, (*values.shape[:-1], cols))
+    if scales.dtype is not torch.uint8 or scales.shape != (*values.shape[:-1], cols) or not scales.is_contiguous():
+        _refuse(what, f"the scales of {name} have to be a contiguous tensor of uint8, {(*values.shape[:-1], cols)}")
     return K
 
 
 def moe_mxfp4_dequantize(values, scales):
     """The bf16 values [..., K] that codes [..., K / 2] and scales [..., S] stand for."""
-    lib, what = load_library(), "moe_mxfp4_dequantize"
+    lib, what = _lib or load_library(), "moe_mxfp4_dequantize"
     K = _mx_check(what, "x", values, scales)
-    _check_tensors(what, values, scales)
-    out = torch.empty((*values.shape[:-1], K), dtype=torch.bfloat16, device=values.device)
-    _done(lib.moe_mxfp4_dequantize(values.data_ptr(), scales.data_ptr(), out.numel() // K, K, out.data_ptr(), K, _stream()), what)
+    dev = _launch_device(what, values, scales)
+    out = values.new_empty((*values.shape[:-1], K), dtype=torch.bfloat16)
+    _done(lib.moe_mxfp4_dequantize(values.data_ptr(), scales.data_ptr(), out.numel() // K, K, out.data_ptr(), K,
+                                   torch._C._cuda_getCurrentRawStream(dev)), what)
     return out
 
 
 def moe_mxfp4_grouped_gemm(x_values, x_scales, w_values, w_scales, offsets, out=None):
     """y[r] = x[r] @ w[e].T on 4-bit rows [n, K / 2] and weights [E, N, K / 2] with their scales; bf16 [n, N]."""
-    lib, what = load_library(), "moe_mxfp4_grouped_gemm"
+    lib, what = _lib or load_library(), "moe_mxfp4_grouped_gemm"
     if x_values.dim() != 2 or w_values.dim() != 3:
         _refuse(what, "x_values has to have two dimensions, w_values three")
     K = _mx_check(what, "x", x_values, x_scales)
     if _mx_check(what, "w", w_values, w_scales) != K:
         _refuse(what, "x and w have to have the same K")
-    E, N = w_values.shape[0], w_values.shape[1]
+    rows, (E, N) = x_values.shape[0], w_values.shape[:2]
     _groups(what, offsets, E)
-    out, ldy = _like_rows(what, "out", out, x_values, x_values.shape[0], N)
-    _check_tensors(what, x_values, x_scales, w_values, w_scales, offsets, out)
+    dev = _launch_device(what, x_values, x_scales, w_values, w_scales, offsets, out)
+    if out is None:
+        out, ldy = x_values.new_empty((rows, N), dtype=torch.bfloat16), N
+    else:
+        ldy = _out_rows(what, "out", out, rows, N)
+    ws, at, n = _workspace(x_values, "moe_mxfp4_grouped_gemm_workspace_bytes", rows, E, K, N)
     _done(lib.moe_mxfp4_grouped_gemm(x_values.data_ptr(), x_scales.data_ptr(), w_values.data_ptr(), w_scales.data_ptr(),
-                                     offsets.data_ptr(), x_values.shape[0], E, K, N, out.data_ptr(), ldy, _stream()), what)
+                                     offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n,
+                                     torch._C._cuda_getCurrentRawStream(dev)), what)
     return out
 
 

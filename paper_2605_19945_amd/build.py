@@ -14,7 +14,8 @@ LIB = os.path.join(PKG, "libmoe_gfx950.so")
 SOURCES = ["moe_api.hip", "moe_route.hip", "moe_permute.hip", "moe_pack.hip", "moe_gemm.hip", "moe_gemm_swiglu.hip",
            "moe_gemm_plain.hip", "moe_gemm_pairsum.hip", "moe_gemm_partial.hip", "moe_gemm_swiglu_stream.hip",
            "moe_gemm_plain_stream.hip", "moe_gemm_partial_stream.hip", "moe_place.hip",
-           "moe_ops_api.hip", "moe_grouped.hip", "moe_grouped_mx.hip", "moe_mxfp4.hip", "moe_swiglu.hip", "moe_grad_norm.hip"]
+           "moe_ops_api.hip", "moe_grouped.hip", "moe_grouped_row_major.hip", "moe_grouped_transposed.hip", "moe_grouped_mx.hip",
+           "moe_grouped_weights.hip", "moe_mxfp4.hip", "moe_swiglu.hip", "moe_grad_norm.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 

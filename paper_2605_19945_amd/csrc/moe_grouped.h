@@ -30,6 +30,9 @@ struct GroupedArgs {
     int M, N;                // M: width of x in the weight gradient (otherwise the experts' rows)
     int kbytes;              // bytes of a LAY_K row; values of the reduction where no operand is LAY_K (0: an expert's rows)
     int scale_ld;            // bytes between rows of scales
+    int splits;              // ranges the reduction is cut into (1: none)
+    float* part;             // their partial sums, laid out like c without gaps (rows N values apart), one slab after the other
+    int64_t slab;            // values of a slab
 };
 
 typedef __attribute__((address_space(3))) char lds_char;
@@ -71,6 +74,7 @@ static __device__ inline void expert_rows(const int32_t* offsets, int e, int cap
 struct GroupedTile {
     int e, lo, n;  // expert, its first row, its rows
     int m0, n0;    // first row (column of x in the weight gradient) and first column of the tile
+    int split;     // range of the reduction
 };
 
 // Inside one expert's mt x nt tiles: bands of up to 8 row tiles, row tiles fastest, so that the 32 compute units of an XCD
@@ -82,13 +86,13 @@ static __device__ inline void place_in_band(int t, int mt, int nt, int* m, int* 
     *m = 8 * band + r - *n * h;
 }
 
-// The list of the row tiles (BM rows) of all experts times nt column tiles, kept by every wave in its registers, 4 experts a lane;
+// The list of the row tiles (BM rows) of all experts times nt column tiles times the ranges of the reduction, kept by every wave in its registers, 4 experts a lane;
 // each XCD (workgroup number % 8) takes one stretch [begin, end) of it.
 template <int BM> struct RowTiles {
     int lo[4], n[4], cnt[4], before, upto;  // row tiles before the lane's experts, and with them
     int nt, begin, end;
 
-    __device__ inline void init(const GroupedArgs& g, int nt_) {
+    __device__ inline void init(const GroupedArgs& g, int nt_, int splits) {
         const int lane = threadIdx.x & 63;
         nt = nt_;
         before = 0;
@@ -107,13 +111,15 @@ template <int BM> struct RowTiles {
             if (lane >= d) upto += o;
         }
         before += upto;
-        const int64_t total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nt;
+        const int64_t total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nt * splits;
         const int xcd = blockIdx.x & 7;
         begin = (int)(total * xcd / 8);
         end = (int)(total * (xcd + 1) / 8);
     }
-    __device__ inline GroupedTile find(int t, int bn) const {
+    __device__ inline GroupedTile find(int t, int bn, int splits) const {
         GroupedTile out = {};
+        out.split = t % splits;
+        t = t / splits;
         const int tm = __builtin_amdgcn_readfirstlane(t / nt);  // an expert's tiles are its row tiles times nt
         const int src = __builtin_ctzll(__ballot(upto > tm));
         int b = __builtin_amdgcn_readlane(before, src), mt = 0;
@@ -153,7 +159,7 @@ constexpr int TILE_COST = 6;
 // Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside.
 constexpr int QUARTER_COST = 5, STEP_COST = 7;
 
-// By one wave.  WEIGHTS: every expert has `per` tiles, which cost what it has rows, and the stretches are of equal cost; otherwise a tile
+// By one wave.  An entry is a tile and a range of its reduction.  WEIGHTS: every expert has `per` entries, which cost what it has rows, and the stretches are of equal cost; otherwise a tile
 // costs the same everywhere.
 template <bool WEIGHTS, int BM> static __device__ inline void make_list(const GroupedArgs& g, int per, TileList* l) {
     const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
@@ -233,9 +239,11 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
 }
 
 template <bool WEIGHTS, int BN>
-static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileList& l, int height, int mt, int nt, int t) {
+static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileList& l, int splits, int height, int mt, int nt, int t) {
     GroupedTile out;
     int e, m, n, r;
+    out.split = t % splits;
+    t = __builtin_amdgcn_readfirstlane(t / splits);
     if (WEIGHTS) {
         e = __builtin_amdgcn_readfirstlane(t / (mt * nt));
         r = t - e * mt * nt;
@@ -431,7 +439,7 @@ static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], void* c, 
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
     constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;
-    constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4;
+    constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4, CUT = BM < 256;  // (where there are few tiles they are small ones)
     constexpr int HALF = BM / 2, GROUP = HALF / WM;  // a wave has GROUP rows of each half of the tile: rows that are missing spare every wave alike
     constexpr int NS = (BM + BN) / 64 / NW;          // loads of scales a wave, every second K step
     static_assert(!MX || NS * 64 * NW == BM + BN, "scale loads");
@@ -442,7 +450,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mt = (g.M + BM - 1) / BM, nt = (g.N + BN - 1) / BN;
-    if (wave == 0) make_list<WEIGHTS, BM>(g, WEIGHTS ? mt * nt : nt, &list);
+    if (wave == 0) make_list<WEIGHTS, BM>(g, (WEIGHTS ? mt * nt : nt) * g.splits, &list);
     block_barrier();
     const int height = WEIGHTS ? BM : __builtin_amdgcn_readfirstlane(list.height);
     int at = __builtin_amdgcn_readfirstlane(list.begin) + (blockIdx.x >> 3);
@@ -453,24 +461,31 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     Loader<LA, HALF, NLA> la[2];
     Loader<LB, BN, NLB> lb;
     GroupedTile lt;
-    int ls = 0, lsteps = 0, lpair = 0;  // its tile, step in it, steps of it; which half of lds_s the last scales went to
-    auto steps_of = [&](const GroupedTile& t) {  // at least two: a step that is not there reads zeros
-        const int red = LA == LAY_K ? g.kbytes / (MX ? 1 : 2) : t.n;
-        return max(2, (red + (MX ? 127 : 63)) / (MX ? 128 : 64));
-    };
+    int ls = 0, lsteps = 0, lfrom = 0, lpair = 0;  // its tile, step in it, steps of it, step of the reduction it begins with; which half
+                                                   // of lds_s the last scales went to
     auto start = [&](const GroupedTile& t) {
         const int mrows = WEIGHTS ? g.M - t.m0 : min(t.n - t.m0, height), ncols = g.N - t.n0;
         const char* wb = g.b + t.e * g.b_expert;
+        // steps [from, to) of the reduction; at least two are gone through, those that are not there read zeros
+        const int red = WEIGHTS ? t.n * 2 : g.kbytes, all = (red + 127) / 128;  // (bytes, as if its values were contiguous)
+        const int from = CUT ? (int)((int64_t)all * t.split / g.splits) : 0, to = CUT ? (int)((int64_t)all * (t.split + 1) / g.splits) : all;
+        const int kb = CUT ? min(red, to * 128) : red;
         repeat<2>([&](auto u) {
             constexpr int R = u.value * HALF;
-            if constexpr (LA == LAY_K) la[u.value].init(g.a + (int64_t)(t.lo + t.m0 + R) * g.lda, g.lda, mrows - R, g.kbytes, wave);
-            else la[u.value].init(g.a + (int64_t)t.lo * g.lda + (int64_t)(t.m0 + R) * 2, g.lda, mrows - R, t.n, wave);
+            if constexpr (LA == LAY_K) la[u.value].init(g.a + (int64_t)(t.lo + t.m0 + R) * g.lda, g.lda, mrows - R, kb, wave);
+            else la[u.value].init(g.a + (int64_t)t.lo * g.lda + (int64_t)(t.m0 + R) * 2, g.lda, mrows - R, kb / 2, wave);
         });
-        if constexpr (LB == LAY_K) lb.init(wb + (int64_t)t.n0 * g.ldb, g.ldb, ncols, g.kbytes, wave);
-        else lb.init(WEIGHTS ? g.b + (int64_t)t.lo * g.ldb + (int64_t)t.n0 * 2 : wb + (int64_t)t.n0 * 2, g.ldb, ncols, WEIGHTS ? t.n : g.kbytes / 2, wave);
+        if constexpr (LB == LAY_K) lb.init(wb + (int64_t)t.n0 * g.ldb, g.ldb, ncols, kb, wave);
+        else lb.init(WEIGHTS ? g.b + (int64_t)t.lo * g.ldb + (int64_t)t.n0 * 2 : wb + (int64_t)t.n0 * 2, g.ldb, ncols, kb / 2, wave);
+        if constexpr (CUT) {
+            la[0].next(from);
+            la[1].next(from);
+            lb.next(from);
+        }
         lt = t;
         ls = 0;
-        lsteps = steps_of(t);
+        if constexpr (CUT) lfrom = from;
+        lsteps = max(2, to - from);
     };
     // The loads of a stage in two parts, 0: upper rows, columns and scales; 1: lower rows.  begin(part), load_scales(), load(part, slot, 0 ..),
     // end(part).
@@ -492,7 +507,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
                 const bool of_b = rows64 * 64 >= BM;
                 const int row = rows64 * 64 - (of_b ? BM : 0), have = min((of_b ? ncols : mrows) - row, 64);
                 const uint8_t* p = of_b ? g.sb + ((int64_t)lt.e * g.N + lt.n0 + row) * g.scale_ld : g.sa + (int64_t)(lt.lo + lt.m0 + row) * g.scale_ld;
-                const u32x4_t d = make_desc((const char*)p + ls * 8, have > 0 && ls * 8 < g.scale_ld ? (have - 1) * g.scale_ld + 16 : 0);
+                const u32x4_t d = make_desc((const char*)p + (lfrom + ls) * 8, have > 0 && (lfrom + ls) * 8 < g.scale_ld ? (have - 1) * g.scale_ld + 16 : 0);
                 load_to_lds(lds_addr(lds_s) + lpair * (BM + BN) * 16 + rows64 * 1024, (threadIdx.x & 63) * g.scale_ld, d);
             });
         }
@@ -589,7 +604,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         }
     };
 
-    start(find_tile<WEIGHTS, BN>(g, list, WEIGHTS ? BM : height, mt, nt, at));
+    start(find_tile<WEIGHTS, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
     repeat<2>([&](auto s) {
         repeat<2>([&](auto part) {
             begin(part);
@@ -617,7 +632,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
             if (left == 2) {                // from here on the loads are the next tile's
                 at += gridDim.x >> 3;
                 if (at < last) {
-                    start(find_tile<WEIGHTS, BN>(g, list, WEIGHTS ? BM : height, mt, nt, at));
+                    start(find_tile<WEIGHTS, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
                 } else {
                     la[0].stop();
                     la[1].stop();
@@ -631,10 +646,24 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         const int m = t.m0 + wm * GROUP, n = t.n0 + wn * FN * 16;
         const int64_t row = WEIGHTS ? (int64_t)t.e * g.M + m : (int64_t)t.lo + m;
         constexpr int esize = OUT == OUT_BF16 ? 2 : 4;
-        if (!(OUT == OUT_F32_ADD && t.n == 0))
+        if (CUT && g.splits > 1) store_tile<OUT_F32, 2 * FH, FN, HALF>(acc, g.part + t.split * g.slab + row * g.N + n, g.N, mrows - wm * GROUP, g.N - n);
+        else if (!(OUT == OUT_F32_ADD && t.n == 0))
             store_tile<OUT, 2 * FH, FN, HALF>(acc, (char*)g.c + (row * g.ldc + n) * esize, g.ldc, mrows - wm * GROUP, g.N - n);
         if (at >= last) break;
         clear();
     }
     wait_loads<0>();  // nothing may arrive in LDS after the workgroup has left it
 }
+
+// One workgroup a compute unit (two where two fit), in eights so that every XCD has as many.
+template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN> static inline hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
+    constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
+    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN><<<blocks, WM * WN * 64, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+// The kernels' units: a product of g on tiles of bm rows.
+hipError_t grouped_launch_row_major(const GroupedArgs& g, int bm, hipStream_t st);
+hipError_t grouped_launch_transposed(const GroupedArgs& g, int bm, hipStream_t st);
+hipError_t grouped_launch_mx(const GroupedArgs& g, int bm, hipStream_t st);
+hipError_t grouped_launch_weights(const GroupedArgs& g, int out, int bm, hipStream_t st);

@@ -1,32 +1,88 @@
 // Launches of the matrix products grouped by expert.
-#include "moe_grouped_stream.h"
+#include "moe_grouped_pick.h"
+#include "moe_grouped.h"
 #include "moe_ops.h"
 
 namespace {
 
-// One workgroup a compute unit (two where two fit), in eights so that every XCD has as many.
-template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN> hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
-    constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
-    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN><<<blocks, WM * WN * 64, 0, st>>>(g);
+// Partial sums of the ranges of a reduction, added in their order: the rows that belong to an expert ...
+__global__ __launch_bounds__(256) void sum_rows_kernel(GroupedArgs g) {
+    const int per = g.N / 8;  // lanes a row
+    for (int e = blockIdx.y; e < g.E; e += gridDim.y) {
+        int lo, n;
+        expert_rows(g.offsets, e, g.rows_cap, &lo, &n);
+        const int64_t total = (int64_t)n * per;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+            const int64_t row = lo + i / per;
+            const int col = (int)(i % per) * 8;
+            const float* from = g.part + row * g.N + col;
+            f32x4_t u = *(const f32x4_t*)from, v = *(const f32x4_t*)(from + 4);
+            for (int s = 1; s < g.splits; ++s) {
+                u += *(const f32x4_t*)(from + s * g.slab);
+                v += *(const f32x4_t*)(from + s * g.slab + 4);
+            }
+            *(u32x4_t*)((uint16_t*)g.c + row * g.ldc + col) = u32x4_t{pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        }
+    }
+}
+
+// ... and the weights (accumulated: of the experts that have rows).
+template <int OUT> __global__ __launch_bounds__(256) void sum_weights_kernel(GroupedArgs g) {
+    const int64_t per = (int64_t)g.M * g.N / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per * g.E; i += (int64_t)gridDim.x * 256) {
+        if (OUT == OUT_F32_ADD) {
+            int lo, n;
+            expert_rows(g.offsets, (int)(i / per), g.rows_cap, &lo, &n);
+            if (n == 0) continue;
+        }
+        const float* from = g.part + i * 8;
+        f32x4_t u = *(const f32x4_t*)from, v = *(const f32x4_t*)(from + 4);
+        for (int s = 1; s < g.splits; ++s) {
+            u += *(const f32x4_t*)(from + s * g.slab);
+            v += *(const f32x4_t*)(from + s * g.slab + 4);
+        }
+        if (OUT == OUT_BF16) {
+            ((u32x4_t*)g.c)[i] = u32x4_t{pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        } else {
+            f32x4_t* to = (f32x4_t*)g.c + 2 * i;
+            to[0] = OUT == OUT_F32_ADD ? to[0] + u : u;
+            to[1] = OUT == OUT_F32_ADD ? to[1] + v : v;
+        }
+    }
+}
+
+int blocks_of(int64_t lanes) {
+    const int64_t want = ceil_div(lanes, 256);
+    return (int)(want < 2048 ? want : 2048);
+}
+
+// A plan carried out: the product, and the sum of its ranges if its reduction was cut.
+template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, void* ws, hipStream_t st, L launch) {
+    const GroupedPlan p = grouped_rows_plan(g.rows_cap, g.E, g.kbytes, g.N, row_major);
+    g.splits = p.splits;
+    g.slab = (int64_t)g.rows_cap * g.N;
+    g.part = (float*)ws;
+    const hipError_t e = launch(g, p.bm, st);
+    if (e != hipSuccess || g.splits == 1) return e;
+    const int experts = g.rows_cap < g.E ? g.rows_cap : g.E;
+    sum_rows_kernel<<<dim3(blocks_of(ceil_div(g.rows_cap, experts) * (g.N / 8)), g.E), 256, 0, st>>>(g);
     return hipGetLastError();
-}
-
-// 256 x 256 tiles where there are enough of them for every compute unit, 128 x 128 ones otherwise.
-bool large_tiles(const GroupedArgs& g, bool weights) {
-    const int64_t nt = (g.N + 255) / 256;
-    if (weights) return g.E * ((g.M + 255) / 256) * nt >= 256;
-    return g.rows_cap / g.E >= 192 && g.rows_cap / 256 * nt >= 256;
-}
-
-template <int OUT> hipError_t launch_weights(const GroupedArgs& g, hipStream_t st) {
-    if (large_tiles(g, true)) return launch_tiles<FMT_BF16, LAY_MN, LAY_MN, OUT, 256, 256, 2, 4>(g, st);
-    return launch_tiles<FMT_BF16, LAY_MN, LAY_MN, OUT, 128, 128, 2, 2>(g, st);
 }
 
 }  // namespace
 
+size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major) {
+    const GroupedPlan p = grouped_rows_plan(rows_cap, E, kbytes, N, row_major);
+    return p.splits > 1 ? (size_t)p.splits * rows_cap * N * 4 : 0;
+}
+
+size_t grouped_weights_workspace(int rows_cap, int E, int K, int N) {
+    const GroupedPlan p = grouped_weights_plan(rows_cap, E, K, N);
+    return p.splits > 1 ? (size_t)p.splits * E * K * N * 4 : 0;
+}
+
 hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool transpose_w, const int32_t* offsets, int rows_cap, int E,
-                               int K, int N, void* y, int64_t ldy, hipStream_t st) {
+                               int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st) {
     GroupedArgs g = {};
     g.a = (const char*)x;
     g.b = (const char*)w;
@@ -40,17 +96,31 @@ hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool t
     g.rows_cap = rows_cap;
     g.N = N;
     g.kbytes = K * 2;
-    if (few_rows(rows_cap, E)) return transpose_w ? launch_stream<FMT_BF16, LAY_K>(g, st) : launch_stream<FMT_BF16, LAY_MN>(g, st);
-    const bool large = large_tiles(g, false);
-    if (transpose_w)
-        return large ? launch_tiles<FMT_BF16, LAY_K, LAY_K, OUT_BF16, 256, 256, 2, 4>(g, st)
-                     : launch_tiles<FMT_BF16, LAY_K, LAY_K, OUT_BF16, 128, 128, 2, 2>(g, st);
-    return large ? launch_tiles<FMT_BF16, LAY_K, LAY_MN, OUT_BF16, 256, 256, 2, 4>(g, st)
-                 : launch_tiles<FMT_BF16, LAY_K, LAY_MN, OUT_BF16, 128, 128, 2, 2>(g, st);
+    return run_rows(g, !transpose_w, ws, st, transpose_w ? grouped_launch_transposed : grouped_launch_row_major);
+}
+
+hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, const void* wsc, const int32_t* offsets, int rows_cap, int E,
+                             int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st) {
+    GroupedArgs g = {};
+    g.a = (const char*)xq;
+    g.b = (const char*)wq;
+    g.sa = (const uint8_t*)xs;
+    g.sb = (const uint8_t*)wsc;
+    g.c = y;
+    g.offsets = offsets;
+    g.lda = g.ldb = K / 2;
+    g.ldc = ldy;
+    g.b_expert = (int64_t)K / 2 * N;
+    g.E = E;
+    g.rows_cap = rows_cap;
+    g.N = N;
+    g.kbytes = K / 2;
+    g.scale_ld = mx_scale_cols(K);
+    return run_rows(g, false, ws, st, grouped_launch_mx);
 }
 
 hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int rows_cap, int E,
-                                int K, int N, void* dw, bool f32, bool add, hipStream_t st) {
+                                int K, int N, void* dw, bool f32, bool add, void* ws, hipStream_t st) {
     GroupedArgs g = {};
     g.a = (const char*)x;
     g.b = (const char*)dy;
@@ -63,6 +133,14 @@ hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int6
     g.rows_cap = rows_cap;
     g.M = K;
     g.N = N;
-    if (add) return launch_weights<OUT_F32_ADD>(g, st);
-    return f32 ? launch_weights<OUT_F32>(g, st) : launch_weights<OUT_BF16>(g, st);
+    const GroupedPlan p = grouped_weights_plan(rows_cap, E, K, N);
+    g.splits = p.splits;
+    g.slab = (int64_t)E * K * N;
+    g.part = (float*)ws;
+    const int out = add ? OUT_F32_ADD : f32 ? OUT_F32 : OUT_BF16;
+    const hipError_t e = grouped_launch_weights(g, out, p.bm, st);
+    if (e != hipSuccess || g.splits == 1) return e;
+    auto kernel = add ? sum_weights_kernel<OUT_F32_ADD> : f32 ? sum_weights_kernel<OUT_F32> : sum_weights_kernel<OUT_BF16>;
+    kernel<<<blocks_of((int64_t)E * K * N / 8), 256, 0, st>>>(g);
+    return hipGetLastError();
 }

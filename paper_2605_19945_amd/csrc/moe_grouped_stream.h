@@ -21,13 +21,15 @@ template <int FMT, int LB, int BM, int RING> __global__ __launch_bounds__(256) v
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
     RowTiles<BM> tiles;
-    tiles.init(g, (g.N + BN - 1) / BN);
+    tiles.init(g, (g.N + BN - 1) / BN, g.splits);
     int at = tiles.begin + (blockIdx.x >> 3);
     if (at >= tiles.end) return;
 
-    // this wave's stages of a tile (4-bit ones in pairs that share a load of scales); as many for every wave, and enough that the
-    // loads are never two tiles ahead: the last ones may read zeros
-    const int mine = max((g.kbytes + SPAN * PER * NW - 1) / (SPAN * PER * NW), (RING + PER - 1) / PER) * PER;
+    // Turns of the waves (a stage each, 4-bit ones a pair that shares a load of scales), cut into the ranges of the reduction.  As many
+    // stages for every wave and range, and enough that the loads are never two tiles ahead: the last ones may read zeros.
+    constexpr int TURN = SPAN * PER * NW;
+    const int turns = (g.kbytes + TURN - 1) / TURN;
+    const int mine = max((turns + g.splits - 1) / g.splits, (RING + PER - 1) / PER) * PER;
     char* ring = lds + wave * WAVE;
     char* scales = ring + RING * (XB + WB);
 
@@ -35,15 +37,18 @@ template <int FMT, int LB, int BM, int RING> __global__ __launch_bounds__(256) v
     Loader<LAY_K, BM, NLX, SPAN> lx;
     Loader<LB, BN, NLW, SPAN> lw;
     GroupedTile lt;
-    int ls = 0, place = 0, half = 0;  // its stage in the tile, its place in the ring, which half of the scales comes next
+    int ls = 0, lfrom = 0;            // its stage in the tile, the turn that begins with
+    int place = 0, half = 0;          // its place in the ring, which half of the scales comes next
     auto start = [&]() {
-        lt = tiles.find(at, BN);
-        lx.init(g.a + (int64_t)(lt.lo + lt.m0) * g.lda, g.lda, lt.n - lt.m0, g.kbytes, 0);
+        lt = tiles.find(at, BN, g.splits);
+        lfrom = turns * lt.split / g.splits;
+        const int kb = min(g.kbytes, turns * (lt.split + 1) / g.splits * TURN);
+        lx.init(g.a + (int64_t)(lt.lo + lt.m0) * g.lda, g.lda, lt.n - lt.m0, kb, 0);
         const char* wb = g.b + lt.e * g.b_expert;
-        if constexpr (LB == LAY_K) lw.init(wb + (int64_t)lt.n0 * g.ldb, g.ldb, g.N - lt.n0, g.kbytes, 0);
-        else lw.init(wb + (int64_t)lt.n0 * 2, g.ldb, g.N - lt.n0, g.kbytes / 2, 0);
-        lx.next(wave * PER);
-        lw.next(wave * PER);
+        if constexpr (LB == LAY_K) lw.init(wb + (int64_t)lt.n0 * g.ldb, g.ldb, g.N - lt.n0, kb, 0);
+        else lw.init(wb + (int64_t)lt.n0 * 2, g.ldb, g.N - lt.n0, kb / 2, 0);
+        lx.next((lfrom * NW + wave) * PER);
+        lw.next((lfrom * NW + wave) * PER);
         ls = 0;
     };
     auto issue = [&]() {
@@ -63,7 +68,7 @@ template <int FMT, int LB, int BM, int RING> __global__ __launch_bounds__(256) v
         const uint32_t to = lds_addr(ring) + place * (XB + WB);
         if constexpr (MX) {
             if ((ls & 1) == 0) {
-                const int k = ((ls >> 1) * NW + wave) * 16, left = ls >= 0 ? g.scale_ld - k : 0;
+                const int k = ((lfrom + (ls >> 1)) * NW + wave) * 16, left = ls >= 0 ? g.scale_ld - k : 0;
                 const uint8_t* px = g.sa + (int64_t)(lt.lo + lt.m0) * g.scale_ld + k;
                 const uint8_t* pw = g.sb + ((int64_t)lt.e * g.N + lt.n0) * g.scale_ld + k;
                 const uint32_t there = lds_addr(scales) + half * (BM + BN) * 16;
@@ -156,6 +161,12 @@ template <int FMT, int LB, int BM, int RING> __global__ __launch_bounds__(256) v
                 u += *(const f32x4_t*)(parts[w] + row * BN + ((2 * c) ^ (row & 7)) * 4);
                 v += *(const f32x4_t*)(parts[w] + row * BN + ((2 * c + 1) ^ (row & 7)) * 4);
             }
+            if (g.splits > 1) {
+                f32x4_t* to = (f32x4_t*)(g.part + t.split * g.slab + (int64_t)(t.lo + t.m0 + row) * g.N + t.n0 + c * 8);
+                to[0] = u;
+                to[1] = v;
+                continue;
+            }
             const u32x4_t o = {pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
             *(u32x4_t*)((uint16_t*)g.c + (int64_t)(t.lo + t.m0 + row) * g.ldc + t.n0 + c * 8) = o;
         }
@@ -165,12 +176,11 @@ template <int FMT, int LB, int BM, int RING> __global__ __launch_bounds__(256) v
     wait_loads<0>();  // nothing may arrive in LDS after the workgroup has left it
 }
 
-template <int FMT, int LB> static inline hipError_t launch_stream(const GroupedArgs& g, hipStream_t st) {
-    const int experts = g.rows_cap < g.E ? g.rows_cap : g.E;
-    if (g.rows_cap <= 8 * experts) grouped_stream_kernel<FMT, LB, 16, 3><<<256, 256, 0, st>>>(g);
-    else grouped_stream_kernel<FMT, LB, 32, 2><<<256, 256, 0, st>>>(g);
+// A product over ragged rows on the kernel with tiles of bm rows.
+template <int FMT, int LB> static inline hipError_t launch_rows(const GroupedArgs& g, int bm, hipStream_t st) {
+    if (bm == 16) grouped_stream_kernel<FMT, LB, 16, 3><<<256, 256, 0, st>>>(g);
+    else if (bm == 32) grouped_stream_kernel<FMT, LB, 32, 2><<<256, 256, 0, st>>>(g);
+    else if (bm == 128) return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 128, 128, 2, 2>(g, st);
+    else return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 256, 256, 2, 4>(g, st);
     return hipGetLastError();
 }
-
-// Where the weights bound the product: up to 32 rows for every expert that can have any.
-static inline bool few_rows(int rows_cap, int E) { return rows_cap <= 32 * (rows_cap < E ? rows_cap : E); }

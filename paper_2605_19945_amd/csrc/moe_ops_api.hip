@@ -30,6 +30,17 @@ moe_status check_grouped(const int32_t* offsets, int32_t rows, int32_t E, int32_
     return MOE_OK;
 }
 
+// a workspace of at least `need` bytes
+moe_status check_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (need == 0) return MOE_OK;
+    if (bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    return workspace == nullptr || !aligned(workspace, 16) ? MOE_ERR_INVALID_ARG : MOE_OK;
+}
+
+bool grouped_shape_ok(int32_t rows, int32_t E, int32_t K, int32_t N, int unit) {
+    return rows >= 0 && rows <= kMaxRows && E >= 1 && E <= kMaxExperts && !bad_width(K, unit) && !bad_width(N, 8);
+}
+
 moe_status check_list(const void* const* grads, void* const* outs, bool with_outs, const int64_t* counts, const int32_t* types, int32_t n,
                       const void* workspace, size_t workspace_bytes, const float* norm) {
     if (n < 0 || norm == nullptr || !aligned(norm, 4) || workspace == nullptr || !aligned(workspace, 8)) return MOE_ERR_INVALID_ARG;
@@ -48,25 +59,39 @@ moe_status check_list(const void* const* grads, void* const* outs, bool with_out
 
 extern "C" {
 
+size_t moe_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, int32_t transpose_w) {
+    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_rows_workspace(n_rows_cap, E, K * 2, N, transpose_w == 0) : 0;
+}
+
 moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t transpose_w, const int32_t* offsets, int32_t n_rows_cap,
-                            int32_t E, int32_t K, int32_t N, void* y, int64_t ldy, void* stream) {
-    const moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 8);
+                            int32_t E, int32_t K, int32_t N, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 8);
     if (st != MOE_OK) return st;
     if (bad(x, 16, n_rows_cap) || bad(w, 16, 1) || bad(y, 16, n_rows_cap)) return MOE_ERR_INVALID_ARG;
     if (bad_ld(ldx, K, 8) || bad_ld(ldy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
-    return from_hip(launch_grouped_gemm(x, ldx, w, transpose_w != 0, offsets, n_rows_cap, E, K, N, y, ldy, (hipStream_t)stream));
+    st = check_workspace(workspace, workspace_bytes, grouped_rows_workspace(n_rows_cap, E, K * 2, N, transpose_w == 0));
+    if (st != MOE_OK) return st;
+    return from_hip(launch_grouped_gemm(x, ldx, w, transpose_w != 0, offsets, n_rows_cap, E, K, N, y, ldy, workspace, (hipStream_t)stream));
+}
+
+size_t moe_grouped_gemm_wgrad_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N) {
+    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_weights_workspace(n_rows_cap, E, K, N) : 0;
 }
 
 moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int32_t n_rows_cap,
-                                  int32_t E, int32_t K, int32_t N, void* dw, int32_t type, int32_t accumulate, void* stream) {
-    const moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 8);
+                                  int32_t E, int32_t K, int32_t N, void* dw, int32_t type, int32_t accumulate, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+    moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 8);
     if (st != MOE_OK) return st;
     if (bad(x, 16, n_rows_cap) || bad(dy, 16, n_rows_cap) || bad(dw, 16, 1)) return MOE_ERR_INVALID_ARG;
     if (bad_ld(ldx, K, 8) || bad_ld(lddy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (type != MOE_BF16 && type != MOE_F32) return MOE_ERR_INVALID_ARG;
     if (accumulate != 0 && type != MOE_F32) return MOE_ERR_INVALID_ARG;
-    return from_hip(launch_grouped_wgrad(x, ldx, dy, lddy, offsets, n_rows_cap, E, K, N, dw, type == MOE_F32, accumulate != 0, (hipStream_t)stream));
+    st = check_workspace(workspace, workspace_bytes, grouped_weights_workspace(n_rows_cap, E, K, N));
+    if (st != MOE_OK) return st;
+    return from_hip(launch_grouped_wgrad(x, ldx, dy, lddy, offsets, n_rows_cap, E, K, N, dw, type == MOE_F32, accumulate != 0, workspace,
+                                         (hipStream_t)stream));
 }
 
 moe_status moe_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int32_t n_rows_cap, int32_t f, void* h, int64_t ldh,
@@ -135,15 +160,21 @@ moe_status moe_mxfp4_dequantize(const void* values, const void* scales, int64_t 
     return from_hip(launch_mx_dequantize(values, scales, rows, K, x, ldx, (hipStream_t)stream));
 }
 
+size_t moe_mxfp4_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N) {
+    return grouped_shape_ok(n_rows_cap, E, K, N, 32) ? grouped_rows_workspace(n_rows_cap, E, K / 2, N, false) : 0;
+}
+
 moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, const void* w_values, const void* w_scales,
                                   const int32_t* offsets, int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y, int64_t ldy,
-                                  void* stream) {
-    const moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 32);
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+    moe_status st = check_grouped(offsets, n_rows_cap, E, K, N, 32);
     if (st != MOE_OK) return st;
     if (bad(x_values, 16, n_rows_cap) || bad(x_scales, 16, n_rows_cap) || bad(w_values, 16, 1) || bad(w_scales, 16, 1)) return MOE_ERR_INVALID_ARG;
     if (bad(y, 16, n_rows_cap) || bad_ld(ldy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
-    return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, (hipStream_t)stream));
+    st = check_workspace(workspace, workspace_bytes, grouped_rows_workspace(n_rows_cap, E, K / 2, N, false));
+    if (st != MOE_OK) return st;
+    return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -59,6 +59,10 @@ SHAPES = [
     ([2], 4104, 1544),                      # one token, long reduction
     ([40, 9], 2056, 2064),
     ([520, 530], 8, 4096),                  # shortest reduction
+    ([3, 0, 1], 14344, 72),                 # few tiles: the reduction is cut into ranges
+    ([0, 90, 200, 1], 4104, 136),
+    ([16, 15], 1032, 8),
+    ([6000, 5], 40, 136),
 ]
 
 
@@ -81,7 +85,7 @@ def test_grouped_wgrad_whole_numbers_exactly(rows, K, N, dtype):
     assert got.dtype == dtype and torch.equal(got.cpu(), ref_wgrad(x, dy, off).to(dtype))
 
 
-@pytest.mark.parametrize("rows,K,N", [([3, 0, 250], 136, 264), ([700, 900], 320, 2064)])
+@pytest.mark.parametrize("rows,K,N", [([3, 0, 250], 136, 264), ([700, 900], 320, 2064), ([0, 4000, 3000], 72, 40)])
 def test_grouped_wgrad_accumulates_and_leaves_empty_experts_alone(rows, K, N):
     off = offsets_of(rows)
     x, dy = whole((int(off[-1]), K), -2, 2, 5), whole((int(off[-1]), N), -2, 2, 6)
@@ -436,7 +440,8 @@ def test_mxfp4_dequantize_every_code_under_every_scale():
 
 
 MX_SHAPES = [([1], 32, 8), ([0, 3, 0], 96, 40), ([5, 17, 0, 33], 544, 136), ([64, 1, 130], 1056, 264), ([300, 0, 257], 288, 520),
-             ([1200, 0, 900, 801], 320, 6152), ([2] * 256, 64, 72), ([1], 14336, 512), ([9, 40], 4096, 1032)]
+             ([1200, 0, 900, 801], 320, 6152), ([2] * 256, 64, 72), ([1], 14336, 512), ([9, 40], 4096, 1032),
+             ([2, 0, 7], 9248, 40), ([100, 70], 4128, 136)]
 
 
 @pytest.mark.parametrize("rows,K,N", MX_SHAPES)

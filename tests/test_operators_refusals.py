@@ -27,7 +27,7 @@ def call(fn, base, **change):
 
 
 def test_grouped_gemm(lib):
-    base = dict(x=P, ldx=64, w=P, t=0, offsets=P, rows=0, E=2, K=64, N=64, y=P, ldy=64, stream=None)
+    base = dict(x=P, ldx=64, w=P, t=0, offsets=P, rows=0, E=2, K=64, N=64, y=P, ldy=64, ws=None, bytes=0, stream=None)
     assert call(lib.moe_grouped_gemm, base) == 0          # no rows: nothing to do
     for change in (dict(rows=-1), dict(rows=(1 << 24) + 1), dict(E=0), dict(offsets=None), dict(offsets=C.c_void_p(4097)), dict(w=None),
                    dict(w=OFF), dict(x=None, rows=1), dict(x=OFF, rows=1), dict(y=None, rows=1), dict(y=OFF), dict(ldx=56), dict(ldx=68),
@@ -38,12 +38,39 @@ def test_grouped_gemm(lib):
 
 
 def test_grouped_wgrad(lib):
-    base = dict(x=P, ldx=64, dy=P, lddy=64, offsets=P, rows=1, E=2, K=64, N=64, dw=P, type=0, acc=0, stream=None)
+    base = dict(x=P, ldx=64, dy=P, lddy=64, offsets=P, rows=1, E=2, K=64, N=64, dw=P, type=0, acc=0, ws=None, bytes=0, stream=None)
     for change in (dict(rows=-1), dict(E=0), dict(offsets=None), dict(dw=None), dict(dw=OFF), dict(x=None), dict(dy=OFF), dict(ldx=32),
                    dict(lddy=65), dict(type=2), dict(type=0, acc=1)):
         assert call(lib.moe_grouped_gemm_wgrad, base, **change) == INVALID, change
     for change in (dict(E=300), dict(K=12), dict(N=1 << 18)):
         assert call(lib.moe_grouped_gemm_wgrad, base, **change) == SHAPE, change
+
+
+def test_workspaces_of_the_grouped_products(lib):
+    """A long reduction of few tiles is cut and needs a workspace, which is checked; sizes that are none need none."""
+    need = lib.moe_grouped_gemm_workspace_bytes(2, 1, 14336, 128, 0)
+    assert need > 0 and need % (2 * 128 * 4) == 0
+    base = dict(x=P, ldx=14336, w=P, t=0, offsets=P, rows=2, E=1, K=14336, N=128, y=P, ldy=128, ws=P, bytes=need - 1, stream=None)
+    assert call(lib.moe_grouped_gemm, base) == WORKSPACE
+    assert call(lib.moe_grouped_gemm, base, bytes=need, ws=None) == INVALID and call(lib.moe_grouped_gemm, base, bytes=need, ws=OFF) == INVALID
+    need = lib.moe_grouped_gemm_wgrad_workspace_bytes(8192, 1, 64, 64)
+    assert need > 0 and need % (64 * 64 * 4) == 0
+    base = dict(x=P, ldx=64, dy=P, lddy=64, offsets=P, rows=8192, E=1, K=64, N=64, dw=P, type=0, acc=0, ws=P, bytes=need - 1, stream=None)
+    assert call(lib.moe_grouped_gemm_wgrad, base) == WORKSPACE
+    assert call(lib.moe_grouped_gemm_wgrad, base, bytes=need, ws=None) == INVALID
+    need = lib.moe_mxfp4_grouped_gemm_workspace_bytes(2, 1, 14336, 64)
+    assert need > 0
+    base = dict(xq=P, xs=P, wq=P, wsc=P, offsets=P, rows=2, E=1, K=14336, N=64, y=P, ldy=64, ws=P, bytes=need - 1, stream=None)
+    assert call(lib.moe_mxfp4_grouped_gemm, base) == WORKSPACE
+    # enough tiles, or sizes that are refused
+    assert lib.moe_grouped_gemm_workspace_bytes(8192, 8, 4096, 28672, 0) == 0
+    assert lib.moe_grouped_gemm_workspace_bytes(-1, 8, 4096, 28672, 0) == 0 and lib.moe_grouped_gemm_workspace_bytes(2, 1, 14337, 128, 0) == 0
+    assert lib.moe_mxfp4_grouped_gemm_workspace_bytes(2, 1, 48, 64) == 0
+    # never past 64 MiB
+    for rows in (1, 100, 5000, 1 << 20):
+        for E, K, N in ((1, 131072, 8), (256, 131072, 8), (1, 131072, 4096), (8, 14336, 512)):
+            assert lib.moe_grouped_gemm_workspace_bytes(rows, E, K, N, 0) <= 64 << 20
+            assert lib.moe_grouped_gemm_wgrad_workspace_bytes(rows, E, K, N) <= 64 << 20
 
 
 def test_swiglu(lib):
@@ -96,7 +123,7 @@ def test_mxfp4(lib):
     assert call(lib.moe_mxfp4_dequantize, base) == 0
     assert call(lib.moe_mxfp4_dequantize, base, rows=-1) == INVALID and call(lib.moe_mxfp4_dequantize, base, ldx=63) == INVALID
     assert call(lib.moe_mxfp4_dequantize, base, K=16) == SHAPE
-    base = dict(xq=P, xs=P, wq=P, ws=P, offsets=P, rows=0, E=2, K=64, N=64, y=P, ldy=64, stream=None)
+    base = dict(xq=P, xs=P, wq=P, ws=P, offsets=P, rows=0, E=2, K=64, N=64, y=P, ldy=64, space=None, bytes=0, stream=None)
     assert call(lib.moe_mxfp4_grouped_gemm, base) == 0
     for change in (dict(rows=-1), dict(offsets=None), dict(xq=OFF), dict(xs=OFF), dict(wq=None), dict(ws=OFF), dict(y=OFF), dict(ldy=8)):
         assert call(lib.moe_mxfp4_grouped_gemm, base, **change) == INVALID, change
