@@ -473,19 +473,18 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
 
 
 def _grad_list(what, tensors):
-    """Host arrays of the addresses, sizes and types of a list of gradients."""
-    f32, bf16 = torch.float32, torch.bfloat16
+    """Host arrays of the addresses, sizes and types of a list of gradients, and their devices.  (map over the unbound
+    methods: a list of a thousand tensors is bound by this.)"""
+    T, f32 = torch.Tensor, torch.float32
     types = [t.dtype for t in tensors]
-    if not all(t is f32 or t is bf16 for t in types) or not all([t.is_contiguous() for t in tensors]):
+    if not all(map(T.is_contiguous, tensors)) or not {f32, torch.bfloat16}.issuperset(types):
         _refuse(what, "gradients have to be contiguous tensors of float32 or bfloat16")
-    n = len(tensors)
-    return (array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", [t.numel() for t in tensors]),
-            array.array("i", [t is f32 for t in types]))
+    return (array.array("Q", map(T.data_ptr, tensors)), array.array("q", map(T.numel, tensors)),
+            array.array("i", [t is f32 for t in types]), set(map(T.get_device, tensors)))
 
 
-def _norm_of(what, tensors, others, call):
+def _norm_of(what, tensors, devices, call):
     if tensors:
-        devices = {t.get_device() for t in tensors} | {t.get_device() for t in others}
         dev = _launch_device(what, tensors[0])
         if len(devices) > 1:
             _refuse(what, "tensors have to be on one device")
@@ -502,9 +501,9 @@ def moe_grad_norm(grads):
     """Norm over all values of a list of gradients (float32 or bfloat16), as a tensor on the GPU."""
     lib, what = _lib or load_library(), "moe_grad_norm"
     grads = list(grads)
-    ptrs, counts, types = _grad_list(what, grads)
+    ptrs, counts, types, devices = _grad_list(what, grads)
     a = [v.buffer_info()[0] for v in (ptrs, counts, types)]
-    return _norm_of(what, grads, (), lambda ws, n, norm, st: lib.moe_grad_norm(*a, len(grads), ws, n, norm, st))
+    return _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_grad_norm(*a, len(grads), ws, n, norm, st))
 
 
 def moe_clip_grad_norm(grads, max_norm, out=None):
@@ -512,14 +511,15 @@ def moe_clip_grad_norm(grads, max_norm, out=None):
     types and sizes, overlapping nothing).  Returns the norm before, as a tensor on the GPU."""
     lib, what = _lib or load_library(), "moe_clip_grad_norm"
     grads = list(grads)
-    ptrs, counts, types = _grad_list(what, grads)
-    outs, out = ptrs, () if out is None else list(out)
-    if out:
-        outs, n_out, out_types = _grad_list(what, out)
+    ptrs, counts, types, devices = _grad_list(what, grads)
+    outs = ptrs
+    if out is not None:
+        outs, n_out, out_types, others = _grad_list(what, list(out))
+        devices |= others
         if n_out != counts or out_types != types:
             _refuse(what, "out has to hold as many tensors of the same types and sizes")
     a = [v.buffer_info()[0] for v in (ptrs, outs, counts, types)]
-    return _norm_of(what, grads, out, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
+    return _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
 
 
 def _mx_pair(what, t, lead, K):

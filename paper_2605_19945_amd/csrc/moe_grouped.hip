@@ -57,8 +57,8 @@ int blocks_of(int64_t lanes) {
 }
 
 // A plan carried out: the product, and the sum of its ranges if its reduction was cut.
-template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, void* ws, hipStream_t st, L launch) {
-    const GroupedPlan p = grouped_rows_plan(g.rows_cap, g.E, g.kbytes, g.N, row_major);
+template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, bool mx, void* ws, hipStream_t st, L launch) {
+    const GroupedPlan p = grouped_rows_plan(g.rows_cap, g.E, g.kbytes, g.N, row_major, mx);
     g.splits = p.splits;
     g.slab = (int64_t)g.rows_cap * g.N;
     g.part = (float*)ws;
@@ -71,8 +71,8 @@ template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, void* 
 
 }  // namespace
 
-size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major) {
-    const GroupedPlan p = grouped_rows_plan(rows_cap, E, kbytes, N, row_major);
+size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major, bool mx) {
+    const GroupedPlan p = grouped_rows_plan(rows_cap, E, kbytes, N, row_major, mx);
     return p.splits > 1 ? (size_t)p.splits * rows_cap * N * 4 : 0;
 }
 
@@ -96,7 +96,7 @@ hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool t
     g.rows_cap = rows_cap;
     g.N = N;
     g.kbytes = K * 2;
-    return run_rows(g, !transpose_w, ws, st, transpose_w ? grouped_launch_transposed : grouped_launch_row_major);
+    return run_rows(g, !transpose_w, false, ws, st, transpose_w ? grouped_launch_transposed : grouped_launch_row_major);
 }
 
 hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, const void* wsc, const int32_t* offsets, int rows_cap, int E,
@@ -116,7 +116,7 @@ hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, con
     g.N = N;
     g.kbytes = K / 2;
     g.scale_ld = mx_scale_cols(K);
-    return run_rows(g, false, ws, st, grouped_launch_mx);
+    return run_rows(g, false, true, ws, st, grouped_launch_mx);
 }
 
 hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int rows_cap, int E,

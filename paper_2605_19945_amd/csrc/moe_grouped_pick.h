@@ -1,5 +1,6 @@
 // Which kernel a product grouped by expert runs on, and into how many ranges its reduction is cut.  Host only; the number of rows
-// of each expert is on the device, so the rules go by the bound and the mean.
+// of each expert is on the device, so the rules go by the bound on the rows and by their mean.  Times in microseconds, fitted to
+// calls of 1 to 65536 rows on 1 to 128 experts.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -12,44 +13,73 @@ struct GroupedPlan {
 constexpr int GROUPED_MAX_SPLITS = 16;
 constexpr size_t GROUPED_MAX_WORKSPACE = (size_t)64 << 20;
 
-// Ranges so that `tiles` tiles of `steps` steps each give every one of `slots` workgroups work, each range at least `least` steps
-// long.
-static inline int grouped_splits(int64_t tiles, int steps, int slots, int least, int64_t outputs) {
-    int64_t s = tiles > 0 ? slots / tiles : 1;
-    if (s > steps / least) s = steps / least;
-    if (s > GROUPED_MAX_SPLITS) s = GROUPED_MAX_SPLITS;
-    while (s > 1 && (size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE) --s;
-    return s > 1 ? (int)s : 1;
-}
-
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Products over ragged rows.  kbytes: of a row of the reduction; row_major: weights [K, N] (tiles of 128 columns where the weights are
-// streamed, otherwise 64).
-static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, bool row_major) {
+// A kernel: `slots` tiles at a time, a unit of a tile's reduction takes idle (few tiles, latency) to idle + load (all slots taken, memory)
+// microseconds, its end `store`; it reads `rate` bytes a microsecond at the most.
+struct GroupedKernel { int bm, slots; double idle, load, store, rate; };
+
+// The fastest cut of `tiles` tiles of `units` units each: a cut costs a second launch and a way to memory and back for its partial
+// sums (one token's reduction of 14336 over 512 columns: 71 us in one piece, 37, 23, 17, 15 in 2, 4, 8, 16; one of 1024 over 1024
+// columns 9, in two pieces 12).  Returns its time.
+static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t units, int64_t outputs, double bytes, int most, int* splits) {
+    double best = 0;
+    *splits = 1;
+    for (int s = 1; s <= most && s <= units; ++s) {
+        if (s > 1 && (size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE) break;
+        const double rounds = (double)(tiles * s) / k.slots, fill = rounds < 1 ? rounds : 1;
+        double t = (rounds < 1 ? 1 : rounds) * ((double)ceil_div(units, s) * (k.idle + k.load * fill) + k.store);
+        if (t < bytes / k.rate) t = bytes / k.rate;
+        if (s > 1) t += 4.0 + 2e-6 * s * (double)outputs;
+        if (s > 1 && t < 6.5) t = 6.5;  // (the host's second launch)
+        if (s == 1 || t < best) {
+            best = t;
+            *splits = s;
+        }
+    }
+    return best;
+}
+
+// Products over ragged rows.  kbytes: of a row of the reduction; row_major: bf16 weights [K, N] (tiles of 128 columns where the weights
+// are streamed, otherwise 64); mx: 4-bit operands.  An expert has one row tile at least, and half a one is lost on average.
+// Measured, 8 experts, 4096 to 14336, us on row tiles of 16 / 32 / 128 / 256: 8 rows an expert 162 / 163 / 180 / 174, 16 230 / 169 / 185 / 175,
+// 32 354 / 258 / 196 / 177, 128 989 / 649 / 282 / 200; 4-bit 41 / 42 / 45 / 50, 53 / 45 / 46 / 50, 86 / 70 / 47 / 51, 242 / 172 / 76 / 65;
+// 8 experts, 1024 to 1024, 256 rows an expert: - / - / 19 / 20.
+static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, bool row_major, bool mx) {
     GroupedPlan p = {128, 1};
     if (rows <= 0) return p;
     const int experts = rows < E ? rows : E;
-    const int64_t outputs = (int64_t)rows * N;
-    if (rows <= 32 * experts) {  // the weights bound it
-        p.bm = rows <= 8 * experts ? 16 : 32;
-        const int64_t tiles = ceil_div(N, row_major ? 128 : 64) * experts;
-        p.splits = grouped_splits(tiles, (int)ceil_div(kbytes, row_major ? 256 : 512), 256, 4, outputs);
-        return p;
+    const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.0, 5.9e6}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.2, 5.9e6},
+                                      {128, 512, 0.8, 0.4, 2.0, 5.2e6}, {256, 256, 0.9, 0.55, 4.0, 5.2e6}};
+    const double bytes = (double)experts * kbytes * N + (double)rows * (kbytes + 2.0 * N);
+    double best = 0;
+    for (int i = 0; i < 4; ++i) {
+        const GroupedKernel& k = kernels[i];
+        if (i == 2 && !mx && rows <= 16 * experts) break;  // (a token on 4 experts, 3448 to 1440: streamed in ranges 14, on tiles in ranges 20)
+        int64_t row_tiles = rows / k.bm + experts / 2;
+        if (row_tiles < experts) row_tiles = experts;
+        const bool stream = k.bm < 128;
+        const int64_t tiles = row_tiles * ceil_div(N, stream ? (row_major ? 128 : 64) : k.bm);
+        const int64_t units = ceil_div(kbytes, stream ? (mx ? 1024 : row_major ? 256 : 512) : 128);
+        int splits;
+        const double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, &splits);
+        if (i == 0 || t < best) {
+            best = t;
+            p = {k.bm, splits};
+        }
     }
-    // half a row tile an expert is lost on average
-    const int64_t t256 = ceil_div(N, 256) * (rows / 256 + ceil_div(experts, 2)), t128 = ceil_div(N, 128) * (rows / 128 + ceil_div(experts, 2));
-    if (rows / experts >= 192 && t256 >= 256) p.bm = 256;
-    else p.splits = grouped_splits(t128, (int)ceil_div(kbytes, 128), 512, 8, outputs);
     return p;
 }
 
-// Weight gradients [E, M, N] from `rows` rows.
+// Weight gradients [E, M, N] from `rows` rows: a K step of a 256 x 256 tile takes 1.5 us and its stores 7.5, of two 128 x 128 ones at a
+// time 1 and 4 (8 experts, 1024 x 1024: 2048 rows 21 and 17 us, 8192 40 and 32; 4096 x 2048 from 4096 rows 98 and 107; 128 experts,
+// 3328 x 160 from 29 rows 58 and 71).
 static inline GroupedPlan grouped_weights_plan(int rows, int E, int M, int N) {
     GroupedPlan p = {128, 1};
     const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256) * E, t128 = ceil_div(M, 128) * ceil_div(N, 128) * E;
     const int experts = rows < E ? rows : E;
-    if (t256 >= 256) p.bm = 256;
-    else if (experts > 0) p.splits = grouped_splits(t128, (int)ceil_div(rows / experts, 64), 512, 8, (int64_t)E * M * N);
+    const int64_t steps = experts > 0 ? ceil_div(ceil_div(rows, experts), 64) : 1;
+    const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, &p.splits);
+    if ((t256 < 256 ? 1.0 : (double)t256 / 256) * ((double)steps * 1.5 + 7.5) < t + 1.0) p = {256, 1};
     return p;
 }

@@ -3,7 +3,7 @@
 #include "moe_internal.h"
 
 // Matrix products grouped by expert; ws: the workspace that the size functions ask for (0 bytes: may be null).  kbytes: of a row of x.
-size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major);
+size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major, bool mx);
 size_t grouped_weights_workspace(int rows_cap, int E, int K, int N);
 hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool transpose_w, const int32_t* offsets, int rows_cap, int E,
                                int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st);
