@@ -75,11 +75,12 @@ struct GroupedTile {
     int e, lo, n;  // expert, its first row, its rows
     int m0, n0;    // first row (column of x in the weight gradient) and first column of the tile
     int split;     // range of the reduction
+    int rows;      // rows (columns of x) of the tile that exist
 };
 
 // Inside one expert's mt x nt tiles: bands of up to BAND row tiles, row tiles fastest, so that the 32 compute units of an XCD work
-// on neighbouring tiles and share their panels in its L2: about 8 x 4 of them, in the gradient of the weights 6 x 5 (128 experts, 2048 x
-// 1536 from 65528 rows 723 -> 675 us, 32 experts, 2048 x 7168 from 5003 rows 415 -> 322; row products the same within 1 %).
+// on neighbouring tiles and share their panels in its L2: about 8 x 4 of them, in the gradient of the weights 5 x 6 (128 experts, 2048 x
+// 1536 from 65528 rows 723 -> 662 us, 32 experts, 2048 x 7168 from 5003 rows 415 -> 319; row products the same within 1 %).
 template <int BAND> static __device__ inline void place_in_band(int t, int mt, int nt, int* m, int* n) {
     const int band = t / (BAND * nt), r = t - band * BAND * nt;
     const int h = min(BAND, mt - BAND * band);
@@ -156,7 +157,7 @@ struct TileList {
 };
 
 // Cost of a tile of a weight gradient beside its K steps, in K steps: its stores.
-constexpr int TILE_COST = 6;
+constexpr int TILE_COST = 5;
 // Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside.
 constexpr int QUARTER_COST = 5, STEP_COST = 7;
 
@@ -239,7 +240,7 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
     }
 }
 
-template <bool WEIGHTS, int BN>
+template <bool WEIGHTS, int BM, int BN>
 static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileList& l, int splits, int height, int mt, int nt, int t) {
     GroupedTile out;
     int e, m, n, r;
@@ -259,11 +260,20 @@ static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileL
     }
     r = __builtin_amdgcn_readfirstlane(r);
     mt = __builtin_amdgcn_readfirstlane(mt);
-    place_in_band<WEIGHTS ? 6 : 8>(r, mt, nt, &m, &n);
+    place_in_band<WEIGHTS ? 5 : 8>(r, mt, nt, &m, &n);
     out.e = e;
     out.lo = __builtin_amdgcn_readfirstlane(l.lo[e]);
     out.n = __builtin_amdgcn_readfirstlane(l.n[e]);
-    out.m0 = __builtin_amdgcn_readfirstlane(m) * height;
+    m = __builtin_amdgcn_readfirstlane(m);
+    if (WEIGHTS) {
+        out.m0 = m * height;
+        out.rows = min(g.M - out.m0, height);
+    } else {  // the expert's rows are cut evenly, in quarters of the tallest tile: neighbours that share a panel stay side by side
+        const int q = (out.n + BM / 4 - 1) / (BM / 4);
+        const int from = __builtin_amdgcn_readfirstlane(m * q / mt), to = __builtin_amdgcn_readfirstlane((m + 1) * q / mt);
+        out.m0 = from * (BM / 4);
+        out.rows = min(out.n, to * (BM / 4)) - out.m0;
+    }
     out.n0 = __builtin_amdgcn_readfirstlane(n) * BN;
     return out;
 }
@@ -514,7 +524,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     int ls = 0, lsteps = 0, lfrom = 0, lpair = 0;  // its tile, step in it, steps of it, step of the reduction it begins with; which half
                                                    // of lds_s the last scales went to
     auto start = [&](const GroupedTile& t) {
-        const int mrows = WEIGHTS ? g.M - t.m0 : min(t.n - t.m0, height), ncols = g.N - t.n0;
+        const int mrows = t.rows, ncols = g.N - t.n0;
         const char* wb = g.b + t.e * g.b_expert;
         // steps [from, to) of the reduction; at least two are gone through, those that are not there read zeros
         const int red = WEIGHTS ? t.n * 2 : g.kbytes, all = (red + 127) / 128;  // (bytes, as if its values were contiguous)
@@ -551,7 +561,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     auto load_scales = [&]() {
         if ((ls & 1) == 0) {
             lpair ^= 1;
-            const int mrows = lt.n - lt.m0, ncols = g.N - lt.n0;
+            const int mrows = lt.rows, ncols = g.N - lt.n0;
             repeat<NS>([&](auto j) {
                 const int rows64 = wave * NS + j.value;  // 64 rows of a, or of b behind them
                 const bool of_b = rows64 * 64 >= BM;
@@ -654,7 +664,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         }
     };
 
-    start(find_tile<WEIGHTS, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
+    start(find_tile<WEIGHTS, BM, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
     repeat<2>([&](auto s) {
         repeat<2>([&](auto part) {
             begin(part);
@@ -674,7 +684,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     repeat<FH>([&](auto f) { fa[0][f.value] = ra.template get<f.value, 0>(lds_a[0][0]); });
     for (;;) {
         const GroupedTile t = lt;
-        const int mrows = WEIGHTS ? g.M - t.m0 : min(t.n - t.m0, height);
+        const int mrows = t.rows;
         live = (mrows > wm * GROUP) + (mrows > HALF + wm * GROUP);
         int left = lsteps;
         for (int kt = 0; left > 0; ++kt, --left) {
@@ -682,7 +692,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
             if (left == 2) {                // from here on the loads are the next tile's
                 at += gridDim.x >> 3;
                 if (at < last) {
-                    start(find_tile<WEIGHTS, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
+                    start(find_tile<WEIGHTS, BM, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
                 } else {
                     la[0].stop();
                     la[1].stop();
