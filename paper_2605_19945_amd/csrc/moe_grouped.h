@@ -159,7 +159,7 @@ struct TileList {
 // Cost of a tile of a weight gradient beside its K steps, in K steps: its stores.
 constexpr int TILE_COST = 5;
 // Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside.
-constexpr int QUARTER_COST = 5, STEP_COST = 7;
+constexpr int QUARTER_COST = 4, STEP_COST = 14;
 
 // By one wave.  An entry is a tile and a range of its reduction.  WEIGHTS: every expert has `per` entries, which cost what it has rows, and the stretches are of equal cost; otherwise a tile
 // costs the same everywhere.
