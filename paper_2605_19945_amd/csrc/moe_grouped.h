@@ -113,7 +113,8 @@ template <int BM> struct RowTiles {
             if (lane >= d) upto += o;
         }
         before += upto;
-        const int64_t total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nt * splits;
+        int64_t total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nt * splits;
+        if (total > 0x7fffffff) total = 0;  // (overlapping experts only: the offsets are none)
         const int xcd = blockIdx.x & 7;
         begin = (int)(total * xcd / 8);
         end = (int)(total * (xcd + 1) / 8);
@@ -211,7 +212,8 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
     }
     const int all = __builtin_amdgcn_readlane(incl, 63);
     int before = incl - sum;
-    const int64_t total = (int64_t)all * per;
+    int64_t total = (int64_t)all * per;
+    if (!WEIGHTS && total > 0x7fffffff) total = 0;  // (overlapping experts only: the offsets are none)
     // the first tile at or behind position `at` of the total cost (of expert e: at = per * before + tile * c)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -269,8 +271,8 @@ static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileL
         out.m0 = m * height;
         out.rows = min(g.M - out.m0, height);
     } else {  // the expert's rows are cut evenly, in quarters of the tallest tile: neighbours that share a panel stay side by side
-        const int q = (out.n + BM / 4 - 1) / (BM / 4);
-        const int from = __builtin_amdgcn_readfirstlane(m * q / mt), to = __builtin_amdgcn_readfirstlane((m + 1) * q / mt);
+        const int q = (out.n + BM / 4 - 1) / (BM / 4), each = q / mt, over = q - each * mt;
+        const int from = __builtin_amdgcn_readfirstlane(m * each + min(m, over)), to = __builtin_amdgcn_readfirstlane((m + 1) * each + min(m + 1, over));
         out.m0 = from * (BM / 4);
         out.rows = min(out.n, to * (BM / 4)) - out.m0;
     }

@@ -1,5 +1,4 @@
 // Launches of the matrix products grouped by expert.
-#include "moe_grouped_pick.h"
 #include "moe_grouped.h"
 #include "moe_ops.h"
 
@@ -57,8 +56,7 @@ int blocks_of(int64_t lanes) {
 }
 
 // A plan carried out: the product, and the sum of its ranges if its reduction was cut.
-template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, bool mx, void* ws, hipStream_t st, L launch) {
-    const GroupedPlan p = grouped_rows_plan(g.rows_cap, g.E, g.kbytes, g.N, row_major, mx);
+template <typename L> hipError_t run_rows(GroupedArgs& g, const GroupedPlan& p, void* ws, hipStream_t st, L launch) {
     g.splits = p.splits;
     g.slab = (int64_t)g.rows_cap * g.N;
     g.part = (float*)ws;
@@ -71,18 +69,8 @@ template <typename L> hipError_t run_rows(GroupedArgs& g, bool row_major, bool m
 
 }  // namespace
 
-size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major, bool mx) {
-    const GroupedPlan p = grouped_rows_plan(rows_cap, E, kbytes, N, row_major, mx);
-    return p.splits > 1 ? (size_t)p.splits * rows_cap * N * 4 : 0;
-}
-
-size_t grouped_weights_workspace(int rows_cap, int E, int K, int N) {
-    const GroupedPlan p = grouped_weights_plan(rows_cap, E, K, N);
-    return p.splits > 1 ? (size_t)p.splits * E * K * N * 4 : 0;
-}
-
 hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool transpose_w, const int32_t* offsets, int rows_cap, int E,
-                               int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st) {
+                               int K, int N, void* y, int64_t ldy, const GroupedPlan& plan, void* ws, hipStream_t st) {
     GroupedArgs g = {};
     g.a = (const char*)x;
     g.b = (const char*)w;
@@ -96,11 +84,11 @@ hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool t
     g.rows_cap = rows_cap;
     g.N = N;
     g.kbytes = K * 2;
-    return run_rows(g, !transpose_w, false, ws, st, transpose_w ? grouped_launch_transposed : grouped_launch_row_major);
+    return run_rows(g, plan, ws, st, transpose_w ? grouped_launch_transposed : grouped_launch_row_major);
 }
 
 hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, const void* wsc, const int32_t* offsets, int rows_cap, int E,
-                             int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st) {
+                             int K, int N, void* y, int64_t ldy, const GroupedPlan& plan, void* ws, hipStream_t st) {
     GroupedArgs g = {};
     g.a = (const char*)xq;
     g.b = (const char*)wq;
@@ -116,11 +104,11 @@ hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, con
     g.N = N;
     g.kbytes = K / 2;
     g.scale_ld = mx_scale_cols(K);
-    return run_rows(g, false, true, ws, st, grouped_launch_mx);
+    return run_rows(g, plan, ws, st, grouped_launch_mx);
 }
 
 hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int rows_cap, int E,
-                                int K, int N, void* dw, bool f32, bool add, void* ws, hipStream_t st) {
+                                int K, int N, void* dw, bool f32, bool add, const GroupedPlan& plan, void* ws, hipStream_t st) {
     GroupedArgs g = {};
     g.a = (const char*)x;
     g.b = (const char*)dy;
@@ -133,12 +121,11 @@ hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int6
     g.rows_cap = rows_cap;
     g.M = K;
     g.N = N;
-    const GroupedPlan p = grouped_weights_plan(rows_cap, E, K, N);
-    g.splits = p.splits;
+    g.splits = plan.splits;
     g.slab = (int64_t)E * K * N;
     g.part = (float*)ws;
     const int out = add ? OUT_F32_ADD : f32 ? OUT_F32 : OUT_BF16;
-    const hipError_t e = grouped_launch_weights(g, out, p.bm, st);
+    const hipError_t e = grouped_launch_weights(g, out, plan.bm, st);
     if (e != hipSuccess || g.splits == 1) return e;
     auto kernel = add ? sum_weights_kernel<OUT_F32_ADD> : f32 ? sum_weights_kernel<OUT_F32> : sum_weights_kernel<OUT_BF16>;
     kernel<<<blocks_of((int64_t)E * K * N / 8), 256, 0, st>>>(g);

@@ -13,11 +13,14 @@ struct GroupedPlan {
 constexpr int GROUPED_MAX_SPLITS = 16;
 constexpr size_t GROUPED_MAX_WORKSPACE = (size_t)64 << 20;
 
-static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // A kernel: `slots` tiles at a time, a unit of a tile's reduction takes idle (few tiles, latency) to idle + load (all slots taken, memory)
 // microseconds, its end `store`; it reads `rate` bytes a microsecond at the most.
 struct GroupedKernel { int bm, slots; double idle, load, store, rate; };
+
+static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Bytes of workspace a plan needs.
+static inline size_t grouped_workspace(const GroupedPlan& p, int64_t outputs) { return p.splits > 1 ? (size_t)p.splits * outputs * 4 : 0; }
 
 // The fastest cut of `tiles` tiles of `units` units each: a cut costs a second launch and a way to memory and back for its partial
 // sums (one token's reduction of 14336 over 512 columns: 71 us in one piece, 37, 23, 17, 15 in 2, 4, 8, 16; one of 1024 over 1024
@@ -26,7 +29,7 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
     double best = 0;
     *splits = 1;
     for (int s = 1; s <= most && s <= units; ++s) {
-        if (s > 1 && (size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE) break;
+        if (s > 1 && ((size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE || tiles * (s - 1) >= 2 * k.slots)) break;
         const double rounds = (double)(tiles * s) / k.slots, fill = rounds < 1 ? rounds : 1;
         double t = (rounds < 1 ? 1 : rounds) * ((double)ceil_div(units, s) * (k.idle + k.load * fill) + k.store);
         if (t < bytes / k.rate) t = bytes / k.rate;

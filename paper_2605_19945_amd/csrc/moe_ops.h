@@ -1,16 +1,15 @@
 // Launchers of the operators around the experts' weights (moe_ops_api.hip checks the arguments).
 #pragma once
+#include "moe_grouped_pick.h"
 #include "moe_internal.h"
 
-// Matrix products grouped by expert; ws: the workspace that the size functions ask for (0 bytes: may be null).  kbytes: of a row of x.
-size_t grouped_rows_workspace(int rows_cap, int E, int kbytes, int N, bool row_major, bool mx);
-size_t grouped_weights_workspace(int rows_cap, int E, int K, int N);
+// Matrix products grouped by expert, as planned; ws: the workspace that the plan needs (none: may be null).
 hipError_t launch_grouped_gemm(const void* x, int64_t ldx, const void* w, bool transpose_w, const int32_t* offsets, int rows_cap, int E,
-                               int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st);
+                               int K, int N, void* y, int64_t ldy, const GroupedPlan& plan, void* ws, hipStream_t st);
 hipError_t launch_grouped_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int rows_cap, int E,
-                                int K, int N, void* dw, bool f32, bool add, void* ws, hipStream_t st);
+                                int K, int N, void* dw, bool f32, bool add, const GroupedPlan& plan, void* ws, hipStream_t st);
 hipError_t launch_grouped_mx(const void* xq, const void* xs, const void* wq, const void* wsc, const int32_t* offsets, int rows_cap, int E,
-                             int K, int N, void* y, int64_t ldy, void* ws, hipStream_t st);
+                             int K, int N, void* y, int64_t ldy, const GroupedPlan& plan, void* ws, hipStream_t st);
 hipError_t launch_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f, void* h, int64_t ldh, hipStream_t st);
 hipError_t launch_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int64_t ldgu, const int32_t* n_rows, int rows, int f,
                                   void* dgu, int64_t lddgu, void* h, int64_t ldh, hipStream_t st);

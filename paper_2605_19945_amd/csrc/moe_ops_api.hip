@@ -60,7 +60,7 @@ moe_status check_list(const void* const* grads, void* const* outs, bool with_out
 extern "C" {
 
 size_t moe_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, int32_t transpose_w) {
-    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_rows_workspace(n_rows_cap, E, K * 2, N, transpose_w == 0, false) : 0;
+    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_workspace(grouped_rows_plan(n_rows_cap, E, K * 2, N, transpose_w == 0, false), (int64_t)n_rows_cap * N) : 0;
 }
 
 moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t transpose_w, const int32_t* offsets, int32_t n_rows_cap,
@@ -70,13 +70,14 @@ moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t t
     if (bad(x, 16, n_rows_cap) || bad(w, 16, 1) || bad(y, 16, n_rows_cap)) return MOE_ERR_INVALID_ARG;
     if (bad_ld(ldx, K, 8) || bad_ld(ldy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
-    st = check_workspace(workspace, workspace_bytes, grouped_rows_workspace(n_rows_cap, E, K * 2, N, transpose_w == 0, false));
+    const GroupedPlan plan = grouped_rows_plan(n_rows_cap, E, K * 2, N, transpose_w == 0, false);
+    st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)n_rows_cap * N));
     if (st != MOE_OK) return st;
-    return from_hip(launch_grouped_gemm(x, ldx, w, transpose_w != 0, offsets, n_rows_cap, E, K, N, y, ldy, workspace, (hipStream_t)stream));
+    return from_hip(launch_grouped_gemm(x, ldx, w, transpose_w != 0, offsets, n_rows_cap, E, K, N, y, ldy, plan, workspace, (hipStream_t)stream));
 }
 
 size_t moe_grouped_gemm_wgrad_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N) {
-    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_weights_workspace(n_rows_cap, E, K, N) : 0;
+    return grouped_shape_ok(n_rows_cap, E, K, N, 8) ? grouped_workspace(grouped_weights_plan(n_rows_cap, E, K, N), (int64_t)E * K * N) : 0;
 }
 
 moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets, int32_t n_rows_cap,
@@ -88,9 +89,10 @@ moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, in
     if (bad_ld(ldx, K, 8) || bad_ld(lddy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (type != MOE_BF16 && type != MOE_F32) return MOE_ERR_INVALID_ARG;
     if (accumulate != 0 && type != MOE_F32) return MOE_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, grouped_weights_workspace(n_rows_cap, E, K, N));
+    const GroupedPlan plan = grouped_weights_plan(n_rows_cap, E, K, N);
+    st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)E * K * N));
     if (st != MOE_OK) return st;
-    return from_hip(launch_grouped_wgrad(x, ldx, dy, lddy, offsets, n_rows_cap, E, K, N, dw, type == MOE_F32, accumulate != 0, workspace,
+    return from_hip(launch_grouped_wgrad(x, ldx, dy, lddy, offsets, n_rows_cap, E, K, N, dw, type == MOE_F32, accumulate != 0, plan, workspace,
                                          (hipStream_t)stream));
 }
 
@@ -161,7 +163,7 @@ moe_status moe_mxfp4_dequantize(const void* values, const void* scales, int64_t 
 }
 
 size_t moe_mxfp4_grouped_gemm_workspace_bytes(int32_t n_rows_cap, int32_t E, int32_t K, int32_t N) {
-    return grouped_shape_ok(n_rows_cap, E, K, N, 32) ? grouped_rows_workspace(n_rows_cap, E, K / 2, N, false, true) : 0;
+    return grouped_shape_ok(n_rows_cap, E, K, N, 32) ? grouped_workspace(grouped_rows_plan(n_rows_cap, E, K / 2, N, false, true), (int64_t)n_rows_cap * N) : 0;
 }
 
 moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, const void* w_values, const void* w_scales,
@@ -172,9 +174,10 @@ moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, co
     if (bad(x_values, 16, n_rows_cap) || bad(x_scales, 16, n_rows_cap) || bad(w_values, 16, 1) || bad(w_scales, 16, 1)) return MOE_ERR_INVALID_ARG;
     if (bad(y, 16, n_rows_cap) || bad_ld(ldy, N, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
-    st = check_workspace(workspace, workspace_bytes, grouped_rows_workspace(n_rows_cap, E, K / 2, N, false, true));
+    const GroupedPlan plan = grouped_rows_plan(n_rows_cap, E, K / 2, N, false, true);
+    st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)n_rows_cap * N));
     if (st != MOE_OK) return st;
-    return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, workspace, (hipStream_t)stream));
+    return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, plan, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"
