@@ -648,7 +648,8 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         };
         if (live > U) {
             repeat<PROD>([&](auto i) {
-                constexpr int m = i.value / FN, n = i.value % FN, M = U * FH + m;
+                // columns there and back: consecutive products share an operand (what does not toggle costs no power, and power bounds the clock)
+                constexpr int m = i.value / FN, n = m & 1 ? FN - 1 - i.value % FN : i.value % FN, M = U * FH + m;
                 acc[M][n] = multiply<FMT, H + 2 * (n & 1), H + 2 * (M & 1)>(fb[H][n], fa[H][m], acc[M][n], sb[n / 2], sa[M / 2]);
                 beside(i);
                 __builtin_amdgcn_sched_barrier(0);
