@@ -14,6 +14,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libmoe_gfx950.so"
 _lib = None
 torch = None  # set by load_library (the mapping search and the argument checks need neither)
+_BF16 = _F32 = _I32T = _U8 = _device = _stream_of = None  # torch's types, current device and raw stream, set with it
 
 FLAG_STAGE_EVENTS = 1
 STAGE_NAMES = ("route", "permute", "gemm1", "gemm2", "combine")
@@ -99,12 +100,14 @@ def exported_symbols():
 
 def load_library():
     """Loads libmoe_gfx950.so from the package directory.  Raises if it has not been built."""
-    global _lib, torch
+    global _lib, torch, _BF16, _F32, _I32T, _U8, _device, _stream_of
     if _lib is not None:
         return _lib
     # PyTorch ships its own HIP runtime; import it first so that the library binds to that one
     # instance instead of bringing a second runtime into the process.
     import torch
+    _BF16, _F32, _I32T, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+    _device, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     path = library_path()
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2605_19945_amd.build` "
@@ -126,7 +129,7 @@ def _ptr(t):
 
 
 def _stream():
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _stream_of(torch.cuda.current_device())
 
 
 class MoEContext:
@@ -302,8 +305,9 @@ def moe_permute_noalloc(x, topk_idx, E, e_lo=0, E_local=-1, xp=None, offsets=Non
 
 
 # ---- operators around the experts' weights (no context) -----------------------------------------------
-# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.  Small calls are bound by
-# this code (a call takes 5 to 6 us, half of it the launch), so the checks are plain comparisons.
+# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.  Small calls are bound by this
+# code, so each one first asks whether all is as it should be, in one expression, and only otherwise goes through the
+# checks one by one, which find what to say or let an unusual layout pass (a product 7.6 -> 6.3 us of host time, SwiGLU 6.6 -> 5.4).
 def _refuse(what, why):
     raise MoEError(1, f"{what}: {why}")
 
@@ -316,8 +320,8 @@ def _launch_device(what, t, *others):
     for o in others:
         if o is not None and o.get_device() != dev:
             _refuse(what, "tensors have to be on one device")
-    if torch._C._cuda_getDevice() != dev:
-        _refuse(what, f"tensors have to be on the current device, cuda:{torch._C._cuda_getDevice()}")
+    if _device() != dev:
+        _refuse(what, f"tensors have to be on the current device, cuda:{_device()}")
     return dev
 
 
@@ -377,32 +381,45 @@ def _workspace(t, name, *sizes):
     n = _workspace_bytes(name, *sizes)
     if n == 0:
         return None, None, 0
-    ws = t.new_empty(n, dtype=torch.uint8)
+    ws = t.new_empty(n, dtype=_U8)
     return ws, ws.data_ptr(), n
+
+
+def _grouped_checked(what, x, K, w, E, offsets, out):
+    """(values between the rows of x, device), or what is wrong."""
+    if w.dim() != 3 or w.dtype is not _BF16 or not w.is_contiguous():
+        _refuse(what, "w has to be a contiguous tensor of bfloat16 with three dimensions")
+    ldx = _rows(what, "x", x, _BF16, K)
+    _groups(what, offsets, E)
+    return ldx, _launch_device(what, x, w, offsets, out)
 
 
 def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
     """y[r] = x[r] @ w[e] (transpose_w: @ w[e].T) for the rows r of every expert e.  x [rows, K] bf16; w [E, K, N]
     (transpose_w: [E, N, K]) bf16; offsets [E + 1] int32.  Rows from offsets[E] on are left as they are."""
     lib, what = _lib or load_library(), "moe_grouped_gemm"
-    if w.dim() != 3 or w.dtype is not torch.bfloat16 or not w.is_contiguous():
-        _refuse(what, "w has to be a contiguous tensor of bfloat16 with three dimensions")
+    if w.dim() != 3 or x.dim() != 2:
+        _grouped_checked(what, x, None, w, -1, offsets, out)
+        _refuse(what, "w has to have three dimensions, x two")
     E, K, N = w.shape
+    t = 0
     if transpose_w:
-        K, N = N, K
-    ldx = _rows(what, "x", x, torch.bfloat16, K)
-    rows = x.shape[0]
-    _groups(what, offsets, E)
-    dev = _launch_device(what, x, w, offsets, out)
+        K, N, t = N, K, 1
+    (rows, width), (ldx, step), dev = x.shape, x.stride(), x.get_device()
+    if not (x.dtype is _BF16 and w.dtype is _BF16 and offsets.dtype is _I32T and width == K and step == 1 and ldx >= K
+            and w.is_contiguous() and offsets.shape == (E + 1,) and offsets.is_contiguous() and dev >= 0 and w.get_device() == dev
+            and offsets.get_device() == dev and _device() == dev):
+        ldx, dev = _grouped_checked(what, x, K, w, E, offsets, out)
     if out is None:
-        out, ldy = x.new_empty((rows, N)), N
+        out, ldy = x.new_empty(rows, N), N
     else:
         ldy = _out_rows(what, "out", out, rows, N)
-    t = 1 if transpose_w else 0
+        _launch_device(what, x, out)
     ws, at, n = _workspace(x, "moe_grouped_gemm_workspace_bytes", rows, E, K, N, t)
     st = lib.moe_grouped_gemm(x.data_ptr(), ldx, w.data_ptr(), t, offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n,
-                              torch._C._cuda_getCurrentRawStream(dev))
-    _done(st, what)
+                              _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return out
 
 
@@ -410,45 +427,51 @@ def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=Fals
     """dw[e] = x[r].T @ dy[r] summed over the rows r of expert e: [E, K, N] of `dtype` (fp32, the default, or bf16).
     accumulate: add to `out` (fp32)."""
     lib, what = _lib or load_library(), "moe_grouped_gemm_wgrad"
-    ldx, lddy = _rows(what, "x", x, torch.bfloat16), _rows(what, "dy", dy, torch.bfloat16)
+    ldx, lddy = _rows(what, "x", x, _BF16), _rows(what, "dy", dy, _BF16)
     rows, K = x.shape
     if dy.shape[0] != rows:
         _refuse(what, "x and dy have to have as many rows")
     E, N = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, dy.shape[1]
     _groups(what, offsets, E)
     if out is not None:
-        if out.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and out.dtype is not dtype):
+        if out.dtype not in (_F32, _BF16) or (dtype is not None and out.dtype is not dtype):
             _refuse(what, "out has to be of dtype, float32 or bfloat16")
         _whole(what, "out", out, out.dtype, (E, K, N))
     elif accumulate:
         _refuse(what, "accumulate needs out")
-    elif dtype not in (None, torch.float32, torch.bfloat16):
+    elif dtype not in (None, _F32, _BF16):
         _refuse(what, "dtype has to be float32 or bfloat16")
     dev = _launch_device(what, x, dy, offsets, out)
     if out is None:
-        out = x.new_empty((max(E, 0), K, N), dtype=dtype or torch.float32)
+        out = x.new_empty((max(E, 0), K, N), dtype=dtype or _F32)
     ws, at, n = _workspace(x, "moe_grouped_gemm_wgrad_workspace_bytes", rows, E, K, N)
     st = lib.moe_grouped_gemm_wgrad(x.data_ptr(), ldx, dy.data_ptr(), lddy, offsets.data_ptr(), rows, E, K, N, out.data_ptr(),
-                                    1 if out.dtype is torch.float32 else 0, 1 if accumulate else 0, at, n,
-                                    torch._C._cuda_getCurrentRawStream(dev))
-    _done(st, what)
+                                    1 if out.dtype is _F32 else 0, 1 if accumulate else 0, at, n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return out
 
 
 def moe_swiglu(gu, offsets=None, out=None):
     """silu(gu[:, :f]) * gu[:, f:] (bf16).  offsets: rows from its last value on are left as they are."""
     lib, what = _lib or load_library(), "moe_swiglu"
-    ldgu, live = _rows(what, "gu", gu, torch.bfloat16), _live(what, offsets)
-    rows, f2 = gu.shape
-    if f2 % 2:
+    live = None if offsets is None else _live(what, offsets)
+    if gu.dim() != 2:
+        _refuse(what, "gu has to be a matrix")
+    (rows, f2), (ldgu, step), dev = gu.shape, gu.stride(), gu.get_device()
+    if f2 & 1:
         _refuse(what, "gu has to have an even number of columns")
-    f = f2 // 2
-    dev = _launch_device(what, gu, offsets, out)
+    if not (gu.dtype is _BF16 and step == 1 and ldgu >= f2 and dev >= 0 and _device() == dev) or offsets is not None:
+        ldgu, dev = _rows(what, "gu", gu, _BF16), _launch_device(what, gu, offsets, out)
+    f = f2 >> 1
     if out is None:
-        out, ldh = gu.new_empty((rows, f)), f
+        out, ldh = gu.new_empty(rows, f), f
     else:
         ldh = _out_rows(what, "out", out, rows, f)
-    _done(lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), ldh, torch._C._cuda_getCurrentRawStream(dev)), what)
+        _launch_device(what, gu, out)
+    st = lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), ldh, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return out
 
 
@@ -456,19 +479,28 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     """The gradient of gu [rows, 2f] from that of moe_swiglu's result.  h: a matrix [rows, f] that gets that result
     again.  out may be gu itself."""
     lib, what = _lib or load_library(), "moe_swiglu_backward"
-    lddh, live = _rows(what, "dh", dh, torch.bfloat16), _live(what, offsets)
-    rows, f = dh.shape
-    ldgu = _rows(what, "gu", gu, torch.bfloat16, 2 * f)
-    if gu.shape[0] != rows:
-        _refuse(what, "dh and gu have to have as many rows")
-    ldh = f if h is None else _out_rows(what, "h", h, rows, f)
-    dev = _launch_device(what, dh, gu, offsets, out, h)
+    live = None if offsets is None else _live(what, offsets)
+    if dh.dim() != 2 or gu.dim() != 2:
+        _refuse(what, "dh and gu have to be matrices")
+    (rows, f), (lddh, s1), (ldgu, s2), dev = dh.shape, dh.stride(), gu.stride(), gu.get_device()
+    if not (dh.dtype is _BF16 and gu.dtype is _BF16 and s1 == 1 and s2 == 1 and lddh >= f and ldgu >= 2 * f and gu.shape == (rows, 2 * f)
+            and dev >= 0 and dh.get_device() == dev and _device() == dev) or offsets is not None:
+        lddh, ldgu = _rows(what, "dh", dh, _BF16), _rows(what, "gu", gu, _BF16, 2 * f)
+        if gu.shape[0] != rows:
+            _refuse(what, "dh and gu have to have as many rows")
+        dev = _launch_device(what, dh, gu, offsets, out, h)
+    ldh, at = f, None
+    if h is not None:
+        ldh, at = _out_rows(what, "h", h, rows, f), h.data_ptr()
+        _launch_device(what, gu, h)
     if out is None:
-        out, lddgu = gu.new_empty((rows, 2 * f)), 2 * f
+        out, lddgu = gu.new_empty(rows, 2 * f), 2 * f
     else:
         lddgu = _out_rows(what, "out", out, rows, 2 * f)
-    _done(lib.moe_swiglu_backward(dh.data_ptr(), lddh, gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), lddgu, _ptr(h), ldh,
-                                  torch._C._cuda_getCurrentRawStream(dev)), what)
+        _launch_device(what, gu, out)
+    st = lib.moe_swiglu_backward(dh.data_ptr(), lddh, gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), lddgu, at, ldh, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return out
 
 
@@ -493,7 +525,7 @@ def _norm_of(what, tensors, devices, call):
     n = _workspace_bytes("moe_grad_norm_workspace_bytes", len(tensors))
     ws = torch.empty(n // 4 + 1, dtype=torch.float32, device=torch.device("cuda", dev))  # the norm lies behind the workspace
     at = ws.data_ptr()
-    _done(call(at, n, at + n, torch._C._cuda_getCurrentRawStream(dev)), what)
+    _done(call(at, n, at + n, _stream_of(dev)), what)
     return ws[n // 4]
 
 
@@ -526,20 +558,27 @@ def _mx_pair(what, t, lead, K):
     cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
     if cols == 0:
         raise MoEError(2, what)
-    return t.new_empty((*lead, K // 2), dtype=torch.uint8), t.new_empty((*lead, cols), dtype=torch.uint8)
+    return t.new_empty((*lead, K // 2), dtype=_U8), t.new_empty((*lead, cols), dtype=_U8)
 
 
 def moe_mxfp4_quantize(x, offsets=None):
     """Rows [n, K] (bf16 or fp32) -> (values [n, K / 2], scales [n, S]), uint8.  offsets: rows from its last value on
     are not quantised."""
     lib, what = _lib or load_library(), "moe_mxfp4_quantize"
-    f32 = x.dtype is torch.float32
-    ldx, live = _rows(what, "x", x, torch.float32 if f32 else torch.bfloat16), _live(what, offsets)
-    rows, K = x.shape
-    dev = _launch_device(what, x, offsets)
-    values, scales = _mx_pair(what, x, (rows,), K)
-    _done(lib.moe_mxfp4_quantize(x.data_ptr(), 1 if f32 else 0, ldx, live, rows, K, values.data_ptr(), scales.data_ptr(),
-                                 torch._C._cuda_getCurrentRawStream(dev)), what)
+    live = None if offsets is None else _live(what, offsets)
+    if x.dim() != 2:
+        _refuse(what, "x has to be a matrix")
+    f32 = x.dtype is _F32
+    (rows, K), (ldx, step), dev = x.shape, x.stride(), x.get_device()
+    if not ((f32 or x.dtype is _BF16) and step == 1 and ldx >= K and dev >= 0 and _device() == dev) or offsets is not None:
+        ldx, dev = _rows(what, "x", x, _F32 if f32 else _BF16), _launch_device(what, x, offsets)
+    cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
+    if cols == 0:
+        raise MoEError(2, what)
+    values, scales = x.new_empty(rows, K // 2, dtype=_U8), x.new_empty(rows, cols, dtype=_U8)
+    st = lib.moe_mxfp4_quantize(x.data_ptr(), 1 if f32 else 0, ldx, live, rows, K, values.data_ptr(), scales.data_ptr(), _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return values, scales
 
 
@@ -552,7 +591,7 @@ def moe_mxfp4_quantize_weights(w):
     dev = _launch_device(what, w)
     values, scales = _mx_pair(what, w, (E, N), K)
     _done(lib.moe_mxfp4_quantize_weights(w.data_ptr(), E, K, N, values.data_ptr(), scales.data_ptr(),
-                                         torch._C._cuda_getCurrentRawStream(dev)), what)
+                                         _stream_of(dev)), what)
     return values, scales
 
 
@@ -576,7 +615,7 @@ def moe_mxfp4_dequantize(values, scales):
     dev = _launch_device(what, values, scales)
     out = values.new_empty((*values.shape[:-1], K), dtype=torch.bfloat16)
     _done(lib.moe_mxfp4_dequantize(values.data_ptr(), scales.data_ptr(), out.numel() // K, K, out.data_ptr(), K,
-                                   torch._C._cuda_getCurrentRawStream(dev)), what)
+                                   _stream_of(dev)), what)
     return out
 
 
@@ -585,20 +624,29 @@ def moe_mxfp4_grouped_gemm(x_values, x_scales, w_values, w_scales, offsets, out=
     lib, what = _lib or load_library(), "moe_mxfp4_grouped_gemm"
     if x_values.dim() != 2 or w_values.dim() != 3:
         _refuse(what, "x_values has to have two dimensions, w_values three")
-    K = _mx_check(what, "x", x_values, x_scales)
-    if _mx_check(what, "w", w_values, w_scales) != K:
-        _refuse(what, "x and w have to have the same K")
-    rows, (E, N) = x_values.shape[0], w_values.shape[:2]
-    _groups(what, offsets, E)
-    dev = _launch_device(what, x_values, x_scales, w_values, w_scales, offsets, out)
+    (rows, half), (E, N, w_half), dev = x_values.shape, w_values.shape, x_values.get_device()
+    K = 2 * half
+    cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
+    if not (x_values.dtype is _U8 and x_scales.dtype is _U8 and w_values.dtype is _U8 and w_scales.dtype is _U8
+            and offsets.dtype is _I32T and half == w_half and cols and x_scales.shape == (rows, cols) and w_scales.shape == (E, N, cols)
+            and offsets.shape == (E + 1,) and x_values.is_contiguous() and x_scales.is_contiguous() and w_values.is_contiguous()
+            and w_scales.is_contiguous() and offsets.is_contiguous() and dev >= 0 and x_scales.get_device() == dev
+            and w_values.get_device() == dev and w_scales.get_device() == dev and offsets.get_device() == dev and _device() == dev):
+        _mx_check(what, "x", x_values, x_scales)
+        if _mx_check(what, "w", w_values, w_scales) != K:
+            _refuse(what, "x and w have to have the same K")
+        _groups(what, offsets, E)
+        dev = _launch_device(what, x_values, x_scales, w_values, w_scales, offsets)
     if out is None:
-        out, ldy = x_values.new_empty((rows, N), dtype=torch.bfloat16), N
+        out, ldy = x_values.new_empty(rows, N, dtype=_BF16), N
     else:
         ldy = _out_rows(what, "out", out, rows, N)
+        _launch_device(what, x_values, out)
     ws, at, n = _workspace(x_values, "moe_mxfp4_grouped_gemm_workspace_bytes", rows, E, K, N)
-    _done(lib.moe_mxfp4_grouped_gemm(x_values.data_ptr(), x_scales.data_ptr(), w_values.data_ptr(), w_scales.data_ptr(),
-                                     offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n,
-                                     torch._C._cuda_getCurrentRawStream(dev)), what)
+    st = lib.moe_mxfp4_grouped_gemm(x_values.data_ptr(), x_scales.data_ptr(), w_values.data_ptr(), w_scales.data_ptr(),
+                                    offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
     return out
 
 
