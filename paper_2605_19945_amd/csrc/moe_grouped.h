@@ -80,7 +80,7 @@ struct GroupedTile {
 
 // Inside one expert's mt x nt tiles: bands of up to BAND row tiles, row tiles fastest, so that the 32 compute units of an XCD work
 // on neighbouring tiles and share their panels in its L2: about 8 x 4 of them, in the gradient of the weights 5 x 6 (128 experts, 2048 x
-// 1536 from 65528 rows 723 -> 662 us, 32 experts, 2048 x 7168 from 5003 rows 415 -> 319; row products the same within 1 %).
+// 1536 from 65528 rows 723 -> 662 us, 32 experts, 2048 x 7168 from 5003 rows 415 -> 319; row products are the same within 1 % at 4, 6, 8, 12).
 template <int BAND> static __device__ inline void place_in_band(int t, int mt, int nt, int* m, int* n) {
     const int band = t / (BAND * nt), r = t - band * BAND * nt;
     const int h = min(BAND, mt - BAND * band);
@@ -88,8 +88,8 @@ template <int BAND> static __device__ inline void place_in_band(int t, int mt, i
     *m = BAND * band + r - *n * h;
 }
 
-// The list of the row tiles (BM rows) of all experts times nt column tiles times the ranges of the reduction, kept by every wave in its registers, 4 experts a lane;
-// each XCD (workgroup number % 8) takes one stretch [begin, end) of it.
+// The list of the row tiles (BM rows) of all experts times nt column tiles times the ranges of the reduction, kept by every wave
+// in its registers, 4 experts a lane; each XCD (workgroup number % 8) takes one stretch [begin, end) of it.
 template <int BM> struct RowTiles {
     int lo[4], n[4], cnt[4], before, upto;  // row tiles before the lane's experts, and with them
     int nt, begin, end;
@@ -157,13 +157,15 @@ struct TileList {
     int height;           // rows of a tile (products over ragged rows)
 };
 
-// Cost of a tile of a weight gradient beside its K steps, in K steps: its stores.
+// Cost of a tile of a weight gradient beside its K steps, in K steps: its stores (32 experts, 2048 x 7168 from 5003 rows 300 / 323 / 392
+// us with 4 / 6 / 12, 128 experts, 2048 x 1536 from 65528 rows 671 / 664 with 4 / 6).
 constexpr int TILE_COST = 5;
-// Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside.
+// Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside (the columns, the barriers and
+// most of the loads' latency: the gradient of 65536 rows of 128 experts 429 us with 4 and 14, 441 with 5 and 7).
 constexpr int QUARTER_COST = 4, STEP_COST = 14;
 
-// By one wave.  An entry is a tile and a range of its reduction.  WEIGHTS: every expert has `per` entries, which cost what it has rows, and the stretches are of equal cost; otherwise a tile
-// costs the same everywhere.
+// By one wave.  An entry is a tile and a range of its reduction.  WEIGHTS: every expert has `per` entries, which cost what it
+// has rows, and the stretches are of equal cost; otherwise a tile costs the same everywhere.
 template <bool WEIGHTS, int BM> static __device__ inline void make_list(const GroupedArgs& g, int per, TileList* l) {
     const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
     int rows[4], c[4], sum = 0;
@@ -498,6 +500,15 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c,
 // Persistent: a workgroup goes through its tiles as one stream of K steps.  The stages of the next tile's first two steps are
 // asked for during the last two of this one, so only the first tile waits for memory, and a tile's stores leave under the next one's
 // products.
+//
+// Why 256 x 256: a K step of it is 64 KB for 8.4 MFLOP (bf16), two stages fit LDS, sums and fragments the 256 registers a lane
+// has at eight waves, and a compute unit asks its L2 for 43 bytes a nanosecond at the rate below; 128 x 128 needs twice that.
+// What bounds it: one product of 8192^3 the power (1400 TFLOP/s forward, 1430 gradient of the rows, 1385 of the weights, 4-bit
+// 4330; MFMA instructions alone sustain 1948).  Ragged rows on many experts the loads, which the L2s fetch 1.2 to 2.6 times, and the steps'
+// barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 912 us = 1055 TFLOP/s (matrix pipes busy 57 % of the time),
+// the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (57 %), 4-bit 8192 rows, 4096 to 28672, 555 us = 3470
+// TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
+// rows, memory: 659 us for 0.93 GB read and 1.62 GB written = 3.9 TB/s.
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
     constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;

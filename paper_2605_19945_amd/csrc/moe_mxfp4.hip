@@ -5,6 +5,8 @@
 // multiple of 16, zeros behind the last block.
 // Memory bounds these kernels: 2 + 17/32 bytes a bf16 value.  Rounding is the conversion instruction's, which rounds to
 // nearest even and saturates.
+// Measured: weights [32, 7168, 4096] 450 us = 5.3 TB/s, back to bf16 510 us = 4.7 TB/s (4 of 5 bytes are written), rows [8192, 4096]
+// 18 us = 4.7 TB/s (a large copy 5.1 TB/s).
 #include "moe_ops.h"
 
 namespace {
