@@ -516,17 +516,20 @@ def _grad_list(what, tensors):
 
 
 def _norm_of(what, tensors, devices, call):
+    n = _workspace_bytes("moe_grad_norm_workspace_bytes", len(tensors))
     if tensors:
         dev = _launch_device(what, tensors[0])
         if len(devices) > 1:
             _refuse(what, "tensors have to be on one device")
+        ws = tensors[0].new_empty(n // 4 + 1, dtype=_F32)  # the norm lies behind the workspace
     else:
         dev = torch.cuda.current_device()
-    n = _workspace_bytes("moe_grad_norm_workspace_bytes", len(tensors))
-    ws = torch.empty(n // 4 + 1, dtype=torch.float32, device=torch.device("cuda", dev))  # the norm lies behind the workspace
+        ws = torch.empty(n // 4 + 1, dtype=_F32, device=torch.device("cuda", dev))
     at = ws.data_ptr()
-    _done(call(at, n, at + n, _stream_of(dev)), what)
-    return ws[n // 4]
+    st = call(at, n, at + n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    return ws.select(0, n // 4)
 
 
 def moe_grad_norm(grads):
