@@ -515,6 +515,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
     constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4, CUT = BM < 256;  // (where there are few tiles they are small ones)
     constexpr int HALF = BM / 2, GROUP = HALF / WM;  // a wave has GROUP rows of each half of the tile: rows that are missing spare every wave alike
     constexpr int NS = (BM + BN) / 64 / NW;          // loads of scales a wave, every second K step
+    constexpr int PER = MX ? 2 : 1;                  // K steps a load of scales is for
     static_assert(!MX || NS * 64 * NW == BM + BN, "scale loads");
     __shared__ __attribute__((aligned(1024))) char lds_a[2][2][HALF * 128];  // [half of the rows][slot]
     __shared__ __attribute__((aligned(1024))) char lds_b[2][BN * 128];
@@ -541,7 +542,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         const char* wb = g.b + t.e * g.b_expert;
         // steps [from, to) of the reduction; at least two are gone through, those that are not there read zeros
         const int red = WEIGHTS ? t.n * 2 : g.kbytes, all = (red + 127) / 128;  // (bytes, as if its values were contiguous)
-        const int from = CUT ? (int)((int64_t)all * t.split / g.splits) : 0, to = CUT ? (int)((int64_t)all * (t.split + 1) / g.splits) : all;
+        // (4-bit: whole pairs, which share a load of scales)
+        const int pairs = (all + PER - 1) / PER;
+        const int from = CUT ? (int)((int64_t)pairs * t.split / g.splits) * PER : 0, to = CUT ? min(all, (int)((int64_t)pairs * (t.split + 1) / g.splits) * PER) : all;
         const int kb = CUT ? min(red, to * 128) : red;
         repeat<2>([&](auto u) {
             constexpr int R = u.value * HALF;
