@@ -75,6 +75,7 @@ struct GroupedTile {
     int e, lo, n;  // expert, its first row, its rows
     int m0, n0;    // first row (column of x in the weight gradient) and first column of the tile
     int split;     // range of the reduction
+    int pieces;    // ranges that its reduction is cut into
     int rows;      // rows (columns of x) of the tile that exist
 };
 
@@ -155,6 +156,7 @@ struct TileList {
     int first[257];       // row tiles before the expert (products over ragged rows)
     int begin, end;       // this XCD's stretch
     int height;           // rows of a tile (products over ragged rows)
+    int pieces, whole, rest;  // tiles [whole, whole + rest) of the stretch are cut into `pieces` ranges, one a workgroup
 };
 
 // Cost of a tile of a weight gradient beside its K steps, in K steps: its stores (32 experts, 2048 x 7168 from 5003 rows 300 / 323 / 392
@@ -164,9 +166,16 @@ constexpr int TILE_COST = 5;
 // most of the loads' latency: the gradient of 65536 rows of 128 experts 429 us with 4 and 14, 441 with 5 and 7).
 constexpr int QUARTER_COST = 4, STEP_COST = 14;
 
+// TAIL: the last round of tiles of 256 rows seldom fills the card.  Where it takes half of an XCD's workgroups or fewer, the
+// reductions of its tiles are cut into ranges for the others too, each leaves its sums in a slot of the workspace, and a second kernel
+// adds them in their order.  PIECE_COST: of a range's way to memory and back, on an XCD.
+constexpr int SIDE = 32;  // workgroups of an XCD
+constexpr int PIECE_COST = 17;
+constexpr int64_t PIECE = 256 * 256;  // values of a slot
+
 // By one wave.  An entry is a tile and a range of its reduction.  WEIGHTS: every expert has `per` entries, which cost what it
 // has rows, and the stretches are of equal cost; otherwise a tile costs the same everywhere.
-template <bool WEIGHTS, int BM> static __device__ inline void make_list(const GroupedArgs& g, int per, TileList* l) {
+template <bool WEIGHTS, int BM, bool TAIL> static __device__ inline void make_list(const GroupedArgs& g, int per, TileList* l) {
     const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
     int rows[4], c[4], sum = 0;
 #pragma unroll
@@ -178,11 +187,11 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
         l->lo[e] = lo;
         l->n[e] = rows[j];
     }
-    int height = BM;
+    int height = BM, pieces = 1;
     if (!WEIGHTS) {
         // Quarters of BM in the height that leaves the least to the busiest workgroup.  A step of a tile takes QUARTER_COST for every
         // quarter and STEP_COST beside.
-        int best = 0x7fffffff;
+        int64_t best = INT64_MAX;
 #pragma unroll
         for (int quarters = 4; quarters > 0; --quarters) {
             const int h = BM / 4 * quarters;
@@ -191,11 +200,32 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
             for (int j = 0; j < 4; ++j) tiles += (rows[j] + h - 1) / h;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d);
-            const int64_t rounds = ((int64_t)tiles * per + gridDim.x - 1) / gridDim.x;
-            const int cost = (int)min(rounds * (STEP_COST + QUARTER_COST * quarters), (int64_t)0x7ffffffe);
-            if (cost < best) {
-                best = cost;
-                height = h;
+            const int step = STEP_COST + QUARTER_COST * quarters;
+            if constexpr (TAIL) {
+                const uint32_t steps = (g.kbytes + 127) / 128, most = (uint32_t)min(((int64_t)tiles * per + 7) / 8, (int64_t)0x7fffffff);
+                const uint32_t full = most / SIDE, rest = most % SIDE;
+                int64_t cost = (int64_t)(full + (rest > 0)) * steps * step;
+                int cut = 1;
+                if (rest > 0 && rest <= SIDE / 2) {
+                    for (uint32_t s = min(SIDE / rest, steps / 4); s > 1; s = s * 3 / 4) {
+                        const int64_t other = ((int64_t)full * steps + (steps + s - 1) / s) * step + PIECE_COST * (int)(rest * s);
+                        if (other < cost) {
+                            cost = other;
+                            cut = (int)s;
+                        }
+                    }
+                }
+                if (cost < best) {
+                    best = cost;
+                    height = h;
+                    pieces = cut;
+                }
+            } else {
+                const int64_t cost = ((int64_t)tiles * per + gridDim.x - 1) / gridDim.x * step;
+                if (cost < best) {
+                    best = cost;
+                    height = h;
+                }
             }
         }
         height = __builtin_amdgcn_readfirstlane(height);
@@ -234,6 +264,13 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
             }
         }
     }
+    if (TAIL && lane == 0) {  // (an XCD's rest is that of the longest stretch or one less)
+        const int begin = (int)(total * xcd / 8), n = (int)(total * (xcd + 1) / 8) - begin, rest = n % SIDE;
+        l->pieces = pieces;
+        l->rest = rest;
+        l->whole = begin + n - rest;
+        if (pieces > 1) l->end = begin + n - rest + rest * pieces;
+    }
     if (!WEIGHTS) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -244,12 +281,21 @@ template <bool WEIGHTS, int BM> static __device__ inline void make_list(const Gr
     }
 }
 
-template <bool WEIGHTS, int BM, int BN>
+template <bool WEIGHTS, int BM, int BN, bool TAIL>
 static __device__ inline GroupedTile find_tile(const GroupedArgs& g, const TileList& l, int splits, int height, int mt, int nt, int t) {
     GroupedTile out;
     int e, m, n, r;
     out.split = t % splits;
+    out.pieces = splits;
     t = __builtin_amdgcn_readfirstlane(t / splits);
+    if (TAIL) {
+        const int j = t - l.whole, pieces = l.pieces;
+        if (pieces > 1 && j >= 0) {  // a range of a tile
+            out.pieces = __builtin_amdgcn_readfirstlane(pieces);
+            out.split = __builtin_amdgcn_readfirstlane((uint32_t)j / l.rest);
+            t = __builtin_amdgcn_readfirstlane(l.whole + (uint32_t)j % l.rest);
+        }
+    }
     if (WEIGHTS) {
         e = __builtin_amdgcn_readfirstlane(t / (mt * nt));
         r = t - e * mt * nt;
@@ -505,14 +551,14 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c,
 // has at eight waves, and a compute unit asks its L2 for 43 bytes a nanosecond at the rate below; 128 x 128 needs twice that.
 // What bounds it: one product of 8192^3 the power (1400 TFLOP/s forward, 1430 gradient of the rows, 1385 of the weights, 4-bit
 // 4330; MFMA instructions alone sustain 1948).  Ragged rows on many experts the loads, which the L2s fetch 1.2 to 2.6 times, and the steps'
-// barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 912 us = 1055 TFLOP/s (matrix pipes busy 57 % of the time),
+// barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 845 us = 1138 TFLOP/s (whole last round: 922),
 // the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (57 %), 4-bit 8192 rows, 4096 to 28672, 555 us = 3470
 // TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
 // rows, memory: 659 us for 0.93 GB read and 1.62 GB written = 3.9 TB/s.
-template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN>
+template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
     constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;
-    constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4, CUT = BM < 256;  // (where there are few tiles they are small ones)
+    constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4, CUT = BM < 256 || TAIL;
     constexpr int HALF = BM / 2, GROUP = HALF / WM;  // a wave has GROUP rows of each half of the tile: rows that are missing spare every wave alike
     constexpr int NS = (BM + BN) / 64 / NW;          // loads of scales a wave, every second K step
     constexpr int PER = MX ? 2 : 1;                  // K steps a load of scales is for
@@ -524,7 +570,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mt = (g.M + BM - 1) / BM, nt = (g.N + BN - 1) / BN;
-    if (wave == 0) make_list<WEIGHTS, BM>(g, (WEIGHTS ? mt * nt : nt) * g.splits, &list);
+    if (wave == 0) make_list<WEIGHTS, BM, TAIL>(g, (WEIGHTS ? mt * nt : nt) * (BM < 256 ? g.splits : 1), &list);
     block_barrier();
     const int height = WEIGHTS ? BM : __builtin_amdgcn_readfirstlane(list.height);
     int at = __builtin_amdgcn_readfirstlane(list.begin) + (blockIdx.x >> 3);
@@ -544,7 +590,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         const int red = WEIGHTS ? t.n * 2 : g.kbytes, all = (red + 127) / 128;  // (bytes, as if its values were contiguous)
         // (4-bit: whole pairs, which share a load of scales)
         const int pairs = (all + PER - 1) / PER;
-        const int from = CUT ? (int)((int64_t)pairs * t.split / g.splits) * PER : 0, to = CUT ? min(all, (int)((int64_t)pairs * (t.split + 1) / g.splits) * PER) : all;
+        const int from = CUT ? (uint32_t)(pairs * t.split) / t.pieces * PER : 0, to = CUT ? min(all, (int)((uint32_t)(pairs * (t.split + 1)) / t.pieces * PER)) : all;
         const int kb = CUT ? min(red, to * 128) : red;
         repeat<2>([&](auto u) {
             constexpr int R = u.value * HALF;
@@ -681,7 +727,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         }
     };
 
-    start(find_tile<WEIGHTS, BM, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
+    start(find_tile<WEIGHTS, BM, BN, TAIL>(g, list, BM < 256 ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
     repeat<2>([&](auto s) {
         repeat<2>([&](auto part) {
             begin(part);
@@ -709,7 +755,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
             if (left == 2) {                // from here on the loads are the next tile's
                 at += gridDim.x >> 3;
                 if (at < last) {
-                    start(find_tile<WEIGHTS, BM, BN>(g, list, CUT ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
+                    start(find_tile<WEIGHTS, BM, BN, TAIL>(g, list, BM < 256 ? g.splits : 1, WEIGHTS ? BM : height, mt, nt, at));
                 } else {
                     la[0].stop();
                     la[1].stop();
@@ -723,7 +769,12 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
         const int m = t.m0 + wm * GROUP, n = t.n0 + wn * FN * 16;
         const int64_t row = WEIGHTS ? (int64_t)t.e * g.M + m : (int64_t)t.lo + m;
         constexpr int esize = OUT == OUT_BF16 ? 2 : 4;
-        if (CUT && g.splits > 1) store_tile<OUT_F32, 2 * FH, FN, HALF>(acc, g.part + t.split * g.slab + row * g.N + n, g.N, mrows - wm * GROUP, g.N - n);
+        if (CUT && t.pieces > 1) {
+            // the ranges of whole products leave slabs like c, those of the last tiles (a workgroup has one at the most, its last) slots
+            float* to = BM < 256 ? g.part + t.split * g.slab + row * g.N + n
+                                 : g.part + ((blockIdx.x & 7) * SIDE + (blockIdx.x >> 3)) * PIECE + wm * GROUP * 256 + wn * FN * 16;
+            store_tile<OUT_F32, 2 * FH, FN, HALF>(acc, to, BM < 256 ? g.N : 256, mrows - wm * GROUP, g.N - n);
+        }
         else if (!(OUT == OUT_F32_ADD && t.n == 0)) {
             char* to = (char*)g.c + (row * g.ldc + n) * esize;
             if constexpr (WEIGHTS) store_lines<OUT, 2 * FH, FN, HALF>(acc, to, g.ldc, mrows - wm * GROUP, g.N - n);
@@ -736,9 +787,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
 }
 
 // One workgroup a compute unit (two where two fit), in eights so that every XCD has as many.
-template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN> static inline hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
+template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL = false> static inline hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
     constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
-    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN><<<blocks, WM * WN * 64, 0, st>>>(g);
+    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN, TAIL><<<blocks, WM * WN * 64, 0, st>>>(g);
     return hipGetLastError();
 }
 

@@ -50,6 +50,34 @@ template <int OUT> __global__ __launch_bounds__(256) void sum_weights_kernel(Gro
     }
 }
 
+// The cut tiles of the last round (256 x 256; a workgroup adds 32 rows of one): the sums of its ranges in their order.
+__global__ __launch_bounds__(256) void sum_pieces_kernel(GroupedArgs g) {
+    __shared__ TileList list;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (g.N + 255) / 256;
+    if (wave == 0) make_list<false, 256, true>(g, nt, &list);
+    __syncthreads();
+    const int pieces = list.pieces, rest = list.rest, unit = blockIdx.x >> 3;
+    if (pieces == 1 || unit >= 8 * rest) return;
+    const int j = unit >> 3;
+    const GroupedTile t = find_tile<false, 256, 256, true>(g, list, 1, list.height, 0, nt, list.whole + j);
+    const int row0 = (unit & 7) * 32 + wave * 8, col = lane * 4, rows = t.rows - row0;
+    if (rows <= 0 || col >= g.N - t.n0) return;
+    const float* from = g.part + ((blockIdx.x & 7) * SIDE + j) * PIECE + row0 * 256 + col;
+    f32x4_t sum[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum[r] = r < rows ? *(const f32x4_t*)(from + r * 256) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s = 1; s < pieces; ++s) {
+        const float* p = from + s * rest * PIECE;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < rows) sum[r] += *(const f32x4_t*)(p + r * 256);
+    }
+    uint16_t* to = (uint16_t*)g.c + ((int64_t)t.lo + t.m0 + row0) * g.ldc + t.n0 + col;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < rows) *(uint2*)(to + r * g.ldc) = uint2{pack_bf16(sum[r][0], sum[r][1]), pack_bf16(sum[r][2], sum[r][3])};
+}
+
 int blocks_of(int64_t lanes) {
     const int64_t want = ceil_div(lanes, 256);
     return (int)(want < 2048 ? want : 2048);
@@ -59,9 +87,13 @@ int blocks_of(int64_t lanes) {
 template <typename L> hipError_t run_rows(GroupedArgs& g, const GroupedPlan& p, void* ws, hipStream_t st, L launch) {
     g.splits = p.splits;
     g.slab = (int64_t)g.rows_cap * g.N;
-    g.part = (float*)ws;
+    g.part = (float*)(p.splits > 1 || p.tail ? ws : nullptr);
     const hipError_t e = launch(g, p.bm, st);
-    if (e != hipSuccess || g.splits == 1) return e;
+    if (e != hipSuccess || g.part == nullptr) return e;
+    if (p.tail) {
+        sum_pieces_kernel<<<8 * 8 * SIDE / 2, 256, 0, st>>>(g);
+        return hipGetLastError();
+    }
     const int experts = g.rows_cap < g.E ? g.rows_cap : g.E;
     sum_rows_kernel<<<dim3(blocks_of(ceil_div(g.rows_cap, experts) * (g.N / 8)), g.E), 256, 0, st>>>(g);
     return hipGetLastError();

@@ -8,6 +8,7 @@
 struct GroupedPlan {
     int bm;      // rows of a tile: 16, 32 (the streaming kernel), 128, 256 (the tile engine)
     int splits;  // ranges of the reduction; their partial sums need splits * outputs * 4 bytes of workspace
+    bool tail;   // the reductions of the last round's tiles (256 rows) may be cut on the device: a slot of workspace for every workgroup
 };
 
 constexpr int GROUPED_MAX_SPLITS = 16;
@@ -20,7 +21,7 @@ struct GroupedKernel { int bm, slots; double idle, load, store, rate; };
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Bytes of workspace a plan needs.
-static inline size_t grouped_workspace(const GroupedPlan& p, int64_t outputs) { return p.splits > 1 ? (size_t)p.splits * outputs * 4 : 0; }
+static inline size_t grouped_workspace(const GroupedPlan& p, int64_t outputs) { return p.tail ? (size_t)256 * 256 * 256 * 4 : p.splits > 1 ? (size_t)p.splits * outputs * 4 : 0; }
 
 // The fastest cut of `tiles` tiles of `units` units each: a cut costs a second launch and a way to memory and back for its partial
 // sums (one token's reduction of 14336 over 512 columns: 71 us in one piece, 37, 23, 17, 15 in 2, 4, 8, 16; one of 1024 over 1024
@@ -30,8 +31,9 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
     *splits = 1;
     for (int s = 1; s <= most && s <= units; ++s) {
         if (s > 1 && ((size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE || tiles * (s - 1) >= 2 * k.slots)) break;
-        const double rounds = (double)(tiles * s) / k.slots, fill = rounds < 1 ? rounds : 1;
-        double t = (rounds < 1 ? 1 : rounds) * ((double)ceil_div(units, s) * (k.idle + k.load * fill) + k.store);
+        const int64_t full = tiles * s / k.slots, rest = tiles * s % k.slots;
+        double t = (double)full * ((double)ceil_div(units, s) * (k.idle + k.load) + k.store);
+        if (rest > 0) t += (double)ceil_div(units, s) * (k.idle + k.load * rest / k.slots) + k.store;
         if (t < bytes / k.rate) t = bytes / k.rate;
         if (s > 1) t += 4.0 + 2e-6 * s * (double)outputs;
         if (s > 1 && t < 6.5) t = 6.5;  // (the host's second launch)
@@ -48,8 +50,14 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
 // Measured, 8 experts, 4096 to 14336, us on row tiles of 16 / 32 / 128 / 256: 8 rows an expert 162 / 163 / 180 / 174, 16 230 / 169 / 185 / 175,
 // 32 354 / 258 / 196 / 177, 128 989 / 649 / 282 / 200; 4-bit 41 / 42 / 45 / 50, 53 / 45 / 46 / 50, 86 / 70 / 47 / 51, 242 / 172 / 76 / 65;
 // 8 experts, 1024 to 1024, 256 rows an expert: - / - / 19 / 20.
+//
+// Tiles of 256 rows with the last round's reductions cut (a piece costs 0.11 us of memory and sum, the second launch and its end 12): surely
+// where all tiles together take half the card or less (1 expert, 14336 to 2048, 1500 rows 130 -> 105 us, 8 experts, 14336 to 1024, 3000
+// rows 174 -> 125; 5120 to 5120, 512 rows, where it does not pay by this reckoning, 43 -> 61), otherwise for reductions of 80 steps and more in up to
+// 12 rounds, where a round is worth the launch (14336 to 4096, 8 experts, two of them leading, 8192 rows 922 -> 845, biased, 4096 rows 561 -> 484,
+// 2 experts, 6144 to 6144, 3000 rows 237 -> 211; nothing left to cut in a last round of 8192 to 2048, 5000 rows 177 -> 180).
 static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, bool row_major, bool mx) {
-    GroupedPlan p = {128, 1};
+    GroupedPlan p = {128, 1, false};
     if (rows <= 0) return p;
     const int experts = rows < E ? rows : E;
     const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.0, 5.9e6}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.2, 5.9e6},
@@ -65,10 +73,22 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
         const int64_t tiles = row_tiles * ceil_div(N, stream ? (row_major ? 128 : 64) : k.bm);
         const int64_t units = ceil_div(kbytes, stream ? (mx ? 1024 : row_major ? 256 : 512) : 128);
         int splits;
-        const double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, &splits);
+        bool tail = false;
+        double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, &splits);
+        if (k.bm == 256 && mx) {
+            // (256 of their values are a step, so few reductions are long enough: 28672 to 8192 in 5000 rows 650 -> 639 us, in 3000 434 -> 442)
+        } else if (k.bm == 256 && 2 * tiles <= k.slots) {
+            for (int64_t s = 2; s <= k.slots / tiles && s <= units / 4; ++s) {
+                const double cut = (double)ceil_div(units, s) * (k.idle + k.load * (tiles * s) / k.slots) + k.store + 12.0 + 0.11 * (tiles * s);
+                tail = tail || cut < t;
+                if (cut < t) t = cut;
+            }
+        } else if (k.bm == 256) {
+            tail = units >= 80 && tiles <= 12 * k.slots && (E > 1 || tiles % k.slots != 0);
+        }
         if (i == 0 || t < best) {
             best = t;
-            p = {k.bm, splits};
+            p = {k.bm, splits, tail};
         }
     }
     return p;
@@ -78,11 +98,11 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
 // time 1 and 4 (8 experts, 1024 x 1024: 2048 rows 21 and 17 us, 8192 40 and 32; 4096 x 2048 from 4096 rows 98 and 107; 128 experts,
 // 3328 x 160 from 29 rows 58 and 71).
 static inline GroupedPlan grouped_weights_plan(int rows, int E, int M, int N) {
-    GroupedPlan p = {128, 1};
+    GroupedPlan p = {128, 1, false};
     const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256) * E, t128 = ceil_div(M, 128) * ceil_div(N, 128) * E;
     const int experts = rows < E ? rows : E;
     const int64_t steps = experts > 0 ? ceil_div(ceil_div(rows, experts), 64) : 1;
     const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, &p.splits);
-    if ((t256 < 256 ? 1.0 : (double)t256 / 256) * ((double)steps * 1.5 + 7.5) < t + 1.0) p = {256, 1};
+    if ((t256 < 256 ? 1.0 : (double)t256 / 256) * ((double)steps * 1.5 + 7.5) < t + 1.0) p = {256, 1, false};
     return p;
 }

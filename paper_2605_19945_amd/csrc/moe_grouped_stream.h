@@ -184,6 +184,9 @@ template <int FMT, int LB> static inline hipError_t launch_rows(const GroupedArg
     if (bm == 16) grouped_stream_kernel<FMT, LB, 16, 3><<<256, 256, 0, st>>>(g);
     else if (bm == 32) grouped_stream_kernel<FMT, LB, 32, 2><<<256, 256, 0, st>>>(g);
     else if (bm == 128) return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 128, 128, 2, 2>(g, st);
-    else return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 256, 256, 2, 4>(g, st);
+    else if constexpr (FMT == FMT_BF16) {
+        if (g.part != nullptr) return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 256, 256, 2, 4, true>(g, st);
+        return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 256, 256, 2, 4>(g, st);
+    } else return launch_tiles<FMT, LAY_K, LB, OUT_BF16, 256, 256, 2, 4>(g, st);
     return hipGetLastError();
 }

@@ -3,7 +3,7 @@
 Bounds.  Products of small whole numbers have sums that 32 bits hold exactly, in any order: results are then the
 exact ones, rounded once to the output's type, and are compared by equality.  Elsewhere a sum of n products in 32 bits is off by at
 most n 2^-23 times the sum of their magnitudes (2^-24 a rounded addition, twice that where one is cut), and a rounding to
-bf16 by 2^-9 of the value."""
+bf16 by 2^-8 of the value."""
 import math
 
 import numpy as np
@@ -74,6 +74,38 @@ def test_grouped_gemm_whole_numbers_exactly(rows, K, N, transpose_w):
     w = whole((len(rows), N, K) if transpose_w else (len(rows), K, N), -2, 2, 2)
     got = moe.moe_grouped_gemm(x.cuda(), w.cuda(), off.cuda(), transpose_w=transpose_w)
     assert got.dtype == BF16 and torch.equal(got.cpu(), ref_gemm(x, w, off, transpose_w).to(BF16))
+
+
+# long reductions in a few of the largest tiles, or in a round of them and a few more: the last ones are cut into ranges
+LONG = [
+    ([4500], 8200, 520, 0),
+    ([2000], 14344, 1000, 0),
+    ([1300, 0, 1700], 8200, 1000, 0),
+    ([2600, 1, 0, 700, 0, 0, 1199, 0], 8200, 1000, 0),
+    ([4200], 5128, 4104, 0),
+    ([2500, 900, 0, 1100], 5128, 4104, 0),
+    ([700, 0, 1, 260], 8200, 1000, 3600),   # most of the rows that there may be are not there
+    ([0, 0, 0], 8200, 1000, 4000),
+    ([1, 1], 14344, 1000, 3500),
+]
+
+
+@pytest.mark.parametrize("rows,K,N,more", LONG)
+@pytest.mark.parametrize("transpose_w", [False, True])
+def test_grouped_gemm_long_reductions_of_few_tiles(rows, K, N, more, transpose_w):
+    off = offsets_of(rows)
+    n = int(off[-1])
+    x = whole((n + more, K), -2, 2, 11).cuda()
+    w = whole((len(rows), N, K) if transpose_w else (len(rows), K, N), -2, 2, 12).cuda()
+    x[n:] = float("nan")
+    out = torch.full((n + more, N + 8), 7.0, dtype=BF16, device="cuda")[:, :N]
+    got = moe.moe_grouped_gemm(x, w, off.cuda(), transpose_w=transpose_w, out=out)
+    for e in range(len(rows)):
+        a, b = int(off[e]), int(off[e + 1])
+        if b > a:
+            ref = torch.mm(x[a:b].double(), (w[e].t().contiguous() if transpose_w else w[e]).double())
+            assert torch.equal(got[a:b], ref.to(BF16)), e
+    assert (got[n:] == 7).all() and (torch.as_strided(out, (n + more, 8), (N + 8, 1), N) == 7).all()
 
 
 @pytest.mark.parametrize("rows,K,N", SHAPES)
