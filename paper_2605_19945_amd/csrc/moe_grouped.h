@@ -552,8 +552,8 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c,
 // What bounds it: one product of 8192^3 the power (1400 TFLOP/s forward, 1430 gradient of the rows, 1385 of the weights, 4-bit
 // 4330; MFMA instructions alone sustain 1948).  Ragged rows on many experts the loads, which the L2s fetch 1.2 to 2.6 times, and the steps'
 // barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 845 us = 1138 TFLOP/s (whole last round: 922),
-// the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (57 %), 4-bit 8192 rows, 4096 to 28672, 555 us = 3470
-// TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
+// the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (matrix pipes busy 57 % of the time), 4-bit 8192 rows, 4096 to 28672, 555 us
+// = 3470 TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
 // rows, memory: 659 us for 0.93 GB read and 1.62 GB written = 3.9 TB/s.
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
