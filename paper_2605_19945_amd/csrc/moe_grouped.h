@@ -461,11 +461,37 @@ template <int FMT, int SB, int SA> static __device__ inline f32x4_t multiply(con
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, c, 4, 4, SB, sb, SA, sa);
 }
 
+// Where a wave's fragments go: a buffer that ends with the last column of the last row that exists, so that rows behind it and
+// columns that are given an offset behind it are not stored, without a branch and with one address register (addresses of 64 bits
+// were spilled, and every reload waited for the stores before it: gradient of 128 experts' weights 666 -> 645 us, of 16 experts',
+// 8544 x 5888, 382 -> 344).
+struct Sink {
+    __amdgpu_buffer_rsrc_t to;
+    uint32_t ld;  // bytes between rows
+    uint32_t end; // bytes of a row that exist
+
+    __device__ inline Sink(void* c, int64_t ldc, int esize, int rows, int cols) {
+        ld = __builtin_amdgcn_readfirstlane((uint32_t)ldc * esize);
+        asm volatile("" : "+s"(ld));  // places are formed where they are used: the compiler would keep them through the tiles
+        end = (uint32_t)max(cols, 0) * esize;
+        to = __builtin_amdgcn_make_buffer_rsrc(c, 0, __builtin_amdgcn_readfirstlane(rows > 0 && cols > 0 ? (rows - 1) * (int)ld + (int)end : 0), 0x27000);
+    }
+    // 16 bytes at byte `at` of row `row`; AUX: 2 is the non-temporal hint
+    template <int AUX> __device__ inline void put(const u32x4_t& v, uint32_t row, uint32_t at) const {
+        __builtin_amdgcn_raw_buffer_store_b128(v, to, at < end ? row * ld + at : OUT_OF_RANGE, 0, AUX);
+    }
+    template <int AUX> __device__ inline void add(const f32x4_t& v, uint32_t row, uint32_t at) const {
+        const uint32_t place = at < end ? row * ld + at : OUT_OF_RANGE;
+        const f32x4_t old = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(to, place, 0, 0));
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, old + v), to, place, 0, AUX);
+    }
+};
+
 // Stores a wave's FM x FN fragments.  The weights are the first operand of the matrix instruction, so a lane has 4
 // neighbouring columns of one row; two fragments change halves between neighbouring rows of 16 lanes, and every lane
 // then stores 8 bf16 columns (16 bytes) of one row.
 template <int OUT, int FM, int FN, int FAR>
-static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], void* c, int64_t ldc, int rows, int cols) {
+static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], const Sink& to) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     repeat<FM>([&](auto mf) {
         const int row = mf.value / (FM / 2) * FAR + mf.value % (FM / 2) * 16 + i;
@@ -474,40 +500,27 @@ static __device__ inline void store_tile(const f32x4_t (&acc)[FM][FN], void* c, 
                 const f32x4_t u = acc[mf.value][2 * p.value], v = acc[mf.value][2 * p.value + 1];
                 const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(u[0], u[1]), pack_bf16(v[0], v[1]), false, false);
                 const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(u[2], u[3]), pack_bf16(v[2], v[3]), false, false);
-                const int col = (2 * p.value + (q & 1)) * 16 + (q >> 1) * 8;
-                if (row < rows && col < cols) {
-                    const u32x4_t w = {lo[0], hi[0], lo[1], hi[1]};
-                    *(u32x4_t*)((uint16_t*)c + row * ldc + col) = w;
-                }
+                to.put<0>(u32x4_t{lo[0], hi[0], lo[1], hi[1]}, row, p.value * 64 + (q & 1) * 32 + (q >> 1) * 16);
             });
         } else {
-            repeat<FN>([&](auto nf) {
-                const int col = nf.value * 16 + q * 4;
-                if (row < rows && col < cols) {
-                    f32x4_t* to = (f32x4_t*)((float*)c + row * ldc + col);
-                    f32x4_t v = acc[mf.value][nf.value];
-                    if (OUT == OUT_F32_ADD) v += *to;
-                    *to = v;
-                }
-            });
+            repeat<FN>([&](auto nf) { to.put<0>(__builtin_bit_cast(u32x4_t, acc[mf.value][nf.value]), row, nf.value * 64 + q * 16); });
         }
     });
 }
 
-// The same for gradients of weights, which are the largest outputs and not read again soon: stores of whole 128-byte lines with the
-// non-temporal hint (with bands of 8: 32 experts, 2048 x 7168 from 5003 rows: 464 -> 415 us; with the hint on stores of 64 bytes 128 experts, 2048 x 1536
-// from 65528 rows take 868 us instead of 721).  Lanes 0 - 7 and 8 - 15 of every 16 change places, so that two stores of 16 rows by 64
-// bytes become two of 8 rows by 128.
-template <int OUT, int FM, int FN, int FAR>
-static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c, int64_t ldc, int rows, int cols) {
+// The same for gradients of weights, which are the largest outputs and not read again soon: stores of whole 128-byte lines, with the
+// non-temporal hint where AUX says so (with bands of 8: 32 experts, 2048 x 7168 from 5003 rows: 464 -> 415 us; with the hint on stores of
+// 64 bytes 128 experts, 2048 x 1536 from 65528 rows take 868 us instead of 721).  Lanes 0 - 7 and 8 - 15 of every 16 change
+// places, so that two stores of 16 rows by 64 bytes become two of 8 rows by 128.
+template <int OUT, int FM, int FN, int FAR, int AUX>
+static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], const Sink& to) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-    constexpr int WIDE = OUT == OUT_BF16 ? 32 : 16;  // columns of a 64-byte piece
     const bool low = i < 8;
     auto turn = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false); };  // from lane i ^ 8 of the 16
     repeat<FM>([&](auto mf) {
         const int row0 = mf.value / (FM / 2) * FAR + mf.value % (FM / 2) * 16 + (i & 7);
-        repeat<FN * 16 / (2 * WIDE)>([&](auto p) {
-            u32x4_t piece[2];
+        repeat<FN * 16 * (OUT == OUT_BF16 ? 2 : 4) / 128>([&](auto p) {
+            u32x4_t piece[2];  // of 64 bytes a row
             repeat<2>([&](auto h) {
                 if constexpr (OUT == OUT_BF16) {
                     constexpr int N = 4 * p.value + 2 * h.value;
@@ -526,19 +539,12 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c,
                 a[w] = low ? piece[0][w] : other;
                 b[w] = low ? other : piece[1][w];
             }
-            const int col = (2 * p.value + (low ? 0 : 1)) * WIDE + (OUT == OUT_BF16 ? (q & 1) * 16 + (q >> 1) * 8 : q * 4);
+            const uint32_t at = p.value * 128 + (low ? 0 : 64) + (OUT == OUT_BF16 ? (q & 1) * 32 + (q >> 1) * 16 : q * 16);
             repeat<2>([&](auto h) {
-                const int row = row0 + 8 * h.value;
-                if (row < rows && col < cols) {
-                    const u32x4_t v = h.value ? b : a;
-                    if constexpr (OUT == OUT_BF16) {
-                        __builtin_nontemporal_store(v, (u32x4_t*)((uint16_t*)c + row * ldc + col));
-                    } else {
-                        f32x4_t* to = (f32x4_t*)((float*)c + row * ldc + col);
-                        __builtin_nontemporal_store(OUT == OUT_F32_ADD ? *to + __builtin_bit_cast(f32x4_t, v) : __builtin_bit_cast(f32x4_t, v), to);
-                    }
-                }
+                if constexpr (OUT == OUT_F32_ADD) to.add<AUX>(__builtin_bit_cast(f32x4_t, h.value ? b : a), row0 + 8 * h.value, at);
+                else to.put<AUX>(h.value ? b : a, row0 + 8 * h.value, at);
             });
+            __builtin_amdgcn_sched_barrier(0);  // (fragments are turned one by one: there are no registers for more)
         });
     });
 }
@@ -555,7 +561,7 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], void* c,
 // the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (matrix pipes busy 57 % of the time), 4-bit 8192 rows, 4096 to 28672, 555 us
 // = 3470 TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
 // rows, memory: 659 us for 0.93 GB read and 1.62 GB written = 3.9 TB/s.
-template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL>
+template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL, bool LINES>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
     constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;
     constexpr bool WEIGHTS = LA == LAY_MN, MX = FMT == FMT_MX4, CUT = BM < 256 || TAIL;
@@ -773,12 +779,11 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
             // the ranges of whole products leave slabs like c, those of the last tiles (a workgroup has one at the most, its last) slots
             float* to = BM < 256 ? g.part + t.split * g.slab + row * g.N + n
                                  : g.part + ((blockIdx.x & 7) * SIDE + (blockIdx.x >> 3)) * PIECE + wm * GROUP * 256 + wn * FN * 16;
-            store_tile<OUT_F32, 2 * FH, FN, HALF>(acc, to, BM < 256 ? g.N : 256, mrows - wm * GROUP, g.N - n);
-        }
-        else if (!(OUT == OUT_F32_ADD && t.n == 0)) {
-            char* to = (char*)g.c + (row * g.ldc + n) * esize;
-            if constexpr (WEIGHTS) store_lines<OUT, 2 * FH, FN, HALF>(acc, to, g.ldc, mrows - wm * GROUP, g.N - n);
-            else store_tile<OUT, 2 * FH, FN, HALF>(acc, to, g.ldc, mrows - wm * GROUP, g.N - n);
+            store_tile<OUT_F32, 2 * FH, FN, HALF>(acc, Sink(to, BM < 256 ? g.N : 256, 4, mrows - wm * GROUP, g.N - n));
+        } else if (!(OUT == OUT_F32_ADD && t.n == 0)) {
+            const Sink to((char*)g.c + (row * g.ldc + n) * esize, g.ldc, esize, mrows - wm * GROUP, g.N - n);
+            if constexpr (!WEIGHTS) store_tile<OUT, 2 * FH, FN, HALF>(acc, to);
+            else store_lines<OUT, 2 * FH, FN, HALF, LINES ? 2 : 0>(acc, to);
         }
         if (at >= last) break;
         clear();
@@ -787,9 +792,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
 }
 
 // One workgroup a compute unit (two where two fit), in eights so that every XCD has as many.
-template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL = false> static inline hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
+template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL = false, bool LINES = false> static inline hipError_t launch_tiles(const GroupedArgs& g, hipStream_t st) {
     constexpr int blocks = BM * BN > 128 * 128 ? 256 : 512;
-    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN, TAIL><<<blocks, WM * WN * 64, 0, st>>>(g);
+    grouped_tile_kernel<FMT, LA, LB, OUT, BM, BN, WM, WN, TAIL, LINES><<<blocks, WM * WN * 64, 0, st>>>(g);
     return hipGetLastError();
 }
 
