@@ -15,8 +15,9 @@ constexpr int GROUPED_MAX_SPLITS = 16;
 constexpr size_t GROUPED_MAX_WORKSPACE = (size_t)64 << 20;
 
 // A kernel: `slots` tiles at a time, a unit of a tile's reduction takes idle (few tiles, latency) to idle + load (all slots taken, memory)
-// microseconds, its end `store`; it reads `rate` bytes a microsecond at the most.
-struct GroupedKernel { int bm, slots; double idle, load, store, rate; };
+// microseconds, its end `store`; it reads `rate` bytes a microsecond at the most.  `least`: units of a tile that are gone through at least
+// (those that are not there take no memory).
+struct GroupedKernel { int bm, slots; double idle, load, store, rate; int least; };
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -32,8 +33,11 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
     for (int s = 1; s <= most && s <= units; ++s) {
         if (s > 1 && ((size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE || tiles * (s - 1) >= 2 * k.slots)) break;
         const int64_t full = tiles * s / k.slots, rest = tiles * s % k.slots;
-        double t = (double)full * ((double)ceil_div(units, s) * (k.idle + k.load) + k.store);
-        if (rest > 0) t += (double)ceil_div(units, s) * (k.idle + k.load * rest / k.slots) + k.store;
+        const double piece = (double)ceil_div(units, s), pad = piece < k.least ? k.idle * (k.least - piece) : 0;
+        // the end of a tile: bf16 results of a streamed one leave under the next one's loads, but for the last; 32 bits do not
+        const double end = pad + (s > 1 && k.store < 2 ? 2 : k.store);
+        double t = (s == 1 && k.store < 2 ? 2 : 0) + (double)full * (piece * (k.idle + k.load) + end);
+        if (rest > 0) t += piece * (k.idle + k.load * rest / k.slots) + end;
         if (t < bytes / k.rate) t = bytes / k.rate;
         if (s > 1) t += 4.0 + 2e-6 * s * (double)outputs;
         if (s > 1 && t < 6.5) t = 6.5;  // (the host's second launch)
@@ -49,7 +53,9 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
 // are streamed, otherwise 64); mx: 4-bit operands.  An expert has one row tile at least, and half a one is lost on average.
 // Measured, 8 experts, 4096 to 14336, us on row tiles of 16 / 32 / 128 / 256: 8 rows an expert 162 / 163 / 180 / 174, 16 230 / 169 / 185 / 175,
 // 32 354 / 258 / 196 / 177, 128 989 / 649 / 282 / 200; 4-bit 41 / 42 / 45 / 50, 53 / 45 / 46 / 50, 86 / 70 / 47 / 51, 242 / 172 / 76 / 65;
-// 8 experts, 1024 to 1024, 256 rows an expert: - / - / 19 / 20.
+// 8 experts, 1024 to 1024, 256 rows an expert: - / - / 19 / 20.  Short reductions, which leave most of a streamed tile's stages empty, on 16 or
+// 32 / 128: 128 experts, 88 to 3344, transposed, 1309 rows 36 / 17, 60 experts, 64 to 4096, 300 rows 23 / 18, 128 experts, 512 to 2048, 600
+// rows 46 / 54.
 //
 // Tiles of 256 rows with the last round's reductions cut (a piece costs 0.11 us of memory and sum, the second launch and its end 12): surely
 // where all tiles together take half the card or less (1 expert, 14336 to 2048, 1500 rows 130 -> 105 us, 8 experts, 14336 to 1024, 3000
@@ -60,13 +66,13 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
     GroupedPlan p = {128, 1, false};
     if (rows <= 0) return p;
     const int experts = rows < E ? rows : E;
-    const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.0, 5.9e6}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, 2.2, 5.9e6},
-                                      {128, 512, 0.8, 0.4, 2.0, 5.2e6}, {256, 256, 0.9, 0.55, 4.0, 5.2e6}};
+    const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.0 : 0.2, 5.9e6, mx ? 2 : 3}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.2 : 0.4, 5.9e6, mx ? 1 : 2},
+                                      {128, 512, 0.8, 0.4, 2.0, 5.2e6, 2}, {256, 256, 0.9, 0.55, 4.0, 5.2e6, 2}};
     const double bytes = (double)experts * kbytes * N + (double)rows * (kbytes + 2.0 * N);
     double best = 0;
     for (int i = 0; i < 4; ++i) {
         const GroupedKernel& k = kernels[i];
-        if (i == 2 && !mx && rows <= 16 * experts) break;  // (a token on 4 experts, 3448 to 1440: streamed in ranges 14, on tiles in ranges 20)
+        if (i == 2 && !mx && rows <= 16 * experts && kbytes > 1024) break;  // (a token on 4 experts, 3448 to 1440: streamed in ranges 14, on tiles in ranges 20)
         int64_t row_tiles = rows / k.bm + experts / 2;
         if (row_tiles < experts) row_tiles = experts;
         const bool stream = k.bm < 128;
@@ -102,7 +108,7 @@ static inline GroupedPlan grouped_weights_plan(int rows, int E, int M, int N) {
     const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256) * E, t128 = ceil_div(M, 128) * ceil_div(N, 128) * E;
     const int experts = rows < E ? rows : E;
     const int64_t steps = experts > 0 ? ceil_div(ceil_div(rows, experts), 64) : 1;
-    const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, &p.splits);
+    const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9, 2}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, &p.splits);
     if ((t256 < 256 ? 1.0 : (double)t256 / 256) * ((double)steps * 1.5 + 7.5) < t + 1.0) p = {256, 1, false};
     return p;
 }
