@@ -163,8 +163,9 @@ struct TileList {
 // us with 4 / 6 / 12, 128 experts, 2048 x 1536 from 65528 rows 671 / 664 with 4 / 6).
 constexpr int TILE_COST = 5;
 // Time of a K step of a tile over ragged rows: a share for every quarter of its height, and one beside (the columns, the barriers and
-// most of the loads' latency: the gradient of 65536 rows of 128 experts 429 us with 4 and 14, 441 with 5 and 7).
-constexpr int QUARTER_COST = 4, STEP_COST = 14;
+// most of the loads' latency: the gradient of 65536 rows of 128 experts 429 us with 2 and 22 or 4 and 14, 441 with 5 and 7; 10432 to 3272,
+// one expert, 7748 rows, whose last round can be cut at three quarters of the height, 465 with 2 and 22, 508 with 4 and 14).
+constexpr int QUARTER_COST = 2, STEP_COST = 22;
 
 // TAIL: the last round of tiles of 256 rows seldom fills the card.  Where it takes half of an XCD's workgroups or fewer, the
 // reductions of its tiles are cut into ranges for the others too, each leaves its sums in a slot of the workspace, and a second kernel

@@ -27,19 +27,21 @@ static inline size_t grouped_workspace(const GroupedPlan& p, int64_t outputs) { 
 // The fastest cut of `tiles` tiles of `units` units each: a cut costs a second launch and a way to memory and back for its partial
 // sums (one token's reduction of 14336 over 512 columns: 71 us in one piece, 37, 23, 17, 15 in 2, 4, 8, 16; one of 1024 over 1024
 // columns 9, in two pieces 12).  Returns its time.
-static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t units, int64_t outputs, double bytes, int most, int* splits) {
+// ragged: the number of tiles is an estimate, and the last round is half full on average.
+static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t units, int64_t outputs, double bytes, int most, bool ragged, int* splits) {
     double best = 0;
     *splits = 1;
     for (int s = 1; s <= most && s <= units; ++s) {
-        if (s > 1 && ((size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE || tiles * (s - 1) >= 2 * k.slots)) break;
-        const int64_t full = tiles * s / k.slots, rest = tiles * s % k.slots;
-        const double piece = (double)ceil_div(units, s), pad = piece < k.least ? k.idle * (k.least - piece) : 0;
+        const double sums = s > 1 ? 4.0 + 2e-6 * s * (double)outputs : 0;
+        if (s > 1 && (sums >= best || (size_t)s * outputs * 4 > GROUPED_MAX_WORKSPACE || tiles * (s - 1) >= 2 * k.slots)) break;
+        const double rounds = (double)(tiles * s) / k.slots, piece = (double)(((int)units + s - 1) / s);
+        const double full = (double)(int64_t)rounds, rest = rounds - full;
         // the end of a tile: bf16 results of a streamed one leave under the next one's loads, but for the last; 32 bits do not
-        const double end = pad + (s > 1 && k.store < 2 ? 2 : k.store);
-        double t = (s == 1 && k.store < 2 ? 2 : 0) + (double)full * (piece * (k.idle + k.load) + end);
-        if (rest > 0) t += piece * (k.idle + k.load * rest / k.slots) + end;
-        if (t < bytes / k.rate) t = bytes / k.rate;
-        if (s > 1) t += 4.0 + 2e-6 * s * (double)outputs;
+        const double end = (piece < k.least ? k.idle * (k.least - piece) : 0) + (s > 1 && k.store < 2 ? 2 : k.store);
+        double t = sums + (s == 1 && k.store < 2 ? 2 : 0) + full * (piece * (k.idle + k.load) + end);
+        if (ragged && full > 0) t += rest * (piece * (k.idle + k.load) + end) + 0.5 * piece * k.idle;
+        else if (rest > 0) t += piece * (k.idle + k.load * rest) + end;
+        if (t < sums + bytes / k.rate) t = sums + bytes / k.rate;
         if (s > 1 && t < 6.5) t = 6.5;  // (the host's second launch)
         if (s == 1 || t < best) {
             best = t;
@@ -59,15 +61,16 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
 //
 // Tiles of 256 rows with the last round's reductions cut (a piece costs 0.11 us of memory and sum, the second launch and its end 12): surely
 // where all tiles together take half the card or less (1 expert, 14336 to 2048, 1500 rows 130 -> 105 us, 8 experts, 14336 to 1024, 3000
-// rows 174 -> 125; 5120 to 5120, 512 rows, where it does not pay by this reckoning, 43 -> 61), otherwise for reductions of 80 steps and more in up to
+// rows 174 -> 125; 5120 to 5120, 512 rows, where it does not pay by this reckoning, 43 -> 61), otherwise for reductions of 60 steps and more in up to
 // 12 rounds, where a round is worth the launch (14336 to 4096, 8 experts, two of them leading, 8192 rows 922 -> 845, biased, 4096 rows 561 -> 484,
-// 2 experts, 6144 to 6144, 3000 rows 237 -> 211; nothing left to cut in a last round of 8192 to 2048, 5000 rows 177 -> 180).
+// 2 experts, 6144 to 6144, 3000 rows 237 -> 211, 8 experts, 5032 to 2016, 8576 rows 257 -> 224; nothing left to cut in a last round of 8192
+// to 2048, 5000 rows 177 -> 180; 49 steps, 3128 to 1024, 8965 rows 65 -> 71).
 static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, bool row_major, bool mx) {
     GroupedPlan p = {128, 1, false};
     if (rows <= 0) return p;
     const int experts = rows < E ? rows : E;
     const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.0 : 0.2, 5.9e6, mx ? 2 : 3}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.2 : 0.4, 5.9e6, mx ? 1 : 2},
-                                      {128, 512, 0.8, 0.4, 2.0, 5.2e6, 2}, {256, 256, 0.9, 0.55, 4.0, 5.2e6, 2}};
+                                      {128, 512, 0.8, 0.4, 2.0, 5.2e6, 2}, {256, 256, 0.9, 0.55, 5.0, 5.2e6, 2}};
     const double bytes = (double)experts * kbytes * N + (double)rows * (kbytes + 2.0 * N);
     double best = 0;
     for (int i = 0; i < 4; ++i) {
@@ -80,7 +83,7 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
         const int64_t units = ceil_div(kbytes, stream ? (mx ? 1024 : row_major ? 256 : 512) : 128);
         int splits;
         bool tail = false;
-        double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, &splits);
+        double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, E > 1 && !stream, &splits);
         if (k.bm == 256 && mx) {
             // (256 of their values are a step, so few reductions are long enough: 28672 to 8192 in 5000 rows 650 -> 639 us, in 3000 434 -> 442)
         } else if (k.bm == 256 && 2 * tiles <= k.slots) {
@@ -90,7 +93,7 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
                 if (cut < t) t = cut;
             }
         } else if (k.bm == 256) {
-            tail = units >= 80 && tiles <= 12 * k.slots && (E > 1 || tiles % k.slots != 0);
+            tail = units >= 60 && tiles <= 12 * k.slots && (E > 1 || tiles % k.slots != 0);
         }
         if (i == 0 || t < best) {
             best = t;
@@ -108,7 +111,7 @@ static inline GroupedPlan grouped_weights_plan(int rows, int E, int M, int N) {
     const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256) * E, t128 = ceil_div(M, 128) * ceil_div(N, 128) * E;
     const int experts = rows < E ? rows : E;
     const int64_t steps = experts > 0 ? ceil_div(ceil_div(rows, experts), 64) : 1;
-    const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9, 2}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, &p.splits);
+    const double t = grouped_cut({128, 512, 1.0, 0.0, 4.0, 1e9, 2}, t128, steps, (int64_t)E * M * N, 0, GROUPED_MAX_SPLITS, false, &p.splits);
     if ((t256 < 256 ? 1.0 : (double)t256 / 256) * ((double)steps * 1.5 + 7.5) < t + 1.0) p = {256, 1, false};
     return p;
 }
