@@ -2,6 +2,7 @@
 // of each expert is on the device, so the rules go by the bound on the rows and by their mean.  Times in microseconds, fitted to
 // calls of 1 to 65536 rows on 1 to 128 experts.
 #pragma once
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -20,6 +21,9 @@ constexpr size_t GROUPED_MAX_WORKSPACE = (size_t)64 << 20;
 struct GroupedKernel { int bm, slots; double idle, load, store, rate; int least; };
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Experts that have rows, on average over rows that pick one each (against min(rows, E): 32 experts, 13624 to 1600, 32 rows 187 -> 162 us).
+static inline int grouped_experts(int rows, int E) { return E == 1 || rows < 1 ? 1 : (int)(E * (1.0 - pow(1.0 - 1.0 / E, rows)) + 0.5); }
 
 // Bytes of workspace a plan needs.
 static inline size_t grouped_workspace(const GroupedPlan& p, int64_t outputs) { return p.tail ? (size_t)256 * 256 * 256 * 4 : p.splits > 1 ? (size_t)p.splits * outputs * 4 : 0; }
@@ -68,7 +72,7 @@ static inline double grouped_cut(const GroupedKernel& k, int64_t tiles, int64_t 
 static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, bool row_major, bool mx) {
     GroupedPlan p = {128, 1, false};
     if (rows <= 0) return p;
-    const int experts = rows < E ? rows : E;
+    const int experts = grouped_experts(rows, E);
     const GroupedKernel kernels[4] = {{16, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.0 : 0.2, 5.9e6, mx ? 2 : 3}, {32, 256, mx ? 1.2 : 0.63, mx ? 0.73 : 0.72, mx ? 2.2 : 0.4, 5.9e6, mx ? 1 : 2},
                                       {128, 512, 0.8, 0.4, 2.0, 5.2e6, 2}, {256, 256, 0.9, 0.55, 5.0, 5.2e6, 2}};
     const double bytes = (double)experts * kbytes * N + (double)rows * (kbytes + 2.0 * N);
