@@ -88,6 +88,7 @@ static inline GroupedPlan grouped_rows_plan(int rows, int E, int kbytes, int N, 
         int splits;
         bool tail = false;
         double t = grouped_cut(k, tiles, units, (int64_t)rows * N, bytes, k.bm < 256 ? GROUPED_MAX_SPLITS : 1, E > 1 && !stream, &splits);
+        if (!stream) t += 1.5;  // (the list of tiles: 8 experts, 128 to 512, 128 rows in a graph 5.6 us streamed, 7.1 on tiles)
         if (k.bm == 256 && mx) {
             // (256 of their values are a step, so few reductions are long enough: 28672 to 8192 in 5000 rows 650 -> 639 us, in 3000 434 -> 442)
         } else if (k.bm == 256 && 2 * tiles <= k.slots) {
