@@ -557,11 +557,11 @@ static __device__ inline void store_lines(const f32x4_t (&acc)[FM][FN], const Si
 // Why 256 x 256: a K step of it is 64 KB for 8.4 MFLOP (bf16), two stages fit LDS, sums and fragments the 256 registers a lane
 // has at eight waves, and a compute unit asks its L2 for 43 bytes a nanosecond at the rate below; 128 x 128 needs twice that.
 // What bounds it: one product of 8192^3 the power (1400 TFLOP/s forward, 1430 gradient of the rows, 1385 of the weights, 4-bit
-// 4330; MFMA instructions alone sustain 1948).  Ragged rows on many experts the loads, which the L2s fetch 1.2 to 2.6 times, and the steps'
-// barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 845 us = 1138 TFLOP/s (whole last round: 922),
-// the gradient of 65536 rows of 128 experts, 1536 to 2048, 414 us = 995 TFLOP/s (matrix pipes busy 57 % of the time), 4-bit 8192 rows, 4096 to 28672, 555 us
-// = 3470 TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of 128 experts' weights, 2048 x 1536 in fp32 from 65528
-// rows, memory: 659 us for 0.93 GB read and 1.62 GB written = 3.9 TB/s.
+// 4330; MFMA instructions alone sustain 1948).  Ragged rows on many experts the loads, of which the L2s fetch 1.3 to 2.1 times what
+// there is, and the steps' barriers behind them: 8192 rows, 14336 to 4096, two of 8 experts leading 831 us = 1160 TFLOP/s (with its last
+// round whole 920; matrix pipes busy 65 % of the time), the gradient of 65536 rows of 128 experts, 1536 to 2048, 425 us = 970
+// TFLOP/s (56 %), 4-bit 8192 rows, 4096 to 28672, 545 us = 3530 TFLOP/s (45 %; its 0.47 GB of results alone take 92 us).  The gradient of
+// 128 experts' weights, 2048 x 1536 in fp32 from 65528 rows, memory: 617 us for 0.74 GB read and 1.61 GB written = 3.8 TB/s.
 template <int FMT, int LA, int LB, int OUT, int BM, int BN, int WM, int WN, bool TAIL, bool LINES>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs g) {
     constexpr int NW = WM * WN, FH = BM / WM / 32, FN = BN / WN / 16, NLA = BM / 16 / NW, NLB = BN / 8 / NW;
