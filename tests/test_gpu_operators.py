@@ -76,6 +76,22 @@ def test_grouped_gemm_whole_numbers_exactly(rows, K, N, transpose_w):
     assert got.dtype == BF16 and torch.equal(got.cpu(), ref_gemm(x, w, off, transpose_w).to(BF16))
 
 
+@pytest.mark.parametrize("K,N", [(264, 520), (72, 64), (1032, 1544)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("ahead", [32, 16, 8])
+def test_grouped_wgrad_into_memory_aligned_otherwise(K, N, dtype, ahead):
+    """Results that begin 16 bytes and more behind a multiple of 64, in rows that do and do not keep to it; what lies
+    before and behind them stays."""
+    rows = [300, 0, 45]
+    off = offsets_of(rows)
+    x, dy = whole((int(off[-1]), K), -2, 2, 13), whole((int(off[-1]), N), -2, 2, 14)
+    flat = torch.full((ahead + len(rows) * K * N + 32,), 7.0, dtype=dtype, device="cuda")
+    out = flat[ahead:ahead + len(rows) * K * N].view(len(rows), K, N)
+    moe.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), off.cuda(), out=out)
+    assert torch.equal(out.cpu(), ref_wgrad(x, dy, off).to(dtype))
+    assert (flat[:ahead] == 7).all() and (flat[ahead + out.numel():] == 7).all()
+
+
 # long reductions in a few of the largest tiles, or in a round of them and a few more: the last ones are cut into ranges
 LONG = [
     ([4500], 8200, 520, 0),
@@ -106,6 +122,30 @@ def test_grouped_gemm_long_reductions_of_few_tiles(rows, K, N, more, transpose_w
             ref = torch.mm(x[a:b].double(), (w[e].t().contiguous() if transpose_w else w[e]).double())
             assert torch.equal(got[a:b], ref.to(BF16)), e
     assert (got[n:] == 7).all() and (torch.as_strided(out, (n + more, 8), (N + 8, 1), N) == 7).all()
+
+
+def test_grouped_gemm_cut_reductions_in_a_graph():
+    """A graph of calls whose reductions are cut, replayed after its inputs have changed."""
+    rows, K, N = [1300, 0, 1700], 8200, 1000
+    off = offsets_of(rows).cuda()
+    n = int(off[-1])
+    x, w = whole((n, K), -2, 2, 15).cuda(), whole((len(rows), K, N), -2, 2, 16).cuda()
+    one = whole((2, K), -2, 2, 17).cuda()
+    few = torch.tensor([0, 1, 1, 2], dtype=torch.int32, device="cuda")
+    moe.moe_grouped_gemm(x, w, off)
+    moe.moe_grouped_gemm(one, w, few)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, z = moe.moe_grouped_gemm(x, w, off), moe.moe_grouped_gemm(one, w, few)
+    for seed in range(3):
+        x.copy_(whole((n, K), -2, 2, 30 + seed))
+        one.copy_(whole((2, K), -2, 2, 40 + seed))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, moe.moe_grouped_gemm(x, w, off)) and torch.equal(z, moe.moe_grouped_gemm(one, w, few))
+        assert torch.equal(y[:1300].cpu(), ref_gemm(x[:1300].cpu(), w[:1].cpu(), off[:2].cpu(), False).to(BF16))
 
 
 @pytest.mark.parametrize("rows,K,N", SHAPES)
