@@ -183,8 +183,8 @@ moe_status moe_layer_forward(moe_ctx* ctx, const void* x, const void* router_pac
 typedef enum { MOE_BF16 = 0, MOE_F32 = 1 } moe_type;
 
 /* The grouped products take a workspace of at least the bytes that their *_workspace_bytes functions give for the same sizes (0: it may be
- * NULL): partial sums where a long reduction of few tiles is cut into ranges.  16-byte aligned, used until the call's work is
- * done; calls that may overlap need one each. */
+ * NULL; 64 MiB at the most): partial sums where a long reduction of few tiles, or of the last ones, is cut into ranges.  16-byte
+ * aligned, used until the call's work is done; calls that may overlap need one each. */
 
 /* y[r, :] = x[r, :] . W[e] for the rows r of every expert e: bf16 operands, fp32 sums, bf16 results rounded once.
  * W is [E, K, N] (transpose_w == 0; the layout of W1, W3 and W2) or [E, N, K] (transpose_w != 0: x times W[e]^T).  The
