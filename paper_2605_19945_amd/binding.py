@@ -307,7 +307,8 @@ def moe_permute_noalloc(x, topk_idx, E, e_lo=0, E_local=-1, xp=None, offsets=Non
 # ---- operators around the experts' weights (no context) -----------------------------------------------
 # Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.  Small calls are bound by this
 # code, so each one first asks whether all is as it should be, in one expression, and only otherwise goes through the
-# checks one by one, which find what to say or let an unusual layout pass (a product 7.6 -> 6.3 us of host time, SwiGLU 6.6 -> 5.4).
+# checks one by one, which find what to say or let an unusual layout pass, such as a single row, whose distance to the next one means
+# nothing (a product 7.6 -> 6.3 us of host time, SwiGLU 6.6 -> 5.4).
 def _refuse(what, why):
     raise MoEError(1, f"{what}: {why}")
 
@@ -406,9 +407,9 @@ def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
     if transpose_w:
         K, N, t = N, K, 1
     (rows, width), (ldx, step), dev = x.shape, x.stride(), x.get_device()
-    if not (x.dtype is _BF16 and w.dtype is _BF16 and offsets.dtype is _I32T and width == K and step == 1 and ldx >= K
-            and w.is_contiguous() and offsets.shape == (E + 1,) and offsets.is_contiguous() and dev >= 0 and w.get_device() == dev
-            and offsets.get_device() == dev and _device() == dev):
+    if not (x.dtype is _BF16 and w.dtype is _BF16 and offsets.dtype is _I32T and width == K and step == 1
+            and (ldx == K or ldx > K and rows > 1) and w.is_contiguous() and offsets.shape == (E + 1,) and offsets.is_contiguous()
+            and dev >= 0 and w.get_device() == dev and offsets.get_device() == dev and _device() == dev):
         ldx, dev = _grouped_checked(what, x, K, w, E, offsets, out)
     if out is None:
         out, ldy = x.new_empty(rows, N), N
@@ -461,7 +462,8 @@ def moe_swiglu(gu, offsets=None, out=None):
     (rows, f2), (ldgu, step), dev = gu.shape, gu.stride(), gu.get_device()
     if f2 & 1:
         _refuse(what, "gu has to have an even number of columns")
-    if not (gu.dtype is _BF16 and step == 1 and ldgu >= f2 and dev >= 0 and _device() == dev) or offsets is not None:
+    if not (gu.dtype is _BF16 and step == 1 and (ldgu == f2 or ldgu > f2 and rows > 1) and dev >= 0
+            and _device() == dev) or offsets is not None:
         ldgu, dev = _rows(what, "gu", gu, _BF16), _launch_device(what, gu, offsets, out)
     f = f2 >> 1
     if out is None:
@@ -483,8 +485,9 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     if dh.dim() != 2 or gu.dim() != 2:
         _refuse(what, "dh and gu have to be matrices")
     (rows, f), (lddh, s1), (ldgu, s2), dev = dh.shape, dh.stride(), gu.stride(), gu.get_device()
-    if not (dh.dtype is _BF16 and gu.dtype is _BF16 and s1 == 1 and s2 == 1 and lddh >= f and ldgu >= 2 * f and gu.shape == (rows, 2 * f)
-            and dev >= 0 and dh.get_device() == dev and _device() == dev) or offsets is not None:
+    if not (dh.dtype is _BF16 and gu.dtype is _BF16 and s1 == 1 and s2 == 1 and gu.shape == (rows, 2 * f)
+            and (lddh == f or lddh > f and rows > 1) and (ldgu == 2 * f or ldgu > 2 * f and rows > 1) and dev >= 0
+            and dh.get_device() == dev and _device() == dev) or offsets is not None:
         lddh, ldgu = _rows(what, "dh", dh, _BF16), _rows(what, "gu", gu, _BF16, 2 * f)
         if gu.shape[0] != rows:
             _refuse(what, "dh and gu have to have as many rows")
@@ -573,7 +576,8 @@ def moe_mxfp4_quantize(x, offsets=None):
         _refuse(what, "x has to be a matrix")
     f32 = x.dtype is _F32
     (rows, K), (ldx, step), dev = x.shape, x.stride(), x.get_device()
-    if not ((f32 or x.dtype is _BF16) and step == 1 and ldx >= K and dev >= 0 and _device() == dev) or offsets is not None:
+    if not ((f32 or x.dtype is _BF16) and step == 1 and (ldx == K or ldx > K and rows > 1) and dev >= 0
+            and _device() == dev) or offsets is not None:
         ldx, dev = _rows(what, "x", x, _F32 if f32 else _BF16), _launch_device(what, x, offsets)
     cols = _workspace_bytes("moe_mxfp4_scale_cols", K)
     if cols == 0:

@@ -1,0 +1,54 @@
+"""How the operators around the experts' weights are called: layouts that have to pass, what a call leaves behind, and what
+it does to its arguments."""
+import pytest
+import torch
+
+import paper_2605_19945_amd as moe
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def whole(shape, seed, dtype=BF16):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-2, 3, shape, generator=g).to(dtype).cuda()
+
+
+# ---- single rows ----
+def alone(t, beside):
+    """The same row as a view whose distance to a next row, which there is none, is `beside` values larger than the row."""
+    view = torch.full((1, t.shape[1] + beside), 7.0, dtype=t.dtype, device="cuda")[:, :t.shape[1]]
+    view.copy_(t)
+    assert view.stride() == (t.shape[1] + beside, 1)
+    return view
+
+
+@pytest.mark.parametrize("beside", [1, 4, 13, 1 << 21])  # no multiples of what rows are apart, and more than they may be
+def test_the_distance_to_a_row_that_is_not_there_does_not_count(beside):
+    K, N, f = 64, 40, 72
+    x, w, off = whole((1, K), 1), whole((2, K, N), 2), torch.tensor([0, 0, 1], dtype=torch.int32).cuda()
+    wt = w.transpose(1, 2).contiguous()
+    gu, dh, dy = whole((1, 2 * f), 3), whole((1, f), 4), whole((1, N), 5)
+    v = alone(x, beside)
+    assert torch.equal(moe.moe_grouped_gemm(v, w, off), moe.moe_grouped_gemm(x, w, off))
+    assert torch.equal(moe.moe_grouped_gemm(v, wt, off, transpose_w=True), moe.moe_grouped_gemm(x, w, off))
+    assert torch.equal(moe.moe_grouped_gemm_wgrad(v, alone(dy, beside), off), moe.moe_grouped_gemm_wgrad(x, dy, off))
+    assert torch.equal(moe.moe_swiglu(alone(gu, beside)), moe.moe_swiglu(gu))
+    for a, b in ((alone(dh, beside), gu), (dh, alone(gu, beside)), (alone(dh, beside), alone(gu, beside))):
+        assert torch.equal(moe.moe_swiglu_backward(a, b), moe.moe_swiglu_backward(dh, gu))
+    for t in (x, x.float()):
+        for got, want in zip(moe.moe_mxfp4_quantize(alone(t, beside)), moe.moe_mxfp4_quantize(t)):
+            assert torch.equal(got, want)
+    out = alone(whole((1, N), 6), beside)
+    assert moe.moe_grouped_gemm(x, w, off, out=out) is out and torch.equal(out, moe.moe_grouped_gemm(x, w, off))
+
+
+@pytest.mark.parametrize("shape", [(64, 13), (64, 4)])
+def test_more_rows_at_such_a_distance_are_refused(shape):
+    K, beside = shape
+    off = torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    x = torch.zeros((2, K + beside), dtype=BF16, device="cuda")[:, :K]
+    for call in (lambda: moe.moe_grouped_gemm(x, whole((2, K, 40), 2), off), lambda: moe.moe_swiglu(x), lambda: moe.moe_mxfp4_quantize(x)):
+        with pytest.raises(moe.MoEError):
+            call()
