@@ -521,18 +521,20 @@ def _grad_list(what, tensors):
 def _norm_of(what, tensors, devices, call):
     n = _workspace_bytes("moe_grad_norm_workspace_bytes", len(tensors))
     if tensors:
-        dev = _launch_device(what, tensors[0])
-        if len(devices) > 1:
+        like = tensors[0]
+        dev = like.get_device()
+        if len(devices) > 1 or dev < 0 or _device() != dev:
+            _launch_device(what, like)
             _refuse(what, "tensors have to be on one device")
-        ws = tensors[0].new_empty(n // 4 + 1, dtype=_F32)  # the norm lies behind the workspace
     else:
         dev = torch.cuda.current_device()
-        ws = torch.empty(n // 4 + 1, dtype=_F32, device=torch.device("cuda", dev))
-    at = ws.data_ptr()
-    st = call(at, n, at + n, _stream_of(dev))
+        like = torch.empty(0, device=torch.device("cuda", dev))
+    # (memory of its own for the norm: programs keep it longer than the workspace)
+    ws, norm = like.new_empty(n, dtype=_U8), like.new_empty((), dtype=_F32)
+    st = call(ws.data_ptr(), n, norm.data_ptr(), _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return ws.select(0, n // 4)
+    return norm
 
 
 def moe_grad_norm(grads):

@@ -52,3 +52,13 @@ def test_more_rows_at_such_a_distance_are_refused(shape):
     for call in (lambda: moe.moe_grouped_gemm(x, whole((2, K, 40), 2), off), lambda: moe.moe_swiglu(x), lambda: moe.moe_mxfp4_quantize(x)):
         with pytest.raises(moe.MoEError):
             call()
+
+
+# ---- what a call leaves behind ----
+def test_a_norm_that_is_kept_keeps_nothing_else():
+    """A program that keeps the norm of every step keeps 4 bytes a step, not a workspace."""
+    for n in (0, 1, 129):
+        grads = [torch.ones(3 + i, device="cuda") for i in range(n)]
+        for norm in (moe.moe_grad_norm(grads), moe.moe_clip_grad_norm(grads, 1e9)):
+            assert norm.dim() == 0 and norm.dtype == F32 and norm.untyped_storage().nbytes() == 4
+            assert abs(float(norm) - sum(3 + i for i in range(n)) ** 0.5) < 1e-4
