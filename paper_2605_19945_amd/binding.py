@@ -14,7 +14,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libmoe_gfx950.so"
 _lib = None
 torch = None  # set by load_library (the mapping search and the argument checks need neither)
-_BF16 = _F32 = _I32T = _U8 = _device = _stream_of = None  # torch's types, current device and raw stream, set with it
+_BF16 = _F32 = _I32T = _U8 = _device = _stream_of = _wrote = None  # torch's types, current device, raw stream and note of a write, set with it
 
 FLAG_STAGE_EVENTS = 1
 STAGE_NAMES = ("route", "permute", "gemm1", "gemm2", "combine")
@@ -100,7 +100,7 @@ def exported_symbols():
 
 def load_library():
     """Loads libmoe_gfx950.so from the package directory.  Raises if it has not been built."""
-    global _lib, torch, _BF16, _F32, _I32T, _U8, _device, _stream_of
+    global _lib, torch, _BF16, _F32, _I32T, _U8, _device, _stream_of, _wrote
     if _lib is not None:
         return _lib
     # PyTorch ships its own HIP runtime; import it first so that the library binds to that one
@@ -108,6 +108,7 @@ def load_library():
     import torch
     _BF16, _F32, _I32T, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
     _device, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    _wrote = torch.autograd.graph.increment_version  # (a saved tensor that a call writes over is then noticed)
     path = library_path()
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2605_19945_amd.build` "
@@ -411,17 +412,20 @@ def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
             and (ldx == K or ldx > K and rows > 1) and w.is_contiguous() and offsets.shape == (E + 1,) and offsets.is_contiguous()
             and dev >= 0 and w.get_device() == dev and offsets.get_device() == dev and _device() == dev):
         ldx, dev = _grouped_checked(what, x, K, w, E, offsets, out)
+    y = out
     if out is None:
-        out, ldy = x.new_empty(rows, N), N
+        y, ldy = x.new_empty(rows, N), N
     else:
         ldy = _out_rows(what, "out", out, rows, N)
         _launch_device(what, x, out)
     ws, at, n = _workspace(x, "moe_grouped_gemm_workspace_bytes", rows, E, K, N, t)
-    st = lib.moe_grouped_gemm(x.data_ptr(), ldx, w.data_ptr(), t, offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n,
+    st = lib.moe_grouped_gemm(x.data_ptr(), ldx, w.data_ptr(), t, offsets.data_ptr(), rows, E, K, N, y.data_ptr(), ldy, at, n,
                               _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return out
+    if out is not None:
+        _wrote(out)
+    return y
 
 
 def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=False):
@@ -443,14 +447,17 @@ def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=Fals
     elif dtype not in (None, _F32, _BF16):
         _refuse(what, "dtype has to be float32 or bfloat16")
     dev = _launch_device(what, x, dy, offsets, out)
+    dw = out
     if out is None:
-        out = x.new_empty((max(E, 0), K, N), dtype=dtype or _F32)
+        dw = x.new_empty((max(E, 0), K, N), dtype=dtype or _F32)
     ws, at, n = _workspace(x, "moe_grouped_gemm_wgrad_workspace_bytes", rows, E, K, N)
-    st = lib.moe_grouped_gemm_wgrad(x.data_ptr(), ldx, dy.data_ptr(), lddy, offsets.data_ptr(), rows, E, K, N, out.data_ptr(),
-                                    1 if out.dtype is _F32 else 0, 1 if accumulate else 0, at, n, _stream_of(dev))
+    st = lib.moe_grouped_gemm_wgrad(x.data_ptr(), ldx, dy.data_ptr(), lddy, offsets.data_ptr(), rows, E, K, N, dw.data_ptr(),
+                                    1 if dw.dtype is _F32 else 0, 1 if accumulate else 0, at, n, _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return out
+    if out is not None:
+        _wrote(out)
+    return dw
 
 
 def moe_swiglu(gu, offsets=None, out=None):
@@ -466,15 +473,18 @@ def moe_swiglu(gu, offsets=None, out=None):
             and _device() == dev) or offsets is not None:
         ldgu, dev = _rows(what, "gu", gu, _BF16), _launch_device(what, gu, offsets, out)
     f = f2 >> 1
+    h = out
     if out is None:
-        out, ldh = gu.new_empty(rows, f), f
+        h, ldh = gu.new_empty(rows, f), f
     else:
         ldh = _out_rows(what, "out", out, rows, f)
         _launch_device(what, gu, out)
-    st = lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), ldh, _stream_of(dev))
+    st = lib.moe_swiglu(gu.data_ptr(), ldgu, live, rows, f, h.data_ptr(), ldh, _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return out
+    if out is not None:
+        _wrote(out)
+    return h
 
 
 def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
@@ -496,15 +506,20 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     if h is not None:
         ldh, at = _out_rows(what, "h", h, rows, f), h.data_ptr()
         _launch_device(what, gu, h)
+    dgu = out
     if out is None:
-        out, lddgu = gu.new_empty(rows, 2 * f), 2 * f
+        dgu, lddgu = gu.new_empty(rows, 2 * f), 2 * f
     else:
         lddgu = _out_rows(what, "out", out, rows, 2 * f)
         _launch_device(what, gu, out)
-    st = lib.moe_swiglu_backward(dh.data_ptr(), lddh, gu.data_ptr(), ldgu, live, rows, f, out.data_ptr(), lddgu, at, ldh, _stream_of(dev))
+    st = lib.moe_swiglu_backward(dh.data_ptr(), lddh, gu.data_ptr(), ldgu, live, rows, f, dgu.data_ptr(), lddgu, at, ldh, _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return out
+    if out is not None:
+        _wrote(out)
+    if h is not None:
+        _wrote(h)
+    return dgu
 
 
 def _grad_list(what, tensors):
@@ -552,14 +567,17 @@ def moe_clip_grad_norm(grads, max_norm, out=None):
     lib, what = _lib or load_library(), "moe_clip_grad_norm"
     grads = list(grads)
     ptrs, counts, types, devices = _grad_list(what, grads)
-    outs = ptrs
+    outs, targets = ptrs, grads
     if out is not None:
-        outs, n_out, out_types, others = _grad_list(what, list(out))
+        targets = list(out)
+        outs, n_out, out_types, others = _grad_list(what, targets)
         devices |= others
         if n_out != counts or out_types != types:
             _refuse(what, "out has to hold as many tensors of the same types and sizes")
     a = [v.buffer_info()[0] for v in (ptrs, outs, counts, types)]
-    return _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
+    norm = _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
+    _wrote(targets)
+    return norm
 
 
 def _mx_pair(what, t, lead, K):
@@ -646,17 +664,20 @@ def moe_mxfp4_grouped_gemm(x_values, x_scales, w_values, w_scales, offsets, out=
             _refuse(what, "x and w have to have the same K")
         _groups(what, offsets, E)
         dev = _launch_device(what, x_values, x_scales, w_values, w_scales, offsets)
+    y = out
     if out is None:
-        out, ldy = x_values.new_empty(rows, N, dtype=_BF16), N
+        y, ldy = x_values.new_empty(rows, N, dtype=_BF16), N
     else:
         ldy = _out_rows(what, "out", out, rows, N)
         _launch_device(what, x_values, out)
     ws, at, n = _workspace(x_values, "moe_mxfp4_grouped_gemm_workspace_bytes", rows, E, K, N)
     st = lib.moe_mxfp4_grouped_gemm(x_values.data_ptr(), x_scales.data_ptr(), w_values.data_ptr(), w_scales.data_ptr(),
-                                    offsets.data_ptr(), rows, E, K, N, out.data_ptr(), ldy, at, n, _stream_of(dev))
+                                    offsets.data_ptr(), rows, E, K, N, y.data_ptr(), ldy, at, n, _stream_of(dev))
     if st != 0:
         raise MoEError(st, what)
-    return out
+    if out is not None:
+        _wrote(out)
+    return y
 
 
 # ---- host-side mapping search (no context, no GPU) ------------------------------------------------

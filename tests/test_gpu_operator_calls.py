@@ -62,3 +62,52 @@ def test_a_norm_that_is_kept_keeps_nothing_else():
         for norm in (moe.moe_grad_norm(grads), moe.moe_clip_grad_norm(grads, 1e9)):
             assert norm.dim() == 0 and norm.dtype == F32 and norm.untyped_storage().nbytes() == 4
             assert abs(float(norm) - sum(3 + i for i in range(n)) ** 0.5) < 1e-4
+
+
+# ---- what torch knows of a tensor that a call has written ----
+def written(out, call):
+    before, other = out._version, out.clone()._version
+    call(out)
+    assert out._version > before and other == 0
+
+
+def test_tensors_that_a_call_writes_count_as_changed():
+    K, N, f = 64, 40, 72
+    x, w, off, dy = whole((3, K), 1), whole((2, K, N), 2), torch.tensor([0, 1, 3], dtype=torch.int32).cuda(), whole((3, N), 3)
+    gu, dh = whole((3, 2 * f), 4), whole((3, f), 5)
+    xq, wq = moe.moe_mxfp4_quantize(x), moe.moe_mxfp4_quantize_weights(w)
+    written(torch.zeros_like(dy), lambda out: moe.moe_grouped_gemm(x, w, off, out=out))
+    written(torch.zeros(2, K, N, device="cuda"), lambda out: moe.moe_grouped_gemm_wgrad(x, dy, off, out=out))
+    written(torch.zeros(2, K, N, device="cuda"), lambda out: moe.moe_grouped_gemm_wgrad(x, dy, off, out=out, accumulate=True))
+    written(torch.zeros_like(dh), lambda out: moe.moe_swiglu(gu, out=out))
+    written(torch.zeros_like(gu), lambda out: moe.moe_swiglu_backward(dh, gu, out=out))
+    written(torch.zeros_like(dh), lambda out: moe.moe_swiglu_backward(dh, gu, h=out))
+    written(torch.zeros_like(dy), lambda out: moe.moe_mxfp4_grouped_gemm(*xq, *wq, off, out=out))
+    written(torch.ones(5, device="cuda"), lambda out: moe.moe_clip_grad_norm([out], 1.0))
+    written(torch.ones(5, device="cuda"), lambda out: moe.moe_clip_grad_norm([torch.ones(5, device="cuda")], 1.0, out=[out]))
+    for t in (x, w, off, dy, gu, dh, *xq, *wq):
+        before = t._version
+        moe.moe_grouped_gemm(x, w, off)
+        moe.moe_swiglu_backward(dh, gu)
+        moe.moe_mxfp4_grouped_gemm(*xq, *wq, off)
+        assert t._version == before
+
+
+def test_a_saved_tensor_that_is_clipped_does_not_give_wrong_gradients():
+    p = torch.ones(8, device="cuda", requires_grad=True)
+    g = torch.full((8,), 3.0, device="cuda")
+    y = (p * g).sum()   # saves g
+    moe.moe_clip_grad_norm([g], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_tensors_of_inference_mode_are_written_as_before():
+    with torch.inference_mode():
+        g, out = torch.full((4,), 3.0, device="cuda"), torch.zeros(4, device="cuda")
+    for _ in range(2):
+        moe.moe_clip_grad_norm([g], 3.0, out=[out])
+        assert torch.allclose(out, torch.full((4,), 1.5, device="cuda"))
+    with torch.inference_mode():
+        moe.moe_clip_grad_norm([g], 3.0)
+    assert torch.equal(g, out)
