@@ -5,10 +5,10 @@ PyTorch is used for device memory and streams: tensors are passed as raw device 
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
 import functools
 import os
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libmoe_gfx950.so"
@@ -522,15 +522,21 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     return dgu
 
 
+@functools.lru_cache(maxsize=64)
+def _packers(n):
+    return tuple(struct.Struct(f"={n}{c}").pack for c in "Qqi")
+
+
 def _grad_list(what, tensors):
-    """Host arrays of the addresses, sizes and types of a list of gradients, and their devices.  (map over the unbound
-    methods: a list of a thousand tensors is bound by this.)"""
+    """Host arrays (bytes) of the addresses, sizes and types of a list of gradients, and their devices.  (map over the unbound
+    methods, and struct instead of array: a list of a thousand tensors is bound by this.)"""
     T, f32 = torch.Tensor, torch.float32
     types = [t.dtype for t in tensors]
     if not all(map(T.is_contiguous, tensors)) or not {f32, torch.bfloat16}.issuperset(types):
         _refuse(what, "gradients have to be contiguous tensors of float32 or bfloat16")
-    return (array.array("Q", map(T.data_ptr, tensors)), array.array("q", map(T.numel, tensors)),
-            array.array("i", [t is f32 for t in types]), set(map(T.get_device, tensors)))
+    pointers, sizes, flags = _packers(len(types))
+    return (pointers(*map(T.data_ptr, tensors)), sizes(*map(T.numel, tensors)), flags(*[t is f32 for t in types]),
+            set(map(T.get_device, tensors)))
 
 
 def _norm_of(what, tensors, devices, call):
@@ -557,8 +563,7 @@ def moe_grad_norm(grads):
     lib, what = _lib or load_library(), "moe_grad_norm"
     grads = list(grads)
     ptrs, counts, types, devices = _grad_list(what, grads)
-    a = [v.buffer_info()[0] for v in (ptrs, counts, types)]
-    return _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_grad_norm(*a, len(grads), ws, n, norm, st))
+    return _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_grad_norm(ptrs, counts, types, len(grads), ws, n, norm, st))
 
 
 def moe_clip_grad_norm(grads, max_norm, out=None):
@@ -574,8 +579,8 @@ def moe_clip_grad_norm(grads, max_norm, out=None):
         devices |= others
         if n_out != counts or out_types != types:
             _refuse(what, "out has to hold as many tensors of the same types and sizes")
-    a = [v.buffer_info()[0] for v in (ptrs, outs, counts, types)]
-    norm = _norm_of(what, grads, devices, lambda ws, n, norm, st: lib.moe_clip_grad_norm(*a, len(grads), max_norm, ws, n, norm, st))
+    norm = _norm_of(what, grads, devices,
+                    lambda ws, n, norm, st: lib.moe_clip_grad_norm(ptrs, outs, counts, types, len(grads), max_norm, ws, n, norm, st))
     _wrote(targets)
     return norm
 
