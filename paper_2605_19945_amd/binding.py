@@ -306,12 +306,19 @@ def moe_permute_noalloc(x, topk_idx, E, e_lo=0, E_local=-1, xp=None, offsets=Non
 
 
 # ---- operators around the experts' weights (no context) -----------------------------------------------
-# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides.  Small calls are bound by this
+# Tensors are checked here for what the C entry points cannot see: type, device, shape, strides, and whether torch would lose a
+# gradient (no call records a graph; norms and clipping, like torch's, and 4-bit codes have none to lose).  Small calls are bound by this
 # code, so each one first asks whether all is as it should be, in one expression, and only otherwise goes through the
 # checks one by one, which find what to say or let an unusual layout pass, such as a single row, whose distance to the next one means
 # nothing (a product 7.6 -> 6.3 us of host time, SwiGLU 6.6 -> 5.4).
 def _refuse(what, why):
     raise MoEError(1, f"{what}: {why}")
+
+
+def _no_graph(what):
+    """A call was given tensors that require gradients: it would lose them where torch records a graph."""
+    if torch.is_grad_enabled():
+        _refuse(what, "the operators record no graph: pass detached tensors, or call them under torch.no_grad()")
 
 
 def _launch_device(what, t, *others):
@@ -403,6 +410,8 @@ def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
     if w.dim() != 3 or x.dim() != 2:
         _grouped_checked(what, x, None, w, -1, offsets, out)
         _refuse(what, "w has to have three dimensions, x two")
+    if x.requires_grad or w.requires_grad or out is not None and out.requires_grad:
+        _no_graph(what)
     E, K, N = w.shape
     t = 0
     if transpose_w:
@@ -432,6 +441,8 @@ def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=Fals
     """dw[e] = x[r].T @ dy[r] summed over the rows r of expert e: [E, K, N] of `dtype` (fp32, the default, or bf16).
     accumulate: add to `out` (fp32)."""
     lib, what = _lib or load_library(), "moe_grouped_gemm_wgrad"
+    if x.requires_grad or dy.requires_grad or out is not None and out.requires_grad:
+        _no_graph(what)
     ldx, lddy = _rows(what, "x", x, _BF16), _rows(what, "dy", dy, _BF16)
     rows, K = x.shape
     if dy.shape[0] != rows:
@@ -463,6 +474,8 @@ def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=Fals
 def moe_swiglu(gu, offsets=None, out=None):
     """silu(gu[:, :f]) * gu[:, f:] (bf16).  offsets: rows from its last value on are left as they are."""
     lib, what = _lib or load_library(), "moe_swiglu"
+    if gu.requires_grad or out is not None and out.requires_grad:
+        _no_graph(what)
     live = None if offsets is None else _live(what, offsets)
     if gu.dim() != 2:
         _refuse(what, "gu has to be a matrix")
@@ -491,6 +504,8 @@ def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     """The gradient of gu [rows, 2f] from that of moe_swiglu's result.  h: a matrix [rows, f] that gets that result
     again.  out may be gu itself."""
     lib, what = _lib or load_library(), "moe_swiglu_backward"
+    if dh.requires_grad or gu.requires_grad or out is not None and out.requires_grad or h is not None and h.requires_grad:
+        _no_graph(what)
     live = None if offsets is None else _live(what, offsets)
     if dh.dim() != 2 or gu.dim() != 2:
         _refuse(what, "dh and gu have to be matrices")
@@ -559,7 +574,7 @@ def _norm_of(what, tensors, devices, call):
 
 
 def moe_grad_norm(grads):
-    """Norm over all values of a list of gradients (float32 or bfloat16), as a tensor on the GPU."""
+    """Norm over all values of a list of gradients (float32 or bfloat16), as a tensor on the GPU.  Records no graph."""
     lib, what = _lib or load_library(), "moe_grad_norm"
     grads = list(grads)
     ptrs, counts, types, devices = _grad_list(what, grads)
@@ -568,7 +583,7 @@ def moe_grad_norm(grads):
 
 def moe_clip_grad_norm(grads, max_norm, out=None):
     """Scales the gradients by min(1, max_norm / (norm + 1e-6)) in place, or into the tensors of `out` (of the same
-    types and sizes, overlapping nothing).  Returns the norm before, as a tensor on the GPU."""
+    types and sizes, overlapping nothing).  Returns the norm before, as a tensor on the GPU.  Records no graph."""
     lib, what = _lib or load_library(), "moe_clip_grad_norm"
     grads = list(grads)
     ptrs, counts, types, devices = _grad_list(what, grads)
@@ -654,6 +669,8 @@ def moe_mxfp4_dequantize(values, scales):
 def moe_mxfp4_grouped_gemm(x_values, x_scales, w_values, w_scales, offsets, out=None):
     """y[r] = x[r] @ w[e].T on 4-bit rows [n, K / 2] and weights [E, N, K / 2] with their scales; bf16 [n, N]."""
     lib, what = _lib or load_library(), "moe_mxfp4_grouped_gemm"
+    if out is not None and out.requires_grad:
+        _no_graph(what)
     if x_values.dim() != 2 or w_values.dim() != 3:
         _refuse(what, "x_values has to have two dimensions, w_values three")
     (rows, half), (E, N, w_half), dev = x_values.shape, w_values.shape, x_values.get_device()
