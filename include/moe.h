@@ -174,7 +174,8 @@ moe_status moe_layer_forward(moe_ctx* ctx, const void* x, const void* router_pac
  * These calls need no context.  Pointers are device memory unless marked "host"; matrices are row-major with rows
  * `ld*` values apart (a multiple of 8 bf16 or 4 fp32 values, at most 2^21), every base pointer 16-byte aligned.
  * Widths (K, N, f) are multiples of 8 (K of 32 for 4-bit values), at most 2^17; E <= 256.  A call only launches
- * kernels on `stream`.  Tensors without rows may be NULL.
+ * kernels on `stream`.  Tensors without rows may be NULL.  Outputs share no byte with inputs or with each other but where a call
+ * says so (MOE_ERR_INVALID_ARG); views into the same wider rows, side by side, are no such case.  Workspaces share none with anything.
  *
  * Rows grouped by expert lie as moe_permute leaves them: expert e has rows [offsets[e], offsets[e+1]), offsets [E+1] is
  * read on the device, n_rows_cap (<= 2^24) is the host's bound on offsets[E] and sizes the launch.  Rows from offsets[E] on are
@@ -204,12 +205,14 @@ moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, in
                                   int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /* h = silu(g) * u with g = gu[:, :f], u = gu[:, f:2f] (bf16).  n_rows: NULL, or the number of rows there are on the device
- * (e.g. offsets + E), at most n_rows_cap; later rows are left alone.  gu [n_rows_cap, 2f], h [n_rows_cap, f]. */
+ * (e.g. offsets + E), at most n_rows_cap; later rows are left alone.  gu [n_rows_cap, 2f], h [n_rows_cap, f].  h may lie in the place of
+ * g or of u. */
 moe_status moe_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int32_t n_rows_cap, int32_t f, void* h,
                       int64_t ldh, void* stream);
 
 /* Gradient of moe_swiglu: dgu[:, :f] = dh u s(g) (1 + g (1 - s(g))), dgu[:, f:] = dh g s(g), s the logistic function.
- * h NULL, or the rows of moe_swiglu formed again (a program then need not keep them).  dgu may be gu itself. */
+ * h NULL, or the rows of moe_swiglu formed again (a program then need not keep them).  dgu may be gu itself; each half of it, and h, may lie
+ * in the place of dh, g or u. */
 moe_status moe_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int64_t ldgu, const int32_t* n_rows,
                                int32_t n_rows_cap, int32_t f, void* dgu, int64_t lddgu, void* h, int64_t ldh, void* stream);
 

@@ -405,7 +405,8 @@ def _grouped_checked(what, x, K, w, E, offsets, out):
 
 def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
     """y[r] = x[r] @ w[e] (transpose_w: @ w[e].T) for the rows r of every expert e.  x [rows, K] bf16; w [E, K, N]
-    (transpose_w: [E, N, K]) bf16; offsets [E + 1] int32.  Rows from offsets[E] on are left as they are."""
+    (transpose_w: [E, N, K]) bf16; offsets [E + 1] int32.  Rows from offsets[E] on are left as they are.
+    out shares no memory with the inputs."""
     lib, what = _lib or load_library(), "moe_grouped_gemm"
     if w.dim() != 3 or x.dim() != 2:
         _grouped_checked(what, x, None, w, -1, offsets, out)
@@ -439,7 +440,7 @@ def moe_grouped_gemm(x, w, offsets, transpose_w=False, out=None):
 
 def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=False):
     """dw[e] = x[r].T @ dy[r] summed over the rows r of expert e: [E, K, N] of `dtype` (fp32, the default, or bf16).
-    accumulate: add to `out` (fp32)."""
+    accumulate: add to `out` (fp32).  out shares no memory with the inputs."""
     lib, what = _lib or load_library(), "moe_grouped_gemm_wgrad"
     if x.requires_grad or dy.requires_grad or out is not None and out.requires_grad:
         _no_graph(what)
@@ -472,7 +473,8 @@ def moe_grouped_gemm_wgrad(x, dy, offsets, dtype=None, out=None, accumulate=Fals
 
 
 def moe_swiglu(gu, offsets=None, out=None):
-    """silu(gu[:, :f]) * gu[:, f:] (bf16).  offsets: rows from its last value on are left as they are."""
+    """silu(gu[:, :f]) * gu[:, f:] (bf16).  offsets: rows from its last value on are left as they are.  out may be gu[:, :f] or
+    gu[:, f:]."""
     lib, what = _lib or load_library(), "moe_swiglu"
     if gu.requires_grad or out is not None and out.requires_grad:
         _no_graph(what)
@@ -502,7 +504,7 @@ def moe_swiglu(gu, offsets=None, out=None):
 
 def moe_swiglu_backward(dh, gu, offsets=None, out=None, h=None):
     """The gradient of gu [rows, 2f] from that of moe_swiglu's result.  h: a matrix [rows, f] that gets that result
-    again.  out may be gu itself."""
+    again.  out may be gu itself, h may be dh or a half of gu."""
     lib, what = _lib or load_library(), "moe_swiglu_backward"
     if dh.requires_grad or gu.requires_grad or out is not None and out.requires_grad or h is not None and h.requires_grad:
         _no_graph(what)

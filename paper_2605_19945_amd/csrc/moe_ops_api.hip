@@ -1,7 +1,10 @@
 // C ABI of the operators around the experts' weights: argument checks and launches.  No kernels here.
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "moe_ops.h"
+#include "moe_overlap.h"
 
 namespace {
 
@@ -35,6 +38,20 @@ moe_status check_workspace(const void* workspace, size_t bytes, size_t need) {
     if (need == 0) return MOE_OK;
     if (bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
     return workspace == nullptr || !aligned(workspace, 16) ? MOE_ERR_INVALID_ARG : MOE_OK;
+}
+
+// An output that shares bytes with one of the others: results would depend on which workgroup ran when.
+bool over(const Rows& out, std::initializer_list<Rows> others) {
+    for (const Rows& o : others)
+        if (overlap(out, o)) return true;
+    return false;
+}
+
+// The same for calls whose lanes read what they need of a place before they write there: an output may be exactly an input.
+bool partly_over(const Rows& out, std::initializer_list<Rows> inputs) {
+    for (const Rows& i : inputs)
+        if (!same_place(out, i) && overlap(out, i)) return true;
+    return false;
 }
 
 bool grouped_shape_ok(int32_t rows, int32_t E, int32_t K, int32_t N, int unit) {
@@ -73,6 +90,8 @@ moe_status moe_grouped_gemm(const void* x, int64_t ldx, const void* w, int32_t t
     const GroupedPlan plan = grouped_rows_plan(n_rows_cap, E, K * 2, N, transpose_w == 0, false);
     st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)n_rows_cap * N));
     if (st != MOE_OK) return st;
+    if (over({y, n_rows_cap, ldy * 2, (int64_t)N * 2}, {{x, n_rows_cap, ldx * 2, (int64_t)K * 2}, {w, 1, 0, (int64_t)E * K * N * 2}, {offsets, 1, 0, (E + 1) * 4}}))
+        return MOE_ERR_INVALID_ARG;
     return from_hip(launch_grouped_gemm(x, ldx, w, transpose_w != 0, offsets, n_rows_cap, E, K, N, y, ldy, plan, workspace, (hipStream_t)stream));
 }
 
@@ -92,6 +111,9 @@ moe_status moe_grouped_gemm_wgrad(const void* x, int64_t ldx, const void* dy, in
     const GroupedPlan plan = grouped_weights_plan(n_rows_cap, E, K, N);
     st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)E * K * N));
     if (st != MOE_OK) return st;
+    if (over({dw, 1, 0, (int64_t)E * K * N * (type == MOE_F32 ? 4 : 2)},
+             {{x, n_rows_cap, ldx * 2, (int64_t)K * 2}, {dy, n_rows_cap, lddy * 2, (int64_t)N * 2}, {offsets, 1, 0, (E + 1) * 4}}))
+        return MOE_ERR_INVALID_ARG;
     return from_hip(launch_grouped_wgrad(x, ldx, dy, lddy, offsets, n_rows_cap, E, K, N, dw, type == MOE_F32, accumulate != 0, plan, workspace,
                                          (hipStream_t)stream));
 }
@@ -103,6 +125,9 @@ moe_status moe_swiglu(const void* gu, int64_t ldgu, const int32_t* n_rows, int32
     if (bad(gu, 16, n_rows_cap) || bad(h, 16, n_rows_cap)) return MOE_ERR_INVALID_ARG;
     if (bad_ld(ldgu, 2 * (int64_t)f, 8) || bad_ld(ldh, f, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
+    const Rows g(gu, n_rows_cap, ldgu * 2, (int64_t)f * 2), u((const char*)gu + (int64_t)f * 2, n_rows_cap, ldgu * 2, (int64_t)f * 2), live(n_rows, 1, 0, 4);
+    const Rows out(h, n_rows_cap, ldh * 2, (int64_t)f * 2);
+    if (partly_over(out, {g, u}) || over(out, {live})) return MOE_ERR_INVALID_ARG;
     return from_hip(launch_swiglu(gu, ldgu, n_rows, n_rows_cap, f, h, ldh, (hipStream_t)stream));
 }
 
@@ -114,6 +139,11 @@ moe_status moe_swiglu_backward(const void* dh, int64_t lddh, const void* gu, int
     if (bad_ld(lddh, f, 8) || bad_ld(ldgu, 2 * (int64_t)f, 8) || bad_ld(lddgu, 2 * (int64_t)f, 8)) return MOE_ERR_INVALID_ARG;
     if (h != nullptr && bad_ld(ldh, f, 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
+    const int64_t n = n_rows_cap, width = (int64_t)f * 2;
+    const Rows d(dh, n, lddh * 2, width), g(gu, n, ldgu * 2, width), u((const char*)gu + width, n, ldgu * 2, width), live(n_rows, 1, 0, 4);
+    const Rows dg(dgu, n, lddgu * 2, width), du((const char*)dgu + width, n, lddgu * 2, width), again(h, n, ldh * 2, width);
+    if (partly_over(dg, {d, g, u}) || partly_over(du, {d, g, u}) || partly_over(again, {d, g, u})) return MOE_ERR_INVALID_ARG;
+    if (over(again, {dg, du}) || over(live, {dg, du, again})) return MOE_ERR_INVALID_ARG;
     return from_hip(launch_swiglu_backward(dh, lddh, gu, ldgu, n_rows, n_rows_cap, f, dgu, lddgu, h, ldh, (hipStream_t)stream));
 }
 
@@ -144,6 +174,9 @@ moe_status moe_mxfp4_quantize(const void* x, int32_t type, int64_t ldx, const in
     if (bad(x, 16, n_rows_cap) || bad(values, 16, n_rows_cap) || bad(scales, 16, n_rows_cap)) return MOE_ERR_INVALID_ARG;
     if (bad_ld(ldx, K, type == MOE_F32 ? 4 : 8)) return MOE_ERR_INVALID_ARG;
     if (n_rows_cap == 0) return MOE_OK;
+    const Rows q(values, 1, 0, (int64_t)n_rows_cap * (K / 2)), s(scales, 1, 0, (int64_t)n_rows_cap * mx_scale_cols(K));
+    const int64_t size = type == MOE_F32 ? 4 : 2;
+    if (over(q, {s}) || over({x, n_rows_cap, ldx * size, K * size}, {q, s}) || over({n_rows, 1, 0, 4}, {q, s})) return MOE_ERR_INVALID_ARG;
     return from_hip(launch_mx_quantize(x, type == MOE_F32, ldx, n_rows, n_rows_cap, K, values, scales, (hipStream_t)stream));
 }
 
@@ -151,6 +184,8 @@ moe_status moe_mxfp4_quantize_weights(const void* w, int32_t E, int32_t K, int32
     if (E < 1) return MOE_ERR_INVALID_ARG;
     if (E > kMaxExperts || bad_width(K, 32) || bad_width(N, 8)) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (bad(w, 16, 1) || bad(values, 16, 1) || bad(scales, 16, 1)) return MOE_ERR_INVALID_ARG;
+    const Rows q(values, 1, 0, (int64_t)E * N * (K / 2)), s(scales, 1, 0, (int64_t)E * N * mx_scale_cols(K));
+    if (over(q, {s}) || over({w, 1, 0, (int64_t)E * K * N * 2}, {q, s})) return MOE_ERR_INVALID_ARG;
     return from_hip(launch_mx_quantize_weights(w, E, K, N, values, scales, (hipStream_t)stream));
 }
 
@@ -159,6 +194,7 @@ moe_status moe_mxfp4_dequantize(const void* values, const void* scales, int64_t 
     if (bad_width(K, 32)) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (bad(values, 16, rows) || bad(scales, 16, rows) || bad(x, 16, rows) || bad_ld(ldx, K, 8)) return MOE_ERR_INVALID_ARG;
     if (rows == 0) return MOE_OK;
+    if (over({x, rows, ldx * 2, (int64_t)K * 2}, {{values, 1, 0, rows * (K / 2)}, {scales, 1, 0, rows * mx_scale_cols(K)}})) return MOE_ERR_INVALID_ARG;
     return from_hip(launch_mx_dequantize(values, scales, rows, K, x, ldx, (hipStream_t)stream));
 }
 
@@ -177,6 +213,10 @@ moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, co
     const GroupedPlan plan = grouped_rows_plan(n_rows_cap, E, K / 2, N, false, true);
     st = check_workspace(workspace, workspace_bytes, grouped_workspace(plan, (int64_t)n_rows_cap * N));
     if (st != MOE_OK) return st;
+    const int64_t cols = mx_scale_cols(K);
+    if (over({y, n_rows_cap, ldy * 2, (int64_t)N * 2}, {{x_values, 1, 0, (int64_t)n_rows_cap * (K / 2)}, {x_scales, 1, 0, n_rows_cap * cols},
+                                                      {w_values, 1, 0, (int64_t)E * N * (K / 2)}, {w_scales, 1, 0, (int64_t)E * N * cols}, {offsets, 1, 0, (E + 1) * 4}}))
+        return MOE_ERR_INVALID_ARG;
     return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, plan, workspace, (hipStream_t)stream));
 }
 

@@ -111,3 +111,47 @@ def test_tensors_of_inference_mode_are_written_as_before():
     with torch.inference_mode():
         moe.moe_clip_grad_norm([g], 3.0)
     assert torch.equal(g, out)
+
+
+# ---- outputs in the place of inputs, beside them, and over them ----
+def test_outputs_beside_and_in_the_place_of_inputs():
+    rows, K, N, f = 37, 64, 40, 72
+    off = torch.tensor([0, 20, rows], dtype=torch.int32).cuda()
+    x, w, gu, dh = whole((rows, K), 1), whole((2, K, N), 2), whole((rows, 2 * f), 3), whole((rows, f), 4)
+    wide = torch.full((rows, K + N + 8), 7.0, dtype=BF16, device="cuda")
+    wide[:, :K] = x
+    want = moe.moe_grouped_gemm(x, w, off)
+    moe.moe_grouped_gemm(wide[:, :K], w, off, out=wide[:, K + 8:])
+    assert torch.equal(wide[:, K + 8:], want) and torch.equal(wide[:, :K], x) and (wide[:, K:K + 8] == 7).all()
+    h, dgu = moe.moe_swiglu(gu), moe.moe_swiglu_backward(dh, gu)
+    for at in (0, f):       # over g, over u
+        t = gu.clone()
+        moe.moe_swiglu(t, out=t[:, at:at + f])
+        assert torch.equal(t[:, at:at + f], h) and torch.equal(t[:, f - at:2 * f - at], gu[:, f - at:2 * f - at])
+        t = gu.clone()
+        assert torch.equal(moe.moe_swiglu_backward(dh, t, h=t[:, at:at + f]), dgu) and torch.equal(t[:, at:at + f], h)
+    t, d = gu.clone(), dh.clone()
+    moe.moe_swiglu_backward(d, t, out=t, h=d)
+    assert torch.equal(t, dgu) and torch.equal(d, h)
+
+
+def test_outputs_over_inputs_are_refused():
+    rows, K = 30, 64
+    off = torch.tensor([0, 20, rows], dtype=torch.int32).cuda()
+    x, w, buf = whole((rows, K), 1), whole((2, K, K), 2), whole((rows + 1, 2 * K), 3)
+    xq, wq = moe.moe_mxfp4_quantize(x), moe.moe_mxfp4_quantize_weights(w)
+    over_codes = wq[0].view(-1).view(BF16)[:rows * K].view(rows, K)
+    tensors = (x, w, buf, *xq, *wq)
+    before = [t.clone() for t in tensors]
+    for call in (lambda: moe.moe_grouped_gemm(x, w, off, out=x),
+                 lambda: moe.moe_grouped_gemm(x, w, off, out=w.view(-1, K)[3:3 + rows]),
+                 lambda: moe.moe_grouped_gemm(buf[:rows, :K], w, off, out=buf[:rows, 8:8 + K]),
+                 lambda: moe.moe_grouped_gemm_wgrad(w.view(-1, K)[:rows], x, off, out=w),
+                 lambda: moe.moe_swiglu(buf[:rows], out=buf[1:, :K]),
+                 lambda: moe.moe_swiglu(buf[:rows], out=buf[:rows, 8:8 + K]),
+                 lambda: moe.moe_swiglu_backward(x, buf[:rows], out=buf[1:]),
+                 lambda: moe.moe_swiglu_backward(x, buf[:rows], out=buf[:rows], h=buf[:rows, :K]),
+                 lambda: moe.moe_mxfp4_grouped_gemm(*xq, *wq, off, out=over_codes)):
+        with pytest.raises(moe.MoEError):
+            call()
+    assert all(torch.equal(a, b) for a, b in zip(tensors, before))
