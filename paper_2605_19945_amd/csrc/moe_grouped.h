@@ -767,7 +767,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tile_kernel(GroupedArgs 
                     la[0].stop();
                     la[1].stop();
                     lb.stop();
-                    ls = 1;  // (no scales either)
+                    ls = 1;  // (one more pair of scales is asked for at the most, of this tile, which nobody reads)
                 }
             }
             const int odd = left == 1 ? 0 : (kt + 1) & 1;

@@ -8,8 +8,7 @@
 // waves.  A workgroup (one a compute unit) goes through its tiles as one stream, so the ring stays full from tile to tile.
 // Measured: two tokens on two experts, 4096 to 28672: 0.47 GB of weights in 79 us = 5.9 TB/s; 128 rows on 8 experts, the same
 // widths in 4 bits: 0.50 GB in 87 us = 5.7 TB/s.  A kernel that only reads reaches 7.1 TB/s; the rest is the first stages' latency
-// and the last tiles' unequal end.  Tiles of 32 rows with three stages in their rings instead of two take the same (8 experts, 4096 to
-// 14336, 128 rows 169 us both ways): more loads on their way are not what is missing.
+// and the last tiles' unequal end.  Rings: what 160 KB of LDS hold beside the partial sums, three stages for 16 rows, two for 32.
 #pragma once
 #include "moe_grouped.h"
 

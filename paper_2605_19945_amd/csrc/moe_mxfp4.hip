@@ -39,7 +39,7 @@ static __device__ inline uint32_t codes8(const float* v, const BlockScale& b) {
     return c;
 }
 
-// Rows: four lanes a block, 8 values a lane.  One more item in a row for every 4 blocks writes the zeros behind the last scale.
+// Rows: four lanes for every scale byte, 8 values a lane; those of the bytes behind the last block have no values and write zeros.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const char* x, int64_t ldx, const int32_t* n_rows, int rows, int K, int S,
                                                                uint8_t* q, uint8_t* s) {
