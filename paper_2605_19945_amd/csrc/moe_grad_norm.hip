@@ -119,7 +119,7 @@ template <bool NT, typename T> static __device__ inline double sum_part(const T*
 template <bool NT, typename T> static __device__ inline void scale_part(const T* g, T* o, int64_t from, int64_t to, float scale) {
     constexpr int PER = Words<T>::PER;
     const int64_t skew = ((uintptr_t)(g + from) & 15) / sizeof(T);
-    const bool alike = (((uintptr_t)g ^ (uintptr_t)o) & 15) == 0;
+    const bool alike = (((uintptr_t)g ^ (uintptr_t)o) & 15) == 0;  // (otherwise value by value)
     const int64_t a = alike ? min(to, from + (skew ? PER - skew : 0)) : to, b = a + (to - a) / PER * PER;
     for (int64_t j = from + threadIdx.x; j < a; j += kThreads) Words<T>::put(o + j, Words<T>::get(g + j) * scale);
     auto put = [&](int64_t i, const u32x4_t& w) {

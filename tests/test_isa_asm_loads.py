@@ -4,7 +4,8 @@ The kernels load from memory into LDS with buffer instructions in asm blocks, wh
 into.  Checked on the compiled code, following branches:
 * a vector-memory instruction reads a scalar register 5 wait states at the earliest after a vector instruction has written it
   (the descriptors end in v_readfirstlane, and spilled scalars come back through v_readlane);
-* the register m0, which says where in LDS, is set one wait state at the least before the load;
+* the register m0, which says where in LDS, is set one wait state at the least before the load, and nothing outside the asm blocks
+  reads or writes it (the compiler is not told that they do);
 * the loads have no output registers, so nothing in flight can be overwritten or copied too early."""
 import os
 import re
@@ -104,6 +105,13 @@ def find_odd_loads(lines):
     return bad
 
 
+def find_other_uses_of_m0(lines):
+    ins, _ = instructions(lines)
+    return [f"line {line}: {op} {ops}" for op, ops, asm, line in ins
+            if not asm and (any(re.search(r"\bm0\b", o) for o in ops) or op.startswith(("v_movrel", "s_movrel", "s_set_gpr_idx", "ds_gws", "v_interp"))
+                            or "load_lds" in op or (op.startswith(("buffer_load", "global_load")) and any(o.endswith(" lds") for o in ops)))]
+
+
 LOAD = ["\t;;#ASMSTART", "\ts_mov_b32 m0, s9", "\ts_nop 0", "\tbuffer_load_dwordx4 v1, s[4:7], 0 offen lds", "\t;;#ASMEND"]
 
 
@@ -126,6 +134,13 @@ def test_lint_flags_an_odd_load():
     assert len(find_odd_loads([LOAD[0], LOAD[1], LOAD[3], LOAD[4]])) == 1
     assert len(find_odd_loads([LOAD[0], "\tglobal_load_dwordx4 v[10:13], v1, s[2:3]", LOAD[4]])) == 1
     assert len(find_odd_loads(LOAD[:3] + ["\tbuffer_load_dwordx4 v[10:13], v1, s[4:7], 0 offen", LOAD[4]])) == 1
+
+
+def test_lint_flags_other_uses_of_m0():
+    assert find_other_uses_of_m0(LOAD) == []
+    for other in ("s_mov_b32 m0, s3", "s_add_i32 s4, m0, s5", "v_movrels_b32_e32 v3, v4", "s_set_gpr_idx_on s4, gpr_idx(SRC0)", "s_sendmsg_m0 m0",
+                  "buffer_load_dword v1, s[4:7], 0 offen lds", "global_load_lds_dwordx4 v[2:3], off"):
+        assert len(find_other_uses_of_m0(LOAD + [other])) == 1, other
 
 
 @pytest.fixture(scope="module")
@@ -153,6 +168,8 @@ def test_no_hazard_around_the_loads_of_the_compiled_kernels(grouped_unit_asm):
         assert n > 50 and not young, f"{unit}:\n" + "\n".join(young[:10])
         odd = find_odd_loads(lines)
         assert not odd, f"{unit}:\n" + "\n".join(odd[:10])
+        others = find_other_uses_of_m0(lines)
+        assert not others, f"{unit}:\n" + "\n".join(others[:10])
 
 
 def test_every_unit_with_loads_of_this_kind_is_looked_at():
