@@ -255,6 +255,47 @@ moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, co
                                   const int32_t* offsets, int32_t n_rows_cap, int32_t E, int32_t K, int32_t N, void* y,
                                   int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- norms around a block ------------------------------------------------------------------------------------------
+ *
+ * What stands before a layer and behind it on the residual stream.  Rows as above, at most 2^24 of them, d values wide: a multiple of
+ * 8, at most 16384.  x_type: moe_type of the stream (x, out, their gradients); y_type: of what goes into a block and comes out of it (y, h,
+ * gates of every value, their gradients), the same as x_type or bf16 beside an fp32 stream.  Weights [d] of w_type, all of a call
+ * alike, 16-byte aligned; NULL: ones.  Gradients of weights [d] are fp32 sums in a fixed order.  n_rows as in moe_swiglu: later rows are left
+ * alone and add nothing.  Sums over a row are in 32 bits (as in any such norm a row whose squares pass their range has the factor 0);
+ * each result is rounded once.  A row that holds a NaN spoils that row and the weights' gradients, no other one.
+ * Row-shaped outputs may each lie exactly in the place of a row-shaped input. */
+
+/* h = x r w with r = 1 / sqrt(mean over the row of x^2 + eps).  eps >= 0.  h is of h_type (as y_type above). */
+moe_status moe_rms_norm(const void* x, int32_t x_type, int64_t ldx, const void* w, int32_t w_type, float eps, const int32_t* n_rows,
+                        int32_t n_rows_cap, int32_t d, void* h, int32_t h_type, int64_t ldh, void* stream);
+
+/* Its gradient: dx = dres + r (p - x r^2 mean(p x)) with p = dh w, dw = sum over the rows of dh x r.  dres (of x_type): NULL, or the
+ * gradient that x has by another way.  dw: NULL: not wanted.  workspace: moe_norm_backward_workspace_bytes bytes (the same for both
+ * gradients below), 16-byte aligned, used until the call's work is done; NULL where no gradient of weights is wanted. */
+size_t moe_norm_backward_workspace_bytes(int32_t n_rows_cap, int32_t d);
+moe_status moe_rms_norm_backward(const void* dh, int32_t h_type, int64_t lddh, const void* x, int32_t x_type, int64_t ldx, const void* w,
+                                 int32_t w_type, float eps, const void* dres, int64_t lddres, const int32_t* n_rows, int32_t n_rows_cap,
+                                 int32_t d, void* dx, int64_t lddx, float* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A block's end: n = y w, or y r_y w where norm != 0 (r_y of y's rows as above);  out = scale x + gate n;  h = out r_out w_next, the norm
+ * of the block behind, taken before out is rounded.  gate: NULL (1); [n_rows_cap] fp32, a number for each row (ldgate 0); or
+ * [n_rows_cap, d] of y_type (ldgate > 0).  h NULL: out alone. */
+moe_status moe_residual_norm(const void* x, int32_t x_type, int64_t ldx, const void* y, int32_t y_type, int64_t ldy, const void* w,
+                             int32_t w_type, int32_t norm, const void* gate, int64_t ldgate, float scale, const void* w_next, float eps,
+                             const int32_t* n_rows, int32_t n_rows_cap, int32_t d, void* out, int64_t ldout, void* h, int64_t ldh,
+                             void* stream);
+
+/* Its gradients, of out (dout, x_type; NULL: zeros) and of h (dh, y_type; NULL: h was not asked for, out is then not read):
+ *   D = dout + r (p - out r^2 mean(p out)) with p = dh w_next and r of out's rows;  dx = scale D;
+ *   dn = gate D;  dy = r_y (q - y r_y^2 mean(q y)) with q = dn w (without a norm: dy = q);  dgate = D n, summed over the row where the gate
+ *   is the row's;  dw = sum over the rows of dn y r_y;  dw_next = sum of dh out r.
+ * dgate (as gate, fp32 [n_rows_cap] or y_type with rows lddgate apart), dw, dw_next: NULL: not wanted. */
+moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const void* dh, int64_t lddh, const void* out, int32_t x_type,
+                                      int64_t ldout, const void* y, int32_t y_type, int64_t ldy, const void* w, int32_t w_type, int32_t norm,
+                                      const void* gate, int64_t ldgate, float scale, const void* w_next, float eps, const int32_t* n_rows,
+                                      int32_t n_rows_cap, int32_t d, void* dx, int64_t lddx, void* dy, int64_t lddy, void* dgate,
+                                      int64_t lddgate, float* dw, float* dw_next, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- introspection --------------------------------------------------------------------------- */
 
 /* Mean milliseconds of each stage over the moe_layer_forward calls made since the previous

@@ -26,4 +26,8 @@ from .binding import (  # noqa: F401
     moe_mxfp4_quantize_weights,
     moe_mxfp4_dequantize,
     moe_mxfp4_grouped_gemm,
+    moe_rms_norm,
+    moe_rms_norm_backward,
+    moe_residual_norm,
+    moe_residual_norm_backward,
 )

@@ -90,6 +90,15 @@ _SIGNATURES = {
     "moe_mxfp4_dequantize": (C.c_int, [_VP, _VP, _I64, _I32, _VP, _I64, _VP]),
     "moe_mxfp4_grouped_gemm_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
     "moe_mxfp4_grouped_gemm": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _SZ, _VP]),
+    "moe_rms_norm": (C.c_int, [_VP, _I32, _I64, _VP, _I32, C.c_float, _VP, _I32, _I32, _VP, _I32, _I64, _VP]),
+    "moe_norm_backward_workspace_bytes": (_SZ, [_I32, _I32]),
+    "moe_rms_norm_backward": (C.c_int, [_VP, _I32, _I64, _VP, _I32, _I64, _VP, _I32, C.c_float, _VP, _I64, _VP, _I32, _I32, _VP, _I64,
+                                        _VP, _VP, _SZ, _VP]),
+    "moe_residual_norm": (C.c_int, [_VP, _I32, _I64, _VP, _I32, _I64, _VP, _I32, _I32, _VP, _I64, C.c_float, _VP, C.c_float, _VP, _I32,
+                                    _I32, _VP, _I64, _VP, _I64, _VP]),
+    "moe_residual_norm_backward": (C.c_int, [_VP, _I64, _VP, _I64, _VP, _I32, _I64, _VP, _I32, _I64, _VP, _I32, _I32, _VP, _I64,
+                                             C.c_float, _VP, C.c_float, _VP, _I32, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP,
+                                             _SZ, _VP]),
     "moe_layer_intermediates": (C.c_int, [_VP, C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP)]),
 }
 
@@ -702,6 +711,216 @@ def moe_mxfp4_grouped_gemm(x_values, x_scales, w_values, w_scales, offsets, out=
     if out is not None:
         _wrote(out)
     return y
+
+
+# ---- norms around a block ----
+def _norm_matrix(what, name, t, rows, d, dtype=None):
+    """Values between the rows of t [rows, d], float32 or bfloat16."""
+    if t.dtype not in (_F32, _BF16) or (dtype is not None and t.dtype is not dtype):
+        _refuse(what, f"{name} has to be of {dtype or 'float32 or bfloat16'}")
+    ld = _rows(what, name, t, t.dtype, d)
+    if t.shape[0] != rows:
+        _refuse(what, f"{name} has to have {rows} rows")
+    return ld
+
+
+def _norm_weights(what, d, *weights):
+    """Type of the weights [d], which have to agree (None: ones)."""
+    dtype = None
+    for w in weights:
+        if w is None:
+            continue
+        if w.dtype not in (_F32, _BF16) or (dtype is not None and w.dtype is not dtype):
+            _refuse(what, "weights have to be float32 or bfloat16, all alike")
+        dtype = w.dtype
+        if w.shape != (d,) or not w.is_contiguous():
+            _refuse(what, f"weights have to be contiguous vectors of {d} values")
+    return 0 if dtype is _BF16 else 1
+
+
+def _norm_types(what, stream, block):
+    if stream not in (_F32, _BF16) or not (block is stream or block is _BF16):
+        _refuse(what, "streams are float32 or bfloat16; what goes into and comes out of a block has their type or is bfloat16")
+
+
+def _no_graphs(what, *tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return _no_graph(what)
+
+
+def _gate_of(what, gate, rows, d, block):
+    """(address, values between its rows; 0: a number for each row) of a gate or its gradient."""
+    if gate is None:
+        return None, 0
+    if gate.dim() == 1:
+        _whole(what, "a gate of rows", gate, _F32, (rows,))
+        return gate.data_ptr(), 0
+    return gate.data_ptr(), _norm_matrix(what, "a gate of values", gate, rows, d, block)
+
+
+def moe_rms_norm(x, weight=None, eps=1e-6, offsets=None, out=None, dtype=None):
+    """x / sqrt(mean(x^2) + eps) * weight for every row of x [rows, d] (float32 or bfloat16), of `dtype`: x's, the default, or bfloat16.
+    offsets: rows from its last value on are left as they are.  out may be x."""
+    lib, what = _lib or load_library(), "moe_rms_norm"
+    if x.requires_grad or weight is not None and weight.requires_grad or out is not None and out.requires_grad:
+        _no_graph(what)
+    live = None if offsets is None else _live(what, offsets)
+    if x.dim() != 2:
+        _refuse(what, "x has to be a matrix")
+    (rows, d), (ldx, step), dev, stream = x.shape, x.stride(), x.get_device(), x.dtype
+    block = dtype or (out.dtype if out is not None else stream)
+    wide = weight is None or weight.dtype is _F32
+    if not ((stream is _BF16 or stream is _F32) and (block is stream or block is _BF16) and step == 1 and (ldx == d or ldx > d and rows > 1)
+            and dev >= 0 and _device() == dev and (weight is None or (wide or weight.dtype is _BF16) and weight.shape == (d,)
+                                                   and weight.is_contiguous() and weight.get_device() == dev)) or offsets is not None:
+        ldx = _norm_matrix(what, "x", x, rows, d)
+        _norm_types(what, stream, block)
+        _norm_weights(what, d, weight)
+        dev = _launch_device(what, x, weight, offsets, out)
+    h, ldh = out, d
+    if out is None:
+        h = x.new_empty(rows, d, dtype=block)
+    else:
+        ldh = _norm_matrix(what, "out", out, rows, d, block)
+        _launch_device(what, x, out)
+    st = lib.moe_rms_norm(x.data_ptr(), 1 if stream is _F32 else 0, ldx, None if weight is None else weight.data_ptr(), 1 if wide else 0, eps,
+                          live, rows, d, h.data_ptr(), 1 if block is _F32 else 0, ldh, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    if out is not None:
+        _wrote(out)
+    return h
+
+
+def moe_rms_norm_backward(dh, x, weight=None, eps=1e-6, dres=None, offsets=None, out=None):
+    """(gradient of x, gradient of the weight in float32; None without a weight) from that of moe_rms_norm's result.  dres: what x gets by another
+    way (the residual's), added.  out: where the gradient of x goes; it may be dh, x or dres."""
+    lib, what = _lib or load_library(), "moe_rms_norm_backward"
+    _no_graphs(what, dh, x, weight, dres, out)
+    live = None if offsets is None else _live(what, offsets)
+    if x.dim() != 2:
+        _refuse(what, "x has to be a matrix")
+    rows, d = x.shape
+    ldx, lddh = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "dh", dh, rows, d)
+    _norm_types(what, x.dtype, dh.dtype)
+    wt = _norm_weights(what, d, weight)
+    lddres = 0 if dres is None else _norm_matrix(what, "dres", dres, rows, d, x.dtype)
+    dev = _launch_device(what, x, dh, weight, dres, offsets, out)
+    dx, lddx = out, d
+    if out is None:
+        dx = x.new_empty(rows, d)
+    else:
+        lddx = _norm_matrix(what, "out", out, rows, d, x.dtype)
+    dw, at, ws, n = None, None, None, 0
+    if weight is not None:
+        dw = x.new_empty(d, dtype=_F32)
+        ws, at, n = _workspace(x, "moe_norm_backward_workspace_bytes", rows, d)
+    st = lib.moe_rms_norm_backward(dh.data_ptr(), 1 if dh.dtype is _F32 else 0, lddh, x.data_ptr(), 1 if x.dtype is _F32 else 0, ldx,
+                                   None if weight is None else weight.data_ptr(), wt, eps, None if dres is None else dres.data_ptr(), lddres,
+                                   live, rows, d, dx.data_ptr(), lddx, None if dw is None else dw.data_ptr(), at, n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    if out is not None:
+        _wrote(out)
+    return dx, dw
+
+
+def moe_residual_norm(x, y, weight=None, norm=True, gate=None, scale=1.0, next_weight=None, eps=1e-6, offsets=None, out=None, h=None):
+    """The end of a block: n = y * weight, with `norm` y / sqrt(mean(y^2) + eps) * weight; out = scale * x + gate * n; and, with
+    next_weight, h = out / sqrt(mean(out^2) + eps) * next_weight, what the next block begins with.  Returns (out, h), h None without
+    next_weight.  x [rows, d] is the residual stream, y the block's output (of x's type or bfloat16); gate [rows] float32 or [rows, d] of
+    y's type.  offsets: rows from its last value on are left as they are.  out and h may each be x, y or a gate of values."""
+    lib, what = _lib or load_library(), "moe_residual_norm"
+    _no_graphs(what, x, y, weight, gate, next_weight, out, h)
+    live = None if offsets is None else _live(what, offsets)
+    if x.dim() != 2:
+        _refuse(what, "x has to be a matrix")
+    rows, d = x.shape
+    stream, block = x.dtype, y.dtype
+    ldx, ldy = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "y", y, rows, d)
+    _norm_types(what, stream, block)
+    wt = _norm_weights(what, d, weight, next_weight)
+    gate_at, ldgate = _gate_of(what, gate, rows, d, block)
+    dev = _launch_device(what, x, y, weight, gate, next_weight, offsets, out, h)
+    if h is not None and next_weight is None:
+        _refuse(what, "h needs next_weight")
+    o, ldo, n, ldh = out, d, h, d
+    if out is None:
+        o = x.new_empty(rows, d)
+    else:
+        ldo = _norm_matrix(what, "out", out, rows, d, stream)
+    if h is not None:
+        ldh = _norm_matrix(what, "h", h, rows, d, block)
+    elif next_weight is not None:
+        n = y.new_empty(rows, d)
+    st = lib.moe_residual_norm(x.data_ptr(), 1 if stream is _F32 else 0, ldx, y.data_ptr(), 1 if block is _F32 else 0, ldy,
+                               None if weight is None else weight.data_ptr(), wt, 1 if norm else 0, gate_at, ldgate, scale,
+                               None if next_weight is None else next_weight.data_ptr(), eps, live, rows, d, o.data_ptr(), ldo,
+                               None if n is None else n.data_ptr(), ldh, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    if out is not None:
+        _wrote(out)
+    if h is not None:
+        _wrote(h)
+    return o, n
+
+
+def moe_residual_norm_backward(dout, y, weight=None, out=None, dh=None, norm=True, gate=None, scale=1.0, next_weight=None, eps=1e-6,
+                               offsets=None, dx=None, dy=None):
+    """Gradients (of x, y, weight, next_weight, gate) from those of moe_residual_norm's results: dout [rows, d] of the stream's type (None:
+    zeros) and dh (with next_weight, which needs `out`, the stream that moe_residual_norm returned; None: h was not used).  Weights' gradients
+    are float32; where there is no weight or gate, None.  dx and dy: where the first two go; they may be dout, dh, out, y or a gate of
+    values, not each other."""
+    lib, what = _lib or load_library(), "moe_residual_norm_backward"
+    _no_graphs(what, dout, y, weight, out, dh, gate, next_weight, dx, dy)
+    live = None if offsets is None else _live(what, offsets)
+    if y.dim() != 2:
+        _refuse(what, "y has to be a matrix")
+    if (dh is None) != (next_weight is None):
+        _refuse(what, "dh and next_weight come together")
+    if dh is not None and out is None:
+        _refuse(what, "dh needs out")
+    if dout is None and dh is None:
+        _refuse(what, "dout or dh has to be there")
+    rows, d = y.shape
+    block, stream = y.dtype, (dout if dout is not None else out).dtype
+    ldy = _norm_matrix(what, "y", y, rows, d)
+    _norm_types(what, stream, block)
+    lddout = 0 if dout is None else _norm_matrix(what, "dout", dout, rows, d, stream)
+    ldo, lddh = (0, 0) if dh is None else (_norm_matrix(what, "out", out, rows, d, stream), _norm_matrix(what, "dh", dh, rows, d, block))
+    wt = _norm_weights(what, d, weight, next_weight)
+    gate_at, ldgate = _gate_of(what, gate, rows, d, block)
+    dev = _launch_device(what, y, dout, weight, out, dh, gate, next_weight, offsets, dx, dy)
+    gx, lddx, gy, lddy = dx, d, dy, d
+    if dx is None:
+        gx = y.new_empty(rows, d, dtype=stream)
+    else:
+        lddx = _norm_matrix(what, "dx", dx, rows, d, stream)
+    if dy is None:
+        gy = y.new_empty(rows, d)
+    else:
+        lddy = _norm_matrix(what, "dy", dy, rows, d, block)
+    dgate = None if gate is None else gate.new_empty(gate.shape)
+    dw = None if weight is None else y.new_empty(d, dtype=_F32)
+    dnext = None if next_weight is None else y.new_empty(d, dtype=_F32)
+    ws, at, n = (None, None, 0) if dw is None and dnext is None else _workspace(y, "moe_norm_backward_workspace_bytes", rows, d)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+
+    st = lib.moe_residual_norm_backward(ptr(dout), lddout, ptr(dh), lddh, ptr(out) if dh is not None else None, 1 if stream is _F32 else 0, ldo,
+                                        y.data_ptr(), 1 if block is _F32 else 0, ldy, ptr(weight), wt, 1 if norm else 0, gate_at, ldgate, scale,
+                                        ptr(next_weight), eps, live, rows, d, gx.data_ptr(), lddx, gy.data_ptr(), lddy, ptr(dgate), d, ptr(dw),
+                                        ptr(dnext), at, n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    if dx is not None:
+        _wrote(dx)
+    if dy is not None:
+        _wrote(dy)
+    return gx, gy, dw, dnext, dgate
 
 
 # ---- host-side mapping search (no context, no GPU) ------------------------------------------------

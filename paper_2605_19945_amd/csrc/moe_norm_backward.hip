@@ -1,0 +1,209 @@
+// Gradients of the norms around a block (moe_norm.hip).  With o the row that the next norm took, p = dh w_next, r its factor:
+//   D = dout + r (p - o r^2 mean(p o)),  dx = scale D,  dw_next = sum over rows of dh o r;
+// and of the join, with n = y r_y w, dn = gate D and q = dn w:
+//   dy = r_y (q - y r_y^2 mean(q y))  (without a norm: q),  dw = sum over rows of dn y r_y,  dgate = D n (its row's sum where the gate is a
+//   row's number).
+// A row's factors come from the rows themselves again, in the same sums as the means, so the forward pass leaves nothing but its
+// results.  Memory bounds it.  The gradients of weights are summed over a workgroup's rows in registers, over the workgroup in LDS and
+// over the workgroups by a second kernel, each in a fixed order.
+#include "moe_norm.h"
+
+namespace {
+
+template <typename S, typename B, int W, int CH, bool JOIN, bool NEXT>
+__global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(NormGradArgs a) {
+    __shared__ float lds[2][8][4];
+    extern __shared__ float sums[];  // [d] where a workgroup has several rows
+    constexpr int ROWS = 8 / W;
+    const int group = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+    const int rows = a.n_rows != nullptr ? min(max(*a.n_rows, 0), a.rows) : a.rows;
+    const float over_d = 1.f / (float)a.d;
+    float dw[JOIN ? CH : 1][8] = {}, dnext[NEXT ? CH : 1][8] = {};
+    int turn = 0;
+    for (int base = blockIdx.x * ROWS; base < rows; base += gridDim.x * ROWS) {
+        const int64_t row = base + group;
+        const bool live = row < rows;
+        float D[CH][8], o[NEXT ? CH : 1][8], dh[NEXT ? CH : 1][8], y[JOIN ? CH : 1][8], g[JOIN ? CH : 1][8], gate = 1.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * 64 * W + lane) * 8;
+            const bool here = live && col < a.d;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) D[c][j] = 0.f;
+            if (here && a.dout != nullptr) Eight<S>::load((const S*)a.dout + row * a.lddout + col, D[c]);
+            if constexpr (NEXT) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[c][j] = dh[c][j] = 0.f;
+                if (here) Eight<S>::load((const S*)a.o + row * a.ldo + col, o[c]);
+                if (here) Eight<B>::load((const B*)a.dh + row * a.lddh + col, dh[c]);
+            }
+            if constexpr (JOIN) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[c][j] = 0.f, g[c][j] = 1.f;
+                if (here) Eight<B>::load((const B*)a.y + row * a.ldy + col, y[c]);
+                if (here && a.ldgate != 0) Eight<B>::load((const B*)a.gate + row * a.ldgate + col, g[c]);
+            }
+        }
+        if (JOIN && a.gate != nullptr && a.ldgate == 0 && live) gate = ((const float*)a.gate)[row];
+        float s[3] = {0.f, 0.f, 0.f};  // sums of o^2, p o and y^2
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * 64 * W + lane) * 8;
+            if constexpr (NEXT) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 1.f;
+                if (a.w_next != nullptr && col < a.d) load_weights(a.w_next, a.w_f32, col, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    s[0] = fmaf(o[c][j], o[c][j], s[0]);
+                    s[1] = fmaf(dh[c][j] * w[j], o[c][j], s[1]);
+                }
+            }
+            if constexpr (JOIN) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[2] = fmaf(y[c][j], y[c][j], s[2]);
+            }
+        }
+        if (NEXT || a.norm) group_sums<W>(s, lds, turn);
+        const float r = rsqrtf(fmaf(s[0], over_d, a.eps)), k = r * r * r * (s[1] * over_d);
+        const float ry = JOIN && a.norm ? rsqrtf(fmaf(s[2], over_d, a.eps)) : 1.f;
+        float u[1] = {0.f};  // sum of g D w y, without the row's gate
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * 64 * W + lane) * 8;
+            if (!(live && col < a.d)) continue;
+            if constexpr (NEXT) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 1.f;
+                if (a.w_next != nullptr) load_weights(a.w_next, a.w_f32, col, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    D[c][j] += r * (dh[c][j] * w[j]) - o[c][j] * k;
+                    dnext[c][j] = fmaf(dh[c][j], o[c][j] * r, dnext[c][j]);
+                }
+            }
+            float out[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) out[j] = JOIN ? a.scale * D[c][j] : D[c][j];
+            Eight<S>::store((S*)a.dx + row * a.lddx + col, out);
+            if constexpr (JOIN) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 1.f;
+                if (a.w != nullptr) load_weights(a.w, a.w_f32, col, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[0] = fmaf(g[c][j] * D[c][j], w[j] * y[c][j], u[0]);
+                if (a.ldgate != 0 && a.dgate != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) out[j] = D[c][j] * (y[c][j] * ry * w[j]);
+                    Eight<B>::store((B*)a.dgate + row * a.lddgate + col, out);
+                }
+            }
+        }
+        if constexpr (JOIN) {
+            const bool row_gate = a.ldgate == 0 && a.dgate != nullptr;
+            if (a.norm || row_gate) group_sums<W>(u, lds, turn);
+            if (row_gate && live && lane == 0) ((float*)a.dgate)[row] = u[0] * ry;
+            const float ky = a.norm ? ry * ry * ry * (gate * u[0] * over_d) : 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (c * 64 * W + lane) * 8;
+                if (!(live && col < a.d)) continue;
+                float w[8], out[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 1.f;
+                if (a.w != nullptr) load_weights(a.w, a.w_f32, col, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float dn = gate * g[c][j] * D[c][j];
+                    out[j] = ry * (dn * w[j]) - y[c][j] * ky;
+                    dw[c][j] = fmaf(dn, y[c][j] * ry, dw[c][j]);
+                }
+                Eight<B>::store((B*)a.dy + row * a.lddy + col, out);
+            }
+        }
+    }
+    // the workgroup's sums, its groups in their order
+    auto leave = [&](float (*v)[8], float* part) {
+        part += (int64_t)blockIdx.x * a.d;
+        if constexpr (ROWS > 1) {
+            for (int i = 0; i < ROWS; ++i) {
+                if (group == i) {
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        const int col = (c * 64 * W + lane) * 8;
+                        if (col >= a.d) continue;
+                        float t[8] = {};
+                        if (i > 0) Eight<float>::load(sums + col, t);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) t[j] += v[c][j];
+                        if (i < ROWS - 1) Eight<float>::store(sums + col, t);
+                        else Eight<float>::store(part + col, t);
+                    }
+                }
+                __syncthreads();
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (c * 64 * W + lane) * 8;
+                if (col < a.d) Eight<float>::store(part + col, v[c]);
+            }
+        }
+    };
+    if (JOIN && a.dw_part != nullptr) leave(dw, a.dw_part);
+    if (NEXT && a.dnext_part != nullptr) leave(dnext, a.dnext_part);
+}
+
+// dw = the sum of the workgroups' rows: 64 columns a workgroup, 16 lanes of 4 across and 16 ranges of the rows down, joined in LDS.
+__global__ __launch_bounds__(256) void norm_weights_kernel(const float* part0, float* out0, const float* part1, float* out1, int n, int d) {
+    __shared__ f32x4_t lds[16][16];
+    const float* part = blockIdx.y == 0 ? part0 : part1;
+    float* out = blockIdx.y == 0 ? out0 : out1;
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, col = blockIdx.x * 64 + x * 4;
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    if (col < d) {
+#pragma unroll 8
+        for (int i = y; i < n; i += 16) s += *(const f32x4_t*)(part + (int64_t)i * d + col);
+    }
+    lds[y][x] = s;
+    __syncthreads();
+    if (y == 0 && col < d) {
+        for (int i = 1; i < 16; ++i) s += lds[i][x];
+        *(f32x4_t*)(out + col) = s;
+    }
+}
+
+template <typename S, typename B> hipError_t launch(const NormGradArgs& a, int grid, hipStream_t st) {
+    return with_layout(a.d, [&](auto l) {
+        constexpr int W = decltype(l)::W, CH = decltype(l)::CH;
+        auto kernel = a.y == nullptr ? norm_backward_kernel<S, B, W, CH, false, true>
+                                     : a.dh != nullptr ? norm_backward_kernel<S, B, W, CH, true, true> : norm_backward_kernel<S, B, W, CH, true, false>;
+        kernel<<<grid, NORM_THREADS, W < 8 ? a.d * 4 : 0, st>>>(a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+int norm_grad_groups(int rows, int d) {
+    const int per = norm_rows_per_group(d), want = (rows + per - 1) / per;
+    return want < NORM_GRAD_GROUPS ? want : NORM_GRAD_GROUPS;
+}
+
+hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float* workspace, hipStream_t st) {
+    const int grid = norm_grad_groups(a.rows, a.d);
+    const bool both = dw != nullptr && dw_next != nullptr;
+    a.dw_part = dw != nullptr ? workspace : nullptr;
+    a.dnext_part = dw_next != nullptr ? workspace + (both ? (int64_t)grid * a.d : 0) : nullptr;
+    if (grid > 0) {
+        const hipError_t e = a.x_f32 ? (a.y_f32 ? launch<float, float>(a, grid, st) : launch<float, uint16_t>(a, grid, st)) : launch<uint16_t, uint16_t>(a, grid, st);
+        if (e != hipSuccess || (dw == nullptr && dw_next == nullptr)) return e;
+    }
+    if (dw == nullptr && dw_next == nullptr) return hipSuccess;
+    const float* p0 = dw != nullptr ? a.dw_part : a.dnext_part;
+    norm_weights_kernel<<<dim3((a.d + 63) / 64, both ? 2 : 1), 256, 0, st>>>(p0, dw != nullptr ? dw : dw_next, a.dnext_part, dw_next, grid, a.d);
+    return hipGetLastError();
+}

@@ -27,3 +27,29 @@ size_t grad_norm_workspace(int64_t n_tensors);
 hipError_t launch_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* f32, int n, double* partials, float* norm, hipStream_t st);
 hipError_t launch_clip_grads(const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* f32, int n, float max_norm,
                              double* partials, float* norm, hipStream_t st);
+
+// ---- norms around a block ----
+struct NormArgs {
+    const void *x, *y, *w, *w_next, *gate;  // y null: the norm of x alone; weights null: ones
+    void *out, *h;                          // h null: without the next norm
+    const int32_t* n_rows;
+    int64_t ldx, ldy, ldgate, ldout, ldh;   // ldgate 0: the gate is a number for each row, in 32 bits
+    int rows, d;
+    float scale, eps;
+    bool x_f32, y_f32, w_f32, norm;         // types of x and out, of y, h and the gate's values, of the weights; is y normalised
+};
+struct NormGradArgs {
+    const void *dout, *dh, *o, *y, *w, *w_next, *gate;  // as above; o: what the next norm took
+    void *dx, *dy, *dgate;
+    const int32_t* n_rows;
+    int64_t lddout, lddh, ldo, ldy, ldgate, lddx, lddy, lddgate;
+    float *dw_part, *dnext_part;                        // the workgroups' sums [groups, d], or null
+    int rows, d;
+    float scale, eps;
+    bool x_f32, y_f32, w_f32, norm;
+};
+constexpr int NORM_MAX_WIDTH = 16384;   // a row stays in the registers of 512 lanes
+constexpr int NORM_GRAD_GROUPS = 1024;  // workgroups of a backward launch, at most
+int norm_grad_groups(int rows, int d);
+hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float* workspace, hipStream_t st);

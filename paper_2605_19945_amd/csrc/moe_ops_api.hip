@@ -72,6 +72,19 @@ moe_status check_list(const void* const* grads, void* const* outs, bool with_out
     return MOE_OK;
 }
 
+// ---- norms around a block ----
+inline bool type_ok(int32_t t) { return t == MOE_BF16 || t == MOE_F32; }
+inline int64_t size_of(int32_t t) { return t == MOE_F32 ? 4 : 2; }
+inline bool bad_rows(const void* p, int64_t rows, int64_t ld, int64_t d, int32_t type) { return bad(p, 16, rows) || bad_ld(ld, d, type == MOE_F32 ? 4 : 8); }
+
+moe_status check_norm(int32_t x_type, int32_t y_type, const void* w, const void* w_next, int32_t w_type, float eps, const int32_t* n_rows, int32_t rows, int32_t d) {
+    if (rows < 0 || rows > kMaxRows || !aligned(n_rows, 4) || !(eps >= 0.f) || eps > 3e38f) return MOE_ERR_INVALID_ARG;
+    if (!type_ok(x_type) || !type_ok(y_type) || (x_type == MOE_BF16 && y_type == MOE_F32)) return MOE_ERR_INVALID_ARG;
+    if ((w != nullptr || w_next != nullptr) && !type_ok(w_type)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(w, 16) || !aligned(w_next, 16)) return MOE_ERR_INVALID_ARG;
+    return d < 8 || d % 8 != 0 || d > NORM_MAX_WIDTH ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -218,6 +231,106 @@ moe_status moe_mxfp4_grouped_gemm(const void* x_values, const void* x_scales, co
                                                       {w_values, 1, 0, (int64_t)E * N * (K / 2)}, {w_scales, 1, 0, (int64_t)E * N * cols}, {offsets, 1, 0, (E + 1) * 4}}))
         return MOE_ERR_INVALID_ARG;
     return from_hip(launch_grouped_mx(x_values, x_scales, w_values, w_scales, offsets, n_rows_cap, E, K, N, y, ldy, plan, workspace, (hipStream_t)stream));
+}
+
+moe_status moe_rms_norm(const void* x, int32_t x_type, int64_t ldx, const void* w, int32_t w_type, float eps, const int32_t* n_rows,
+                        int32_t n_rows_cap, int32_t d, void* h, int32_t h_type, int64_t ldh, void* stream) {
+    const moe_status st = check_norm(x_type, h_type, w, nullptr, w_type, eps, n_rows, n_rows_cap, d);
+    if (st != MOE_OK) return st;
+    const int64_t n = n_rows_cap;
+    if (bad_rows(x, n, ldx, d, x_type) || bad_rows(h, n, ldh, d, h_type)) return MOE_ERR_INVALID_ARG;
+    if (n == 0) return MOE_OK;
+    const Rows out(h, n, ldh * size_of(h_type), d * size_of(h_type));
+    if (partly_over(out, {{x, n, ldx * size_of(x_type), d * size_of(x_type)}}) || over(out, {{w, 1, 0, d * size_of(w_type)}, {n_rows, 1, 0, 4}})) return MOE_ERR_INVALID_ARG;
+    NormArgs a = {};
+    a.x = x, a.ldx = ldx, a.w_next = w, a.h = h, a.ldh = ldh, a.n_rows = n_rows, a.rows = n_rows_cap, a.d = d, a.eps = eps, a.scale = 1.f;
+    a.x_f32 = x_type == MOE_F32, a.y_f32 = h_type == MOE_F32, a.w_f32 = w_type == MOE_F32;
+    return from_hip(launch_norm(a, (hipStream_t)stream));
+}
+
+size_t moe_norm_backward_workspace_bytes(int32_t n_rows_cap, int32_t d) {
+    if (n_rows_cap < 0 || n_rows_cap > kMaxRows || d < 8 || d % 8 != 0 || d > NORM_MAX_WIDTH) return 0;
+    return (size_t)norm_grad_groups(n_rows_cap, d) * d * 4 * 2;
+}
+
+moe_status moe_rms_norm_backward(const void* dh, int32_t h_type, int64_t lddh, const void* x, int32_t x_type, int64_t ldx, const void* w,
+                                 int32_t w_type, float eps, const void* dres, int64_t lddres, const int32_t* n_rows, int32_t n_rows_cap,
+                                 int32_t d, void* dx, int64_t lddx, float* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    moe_status st = check_norm(x_type, h_type, w, nullptr, w_type, eps, n_rows, n_rows_cap, d);
+    if (st != MOE_OK) return st;
+    const int64_t n = n_rows_cap, xs = size_of(x_type), hs = size_of(h_type);
+    if (bad_rows(dh, n, lddh, d, h_type) || bad_rows(x, n, ldx, d, x_type) || bad_rows(dx, n, lddx, d, x_type) || !aligned(dw, 16)) return MOE_ERR_INVALID_ARG;
+    if (dres != nullptr && bad_rows(dres, n, lddres, d, x_type)) return MOE_ERR_INVALID_ARG;
+    if (n == 0 && dw == nullptr) return MOE_OK;
+    const size_t need = dw != nullptr ? moe_norm_backward_workspace_bytes(n_rows_cap, d) : 0;
+    st = check_workspace(workspace, workspace_bytes, need);
+    if (st != MOE_OK) return st;
+    const Rows rh(dh, n, lddh * hs, d * hs), rx(x, n, ldx * xs, d * xs), rr(dres, n, lddres * xs, d * xs), out(dx, n, lddx * xs, d * xs);
+    const Rows rw(w, 1, 0, d * size_of(w_type)), live(n_rows, 1, 0, 4), rdw(dw, 1, 0, (int64_t)d * 4), ws(need > 0 ? workspace : nullptr, 1, 0, (int64_t)need);
+    if (partly_over(out, {rh, rx, rr}) || over(out, {rw, live}) || over(rdw, {rh, rx, rr, out, rw, live}) || over(ws, {rh, rx, rr, out, rw, live, rdw})) return MOE_ERR_INVALID_ARG;
+    NormGradArgs a = {};
+    a.dout = dres, a.lddout = lddres, a.dh = dh, a.lddh = lddh, a.o = x, a.ldo = ldx, a.w_next = w, a.dx = dx, a.lddx = lddx, a.n_rows = n_rows;
+    a.rows = n_rows_cap, a.d = d, a.eps = eps, a.scale = 1.f, a.x_f32 = x_type == MOE_F32, a.y_f32 = h_type == MOE_F32, a.w_f32 = w_type == MOE_F32;
+    return from_hip(launch_norm_backward(a, nullptr, dw, (float*)workspace, (hipStream_t)stream));
+}
+
+moe_status moe_residual_norm(const void* x, int32_t x_type, int64_t ldx, const void* y, int32_t y_type, int64_t ldy, const void* w,
+                             int32_t w_type, int32_t norm, const void* gate, int64_t ldgate, float scale, const void* w_next, float eps,
+                             const int32_t* n_rows, int32_t n_rows_cap, int32_t d, void* out, int64_t ldout, void* h, int64_t ldh,
+                             void* stream) {
+    const moe_status st = check_norm(x_type, y_type, w, w_next, w_type, eps, n_rows, n_rows_cap, d);
+    if (st != MOE_OK) return st;
+    const int64_t n = n_rows_cap, xs = size_of(x_type), ys = size_of(y_type);
+    if (bad_rows(x, n, ldx, d, x_type) || bad_rows(y, n, ldy, d, y_type) || bad_rows(out, n, ldout, d, x_type)) return MOE_ERR_INVALID_ARG;
+    if (h != nullptr ? bad_rows(h, n, ldh, d, y_type) : w_next != nullptr && n > 0) return MOE_ERR_INVALID_ARG;
+    if (gate == nullptr ? ldgate != 0 : ldgate != 0 ? bad_rows(gate, n, ldgate, d, y_type) : !aligned(gate, 4)) return MOE_ERR_INVALID_ARG;
+    if (n == 0) return MOE_OK;
+    const Rows rx(x, n, ldx * xs, d * xs), ry(y, n, ldy * ys, d * ys), full(ldgate != 0 ? gate : nullptr, n, ldgate * ys, d * ys);
+    const Rows each(ldgate == 0 ? gate : nullptr, 1, 0, n * 4), rw(w, 1, 0, d * size_of(w_type)), rn(w_next, 1, 0, d * size_of(w_type)), live(n_rows, 1, 0, 4);
+    const Rows ro(out, n, ldout * xs, d * xs), rh(h, n, ldh * ys, d * ys);
+    if (partly_over(ro, {rx, ry, full}) || over(ro, {each, rw, rn, live, rh}) || partly_over(rh, {rx, ry, full}) || over(rh, {each, rw, rn, live})) return MOE_ERR_INVALID_ARG;
+    NormArgs a = {};
+    a.x = x, a.ldx = ldx, a.y = y, a.ldy = ldy, a.w = w, a.w_next = w_next, a.gate = gate, a.ldgate = ldgate, a.out = out, a.ldout = ldout, a.h = h, a.ldh = ldh;
+    a.n_rows = n_rows, a.rows = n_rows_cap, a.d = d, a.scale = scale, a.eps = eps, a.norm = norm != 0;
+    a.x_f32 = x_type == MOE_F32, a.y_f32 = y_type == MOE_F32, a.w_f32 = w_type == MOE_F32;
+    return from_hip(launch_norm(a, (hipStream_t)stream));
+}
+
+moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const void* dh, int64_t lddh, const void* out, int32_t x_type,
+                                      int64_t ldout, const void* y, int32_t y_type, int64_t ldy, const void* w, int32_t w_type, int32_t norm,
+                                      const void* gate, int64_t ldgate, float scale, const void* w_next, float eps, const int32_t* n_rows,
+                                      int32_t n_rows_cap, int32_t d, void* dx, int64_t lddx, void* dy, int64_t lddy, void* dgate,
+                                      int64_t lddgate, float* dw, float* dw_next, void* workspace, size_t workspace_bytes, void* stream) {
+    moe_status st = check_norm(x_type, y_type, w, w_next, w_type, eps, n_rows, n_rows_cap, d);
+    if (st != MOE_OK) return st;
+    const int64_t n = n_rows_cap, xs = size_of(x_type), ys = size_of(y_type);
+    if (dout != nullptr && bad_rows(dout, n, lddout, d, x_type)) return MOE_ERR_INVALID_ARG;
+    if (dh != nullptr ? bad_rows(dh, n, lddh, d, y_type) || bad_rows(out, n, ldout, d, x_type) : n > 0 && (w_next != nullptr || dw_next != nullptr)) return MOE_ERR_INVALID_ARG;
+    if (bad_rows(y, n, ldy, d, y_type) || bad_rows(dx, n, lddx, d, x_type) || bad_rows(dy, n, lddy, d, y_type)) return MOE_ERR_INVALID_ARG;
+    if (gate == nullptr ? ldgate != 0 || dgate != nullptr : ldgate != 0 ? bad_rows(gate, n, ldgate, d, y_type) : !aligned(gate, 4)) return MOE_ERR_INVALID_ARG;
+    if (dgate != nullptr && (ldgate != 0 ? bad_rows(dgate, n, lddgate, d, y_type) : !aligned(dgate, 4))) return MOE_ERR_INVALID_ARG;
+    if (!aligned(dw, 16) || !aligned(dw_next, 16)) return MOE_ERR_INVALID_ARG;
+    if (n == 0 && dw == nullptr && dw_next == nullptr) return MOE_OK;
+    const size_t need = dw != nullptr || dw_next != nullptr ? moe_norm_backward_workspace_bytes(n_rows_cap, d) : 0;
+    st = check_workspace(workspace, workspace_bytes, need);
+    if (st != MOE_OK) return st;
+    const void* o = dh != nullptr ? out : nullptr;
+    const Rows rd(dout, n, lddout * xs, d * xs), rh(dh, n, lddh * ys, d * ys), ro(o, n, ldout * xs, d * xs), ry(y, n, ldy * ys, d * ys);
+    const Rows full(ldgate != 0 ? gate : nullptr, n, ldgate * ys, d * ys), each(ldgate == 0 ? gate : nullptr, 1, 0, n * 4);
+    const Rows rw(w, 1, 0, d * size_of(w_type)), rn(w_next, 1, 0, d * size_of(w_type)), live(n_rows, 1, 0, 4);
+    const Rows gx(dx, n, lddx * xs, d * xs), gy(dy, n, lddy * ys, d * ys), gf(ldgate != 0 ? dgate : nullptr, n, lddgate * ys, d * ys);
+    const Rows ge(ldgate == 0 ? dgate : nullptr, 1, 0, n * 4), gw(dw, 1, 0, (int64_t)d * 4), gn(dw_next, 1, 0, (int64_t)d * 4), ws(need > 0 ? workspace : nullptr, 1, 0, (int64_t)need);
+    for (const Rows* g : {&gx, &gy, &gf})
+        if (partly_over(*g, {rd, rh, ro, ry, full}) || over(*g, {each, rw, rn, live, ge, gw, gn, ws})) return MOE_ERR_INVALID_ARG;
+    if (over(gx, {gy, gf}) || over(gy, {gf}) || over(gw, {gn})) return MOE_ERR_INVALID_ARG;
+    for (const Rows* g : {&ge, &gw, &gn, &ws})
+        if (over(*g, {rd, rh, ro, ry, full, each, rw, rn, live})) return MOE_ERR_INVALID_ARG;
+    if (over(ge, {gw, gn, ws}) || over(ws, {gw, gn})) return MOE_ERR_INVALID_ARG;
+    NormGradArgs a = {};
+    a.dout = dout, a.lddout = lddout, a.dh = dh, a.lddh = lddh, a.o = o, a.ldo = ldout, a.y = y, a.ldy = ldy, a.w = w, a.w_next = w_next, a.gate = gate, a.ldgate = ldgate;
+    a.dx = dx, a.lddx = lddx, a.dy = dy, a.lddy = lddy, a.dgate = dgate, a.lddgate = lddgate, a.n_rows = n_rows, a.rows = n_rows_cap, a.d = d;
+    a.scale = scale, a.eps = eps, a.norm = norm != 0, a.x_f32 = x_type == MOE_F32, a.y_f32 = y_type == MOE_F32, a.w_f32 = w_type == MOE_F32;
+    return from_hip(launch_norm_backward(a, dw, dw_next, (float*)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"
