@@ -296,6 +296,25 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
                                       int32_t n_rows_cap, int32_t d, void* dx, int64_t lddx, void* dy, int64_t lddy, void* dgate,
                                       int64_t lddgate, float* dw, float* dw_next, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- orthogonalised updates ------------------------------------------------------------------------------------------
+ *
+ * Each matrix of a stack g [E, rows, cols] brought near the orthogonal matrix next to it (the same singular vectors, singular values near 1):
+ *   X = g / (|g| + eps), |g| the root of the sum of its squares;  for (a, b, c) of each step:  S = X X^T,  X = a X + (b S + c S S) X;
+ *   out = scale X
+ * (where rows > cols: the same on the transpose).  coefficients: host, [steps][3], read before the call returns; steps from 1 to 64.
+ * Operands of the products are kept in one or two 16-bit parts, sums in 32 bits, |g| in 64: an fp32 result is as far from the exact one
+ * as with products in 32 bits, a bf16 result about as far as its own rounding.  Singular values up to 4 and entries of b S + c S S up to 16 are
+ * in range on the way (coefficients that keep the singular values below 1.5, as such steps do, stay far below).  A matrix of zeros gives
+ * zeros (eps > 0); one that holds a NaN or an infinity gives NaN and spoils no other.
+ * g and out: rows ldg / ldout values apart (at least cols), matrices stride_g / stride_out values apart, pointers aligned to their values; any
+ * sizes from 1 to 2^17, E <= 256.  out may be exactly g (of the same type); otherwise they share no byte.
+ * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done; up to about 12 bytes for every
+ * value of the stack, where that is more than 8 GiB for the matrices that are gone through at a time (one at least).  0: sizes that are refused. */
+size_t moe_orthogonalize_workspace_bytes(int32_t E, int32_t rows, int32_t cols);
+moe_status moe_orthogonalize(const void* g, int32_t type, int64_t stride_g, int64_t ldg, int32_t E, int32_t rows, int32_t cols,
+                             const float* coefficients /* host */, int32_t steps, float eps, float scale, void* out, int32_t out_type,
+                             int64_t stride_out, int64_t ldout, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- introspection --------------------------------------------------------------------------- */
 
 /* Mean milliseconds of each stage over the moe_layer_forward calls made since the previous

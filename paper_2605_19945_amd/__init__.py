@@ -30,4 +30,5 @@ from .binding import (  # noqa: F401
     moe_rms_norm_backward,
     moe_residual_norm,
     moe_residual_norm_backward,
+    moe_orthogonalize,
 )

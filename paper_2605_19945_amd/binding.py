@@ -99,6 +99,9 @@ _SIGNATURES = {
     "moe_residual_norm_backward": (C.c_int, [_VP, _I64, _VP, _I64, _VP, _I32, _I64, _VP, _I32, _I64, _VP, _I32, _I32, _VP, _I64,
                                              C.c_float, _VP, C.c_float, _VP, _I32, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP,
                                              _SZ, _VP]),
+    "moe_orthogonalize_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
+    "moe_orthogonalize": (C.c_int, [_VP, _I32, _I64, _I64, _I32, _I32, _I32, _VP, _I32, C.c_float, C.c_float, _VP, _I32, _I64, _I64, _VP, _SZ,
+                                    _VP]),
     "moe_layer_intermediates": (C.c_int, [_VP, C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_VP)]),
 }
 
@@ -921,6 +924,65 @@ def moe_residual_norm_backward(dout, y, weight=None, out=None, dh=None, norm=Tru
     if dy is not None:
         _wrote(dy)
     return gx, gy, dw, dnext, dgate
+
+
+# ---- orthogonalised updates ----
+@functools.lru_cache(maxsize=64)
+def _coefficients(values, steps):
+    """Host array (bytes) of the coefficients [steps][3], or None."""
+    try:
+        rows = [values] * steps if len(values) == 3 and not hasattr(values[0], "__len__") else values
+        if len(rows) != steps or any(len(r) != 3 for r in rows):
+            return None
+        return struct.pack(f"={3 * steps}f", *[float(v) for r in rows for v in r])
+    except (TypeError, ValueError, OverflowError):
+        return None
+
+
+def _stack(what, name, t):
+    """(E, rows, cols, values between matrices, between rows) of a matrix or a stack of them, float32 or bfloat16."""
+    if t.dim() not in (2, 3) or t.dtype not in (_F32, _BF16):
+        _refuse(what, f"{name} has to be a matrix or a stack of matrices, float32 or bfloat16")
+    E, rows, cols = t.shape if t.dim() == 3 else (1, *t.shape)
+    *first, ld, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(what, f"the rows of {name} have to be contiguous")
+    return E, rows, cols, first[0] if first and E > 1 else 0, ld if rows > 1 else max(cols, 1)
+
+
+def moe_orthogonalize(g, steps=5, scale=1.0, eps=1e-7, coefficients=(3.4445, -4.7750, 2.0315), out=None, dtype=None):
+    """Each matrix of g [rows, cols] or [E, rows, cols] (float32 or bfloat16) near the orthogonal matrix next to it: X = g / (|g| + eps),
+    then `steps` times X = a X + (b S + c S S) X with S = X X^T (rows > cols: on the transpose), times scale; of `dtype`, g's by default.
+    coefficients: (a, b, c), or one such triple for each step.  out may be g.  Views whose last dimension is contiguous are taken as they are."""
+    lib, what = _lib or load_library(), "moe_orthogonalize"
+    _no_graphs(what, g, out)
+    E, rows, cols, stride, ld = _stack(what, "g", g)
+    dtype = dtype or (out.dtype if out is not None else g.dtype)
+    if dtype not in (_F32, _BF16):
+        _refuse(what, "dtype has to be float32 or bfloat16")
+    if not isinstance(coefficients, tuple):
+        coefficients = tuple(map(tuple, coefficients))
+    abc = _coefficients(coefficients, steps)
+    if abc is None:
+        _refuse(what, "coefficients have to be three numbers, or three for each step")
+    dev = _launch_device(what, g, out)
+    x, ostride, ldo = out, rows * cols, cols
+    if out is None:
+        x = g.new_empty(g.shape, dtype=dtype)
+    else:
+        if out.shape != g.shape or out.dtype is not dtype:
+            _refuse(what, "out has to be of g's shape and of dtype")
+        *_, ostride, ldo = _stack(what, "out", out)
+    if g.numel() == 0:
+        return x
+    ws, at, n = _workspace(g, "moe_orthogonalize_workspace_bytes", E, rows, cols)
+    st = lib.moe_orthogonalize(g.data_ptr(), 1 if g.dtype is _F32 else 0, stride, ld, E, rows, cols, abc, steps, eps, scale, x.data_ptr(),
+                               1 if dtype is _F32 else 0, ostride, ldo, at, n, _stream_of(dev))
+    if st != 0:
+        raise MoEError(st, what)
+    if out is not None:
+        _wrote(out)
+    return x
 
 
 # ---- host-side mapping search (no context, no GPU) ------------------------------------------------

@@ -53,3 +53,16 @@ constexpr int NORM_GRAD_GROUPS = 1024;  // workgroups of a backward launch, at m
 int norm_grad_groups(int rows, int d);
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float* workspace, hipStream_t st);
+
+// ---- orthogonalised updates ----
+struct OrthTask {
+    const void* g;
+    void* out;
+    int64_t g_matrix, g_ld, out_matrix, out_ld;  // values from one matrix, one row to the next
+    int E, rows, cols, steps;
+    const float* coefficients;                   // [steps][3]
+    float scale, eps;
+    bool in_f32, out_f32;
+};
+size_t orth_workspace(int E, int rows, int cols);
+hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st);

@@ -85,6 +85,20 @@ moe_status check_norm(int32_t x_type, int32_t y_type, const void* w, const void*
     return d < 8 || d % 8 != 0 || d > NORM_MAX_WIDTH ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
 }
 
+// ---- orthogonalised updates ----
+// Two stacks of E matrices that share bytes
+bool stacks_overlap(const char* a, int64_t a_matrix, int64_t a_ld, int64_t a_width, const char* b, int64_t b_matrix, int64_t b_ld, int64_t b_width, int E, int rows) {
+    const Rows whole_a(a, 1, 0, (E - 1) * a_matrix + (rows - 1) * a_ld + a_width), whole_b(b, 1, 0, (E - 1) * b_matrix + (rows - 1) * b_ld + b_width);
+    if (!overlap(whole_a, whole_b)) return false;
+    for (int i = 0; i < E; ++i)
+        for (int j = 0; j < E; ++j)
+            if (overlap({a + i * a_matrix, rows, a_ld, a_width}, {b + j * b_matrix, rows, b_ld, b_width})) return true;
+    return false;
+}
+inline bool orth_shape_ok(int32_t E, int32_t rows, int32_t cols) {
+    return E >= 1 && E <= kMaxExperts && rows >= 1 && rows <= kMaxWidth && cols >= 1 && cols <= kMaxWidth;
+}
+
 }  // namespace
 
 extern "C" {
@@ -331,6 +345,38 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
     a.dx = dx, a.lddx = lddx, a.dy = dy, a.lddy = lddy, a.dgate = dgate, a.lddgate = lddgate, a.n_rows = n_rows, a.rows = n_rows_cap, a.d = d;
     a.scale = scale, a.eps = eps, a.norm = norm != 0, a.x_f32 = x_type == MOE_F32, a.y_f32 = y_type == MOE_F32, a.w_f32 = w_type == MOE_F32;
     return from_hip(launch_norm_backward(a, dw, dw_next, (float*)workspace, (hipStream_t)stream));
+}
+
+size_t moe_orthogonalize_workspace_bytes(int32_t E, int32_t rows, int32_t cols) { return orth_shape_ok(E, rows, cols) ? orth_workspace(E, rows, cols) : 0; }
+
+moe_status moe_orthogonalize(const void* g, int32_t type, int64_t stride_g, int64_t ldg, int32_t E, int32_t rows, int32_t cols,
+                             const float* coefficients, int32_t steps, float eps, float scale, void* out, int32_t out_type,
+                             int64_t stride_out, int64_t ldout, void* workspace, size_t workspace_bytes, void* stream) {
+    if (E < 1 || rows < 1 || cols < 1 || !type_ok(type) || !type_ok(out_type)) return MOE_ERR_INVALID_ARG;
+    if (!orth_shape_ok(E, rows, cols)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (g == nullptr || out == nullptr || !aligned(g, size_of(type)) || !aligned(out, size_of(out_type))) return MOE_ERR_INVALID_ARG;
+    if (coefficients == nullptr || steps < 1 || steps > 64 || !(eps >= 0.f) || eps > 3e38f || !(scale >= -3e38f && scale <= 3e38f)) return MOE_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < 3 * steps; ++i)
+        if (!(coefficients[i] >= -1e6f && coefficients[i] <= 1e6f)) return MOE_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 40;
+    if (ldg < cols || ldout < cols || ldg > kMaxLd || ldout > kMaxLd) return MOE_ERR_INVALID_ARG;
+    // matrices of a stack lie one behind the other, or side by side in the same rows
+    auto apart = [&](int64_t stride, int64_t ld) { return E == 1 || (stride <= most && (stride >= (rows - 1) * ld + cols || (stride >= cols && (E - 1) * stride + cols <= ld))); };
+    if (!apart(stride_g, ldg) || !apart(stride_out, ldout)) return MOE_ERR_INVALID_ARG;
+    const size_t need = orth_workspace(E, rows, cols);
+    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace == nullptr || !aligned(workspace, 256)) return MOE_ERR_INVALID_ARG;
+    if (E == 1) stride_g = stride_out = 0;
+    const int64_t gs = size_of(type), os = size_of(out_type);
+    const bool same = g == out && type == out_type && stride_g == stride_out && (rows == 1 || ldg == ldout);
+    if (!same && stacks_overlap((const char*)g, stride_g * gs, ldg * gs, cols * gs, (const char*)out, stride_out * os, ldout * os, cols * os, E, rows)) return MOE_ERR_INVALID_ARG;
+    const Rows ws(workspace, 1, 0, (int64_t)need);
+    for (int32_t e = 0; e < E; ++e)
+        if (over(ws, {{(const char*)g + e * stride_g * gs, rows, ldg * gs, cols * gs}, {(const char*)out + e * stride_out * os, rows, ldout * os, cols * os}})) return MOE_ERR_INVALID_ARG;
+    OrthTask t = {};
+    t.g = g, t.out = out, t.g_matrix = stride_g, t.g_ld = ldg, t.out_matrix = stride_out, t.out_ld = ldout, t.E = E, t.rows = rows, t.cols = cols;
+    t.steps = steps, t.coefficients = coefficients, t.scale = scale, t.eps = eps, t.in_f32 = type == MOE_F32, t.out_f32 = out_type == MOE_F32;
+    return from_hip(launch_orth(t, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,191 @@
+"""Orthogonalised updates against the same steps in 64 bits.
+
+Bounds.  What a step rounds is carried on by the steps behind it, by more than a norm of the map tells (its derivative's bound to the power of the
+steps) and differently for every spectrum, so the bound of a case is found by carrying it on: the steps in 64 bits on the same matrix, each operand and
+product off by a random share, uniform to either side, of what its rounding may be off by (one part of fp16: 2^-11 of the value; two: 2^-22; a
+product's 32-bit sums: 2^-22 of the product of the magnitudes), give a deviation D; |D| is the root of its mean square over a few draws (of small
+matrices more: one draw of a few numbers can come near zero).  The kernel's errors are of the same sizes or smaller.  In the smallest matrices they
+are 15 numbers at least (X, S and P of five steps), each at most 3^1/2 times its root mean square, so by Cauchy and Schwarz together at most 45^1/2 < 8 times
+that of their sum; in larger ones there are more of them and they come nearer to it.  So their norm is below 8 |D|; a single value of n m is within 6
+times its share of that (and never past the norm).
+A bf16 result adds 2^-8 of the value, an fp32 one 2^-24."""
+import pytest
+import torch
+
+import paper_2605_19945_amd as moe
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+ABC = (3.4445, -4.7750, 2.0315)
+
+
+def gradient(shape, seed, dtype, kind="gauss", std=1e-3):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randn(shape, generator=g, dtype=F64)
+    if kind == "steep":      # a few directions carry most of the norm
+        a, b = torch.randn((*shape[:-1], 2), generator=g, dtype=F64), torch.randn((*shape[:-2], 2, shape[-1]), generator=g, dtype=F64)
+        t = a @ b + 0.03 * t
+    return (t * std).to(dtype)
+
+
+def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
+    """64 bits; noise: (parts of X in S, of P, generator) for the deviated run."""
+    tall = G.shape[0] > G.shape[1]
+    X = (G.t() if tall else G).double()
+    X = X / (X.square().sum().sqrt() + eps)
+
+    def off(t, share):
+        if noise is None:
+            return t
+        return t + (torch.rand(t.shape, generator=noise[2], dtype=F64) * 2 - 1) * share
+
+    def part(t, parts):
+        return off(t, t.abs() * (2.0 ** -11 if parts == 1 else 2.0 ** -22))
+
+    def product(A, B):
+        return off(A @ B, 2.0 ** -22 * (A.abs() @ B.abs())) if noise else A @ B
+
+    px, pp = noise[:2] if noise else (2, 2)
+    for a, b, c in coefficients:
+        X = part(X, 2)
+        Y = part(X, px)
+        S = part(product(Y, Y.t()), 2)
+        P = part(b * S + c * product(S, S), pp)
+        X = a * X + product(P, X)
+    return scale * (X.t() if tall else X)
+
+
+def check(got, G, coefficients=(ABC,) * 5, scale=1.0, eps=1e-7):
+    stack = G if G.dim() == 3 else G[None]
+    out = got.cpu() if G.dim() == 3 else got.cpu()[None]
+    parts = (2, 2) if out.dtype is F32 else (1, 1)
+    half = torch.finfo(out.dtype).eps / 2
+    for e in range(stack.shape[0]):
+        ref = steps_of(stack[e], coefficients, scale, eps)
+        noise, draws = torch.Generator().manual_seed(e), 16 if min(ref.shape) <= 40 else 2
+        D = [steps_of(stack[e], coefficients, scale, eps, (*parts, noise)) - ref for _ in range(draws)]
+        err, norm = out[e].double() - ref, (sum(float(d.square().sum()) for d in D) / draws) ** 0.5
+        assert float(err.norm()) <= 8 * norm + half * float(ref.norm()), (e, float(err.norm()), norm, float(ref.norm()))
+        one = min(1.0, 6 / ref.numel() ** 0.5) * 8 * norm
+        assert float((err.abs() - half * ref.abs()).max()) <= one * (1 + half), e
+
+
+SIZES = [(1, 1, 1), (2, 1, 9), (1, 70, 1), (3, 8, 8), (2, 31, 65), (1, 64, 200), (2, 128, 256), (2, 129, 127), (3, 300, 40), (1, 17, 1000), (1, 257, 513), (2, 260, 520),
+         (1, 520, 520), (2, 700, 300), (1, 384, 2056)]
+
+
+@pytest.mark.parametrize("E,rows,cols", SIZES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["gauss", "steep"])
+def test_against_64_bits(E, rows, cols, dtype, kind):
+    G = gradient((E, rows, cols), rows + cols, dtype, kind)
+    got = moe.moe_orthogonalize(G.cuda(), scale=0.5)
+    assert got.dtype is dtype and got.shape == G.shape
+    check(got, G, scale=0.5)
+
+
+@pytest.mark.parametrize("rows,cols", [(96, 160), (160, 96), (300, 270)])
+def test_types_steps_and_coefficients(rows, cols):
+    G = gradient((2, rows, cols), 3, F32)
+    check(moe.moe_orthogonalize(G.cuda(), dtype=BF16), G)
+    check(moe.moe_orthogonalize(G.to(BF16).cuda(), dtype=F32), G.to(BF16))
+    check(moe.moe_orthogonalize(G[0].cuda(), steps=1), G[0], (ABC,))
+    many = [(4.0, -6.0, 3.0), ABC, (2.0, -1.5, 0.5), (1.5, -0.5, 0.0)]
+    check(moe.moe_orthogonalize(G.cuda(), steps=4, coefficients=many, eps=1e-3, scale=-3.0), G, many, -3.0, 1e-3)
+
+
+def test_permutations_exactly_but_for_scalars():
+    """A permutation times a number has one singular value, so every step is a step of that number; what is zero stays zero."""
+    for rows, cols in ((40, 40), (40, 100), (200, 40), (300, 300)):
+        n = min(rows, cols)
+        p = torch.zeros(rows, cols)
+        p[torch.randperm(rows, generator=torch.Generator().manual_seed(1))[:n], torch.randperm(cols, generator=torch.Generator().manual_seed(2))[:n]] = 0.25
+        x = 0.25 / (0.25 * n ** 0.5 + 1e-7)
+        for _ in range(5):
+            x = ABC[0] * x + ABC[1] * x ** 3 + ABC[2] * x ** 5
+        for dtype, rel in ((F32, 2.0 ** -16), (BF16, 2.0 ** -8 + 5 * 8 * 2.0 ** -11)):  # five steps, at most 8 times a rounding each
+            got = moe.moe_orthogonalize(p.to(dtype).cuda()).cpu().double()
+            assert (got[p == 0] == 0).all() and float((got[p != 0] - x).abs().max()) <= rel * abs(x)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_views_and_results_in_place(dtype):
+    for rows, cols, pad in ((70, 200, 200), (200, 70, 3), (129, 131, 1)):
+        wide = gradient((3, rows, cols + pad), 5, dtype).cuda()
+        G = wide[:, :, :cols]
+        want = moe.moe_orthogonalize(G.contiguous())
+        assert torch.equal(moe.moe_orthogonalize(G), want)
+        out = torch.full((3, rows + 2, cols + 5), 7.0, dtype=dtype, device="cuda")
+        view = out[:, 1:rows + 1, 3:cols + 3]
+        moe.moe_orthogonalize(G, out=view)
+        assert torch.equal(view, want)
+        out[:, 1:rows + 1, 3:cols + 3] = 7.0
+        assert (out == 7.0).all()
+        rest = wide[:, :, cols:].clone()
+        moe.moe_orthogonalize(G, out=G)
+        assert torch.equal(wide[:, :, :cols], want) and torch.equal(wide[:, :, cols:], rest)
+    # one matrix, and matrices side by side in the same rows
+    m = gradient((90, 3, 50), 6, dtype).cuda()
+    side = m.transpose(0, 1)
+    assert torch.equal(moe.moe_orthogonalize(side), moe.moe_orthogonalize(side.contiguous()))
+    assert torch.equal(moe.moe_orthogonalize(m[:, 1]), moe.moe_orthogonalize(m[:, 1].contiguous()))
+    assert moe.moe_orthogonalize(m[:0, 1]).shape == (0, 50) and moe.moe_orthogonalize(m[:, :, :0]).shape == (90, 3, 0)
+
+
+def test_a_spoilt_matrix_spoils_no_other():
+    for rows, cols in ((60, 150), (300, 280)):
+        G = gradient((4, rows, cols), 7, F32)
+        want = moe.moe_orthogonalize(G.cuda())
+        G[0] = 0
+        G[2, 5, 7], G[3, 1, 1] = float("nan"), float("inf")
+        got = moe.moe_orthogonalize(G.cuda())
+        assert not got[0].any() and torch.equal(got[1], want[1]) and torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+
+
+def test_far_scales():
+    G = gradient((64, 96), 8, F32)
+    for std in (1e-30, 1e-12, 1e20, 1e34):
+        H = (G.double() * std * 1e3).float()
+        check(moe.moe_orthogonalize(H.cuda(), eps=0.0), H, eps=0.0)
+
+
+def test_a_stack_is_its_matrices():
+    G = gradient((5, 260, 300), 9, BF16).cuda()
+    got = moe.moe_orthogonalize(G)
+    for e in range(5):
+        assert torch.equal(moe.moe_orthogonalize(G[e]), got[e])
+
+
+def test_more_matrices_than_the_workspace_holds():
+    """Stacks past the workspace's 8 GiB are gone through in turns."""
+    lib = moe.load_library()
+    one, E = lib.moe_orthogonalize_workspace_bytes(1, 2048, 2048), 0
+    E = (8 << 30) // one + 2
+    assert 16 < E <= 256 and lib.moe_orthogonalize_workspace_bytes(E, 2048, 2048) <= 8 << 30
+    g = torch.Generator(device="cuda").manual_seed(1)
+    G = torch.empty(E, 2048, 2048, dtype=BF16, device="cuda").normal_(generator=g)
+    got = moe.moe_orthogonalize(G)
+    for e in (0, E - 3, E - 2, E - 1):
+        assert torch.equal(moe.moe_orthogonalize(G[e]), got[e]), e
+
+
+def test_streams_and_graphs():
+    a, b = gradient((2, 200, 300), 10, F32).cuda(), gradient((3, 96, 64), 11, BF16).cuda()
+    want = moe.moe_orthogonalize(a), moe.moe_orthogonalize(b)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s, t in zip(streams, (a, b)):        # two calls at once
+        with torch.cuda.stream(s):
+            got.append([moe.moe_orthogonalize(t) for _ in range(3)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(w, t) for w, ts in zip(want, got) for t in ts)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = moe.moe_orthogonalize(a)
+    for k in range(4):
+        a.copy_(gradient((2, 200, 300), 20 + k, F32).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, moe.moe_orthogonalize(a)), k
