@@ -68,6 +68,14 @@ static __device__ inline uint32_t pack_f16(float lo, float hi) {
 static __device__ inline float f16_lo(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)w); }
 static __device__ inline float f16_hi(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16)); }
 
+template <int I> struct OrthInt { static constexpr int value = I; };
+template <int N, int I = 0, typename F> static __device__ inline void orth_repeat(F&& f) {  // f(0) .. f(N - 1), each a constant
+    if constexpr (I < N) {
+        f(OrthInt<I>{});
+        orth_repeat<N, I + 1>(f);
+    }
+}
+
 // From the lane 1 (STEP 1) or 2 further on or back among 4
 template <int STEP> static __device__ inline uint32_t lane_xor(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, STEP == 1 ? 0xb1 : 0x4e, 0xf, 0xf, false);

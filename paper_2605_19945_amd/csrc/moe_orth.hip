@@ -32,9 +32,9 @@ static __device__ inline void place_symmetric(int t, int mt, int* m, int* n) {
 // PA, PB: parts of A and B.  WM x WN wavefronts of FM x FN fragments (16 x 16).  STAGES of 32 values of the reduction in LDS: the next
 // ones but one arrive while one is multiplied.  CIN: parts of what beta multiplies (0: none).  OUT: parts of the result in blocks (1, 2) or
 // its type in the caller's rows.  SYM: the result is symmetric; tiles above the diagonal are written to both sides.
-template <int PA, int PB, int WM, int WN, int FM, int FN, int STAGES, int CIN, int PARTS, int OUT>
+template <int PA, int PB, int WM, int WN, int FM, int FN, int KS, int STAGES, int CIN, int PARTS, int OUT>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
-    constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = FA * PA + FB * PB, LOADS = FRAGS / WAVES;
+    constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
     static_assert(FA % WAVES == 0 && FB % WAVES == 0, "a load's operand does not depend on the wavefront");
     constexpr bool SYM = OUT == ORTH_SQUARE;
     extern __shared__ __align__(1024) char lds[];
@@ -68,17 +68,14 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) offset[i] = (uint32_t)(i * WAVES + wave) * panel + lane * 16;
     const uint32_t base = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)) + wave * ORTH_BLOCK;
-    auto issue = [&](int step, int stage) {
-        const uint32_t at = (uint32_t)step * ORTH_BLOCK, to = base + stage * (FRAGS * ORTH_BLOCK);
-#pragma unroll
-        for (int p = 0; p < PA; ++p)
-#pragma unroll
-            for (int i = 0; i < FA / WAVES; ++i) orth_load(to + (p * FA + i * WAVES) * ORTH_BLOCK, offset[i], da[p], at);
-#pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-            for (int i = 0; i < FB / WAVES; ++i) orth_load(to + (PA * FA + p * FB + i * WAVES) * ORTH_BLOCK, offset[i], db[p], at);
+    constexpr int NA = FA / WAVES, NB = FB / WAVES, PER = PA * NA + PB * NB;  // loads of a block of the reduction
+    auto issue_one = [&](auto load, int s, int place) {  // one load of stage s
+        constexpr int k = decltype(load)::value / PER, i = decltype(load)::value % PER, ib = i - PA * NA;
+        const uint32_t to = base + place * (FRAGS * ORTH_BLOCK), at = (uint32_t)(s * KS + k) * ORTH_BLOCK;
+        if constexpr (i < PA * NA) orth_load(to + (KS * (i / NA) * FA + k * FA + i % NA * WAVES) * ORTH_BLOCK, offset[i % NA], da[i / NA], at);
+        else orth_load(to + (KS * (PA * FA + ib / NB * FB) + k * FB + ib % NB * WAVES) * ORTH_BLOCK, offset[ib % NB], db[ib / NB], at);
     };
+    auto issue = [&](int s, int place) { orth_repeat<LOADS>([&](auto load) { issue_one(load, s, place); }); };
 
     f32x4_t acc[FM][FN];
 #pragma unroll
@@ -86,41 +83,111 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+    if constexpr (WAVES == 8) {
+        // Two groups of four wavefronts, one of each on every SIMD, take turns: while one group multiplies, the other reads its next
+        // fragments, so the matrix cores always have a wavefront whose operands are there.  In turn 2 s the first group reads stage s (and
+        // asks for stage s + 1, into the place that the second group left in the turn before), in 2 s + 1 the second; a stage has two turns to
+        // arrive.
+        f16x8_t a[KS][PA][FM], b[KS][PB][FN];
+        const int stages = g.steps / KS;
+        auto read = [&](int s) {
+            const char* at = lds + (s & 1) * (FRAGS * ORTH_BLOCK) + lane * 16;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
-        if (s < g.steps) issue(s, s);
-    int stage = 0;
-    for (int step = 0; step < g.steps; ++step) {
-        // this step's stage has arrived; the last steps have fewer behind them and wait for all
-        if (step + STAGES - 1 <= g.steps) orth_wait<(STAGES - 2) * LOADS>();
-        else orth_wait<0>();
-        orth_barrier();  // of every wavefront's; and all are done with the stage before
-        if (step + STAGES - 1 < g.steps) issue(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-        const char* at = lds + stage * (FRAGS * ORTH_BLOCK) + lane * 16;
-        const char* fa = at + wm * FM * ORTH_BLOCK;
-        const char* fb = at + (PA * FA + wn * FN) * ORTH_BLOCK;
-        f16x8_t b[PB][FN];
+            for (int k = 0; k < KS; ++k) {
 #pragma unroll
-        for (int p = 0; p < PB; ++p)
+                for (int p = 0; p < PB; ++p)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) b[p][j] = *(const f16x8_t*)(fb + (p * FB + j) * ORTH_BLOCK);
+                    for (int j = 0; j < FN; ++j) b[k][p][j] = *(const f16x8_t*)(at + (KS * (PA * FA + p * FB) + k * FB + wn * FN + j) * ORTH_BLOCK);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            f16x8_t a[PA];
+                for (int p = 0; p < PA; ++p)
 #pragma unroll
-            for (int p = 0; p < PA; ++p) a[p] = *(const f16x8_t*)(fa + (p * FA + i) * ORTH_BLOCK);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[0], acc[i][j], 0, 0, 0);
-            if constexpr (PB == 2) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][j], a[0], acc[i][j], 0, 0, 0);
+                    for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK);
             }
-            if constexpr (PA == 2) {
+        };
+        constexpr int PAIRS = PA + PB - 1, ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
+        auto multiply = [&](auto&& beside) {
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            orth_repeat<ROWS>([&](auto row) {
+                constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
+                constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : 0;  // hi hi, hi lo, lo hi
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[1], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k][q][j], a[k][p][i], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                beside(row);
+            });
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        issue(0, 0);
+        orth_wait<0>();
+        orth_barrier();
+        if (wave < 4) {
+            for (int s = 0; s < stages; ++s) {
+                read(s);
+                if (s + 1 < stages) issue(s + 1, (s + 1) & 1);
+                orth_barrier();
+                multiply([](auto) {});
+                orth_wait<0>();
+                orth_barrier();
+            }
+            orth_barrier();
+        } else {
+            if (1 < stages) issue(1, 1);
+            orth_barrier();
+            for (int s = 0; s < stages; ++s) {
+                read(s);
+                orth_wait<0>();
+                orth_barrier();
+                const bool more = s + 2 < stages;
+                multiply([&](auto row) {  // its loads among the products
+                    constexpr int r = decltype(row)::value;
+                    if constexpr (r * LOADS % ROWS < LOADS && r * LOADS / ROWS < LOADS) {
+                        if (more) issue_one(OrthInt<r * LOADS / ROWS>{}, s + 2, s & 1);
+                    }
+                });
+                orth_barrier();
             }
         }
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+    } else {
+        static_assert(WAVES == 8 || KS == 1, "");
+        const int stages = g.steps;
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < stages) issue(s, s);
+        int stage = 0;
+        for (int step = 0; step < stages; ++step) {
+            // this step's stage has arrived; the last steps have fewer behind them and wait for all
+            if (step + STAGES - 1 <= stages) orth_wait<(STAGES - 2) * LOADS>();
+            else orth_wait<0>();
+            orth_barrier();  // of every wavefront's; and all are done with the stage before
+            if (step + STAGES - 1 < stages) issue(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+            const char* at = lds + stage * (FRAGS * ORTH_BLOCK) + lane * 16;
+            const char* fa = at + wm * FM * ORTH_BLOCK;
+            const char* fb = at + (PA * FA + wn * FN) * ORTH_BLOCK;
+            f16x8_t b[PB][FN];
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) b[p][j] = *(const f16x8_t*)(fb + (p * FB + j) * ORTH_BLOCK);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                f16x8_t a[PA];
+#pragma unroll
+                for (int p = 0; p < PA; ++p) a[p] = *(const f16x8_t*)(fa + (p * FA + i) * ORTH_BLOCK);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[0], acc[i][j], 0, 0, 0);
+                if constexpr (PB == 2) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][j], a[0], acc[i][j], 0, 0, 0);
+                }
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[1], acc[i][j], 0, 0, 0);
+                }
+            }
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+        }
     }
 
     // A lane has the columns 4 (lane / 16) + 0..3 of row lane % 16 of every fragment.
@@ -295,16 +362,15 @@ Size size_of_matrix(int rows, int cols) {
 int64_t matrix_bytes(const Size& z) { return 6 * z.x + 4 * z.s + 4096; }
 
 template <int PA, int PB, int CIN, int PARTS, int OUT> hipError_t product(const OrthArgs& g, int tile, hipStream_t st) {
-    constexpr int STAGES = PA + PB == 2 ? 4 : PA + PB == 3 ? 3 : 2;
-    auto run = [&](auto kernel, int frags, int threads) {
-        const int bytes = frags * ORTH_BLOCK * STAGES;
+    auto run = [&](auto kernel, int bytes, int threads) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         kernel<<<g.tiles * g.matrices, threads, bytes, st>>>(g);
         return hipGetLastError();
     };
-    if (tile == 256) return run(orth_product_kernel<PA, PB, 2, 4, 8, 4, STAGES, CIN, PARTS, OUT>, 16 * (PA + PB), 512);
-    return run(orth_product_kernel<PA, PB, 2, 2, 4, 4, STAGES, CIN, PARTS, OUT>, 8 * (PA + PB), 256);
+    constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
+    if (tile == 256) return run(orth_product_kernel<PA, PB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
+    return run(orth_product_kernel<PA, PB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
 }
 
 OrthOperand operand(char*& at, int64_t plane, int parts, int blocks, int matrices) {
