@@ -96,7 +96,7 @@ bool stacks_overlap(const char* a, int64_t a_matrix, int64_t a_ld, int64_t a_wid
     return false;
 }
 inline bool orth_shape_ok(int32_t E, int32_t rows, int32_t cols) {
-    return E >= 1 && E <= kMaxExperts && rows >= 1 && rows <= kMaxWidth && cols >= 1 && cols <= kMaxWidth;
+    return E >= 1 && E <= kMaxExperts && rows >= 1 && rows <= kMaxWidth && cols >= 1 && cols <= kMaxWidth && (int64_t)rows * cols <= (int64_t)1 << 29;
 }
 
 }  // namespace

@@ -1,9 +1,10 @@
 // Tile engine of the orthogonalising products (moe_orth.hip): one workgroup computes a tile C[i][j] = sum_k A[i][k] B[j][k] of one matrix.
 //
-// Operands are matrices of this unit's own making, kept as the matrix instructions read them: 16 rows by 32 values of the reduction are a
-// block of 1 KiB, in which lane l has the 8 values from 8 (l / 16) on of row l % 16; the blocks of 16 rows follow each other along the reduction.
-// So a load into LDS is one block, whole lines of memory, and a fragment is a 16-byte LDS read at neighbouring addresses: no swizzle,
-// no bank conflicts.  Rows and reduction are padded with zeros to whole tiles, so there are no edges.
+// Operands are matrices of this unit's own making, kept as the matrix instructions read them: 16 rows by 32 columns are a block of 1 KiB, in
+// which 8 neighbouring columns of a row are a piece of 16 bytes; blocks follow each other along the columns.  A load into LDS is one block,
+// whole lines of memory.  Fragments whose reduction runs along the columns are 16-byte LDS reads, those whose reduction runs along the
+// rows come from the transposing 8-byte read, so a matrix is kept once whichever way it is multiplied.  A block's pieces are placed (orth_piece)
+// so that both reads fall on all banks.  Rows and columns are padded with zeros to whole tiles, so there are no edges.
 //
 // Values are held as fp16 times a power of two, as one part (11 bits) or as two whose sum has 22: v = hi + lo, hi = fp16(v), lo = fp16(v - hi).
 // A product of such parts takes hi hi, hi lo and lo hi (what there is of them; lo lo lies below the 32-bit sums' rounding).
@@ -19,14 +20,15 @@ constexpr int ORTH_BLOCK = 1024;  // bytes of a block of 16 rows by 32 values
 struct OrthOperand {
     char* part[2];
     int64_t matrix;  // bytes from one matrix to the next
-    int blocks;      // blocks of 16 rows follow each other along `blocks` blocks of the reduction
+    int blocks;      // along the columns
 };
 
 struct OrthArgs {
     OrthOperand a, b;
     OrthOperand cin;       // beta times this is added
-    OrthOperand c, ct;     // the result and its transpose, in blocks again
+    OrthOperand c;         // the result
     float alpha, beta;
+    float diagonal;        // added to the diagonal of a symmetric result; or, times b, to a product that is not (in the units of a)
     int steps;             // blocks of the reduction
     int mt, nt;            // tiles of a matrix (symmetric: mt == nt, those on and above the diagonal)
     int tiles, matrices;   // tiles of a matrix that are computed
@@ -39,6 +41,11 @@ struct OrthArgs {
 };
 
 enum { ORTH_SQUARE = 0, ORTH_BLOCKS = 1, ORTH_BF16 = 2, ORTH_F32 = 3 };
+
+// Place of a piece in its block: 8 columns from 8 * g on of a row.  A 16-byte read serves lanes 0-3, 12-15 and 20-27 together, the rows 0-3 and 12-15
+// of one g and 4-11 of the next; a transposing read the rows 0-3 and 8-11 (or 4-7 and 12-15) of two neighbouring g.  Rows change places by 12 in
+// every other g, so that both find 16 pieces of different banks.
+static __device__ __host__ inline int orth_piece(int row, int g) { return 16 * g + (row ^ (g & 1) * 12); }
 
 static __device__ inline uint32_t orth_lds_addr(const void* p) { return (uint32_t)(uintptr_t)(const orth_lds_char*)p; }
 

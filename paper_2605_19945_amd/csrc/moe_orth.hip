@@ -8,15 +8,15 @@
 // two: 22 bits, results as far from the exact ones as those of 32-bit products (4e-7 to 2e-6 of their norm, on flat and steep spectra).
 // For a bf16 result X where it is multiplied by P, and S, have two, X in S and P one: 2e-5 to 1.2e-3 of the norm, below the 1.7e-3 of
 // the result's own rounding; with one part throughout steep spectra lose 8e-3, in bf16 6e-2.
-//
-// S = X X^T wants X with the reduction along m, P X wants it along n: the epilogue of the last product of a step writes X and X^T.
 #include "moe_orth.h"
+
+#include <initializer_list>
 
 namespace {
 
 // X, S and P are held times these powers of two: in the middle of fp16's range, singular values up to 4 allowed for, so that the
 // second parts are seldom subnormal.
-constexpr float X_SCALE = 8192.f, S_SCALE = 4096.f, P_SCALE = 4096.f;
+constexpr float X_SCALE = 8192.f, S_SCALE = 4096.f, Q_SCALE = 2048.f;
 
 // ---- the products ----
 // Tile t of a symmetric matrix's mt x mt, row by row on and above the diagonal
@@ -29,17 +29,18 @@ static __device__ inline void place_symmetric(int t, int mt, int* m, int* n) {
     *n = r + t - (r * mt - r * (r - 1) / 2);
 }
 
-// PA, PB: parts of A and B.  WM x WN wavefronts of FM x FN fragments (16 x 16).  STAGES of 32 values of the reduction in LDS: the next
-// ones but one arrive while one is multiplied.  CIN: parts of what beta multiplies (0: none).  OUT: parts of the result in blocks (1, 2) or
-// its type in the caller's rows.  SYM: the result is symmetric; tiles above the diagonal are written to both sides.
-template <int PA, int PB, int WM, int WN, int FM, int FN, int KS, int STAGES, int CIN, int PARTS, int OUT>
+// PA, PB: parts of A and B.  TB: B lies with the reduction along its rows (otherwise along its columns).  WM x WN wavefronts of FM x FN
+// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN: beta times another matrix (in two parts) is added.
+// OUT: a symmetric result in blocks, whose tiles above the diagonal are written to both sides; any result in blocks; or its type in the caller's
+// rows.  PARTS: of a result in blocks.  DIAG: A is multiplied with `diagonal` added to its diagonal.
+template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool CIN, int PARTS, int OUT, bool DIAG>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
-    static_assert(FA % WAVES == 0 && FB % WAVES == 0, "a load's operand does not depend on the wavefront");
+    static_assert(FA % WAVES == 0 && FB == 2 * WAVES, "a load's operand and block row do not depend on the wavefront");
     constexpr bool SYM = OUT == ORTH_SQUARE;
     extern __shared__ __align__(1024) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / WN, wn = wave % WN;
+    const int wm = wave / WN, wn = wave % WN, i16 = lane & 15, q16 = lane >> 4;
 
     // neighbouring tiles on one XCD (workgroup number % 8): one stretch of the list each
     const int total = g.tiles * g.matrices, xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
@@ -56,24 +57,28 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
 
-    // loads: block row i * WAVES + wave of the operand that load i belongs to
-    const uint32_t panel = (uint32_t)g.steps * ORTH_BLOCK;
+    // A stage's loads: block row i * WAVES + wave of an operand along its columns; of one along its rows block row i, block column wave.
+    const uint32_t panel = (uint32_t)g.a.blocks * ORTH_BLOCK, panel_b = (uint32_t)g.b.blocks * ORTH_BLOCK;
     u32x4_t da[PA], db[PB];
 #pragma unroll
     for (int p = 0; p < PA; ++p) da[p] = orth_desc(g.a.part[p] + matrix * g.a.matrix + (int64_t)tm * FA * panel, FA * panel);
 #pragma unroll
-    for (int p = 0; p < PB; ++p) db[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix + (int64_t)tn * FB * panel, FB * panel);
-    constexpr int ROUNDS = (FA > FB ? FA : FB) / WAVES;
-    uint32_t offset[ROUNDS];
-#pragma unroll
-    for (int i = 0; i < ROUNDS; ++i) offset[i] = (uint32_t)(i * WAVES + wave) * panel + lane * 16;
-    const uint32_t base = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)) + wave * ORTH_BLOCK;
+    for (int p = 0; p < PB; ++p) {
+        const int64_t at = TB ? (int64_t)tn * (FB / 2) * ORTH_BLOCK : (int64_t)tn * FB * panel_b;
+        db[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix + at, TB ? (uint32_t)(g.b.matrix - at) : FB * panel_b);
+    }
     constexpr int NA = FA / WAVES, NB = FB / WAVES, PER = PA * NA + PB * NB;  // loads of a block of the reduction
+    uint32_t offset[NA], offset_b[NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) offset[i] = (uint32_t)(i * WAVES + wave) * panel + lane * 16;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) offset_b[i] = (TB ? i * panel_b + wave * ORTH_BLOCK : (uint32_t)(i * WAVES + wave) * panel_b) + lane * 16;
+    const uint32_t base = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)) + wave * ORTH_BLOCK;
     auto issue_one = [&](auto load, int s, int place) {  // one load of stage s
         constexpr int k = decltype(load)::value / PER, i = decltype(load)::value % PER, ib = i - PA * NA;
         const uint32_t to = base + place * (FRAGS * ORTH_BLOCK), at = (uint32_t)(s * KS + k) * ORTH_BLOCK;
         if constexpr (i < PA * NA) orth_load(to + (KS * (i / NA) * FA + k * FA + i % NA * WAVES) * ORTH_BLOCK, offset[i % NA], da[i / NA], at);
-        else orth_load(to + (KS * (PA * FA + ib / NB * FB) + k * FB + ib % NB * WAVES) * ORTH_BLOCK, offset[ib % NB], db[ib / NB], at);
+        else orth_load(to + (KS * (PA * FA + ib / NB * FB) + k * FB + ib % NB * WAVES) * ORTH_BLOCK, offset_b[ib % NB], db[ib / NB], TB ? (uint32_t)(s * KS + k) * 2 * panel_b : at);
     };
     auto issue = [&](int s, int place) { orth_repeat<LOADS>([&](auto load) { issue_one(load, s, place); }); };
 
@@ -83,51 +88,100 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+    f16x8_t a[KS][PA][FM], b[KS][PB][FN];
+    const int stages = g.steps / KS;
+    const int at_row = orth_piece(i16, q16) * 16;
+    // of the transposing read: lane i of 16 asks for 4 columns of row 8 (q % 2) + i / 4 and is given column i of 4 rows; the next 4 rows lie where
+    // the exclusive or with 12 of the rows puts them
+    const int t_row = 8 * (q16 & 1) + (i16 >> 2), t_g = (i16 & 3) >> 1;
+    const int at_turn = orth_piece(t_row, t_g) * 16 + (i16 & 1) * 8, at_next = orth_piece(t_row + 4, t_g) * 16 + (i16 & 1) * 8;
+    auto read = [&](int place) {
+        const char* at = lds + place * (FRAGS * ORTH_BLOCK);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const char* block = at + (KS * (PA * FA + p * FB) + k * FB) * ORTH_BLOCK;
+                    if constexpr (TB) {
+                        typedef short s16x4_t __attribute__((ext_vector_type(4)));
+                        typedef short s16x8_t __attribute__((ext_vector_type(8)));
+                        typedef __attribute__((address_space(3))) s16x4_t lds4;
+                        block += ((q16 >> 1) * WAVES + (wn * FN + j) / 2) * ORTH_BLOCK + j % 2 * 512;
+                        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_turn)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_next));
+                        b[k][p][j] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    } else {
+                        b[k][p][j] = *(const f16x8_t*)(block + (wn * FN + j) * ORTH_BLOCK + at_row);
+                    }
+                }
+#pragma unroll
+            for (int p = 0; p < PA; ++p)
+#pragma unroll
+                for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK + at_row);
+        }
+    };
+    constexpr int PAIRS = PA + PB - 1, ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
+    auto multiply = [&](int s, auto&& beside) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        orth_repeat<ROWS>([&](auto row) {
+            constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
+            constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : 0;  // hi hi, hi lo, lo hi
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k][q][j], a[k][p][i], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            beside(row);
+        });
+        if constexpr (DIAG) {
+            // 32 of the reduction that are 32 of the wavefront's rows: the diagonal number, in two parts, times them
+            static_assert(KS == 1 && PB == 2 && FM % 2 == 0, "");
+            const int from = 2 * s - (tm * FA + wm * FM);
+            if (from >= 0 && from < FM) {
+                const _Float16 hi = (_Float16)g.diagonal, lo = (_Float16)(g.diagonal - (float)hi);
+                f16x8_t e[2][2];  // [of the first, the second 16 rows][part]
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool on = 8 * q16 + j == 16 * h + i16;
+                        e[h][0][j] = on ? hi : (_Float16)0.f;
+                        e[h][1][j] = on ? lo : (_Float16)0.f;
+                    }
+                orth_repeat<FM / 2>([&](auto pair) {
+                    constexpr int i = 2 * decltype(pair)::value;
+                    if (from == i) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int j = 0; j < FN; ++j) {
+                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][0][j], e[h][0], acc[i + h][j], 0, 0, 0);
+                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][1][j], e[h][0], acc[i + h][j], 0, 0, 0);
+                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][0][j], e[h][1], acc[i + h][j], 0, 0, 0);
+                            }
+                    }
+                });
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
     if constexpr (WAVES == 8) {
         // Two groups of four wavefronts, one of each on every SIMD, take turns: while one group multiplies, the other reads its next
         // fragments, so the matrix cores always have a wavefront whose operands are there.  In turn 2 s the first group reads stage s (and
         // asks for stage s + 1, into the place that the second group left in the turn before), in 2 s + 1 the second; a stage has two turns to
         // arrive.
-        f16x8_t a[KS][PA][FM], b[KS][PB][FN];
-        const int stages = g.steps / KS;
-        auto read = [&](int s) {
-            const char* at = lds + (s & 1) * (FRAGS * ORTH_BLOCK) + lane * 16;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-#pragma unroll
-                for (int p = 0; p < PB; ++p)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) b[k][p][j] = *(const f16x8_t*)(at + (KS * (PA * FA + p * FB) + k * FB + wn * FN + j) * ORTH_BLOCK);
-#pragma unroll
-                for (int p = 0; p < PA; ++p)
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK);
-            }
-        };
-        constexpr int PAIRS = PA + PB - 1, ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
-        auto multiply = [&](auto&& beside) {
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            orth_repeat<ROWS>([&](auto row) {
-                constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
-                constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : 0;  // hi hi, hi lo, lo hi
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k][q][j], a[k][p][i], acc[i][j], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                beside(row);
-            });
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-        };
+        static_assert(STAGES == 2, "");
         issue(0, 0);
         orth_wait<0>();
         orth_barrier();
         if (wave < 4) {
             for (int s = 0; s < stages; ++s) {
-                read(s);
+                read(s & 1);
                 if (s + 1 < stages) issue(s + 1, (s + 1) & 1);
                 orth_barrier();
-                multiply([](auto) {});
+                multiply(s, [](auto) {});
                 orth_wait<0>();
                 orth_barrier();
             }
@@ -136,11 +190,11 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             if (1 < stages) issue(1, 1);
             orth_barrier();
             for (int s = 0; s < stages; ++s) {
-                read(s);
+                read(s & 1);
                 orth_wait<0>();
                 orth_barrier();
                 const bool more = s + 2 < stages;
-                multiply([&](auto row) {  // its loads among the products
+                multiply(s, [&](auto row) {  // its loads among the products
                     constexpr int r = decltype(row)::value;
                     if constexpr (r * LOADS % ROWS < LOADS && r * LOADS / ROWS < LOADS) {
                         if (more) issue_one(OrthInt<r * LOADS / ROWS>{}, s + 2, s & 1);
@@ -150,48 +204,24 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             }
         }
     } else {
-        static_assert(WAVES == 8 || KS == 1, "");
-        const int stages = g.steps;
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
-            if (s < stages) issue(s, s);
-        int stage = 0;
-        for (int step = 0; step < stages; ++step) {
-            // this step's stage has arrived; the last steps have fewer behind them and wait for all
-            if (step + STAGES - 1 <= stages) orth_wait<(STAGES - 2) * LOADS>();
+        orth_repeat<STAGES - 1>([&](auto s) {
+            if (decltype(s)::value < stages) issue(decltype(s)::value, decltype(s)::value);
+        });
+        int place = 0;
+        for (int s = 0; s < stages; ++s) {
+            // this stage has arrived; the last ones have fewer behind them and wait for all
+            if (s + STAGES - 1 <= stages) orth_wait<(STAGES - 2) * LOADS>();
             else orth_wait<0>();
             orth_barrier();  // of every wavefront's; and all are done with the stage before
-            if (step + STAGES - 1 < stages) issue(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-            const char* at = lds + stage * (FRAGS * ORTH_BLOCK) + lane * 16;
-            const char* fa = at + wm * FM * ORTH_BLOCK;
-            const char* fb = at + (PA * FA + wn * FN) * ORTH_BLOCK;
-            f16x8_t b[PB][FN];
-#pragma unroll
-            for (int p = 0; p < PB; ++p)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) b[p][j] = *(const f16x8_t*)(fb + (p * FB + j) * ORTH_BLOCK);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                f16x8_t a[PA];
-#pragma unroll
-                for (int p = 0; p < PA; ++p) a[p] = *(const f16x8_t*)(fa + (p * FA + i) * ORTH_BLOCK);
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[0], acc[i][j], 0, 0, 0);
-                if constexpr (PB == 2) {
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][j], a[0], acc[i][j], 0, 0, 0);
-                }
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][j], a[1], acc[i][j], 0, 0, 0);
-                }
-            }
-            stage = stage == STAGES - 1 ? 0 : stage + 1;
+            if (s + STAGES - 1 < stages) issue(s + STAGES - 1, place == 0 ? STAGES - 1 : place - 1);
+            read(place);
+            multiply(s, [](auto) {});
+            place = place == STAGES - 1 ? 0 : place + 1;
         }
     }
 
-    // A lane has the columns 4 (lane / 16) + 0..3 of row lane % 16 of every fragment.
-    const int i = lane & 15, q = lane >> 4;
+    // A lane has the columns 4 q + 0..3 of row i of every fragment.
+    const int i = i16, q = q16;
     const int row0 = (tm * FA + wm * FM) * 16, col0 = (tn * FB + wn * FN) * 16;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
@@ -201,22 +231,22 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             f32x4_t v = acc[m][n];
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] *= g.alpha;
-            // within the block of 32 columns: 16 rows times (c % 32) / 8 columns of eight
-            const int64_t here = ((int64_t)(r >> 4) * (CIN > 0 ? g.cin.blocks : g.c.blocks) + (c >> 5)) * ORTH_BLOCK + (i + 16 * ((c >> 3 & 2) + (q >> 1))) * 16 + (q & 1) * 8;
-            if constexpr (CIN > 0) {
-                const char* in = g.cin.part[0] + matrix * g.cin.matrix + here;
-                const u32x2_t hi = *(const u32x2_t*)in;
-                v[0] = fmaf(g.beta, f16_lo(hi[0]), v[0]), v[1] = fmaf(g.beta, f16_hi(hi[0]), v[1]);
-                v[2] = fmaf(g.beta, f16_lo(hi[1]), v[2]), v[3] = fmaf(g.beta, f16_hi(hi[1]), v[3]);
-                if constexpr (CIN == 2) {
-                    const u32x2_t lo = *(const u32x2_t*)(g.cin.part[1] + matrix * g.cin.matrix + here);
-                    v[0] = fmaf(g.beta, f16_lo(lo[0]), v[0]), v[1] = fmaf(g.beta, f16_hi(lo[0]), v[1]);
-                    v[2] = fmaf(g.beta, f16_lo(lo[1]), v[2]), v[3] = fmaf(g.beta, f16_hi(lo[1]), v[3]);
+            const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (c >> 3 & 2) + (q >> 1)) * 16 + (q & 1) * 8;
+            if constexpr (CIN) {
+                const u32x2_t hi = *(const u32x2_t*)(g.cin.part[0] + matrix * g.cin.matrix + here), lo = *(const u32x2_t*)(g.cin.part[1] + matrix * g.cin.matrix + here);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t h = hi[j >> 1], l = lo[j >> 1];
+                    v[j] = fmaf(g.beta, j & 1 ? f16_hi(h) + f16_hi(l) : f16_lo(h) + f16_lo(l), v[j]);
+                }
+            }
+            if constexpr (SYM) {
+                if (r == c) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] += 4 * q + j == i ? g.diagonal : 0.f;
                 }
             }
             if constexpr (OUT == ORTH_SQUARE || OUT == ORTH_BLOCKS) {
-                // the transpose's block: 16 columns times (r % 32) / 8 groups of eight rows
-                const int64_t there = ((int64_t)(c >> 4) * g.ct.blocks + (r >> 5)) * ORTH_BLOCK + (4 * q + (i & 3) + 16 * ((r >> 3 & 2) + (i >> 3))) * 16 + (i >> 2 & 1) * 8;
                 uint32_t w[2] = {pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
@@ -225,11 +255,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
                         w[0] = pack_f16(v[0] - f16_lo(h0), v[1] - f16_hi(h0));
                         w[1] = pack_f16(v[2] - f16_lo(h1), v[3] - f16_hi(h1));
                     }
-                    *(u32x2_t*)(g.c.part[p] + matrix * g.c.matrix + here) = u32x2_t{w[0], w[1]};
-                    if (!SYM || tm != tn) {
+                    char* to = g.c.part[p] + matrix * g.c.matrix;
+                    *(u32x2_t*)(to + here) = u32x2_t{w[0], w[1]};
+                    if (SYM && tm != tn) {  // the same on the other side, 4 rows of a column a lane
+                        const int64_t there = ((int64_t)(c >> 4) * g.c.blocks + (r >> 5)) * ORTH_BLOCK + orth_piece(4 * q + (i & 3), (r >> 3 & 2) + (i >> 3)) * 16 + (i >> 2 & 1) * 8;
                         uint32_t x = w[0], y = w[1];
                         turn_f16(x, y);
-                        *(u32x2_t*)(g.ct.part[p] + matrix * g.ct.matrix + there) = u32x2_t{x, y};
+                        *(u32x2_t*)(to + there) = u32x2_t{x, y};
                     }
                 }
             } else {
@@ -269,7 +301,8 @@ struct OrthIn {
     double* partials;    // [matrices][parts]
     int parts;
     float eps;
-    OrthOperand x, xt;   // G in blocks along its columns, and along its rows
+    int tall;            // G^T is what is put into blocks
+    OrthOperand x;
 };
 
 template <typename T> static __device__ inline float value_of(const T* p) { return (float)*p; }
@@ -301,7 +334,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_squares_k
     if (threadIdx.x == 0) in.partials[(int64_t)blockIdx.y * in.parts + blockIdx.x] = s;
 }
 
-// 64 x 64 values into blocks of both kinds, in two parts
+// 64 x 64 values into blocks, in two parts
 template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_kernel(OrthIn in) {
     __shared__ double lds[kThreads / 64];
     __shared__ float tile[64][65];
@@ -315,24 +348,21 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
         tile[r][c] = r0 + r < in.rows && c0 + c < in.cols ? (float)((double)value_of(g + (int64_t)(r0 + r) * in.ld + c0 + c) * scale) : 0.f;
     }
     __syncthreads();
-    for (int k = threadIdx.x; k < 2 * 512; k += kThreads) {  // 16-byte pieces: 8 blocks of 64 lanes of each kind
-        const bool turned = k >= 512;
-        const int piece = k & 511, l = piece & 63, br = piece >> 7, bc = piece >> 6 & 1;  // 4 x 2 blocks
-        const int row = br * 16 + (l & 15), col = bc * 32 + (l >> 4) * 8;
+    for (int k = threadIdx.x; k < 512; k += kThreads) {  // 4 x 2 blocks of 64 pieces
+        const int row = (k >> 7) * 16 + (k & 15), g8 = k >> 4 & 3, col = (k >> 6 & 1) * 32 + g8 * 8;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = turned ? tile[col + j][row] : tile[row][col + j];
+        for (int j = 0; j < 8; ++j) v[j] = in.tall ? tile[col + j][row] : tile[row][col + j];
         u32x4_t hi, lo;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             hi[j] = pack_f16(v[2 * j], v[2 * j + 1]);
             lo[j] = pack_f16(v[2 * j] - f16_lo(hi[j]), v[2 * j + 1] - f16_hi(hi[j]));
         }
-        const OrthOperand& o = turned ? in.xt : in.x;
-        const int R = (turned ? c0 : r0) / 16 + br, C = (turned ? r0 : c0) / 32 + bc;
-        const int64_t at = matrix * o.matrix + ((int64_t)R * o.blocks + C) * ORTH_BLOCK + l * 16;
-        *(u32x4_t*)(o.part[0] + at) = hi;
-        *(u32x4_t*)(o.part[1] + at) = lo;
+        const int R = (in.tall ? c0 : r0) / 16 + (k >> 7), C = (in.tall ? r0 : c0) / 32 + (k >> 6 & 1);
+        const int64_t at = matrix * in.x.matrix + ((int64_t)R * in.x.blocks + C) * ORTH_BLOCK + orth_piece(k & 15, g8) * 16;
+        *(u32x4_t*)(in.x.part[0] + at) = hi;
+        *(u32x4_t*)(in.x.part[1] + at) = lo;
     }
 }
 
@@ -358,10 +388,10 @@ Size size_of_matrix(int rows, int cols) {
     return z;
 }
 
-// X in two parts, X^T in two parts twice (one is read while the next is written), S and P in two parts; the partial sums
-int64_t matrix_bytes(const Size& z) { return 6 * z.x + 4 * z.s + 4096; }
+// X in two parts, twice (one is read while the next is written); S, Q, T and R in two parts; the partial sums
+int64_t matrix_bytes(const Size& z) { return 4 * z.x + 8 * z.s + 4096; }
 
-template <int PA, int PB, int CIN, int PARTS, int OUT> hipError_t product(const OrthArgs& g, int tile, hipStream_t st) {
+template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipError_t product(const OrthArgs& g, int tile, hipStream_t st) {
     auto run = [&](auto kernel, int bytes, int threads) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
@@ -369,13 +399,15 @@ template <int PA, int PB, int CIN, int PARTS, int OUT> hipError_t product(const 
         return hipGetLastError();
     };
     constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
-    if (tile == 256) return run(orth_product_kernel<PA, PB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
-    return run(orth_product_kernel<PA, PB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    if (tile == 256) return run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
+    return run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
 }
 
-OrthOperand operand(char*& at, int64_t plane, int parts, int blocks, int matrices) {
+struct Buffers { OrthOperand x[2], s, q, t, r; };
+
+OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
     OrthOperand o = {};
-    for (int p = 0; p < parts; ++p) {
+    for (int p = 0; p < 2; ++p) {
         o.part[p] = at;
         at += plane * matrices;
     }
@@ -384,42 +416,40 @@ OrthOperand operand(char*& at, int64_t plane, int parts, int blocks, int matrice
     return o;
 }
 
-template <bool F32> hipError_t steps_of(const OrthTask& t, const Size& z, const OrthIn& in, OrthOperand x, OrthOperand xt, OrthOperand xt2, OrthOperand s,
-                                        OrthOperand p, int count, void* out, hipStream_t st) {
-    constexpr int PARTS = F32 ? 2 : 1;
-    const int nt = z.n / z.tile, mt = z.m / z.tile;
-    for (int k = 0; k < t.steps; ++k) {
-        const float *abc = t.coefficients + 3 * k, a = abc[0], b = abc[1], c = abc[2];
+// The steps of `count` matrices whose X lies in w.x[0]
+template <bool F32> struct Steps {
+    const OrthTask& t;
+    const Size& z;
+    Buffers& w;
+    int count;
+    void* out;
+    hipStream_t st;
+
+    OrthArgs square(const OrthOperand& a, const OrthOperand& b, const OrthOperand& c, float alpha) const {  // c = alpha a b, symmetric
         OrthArgs g = {};
         g.matrices = count;
-        g.mt = g.nt = nt;
-        g.tiles = nt * (nt + 1) / 2;
-        g.a = g.b = x;
-        g.c = g.ct = s;
-        g.steps = z.m / 32;
-        g.alpha = S_SCALE / (X_SCALE * X_SCALE);
-        hipError_t e = product<PARTS, PARTS, 0, 2, ORTH_SQUARE>(g, z.tile, st);
-        if (e != hipSuccess) return e;
-        g.a = g.b = g.cin = s;
-        g.c = g.ct = p;
+        g.mt = g.nt = z.n / z.tile;
+        g.tiles = g.mt * (g.mt + 1) / 2;
+        g.a = a, g.b = b, g.c = c;
+        g.steps = a.blocks;
+        g.alpha = alpha;
+        return g;
+    }
+    // X = (q + diagonal I) X, into the other buffer or to the caller
+    template <int PARTS, bool DIAG> hipError_t apply(const OrthOperand& q, float diagonal, bool last) {
+        OrthArgs g = {};
+        g.matrices = count;
+        g.mt = z.n / z.tile, g.nt = z.m / z.tile;
+        g.tiles = g.mt * g.nt;
+        g.a = q, g.b = w.x[0], g.c = w.x[1];
         g.steps = z.n / 32;
-        g.alpha = c * P_SCALE / (S_SCALE * S_SCALE);
-        g.beta = b * P_SCALE / S_SCALE;
-        e = product<2, 2, 2, PARTS, ORTH_SQUARE>(g, z.tile, st);
-        if (e != hipSuccess) return e;
-        g.a = p;
-        g.b = xt;
-        g.cin = g.c = x;
-        g.ct = xt2;
-        g.mt = nt;
-        g.nt = mt;
-        g.tiles = nt * mt;
-        const bool last = k == t.steps - 1;
-        g.alpha = (last ? t.scale / X_SCALE : 1.f) / P_SCALE;
-        g.beta = last ? t.scale / X_SCALE * a : a;
+        g.alpha = 1.f / Q_SCALE;
+        g.diagonal = diagonal * Q_SCALE;
+        hipError_t e;
         if (!last) {
-            e = product<PARTS, 2, 2, 2, ORTH_BLOCKS>(g, z.tile, st);
+            e = product<PARTS, 2, true, false, 2, ORTH_BLOCKS, DIAG>(g, z.tile, st);
         } else {
+            g.alpha *= t.scale / X_SCALE;
             g.out = out;
             g.out_matrix = t.out_matrix;
             g.out_ld = t.out_ld;
@@ -428,15 +458,31 @@ template <bool F32> hipError_t steps_of(const OrthTask& t, const Size& z, const 
             g.cols = g.tall ? t.rows : t.cols;
             const int size = F32 ? 4 : 2;
             g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
-            e = product<PARTS, 2, 2, 0, F32 ? ORTH_F32 : ORTH_BF16>(g, z.tile, st);
+            e = product<PARTS, 2, true, false, 0, F32 ? ORTH_F32 : ORTH_BF16, DIAG>(g, z.tile, st);
         }
-        if (e != hipSuccess) return e;
-        const OrthOperand o = xt;
-        xt = xt2;
-        xt2 = o;
+        const OrthOperand o = w.x[0];
+        w.x[0] = w.x[1];
+        w.x[1] = o;
+        return e;
     }
-    return hipSuccess;
-}
+    hipError_t run() {
+        constexpr int PARTS = F32 ? 2 : 1;
+        hipError_t e = hipSuccess;
+        for (int k = 0; k < t.steps && e == hipSuccess; ++k) {
+            const float *abc = t.coefficients + 3 * k, a = abc[0], b = abc[1], c = abc[2];
+            e = product<PARTS, PARTS, false, false, 2, ORTH_SQUARE, false>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
+            if (e != hipSuccess) break;
+            OrthArgs g = square(w.s, w.s, w.q, c * Q_SCALE / (S_SCALE * S_SCALE));
+            g.cin = w.s;
+            g.beta = b * Q_SCALE / S_SCALE;
+            g.diagonal = F32 ? a * Q_SCALE : 0.f;  // (one part has too few digits for it: apply adds it)
+            e = product<2, 2, false, true, PARTS, ORTH_SQUARE, false>(g, z.tile, st);
+            if (e != hipSuccess) break;
+            e = apply<PARTS, PARTS == 1>(w.q, a, k == t.steps - 1);
+        }
+        return e;
+    }
+};
 
 }  // namespace
 
@@ -458,8 +504,9 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
     for (int e0 = 0; e0 < t.E; e0 += at_once) {
         const int count = t.E - e0 < at_once ? t.E - e0 : at_once;
         char* at = (char*)workspace;
-        const OrthOperand x = operand(at, z.x, 2, z.m / 32, count), xt = operand(at, z.x, 2, z.n / 32, count), xt2 = operand(at, z.x, 2, z.n / 32, count);
-        const OrthOperand s = operand(at, z.s, 2, z.n / 32, count), p = operand(at, z.s, 2, z.n / 32, count);
+        Buffers w;
+        for (OrthOperand& x : w.x) x = operand(at, z.x, z.m / 32, count);
+        for (OrthOperand* o : {&w.s, &w.q, &w.t, &w.r}) *o = operand(at, z.s, z.n / 32, count);
         OrthIn in = {};
         in.g = (const char*)t.g + e0 * t.g_matrix * size_in;
         in.matrix = t.g_matrix;
@@ -469,8 +516,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.partials = (double*)at;
         in.parts = z.parts;
         in.eps = t.eps;
-        in.x = tall ? xt : x;
-        in.xt = tall ? x : xt;
+        in.tall = tall;
+        in.x = w.x[0];
         const dim3 blocks((tall ? z.n : z.m) / 64, (tall ? z.m : z.n) / 64, count);
         if (t.in_f32) {
             orth_squares_kernel<float><<<dim3(z.parts, count), kThreads, 0, st>>>(in);
@@ -482,7 +529,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         void* out = (char*)t.out + e0 * t.out_matrix * size_out;
-        e = t.out_f32 ? steps_of<true>(t, z, in, x, xt, xt2, s, p, count, out, st) : steps_of<false>(t, z, in, x, xt, xt2, s, p, count, out, st);
+        e = t.out_f32 ? Steps<true>{t, z, w, count, out, st}.run() : Steps<false>{t, z, w, count, out, st}.run();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

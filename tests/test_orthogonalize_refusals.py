@@ -39,7 +39,7 @@ def test_c_entry(lib):
                    dict(sg=6399), dict(so=0), dict(sg=1 << 41), dict(ldg=(1 << 21) + 1), dict(ws=None), dict(ws=at(2, 16)), dict(out=at(0)), dict(out=at(0, 400)),
                    dict(out=at(0, 4), ot=1), dict(ws=at(0)), dict(ws=at(1)), dict(out=at(0), ot=1, so=6500)):
         assert call(**change) == INVALID, change
-    for change in (dict(E=257), dict(rows=(1 << 17) + 1), dict(cols=(1 << 17) + 1)):
+    for change in (dict(E=257), dict(rows=(1 << 17) + 1), dict(cols=(1 << 17) + 1), dict(rows=1 << 15, cols=(1 << 14) + 1)):
         assert call(**change) == SHAPE, change
 
 
@@ -48,8 +48,8 @@ def test_workspace(lib):
     assert ws(0, 8, 8) == ws(257, 8, 8) == ws(1, 0, 8) == ws(1, 8, (1 << 17) + 1) == 0
     assert ws(8, 100, 50) == ws(8, 50, 100) <= 8 * ws(1, 100, 50)
     assert ws(256, 2048, 2048) <= 8 << 30 < 256 * ws(1, 2048, 2048)
-    for rows, cols in ((1, 1), (4096, 14336), (7168, 2048)):   # about 12 bytes a value, and whole tiles
-        assert ws(1, rows, cols) <= 12 * (rows + 256) * (cols + 256) + 16 * (min(rows, cols) + 256) ** 2
+    for rows, cols in ((1, 1), (4096, 14336), (7168, 2048)):   # about 8 bytes a value, and whole tiles
+        assert ws(1, rows, cols) <= 8 * (rows + 256) * (cols + 256) + 16 * (min(rows, cols) + 256) ** 2
 
 
 def test_the_binding_refuses(lib):
