@@ -388,8 +388,8 @@ Size size_of_matrix(int rows, int cols) {
     return z;
 }
 
-// X in two parts, twice (one is read while the next is written); S, Q, T and R in two parts; the partial sums
-int64_t matrix_bytes(const Size& z) { return 4 * z.x + 8 * z.s + 4096; }
+// X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums
+int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + 4096; }
 
 template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipError_t product(const OrthArgs& g, int tile, hipStream_t st) {
     auto run = [&](auto kernel, int bytes, int threads) {
@@ -403,7 +403,7 @@ template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipE
     return run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
 }
 
-struct Buffers { OrthOperand x[2], s, q, t, r; };
+struct Buffers { OrthOperand x[2], s, q, t; };
 
 OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
     OrthOperand o = {};
@@ -465,20 +465,49 @@ template <bool F32> struct Steps {
         w.x[1] = o;
         return e;
     }
+    // S = X X^T
+    hipError_t gram() const {
+        return product<F32 ? 2 : 1, F32 ? 2 : 1, false, false, 2, ORTH_SQUARE, false>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
+    }
+    // to = a I + b S + c S S; in one part without a I, for which it has too few digits
+    template <int PARTS> hipError_t polynomial(const OrthOperand& to, const float* abc) const {
+        OrthArgs g = square(w.s, w.s, to, abc[2] * Q_SCALE / (S_SCALE * S_SCALE));
+        g.cin = w.s;
+        g.beta = abc[1] * Q_SCALE / S_SCALE;
+        g.diagonal = PARTS == 2 ? abc[0] * Q_SCALE : 0.f;
+        return product<2, 2, false, true, PARTS, ORTH_SQUARE, false>(g, z.tile, st);
+    }
+    // to = a q, of matrices that commute
+    hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to) const {
+        return product<2, 2, false, false, 2, ORTH_SQUARE, false>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
+    }
+    hipError_t one_step(const float* abc, bool last) {
+        hipError_t e = gram();
+        if (e == hipSuccess) e = polynomial<F32 ? 2 : 1>(w.q, abc);
+        if (e == hipSuccess) e = apply<F32 ? 2 : 1, !F32>(w.q, abc[0], last);
+        return e;
+    }
+    hipError_t two_steps(const float* abc, bool last) {
+        hipError_t e = gram();
+        if (e == hipSuccess) e = polynomial<2>(w.q, abc);
+        if (e == hipSuccess) e = times(w.s, w.q, w.t);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s);  // Q S Q = (Q X) (Q X)^T
+        if (e == hipSuccess) e = polynomial<2>(w.t, abc + 3);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s);
+        if (e == hipSuccess) e = apply<2, false>(w.s, 0.f, last);
+        return e;
+    }
     hipError_t run() {
-        constexpr int PARTS = F32 ? 2 : 1;
+        // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones (with one part of X in S
+        // and P nine times their cost, for everything between has two parts then).  Where X is wide that is less work.
+        const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
+        const bool pairs = half * mt + nt * mt * nt > (F32 ? 3 : 9) * half * nt;
         hipError_t e = hipSuccess;
-        for (int k = 0; k < t.steps && e == hipSuccess; ++k) {
-            const float *abc = t.coefficients + 3 * k, a = abc[0], b = abc[1], c = abc[2];
-            e = product<PARTS, PARTS, false, false, 2, ORTH_SQUARE, false>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
-            if (e != hipSuccess) break;
-            OrthArgs g = square(w.s, w.s, w.q, c * Q_SCALE / (S_SCALE * S_SCALE));
-            g.cin = w.s;
-            g.beta = b * Q_SCALE / S_SCALE;
-            g.diagonal = F32 ? a * Q_SCALE : 0.f;  // (one part has too few digits for it: apply adds it)
-            e = product<2, 2, false, true, PARTS, ORTH_SQUARE, false>(g, z.tile, st);
-            if (e != hipSuccess) break;
-            e = apply<PARTS, PARTS == 1>(w.q, a, k == t.steps - 1);
+        for (int k = 0; k < t.steps && e == hipSuccess;) {
+            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
+            const float* abc = t.coefficients + 3 * k;
+            k += n;
+            e = n == 2 ? two_steps(abc, k == t.steps) : one_step(abc, k == t.steps);
         }
         return e;
     }
@@ -506,7 +535,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         char* at = (char*)workspace;
         Buffers w;
         for (OrthOperand& x : w.x) x = operand(at, z.x, z.m / 32, count);
-        for (OrthOperand* o : {&w.s, &w.q, &w.t, &w.r}) *o = operand(at, z.s, z.n / 32, count);
+        for (OrthOperand* o : {&w.s, &w.q, &w.t}) *o = operand(at, z.s, z.n / 32, count);
         OrthIn in = {};
         in.g = (const char*)t.g + e0 * t.g_matrix * size_in;
         in.matrix = t.g_matrix;
