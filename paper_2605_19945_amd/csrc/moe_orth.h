@@ -30,6 +30,8 @@ struct OrthArgs {
     float alpha, beta;
     float diagonal;        // added to the diagonal of a symmetric result; or, times b, to a product that is not (in the units of a)
     int steps;             // blocks of the reduction
+    int splits;            // ranges that it is cut into; with more than one, sums go to `part`
+    float* part;           // [matrices][tiles][splits][fragments of a tile][64 lanes][4]
     int mt, nt;            // tiles of a matrix (symmetric: mt == nt, those on and above the diagonal)
     int tiles, matrices;   // tiles of a matrix that are computed
     // the last product: results in the caller's rows

@@ -29,10 +29,87 @@ static __device__ inline void place_symmetric(int t, int mt, int* m, int* n) {
     *n = r + t - (r * mt - r * (r - 1) / 2);
 }
 
+// The tile t of a matrix: (row, column) of tiles
+template <bool SYM> static __device__ inline void place(const OrthArgs& g, int t, int* tm, int* tn) {
+    int m, n;
+    if constexpr (SYM) {
+        place_symmetric(t, g.mt, &m, &n);
+    } else {  // bands of 8 tiles
+        const int band = t / (8 * g.nt), r = t - band * 8 * g.nt, h = min(8, g.mt - 8 * band);
+        n = r / h;
+        m = 8 * band + r - n * h;
+    }
+    *tm = __builtin_amdgcn_readfirstlane(m);
+    *tn = __builtin_amdgcn_readfirstlane(n);
+}
+
+// A fragment's sums on their way out: a lane has the columns c + 4 q + 0..3 of row r + i (i = lane % 16, q = lane / 16).  CIN: beta times another
+// matrix (in two parts) is added.  OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any
+// result in blocks; or its type in the caller's rows.  PARTS: of a result in blocks.
+template <bool CIN, int PARTS, int OUT> static __device__ inline void finish(const OrthArgs& g, f32x4_t v, int lane, int matrix, int r, int c, bool both) {
+    const int i = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= g.alpha;
+    const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (c >> 3 & 2) + (q >> 1)) * 16 + (q & 1) * 8;
+    if constexpr (CIN) {
+        const u32x2_t hi = *(const u32x2_t*)(g.cin.part[0] + matrix * g.cin.matrix + here), lo = *(const u32x2_t*)(g.cin.part[1] + matrix * g.cin.matrix + here);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t h = hi[j >> 1], l = lo[j >> 1];
+            v[j] = fmaf(g.beta, j & 1 ? f16_hi(h) + f16_hi(l) : f16_lo(h) + f16_lo(l), v[j]);
+        }
+    }
+    if constexpr (OUT == ORTH_SQUARE) {
+        if (r == c) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += 4 * q + j == i ? g.diagonal : 0.f;
+        }
+    }
+    if constexpr (OUT == ORTH_SQUARE || OUT == ORTH_BLOCKS) {
+        uint32_t w[2] = {pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            if (p == 1) {
+                const uint32_t h0 = w[0], h1 = w[1];
+                w[0] = pack_f16(v[0] - f16_lo(h0), v[1] - f16_hi(h0));
+                w[1] = pack_f16(v[2] - f16_lo(h1), v[3] - f16_hi(h1));
+            }
+            char* to = g.c.part[p] + matrix * g.c.matrix;
+            *(u32x2_t*)(to + here) = u32x2_t{w[0], w[1]};
+            if (OUT == ORTH_SQUARE && both) {  // the same on the other side, 4 rows of a column a lane
+                const int64_t there = ((int64_t)(c >> 4) * g.c.blocks + (r >> 5)) * ORTH_BLOCK + orth_piece(4 * q + (i & 3), (r >> 3 & 2) + (i >> 3)) * 16 + (i >> 2 & 1) * 8;
+                uint32_t x = w[0], y = w[1];
+                turn_f16(x, y);
+                *(u32x2_t*)(to + there) = u32x2_t{x, y};
+            }
+        }
+    } else {
+        if (g.tall) turn_f32(v);  // rows and columns change places: 4 of the caller's neighbouring values again
+        const int rr = g.tall ? c + 4 * q + (i & 3) : r + i, cc = g.tall ? r + (i & 12) : c + 4 * q;
+        const int rows = g.tall ? g.cols : g.rows, cols = g.tall ? g.rows : g.cols;
+        if (rr >= rows) return;
+        const int64_t to = matrix * g.out_matrix + rr * g.out_ld + cc;
+        if (g.vec && cc + 3 < cols) {
+            if constexpr (OUT == ORTH_F32) {
+                *(f32x4_t*)((float*)g.out + to) = v;
+            } else {
+                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+                *(bf16x4_t*)((uint16_t*)g.out + to) = bf16x4_t{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (cc + j >= cols) continue;
+                if constexpr (OUT == ORTH_F32) ((float*)g.out)[to + j] = v[j];
+                else ((__bf16*)g.out)[to + j] = (__bf16)v[j];
+            }
+        }
+    }
+}
+
 // PA, PB: parts of A and B.  TB: B lies with the reduction along its rows (otherwise along its columns).  WM x WN wavefronts of FM x FN
-// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN: beta times another matrix (in two parts) is added.
-// OUT: a symmetric result in blocks, whose tiles above the diagonal are written to both sides; any result in blocks; or its type in the caller's
-// rows.  PARTS: of a result in blocks.  DIAG: A is multiplied with `diagonal` added to its diagonal.
+// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN, PARTS, OUT: what finish makes of the sums.
+// DIAG: A is multiplied with `diagonal` added to its diagonal.
 template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool CIN, int PARTS, int OUT, bool DIAG>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
@@ -43,19 +120,14 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     const int wm = wave / WN, wn = wave % WN, i16 = lane & 15, q16 = lane >> 4;
 
     // neighbouring tiles on one XCD (workgroup number % 8): one stretch of the list each
-    const int total = g.tiles * g.matrices, xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
-    const int item = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
-    const int matrix = item / g.tiles, t = item - matrix * g.tiles;
+    const int total = g.tiles * g.matrices * g.splits, xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
+    int item = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
+    const int64_t slot = item;
+    const int split = item % g.splits;
+    item /= g.splits;
+    const int matrix = item / g.tiles;
     int tm, tn;
-    if constexpr (SYM) {
-        place_symmetric(t, g.mt, &tm, &tn);
-    } else {  // bands of 8 tiles
-        const int band = t / (8 * g.nt), r = t - band * 8 * g.nt, h = min(8, g.mt - 8 * band);
-        tn = r / h;
-        tm = 8 * band + r - tn * h;
-    }
-    tm = __builtin_amdgcn_readfirstlane(tm);
-    tn = __builtin_amdgcn_readfirstlane(tn);
+    place<SYM>(g, item - matrix * g.tiles, &tm, &tn);
 
     // A stage's loads: block row i * WAVES + wave of an operand along its columns; of one along its rows block row i, block column wave.
     const uint32_t panel = (uint32_t)g.a.blocks * ORTH_BLOCK, panel_b = (uint32_t)g.b.blocks * ORTH_BLOCK;
@@ -68,17 +140,18 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         db[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix + at, TB ? (uint32_t)(g.b.matrix - at) : FB * panel_b);
     }
     constexpr int NA = FA / WAVES, NB = FB / WAVES, PER = PA * NA + PB * NB;  // loads of a block of the reduction
-    uint32_t offset[NA], offset_b[NB];
-#pragma unroll
-    for (int i = 0; i < NA; ++i) offset[i] = (uint32_t)(i * WAVES + wave) * panel + lane * 16;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) offset_b[i] = (TB ? i * panel_b + wave * ORTH_BLOCK : (uint32_t)(i * WAVES + wave) * panel_b) + lane * 16;
+    // (places beside the lane's are scalars: a register a load more, and the longest loop spilled)
+    const uint32_t mine = lane * 16, wave_a = wave * panel, wave_b = TB ? wave * ORTH_BLOCK : wave * panel_b;
     const uint32_t base = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)) + wave * ORTH_BLOCK;
     auto issue_one = [&](auto load, int s, int place) {  // one load of stage s
         constexpr int k = decltype(load)::value / PER, i = decltype(load)::value % PER, ib = i - PA * NA;
-        const uint32_t to = base + place * (FRAGS * ORTH_BLOCK), at = (uint32_t)(s * KS + k) * ORTH_BLOCK;
-        if constexpr (i < PA * NA) orth_load(to + (KS * (i / NA) * FA + k * FA + i % NA * WAVES) * ORTH_BLOCK, offset[i % NA], da[i / NA], at);
-        else orth_load(to + (KS * (PA * FA + ib / NB * FB) + k * FB + ib % NB * WAVES) * ORTH_BLOCK, offset_b[ib % NB], db[ib / NB], TB ? (uint32_t)(s * KS + k) * 2 * panel_b : at);
+        const uint32_t to = base + place * (FRAGS * ORTH_BLOCK), at = (uint32_t)(s * KS + k);
+        if constexpr (i < PA * NA) {
+            orth_load(to + (KS * (i / NA) * FA + k * FA + i % NA * WAVES) * ORTH_BLOCK, mine, da[i / NA], at * ORTH_BLOCK + wave_a + i % NA * WAVES * panel);
+        } else {
+            const uint32_t rows = TB ? (2 * at + ib % NB) * panel_b : at * ORTH_BLOCK + ib % NB * WAVES * panel_b;
+            orth_load(to + (KS * (PA * FA + ib / NB * FB) + k * FB + ib % NB * WAVES) * ORTH_BLOCK, mine, db[ib / NB], rows + wave_b);
+        }
     };
     auto issue = [&](int s, int place) { orth_repeat<LOADS>([&](auto load) { issue_one(load, s, place); }); };
 
@@ -89,7 +162,7 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     f16x8_t a[KS][PA][FM], b[KS][PB][FN];
-    const int stages = g.steps / KS;
+    const int stages = g.steps / KS, first = (int)((int64_t)stages * split / g.splits), end = (int)((int64_t)stages * (split + 1) / g.splits);
     const int at_row = orth_piece(i16, q16) * 16;
     // of the transposing read: lane i of 16 asks for 4 columns of row 8 (q % 2) + i / 4 and is given column i of 4 rows; the next 4 rows lie where
     // the exclusive or with 12 of the rows puts them
@@ -173,13 +246,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         // asks for stage s + 1, into the place that the second group left in the turn before), in 2 s + 1 the second; a stage has two turns to
         // arrive.
         static_assert(STAGES == 2, "");
-        issue(0, 0);
+        issue(first, first & 1);
         orth_wait<0>();
         orth_barrier();
         if (wave < 4) {
-            for (int s = 0; s < stages; ++s) {
+            for (int s = first; s < end; ++s) {
                 read(s & 1);
-                if (s + 1 < stages) issue(s + 1, (s + 1) & 1);
+                if (s + 1 < end) issue(s + 1, (s + 1) & 1);
                 orth_barrier();
                 multiply(s, [](auto) {});
                 orth_wait<0>();
@@ -187,13 +260,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             }
             orth_barrier();
         } else {
-            if (1 < stages) issue(1, 1);
+            if (first + 1 < end) issue(first + 1, (first + 1) & 1);
             orth_barrier();
-            for (int s = 0; s < stages; ++s) {
+            for (int s = first; s < end; ++s) {
                 read(s & 1);
                 orth_wait<0>();
                 orth_barrier();
-                const bool more = s + 2 < stages;
+                const bool more = s + 2 < end;
                 multiply(s, [&](auto row) {  // its loads among the products
                     constexpr int r = decltype(row)::value;
                     if constexpr (r * LOADS % ROWS < LOADS && r * LOADS / ROWS < LOADS) {
@@ -205,90 +278,131 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         }
     } else {
         orth_repeat<STAGES - 1>([&](auto s) {
-            if (decltype(s)::value < stages) issue(decltype(s)::value, decltype(s)::value);
+            if (first + decltype(s)::value < end) issue(first + decltype(s)::value, decltype(s)::value);
         });
         int place = 0;
-        for (int s = 0; s < stages; ++s) {
+        for (int s = first; s < end; ++s) {
             // this stage has arrived; the last ones have fewer behind them and wait for all
-            if (s + STAGES - 1 <= stages) orth_wait<(STAGES - 2) * LOADS>();
+            if (s + STAGES - 1 <= end) orth_wait<(STAGES - 2) * LOADS>();
             else orth_wait<0>();
             orth_barrier();  // of every wavefront's; and all are done with the stage before
-            if (s + STAGES - 1 < stages) issue(s + STAGES - 1, place == 0 ? STAGES - 1 : place - 1);
+            if (s + STAGES - 1 < end) issue(s + STAGES - 1, place == 0 ? STAGES - 1 : place - 1);
             read(place);
             multiply(s, [](auto) {});
             place = place == STAGES - 1 ? 0 : place + 1;
         }
     }
 
-    // A lane has the columns 4 q + 0..3 of row i of every fragment.
-    const int i = i16, q = q16;
+    int out_lane = lane;
+    asm volatile("" : "+v"(out_lane));  // the compiler would form the results' places before the loop and spill them
+    if (g.splits > 1) {
+        f32x4_t* part = (f32x4_t*)g.part + slot * (FA * FB * 64) + out_lane;
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n) part[((wm * FM + m) * FB + wn * FN + n) * 64] = acc[m][n];
+        return;
+    }
     const int row0 = (tm * FA + wm * FM) * 16, col0 = (tn * FB + wn * FN) * 16;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
+        if (CIN) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < FN; ++n) {
-            const int r = row0 + m * 16, c = col0 + n * 16;  // of the fragment
-            f32x4_t v = acc[m][n];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] *= g.alpha;
-            const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (c >> 3 & 2) + (q >> 1)) * 16 + (q & 1) * 8;
-            if constexpr (CIN) {
-                const u32x2_t hi = *(const u32x2_t*)(g.cin.part[0] + matrix * g.cin.matrix + here), lo = *(const u32x2_t*)(g.cin.part[1] + matrix * g.cin.matrix + here);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t h = hi[j >> 1], l = lo[j >> 1];
-                    v[j] = fmaf(g.beta, j & 1 ? f16_hi(h) + f16_hi(l) : f16_lo(h) + f16_lo(l), v[j]);
-                }
-            }
-            if constexpr (SYM) {
-                if (r == c) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] += 4 * q + j == i ? g.diagonal : 0.f;
-                }
-            }
-            if constexpr (OUT == ORTH_SQUARE || OUT == ORTH_BLOCKS) {
-                uint32_t w[2] = {pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    if (p == 1) {
-                        const uint32_t h0 = w[0], h1 = w[1];
-                        w[0] = pack_f16(v[0] - f16_lo(h0), v[1] - f16_hi(h0));
-                        w[1] = pack_f16(v[2] - f16_lo(h1), v[3] - f16_hi(h1));
-                    }
-                    char* to = g.c.part[p] + matrix * g.c.matrix;
-                    *(u32x2_t*)(to + here) = u32x2_t{w[0], w[1]};
-                    if (SYM && tm != tn) {  // the same on the other side, 4 rows of a column a lane
-                        const int64_t there = ((int64_t)(c >> 4) * g.c.blocks + (r >> 5)) * ORTH_BLOCK + orth_piece(4 * q + (i & 3), (r >> 3 & 2) + (i >> 3)) * 16 + (i >> 2 & 1) * 8;
-                        uint32_t x = w[0], y = w[1];
-                        turn_f16(x, y);
-                        *(u32x2_t*)(to + there) = u32x2_t{x, y};
-                    }
-                }
-            } else {
-                if (g.tall) turn_f32(v);  // rows and columns change places: 4 of the caller's neighbouring values again
-                const int rr = g.tall ? c + 4 * q + (i & 3) : r + i, cc = g.tall ? r + (i & 12) : c + 4 * q;
-                const int rows = g.tall ? g.cols : g.rows, cols = g.tall ? g.rows : g.cols;
-                if (rr < rows) {
-                    const int64_t to = matrix * g.out_matrix + rr * g.out_ld + cc;
-                    if (g.vec && cc + 3 < cols) {
-                        if constexpr (OUT == ORTH_F32) {
-                            *(f32x4_t*)((float*)g.out + to) = v;
-                        } else {
-                            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-                            *(bf16x4_t*)((uint16_t*)g.out + to) = bf16x4_t{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (cc + j >= cols) continue;
-                            if constexpr (OUT == ORTH_F32) ((float*)g.out)[to + j] = v[j];
-                            else ((__bf16*)g.out)[to + j] = (__bf16)v[j];
-                        }
-                    }
-                }
-            }
-        }
+        for (int n = 0; n < FN; ++n) finish<CIN, PARTS, OUT>(g, acc[m][n], out_lane, matrix, row0 + m * 16, col0 + n * 16, tm != tn);
     }
+}
+
+// The ranges' sums added in their order, a wavefront a fragment; F x F fragments a tile
+template <int F, bool CIN, int PARTS, int OUT> __global__ __launch_bounds__(256) void orth_sums_kernel(OrthArgs g) {
+    const int64_t fragment = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = fragment / (F * F);
+    const int f = (int)(fragment - item * (F * F)), matrix = (int)(item / g.tiles), lane = threadIdx.x & 63;
+    int tm, tn;
+    place<OUT == ORTH_SQUARE>(g, (int)(item - (int64_t)matrix * g.tiles), &tm, &tn);
+    const f32x4_t* part = (const f32x4_t*)g.part + (item * g.splits * (F * F) + f) * 64 + lane;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < g.splits; ++s) v += part[(int64_t)s * (F * F * 64)];
+    finish<CIN, PARTS, OUT>(g, v, lane, matrix, (tm * F + f / F) * 16, (tn * F + f % F) * 16, tm != tn);
+}
+
+// ---- the small products of matrices of one tile of 128, S in ranges -> a I + b S + c S S, or of two steps the product of both ----
+// One workgroup a matrix, everything in LDS: two matrices of 128 x 128 in two parts, in blocks.  Wavefronts 4 x 2 of 2 x 4 fragments.
+__global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
+    extern __shared__ __align__(1024) char lds[];
+    constexpr int PLANE = 32 * ORTH_BLOCK, FM = 2, FN = 4;  // 8 x 4 blocks
+    char *s = lds, *q = lds + 2 * PLANE;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, matrix = blockIdx.x;
+    const int at_row = orth_piece(lane & 15, lane >> 4) * 16;
+    f32x4_t v[FM][FN];
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n) f(m, n, wm * FM + m, wn * FN + n);
+    };
+    // where a lane's 4 values of a fragment lie: columns 16 fn + 4 (lane / 16) + 0..3 of row 16 fm + lane % 16
+    auto at = [&](int fm, int fn) { return (fm * 4 + (fn >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (fn & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
+    auto put = [&](char* to, int64_t plane) {
+        each([&](int m, int n, int fm, int fn) {
+            const f32x4_t& x = v[m][n];
+            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
+            *(u32x2_t*)(to + at(fm, fn)) = u32x2_t{h0, h1};
+            *(u32x2_t*)(to + plane + at(fm, fn)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+        });
+    };
+    auto multiply = [&](const char* x, const char* y, float scale) {  // v = scale x y, y symmetric
+        each([&](int m, int n, int, int) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f16x8_t a[2][FM], b[2][FN];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+#pragma unroll
+                for (int m = 0; m < FM; ++m) a[p][m] = *(const f16x8_t*)(x + p * PLANE + ((wm * FM + m) * 4 + k) * ORTH_BLOCK + at_row);
+#pragma unroll
+                for (int n = 0; n < FN; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + ((wn * FN + n) * 4 + k) * ORTH_BLOCK + at_row);
+            }
+            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[0][m], v[m][n], 0, 0, 0); });
+            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][n], a[0][m], v[m][n], 0, 0, 0); });
+            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[1][m], v[m][n], 0, 0, 0); });
+        }
+        each([&](int m, int n, int, int) { v[m][n] *= scale; });
+    };
+    auto polynomial = [&](float a, float b, float c) {  // v = a I + b s + c s s
+        multiply(s, s, c * (Q_SCALE / (S_SCALE * S_SCALE)));
+        each([&](int m, int n, int fm, int fn) {
+            const u32x2_t hi = *(const u32x2_t*)(s + at(fm, fn)), lo = *(const u32x2_t*)(s + PLANE + at(fm, fn));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]);
+                v[m][n][j] = fmaf(b * (Q_SCALE / S_SCALE), x, v[m][n][j]) + (fm == fn && 4 * (lane >> 4) + j == (lane & 15) ? a * Q_SCALE : 0.f);
+            }
+        });
+    };
+
+    const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * splits * (64 * 64) + lane;
+    each([&](int m, int n, int, int) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+    for (int i = 0; i < splits; ++i) each([&](int m, int n, int fm, int fn) { v[m][n] += part[((int64_t)i * 64 + fm * 8 + fn) * 64]; });
+    each([&](int m, int n, int, int) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
+    put(s, PLANE);
+    __syncthreads();
+    polynomial(a1, b1, c1);
+    if (two) {
+        put(q, PLANE);
+        __syncthreads();
+        for (int i = 0; i < 2; ++i) {  // s = q s q = (q x) (q x)^T: they commute
+            multiply(s, q, 1.f / Q_SCALE);
+            __syncthreads();
+            put(s, PLANE);
+            __syncthreads();
+        }
+        polynomial(a2, b2, c2);
+        __syncthreads();
+        put(s, PLANE);
+        __syncthreads();
+        multiply(s, q, 1.f / Q_SCALE);
+    }
+    put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0]);
 }
 
 // ---- the way in ----
@@ -302,11 +416,32 @@ struct OrthIn {
     int parts;
     float eps;
     int tall;            // G^T is what is put into blocks
+    int vec;             // rows begin at multiples of 16 bytes
     OrthOperand x;
 };
 
 template <typename T> static __device__ inline float value_of(const T* p) { return (float)*p; }
 template <> __device__ inline float value_of<uint16_t>(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+
+// 16 bytes of values
+template <typename T> struct Words;
+template <> struct Words<float> {
+    static constexpr int N = 4;
+    static __device__ inline void open(const u32x4_t& w, float* v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
+    }
+};
+template <> struct Words<uint16_t> {
+    static constexpr int N = 8;
+    static __device__ inline void open(const u32x4_t& w, float* v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    }
+};
 
 static __device__ inline double block_sum(double v, double* lds) {
 #pragma unroll
@@ -322,13 +457,38 @@ static __device__ inline double block_sum(double v, double* lds) {
 // Squares of a matrix, in 64 bits: part blockIdx.x of the rows.
 template <typename T> __global__ __launch_bounds__(kThreads) void orth_squares_kernel(OrthIn in) {
     __shared__ double lds[kThreads / 64];
-    const T* g = (const T*)in.g + blockIdx.y * in.matrix;
-    const int per = (in.rows + in.parts - 1) / in.parts, from = blockIdx.x * per, to = min(from + per, in.rows);
+    constexpr int N = Words<T>::N;
+    const int per = (in.rows + in.parts - 1) / in.parts, from = blockIdx.x * per, to = max(min(from + per, in.rows), from);
+    const T* g = (const T*)in.g + blockIdx.y * in.matrix + from * in.ld;
     double s = 0;
-    for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * in.cols; i += kThreads) {
-        const int64_t r = i / in.cols;
-        const double v = value_of(g + (from + r) * in.ld + (i - r * in.cols));
-        s = fma(v, v, s);
+    const uint32_t words = in.vec ? in.cols / N : 0, rest = in.cols - words * N, total = (to - from) * words;
+    uint32_t i = threadIdx.x;
+    auto word = [&](uint32_t k) {
+        const uint32_t r = k / words;
+        return *(const u32x4_t*)(g + r * in.ld + (k - r * words) * N);
+    };
+    auto add = [&](const u32x4_t& w) {
+        float v[N];
+        Words<T>::open(w, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s = fma((double)v[j], (double)v[j], s);
+    };
+    if (words > 0) {
+        for (; i + 3 * kThreads < total; i += 4 * kThreads) {  // four words on their way
+            u32x4_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = word(i + k * kThreads);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) add(w[k]);
+        }
+        for (; i < total; i += kThreads) add(word(i));
+    }
+    if (rest > 0) {
+        for (uint32_t k = threadIdx.x; k < (to - from) * rest; k += kThreads) {
+            const uint32_t r = k / rest;
+            const double v = value_of(g + r * in.ld + words * N + (k - r * rest));
+            s = fma(v, v, s);
+        }
     }
     s = block_sum(s, lds);
     if (threadIdx.x == 0) in.partials[(int64_t)blockIdx.y * in.parts + blockIdx.x] = s;
@@ -338,14 +498,33 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_squares_k
 template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_kernel(OrthIn in) {
     __shared__ double lds[kThreads / 64];
     __shared__ float tile[64][65];
+    constexpr int N = Words<T>::N;
     const int matrix = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
     const T* g = (const T*)in.g + matrix * in.matrix;
+    const bool whole = in.vec && c0 + 64 <= in.cols;  // 16 values of a row a lane
+    const int row = threadIdx.x >> 2, col = (threadIdx.x & 3) * 16;
+    u32x4_t w[16 / N] = {};
+    if (whole && r0 + row < in.rows) {
+#pragma unroll
+        for (int k = 0; k < 16 / N; ++k) w[k] = *(const u32x4_t*)(g + (int64_t)(r0 + row) * in.ld + c0 + col + k * N);
+    }
     double s = 0;
     for (int i = threadIdx.x; i < in.parts; i += kThreads) s += in.partials[(int64_t)matrix * in.parts + i];
     const double scale = (double)X_SCALE / (sqrt(block_sum(s, lds)) + (double)in.eps);
-    for (int i = threadIdx.x; i < 64 * 64; i += kThreads) {
-        const int r = i >> 6, c = i & 63;
-        tile[r][c] = r0 + r < in.rows && c0 + c < in.cols ? (float)((double)value_of(g + (int64_t)(r0 + r) * in.ld + c0 + c) * scale) : 0.f;
+    if (whole) {
+        const bool live = r0 + row < in.rows;
+#pragma unroll
+        for (int k = 0; k < 16 / N; ++k) {
+            float v[N];
+            Words<T>::open(w[k], v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) tile[row][col + k * N + j] = live ? (float)((double)v[j] * scale) : 0.f;
+        }
+    } else {
+        for (int i = threadIdx.x; i < 64 * 64; i += kThreads) {
+            const int r = i >> 6, c = i & 63;
+            tile[r][c] = r0 + r < in.rows && c0 + c < in.cols ? (float)((double)value_of(g + (int64_t)(r0 + r) * in.ld + c0 + c) * scale) : 0.f;
+        }
     }
     __syncthreads();
     for (int k = threadIdx.x; k < 512; k += kThreads) {  // 4 x 2 blocks of 64 pieces
@@ -374,36 +553,82 @@ struct Size {
     int64_t x, s;    // bytes of a plane of X and of S
 };
 
-Size size_of_matrix(int rows, int cols) {
+constexpr int kUnits = 256;  // compute units
+
+// Ranges a reduction of `stages` is cut into where `tiles` tiles leave compute units without one (two small tiles share a unit): four stages
+// a range at least.
+int splits_of(int64_t tiles, int stages, int tile) {
+    const int64_t room = (tile == 256 ? kUnits : 2 * kUnits) / tiles, most = stages / 4;
+    const int64_t s = room < most ? room : most;
+    return s > 1 ? (int)s : 1;
+}
+
+// Time of one step of E matrices in tiles of this size, roughly, in steps of 32 of the reduction of a tile of 256
+double step_time(int E, int n, int m, int tile) {
+    const int64_t nt = (n + tile - 1) / tile, mt = (m + tile - 1) / tile, half = nt * (nt + 1) / 2;
+    auto product = [&](int64_t tiles, int64_t steps) {
+        tiles *= E;
+        const int s = splits_of(tiles, (int)steps, tile), at_once = tile == 256 ? kUnits : 2 * kUnits;
+        const int64_t rounds = (tiles * s + at_once - 1) / at_once;
+        return (double)rounds * ((double)steps / s + 6) * (tile == 256 ? 1.0 : 0.7) + (s > 1 ? 4 : 0);
+    };
+    return product(half, (int64_t)mt * tile / 32) + product(half, (int64_t)nt * tile / 32) + product(nt * mt, (int64_t)nt * tile / 32);
+}
+
+Size size_of_matrix(int E, int rows, int cols) {
     Size z;
     const int n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    z.tile = n > 256 ? 256 : 128;
+    z.tile = n > 128 && step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
     z.n = (n + z.tile - 1) / z.tile * z.tile;
     z.m = (m + z.tile - 1) / z.tile * z.tile;
     z.x = (int64_t)z.n * z.m * 2;
     z.s = (int64_t)z.n * z.n * 2;
     const int64_t want = ((int64_t)rows * cols + 16383) / 16384;
-    z.parts = (int)(want < 256 ? want : 256);
+    z.parts = (int)(want < 512 ? want : 512);
     if (z.parts > rows) z.parts = rows;
     return z;
 }
 
-// X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums
+// X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares
 int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + 4096; }
+// Sums of the cut reductions of `count` matrices
+int64_t part_bytes(int count, const Size& z) {
+    const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
+    int64_t slots = 0;
+    auto product = [&](int64_t tiles, int64_t steps, int least) {
+        const int s = splits_of(tiles, (int)steps, z.tile), n = s > least ? s : least;
+        if (n > 1 && tiles * n > slots) slots = tiles * n;
+    };
+    product(half, z.m / 32, z.n == 128 ? 2 : 1);
+    product(half, z.n / 32, 1);
+    product(all, z.n / 32, 1);
+    return slots * z.tile * z.tile * 4;
+}
+// ... where there are any, at most
+constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 
-template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipError_t product(const OrthArgs& g, int tile, hipStream_t st) {
+template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
+    constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
+    const int64_t tiles = (int64_t)g.tiles * g.matrices;
+    if (g.splits == 0) g.splits = splits_of(tiles, g.steps / (tile == 256 ? KS : 1), tile);
     auto run = [&](auto kernel, int bytes, int threads) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        kernel<<<g.tiles * g.matrices, threads, bytes, st>>>(g);
+        kernel<<<tiles * g.splits, threads, bytes, st>>>(g);
         return hipGetLastError();
     };
-    constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
-    if (tile == 256) return run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
-    return run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    const hipError_t e = tile == 256 ? run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512)
+                                     : run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    if (e != hipSuccess || g.splits == 1 || !sums) return e;
+    if (tile == 256) orth_sums_kernel<16, CIN, PARTS, OUT><<<tiles * 64, 256, 0, st>>>(g);
+    else orth_sums_kernel<8, CIN, PARTS, OUT><<<tiles * 16, 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
-struct Buffers { OrthOperand x[2], s, q, t; };
+struct Buffers {
+    OrthOperand x[2], s, q, t;
+    float* part;
+};
 
 OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
     OrthOperand o = {};
@@ -433,6 +658,7 @@ template <bool F32> struct Steps {
         g.a = a, g.b = b, g.c = c;
         g.steps = a.blocks;
         g.alpha = alpha;
+        g.part = w.part;
         return g;
     }
     // X = (q + diagonal I) X, into the other buffer or to the caller
@@ -445,6 +671,7 @@ template <bool F32> struct Steps {
         g.steps = z.n / 32;
         g.alpha = 1.f / Q_SCALE;
         g.diagonal = diagonal * Q_SCALE;
+        g.part = w.part;
         hipError_t e;
         if (!last) {
             e = product<PARTS, 2, true, false, 2, ORTH_BLOCKS, DIAG>(g, z.tile, st);
@@ -497,6 +724,20 @@ template <bool F32> struct Steps {
         if (e == hipSuccess) e = apply<2, false>(w.s, 0.f, last);
         return e;
     }
+    // One or two steps of matrices of one tile: all between S and the last product in one launch
+    hipError_t chain(const float* abc, int n, bool last) {
+        OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
+        const int splits = splits_of(count, g.steps, z.tile);
+        g.splits = splits > 1 ? splits : 2;  // (sums in any case)
+        hipError_t e = product<2, 2, false, false, 2, ORTH_SQUARE, false>(g, z.tile, st, false);
+        if (e != hipSuccess) return e;
+        constexpr int bytes = 4 * 32 * ORTH_BLOCK;
+        e = hipFuncSetAttribute((const void*)orth_chain_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+        orth_chain_kernel<<<count, 512, bytes, st>>>(g, g.splits, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
+        e = hipGetLastError();
+        return e != hipSuccess ? e : apply<2, false>(w.q, 0.f, last);
+    }
     hipError_t run() {
         // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones (with one part of X in S
         // and P nine times their cost, for everything between has two parts then).  Where X is wide that is less work.
@@ -504,10 +745,10 @@ template <bool F32> struct Steps {
         const bool pairs = half * mt + nt * mt * nt > (F32 ? 3 : 9) * half * nt;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
+            const int n = (pairs || z.n == 128) && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
-            e = n == 2 ? two_steps(abc, k == t.steps) : one_step(abc, k == t.steps);
+            e = z.n == 128 ? chain(abc, n, k == t.steps) : n == 2 ? two_steps(abc, k == t.steps) : one_step(abc, k == t.steps);
         }
         return e;
     }
@@ -518,22 +759,29 @@ template <bool F32> struct Steps {
 // A few matrices at a time where the whole stack would take more than this
 constexpr int64_t ORTH_WORKSPACE = (int64_t)8 << 30;
 
+int at_once(int E, const Size& z) {
+    const int64_t n = (ORTH_WORKSPACE - kPartBytes) / matrix_bytes(z);
+    return n < 1 ? 1 : n < E ? (int)n : E;
+}
+
 size_t orth_workspace(int E, int rows, int cols) {
-    const int64_t one = matrix_bytes(size_of_matrix(rows, cols));
-    int64_t count = ORTH_WORKSPACE / one;
-    if (count > E) count = E;
-    return (size_t)((count > 1 ? count : 1) * one);
+    const Size z = size_of_matrix(E, rows, cols);
+    const int turn = at_once(E, z);
+    return (size_t)(turn * matrix_bytes(z) + (turn < E ? kPartBytes : part_bytes(E, z)));
 }
 
 hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
-    const Size z = size_of_matrix(t.rows, t.cols);
-    const int at_once = (int)(orth_workspace(t.E, t.rows, t.cols) / matrix_bytes(z));
+    const Size z = size_of_matrix(t.E, t.rows, t.cols);
+    const int turn = at_once(t.E, z);
+    const int64_t part = turn < t.E ? kPartBytes : part_bytes(t.E, z);
     const bool tall = t.rows > t.cols;
     const int size_in = t.in_f32 ? 4 : 2, size_out = t.out_f32 ? 4 : 2;
-    for (int e0 = 0; e0 < t.E; e0 += at_once) {
-        const int count = t.E - e0 < at_once ? t.E - e0 : at_once;
+    for (int e0 = 0; e0 < t.E; e0 += turn) {
+        const int count = t.E - e0 < turn ? t.E - e0 : turn;
         char* at = (char*)workspace;
         Buffers w;
+        w.part = (float*)at;
+        at += part;
         for (OrthOperand& x : w.x) x = operand(at, z.x, z.m / 32, count);
         for (OrthOperand* o : {&w.s, &w.q, &w.t}) *o = operand(at, z.s, z.n / 32, count);
         OrthIn in = {};
@@ -546,6 +794,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.parts = z.parts;
         in.eps = t.eps;
         in.tall = tall;
+        in.vec = ((uintptr_t)in.g & 15) == 0 && t.g_ld * size_in % 16 == 0 && (count == 1 || t.g_matrix * size_in % 16 == 0);
         in.x = w.x[0];
         const dim3 blocks((tall ? z.n : z.m) / 64, (tall ? z.m : z.n) / 64, count);
         if (t.in_f32) {

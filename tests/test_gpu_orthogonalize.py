@@ -6,8 +6,9 @@ product off by a random share, uniform to either side, of what its rounding may 
 product's 32-bit sums: 2^-22 of the product of the magnitudes), give a deviation D; |D| is the root of its mean square over a few draws (of small
 matrices more: one draw of a few numbers can come near zero).  The kernel's errors are of the same sizes or smaller.  In the smallest matrices they
 are 15 numbers at least (X, S and P of five steps), each at most 3^1/2 times its root mean square, so by Cauchy and Schwarz together at most 45^1/2 < 8 times
-that of their sum; in larger ones there are more of them and they come nearer to it.  So their norm is below 8 |D|; a single value of n m is within 6
-times its share of that (and never past the norm).
+that of their sum; in larger ones there are more of them and they come nearer to it.  So their norm is below 8 |D|; a single value is within 6
+times its share of that (and never past the norm).  Where a few directions u v^T carry the errors, as on steep spectra, the value in row i and column j of each is
+|u_i| |v_j|, so its share is that of row i times that of column j of the whole, not 1 / (n m)^1/2 of it.
 A bf16 result adds 2^-8 of the value, an fp32 one 2^-24."""
 import pytest
 import torch
@@ -35,10 +36,13 @@ def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
     X = (G.t() if tall else G).double()
     X = X / (X.square().sum().sqrt() + eps)
 
+    def random(shape):
+        return torch.rand(shape, generator=noise[2], dtype=F64, device=noise[2].device) * 2 - 1
+
     def off(t, share):
         if noise is None:
             return t
-        return t + (torch.rand(t.shape, generator=noise[2], dtype=F64) * 2 - 1) * share
+        return t + random(t.shape) * share
 
     def part(t, parts):
         return off(t, t.abs() * (2.0 ** -11 if parts == 1 else 2.0 ** -22))
@@ -57,18 +61,21 @@ def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
 
 
 def check(got, G, coefficients=(ABC,) * 5, scale=1.0, eps=1e-7):
+    """On G's device."""
     stack = G if G.dim() == 3 else G[None]
-    out = got.cpu() if G.dim() == 3 else got.cpu()[None]
+    out = (got if G.dim() == 3 else got[None]).to(G.device)
     parts = (2, 2) if out.dtype is F32 else (1, 1)
     half = torch.finfo(out.dtype).eps / 2
     for e in range(stack.shape[0]):
         ref = steps_of(stack[e], coefficients, scale, eps)
-        noise, draws = torch.Generator().manual_seed(e), 16 if min(ref.shape) <= 40 else 2
+        noise, draws = torch.Generator(device=G.device).manual_seed(e), 16 if min(ref.shape) <= 40 else 2
         D = [steps_of(stack[e], coefficients, scale, eps, (*parts, noise)) - ref for _ in range(draws)]
         err, norm = out[e].double() - ref, (sum(float(d.square().sum()) for d in D) / draws) ** 0.5
         assert float(err.norm()) <= 8 * norm + half * float(ref.norm()), (e, float(err.norm()), norm, float(ref.norm()))
-        one = min(1.0, 6 / ref.numel() ** 0.5) * 8 * norm
-        assert float((err.abs() - half * ref.abs()).max()) <= one * (1 + half), e
+        square = sum(d.square() for d in D) / draws
+        share = (square.sum(1, keepdim=True) * square.sum(0)).sqrt() / max(norm, 1e-300)
+        one = 8 * (6 * share.clamp(min=norm / ref.numel() ** 0.5)).clamp(max=norm)
+        assert float((err.abs() - half * ref.abs() - one * (1 + half)).max()) <= 0.0, e
 
 
 SIZES = [(1, 1, 1), (2, 1, 9), (1, 70, 1), (3, 8, 8), (2, 31, 65), (1, 64, 200), (2, 128, 256), (2, 129, 127), (3, 300, 40), (1, 17, 1000), (1, 257, 513), (2, 260, 520),
@@ -151,23 +158,36 @@ def test_far_scales():
 
 
 def test_a_stack_is_its_matrices():
+    """Each matrix alone and in the stack (whose reductions may be cut otherwise): both as near the exact one, and the same bits twice."""
     G = gradient((5, 260, 300), 9, BF16).cuda()
     got = moe.moe_orthogonalize(G)
+    check(got, G)
+    assert torch.equal(moe.moe_orthogonalize(G), got)
     for e in range(5):
-        assert torch.equal(moe.moe_orthogonalize(G[e]), got[e])
+        check(moe.moe_orthogonalize(G[e]), G[e])
+
+
+@pytest.mark.parametrize("E,rows,cols", [(1, 100, 5000), (1, 6000, 20), (3, 130, 9000), (1, 256, 14336), (1, 1000, 1100), (2, 2000, 640), (40, 16, 500), (130, 24, 40), (1, 2048, 4096),
+                                         (1, 1536, 1536), (7, 513, 770), (64, 600, 300)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_and_many_tiles(E, rows, cols, dtype):
+    """Cut reductions, both sizes of tiles, steps in pairs; compared on the GPU in 64 bits."""
+    G = gradient((E, rows, cols), E + rows, dtype, "steep").cuda()
+    check(moe.moe_orthogonalize(G)[:3], G[:3])
+    check(moe.moe_orthogonalize(G, steps=2)[-1], G[-1], (ABC,) * 2)
 
 
 def test_more_matrices_than_the_workspace_holds():
     """Stacks past the workspace's 8 GiB are gone through in turns."""
     lib = moe.load_library()
-    one, E = lib.moe_orthogonalize_workspace_bytes(1, 2048, 2048), 0
+    one = lib.moe_orthogonalize_workspace_bytes(8, 2048, 2048) // 8
     E = (8 << 30) // one + 2
     assert 16 < E <= 256 and lib.moe_orthogonalize_workspace_bytes(E, 2048, 2048) <= 8 << 30
     g = torch.Generator(device="cuda").manual_seed(1)
     G = torch.empty(E, 2048, 2048, dtype=BF16, device="cuda").normal_(generator=g)
     got = moe.moe_orthogonalize(G)
-    for e in (0, E - 3, E - 2, E - 1):
-        assert torch.equal(moe.moe_orthogonalize(G[e]), got[e]), e
+    for e in (0, E - 4, E - 3, E - 2, E - 1):
+        check(got[e], G[e])
 
 
 def test_streams_and_graphs():
