@@ -109,8 +109,8 @@ template <bool CIN, int PARTS, int OUT> static __device__ inline void finish(con
 
 // PA, PB: parts of A and B.  TB: B lies with the reduction along its rows (otherwise along its columns).  WM x WN wavefronts of FM x FN
 // fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN, PARTS, OUT: what finish makes of the sums.
-// DIAG: A is multiplied with `diagonal` added to its diagonal.
-template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool CIN, int PARTS, int OUT, bool DIAG>
+// DIAG: A is multiplied with `diagonal` added to its diagonal.  LOLO: the product of the second parts too.
+template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool CIN, int PARTS, int OUT, bool DIAG, bool LOLO>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
     static_assert(FA % WAVES == 0 && FB == 2 * WAVES, "a load's operand and block row do not depend on the wavefront");
@@ -194,13 +194,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
                 for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK + at_row);
         }
     };
-    constexpr int PAIRS = PA + PB - 1, ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
+    constexpr int PAIRS = PA + PB - 1 + (LOLO ? 1 : 0), ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
     auto multiply = [&](int s, auto&& beside) {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
         orth_repeat<ROWS>([&](auto row) {
             constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
-            constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : 0;  // hi hi, hi lo, lo hi
+            constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : pair - PB;  // hi hi, hi lo, lo hi, lo lo
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k][q][j], a[k][p][i], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -365,6 +365,7 @@ __global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int splits,
             each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[0][m], v[m][n], 0, 0, 0); });
             each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][n], a[0][m], v[m][n], 0, 0, 0); });
             each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[1][m], v[m][n], 0, 0, 0); });
+            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][n], a[1][m], v[m][n], 0, 0, 0); });
         }
         each([&](int m, int n, int, int) { v[m][n] *= scale; });
     };
@@ -607,7 +608,7 @@ int64_t part_bytes(int count, const Size& z) {
 // ... where there are any, at most
 constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 
-template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
+template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG, bool LOLO = false> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
     constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
     const int64_t tiles = (int64_t)g.tiles * g.matrices;
     if (g.splits == 0) g.splits = splits_of(tiles, g.steps / (tile == 256 ? KS : 1), tile);
@@ -617,8 +618,9 @@ template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG> hipE
         kernel<<<tiles * g.splits, threads, bytes, st>>>(g);
         return hipGetLastError();
     };
-    const hipError_t e = tile == 256 ? run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512)
-                                     : run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    hipError_t e;
+    if (!LOLO && tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG, false>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
+    else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG, LOLO>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
     if (e != hipSuccess || g.splits == 1 || !sums) return e;
     if (tile == 256) orth_sums_kernel<16, CIN, PARTS, OUT><<<tiles * 64, 256, 0, st>>>(g);
     else orth_sums_kernel<8, CIN, PARTS, OUT><<<tiles * 16, 256, 0, st>>>(g);
@@ -662,7 +664,7 @@ template <bool F32> struct Steps {
         return g;
     }
     // X = (q + diagonal I) X, into the other buffer or to the caller
-    template <int PARTS, bool DIAG> hipError_t apply(const OrthOperand& q, float diagonal, bool last) {
+    template <int PARTS, bool DIAG, bool LOLO = false> hipError_t apply(const OrthOperand& q, float diagonal, bool last) {
         OrthArgs g = {};
         g.matrices = count;
         g.mt = z.n / z.tile, g.nt = z.m / z.tile;
@@ -674,7 +676,7 @@ template <bool F32> struct Steps {
         g.part = w.part;
         hipError_t e;
         if (!last) {
-            e = product<PARTS, 2, true, false, 2, ORTH_BLOCKS, DIAG>(g, z.tile, st);
+            e = product<PARTS, 2, true, false, 2, ORTH_BLOCKS, DIAG, LOLO>(g, z.tile, st);
         } else {
             g.alpha *= t.scale / X_SCALE;
             g.out = out;
@@ -685,7 +687,7 @@ template <bool F32> struct Steps {
             g.cols = g.tall ? t.rows : t.cols;
             const int size = F32 ? 4 : 2;
             g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
-            e = product<PARTS, 2, true, false, 0, F32 ? ORTH_F32 : ORTH_BF16, DIAG>(g, z.tile, st);
+            e = product<PARTS, 2, true, false, 0, F32 ? ORTH_F32 : ORTH_BF16, DIAG, LOLO>(g, z.tile, st);
         }
         const OrthOperand o = w.x[0];
         w.x[0] = w.x[1];
@@ -729,23 +731,28 @@ template <bool F32> struct Steps {
         OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
         const int splits = splits_of(count, g.steps, z.tile);
         g.splits = splits > 1 ? splits : 2;  // (sums in any case)
-        hipError_t e = product<2, 2, false, false, 2, ORTH_SQUARE, false>(g, z.tile, st, false);
+        hipError_t e = product<2, 2, false, false, 2, ORTH_SQUARE, false, true>(g, z.tile, st, false);
         if (e != hipSuccess) return e;
         constexpr int bytes = 4 * 32 * ORTH_BLOCK;
         e = hipFuncSetAttribute((const void*)orth_chain_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         orth_chain_kernel<<<count, 512, bytes, st>>>(g, g.splits, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
         e = hipGetLastError();
-        return e != hipSuccess ? e : apply<2, false>(w.q, 0.f, last);
+        return e != hipSuccess ? e : apply<2, false, true>(w.q, 0.f, last);
     }
     hipError_t run() {
         // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones (with one part of X in S
         // and P nine times their cost, for everything between has two parts then).  Where X is wide that is less work.
         const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
         const bool pairs = half * mt + nt * mt * nt > (F32 ? 3 : 9) * half * nt;
+        // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second
+        // parts are multiplied with each other too (up to 128 rows), and steps taken one by one (up to 64 rows; 2 x 24 x 24: 1.6e-6 of the norm
+        // in pairs without, 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
+        const int small = t.rows < t.cols ? t.rows : t.cols;
+        const bool two = z.n == 128 ? !(F32 && small <= 64) : pairs;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = (pairs || z.n == 128) && k + 2 <= t.steps ? 2 : 1;
+            const int n = two && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
             e = z.n == 128 ? chain(abc, n, k == t.steps) : n == 2 ? two_steps(abc, k == t.steps) : one_step(abc, k == t.steps);
