@@ -25,10 +25,12 @@ struct OrthOperand {
 
 struct OrthArgs {
     OrthOperand a, b;
-    OrthOperand cin;       // beta times this is added
+    OrthOperand cin;       // beta times this is added, or (beta + rest of the row) times
+    float* rest;           // what one part leaves of a symmetric result's diagonal: [matrices][its rows]
     OrthOperand c;         // the result
     float alpha, beta;
-    float diagonal;        // added to the diagonal of a symmetric result; or, times b, to a product that is not (in the units of a)
+    float diagonal;        // added to the diagonal of a symmetric result
+    int square;            // rows of a symmetric operand
     int steps;             // blocks of the reduction
     int splits;            // ranges that it is cut into; with more than one, sums go to `part`
     float* part;           // [matrices][tiles][splits][fragments of a tile][64 lanes][4]
@@ -91,8 +93,8 @@ template <int STEP> static __device__ inline uint32_t lane_xor(uint32_t v) {
 }
 
 // 4 lanes have 4 fp16 values each (of row lane % 4, columns 0..3): afterwards each has column lane % 4 of the rows 0..3
-static __device__ inline void turn_f16(uint32_t& a, uint32_t& b) {
-    const int t = threadIdx.x & 3;
+static __device__ inline void turn_f16(uint32_t& a, uint32_t& b, int lane) {
+    const int t = lane & 3;
     // pairs of lanes: a = (c0, c1) and b = (c2, c3) of one row -> one column of two rows
     const uint32_t xa = lane_xor<1>(a), xb = lane_xor<1>(b);
     const uint32_t a1 = t & 1 ? (xa >> 16) | (a & 0xffff0000u) : (a & 0xffffu) | (xa << 16);
@@ -102,8 +104,8 @@ static __device__ inline void turn_f16(uint32_t& a, uint32_t& b) {
     a = t & 2 ? yb : a1;
     b = t & 2 ? b1 : ya;
 }
-static __device__ inline void turn_f32(f32x4_t& v) {
-    const int t = threadIdx.x & 3;
+static __device__ inline void turn_f32(f32x4_t& v, int lane) {
+    const int t = lane & 3;
     // even lanes keep column 0 (2), odd ones 1 (3): lane t has (own, neighbour's) of that column
     const float o0 = __uint_as_float(lane_xor<1>(__float_as_uint(v[0]))), o1 = __uint_as_float(lane_xor<1>(__float_as_uint(v[1])));
     const float o2 = __uint_as_float(lane_xor<1>(__float_as_uint(v[2]))), o3 = __uint_as_float(lane_xor<1>(__float_as_uint(v[3])));

@@ -43,74 +43,99 @@ template <bool SYM> static __device__ inline void place(const OrthArgs& g, int t
     *tn = __builtin_amdgcn_readfirstlane(n);
 }
 
-// A fragment's sums on their way out: a lane has the columns c + 4 q + 0..3 of row r + i (i = lane % 16, q = lane / 16).  CIN: beta times another
-// matrix (in two parts) is added.  OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any
-// result in blocks; or its type in the caller's rows.  PARTS: of a result in blocks.
-template <bool CIN, int PARTS, int OUT> static __device__ inline void finish(const OrthArgs& g, f32x4_t v, int lane, int matrix, int r, int c, bool both) {
+// The sums of two neighbouring fragments on their way out: a lane has the columns c + 4 q + 0..3 and c + 16 + 4 q + 0..3 of row r + i (i = lane % 16,
+// q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each of its rows (beta + what the diagonal of A has left) times.
+// OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any result in blocks; or its type in
+// the caller's rows.  PARTS: of a result in blocks.
+// In a block a lane's 4 values are half a piece, and lanes of neighbouring q change halves for accesses of 16 bytes.
+template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void finish(const OrthArgs& g, f32x4_t u, f32x4_t v, int lane, int matrix, int r, int c, bool both) {
     const int i = lane & 15, q = lane >> 4;
+    const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (q & 1) * 2 + (q >> 1)) * 16;
+    u *= g.alpha;
+    v *= g.alpha;
+    if constexpr (CIN > 0) {
+        const float beta = ROWS ? g.beta * (g.diagonal + g.rest[(int64_t)matrix * (g.square) + r + i]) : g.beta;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] *= g.alpha;
-    const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (c >> 3 & 2) + (q >> 1)) * 16 + (q & 1) * 8;
-    if constexpr (CIN) {
-        const u32x2_t hi = *(const u32x2_t*)(g.cin.part[0] + matrix * g.cin.matrix + here), lo = *(const u32x2_t*)(g.cin.part[1] + matrix * g.cin.matrix + here);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t h = hi[j >> 1], l = lo[j >> 1];
-            v[j] = fmaf(g.beta, j & 1 ? f16_hi(h) + f16_hi(l) : f16_lo(h) + f16_lo(l), v[j]);
+        for (int p = 0; p < CIN; ++p) {
+            const u32x4_t w = *(const u32x4_t*)(g.cin.part[p] + matrix * g.cin.matrix + here);
+            const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane16_swap(w[1], w[3], false, false);
+            u[0] = fmaf(beta, f16_lo(x[0]), u[0]), u[1] = fmaf(beta, f16_hi(x[0]), u[1]), u[2] = fmaf(beta, f16_lo(y[0]), u[2]), u[3] = fmaf(beta, f16_hi(y[0]), u[3]);
+            v[0] = fmaf(beta, f16_lo(x[1]), v[0]), v[1] = fmaf(beta, f16_hi(x[1]), v[1]), v[2] = fmaf(beta, f16_lo(y[1]), v[2]), v[3] = fmaf(beta, f16_hi(y[1]), v[3]);
         }
     }
     if constexpr (OUT == ORTH_SQUARE) {
-        if (r == c) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += 4 * q + j == i ? g.diagonal : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            if (r == c) u[j] += 4 * q + j == i ? g.diagonal : 0.f;
+            if (r == c + 16) v[j] += 4 * q + j == i ? g.diagonal : 0.f;
         }
     }
     if constexpr (OUT == ORTH_SQUARE || OUT == ORTH_BLOCKS) {
-        uint32_t w[2] = {pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+        uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+        if constexpr (OUT == ORTH_SQUARE && PARTS == 1) {
+            if (g.rest != nullptr && (r == c || r == c + 16)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = r == c ? u[j] : v[j];
+                    if (4 * q + j == i) g.rest[(int64_t)matrix * (g.square) + r + i] = (x - (float)(_Float16)x) * (1.f / Q_SCALE);
+                }
+            }
+        }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             if (p == 1) {
-                const uint32_t h0 = w[0], h1 = w[1];
-                w[0] = pack_f16(v[0] - f16_lo(h0), v[1] - f16_hi(h0));
-                w[1] = pack_f16(v[2] - f16_lo(h1), v[3] - f16_hi(h1));
+                const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
+                a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
+                a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
+                a[2] = pack_f16(v[0] - f16_lo(h[2]), v[1] - f16_hi(h[2]));
+                a[3] = pack_f16(v[2] - f16_lo(h[3]), v[3] - f16_hi(h[3]));
             }
             char* to = g.c.part[p] + matrix * g.c.matrix;
-            *(u32x2_t*)(to + here) = u32x2_t{w[0], w[1]};
+            const auto x = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
+            *(u32x4_t*)(to + here) = u32x4_t{x[0], y[0], x[1], y[1]};
             if (OUT == ORTH_SQUARE && both) {  // the same on the other side, 4 rows of a column a lane
                 const int64_t there = ((int64_t)(c >> 4) * g.c.blocks + (r >> 5)) * ORTH_BLOCK + orth_piece(4 * q + (i & 3), (r >> 3 & 2) + (i >> 3)) * 16 + (i >> 2 & 1) * 8;
-                uint32_t x = w[0], y = w[1];
-                turn_f16(x, y);
-                *(u32x2_t*)(to + there) = u32x2_t{x, y};
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    uint32_t s = a[2 * f], t = a[2 * f + 1];
+                    turn_f16(s, t, lane);
+                    *(u32x2_t*)(to + there + f * (int64_t)g.c.blocks * ORTH_BLOCK) = u32x2_t{s, t};
+                }
             }
         }
     } else {
-        if (g.tall) turn_f32(v);  // rows and columns change places: 4 of the caller's neighbouring values again
-        const int rr = g.tall ? c + 4 * q + (i & 3) : r + i, cc = g.tall ? r + (i & 12) : c + 4 * q;
-        const int rows = g.tall ? g.cols : g.rows, cols = g.tall ? g.rows : g.cols;
-        if (rr >= rows) return;
-        const int64_t to = matrix * g.out_matrix + rr * g.out_ld + cc;
-        if (g.vec && cc + 3 < cols) {
-            if constexpr (OUT == ORTH_F32) {
-                *(f32x4_t*)((float*)g.out + to) = v;
-            } else {
-                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-                *(bf16x4_t*)((uint16_t*)g.out + to) = bf16x4_t{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-            }
-        } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (cc + j >= cols) continue;
-                if constexpr (OUT == ORTH_F32) ((float*)g.out)[to + j] = v[j];
-                else ((__bf16*)g.out)[to + j] = (__bf16)v[j];
+        for (int f = 0; f < 2; ++f) {
+            f32x4_t x = f == 0 ? u : v;
+            const int cf = c + 16 * f;
+            if (g.tall) turn_f32(x, lane);  // rows and columns change places: 4 of the caller's neighbouring values again
+            const int rr = g.tall ? cf + 4 * q + (i & 3) : r + i, cc = g.tall ? r + (i & 12) : cf + 4 * q;
+            const int rows = g.tall ? g.cols : g.rows, cols = g.tall ? g.rows : g.cols;
+            if (rr >= rows) continue;
+            const int64_t to = matrix * g.out_matrix + rr * g.out_ld + cc;
+            if (g.vec && cc + 3 < cols) {
+                if constexpr (OUT == ORTH_F32) {
+                    *(f32x4_t*)((float*)g.out + to) = x;
+                } else {
+                    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+                    *(bf16x4_t*)((uint16_t*)g.out + to) = bf16x4_t{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (cc + j >= cols) continue;
+                    if constexpr (OUT == ORTH_F32) ((float*)g.out)[to + j] = x[j];
+                    else ((__bf16*)g.out)[to + j] = (__bf16)x[j];
+                }
             }
         }
     }
 }
 
 // PA, PB: parts of A and B.  TB: B lies with the reduction along its rows (otherwise along its columns).  WM x WN wavefronts of FM x FN
-// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN, PARTS, OUT: what finish makes of the sums.
-// DIAG: A is multiplied with `diagonal` added to its diagonal.  LOLO: the product of the second parts too.
-template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool CIN, int PARTS, int OUT, bool DIAG, bool LOLO>
+// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  LOLO: the product of the second parts too.  CIN, ROWS,
+// PARTS, OUT: what finish makes of the sums.
+template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool LOLO, int CIN, bool ROWS, int PARTS, int OUT>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
     static_assert(FA % WAVES == 0 && FB == 2 * WAVES, "a load's operand and block row do not depend on the wavefront");
@@ -194,11 +219,11 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
                 for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK + at_row);
         }
     };
-    constexpr int PAIRS = PA + PB - 1 + (LOLO ? 1 : 0), ROWS = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
-    auto multiply = [&](int s, auto&& beside) {
+    constexpr int PAIRS = PA + PB - 1 + (LOLO ? 1 : 0), LINES = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
+    auto multiply = [&](auto&& beside) {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
-        orth_repeat<ROWS>([&](auto row) {
+        orth_repeat<LINES>([&](auto row) {
             constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
             constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : pair - PB;  // hi hi, hi lo, lo hi, lo lo
 #pragma unroll
@@ -206,36 +231,6 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             __builtin_amdgcn_sched_barrier(0);
             beside(row);
         });
-        if constexpr (DIAG) {
-            // 32 of the reduction that are 32 of the wavefront's rows: the diagonal number, in two parts, times them
-            static_assert(KS == 1 && PB == 2 && FM % 2 == 0, "");
-            const int from = 2 * s - (tm * FA + wm * FM);
-            if (from >= 0 && from < FM) {
-                const _Float16 hi = (_Float16)g.diagonal, lo = (_Float16)(g.diagonal - (float)hi);
-                f16x8_t e[2][2];  // [of the first, the second 16 rows][part]
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool on = 8 * q16 + j == 16 * h + i16;
-                        e[h][0][j] = on ? hi : (_Float16)0.f;
-                        e[h][1][j] = on ? lo : (_Float16)0.f;
-                    }
-                orth_repeat<FM / 2>([&](auto pair) {
-                    constexpr int i = 2 * decltype(pair)::value;
-                    if (from == i) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int j = 0; j < FN; ++j) {
-                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][0][j], e[h][0], acc[i + h][j], 0, 0, 0);
-                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][1][j], e[h][0], acc[i + h][j], 0, 0, 0);
-                                acc[i + h][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][0][j], e[h][1], acc[i + h][j], 0, 0, 0);
-                            }
-                    }
-                });
-            }
-        }
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -249,33 +244,30 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         issue(first, first & 1);
         orth_wait<0>();
         orth_barrier();
-        if (wave < 4) {
-            for (int s = first; s < end; ++s) {
-                read(s & 1);
-                if (s + 1 < end) issue(s + 1, (s + 1) & 1);
-                orth_barrier();
-                multiply(s, [](auto) {});
-                orth_wait<0>();
-                orth_barrier();
-            }
-            orth_barrier();
-        } else {
+        const bool ahead = wave < 4;
+        if (!ahead) {
             if (first + 1 < end) issue(first + 1, (first + 1) & 1);
             orth_barrier();
-            for (int s = first; s < end; ++s) {
-                read(s & 1);
-                orth_wait<0>();
-                orth_barrier();
-                const bool more = s + 2 < end;
-                multiply(s, [&](auto row) {  // its loads among the products
-                    constexpr int r = decltype(row)::value;
-                    if constexpr (r * LOADS % ROWS < LOADS && r * LOADS / ROWS < LOADS) {
-                        if (more) issue_one(OrthInt<r * LOADS / ROWS>{}, s + 2, s & 1);
-                    }
-                });
-                orth_barrier();
-            }
         }
+        for (int s = first; s < end; ++s) {  // one loop for both groups: two copies of it cost registers
+            read(s & 1);
+            if (ahead) {
+                if (s + 1 < end) issue(s + 1, (s + 1) & 1);
+            } else {
+                orth_wait<0>();
+            }
+            orth_barrier();
+            const bool more = !ahead && s + 2 < end;
+            multiply([&](auto row) {  // the second group's loads among its products
+                constexpr int r = decltype(row)::value;
+                if constexpr (r * LOADS % LINES < LOADS && r * LOADS / LINES < LOADS) {
+                    if (more) issue_one(OrthInt<r * LOADS / LINES>{}, s + 2, s & 1);
+                }
+            });
+            if (ahead) orth_wait<0>();
+            orth_barrier();
+        }
+        if (ahead) orth_barrier();
     } else {
         orth_repeat<STAGES - 1>([&](auto s) {
             if (first + decltype(s)::value < end) issue(first + decltype(s)::value, decltype(s)::value);
@@ -288,7 +280,7 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
             orth_barrier();  // of every wavefront's; and all are done with the stage before
             if (s + STAGES - 1 < end) issue(s + STAGES - 1, place == 0 ? STAGES - 1 : place - 1);
             read(place);
-            multiply(s, [](auto) {});
+            multiply([](auto) {});
             place = place == STAGES - 1 ? 0 : place + 1;
         }
     }
@@ -306,23 +298,26 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     const int row0 = (tm * FA + wm * FM) * 16, col0 = (tn * FB + wn * FN) * 16;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
-        if (CIN) __builtin_amdgcn_sched_barrier(0);
+        if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < FN; ++n) finish<CIN, PARTS, OUT>(g, acc[m][n], out_lane, matrix, row0 + m * 16, col0 + n * 16, tm != tn);
+        for (int n = 0; n < FN; n += 2) finish<CIN, ROWS, PARTS, OUT>(g, acc[m][n], acc[m][n + 1], out_lane, matrix, row0 + m * 16, col0 + n * 16, tm != tn);
     }
 }
 
-// The ranges' sums added in their order, a wavefront a fragment; F x F fragments a tile
-template <int F, bool CIN, int PARTS, int OUT> __global__ __launch_bounds__(256) void orth_sums_kernel(OrthArgs g) {
-    const int64_t fragment = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = fragment / (F * F);
-    const int f = (int)(fragment - item * (F * F)), matrix = (int)(item / g.tiles), lane = threadIdx.x & 63;
+// The ranges' sums added in their order, a wavefront two fragments; F x F fragments a tile
+template <int F, int CIN, bool ROWS, int PARTS, int OUT> __global__ __launch_bounds__(256) void orth_sums_kernel(OrthArgs g) {
+    const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = pair / (F * F / 2);
+    const int f = (int)(pair - item * (F * F / 2)) * 2, matrix = (int)(item / g.tiles), lane = threadIdx.x & 63;
     int tm, tn;
     place<OUT == ORTH_SQUARE>(g, (int)(item - (int64_t)matrix * g.tiles), &tm, &tn);
     const f32x4_t* part = (const f32x4_t*)g.part + (item * g.splits * (F * F) + f) * 64 + lane;
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) v += part[(int64_t)s * (F * F * 64)];
-    finish<CIN, PARTS, OUT>(g, v, lane, matrix, (tm * F + f / F) * 16, (tn * F + f % F) * 16, tm != tn);
+    f32x4_t u = {0.f, 0.f, 0.f, 0.f}, v = u;
+#pragma unroll 4
+    for (int s = 0; s < g.splits; ++s) {
+        u += part[(int64_t)s * (F * F * 64)];
+        v += part[(int64_t)s * (F * F * 64) + 64];
+    }
+    finish<CIN, ROWS, PARTS, OUT>(g, u, v, lane, matrix, (tm * F + f / F) * 16, (tn * F + f % F) * 16, tm != tn);
 }
 
 // ---- the small products of matrices of one tile of 128, S in ranges -> a I + b S + c S S, or of two steps the product of both ----
@@ -556,12 +551,12 @@ struct Size {
 
 constexpr int kUnits = 256;  // compute units
 
-// Ranges a reduction of `stages` is cut into where `tiles` tiles leave compute units without one (two small tiles share a unit): four stages
-// a range at least.
-int splits_of(int64_t tiles, int stages, int tile) {
-    const int64_t room = (tile == 256 ? kUnits : 2 * kUnits) / tiles, most = stages / 4;
+// Ranges a reduction of `steps` blocks is cut into where `tiles` tiles leave compute units without one (two small tiles share a unit): four blocks
+// a range at least, and ten blocks' time saved at least, about what a second launch and the sums' way to memory and back cost.
+int splits_of(int64_t tiles, int steps, int tile) {
+    const int64_t room = (tile == 256 ? kUnits : 2 * kUnits) / tiles, most = steps / 4;
     const int64_t s = room < most ? room : most;
-    return s > 1 ? (int)s : 1;
+    return s > 1 && steps - steps / s >= 10 ? (int)s : 1;
 }
 
 // Time of one step of E matrices in tiles of this size, roughly, in steps of 32 of the reduction of a tile of 256
@@ -571,7 +566,7 @@ double step_time(int E, int n, int m, int tile) {
         tiles *= E;
         const int s = splits_of(tiles, (int)steps, tile), at_once = tile == 256 ? kUnits : 2 * kUnits;
         const int64_t rounds = (tiles * s + at_once - 1) / at_once;
-        return (double)rounds * ((double)steps / s + 6) * (tile == 256 ? 1.0 : 0.7) + (s > 1 ? 4 : 0);
+        return (double)rounds * ((double)steps / s + 8) * (tile == 256 ? 1.0 : 0.7) + (s > 1 ? 8 : 0);
     };
     return product(half, (int64_t)mt * tile / 32) + product(half, (int64_t)nt * tile / 32) + product(nt * mt, (int64_t)nt * tile / 32);
 }
@@ -591,7 +586,7 @@ Size size_of_matrix(int E, int rows, int cols) {
 }
 
 // X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares
-int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + 4096; }
+int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096; }
 // Sums of the cut reductions of `count` matrices
 int64_t part_bytes(int count, const Size& z) {
     const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
@@ -608,10 +603,10 @@ int64_t part_bytes(int count, const Size& z) {
 // ... where there are any, at most
 constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 
-template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG, bool LOLO = false> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
-    constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : PLANES == 3 ? 3 : 2;
+template <int PA, int PB, bool TB, bool LOLO, int CIN, bool ROWS, int PARTS, int OUT> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
+    constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : 2;
     const int64_t tiles = (int64_t)g.tiles * g.matrices;
-    if (g.splits == 0) g.splits = splits_of(tiles, g.steps / (tile == 256 ? KS : 1), tile);
+    if (g.splits == 0) g.splits = splits_of(tiles, g.steps, tile);
     auto run = [&](auto kernel, int bytes, int threads) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
@@ -619,17 +614,17 @@ template <int PA, int PB, bool TB, bool CIN, int PARTS, int OUT, bool DIAG, bool
         return hipGetLastError();
     };
     hipError_t e;
-    if (!LOLO && tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, PARTS, OUT, DIAG, false>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
-    else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, PARTS, OUT, DIAG, LOLO>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    if (!LOLO && tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, false, CIN, ROWS, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
+    else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, LOLO, CIN, ROWS, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
     if (e != hipSuccess || g.splits == 1 || !sums) return e;
-    if (tile == 256) orth_sums_kernel<16, CIN, PARTS, OUT><<<tiles * 64, 256, 0, st>>>(g);
-    else orth_sums_kernel<8, CIN, PARTS, OUT><<<tiles * 16, 256, 0, st>>>(g);
+    if (tile == 256) orth_sums_kernel<16, CIN, ROWS, PARTS, OUT><<<tiles * 32, 256, 0, st>>>(g);
+    else orth_sums_kernel<8, CIN, ROWS, PARTS, OUT><<<tiles * 8, 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
 struct Buffers {
     OrthOperand x[2], s, q, t;
-    float* part;
+    float *part, *rest;
 };
 
 OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
@@ -661,24 +656,30 @@ template <bool F32> struct Steps {
         g.steps = a.blocks;
         g.alpha = alpha;
         g.part = w.part;
+        g.square = z.n;
         return g;
     }
-    // X = (q + diagonal I) X, into the other buffer or to the caller
-    template <int PARTS, bool DIAG, bool LOLO = false> hipError_t apply(const OrthOperand& q, float diagonal, bool last) {
+    // X = q X, into the other buffer or to the caller; where q has one part, X = (a + rest) X + q X of X's first part
+    template <bool TWO, bool LOLO = false> hipError_t apply(const OrthOperand& q, float a, bool last) {
+        constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 2;
         OrthArgs g = {};
         g.matrices = count;
         g.mt = z.n / z.tile, g.nt = z.m / z.tile;
         g.tiles = g.mt * g.nt;
-        g.a = q, g.b = w.x[0], g.c = w.x[1];
+        g.square = z.n;
+        g.a = q, g.b = w.x[0], g.c = w.x[1], g.cin = w.x[0];
+        g.rest = w.rest;
         g.steps = z.n / 32;
         g.alpha = 1.f / Q_SCALE;
-        g.diagonal = diagonal * Q_SCALE;
+        g.beta = 1.f;
+        g.diagonal = a;
         g.part = w.part;
         hipError_t e;
         if (!last) {
-            e = product<PARTS, 2, true, false, 2, ORTH_BLOCKS, DIAG, LOLO>(g, z.tile, st);
+            e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 2, ORTH_BLOCKS>(g, z.tile, st);
         } else {
             g.alpha *= t.scale / X_SCALE;
+            g.beta *= t.scale / X_SCALE;
             g.out = out;
             g.out_matrix = t.out_matrix;
             g.out_ld = t.out_ld;
@@ -687,7 +688,7 @@ template <bool F32> struct Steps {
             g.cols = g.tall ? t.rows : t.cols;
             const int size = F32 ? 4 : 2;
             g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
-            e = product<PARTS, 2, true, false, 0, F32 ? ORTH_F32 : ORTH_BF16, DIAG, LOLO>(g, z.tile, st);
+            e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 0, F32 ? ORTH_F32 : ORTH_BF16>(g, z.tile, st);
         }
         const OrthOperand o = w.x[0];
         w.x[0] = w.x[1];
@@ -696,34 +697,37 @@ template <bool F32> struct Steps {
     }
     // S = X X^T
     hipError_t gram() const {
-        return product<F32 ? 2 : 1, F32 ? 2 : 1, false, false, 2, ORTH_SQUARE, false>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
+        constexpr int PARTS = F32 ? 2 : 1;
+        return product<PARTS, PARTS, false, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
     }
-    // to = a I + b S + c S S; in one part without a I, for which it has too few digits
-    template <int PARTS> hipError_t polynomial(const OrthOperand& to, const float* abc) const {
+    // to = a I + b S + c S S; in one part without a I, for which it has too few digits, and with what it has too few for on its diagonal aside
+    hipError_t polynomial(const OrthOperand& to, const float* abc) const {
+        constexpr int PARTS = F32 ? 2 : 1;
         OrthArgs g = square(w.s, w.s, to, abc[2] * Q_SCALE / (S_SCALE * S_SCALE));
         g.cin = w.s;
         g.beta = abc[1] * Q_SCALE / S_SCALE;
-        g.diagonal = PARTS == 2 ? abc[0] * Q_SCALE : 0.f;
-        return product<2, 2, false, true, PARTS, ORTH_SQUARE, false>(g, z.tile, st);
+        g.diagonal = F32 ? abc[0] * Q_SCALE : 0.f;
+        g.rest = F32 ? nullptr : w.rest;
+        return product<PARTS, PARTS, false, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
     // to = a q, of matrices that commute
     hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to) const {
-        return product<2, 2, false, false, 2, ORTH_SQUARE, false>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
+        return product<2, 2, false, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
     }
     hipError_t one_step(const float* abc, bool last) {
         hipError_t e = gram();
-        if (e == hipSuccess) e = polynomial<F32 ? 2 : 1>(w.q, abc);
-        if (e == hipSuccess) e = apply<F32 ? 2 : 1, !F32>(w.q, abc[0], last);
+        if (e == hipSuccess) e = polynomial(w.q, abc);
+        if (e == hipSuccess) e = apply<F32>(w.q, abc[0], last);
         return e;
     }
     hipError_t two_steps(const float* abc, bool last) {
         hipError_t e = gram();
-        if (e == hipSuccess) e = polynomial<2>(w.q, abc);
+        if (e == hipSuccess) e = polynomial(w.q, abc);
         if (e == hipSuccess) e = times(w.s, w.q, w.t);
         if (e == hipSuccess) e = times(w.t, w.q, w.s);  // Q S Q = (Q X) (Q X)^T
-        if (e == hipSuccess) e = polynomial<2>(w.t, abc + 3);
+        if (e == hipSuccess) e = polynomial(w.t, abc + 3);
         if (e == hipSuccess) e = times(w.t, w.q, w.s);
-        if (e == hipSuccess) e = apply<2, false>(w.s, 0.f, last);
+        if (e == hipSuccess) e = apply<true>(w.s, 0.f, last);
         return e;
     }
     // One or two steps of matrices of one tile: all between S and the last product in one launch
@@ -731,20 +735,20 @@ template <bool F32> struct Steps {
         OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
         const int splits = splits_of(count, g.steps, z.tile);
         g.splits = splits > 1 ? splits : 2;  // (sums in any case)
-        hipError_t e = product<2, 2, false, false, 2, ORTH_SQUARE, false, true>(g, z.tile, st, false);
+        hipError_t e = product<2, 2, false, true, 0, false, 2, ORTH_SQUARE>(g, z.tile, st, false);
         if (e != hipSuccess) return e;
         constexpr int bytes = 4 * 32 * ORTH_BLOCK;
         e = hipFuncSetAttribute((const void*)orth_chain_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         orth_chain_kernel<<<count, 512, bytes, st>>>(g, g.splits, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
         e = hipGetLastError();
-        return e != hipSuccess ? e : apply<2, false, true>(w.q, 0.f, last);
+        return e != hipSuccess ? e : apply<true, true>(w.q, 0.f, last);
     }
     hipError_t run() {
-        // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones (with one part of X in S
-        // and P nine times their cost, for everything between has two parts then).  Where X is wide that is less work.
+        // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones: less work where X is
+        // wide.  (With operands in one part the small ones would need two and cost more than that gains.)
         const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
-        const bool pairs = half * mt + nt * mt * nt > (F32 ? 3 : 9) * half * nt;
+        const bool pairs = F32 && half * mt + nt * mt * nt > 3 * half * nt;
         // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second
         // parts are multiplied with each other too (up to 128 rows), and steps taken one by one (up to 64 rows; 2 x 24 x 24: 1.6e-6 of the norm
         // in pairs without, 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
@@ -755,7 +759,10 @@ template <bool F32> struct Steps {
             const int n = two && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
-            e = z.n == 128 ? chain(abc, n, k == t.steps) : n == 2 ? two_steps(abc, k == t.steps) : one_step(abc, k == t.steps);
+            const bool last = k == t.steps;
+            if (z.n == 128) e = chain(abc, n, last);
+            else if constexpr (F32) e = n == 2 ? two_steps(abc, last) : one_step(abc, last);
+            else e = one_step(abc, last);
         }
         return e;
     }
@@ -797,7 +804,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.ld = t.g_ld;
         in.rows = t.rows;
         in.cols = t.cols;
-        in.partials = (double*)at;
+        w.rest = (float*)at;
+        in.partials = (double*)(at + (int64_t)z.n * 4 * count);
         in.parts = z.parts;
         in.eps = t.eps;
         in.tall = tall;

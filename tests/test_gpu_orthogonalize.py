@@ -31,13 +31,13 @@ def gradient(shape, seed, dtype, kind="gauss", std=1e-3):
 
 
 def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
-    """64 bits; noise: (parts of X in S, of P, generator) for the deviated run."""
+    """64 bits; noise: (parts of S, P and of X where they are formed and multiplied, generator) for the deviated run."""
     tall = G.shape[0] > G.shape[1]
     X = (G.t() if tall else G).double()
     X = X / (X.square().sum().sqrt() + eps)
 
     def random(shape):
-        return torch.rand(shape, generator=noise[2], dtype=F64, device=noise[2].device) * 2 - 1
+        return torch.rand(shape, generator=noise[1], dtype=F64, device=noise[1].device) * 2 - 1
 
     def off(t, share):
         if noise is None:
@@ -50,13 +50,13 @@ def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
     def product(A, B):
         return off(A @ B, 2.0 ** -22 * (A.abs() @ B.abs())) if noise else A @ B
 
-    px, pp = noise[:2] if noise else (2, 2)
+    parts = noise[0] if noise else 2
     for a, b, c in coefficients:
         X = part(X, 2)
-        Y = part(X, px)
-        S = part(product(Y, Y.t()), 2)
-        P = part(b * S + c * product(S, S), pp)
-        X = a * X + product(P, X)
+        Y = part(X, parts)
+        S = part(product(Y, Y.t()), parts)
+        P = part(b * S + c * product(S, S), parts)
+        X = a * X + product(P, Y)
     return scale * (X.t() if tall else X)
 
 
@@ -64,12 +64,12 @@ def check(got, G, coefficients=(ABC,) * 5, scale=1.0, eps=1e-7):
     """On G's device."""
     stack = G if G.dim() == 3 else G[None]
     out = (got if G.dim() == 3 else got[None]).to(G.device)
-    parts = (2, 2) if out.dtype is F32 else (1, 1)
+    parts = 2 if out.dtype is F32 else 1
     half = torch.finfo(out.dtype).eps / 2
     for e in range(stack.shape[0]):
         ref = steps_of(stack[e], coefficients, scale, eps)
         noise, draws = torch.Generator(device=G.device).manual_seed(e), 16 if min(ref.shape) <= 40 else 2
-        D = [steps_of(stack[e], coefficients, scale, eps, (*parts, noise)) - ref for _ in range(draws)]
+        D = [steps_of(stack[e], coefficients, scale, eps, (parts, noise)) - ref for _ in range(draws)]
         err, norm = out[e].double() - ref, (sum(float(d.square().sum()) for d in D) / draws) ** 0.5
         assert float(err.norm()) <= 8 * norm + half * float(ref.norm()), (e, float(err.norm()), norm, float(ref.norm()))
         square = sum(d.square() for d in D) / draws
