@@ -32,8 +32,9 @@ struct OrthArgs {
     float diagonal;        // added to the diagonal of a symmetric result
     int square;            // rows of a symmetric operand
     int steps;             // blocks of the reduction
-    int splits;            // ranges that it is cut into; with more than one, sums go to `part`
-    float* part;           // [matrices][tiles][splits][fragments of a tile][64 lanes][4]
+    int whole;             // of all matrices' tiles the first `whole` take their reduction whole; the others' is cut into `splits` ranges, whose
+    int splits;            // sums go to `part`: [those tiles][splits][fragments of a tile][64 lanes][4]
+    float* part;
     int mt, nt;            // tiles of a matrix (symmetric: mt == nt, those on and above the diagonal)
     int tiles, matrices;   // tiles of a matrix that are computed
     // the last product: results in the caller's rows

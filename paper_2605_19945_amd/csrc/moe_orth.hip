@@ -145,11 +145,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     const int wm = wave / WN, wn = wave % WN, i16 = lane & 15, q16 = lane >> 4;
 
     // neighbouring tiles on one XCD (workgroup number % 8): one stretch of the list each
-    const int total = g.tiles * g.matrices * g.splits, xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
-    int item = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
+    const bool cut = (int)blockIdx.x >= g.whole;
+    const int number = blockIdx.x - (cut ? g.whole : 0), total = cut ? (g.tiles * g.matrices - g.whole) * g.splits : g.whole;
+    const int xcd = number & 7, each = total >> 3, rest = total & 7;
+    int item = xcd * each + min(xcd, rest) + (number >> 3);
     const int64_t slot = item;
-    const int split = item % g.splits;
-    item /= g.splits;
+    const int splits = cut ? g.splits : 1, split = item % splits;
+    item = cut ? g.whole + item / splits : item;
     const int matrix = item / g.tiles;
     int tm, tn;
     place<SYM>(g, item - matrix * g.tiles, &tm, &tn);
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     f16x8_t a[KS][PA][FM], b[KS][PB][FN];
-    const int stages = g.steps / KS, first = (int)((int64_t)stages * split / g.splits), end = (int)((int64_t)stages * (split + 1) / g.splits);
+    const int stages = g.steps / KS, first = (int)((int64_t)stages * split / splits), end = (int)((int64_t)stages * (split + 1) / splits);
     const int at_row = orth_piece(i16, q16) * 16;
     // of the transposing read: lane i of 16 asks for 4 columns of row 8 (q % 2) + i / 4 and is given column i of 4 rows; the next 4 rows lie where
     // the exclusive or with 12 of the rows puts them
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
 
     int out_lane = lane;
     asm volatile("" : "+v"(out_lane));  // the compiler would form the results' places before the loop and spill them
-    if (g.splits > 1) {
+    if (cut) {
         f32x4_t* part = (f32x4_t*)g.part + slot * (FA * FB * 64) + out_lane;
 #pragma unroll
         for (int m = 0; m < FM; ++m)
@@ -307,9 +309,9 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
 // The ranges' sums added in their order, a wavefront two fragments; F x F fragments a tile
 template <int F, int CIN, bool ROWS, int PARTS, int OUT> __global__ __launch_bounds__(256) void orth_sums_kernel(OrthArgs g) {
     const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = pair / (F * F / 2);
-    const int f = (int)(pair - item * (F * F / 2)) * 2, matrix = (int)(item / g.tiles), lane = threadIdx.x & 63;
+    const int f = (int)(pair - item * (F * F / 2)) * 2, tile = g.whole + (int)item, matrix = tile / g.tiles, lane = threadIdx.x & 63;
     int tm, tn;
-    place<OUT == ORTH_SQUARE>(g, (int)(item - (int64_t)matrix * g.tiles), &tm, &tn);
+    place<OUT == ORTH_SQUARE>(g, tile - matrix * g.tiles, &tm, &tn);
     const f32x4_t* part = (const f32x4_t*)g.part + (item * g.splits * (F * F) + f) * 64 + lane;
     f32x4_t u = {0.f, 0.f, 0.f, 0.f}, v = u;
 #pragma unroll 4
@@ -336,13 +338,13 @@ __global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int splits,
             for (int n = 0; n < FN; ++n) f(m, n, wm * FM + m, wn * FN + n);
     };
     // where a lane's 4 values of a fragment lie: columns 16 fn + 4 (lane / 16) + 0..3 of row 16 fm + lane % 16
-    auto at = [&](int fm, int fn) { return (fm * 4 + (fn >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (fn & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
-    auto put = [&](char* to, int64_t plane) {
+    auto at = [&](int fm, int fn, int blocks = 4) { return (fm * blocks + (fn >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (fn & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
+    auto put = [&](char* to, int64_t plane, int blocks = 4) {
         each([&](int m, int n, int fm, int fn) {
             const f32x4_t& x = v[m][n];
             const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
-            *(u32x2_t*)(to + at(fm, fn)) = u32x2_t{h0, h1};
-            *(u32x2_t*)(to + plane + at(fm, fn)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+            *(u32x2_t*)(to + at(fm, fn, blocks)) = u32x2_t{h0, h1};
+            *(u32x2_t*)(to + plane + at(fm, fn, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
         });
     };
     auto multiply = [&](const char* x, const char* y, float scale) {  // v = scale x y, y symmetric
@@ -398,7 +400,7 @@ __global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int splits,
         __syncthreads();
         multiply(s, q, 1.f / Q_SCALE);
     }
-    put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0]);
+    put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
 }
 
 // ---- the way in ----
@@ -546,17 +548,24 @@ struct Size {
     int n, m;        // of X, padded
     int tile;        // 256 or 128
     int parts;       // of the squares
+    // Blocks along the rows of X and of S: an odd number, so that the block rows that are loaded together begin in different places of the memory
+    // channels' interleaving (a power of two put them all on the same few).
+    int xb, sb;
     int64_t x, s;    // bytes of a plane of X and of S
 };
 
 constexpr int kUnits = 256;  // compute units
 
-// Ranges a reduction of `steps` blocks is cut into where `tiles` tiles leave compute units without one (two small tiles share a unit): four blocks
-// a range at least, and ten blocks' time saved at least, about what a second launch and the sums' way to memory and back cost.
-int splits_of(int64_t tiles, int steps, int tile) {
-    const int64_t room = (tile == 256 ? kUnits : 2 * kUnits) / tiles, most = steps / 4;
-    const int64_t s = room < most ? room : most;
-    return s > 1 && steps - steps / s >= 10 ? (int)s : 1;
+// How the tiles of a launch take their reductions of `steps` blocks: whole ones in full rounds of the compute units (two small tiles share a unit),
+// those of the last round, or of the only one, in ranges for the units that would have none: four blocks a range at least, and ten blocks'
+// time saved at least, about what a second launch and the sums' way to memory and back cost.
+struct Cut { int whole, splits; };
+Cut cut_of(int64_t tiles, int steps, int tile) {
+    const int units = tile == 256 ? kUnits : 2 * kUnits;
+    const int rest = (int)(tiles % units), most = steps / 4;
+    const int room = rest > 0 ? units / rest : 1, s = room < most ? room : most;
+    if (s > 1 && steps - steps / s >= 10) return {(int)(tiles - rest), s};
+    return {(int)tiles, 1};
 }
 
 // Time of one step of E matrices in tiles of this size, roughly, in steps of 32 of the reduction of a tile of 256
@@ -564,9 +573,9 @@ double step_time(int E, int n, int m, int tile) {
     const int64_t nt = (n + tile - 1) / tile, mt = (m + tile - 1) / tile, half = nt * (nt + 1) / 2;
     auto product = [&](int64_t tiles, int64_t steps) {
         tiles *= E;
-        const int s = splits_of(tiles, (int)steps, tile), at_once = tile == 256 ? kUnits : 2 * kUnits;
-        const int64_t rounds = (tiles * s + at_once - 1) / at_once;
-        return (double)rounds * ((double)steps / s + 8) * (tile == 256 ? 1.0 : 0.7) + (s > 1 ? 8 : 0);
+        const Cut c = cut_of(tiles, (int)steps, tile);
+        const int64_t units = tile == 256 ? kUnits : 2 * kUnits, rounds = (c.whole + units - 1) / units;
+        return ((double)rounds * (steps + 8) + (c.splits > 1 ? (double)steps / c.splits + 16 : 0)) * (tile == 256 ? 1.0 : 0.7);
     };
     return product(half, (int64_t)mt * tile / 32) + product(half, (int64_t)nt * tile / 32) + product(nt * mt, (int64_t)nt * tile / 32);
 }
@@ -577,8 +586,9 @@ Size size_of_matrix(int E, int rows, int cols) {
     z.tile = n > 128 && step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
     z.n = (n + z.tile - 1) / z.tile * z.tile;
     z.m = (m + z.tile - 1) / z.tile * z.tile;
-    z.x = (int64_t)z.n * z.m * 2;
-    z.s = (int64_t)z.n * z.n * 2;
+    z.xb = z.m / 32 + 1, z.sb = z.n / 32 + 1;
+    z.x = (int64_t)z.n / 16 * z.xb * ORTH_BLOCK;
+    z.s = (int64_t)z.n / 16 * z.sb * ORTH_BLOCK;
     const int64_t want = ((int64_t)rows * cols + 16383) / 16384;
     z.parts = (int)(want < 512 ? want : 512);
     if (z.parts > rows) z.parts = rows;
@@ -587,17 +597,23 @@ Size size_of_matrix(int E, int rows, int cols) {
 
 // X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares
 int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096; }
+// The same for S of matrices of one tile, whose sums go on in one launch in any case
+int chain_splits(int count, int steps) {
+    const int room = 2 * kUnits / count, s = room < steps / 4 ? room : steps / 4;
+    return s > 1 ? s : 1;
+}
 // Sums of the cut reductions of `count` matrices
 int64_t part_bytes(int count, const Size& z) {
     const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
     int64_t slots = 0;
-    auto product = [&](int64_t tiles, int64_t steps, int least) {
-        const int s = splits_of(tiles, (int)steps, z.tile), n = s > least ? s : least;
-        if (n > 1 && tiles * n > slots) slots = tiles * n;
+    auto product = [&](int64_t tiles, int64_t steps) {
+        const Cut c = cut_of(tiles, (int)steps, z.tile);
+        if (c.splits > 1 && (tiles - c.whole) * c.splits > slots) slots = (tiles - c.whole) * c.splits;
     };
-    product(half, z.m / 32, z.n == 128 ? 2 : 1);
-    product(half, z.n / 32, 1);
-    product(all, z.n / 32, 1);
+    product(half, z.m / 32);
+    product(half, z.n / 32);
+    product(all, z.n / 32);
+    if (z.n == 128 && slots < half * chain_splits(count, z.m / 32)) slots = half * chain_splits(count, z.m / 32);
     return slots * z.tile * z.tile * 4;
 }
 // ... where there are any, at most
@@ -606,19 +622,24 @@ constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 template <int PA, int PB, bool TB, bool LOLO, int CIN, bool ROWS, int PARTS, int OUT> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
     constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : 2;
     const int64_t tiles = (int64_t)g.tiles * g.matrices;
-    if (g.splits == 0) g.splits = splits_of(tiles, g.steps, tile);
+    if (g.splits == 0) {
+        const Cut c = cut_of(tiles, g.steps, tile);
+        g.whole = c.whole;
+        g.splits = c.splits;
+    }
+    const int64_t cut = tiles - g.whole;
     auto run = [&](auto kernel, int bytes, int threads) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        kernel<<<tiles * g.splits, threads, bytes, st>>>(g);
+        kernel<<<g.whole + cut * g.splits, threads, bytes, st>>>(g);
         return hipGetLastError();
     };
     hipError_t e;
     if (!LOLO && tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, false, CIN, ROWS, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
     else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, LOLO, CIN, ROWS, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
-    if (e != hipSuccess || g.splits == 1 || !sums) return e;
-    if (tile == 256) orth_sums_kernel<16, CIN, ROWS, PARTS, OUT><<<tiles * 32, 256, 0, st>>>(g);
-    else orth_sums_kernel<8, CIN, ROWS, PARTS, OUT><<<tiles * 8, 256, 0, st>>>(g);
+    if (e != hipSuccess || cut == 0 || !sums) return e;
+    if (tile == 256) orth_sums_kernel<16, CIN, ROWS, PARTS, OUT><<<cut * 32, 256, 0, st>>>(g);
+    else orth_sums_kernel<8, CIN, ROWS, PARTS, OUT><<<cut * 8, 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -653,7 +674,7 @@ template <bool F32> struct Steps {
         g.mt = g.nt = z.n / z.tile;
         g.tiles = g.mt * (g.mt + 1) / 2;
         g.a = a, g.b = b, g.c = c;
-        g.steps = a.blocks;
+        g.steps = a.blocks - 1;
         g.alpha = alpha;
         g.part = w.part;
         g.square = z.n;
@@ -733,8 +754,7 @@ template <bool F32> struct Steps {
     // One or two steps of matrices of one tile: all between S and the last product in one launch
     hipError_t chain(const float* abc, int n, bool last) {
         OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
-        const int splits = splits_of(count, g.steps, z.tile);
-        g.splits = splits > 1 ? splits : 2;  // (sums in any case)
+        g.splits = chain_splits(count, g.steps);  // (whole: none, so the sums go to memory in any case)
         hipError_t e = product<2, 2, false, true, 0, false, 2, ORTH_SQUARE>(g, z.tile, st, false);
         if (e != hipSuccess) return e;
         constexpr int bytes = 4 * 32 * ORTH_BLOCK;
@@ -796,8 +816,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         Buffers w;
         w.part = (float*)at;
         at += part;
-        for (OrthOperand& x : w.x) x = operand(at, z.x, z.m / 32, count);
-        for (OrthOperand* o : {&w.s, &w.q, &w.t}) *o = operand(at, z.s, z.n / 32, count);
+        for (OrthOperand& x : w.x) x = operand(at, z.x, z.xb, count);
+        for (OrthOperand* o : {&w.s, &w.q, &w.t}) *o = operand(at, z.s, z.sb, count);
         OrthIn in = {};
         in.g = (const char*)t.g + e0 * t.g_matrix * size_in;
         in.matrix = t.g_matrix;
