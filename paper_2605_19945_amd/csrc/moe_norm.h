@@ -8,18 +8,27 @@
 
 constexpr int NORM_THREADS = 512;
 
-// 8 neighbouring values: 16 bytes of bf16, 32 of fp32
+// 8 neighbouring values as they lie in memory: 16 bytes of bf16, 32 of fp32.  NT: the non-temporal hint, for rows that no cache holds until their
+// next use.
+template <bool NT> static __device__ inline u32x4_t load_word(const void* p) { return NT ? __builtin_nontemporal_load((const u32x4_t*)p) : *(const u32x4_t*)p; }
+template <bool NT> static __device__ inline void store_word(void* p, const u32x4_t& w) {
+    if (NT) __builtin_nontemporal_store(w, (u32x4_t*)p);
+    else *(u32x4_t*)p = w;
+}
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
-    static __device__ inline void load(const uint16_t* p, float (&v)[8]) {
-        const u32x4_t w = *(const u32x4_t*)p;
+    u32x4_t w;
+    template <bool NT> __device__ inline void load(const uint16_t* p) { w = load_word<NT>(p); }
+    __device__ inline void zero() { w = u32x4_t{0, 0, 0, 0}; }
+    __device__ inline void hold() { asm volatile("" : "+v"(w)); }  // what was opened before is opened again rather than kept
+    __device__ inline void open(float (&v)[8]) const {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v[2 * j] = __uint_as_float(w[j] << 16);
             v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
         }
     }
-    static __device__ inline void store(uint16_t* p, const float (&v)[8]) {
+    template <bool NT> static __device__ inline void store(uint16_t* p, const float (&v)[8]) {
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
         u32x4_t w;
 #pragma unroll
@@ -27,26 +36,60 @@ template <> struct Eight<uint16_t> {
             const bf16x2_t t = {(__bf16)v[2 * j], (__bf16)v[2 * j + 1]};  // to nearest even
             w[j] = __builtin_bit_cast(uint32_t, t);
         }
-        *(u32x4_t*)p = w;
+        store_word<NT>(p, w);
     }
 };
 template <> struct Eight<float> {
-    static __device__ inline void load(const float* p, float (&v)[8]) {
-        const f32x4_t a = *(const f32x4_t*)p, b = *(const f32x4_t*)(p + 4);
+    u32x4_t w[2];
+    template <bool NT> __device__ inline void load(const float* p) { w[0] = load_word<NT>(p), w[1] = load_word<NT>(p + 4); }
+    __device__ inline void zero() { w[0] = w[1] = u32x4_t{0, 0, 0, 0}; }
+    __device__ inline void hold() {}
+    __device__ inline void open(float (&v)[8]) const {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j >> 2][j & 3]);
     }
-    static __device__ inline void store(float* p, const float (&v)[8]) {
-        *(f32x4_t*)p = f32x4_t{v[0], v[1], v[2], v[3]};
-        *(f32x4_t*)(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+    template <bool NT> static __device__ inline void store(float* p, const float (&v)[8]) {
+        u32x4_t a, b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(v[j]), b[j] = __float_as_uint(v[4 + j]);
+        store_word<NT>(p, a);
+        store_word<NT>(p + 4, b);
     }
 };
 
-// Weights are read again for every row, from the caches: in registers they would cost a row's chunk twice over.
 static __device__ inline void load_weights(const void* w, bool f32, int col, float (&v)[8]) {
-    if (f32) Eight<float>::load((const float*)w + col, v);
-    else Eight<uint16_t>::load((const uint16_t*)w + col, v);
+    if (w == nullptr) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 1.f;
+    } else if (f32) {
+        Eight<float> e;
+        e.load<false>((const float*)w + col);
+        e.open(v);
+    } else {
+        Eight<uint16_t> e;
+        e.load<false>((const uint16_t*)w + col);
+        e.open(v);
+    }
 }
+// A lane's weights: kept where it has one chunk of a row, otherwise read again for every row, from the caches (in registers they would cost as much
+// as a row's chunks).
+template <int CH> struct Weights {
+    static constexpr bool KEPT = CH == 1;
+    const void* at;
+    bool f32;
+    float kept[8];
+    __device__ inline Weights(const void* w, bool f32_, int col, int d) : at(w), f32(f32_) {
+        if (KEPT && col < d) load_weights(at, f32, col, kept);
+    }
+    __device__ inline void get(int col, float (&v)[8]) const {
+        if (KEPT) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = kept[j];
+        } else {
+            load_weights(at, f32, col, v);
+        }
+    }
+};
 
 static __device__ inline float wave_sum(float v) {
 #pragma unroll
@@ -86,4 +129,6 @@ template <typename F> static inline hipError_t with_layout(int d, F&& f) {
     if (d <= 8192) return f(Layout<8, 2>{});
     return f(Layout<8, 4>{});
 }
+// Tensors that the last-level cache (256 MB) does not hold until their next use: `bytes` of all that a call reads and writes.
+static inline bool norm_streams(int64_t bytes) { return bytes > (int64_t)256 << 20; }
 static inline int norm_rows_per_group(int d) { return d <= 1024 ? 8 : d <= 2048 ? 2 : 1; }

@@ -10,118 +10,149 @@
 
 namespace {
 
-template <typename S, typename B, int W, int CH, bool JOIN, bool NEXT>
-__global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(NormGradArgs a) {
+// A lane's chunks of one row
+template <typename S, typename B, int CH, bool JOIN, bool NEXT> struct Row {
+    Eight<S> D[CH], o[NEXT ? CH : 1];
+    Eight<B> dh[NEXT ? CH : 1], y[JOIN ? CH : 1], g[JOIN ? CH : 1];
+    float gate;
+};
+
+template <typename S, typename B, int W, int CH, bool JOIN, bool NEXT, bool NT>
+__global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4 : 2) void norm_backward_kernel(NormGradArgs a) {
     __shared__ float lds[2][8][4];
     extern __shared__ float sums[];  // [d] where a workgroup has several rows
     constexpr int ROWS = 8 / W;
-    const int group = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+    constexpr bool AHEAD = !(JOIN && NEXT) && CH * (sizeof(S) + sizeof(B)) <= 8;  // the next row is asked for before this one is summed (where registers are left)
+    const int group = W == 8 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)), lane = threadIdx.x % (64 * W);
     const int rows = a.n_rows != nullptr ? min(max(*a.n_rows, 0), a.rows) : a.rows;
     const float over_d = 1.f / (float)a.d;
+    const Weights<CH> weights(JOIN ? a.w : nullptr, a.w_f32, lane * 8, a.d), weights_next(NEXT ? a.w_next : nullptr, a.w_f32, lane * 8, a.d);
     float dw[JOIN ? CH : 1][8] = {}, dnext[NEXT ? CH : 1][8] = {};
     int turn = 0;
-    for (int base = blockIdx.x * ROWS; base < rows; base += gridDim.x * ROWS) {
+    auto fetch = [&](Row<S, B, CH, JOIN, NEXT>& f, int base) {
         const int64_t row = base + group;
         const bool live = row < rows;
-        float D[CH][8], o[NEXT ? CH : 1][8], dh[NEXT ? CH : 1][8], y[JOIN ? CH : 1][8], g[JOIN ? CH : 1][8], gate = 1.f;
+        f.gate = 1.f;
+        if (JOIN && a.gate != nullptr && a.ldgate == 0 && live) f.gate = ((const float*)a.gate)[row];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * 64 * W + lane) * 8;
             const bool here = live && col < a.d;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) D[c][j] = 0.f;
-            if (here && a.dout != nullptr) Eight<S>::load((const S*)a.dout + row * a.lddout + col, D[c]);
+            f.D[c].zero();
+            if (here && a.dout != nullptr) f.D[c].template load<NT>((const S*)a.dout + row * a.lddout + col);
             if constexpr (NEXT) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[c][j] = dh[c][j] = 0.f;
-                if (here) Eight<S>::load((const S*)a.o + row * a.ldo + col, o[c]);
-                if (here) Eight<B>::load((const B*)a.dh + row * a.lddh + col, dh[c]);
+                f.o[c].zero(), f.dh[c].zero();
+                if (here) f.o[c].template load<NT>((const S*)a.o + row * a.ldo + col), f.dh[c].template load<NT>((const B*)a.dh + row * a.lddh + col);
             }
             if constexpr (JOIN) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[c][j] = 0.f, g[c][j] = 1.f;
-                if (here) Eight<B>::load((const B*)a.y + row * a.ldy + col, y[c]);
-                if (here && a.ldgate != 0) Eight<B>::load((const B*)a.gate + row * a.ldgate + col, g[c]);
+                f.y[c].zero(), f.g[c].zero();
+                if (here) f.y[c].template load<NT>((const B*)a.y + row * a.ldy + col);
+                if (here && a.ldgate != 0) f.g[c].template load<NT>((const B*)a.gate + row * a.ldgate + col);
             }
         }
-        if (JOIN && a.gate != nullptr && a.ldgate == 0 && live) gate = ((const float*)a.gate)[row];
+    };
+    auto open_gate = [&](const Row<S, B, CH, JOIN, NEXT>& f, int c, float (&g)[8]) {
+        if (a.ldgate != 0) {
+            f.g[c].open(g);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = 1.f;
+        }
+    };
+    Row<S, B, CH, JOIN, NEXT> next;
+    if (AHEAD) fetch(next, blockIdx.x * ROWS);
+    for (int base = blockIdx.x * ROWS; base < rows; base += gridDim.x * ROWS) {
+        const int64_t row = base + group;
+        const bool live = row < rows;
+        if (!AHEAD) fetch(next, base);
+        Row<S, B, CH, JOIN, NEXT> f = next;
+        if (AHEAD) fetch(next, base + gridDim.x * ROWS);  // (behind the last row: nothing)
         float s[3] = {0.f, 0.f, 0.f};  // sums of o^2, p o and y^2
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * 64 * W + lane) * 8;
             if constexpr (NEXT) {
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.f;
-                if (a.w_next != nullptr && col < a.d) load_weights(a.w_next, a.w_f32, col, w);
+                float w[8] = {}, o[8], dh[8];
+                if (col < a.d) weights_next.get(col, w);
+                f.o[c].open(o), f.dh[c].open(dh);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    s[0] = fmaf(o[c][j], o[c][j], s[0]);
-                    s[1] = fmaf(dh[c][j] * w[j], o[c][j], s[1]);
+                    s[0] = fmaf(o[j], o[j], s[0]);
+                    s[1] = fmaf(dh[j] * w[j], o[j], s[1]);
                 }
+                f.o[c].hold(), f.dh[c].hold();
             }
             if constexpr (JOIN) {
+                float y[8];
+                f.y[c].open(y);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[2] = fmaf(y[c][j], y[c][j], s[2]);
+                for (int j = 0; j < 8; ++j) s[2] = fmaf(y[j], y[j], s[2]);
+                f.y[c].hold();
             }
         }
         if (NEXT || a.norm) group_sums<W>(s, lds, turn);
         const float r = rsqrtf(fmaf(s[0], over_d, a.eps)), k = r * r * r * (s[1] * over_d);
         const float ry = JOIN && a.norm ? rsqrtf(fmaf(s[2], over_d, a.eps)) : 1.f;
         float u[1] = {0.f};  // sum of g D w y, without the row's gate
+        float D[JOIN ? CH : 1][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * 64 * W + lane) * 8;
             if (!(live && col < a.d)) continue;
+            float* Dc = D[JOIN ? c : 0];
+            float out[8];
+            f.D[c].open(out);
             if constexpr (NEXT) {
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.f;
-                if (a.w_next != nullptr) load_weights(a.w_next, a.w_f32, col, w);
+                float w[8], o[8], dh[8];
+                weights_next.get(col, w);
+                f.o[c].open(o), f.dh[c].open(dh);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    D[c][j] += r * (dh[c][j] * w[j]) - o[c][j] * k;
-                    dnext[c][j] = fmaf(dh[c][j], o[c][j] * r, dnext[c][j]);
+                    out[j] += r * (dh[j] * w[j]) - o[j] * k;
+                    dnext[c][j] = fmaf(dh[j], o[j] * r, dnext[c][j]);
                 }
             }
-            float out[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) out[j] = JOIN ? a.scale * D[c][j] : D[c][j];
-            Eight<S>::store((S*)a.dx + row * a.lddx + col, out);
+            for (int j = 0; j < 8; ++j) {
+                Dc[j] = out[j];
+                if (JOIN) out[j] *= a.scale;
+            }
+            Eight<S>::template store<NT>((S*)a.dx + row * a.lddx + col, out);
             if constexpr (JOIN) {
-                float w[8];
+                float w[8], y[8], g[8];
+                weights.get(col, w);
+                f.y[c].open(y);
+                open_gate(f, c, g);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.f;
-                if (a.w != nullptr) load_weights(a.w, a.w_f32, col, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[0] = fmaf(g[c][j] * D[c][j], w[j] * y[c][j], u[0]);
+                for (int j = 0; j < 8; ++j) u[0] = fmaf(g[j] * Dc[j], w[j] * y[j], u[0]);
                 if (a.ldgate != 0 && a.dgate != nullptr) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) out[j] = D[c][j] * (y[c][j] * ry * w[j]);
-                    Eight<B>::store((B*)a.dgate + row * a.lddgate + col, out);
+                    for (int j = 0; j < 8; ++j) out[j] = Dc[j] * (y[j] * ry * w[j]);
+                    Eight<B>::template store<NT>((B*)a.dgate + row * a.lddgate + col, out);
                 }
+                f.y[c].hold(), f.g[c].hold();
             }
         }
         if constexpr (JOIN) {
             const bool row_gate = a.ldgate == 0 && a.dgate != nullptr;
             if (a.norm || row_gate) group_sums<W>(u, lds, turn);
             if (row_gate && live && lane == 0) ((float*)a.dgate)[row] = u[0] * ry;
-            const float ky = a.norm ? ry * ry * ry * (gate * u[0] * over_d) : 0.f;
+            const float ky = a.norm ? ry * ry * ry * (f.gate * u[0] * over_d) : 0.f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (c * 64 * W + lane) * 8;
                 if (!(live && col < a.d)) continue;
-                float w[8], out[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.f;
-                if (a.w != nullptr) load_weights(a.w, a.w_f32, col, w);
+                float w[8], y[8], g[8], out[8];
+                weights.get(col, w);
+                f.y[c].open(y);
+                open_gate(f, c, g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float dn = gate * g[c][j] * D[c][j];
-                    out[j] = ry * (dn * w[j]) - y[c][j] * ky;
-                    dw[c][j] = fmaf(dn, y[c][j] * ry, dw[c][j]);
+                    const float dn = f.gate * g[j] * D[c][j];
+                    out[j] = ry * (dn * w[j]) - y[j] * ky;
+                    dw[c][j] = fmaf(dn, y[j] * ry, dw[c][j]);
                 }
-                Eight<B>::store((B*)a.dy + row * a.lddy + col, out);
+                Eight<B>::template store<NT>((B*)a.dy + row * a.lddy + col, out);
             }
         }
     }
@@ -136,11 +167,10 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(NormGradArg
                         const int col = (c * 64 * W + lane) * 8;
                         if (col >= a.d) continue;
                         float t[8] = {};
-                        if (i > 0) Eight<float>::load(sums + col, t);
+                        if (i > 0) load_weights(sums, true, col, t);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) t[j] += v[c][j];
-                        if (i < ROWS - 1) Eight<float>::store(sums + col, t);
-                        else Eight<float>::store(part + col, t);
+                        Eight<float>::store<false>((i < ROWS - 1 ? sums : part) + col, t);
                     }
                 }
                 __syncthreads();
@@ -149,7 +179,7 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(NormGradArg
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (c * 64 * W + lane) * 8;
-                if (col < a.d) Eight<float>::store(part + col, v[c]);
+                if (col < a.d) Eight<float>::store<false>(part + col, v[c]);
             }
         }
     };
@@ -176,14 +206,20 @@ __global__ __launch_bounds__(256) void norm_weights_kernel(const float* part0, f
     }
 }
 
-template <typename S, typename B> hipError_t launch(const NormGradArgs& a, int grid, hipStream_t st) {
+template <typename S, typename B, bool NT> hipError_t launch(const NormGradArgs& a, int grid, hipStream_t st) {
     return with_layout(a.d, [&](auto l) {
         constexpr int W = decltype(l)::W, CH = decltype(l)::CH;
-        auto kernel = a.y == nullptr ? norm_backward_kernel<S, B, W, CH, false, true>
-                                     : a.dh != nullptr ? norm_backward_kernel<S, B, W, CH, true, true> : norm_backward_kernel<S, B, W, CH, true, false>;
+        auto kernel = a.y == nullptr ? norm_backward_kernel<S, B, W, CH, false, true, NT>
+                                     : a.dh != nullptr ? norm_backward_kernel<S, B, W, CH, true, true, NT> : norm_backward_kernel<S, B, W, CH, true, false, NT>;
         kernel<<<grid, NORM_THREADS, W < 8 ? a.d * 4 : 0, st>>>(a);
         return hipGetLastError();
     });
+}
+
+template <typename S, typename B> hipError_t launch(const NormGradArgs& a, int grid, hipStream_t st) {
+    const int64_t n = (int64_t)a.rows * a.d, stream = sizeof(S) * (1 + (a.dout != nullptr) + (a.dh != nullptr)),
+                  block = sizeof(B) * ((a.dh != nullptr) + (a.y != nullptr ? 2 : 0) + (a.ldgate != 0 ? 2 : 0));
+    return norm_streams(n * (stream + block)) ? launch<S, B, true>(a, grid, st) : launch<S, B, false>(a, grid, st);
 }
 
 }  // namespace
