@@ -752,6 +752,18 @@ def _no_graphs(what, *tensors):
             return _no_graph(what)
 
 
+def _plain(t, dev):
+    return t.is_contiguous() and t.get_device() == dev
+
+
+def _fits(stream, block):
+    return (stream is _BF16 or stream is _F32) and (block is stream or block is _BF16)
+
+
+def _weight_ok(w, d, dev):
+    return (w.dtype is _F32 or w.dtype is _BF16) and w.shape == (d,) and w.is_contiguous() and w.get_device() == dev
+
+
 def _gate_of(what, gate, rows, d, block):
     """(address, values between its rows; 0: a number for each row) of a gate or its gradient."""
     if gate is None:
@@ -800,16 +812,24 @@ def moe_rms_norm_backward(dh, x, weight=None, eps=1e-6, dres=None, offsets=None,
     """(gradient of x, gradient of the weight in float32; None without a weight) from that of moe_rms_norm's result.  dres: what x gets by another
     way (the residual's), added.  out: where the gradient of x goes; it may be dh, x or dres."""
     lib, what = _lib or load_library(), "moe_rms_norm_backward"
-    _no_graphs(what, dh, x, weight, dres, out)
+    if (x.requires_grad or dh.requires_grad or weight is not None and weight.requires_grad or dres is not None and dres.requires_grad
+            or out is not None and out.requires_grad):
+        _no_graph(what)
     live = None if offsets is None else _live(what, offsets)
     if x.dim() != 2:
         _refuse(what, "x has to be a matrix")
-    rows, d = x.shape
-    ldx, lddh = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "dh", dh, rows, d)
-    _norm_types(what, x.dtype, dh.dtype)
-    wt = _norm_weights(what, d, weight)
-    lddres = 0 if dres is None else _norm_matrix(what, "dres", dres, rows, d, x.dtype)
-    dev = _launch_device(what, x, dh, weight, dres, offsets, out)
+    (rows, d), dev, stream, block = x.shape, x.get_device(), x.dtype, dh.dtype
+    if (offsets is None and out is None and dh.shape == (rows, d) and _plain(x, dev) and _plain(dh, dev) and _fits(stream, block) and dev >= 0
+            and _device() == dev and (weight is None or _weight_ok(weight, d, dev))
+            and (dres is None or dres.dtype is stream and dres.shape == (rows, d) and _plain(dres, dev))):
+        ldx = lddh = lddres = d
+        wt = 0 if weight is not None and weight.dtype is _BF16 else 1
+    else:
+        ldx, lddh = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "dh", dh, rows, d)
+        _norm_types(what, stream, block)
+        wt = _norm_weights(what, d, weight)
+        lddres = 0 if dres is None else _norm_matrix(what, "dres", dres, rows, d, stream)
+        dev = _launch_device(what, x, dh, weight, dres, offsets, out)
     dx, lddx = out, d
     if out is None:
         dx = x.new_empty(rows, d)
@@ -835,17 +855,25 @@ def moe_residual_norm(x, y, weight=None, norm=True, gate=None, scale=1.0, next_w
     next_weight.  x [rows, d] is the residual stream, y the block's output (of x's type or bfloat16); gate [rows] float32 or [rows, d] of
     y's type.  offsets: rows from its last value on are left as they are.  out and h may each be x, y or a gate of values."""
     lib, what = _lib or load_library(), "moe_residual_norm"
-    _no_graphs(what, x, y, weight, gate, next_weight, out, h)
+    if (x.requires_grad or y.requires_grad or weight is not None and weight.requires_grad or gate is not None and gate.requires_grad
+            or next_weight is not None and next_weight.requires_grad or out is not None and out.requires_grad or h is not None and h.requires_grad):
+        _no_graph(what)
     live = None if offsets is None else _live(what, offsets)
     if x.dim() != 2:
         _refuse(what, "x has to be a matrix")
-    rows, d = x.shape
-    stream, block = x.dtype, y.dtype
-    ldx, ldy = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "y", y, rows, d)
-    _norm_types(what, stream, block)
-    wt = _norm_weights(what, d, weight, next_weight)
-    gate_at, ldgate = _gate_of(what, gate, rows, d, block)
-    dev = _launch_device(what, x, y, weight, gate, next_weight, offsets, out, h)
+    (rows, d), dev, stream, block = x.shape, x.get_device(), x.dtype, y.dtype
+    if (offsets is None and out is None and h is None and (gate is None or gate.dtype is _F32 and gate.shape == (rows,) and _plain(gate, dev)) and y.shape == (rows, d) and _plain(x, dev) and _plain(y, dev)
+            and _fits(stream, block) and dev >= 0 and _device() == dev and (weight is None or _weight_ok(weight, d, dev))
+            and (next_weight is None or _weight_ok(next_weight, d, dev) and (weight is None or weight.dtype is next_weight.dtype))):
+        ldx = ldy = d
+        some = weight if weight is not None else next_weight
+        wt, gate_at, ldgate = 0 if some is not None and some.dtype is _BF16 else 1, None if gate is None else gate.data_ptr(), 0
+    else:
+        ldx, ldy = _norm_matrix(what, "x", x, rows, d), _norm_matrix(what, "y", y, rows, d)
+        _norm_types(what, stream, block)
+        wt = _norm_weights(what, d, weight, next_weight)
+        gate_at, ldgate = _gate_of(what, gate, rows, d, block)
+        dev = _launch_device(what, x, y, weight, gate, next_weight, offsets, out, h)
     if h is not None and next_weight is None:
         _refuse(what, "h needs next_weight")
     o, ldo, n, ldh = out, d, h, d
@@ -877,7 +905,10 @@ def moe_residual_norm_backward(dout, y, weight=None, out=None, dh=None, norm=Tru
     are float32; where there is no weight or gate, None.  dx and dy: where the first two go; they may be dout, dh, out, y or a gate of
     values, not each other."""
     lib, what = _lib or load_library(), "moe_residual_norm_backward"
-    _no_graphs(what, dout, y, weight, out, dh, gate, next_weight, dx, dy)
+    if (y.requires_grad or dout is not None and dout.requires_grad or weight is not None and weight.requires_grad or out is not None and out.requires_grad
+            or dh is not None and dh.requires_grad or gate is not None and gate.requires_grad or next_weight is not None and next_weight.requires_grad
+            or dx is not None and dx.requires_grad or dy is not None and dy.requires_grad):
+        _no_graph(what)
     live = None if offsets is None else _live(what, offsets)
     if y.dim() != 2:
         _refuse(what, "y has to be a matrix")
@@ -887,15 +918,24 @@ def moe_residual_norm_backward(dout, y, weight=None, out=None, dh=None, norm=Tru
         _refuse(what, "dh needs out")
     if dout is None and dh is None:
         _refuse(what, "dout or dh has to be there")
-    rows, d = y.shape
-    block, stream = y.dtype, (dout if dout is not None else out).dtype
-    ldy = _norm_matrix(what, "y", y, rows, d)
-    _norm_types(what, stream, block)
-    lddout = 0 if dout is None else _norm_matrix(what, "dout", dout, rows, d, stream)
-    ldo, lddh = (0, 0) if dh is None else (_norm_matrix(what, "out", out, rows, d, stream), _norm_matrix(what, "dh", dh, rows, d, block))
-    wt = _norm_weights(what, d, weight, next_weight)
-    gate_at, ldgate = _gate_of(what, gate, rows, d, block)
-    dev = _launch_device(what, y, dout, weight, out, dh, gate, next_weight, offsets, dx, dy)
+    (rows, d), dev, block, stream = y.shape, y.get_device(), y.dtype, (dout if dout is not None else out).dtype
+    if (offsets is None and dx is None and dy is None and dout is not None and dout.shape == (rows, d) and _plain(y, dev) and _plain(dout, dev)
+            and _fits(stream, block) and dev >= 0 and _device() == dev and (weight is None or _weight_ok(weight, d, dev))
+            and (dh is None or dh.dtype is block and out.dtype is stream and dh.shape == (rows, d) and out.shape == (rows, d) and _plain(dh, dev)
+                 and _plain(out, dev) and _weight_ok(next_weight, d, dev) and (weight is None or weight.dtype is next_weight.dtype))
+            and (gate is None or _plain(gate, dev) and (gate.dtype is _F32 and gate.shape == (rows,) or gate.dtype is block and gate.shape == (rows, d)))):
+        ldy = lddout = ldo = lddh = d
+        some = weight if weight is not None else next_weight
+        wt = 0 if some is not None and some.dtype is _BF16 else 1
+        gate_at, ldgate = (None, 0) if gate is None else (gate.data_ptr(), 0 if gate.dim() == 1 else d)
+    else:
+        ldy = _norm_matrix(what, "y", y, rows, d)
+        _norm_types(what, stream, block)
+        lddout = 0 if dout is None else _norm_matrix(what, "dout", dout, rows, d, stream)
+        ldo, lddh = (0, 0) if dh is None else (_norm_matrix(what, "out", out, rows, d, stream), _norm_matrix(what, "dh", dh, rows, d, block))
+        wt = _norm_weights(what, d, weight, next_weight)
+        gate_at, ldgate = _gate_of(what, gate, rows, d, block)
+        dev = _launch_device(what, y, dout, weight, out, dh, gate, next_weight, offsets, dx, dy)
     gx, lddx, gy, lddy = dx, d, dy, d
     if dx is None:
         gx = y.new_empty(rows, d, dtype=stream)
