@@ -322,85 +322,224 @@ template <int F, int CIN, bool ROWS, int PARTS, int OUT> __global__ __launch_bou
     finish<CIN, ROWS, PARTS, OUT>(g, u, v, lane, matrix, (tm * F + f / F) * 16, (tn * F + f % F) * 16, tm != tn);
 }
 
-// ---- the small products of matrices of one tile of 128, S in ranges -> a I + b S + c S S, or of two steps the product of both ----
-// One workgroup a matrix, everything in LDS: two matrices of 128 x 128 in two parts, in blocks.  Wavefronts 4 x 2 of 2 x 4 fragments.
-__global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
+// ... into the first range's place, where one workgroup alone would be long at it: 4 of F fragments a workgroup
+__global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits, int F) {
+    f32x4_t* p = (f32x4_t*)part + (int64_t)blockIdx.y * splits * (F * 64) + (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) v += p[(int64_t)s * (F * 64)];
+    *p = v;
+}
+
+// ---- all between S and the next product with X, for matrices of up to 128 rows ----
+// S's ranges -> a I + b S + c S S, or of two steps the product of both.  One workgroup a matrix, everything in LDS: two matrices of 16 NF rows in
+// two parts, in blocks; a wavefront has a row of fragments.
+template <int NF> __global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
     extern __shared__ __align__(1024) char lds[];
-    constexpr int PLANE = 32 * ORTH_BLOCK, FM = 2, FN = 4;  // 8 x 4 blocks
+    constexpr int KB = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
     char *s = lds, *q = lds + 2 * PLANE;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, matrix = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.x;
+    const bool on = wave < NF;
     const int at_row = orth_piece(lane & 15, lane >> 4) * 16;
-    f32x4_t v[FM][FN];
-    auto each = [&](auto&& f) {
+    f32x4_t v[NF];
+    // where a lane's 4 values of a fragment lie: columns 16 n + 4 (lane / 16) + 0..3 of row 16 wave + lane % 16
+    auto at = [&](int n, int blocks) { return (wave * blocks + (n >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (n & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
+    auto put = [&](char* to, int64_t plane, int blocks) {
+        if (!on) return;
 #pragma unroll
-        for (int m = 0; m < FM; ++m)
-#pragma unroll
-            for (int n = 0; n < FN; ++n) f(m, n, wm * FM + m, wn * FN + n);
-    };
-    // where a lane's 4 values of a fragment lie: columns 16 fn + 4 (lane / 16) + 0..3 of row 16 fm + lane % 16
-    auto at = [&](int fm, int fn, int blocks = 4) { return (fm * blocks + (fn >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (fn & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
-    auto put = [&](char* to, int64_t plane, int blocks = 4) {
-        each([&](int m, int n, int fm, int fn) {
-            const f32x4_t& x = v[m][n];
+        for (int n = 0; n < NF; ++n) {
+            const f32x4_t& x = v[n];
             const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
-            *(u32x2_t*)(to + at(fm, fn, blocks)) = u32x2_t{h0, h1};
-            *(u32x2_t*)(to + plane + at(fm, fn, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
-        });
+            *(u32x2_t*)(to + at(n, blocks)) = u32x2_t{h0, h1};
+            *(u32x2_t*)(to + plane + at(n, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+        }
     };
     auto multiply = [&](const char* x, const char* y, float scale) {  // v = scale x y, y symmetric
-        each([&](int m, int n, int, int) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+        if (!on) return;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            f16x8_t a[2][FM], b[2][FN];
+        for (int n = 0; n < NF; ++n) v[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KB; ++k) {
+            f16x8_t a[2], b[2][NF];
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
+                a[p] = *(const f16x8_t*)(x + p * PLANE + (wave * KB + k) * ORTH_BLOCK + at_row);
 #pragma unroll
-                for (int m = 0; m < FM; ++m) a[p][m] = *(const f16x8_t*)(x + p * PLANE + ((wm * FM + m) * 4 + k) * ORTH_BLOCK + at_row);
-#pragma unroll
-                for (int n = 0; n < FN; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + ((wn * FN + n) * 4 + k) * ORTH_BLOCK + at_row);
+                for (int n = 0; n < NF; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + (n * KB + k) * ORTH_BLOCK + at_row);
             }
-            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[0][m], v[m][n], 0, 0, 0); });
-            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][n], a[0][m], v[m][n], 0, 0, 0); });
-            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][n], a[1][m], v[m][n], 0, 0, 0); });
-            each([&](int m, int n, int, int) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][n], a[1][m], v[m][n], 0, 0, 0); });
+            orth_repeat<4>([&](auto pair) {
+                constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
+#pragma unroll
+                for (int n = 0; n < NF; ++n) v[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p], v[n], 0, 0, 0);
+            });
         }
-        each([&](int m, int n, int, int) { v[m][n] *= scale; });
+#pragma unroll
+        for (int n = 0; n < NF; ++n) v[n] *= scale;
     };
     auto polynomial = [&](float a, float b, float c) {  // v = a I + b s + c s s
         multiply(s, s, c * (Q_SCALE / (S_SCALE * S_SCALE)));
-        each([&](int m, int n, int fm, int fn) {
-            const u32x2_t hi = *(const u32x2_t*)(s + at(fm, fn)), lo = *(const u32x2_t*)(s + PLANE + at(fm, fn));
+        if (!on) return;
+#pragma unroll
+        for (int n = 0; n < NF; ++n) {
+            const u32x2_t hi = *(const u32x2_t*)(s + at(n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(n, KB));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float x = j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]);
-                v[m][n][j] = fmaf(b * (Q_SCALE / S_SCALE), x, v[m][n][j]) + (fm == fn && 4 * (lane >> 4) + j == (lane & 15) ? a * Q_SCALE : 0.f);
+                v[n][j] = fmaf(b * (Q_SCALE / S_SCALE), x, v[n][j]) + (wave == n && 4 * (lane >> 4) + j == (lane & 15) ? a * Q_SCALE : 0.f);
             }
-        });
+        }
     };
 
-    const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * splits * (64 * 64) + lane;
-    each([&](int m, int n, int, int) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
-    for (int i = 0; i < splits; ++i) each([&](int m, int n, int fm, int fn) { v[m][n] += part[((int64_t)i * 64 + fm * 8 + fn) * 64]; });
-    each([&](int m, int n, int, int) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
-    put(s, PLANE);
+    if (on) {
+        const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * apart * (NF * NF * 64) + wave * NF * 64 + lane;  // (apart: ranges between matrices)
+#pragma unroll
+        for (int n = 0; n < NF; ++n) v[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int i = 0; i < splits; ++i) {
+#pragma unroll
+            for (int n = 0; n < NF; ++n) v[n] += part[((int64_t)i * NF * NF + n) * 64];
+        }
+#pragma unroll
+        for (int n = 0; n < NF; ++n) v[n] *= S_SCALE / (X_SCALE * X_SCALE);
+    }
+    put(s, PLANE, KB);
     __syncthreads();
     polynomial(a1, b1, c1);
     if (two) {
-        put(q, PLANE);
+        put(q, PLANE, KB);
         __syncthreads();
         for (int i = 0; i < 2; ++i) {  // s = q s q = (q x) (q x)^T: they commute
             multiply(s, q, 1.f / Q_SCALE);
             __syncthreads();
-            put(s, PLANE);
+            put(s, PLANE, KB);
             __syncthreads();
         }
         polynomial(a2, b2, c2);
         __syncthreads();
-        put(s, PLANE);
+        put(s, PLANE, KB);
         __syncthreads();
         multiply(s, q, 1.f / Q_SCALE);
     }
     put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
+}
+
+// ---- matrices of up to 64 rows ----
+// A wavefront takes 32 columns of X at a time, all its rows (16 NF): they are few enough that Q X and the new S = X X^T of these columns are formed
+// one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it.  MODE 0: S of X as it is;
+// 1: X = Q X and its S; 2: X = Q X to the caller.
+// The results' lanes have the columns 4 q + 0..3 and 16 + 4 q + 0..3 of row i; after the change of halves that the stores want, lane (i, q) has 8
+// neighbouring columns of row i, in another order of q than an operand's lanes.  S sums over the columns, so any order will do that both of
+// its operands have: the results are operands as they are.
+template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void orth_thin_kernel(OrthArgs g) {
+    constexpr int KB = NF / 2;
+    extern __shared__ __align__(1024) char lds[];  // a wavefront's blocks, NF of each part; then the wavefronts' S
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, i16 = lane & 15, q16 = lane >> 4;
+    const int at_row = orth_piece(i16, q16) * 16;
+    const int t_row = 8 * (q16 & 1) + (i16 >> 2), t_g = (i16 & 3) >> 1;
+    const int at_turn = orth_piece(t_row, t_g) * 16 + (i16 & 1) * 8, at_next = orth_piece(t_row + 4, t_g) * 16 + (i16 & 1) * 8;
+    char* mine = lds + wave * (2 * NF * ORTH_BLOCK);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)) + wave * (2 * NF * ORTH_BLOCK);
+    const uint32_t line = (uint32_t)g.b.blocks * ORTH_BLOCK;
+    u32x4_t desc[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) desc[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix, (uint32_t)g.b.matrix);
+    f16x8_t q[2][NF][KB];
+    if constexpr (MODE > 0) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int m = 0; m < NF; ++m)
+#pragma unroll
+                for (int k = 0; k < KB; ++k) q[p][m][k] = *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + (m * g.a.blocks + k) * ORTH_BLOCK + at_row);
+    }
+    f32x4_t s[NF][NF];
+#pragma unroll
+    for (int m = 0; m < NF; ++m)
+#pragma unroll
+        for (int n = 0; n < NF; ++n) s[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int c = blockIdx.x * 4 + wave; c < g.steps; c += gridDim.x * 4) {
+        f16x8_t x[2][NF];  // rows of the new X: what S is of
+        if constexpr (MODE == 0) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int m = 0; m < NF; ++m) x[p][m] = *(const f16x8_t*)(g.b.part[p] + matrix * g.b.matrix + (int64_t)m * line + c * ORTH_BLOCK + at_row);
+        } else {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the columns before have been read)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int m = 0; m < NF; ++m) orth_load(to + (p * NF + m) * ORTH_BLOCK, lane * 16, desc[p], m * line + c * ORTH_BLOCK);
+            orth_wait<0>();
+            f32x4_t v[NF][2];
+#pragma unroll
+            for (int m = 0; m < NF; ++m) v[m][0] = v[m][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                f16x8_t b[2][2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        typedef short s16x4_t __attribute__((ext_vector_type(4)));
+                        typedef __attribute__((address_space(3))) s16x4_t lds4;
+                        const char* block = mine + (p * NF + 2 * k + (q16 >> 1)) * ORTH_BLOCK + j * 512;
+                        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_turn)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_next));
+                        b[p][j] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+                orth_repeat<4>([&](auto pair) {
+                    constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
+#pragma unroll
+                    for (int m = 0; m < NF; ++m)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) v[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][j], q[p][m][k], v[m][j], 0, 0, 0);
+                });
+            }
+#pragma unroll
+            for (int m = 0; m < NF; ++m) {
+                if constexpr (MODE == 2) {
+                    finish<0, false, 0, OUT>(g, v[m][0], v[m][1], lane, matrix, m * 16, c * 32, false);
+                } else {
+                    f32x4_t u = v[m][0] * g.alpha, w = v[m][1] * g.alpha;
+                    uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        if (p == 1) {
+                            const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
+                            a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
+                            a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
+                            a[2] = pack_f16(w[0] - f16_lo(h[2]), w[1] - f16_hi(h[2]));
+                            a[3] = pack_f16(w[2] - f16_lo(h[3]), w[3] - f16_hi(h[3]));
+                        }
+                        const auto y = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), z = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
+                        const u32x4_t piece = {y[0], z[0], y[1], z[1]};
+                        x[p][m] = __builtin_bit_cast(f16x8_t, piece);
+                        *(u32x4_t*)(g.c.part[p] + matrix * g.c.matrix + (int64_t)m * line + c * ORTH_BLOCK + orth_piece(i16, (q16 & 1) * 2 + (q16 >> 1)) * 16) = piece;
+                    }
+                }
+            }
+        }
+        if constexpr (MODE < 2) {
+            orth_repeat<4>([&](auto pair) {
+                constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
+#pragma unroll
+                for (int m = 0; m < NF; ++m)
+#pragma unroll
+                    for (int n = 0; n < NF; ++n) s[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[r][n], x[p][m], s[m][n], 0, 0, 0);
+            });
+        }
+    }
+    if constexpr (MODE < 2) {  // the four wavefronts' sums, in their order
+        __syncthreads();
+        f32x4_t* all = (f32x4_t*)lds;
+#pragma unroll
+        for (int m = 0; m < NF; ++m)
+#pragma unroll
+            for (int n = 0; n < NF; ++n) all[(wave * NF * NF + m * NF + n) * 64 + lane] = s[m][n];
+        __syncthreads();
+        f32x4_t* part = (f32x4_t*)g.part + ((int64_t)matrix * gridDim.x + blockIdx.x) * (NF * NF * 64);
+        for (int i = threadIdx.x; i < NF * NF * 64; i += 256) part[i] = all[i] + all[i + NF * NF * 64] + all[i + 2 * NF * NF * 64] + all[i + 3 * NF * NF * 64];
+    }
 }
 
 // ---- the way in ----
@@ -415,6 +554,7 @@ struct OrthIn {
     float eps;
     int tall;            // G^T is what is put into blocks
     int vec;             // rows begin at multiples of 16 bytes
+    int block_rows;      // of x
     OrthOperand x;
 };
 
@@ -537,6 +677,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
             lo[j] = pack_f16(v[2 * j] - f16_lo(hi[j]), v[2 * j + 1] - f16_hi(hi[j]));
         }
         const int R = (in.tall ? c0 : r0) / 16 + (k >> 7), C = (in.tall ? r0 : c0) / 32 + (k >> 6 & 1);
+        if (R >= in.block_rows) continue;
         const int64_t at = matrix * in.x.matrix + ((int64_t)R * in.x.blocks + C) * ORTH_BLOCK + orth_piece(k & 15, g8) * 16;
         *(u32x4_t*)(in.x.part[0] + at) = hi;
         *(u32x4_t*)(in.x.part[1] + at) = lo;
@@ -546,7 +687,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
 // ---- plan ----
 struct Size {
     int n, m;        // of X, padded
-    int tile;        // 256 or 128
+    int tile;        // 256 or 128; 0: all rows and 32 columns at a time (up to 64 rows)
     int parts;       // of the squares
     // Blocks along the rows of X and of S: an odd number, so that the block rows that are loaded together begin in different places of the memory
     // channels' interleaving (a power of two put them all on the same few).
@@ -583,9 +724,9 @@ double step_time(int E, int n, int m, int tile) {
 Size size_of_matrix(int E, int rows, int cols) {
     Size z;
     const int n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    z.tile = n > 128 && step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
-    z.n = (n + z.tile - 1) / z.tile * z.tile;
-    z.m = (m + z.tile - 1) / z.tile * z.tile;
+    z.tile = n <= 64 ? 0 : n > 128 && step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
+    z.n = z.tile == 0 ? (n <= 32 ? 32 : 64) : (n + z.tile - 1) / z.tile * z.tile;
+    z.m = z.tile == 0 ? (m + 63) / 64 * 64 : (m + z.tile - 1) / z.tile * z.tile;
     z.xb = z.m / 32 + 1, z.sb = z.n / 32 + 1;
     z.x = (int64_t)z.n / 16 * z.xb * ORTH_BLOCK;
     z.s = (int64_t)z.n / 16 * z.sb * ORTH_BLOCK;
@@ -602,8 +743,14 @@ int chain_splits(int count, int steps) {
     const int room = 2 * kUnits / count, s = room < steps / 4 ? room : steps / 4;
     return s > 1 ? s : 1;
 }
+// Workgroups that share the columns of a matrix of up to 64 rows, of which each leaves sums
+int thin_groups(int count, int m) {
+    const int want = (m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1;
+    return want < room ? want : room;
+}
 // Sums of the cut reductions of `count` matrices
 int64_t part_bytes(int count, const Size& z) {
+    if (z.tile == 0) return (int64_t)count * thin_groups(count, z.m) * z.n * z.n * 4;
     const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
     int64_t slots = 0;
     auto product = [&](int64_t tiles, int64_t steps) {
@@ -680,6 +827,18 @@ template <bool F32> struct Steps {
         g.square = z.n;
         return g;
     }
+    void to_caller(OrthArgs& g) const {
+        g.alpha *= t.scale / X_SCALE;
+        g.beta *= t.scale / X_SCALE;
+        g.out = out;
+        g.out_matrix = t.out_matrix;
+        g.out_ld = t.out_ld;
+        g.tall = t.rows > t.cols;
+        g.rows = g.tall ? t.cols : t.rows;
+        g.cols = g.tall ? t.rows : t.cols;
+        const int size = F32 ? 4 : 2;
+        g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
+    }
     // X = q X, into the other buffer or to the caller; where q has one part, X = (a + rest) X + q X of X's first part
     template <bool TWO, bool LOLO = false> hipError_t apply(const OrthOperand& q, float a, bool last) {
         constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 2;
@@ -699,16 +858,7 @@ template <bool F32> struct Steps {
         if (!last) {
             e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 2, ORTH_BLOCKS>(g, z.tile, st);
         } else {
-            g.alpha *= t.scale / X_SCALE;
-            g.beta *= t.scale / X_SCALE;
-            g.out = out;
-            g.out_matrix = t.out_matrix;
-            g.out_ld = t.out_ld;
-            g.tall = t.rows > t.cols;
-            g.rows = g.tall ? t.cols : t.rows;
-            g.cols = g.tall ? t.rows : t.cols;
-            const int size = F32 ? 4 : 2;
-            g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
+            to_caller(g);
             e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 0, F32 ? ORTH_F32 : ORTH_BF16>(g, z.tile, st);
         }
         const OrthOperand o = w.x[0];
@@ -755,25 +905,72 @@ template <bool F32> struct Steps {
     hipError_t chain(const float* abc, int n, bool last) {
         OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
         g.splits = chain_splits(count, g.steps);  // (whole: none, so the sums go to memory in any case)
-        hipError_t e = product<2, 2, false, true, 0, false, 2, ORTH_SQUARE>(g, z.tile, st, false);
+        const hipError_t e = product<2, 2, false, true, 0, false, 2, ORTH_SQUARE>(g, z.tile, st, false);
         if (e != hipSuccess) return e;
-        constexpr int bytes = 4 * 32 * ORTH_BLOCK;
-        e = hipFuncSetAttribute((const void*)orth_chain_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t f = link<8>(g, g.splits, abc, n);
+        return f != hipSuccess ? f : apply<true, true>(w.q, 0.f, last);
+    }
+    template <int NF> hipError_t link(const OrthArgs& g, int splits, const float* abc, int n) {
+        int ranges = splits;
+        if (ranges > 8) {
+            orth_fold_kernel<<<dim3(NF * NF / 4, count), 256, 0, st>>>(w.part, ranges, NF * NF);
+            ranges = 1;
+        }
+        constexpr int bytes = 4 * NF * (NF / 2) * ORTH_BLOCK;
+        const hipError_t e = hipFuncSetAttribute((const void*)orth_chain_kernel<NF>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        orth_chain_kernel<<<count, 512, bytes, st>>>(g, g.splits, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
-        e = hipGetLastError();
-        return e != hipSuccess ? e : apply<true, true>(w.q, 0.f, last);
+        orth_chain_kernel<NF><<<count, 512, bytes, st>>>(g, splits, ranges, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
+        return hipGetLastError();
+    }
+    // Matrices of up to 64 rows (16 NF padded)
+    template <int NF> hipError_t thin() {
+        const int groups = thin_groups(count, z.m);
+        auto launch = [&](auto kernel, const OrthArgs& g) {
+            const int bytes = 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF) * ORTH_BLOCK;
+            const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            if (e != hipSuccess) return e;
+            kernel<<<dim3(groups, count), 256, bytes, st>>>(g);
+            return hipGetLastError();
+        };
+        OrthArgs g = {};
+        g.matrices = count;
+        g.a = w.q, g.b = w.x[0];
+        g.steps = z.m / 32;
+        g.part = w.part;
+        hipError_t e = launch(orth_thin_kernel<NF, 0, ORTH_BLOCKS>, g);
+        for (int k = 0; k < t.steps && e == hipSuccess;) {
+            const int n = !F32 && k + 2 <= t.steps ? 2 : 1;
+            const float* abc = t.coefficients + 3 * k;
+            k += n;
+            OrthArgs l = {};
+            l.c = w.q;
+            l.part = w.part;
+            e = link<NF>(l, groups, abc, n);
+            if (e != hipSuccess) break;
+            g.b = w.x[0], g.c = w.x[1];
+            g.alpha = 1.f / Q_SCALE;
+            if (k < t.steps) {
+                e = launch(orth_thin_kernel<NF, 1, ORTH_BLOCKS>, g);
+            } else {
+                to_caller(g);
+                e = launch(orth_thin_kernel<NF, 2, F32 ? ORTH_F32 : ORTH_BF16>, g);
+            }
+            const OrthOperand o = w.x[0];
+            w.x[0] = w.x[1];
+            w.x[1] = o;
+        }
+        return e;
     }
     hipError_t run() {
+        if (z.tile == 0) return z.n == 32 ? thin<2>() : thin<4>();
         // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones: less work where X is
         // wide.  (With operands in one part the small ones would need two and cost more than that gains.)
         const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
         const bool pairs = F32 && half * mt + nt * mt * nt > 3 * half * nt;
         // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second
-        // parts are multiplied with each other too (up to 128 rows), and steps taken one by one (up to 64 rows; 2 x 24 x 24: 1.6e-6 of the norm
-        // in pairs without, 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
-        const int small = t.rows < t.cols ? t.rows : t.cols;
-        const bool two = z.n == 128 ? !(F32 && small <= 64) : pairs;
+        // parts are multiplied with each other too (up to 128 rows), and steps taken one by one (up to 64 rows, in thin(); 2 x 24 x 24: 1.6e-6 of the
+        // norm in pairs without, 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
+        const bool two = z.n == 128 || pairs;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
             const int n = two && k + 2 <= t.steps ? 2 : 1;
@@ -831,7 +1028,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.tall = tall;
         in.vec = ((uintptr_t)in.g & 15) == 0 && t.g_ld * size_in % 16 == 0 && (count == 1 || t.g_matrix * size_in % 16 == 0);
         in.x = w.x[0];
-        const dim3 blocks((tall ? z.n : z.m) / 64, (tall ? z.m : z.n) / 64, count);
+        in.block_rows = z.n / 16;
+        const dim3 blocks(((tall ? z.n : z.m) + 63) / 64, ((tall ? z.m : z.n) + 63) / 64, count);
         if (t.in_f32) {
             orth_squares_kernel<float><<<dim3(z.parts, count), kThreads, 0, st>>>(in);
             orth_blocks_kernel<float><<<blocks, kThreads, 0, st>>>(in);
