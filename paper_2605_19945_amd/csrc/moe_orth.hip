@@ -133,9 +133,8 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
 }
 
 // PA, PB: parts of A and B.  TB: B lies with the reduction along its rows (otherwise along its columns).  WM x WN wavefronts of FM x FN
-// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  LOLO: the product of the second parts too.  CIN, ROWS,
-// PARTS, OUT: what finish makes of the sums.
-template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, bool LOLO, int CIN, bool ROWS, int PARTS, int OUT>
+// fragments (16 x 16).  A stage is KS blocks of 32 of the reduction, STAGES of them in LDS.  CIN, ROWS, PARTS, OUT: what finish makes of the sums.
+template <int PA, int PB, bool TB, int WM, int WN, int FM, int FN, int KS, int STAGES, int CIN, bool ROWS, int PARTS, int OUT>
 __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
     constexpr int WAVES = WM * WN, FA = WM * FM, FB = WN * FN, FRAGS = KS * (FA * PA + FB * PB), LOADS = FRAGS / WAVES;
     static_assert(FA % WAVES == 0 && FB == 2 * WAVES, "a load's operand and block row do not depend on the wavefront");
@@ -221,13 +220,13 @@ __global__ __launch_bounds__(WM* WN * 64) void orth_product_kernel(OrthArgs g) {
                 for (int i = 0; i < FM; ++i) a[k][p][i] = *(const f16x8_t*)(at + (KS * p * FA + k * FA + wm * FM + i) * ORTH_BLOCK + at_row);
         }
     };
-    constexpr int PAIRS = PA + PB - 1 + (LOLO ? 1 : 0), LINES = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
+    constexpr int PAIRS = PA + PB - 1, LINES = KS * PAIRS * FM;  // rows of fragments that a stage's products come in
     auto multiply = [&](auto&& beside) {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
         orth_repeat<LINES>([&](auto row) {
             constexpr int k = decltype(row)::value / (PAIRS * FM), pair = decltype(row)::value / FM % PAIRS, i = decltype(row)::value % FM;
-            constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : pair - PB;  // hi hi, hi lo, lo hi, lo lo
+            constexpr int p = pair < PB ? 0 : 1, q = pair < PB ? pair : 0;  // hi hi, hi lo, lo hi
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k][q][j], a[k][p][i], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -423,6 +422,23 @@ template <int NF> __global__ __launch_bounds__(512) void orth_chain_kernel(OrthA
     put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
 }
 
+// Two neighbouring fragments' values as the pieces of a block that a lane stores, in two parts
+static __device__ inline void pieces_of(const f32x4_t& u, const f32x4_t& v, u32x4_t (&piece)[2]) {
+    uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        if (p == 1) {
+            const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
+            a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
+            a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
+            a[2] = pack_f16(v[0] - f16_lo(h[2]), v[1] - f16_hi(h[2]));
+            a[3] = pack_f16(v[2] - f16_lo(h[3]), v[3] - f16_hi(h[3]));
+        }
+        const auto x = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
+        piece[p] = u32x4_t{x[0], y[0], x[1], y[1]};
+    }
+}
+
 // ---- matrices of up to 64 rows ----
 // A wavefront takes 32 columns of X at a time, all its rows (16 NF): they are few enough that Q X and the new S = X X^T of these columns are formed
 // one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it.  MODE 0: S of X as it is;
@@ -500,21 +516,12 @@ template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void o
                 if constexpr (MODE == 2) {
                     finish<0, false, 0, OUT>(g, v[m][0], v[m][1], lane, matrix, m * 16, c * 32, false);
                 } else {
-                    f32x4_t u = v[m][0] * g.alpha, w = v[m][1] * g.alpha;
-                    uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
+                    u32x4_t piece[2];
+                    pieces_of(v[m][0] * g.alpha, v[m][1] * g.alpha, piece);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        if (p == 1) {
-                            const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
-                            a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
-                            a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
-                            a[2] = pack_f16(w[0] - f16_lo(h[2]), w[1] - f16_hi(h[2]));
-                            a[3] = pack_f16(w[2] - f16_lo(h[3]), w[3] - f16_hi(h[3]));
-                        }
-                        const auto y = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), z = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
-                        const u32x4_t piece = {y[0], z[0], y[1], z[1]};
-                        x[p][m] = __builtin_bit_cast(f16x8_t, piece);
-                        *(u32x4_t*)(g.c.part[p] + matrix * g.c.matrix + (int64_t)m * line + c * ORTH_BLOCK + orth_piece(i16, (q16 & 1) * 2 + (q16 >> 1)) * 16) = piece;
+                        x[p][m] = __builtin_bit_cast(f16x8_t, piece[p]);
+                        *(u32x4_t*)(g.c.part[p] + matrix * g.c.matrix + (int64_t)m * line + c * ORTH_BLOCK + orth_piece(i16, (q16 & 1) * 2 + (q16 >> 1)) * 16) = piece[p];
                     }
                 }
             }
@@ -539,6 +546,130 @@ template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void o
         __syncthreads();
         f32x4_t* part = (f32x4_t*)g.part + ((int64_t)matrix * gridDim.x + blockIdx.x) * (NF * NF * 64);
         for (int i = threadIdx.x; i < NF * NF * 64; i += 256) part[i] = all[i] + all[i + NF * NF * 64] + all[i + 2 * NF * NF * 64] + all[i + 3 * NF * NF * 64];
+    }
+}
+
+// ---- matrices of 65 to 128 rows ----
+// The same by four wavefronts together, 32 rows each: X's blocks and the new X's pieces go through LDS to all of them, and each keeps its rows of Q
+// and of S.  The next columns are asked for while these are multiplied.
+template <int MODE, int OUT> __global__ __launch_bounds__(256, 2) void orth_rows_kernel(OrthArgs g) {
+    constexpr int NF = 8, KB = 4, FM = 2, STAGE = 2 * NF * ORTH_BLOCK;
+    extern __shared__ __align__(1024) char lds[];  // two stages of X's blocks [part][row], the new X's [part][row]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, i16 = lane & 15, q16 = lane >> 4;
+    const int at_row = orth_piece(i16, q16) * 16;
+    const int t_row = 8 * (q16 & 1) + (i16 >> 2), t_g = (i16 & 3) >> 1;
+    const int at_turn = orth_piece(t_row, t_g) * 16 + (i16 & 1) * 8, at_next = orth_piece(t_row + 4, t_g) * 16 + (i16 & 1) * 8;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(orth_lds_addr(lds)), line = (uint32_t)g.b.blocks * ORTH_BLOCK;
+    u32x4_t desc[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) desc[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix, (uint32_t)g.b.matrix);
+    auto issue = [&](int c, int stage) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) orth_load(to + stage * STAGE + (p * NF + m * 4 + wave) * ORTH_BLOCK, lane * 16, desc[p], (m * 4 + wave) * line + c * ORTH_BLOCK);
+    };
+    f16x8_t q[2][FM][KB];
+    if constexpr (MODE > 0) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int k = 0; k < KB; ++k) q[p][m][k] = *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + ((wave * FM + m) * g.a.blocks + k) * ORTH_BLOCK + at_row);
+    }
+    f32x4_t s[FM][NF];
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < NF; ++n) s[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    char* fresh = lds + 2 * STAGE;
+    int stage = 0;
+    if (MODE > 0 && (int)blockIdx.x < g.steps) issue(blockIdx.x, 0);
+    for (int c = blockIdx.x; c < g.steps; c += gridDim.x) {
+        f16x8_t x[2][NF];
+        if constexpr (MODE == 0) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int m = 0; m < NF; ++m) x[p][m] = *(const f16x8_t*)(g.b.part[p] + matrix * g.b.matrix + (int64_t)m * line + c * ORTH_BLOCK + at_row);
+        } else {
+            orth_wait<0>();
+            orth_barrier();  // of every wavefront's; and all are done with the columns before
+            if (c + (int)gridDim.x < g.steps) issue(c + gridDim.x, stage ^ 1);
+            f32x4_t v[FM][2];
+#pragma unroll
+            for (int m = 0; m < FM; ++m) v[m][0] = v[m][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                f16x8_t b[2][2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        typedef short s16x4_t __attribute__((ext_vector_type(4)));
+                        typedef __attribute__((address_space(3))) s16x4_t lds4;
+                        const char* block = lds + stage * STAGE + (p * NF + 2 * k + (q16 >> 1)) * ORTH_BLOCK + j * 512;
+                        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_turn)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_next));
+                        b[p][j] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+                orth_repeat<4>([&](auto pair) {
+                    constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
+#pragma unroll
+                    for (int m = 0; m < FM; ++m)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) v[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][j], q[p][m][k], v[m][j], 0, 0, 0);
+                });
+            }
+            stage ^= 1;
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                const int row = wave * FM + m;
+                if constexpr (MODE == 2) {
+                    finish<0, false, 0, OUT>(g, v[m][0], v[m][1], lane, matrix, row * 16, c * 32, false);
+                } else {
+                    u32x4_t piece[2];
+                    pieces_of(v[m][0] * g.alpha, v[m][1] * g.alpha, piece);
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        *(u32x4_t*)(g.c.part[p] + matrix * g.c.matrix + (int64_t)row * line + c * ORTH_BLOCK + orth_piece(i16, (q16 & 1) * 2 + (q16 >> 1)) * 16) = piece[p];
+                        *(u32x4_t*)(fresh + (p * NF + row) * ORTH_BLOCK + lane * 16) = piece[p];
+                    }
+                }
+            }
+            if constexpr (MODE == 1) {
+                orth_barrier();
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int m = 0; m < NF; ++m) x[p][m] = *(const f16x8_t*)(fresh + (p * NF + m) * ORTH_BLOCK + lane * 16);
+            }
+        }
+        if constexpr (MODE < 2) {
+            f16x8_t own[2][FM];  // this wavefront's rows of x
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) {
+                    own[p][m] = x[p][m];
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) own[p][m] = wave == w ? x[p][w * FM + m] : own[p][m];
+                }
+            orth_repeat<4>([&](auto pair) {
+                constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
+#pragma unroll
+                for (int m = 0; m < FM; ++m)
+#pragma unroll
+                    for (int n = 0; n < NF; ++n) s[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[r][n], own[p][m], s[m][n], 0, 0, 0);
+            });
+        }
+    }
+    if constexpr (MODE < 2) {
+        f32x4_t* part = (f32x4_t*)g.part + ((int64_t)matrix * gridDim.x + blockIdx.x) * (NF * NF * 64) + lane;
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < NF; ++n) part[((wave * FM + m) * NF + n) * 64] = s[m][n];
     }
 }
 
@@ -687,7 +818,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
 // ---- plan ----
 struct Size {
     int n, m;        // of X, padded
-    int tile;        // 256 or 128; 0: all rows and 32 columns at a time (up to 64 rows)
+    int tile;        // 256 or 128; 0: all rows and 32 columns at a time (up to 128 rows)
     int parts;       // of the squares
     // Blocks along the rows of X and of S: an odd number, so that the block rows that are loaded together begin in different places of the memory
     // channels' interleaving (a power of two put them all on the same few).
@@ -724,8 +855,8 @@ double step_time(int E, int n, int m, int tile) {
 Size size_of_matrix(int E, int rows, int cols) {
     Size z;
     const int n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    z.tile = n <= 64 ? 0 : n > 128 && step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
-    z.n = z.tile == 0 ? (n <= 32 ? 32 : 64) : (n + z.tile - 1) / z.tile * z.tile;
+    z.tile = n <= 128 ? 0 : step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
+    z.n = z.tile == 0 ? (n <= 32 ? 32 : n <= 64 ? 64 : 128) : (n + z.tile - 1) / z.tile * z.tile;
     z.m = z.tile == 0 ? (m + 63) / 64 * 64 : (m + z.tile - 1) / z.tile * z.tile;
     z.xb = z.m / 32 + 1, z.sb = z.n / 32 + 1;
     z.x = (int64_t)z.n / 16 * z.xb * ORTH_BLOCK;
@@ -738,19 +869,14 @@ Size size_of_matrix(int E, int rows, int cols) {
 
 // X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares
 int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096; }
-// The same for S of matrices of one tile, whose sums go on in one launch in any case
-int chain_splits(int count, int steps) {
-    const int room = 2 * kUnits / count, s = room < steps / 4 ? room : steps / 4;
-    return s > 1 ? s : 1;
-}
-// Workgroups that share the columns of a matrix of up to 64 rows, of which each leaves sums
-int thin_groups(int count, int m) {
-    const int want = (m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1;
-    return want < room ? want : room;
+// Workgroups that share the columns of a matrix of up to 128 rows, of which each leaves sums; fewer of the tallest, whose sums are larger
+int thin_groups(int count, const Size& z) {
+    const int want = z.n == 128 ? z.m / 32 : (z.m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1, most = z.n == 128 && room > 128 ? 128 : room;
+    return want < most ? want : most;
 }
 // Sums of the cut reductions of `count` matrices
 int64_t part_bytes(int count, const Size& z) {
-    if (z.tile == 0) return (int64_t)count * thin_groups(count, z.m) * z.n * z.n * 4;
+    if (z.tile == 0) return (int64_t)count * thin_groups(count, z) * z.n * z.n * 4;
     const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
     int64_t slots = 0;
     auto product = [&](int64_t tiles, int64_t steps) {
@@ -760,13 +886,12 @@ int64_t part_bytes(int count, const Size& z) {
     product(half, z.m / 32);
     product(half, z.n / 32);
     product(all, z.n / 32);
-    if (z.n == 128 && slots < half * chain_splits(count, z.m / 32)) slots = half * chain_splits(count, z.m / 32);
     return slots * z.tile * z.tile * 4;
 }
 // ... where there are any, at most
 constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 
-template <int PA, int PB, bool TB, bool LOLO, int CIN, bool ROWS, int PARTS, int OUT> hipError_t product(OrthArgs g, int tile, hipStream_t st, bool sums = true) {
+template <int PA, int PB, bool TB, int CIN, bool ROWS, int PARTS, int OUT> hipError_t product(OrthArgs g, int tile, hipStream_t st) {
     constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : 2;
     const int64_t tiles = (int64_t)g.tiles * g.matrices;
     if (g.splits == 0) {
@@ -782,9 +907,9 @@ template <int PA, int PB, bool TB, bool LOLO, int CIN, bool ROWS, int PARTS, int
         return hipGetLastError();
     };
     hipError_t e;
-    if (!LOLO && tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, false, CIN, ROWS, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
-    else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, LOLO, CIN, ROWS, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
-    if (e != hipSuccess || cut == 0 || !sums) return e;
+    if (tile == 256) e = run(orth_product_kernel<PA, PB, TB, 2, 4, 8, 4, KS, 2, CIN, ROWS, PARTS, OUT>, 16 * PLANES * KS * 2 * ORTH_BLOCK, 512);
+    else e = run(orth_product_kernel<PA, PB, TB, 2, 2, 4, 4, 1, STAGES, CIN, ROWS, PARTS, OUT>, 8 * PLANES * STAGES * ORTH_BLOCK, 256);
+    if (e != hipSuccess || cut == 0) return e;
     if (tile == 256) orth_sums_kernel<16, CIN, ROWS, PARTS, OUT><<<cut * 32, 256, 0, st>>>(g);
     else orth_sums_kernel<8, CIN, ROWS, PARTS, OUT><<<cut * 8, 256, 0, st>>>(g);
     return hipGetLastError();
@@ -840,7 +965,7 @@ template <bool F32> struct Steps {
         g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
     }
     // X = q X, into the other buffer or to the caller; where q has one part, X = (a + rest) X + q X of X's first part
-    template <bool TWO, bool LOLO = false> hipError_t apply(const OrthOperand& q, float a, bool last) {
+    template <bool TWO> hipError_t apply(const OrthOperand& q, float a, bool last) {
         constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 2;
         OrthArgs g = {};
         g.matrices = count;
@@ -856,10 +981,10 @@ template <bool F32> struct Steps {
         g.part = w.part;
         hipError_t e;
         if (!last) {
-            e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 2, ORTH_BLOCKS>(g, z.tile, st);
+            e = product<PARTS, PARTS, true, CIN, !TWO, 2, ORTH_BLOCKS>(g, z.tile, st);
         } else {
             to_caller(g);
-            e = product<PARTS, PARTS, true, LOLO, CIN, !TWO, 0, F32 ? ORTH_F32 : ORTH_BF16>(g, z.tile, st);
+            e = product<PARTS, PARTS, true, CIN, !TWO, 0, F32 ? ORTH_F32 : ORTH_BF16>(g, z.tile, st);
         }
         const OrthOperand o = w.x[0];
         w.x[0] = w.x[1];
@@ -869,7 +994,7 @@ template <bool F32> struct Steps {
     // S = X X^T
     hipError_t gram() const {
         constexpr int PARTS = F32 ? 2 : 1;
-        return product<PARTS, PARTS, false, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
+        return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
     }
     // to = a I + b S + c S S; in one part without a I, for which it has too few digits, and with what it has too few for on its diagonal aside
     hipError_t polynomial(const OrthOperand& to, const float* abc) const {
@@ -879,11 +1004,11 @@ template <bool F32> struct Steps {
         g.beta = abc[1] * Q_SCALE / S_SCALE;
         g.diagonal = F32 ? abc[0] * Q_SCALE : 0.f;
         g.rest = F32 ? nullptr : w.rest;
-        return product<PARTS, PARTS, false, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
+        return product<PARTS, PARTS, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
     // to = a q, of matrices that commute
     hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to) const {
-        return product<2, 2, false, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
+        return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
     }
     hipError_t one_step(const float* abc, bool last) {
         hipError_t e = gram();
@@ -901,15 +1026,7 @@ template <bool F32> struct Steps {
         if (e == hipSuccess) e = apply<true>(w.s, 0.f, last);
         return e;
     }
-    // One or two steps of matrices of one tile: all between S and the last product in one launch
-    hipError_t chain(const float* abc, int n, bool last) {
-        OrthArgs g = square(w.x[0], w.x[0], w.q, 0.f);
-        g.splits = chain_splits(count, g.steps);  // (whole: none, so the sums go to memory in any case)
-        const hipError_t e = product<2, 2, false, true, 0, false, 2, ORTH_SQUARE>(g, z.tile, st, false);
-        if (e != hipSuccess) return e;
-        const hipError_t f = link<8>(g, g.splits, abc, n);
-        return f != hipSuccess ? f : apply<true, true>(w.q, 0.f, last);
-    }
+    // One or two steps: all between S and the last product in one launch
     template <int NF> hipError_t link(const OrthArgs& g, int splits, const float* abc, int n) {
         int ranges = splits;
         if (ranges > 8) {
@@ -922,11 +1039,15 @@ template <bool F32> struct Steps {
         orth_chain_kernel<NF><<<count, 512, bytes, st>>>(g, splits, ranges, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
         return hipGetLastError();
     }
-    // Matrices of up to 64 rows (16 NF padded)
+    // Matrices of up to 128 rows (16 NF padded)
+    template <int NF, int MODE, int OUT> static auto step_kernel() {
+        if constexpr (NF == 8) return orth_rows_kernel<MODE, OUT>;
+        else return orth_thin_kernel<NF, MODE, OUT>;
+    }
     template <int NF> hipError_t thin() {
-        const int groups = thin_groups(count, z.m);
+        const int groups = thin_groups(count, z);
         auto launch = [&](auto kernel, const OrthArgs& g) {
-            const int bytes = 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF) * ORTH_BLOCK;
+            const int bytes = (NF == 8 ? 6 * NF : 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF)) * ORTH_BLOCK;
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
             if (e != hipSuccess) return e;
             kernel<<<dim3(groups, count), 256, bytes, st>>>(g);
@@ -937,9 +1058,12 @@ template <bool F32> struct Steps {
         g.a = w.q, g.b = w.x[0];
         g.steps = z.m / 32;
         g.part = w.part;
-        hipError_t e = launch(orth_thin_kernel<NF, 0, ORTH_BLOCKS>, g);
+        hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS>(), g);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = !F32 && k + 2 <= t.steps ? 2 : 1;
+            // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second parts
+            // are multiplied with each other too, and, up to 64 rows, steps taken one by one (2 x 24 x 24: 1.6e-6 of the norm in pairs without,
+            // 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
+            const int n = (!F32 || NF == 8) && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
             OrthArgs l = {};
@@ -950,10 +1074,10 @@ template <bool F32> struct Steps {
             g.b = w.x[0], g.c = w.x[1];
             g.alpha = 1.f / Q_SCALE;
             if (k < t.steps) {
-                e = launch(orth_thin_kernel<NF, 1, ORTH_BLOCKS>, g);
+                e = launch(step_kernel<NF, 1, ORTH_BLOCKS>(), g);
             } else {
                 to_caller(g);
-                e = launch(orth_thin_kernel<NF, 2, F32 ? ORTH_F32 : ORTH_BF16>, g);
+                e = launch(step_kernel<NF, 2, F32 ? ORTH_F32 : ORTH_BF16>(), g);
             }
             const OrthOperand o = w.x[0];
             w.x[0] = w.x[1];
@@ -962,23 +1086,18 @@ template <bool F32> struct Steps {
         return e;
     }
     hipError_t run() {
-        if (z.tile == 0) return z.n == 32 ? thin<2>() : thin<4>();
+        if (z.tile == 0) return z.n == 32 ? thin<2>() : z.n == 64 ? thin<4>() : thin<8>();
         // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones: less work where X is
         // wide.  (With operands in one part the small ones would need two and cost more than that gains.)
         const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
         const bool pairs = F32 && half * mt + nt * mt * nt > 3 * half * nt;
-        // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second
-        // parts are multiplied with each other too (up to 128 rows), and steps taken one by one (up to 64 rows, in thin(); 2 x 24 x 24: 1.6e-6 of the
-        // norm in pairs without, 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
-        const bool two = z.n == 128 || pairs;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = two && k + 2 <= t.steps ? 2 : 1;
+            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
             const bool last = k == t.steps;
-            if (z.n == 128) e = chain(abc, n, last);
-            else if constexpr (F32) e = n == 2 ? two_steps(abc, last) : one_step(abc, last);
+            if constexpr (F32) e = n == 2 ? two_steps(abc, last) : one_step(abc, last);
             else e = one_step(abc, last);
         }
         return e;
