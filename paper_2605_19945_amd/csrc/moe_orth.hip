@@ -331,95 +331,81 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 }
 
 // ---- all between S and the next product with X, for matrices of up to 128 rows ----
-// S's ranges -> a I + b S + c S S, or of two steps the product of both.  One workgroup a matrix, everything in LDS: two matrices of 16 NF rows in
-// two parts, in blocks; a wavefront has a row of fragments.
-template <int NF> __global__ __launch_bounds__(512) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
+// S's ranges -> a I + b S + c S S, or of two steps the product of both.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
+// of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  LOLO: the product of the second parts too.
+// One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
+// latencies are what it takes (8 matrices of 128 rows, two steps: unrolled with all its products 54 us; only the columns from the diagonal on,
+// half the products, but branches, 28).
+template <int NF, bool LOLO> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
     extern __shared__ __align__(1024) char lds[];
-    constexpr int KB = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
+    constexpr int KB = NF / 2, FN = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
     char *s = lds, *q = lds + 2 * PLANE;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.x;
-    const bool on = wave < NF;
-    const int at_row = orth_piece(lane & 15, lane >> 4) * 16;
-    f32x4_t v[NF];
-    // where a lane's 4 values of a fragment lie: columns 16 n + 4 (lane / 16) + 0..3 of row 16 wave + lane % 16
-    auto at = [&](int n, int blocks) { return (wave * blocks + (n >> 1)) * ORTH_BLOCK + orth_piece(lane & 15, (n & 1) * 2 + (lane >> 5)) * 16 + (lane >> 4 & 1) * 8; };
-    auto put = [&](char* to, int64_t plane, int blocks) {
-        if (!on) return;
+    const int row0 = wave >> 1 << 1, col0 = (wave & 1) * FN, i = lane & 15, q4 = lane >> 4;
+    const int at_row = orth_piece(i, q4) * 16;
+    f32x4_t v[2][FN];
+    auto each = [&](auto&& f) {
 #pragma unroll
-        for (int n = 0; n < NF; ++n) {
-            const f32x4_t& x = v[n];
-            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
-            *(u32x2_t*)(to + at(n, blocks)) = u32x2_t{h0, h1};
-            *(u32x2_t*)(to + plane + at(n, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
-        }
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n) f(m, n);
     };
-    auto multiply = [&](const char* x, const char* y, float scale) {  // v = scale x y, y symmetric
-        if (!on) return;
-#pragma unroll
-        for (int n = 0; n < NF; ++n) v[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // a lane's 4 values of a fragment: columns 16 n + 4 (lane / 16) + 0..3 of row 16 m + lane % 16
+    auto at = [&](int m, int n, int blocks) { return ((row0 + m) * blocks + ((col0 + n) >> 1)) * ORTH_BLOCK + orth_piece(i, ((col0 + n) & 1) * 2 + (q4 >> 1)) * 16 + (q4 & 1) * 8; };
+    auto put = [&](char* to, int64_t plane, int blocks) {
+        each([&](int m, int n) {
+            const f32x4_t& x = v[m][n];
+            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
+            *(u32x2_t*)(to + at(m, n, blocks)) = u32x2_t{h0, h1};
+            *(u32x2_t*)(to + plane + at(m, n, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+        });
+    };
+
+    const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * apart * (NF * NF * 64) + lane;  // (apart: ranges between matrices)
+    each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+#pragma unroll 4
+    for (int r = 0; r < splits; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + col0 + n) * 64]; });
+    each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
+    put(s, PLANE, KB);
+    __syncthreads();
+    const int last = two ? 4 : 0;
+#pragma unroll 1
+    for (int op = 0; op <= last; ++op) {
+        const bool sum = op == 0 || op == 3;  // of s: a I + b s + c s s; the others: s q
+        const char* y = sum ? s : q;
+        each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
-            f16x8_t a[2], b[2][NF];
+            f16x8_t a[2][2], b[2][FN];
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                a[p] = *(const f16x8_t*)(x + p * PLANE + (wave * KB + k) * ORTH_BLOCK + at_row);
 #pragma unroll
-                for (int n = 0; n < NF; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + (n * KB + k) * ORTH_BLOCK + at_row);
+                for (int m = 0; m < 2; ++m) a[p][m] = *(const f16x8_t*)(s + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
+#pragma unroll
+                for (int n = 0; n < FN; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + ((col0 + n) * KB + k) * ORTH_BLOCK + at_row);
             }
-            orth_repeat<4>([&](auto pair) {
-                constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
-#pragma unroll
-                for (int n = 0; n < NF; ++n) v[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p], v[n], 0, 0, 0);
+            orth_repeat<LOLO ? 4 : 3>([&](auto parts) {
+                constexpr int p = decltype(parts)::value >> 1, r = decltype(parts)::value & 1;
+                each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p][m], v[m][n], 0, 0, 0); });
             });
         }
-#pragma unroll
-        for (int n = 0; n < NF; ++n) v[n] *= scale;
-    };
-    auto polynomial = [&](float a, float b, float c) {  // v = a I + b s + c s s
-        multiply(s, s, c * (Q_SCALE / (S_SCALE * S_SCALE)));
-        if (!on) return;
-#pragma unroll
-        for (int n = 0; n < NF; ++n) {
-            const u32x2_t hi = *(const u32x2_t*)(s + at(n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(n, KB));
+        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : 1.f / Q_SCALE;
+        const float ca = !sum ? 0.f : (op == 0 ? a1 : a2) * Q_SCALE, cb = !sum ? 0.f : (op == 0 ? b1 : b2) * (Q_SCALE / S_SCALE);
+        each([&](int m, int n) {
+            const u32x2_t hi = *(const u32x2_t*)(s + at(m, n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(m, n, KB));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float x = j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]);
-                v[n][j] = fmaf(b * (Q_SCALE / S_SCALE), x, v[n][j]) + (wave == n && 4 * (lane >> 4) + j == (lane & 15) ? a * Q_SCALE : 0.f);
+                v[m][n][j] *= scale;
+                if (sum) v[m][n][j] = fmaf(cb, x, v[m][n][j]) + (row0 + m == col0 + n && 4 * q4 + j == i ? ca : 0.f);
             }
-        }
-    };
-
-    if (on) {
-        const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * apart * (NF * NF * 64) + wave * NF * 64 + lane;  // (apart: ranges between matrices)
-#pragma unroll
-        for (int n = 0; n < NF; ++n) v[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int i = 0; i < splits; ++i) {
-#pragma unroll
-            for (int n = 0; n < NF; ++n) v[n] += part[((int64_t)i * NF * NF + n) * 64];
-        }
-#pragma unroll
-        for (int n = 0; n < NF; ++n) v[n] *= S_SCALE / (X_SCALE * X_SCALE);
+        });
+        __syncthreads();
+        // op 1 and 2: s = q s q = (q x) (q x)^T: they commute
+        if (op == last) put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
+        else put(op == 0 ? q : s, PLANE, KB);
+        __syncthreads();
     }
-    put(s, PLANE, KB);
-    __syncthreads();
-    polynomial(a1, b1, c1);
-    if (two) {
-        put(q, PLANE, KB);
-        __syncthreads();
-        for (int i = 0; i < 2; ++i) {  // s = q s q = (q x) (q x)^T: they commute
-            multiply(s, q, 1.f / Q_SCALE);
-            __syncthreads();
-            put(s, PLANE, KB);
-            __syncthreads();
-        }
-        polynomial(a2, b2, c2);
-        __syncthreads();
-        put(s, PLANE, KB);
-        __syncthreads();
-        multiply(s, q, 1.f / Q_SCALE);
-    }
-    put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
 }
 
 // Two neighbouring fragments' values as the pieces of a block that a lane stores, in two parts
@@ -871,7 +857,7 @@ Size size_of_matrix(int E, int rows, int cols) {
 int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096; }
 // Workgroups that share the columns of a matrix of up to 128 rows, of which each leaves sums; fewer of the tallest, whose sums are larger
 int thin_groups(int count, const Size& z) {
-    const int want = z.n == 128 ? z.m / 32 : (z.m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1, most = z.n == 128 && room > 128 ? 128 : room;
+    const int want = z.n == 128 ? (z.m / 32 + 1) / 2 : (z.m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1, most = z.n == 128 && room > 128 ? 128 : room;
     return want < most ? want : most;
 }
 // Sums of the cut reductions of `count` matrices
@@ -1034,9 +1020,9 @@ template <bool F32> struct Steps {
             ranges = 1;
         }
         constexpr int bytes = 4 * NF * (NF / 2) * ORTH_BLOCK;
-        const hipError_t e = hipFuncSetAttribute((const void*)orth_chain_kernel<NF>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)orth_chain_kernel<NF, (NF < 8)>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        orth_chain_kernel<NF><<<count, 512, bytes, st>>>(g, splits, ranges, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
+        orth_chain_kernel<NF, (NF < 8)><<<count, NF * 64, bytes, st>>>(g, splits, ranges, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
         return hipGetLastError();
     }
     // Matrices of up to 128 rows (16 NF padded)
