@@ -37,6 +37,10 @@ struct OrthArgs {
     float* part;
     int mt, nt;            // tiles of a matrix (symmetric: mt == nt, those on and above the diagonal)
     int tiles, matrices;   // tiles of a matrix that are computed
+    // of matrices of up to 128 rows: S in `ranges` sums, `apart` of them a matrix, of which the coefficients give Q
+    const float* sums;
+    int ranges, apart;
+    float abc[3];
     // the last product: results in the caller's rows
     void* out;
     int64_t out_matrix, out_ld;  // values from one matrix, one row to the next

@@ -330,13 +330,14 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
     *p = v;
 }
 
-// ---- all between S and the next product with X, for matrices of up to 128 rows ----
-// S's ranges -> a I + b S + c S S, or of two steps the product of both.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
-// of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  LOLO: the product of the second parts too.
+// ---- between S and the next product with X, for matrices of up to 128 rows ----
+// Of two steps' Q = a I + b S + c S S the product, from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
+// of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  All four products
+// of the parts are formed: small matrices have few values to average over (8 x 128 x 256 in fp32: 1.7e-6 of the norm with three, 1.35e-6 with four).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
 // latencies are what it takes (8 matrices of 128 rows, two steps: unrolled with all its products 54 us; only the columns from the diagonal on,
 // half the products, but branches, 28).
-template <int NF, bool LOLO> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, int two, float a2, float b2, float c2) {
+template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2) {
     extern __shared__ __align__(1024) char lds[];
     constexpr int KB = NF / 2, FN = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
     char *s = lds, *q = lds + 2 * PLANE;
@@ -368,38 +369,47 @@ template <int NF, bool LOLO> __global__ __launch_bounds__(NF * 64) void orth_cha
     each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
     put(s, PLANE, KB);
     __syncthreads();
-    const int last = two ? 4 : 0;
+    constexpr int last = 4;
 #pragma unroll 1
     for (int op = 0; op <= last; ++op) {
         const bool sum = op == 0 || op == 3;  // of s: a I + b s + c s s; the others: s q
         const char* y = sum ? s : q;
         each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
-#pragma unroll
-        for (int k = 0; k < KB; ++k) {
-            f16x8_t a[2][2], b[2][FN];
+        f16x8_t a[2][2][2], b[2][2][FN];  // the next block's are read while this one's are multiplied
+        auto read = [&](int k) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) a[p][m] = *(const f16x8_t*)(s + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
+                for (int m = 0; m < 2; ++m) a[k & 1][p][m] = *(const f16x8_t*)(s + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
 #pragma unroll
-                for (int n = 0; n < FN; ++n) b[p][n] = *(const f16x8_t*)(y + p * PLANE + ((col0 + n) * KB + k) * ORTH_BLOCK + at_row);
+                for (int n = 0; n < FN; ++n) b[k & 1][p][n] = *(const f16x8_t*)(y + p * PLANE + ((col0 + n) * KB + k) * ORTH_BLOCK + at_row);
             }
-            orth_repeat<LOLO ? 4 : 3>([&](auto parts) {
+        };
+        read(0);
+        orth_repeat<KB>([&](auto block) {
+            constexpr int k = decltype(block)::value;
+            if constexpr (k + 1 < KB) read(k + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            orth_repeat<4>([&](auto parts) {
                 constexpr int p = decltype(parts)::value >> 1, r = decltype(parts)::value & 1;
-                each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p][m], v[m][n], 0, 0, 0); });
+                each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k & 1][r][n], a[k & 1][p][m], v[m][n], 0, 0, 0); });
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : 1.f / Q_SCALE;
+        each([&](int m, int n) { v[m][n] *= scale; });
+        if (sum) {
+            const float ca = (op == 0 ? a1 : a2) * Q_SCALE, cb = (op == 0 ? b1 : b2) * (Q_SCALE / S_SCALE);
+            each([&](int m, int n) {
+                const u32x2_t hi = *(const u32x2_t*)(s + at(m, n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(m, n, KB));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[m][n][j] = fmaf(cb, j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]), v[m][n][j]);
+                if (row0 + m == col0 + n) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[m][n][j] += 4 * q4 + j == i ? ca : 0.f;
+                }
             });
         }
-        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : 1.f / Q_SCALE;
-        const float ca = !sum ? 0.f : (op == 0 ? a1 : a2) * Q_SCALE, cb = !sum ? 0.f : (op == 0 ? b1 : b2) * (Q_SCALE / S_SCALE);
-        each([&](int m, int n) {
-            const u32x2_t hi = *(const u32x2_t*)(s + at(m, n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(m, n, KB));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]);
-                v[m][n][j] *= scale;
-                if (sum) v[m][n][j] = fmaf(cb, x, v[m][n][j]) + (row0 + m == col0 + n && 4 * q4 + j == i ? ca : 0.f);
-            }
-        });
         __syncthreads();
         // op 1 and 2: s = q s q = (q x) (q x)^T: they commute
         if (op == last) put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
@@ -425,14 +435,75 @@ static __device__ inline void pieces_of(const f32x4_t& u, const f32x4_t& v, u32x
     }
 }
 
+// Q = a I + b S + c S S in LDS, in two parts, in blocks, from S's ranges, by four wavefronts: each workgroup that multiplies with Q forms it by itself,
+// which costs less than a launch in between.  NF / 4 rows of fragments a wavefront (one, of fewer wavefronts, where there are two).
+template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* s, int matrix) {
+    constexpr int KB = NF / 2, PLANE = NF * KB * ORTH_BLOCK, FM = NF == 8 ? 2 : 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q4 = lane >> 4;
+    const bool on = wave * FM < NF;
+    const int row0 = on ? wave * FM : 0, at_row = orth_piece(i, q4) * 16;
+    f32x4_t v[FM][NF];
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < NF; ++n) f(m, n);
+    };
+    auto at = [&](int m, int n) { return ((row0 + m) * KB + (n >> 1)) * ORTH_BLOCK + orth_piece(i, (n & 1) * 2 + (q4 >> 1)) * 16 + (q4 & 1) * 8; };
+    auto put = [&] {
+        each([&](int m, int n) {
+            const f32x4_t& x = v[m][n];
+            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
+            *(u32x2_t*)(s + at(m, n)) = u32x2_t{h0, h1};
+            *(u32x2_t*)(s + PLANE + at(m, n)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+        });
+    };
+    const f32x4_t* part = (const f32x4_t*)g.sums + (int64_t)matrix * g.apart * (NF * NF * 64) + lane;
+    each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+#pragma unroll 2
+    for (int r = 0; r < g.ranges; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + n) * 64]; });
+    each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
+    if (on) put();
+    __syncthreads();
+    each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+        f16x8_t a[2][FM], b[2][NF];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+#pragma unroll
+            for (int m = 0; m < FM; ++m) a[p][m] = *(const f16x8_t*)(s + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
+#pragma unroll
+            for (int n = 0; n < NF; ++n) b[p][n] = *(const f16x8_t*)(s + p * PLANE + (n * KB + k) * ORTH_BLOCK + at_row);
+        }
+        orth_repeat<4>([&](auto parts) {
+            constexpr int p = decltype(parts)::value >> 1, r = decltype(parts)::value & 1;
+            each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p][m], v[m][n], 0, 0, 0); });
+        });
+    }
+    const float scale = g.abc[2] * (Q_SCALE / (S_SCALE * S_SCALE)), ca = g.abc[0] * Q_SCALE, cb = g.abc[1] * (Q_SCALE / S_SCALE);
+    each([&](int m, int n) {
+        const u32x2_t hi = *(const u32x2_t*)(s + at(m, n)), lo = *(const u32x2_t*)(s + PLANE + at(m, n));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[m][n][j] = fmaf(cb, j & 1 ? f16_hi(hi[j >> 1]) + f16_hi(lo[j >> 1]) : f16_lo(hi[j >> 1]) + f16_lo(lo[j >> 1]), v[m][n][j] * scale);
+        if (row0 + m == n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[m][n][j] += 4 * q4 + j == i ? ca : 0.f;
+        }
+    });
+    __syncthreads();
+    if (on) put();
+    __syncthreads();
+}
+
 // ---- matrices of up to 64 rows ----
 // A wavefront takes 32 columns of X at a time, all its rows (16 NF): they are few enough that Q X and the new S = X X^T of these columns are formed
 // one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it.  MODE 0: S of X as it is;
-// 1: X = Q X and its S; 2: X = Q X to the caller.
+// 1: X = Q X and its S; 2: X = Q X to the caller.  OWN: Q is formed here, from the sums that the launch before has left.
 // The results' lanes have the columns 4 q + 0..3 and 16 + 4 q + 0..3 of row i; after the change of halves that the stores want, lane (i, q) has 8
 // neighbouring columns of row i, in another order of q than an operand's lanes.  S sums over the columns, so any order will do that both of
 // its operands have: the results are operands as they are.
-template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void orth_thin_kernel(OrthArgs g) {
+template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, 2) void orth_thin_kernel(OrthArgs g) {
     constexpr int KB = NF / 2;
     extern __shared__ __align__(1024) char lds[];  // a wavefront's blocks, NF of each part; then the wavefronts' S
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, i16 = lane & 15, q16 = lane >> 4;
@@ -447,12 +518,16 @@ template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void o
     for (int p = 0; p < 2; ++p) desc[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix, (uint32_t)g.b.matrix);
     f16x8_t q[2][NF][KB];
     if constexpr (MODE > 0) {
+        char* own = lds + 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF) * ORTH_BLOCK;
+        if constexpr (OWN) orth_q<NF>(g, own, matrix);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int m = 0; m < NF; ++m)
 #pragma unroll
-                for (int k = 0; k < KB; ++k) q[p][m][k] = *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + (m * g.a.blocks + k) * ORTH_BLOCK + at_row);
+                for (int k = 0; k < KB; ++k)
+                    q[p][m][k] = OWN ? *(const f16x8_t*)(own + (p * NF * KB + m * KB + k) * ORTH_BLOCK + at_row)
+                                     : *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + (m * g.a.blocks + k) * ORTH_BLOCK + at_row);
     }
     f32x4_t s[NF][NF];
 #pragma unroll
@@ -538,7 +613,7 @@ template <int NF, int MODE, int OUT> __global__ __launch_bounds__(256, 2) void o
 // ---- matrices of 65 to 128 rows ----
 // The same by four wavefronts together, 32 rows each: X's blocks and the new X's pieces go through LDS to all of them, and each keeps its rows of Q
 // and of S.  The next columns are asked for while these are multiplied.
-template <int MODE, int OUT> __global__ __launch_bounds__(256, 2) void orth_rows_kernel(OrthArgs g) {
+template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1 : 2) void orth_rows_kernel(OrthArgs g) {
     constexpr int NF = 8, KB = 4, FM = 2, STAGE = 2 * NF * ORTH_BLOCK;
     extern __shared__ __align__(1024) char lds[];  // two stages of X's blocks [part][row], the new X's [part][row]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, i16 = lane & 15, q16 = lane >> 4;
@@ -555,23 +630,27 @@ template <int MODE, int OUT> __global__ __launch_bounds__(256, 2) void orth_rows
 #pragma unroll
             for (int m = 0; m < 2; ++m) orth_load(to + stage * STAGE + (p * NF + m * 4 + wave) * ORTH_BLOCK, lane * 16, desc[p], (m * 4 + wave) * line + c * ORTH_BLOCK);
     };
+    char* fresh = lds + 2 * STAGE;
+    int stage = 0;
+    if (MODE > 0 && (int)blockIdx.x < g.steps) issue(blockIdx.x, 0);
     f16x8_t q[2][FM][KB];
     if constexpr (MODE > 0) {
+        char* own = lds + 3 * STAGE;
+        if constexpr (OWN) orth_q<NF>(g, own, matrix);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int m = 0; m < FM; ++m)
 #pragma unroll
-                for (int k = 0; k < KB; ++k) q[p][m][k] = *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + ((wave * FM + m) * g.a.blocks + k) * ORTH_BLOCK + at_row);
+                for (int k = 0; k < KB; ++k)
+                    q[p][m][k] = OWN ? *(const f16x8_t*)(own + (p * NF * KB + (wave * FM + m) * KB + k) * ORTH_BLOCK + at_row)
+                                     : *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + ((wave * FM + m) * g.a.blocks + k) * ORTH_BLOCK + at_row);
     }
     f32x4_t s[FM][NF];
 #pragma unroll
     for (int m = 0; m < FM; ++m)
 #pragma unroll
         for (int n = 0; n < NF; ++n) s[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    char* fresh = lds + 2 * STAGE;
-    int stage = 0;
-    if (MODE > 0 && (int)blockIdx.x < g.steps) issue(blockIdx.x, 0);
     for (int c = blockIdx.x; c < g.steps; c += gridDim.x) {
         f16x8_t x[2][NF];
         if constexpr (MODE == 0) {
@@ -862,7 +941,7 @@ int thin_groups(int count, const Size& z) {
 }
 // Sums of the cut reductions of `count` matrices
 int64_t part_bytes(int count, const Size& z) {
-    if (z.tile == 0) return (int64_t)count * thin_groups(count, z) * z.n * z.n * 4;
+    if (z.tile == 0) return (int64_t)count * thin_groups(count, z) * z.n * z.n * 4 * 2;
     const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2 * count, all = nt * mt * count;
     int64_t slots = 0;
     auto product = [&](int64_t tiles, int64_t steps) {
@@ -1012,28 +1091,27 @@ template <bool F32> struct Steps {
         if (e == hipSuccess) e = apply<true>(w.s, 0.f, last);
         return e;
     }
-    // One or two steps: all between S and the last product in one launch
-    template <int NF> hipError_t link(const OrthArgs& g, int splits, const float* abc, int n) {
-        int ranges = splits;
-        if (ranges > 8) {
-            orth_fold_kernel<<<dim3(NF * NF / 4, count), 256, 0, st>>>(w.part, ranges, NF * NF);
-            ranges = 1;
-        }
+    // Two steps' Q in one launch
+    template <int NF> hipError_t link(float* sums, const OrthArgs& of, const float* abc) {
+        OrthArgs g = {};
+        g.part = sums;
+        g.c = w.q;
         constexpr int bytes = 4 * NF * (NF / 2) * ORTH_BLOCK;
-        const hipError_t e = hipFuncSetAttribute((const void*)orth_chain_kernel<NF, (NF < 8)>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        auto kernel = orth_chain_kernel<NF>;
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        orth_chain_kernel<NF, (NF < 8)><<<count, NF * 64, bytes, st>>>(g, splits, ranges, abc[0], abc[1], abc[2], n == 2, n == 2 ? abc[3] : 0.f, n == 2 ? abc[4] : 0.f, n == 2 ? abc[5] : 0.f);
+        kernel<<<count, NF * 64, bytes, st>>>(g, of.apart, of.ranges, abc[0], abc[1], abc[2], abc[3], abc[4], abc[5]);
         return hipGetLastError();
     }
     // Matrices of up to 128 rows (16 NF padded)
-    template <int NF, int MODE, int OUT> static auto step_kernel() {
-        if constexpr (NF == 8) return orth_rows_kernel<MODE, OUT>;
-        else return orth_thin_kernel<NF, MODE, OUT>;
+    template <int NF, int MODE, int OUT, bool OWN> static auto step_kernel() {
+        if constexpr (NF == 8) return orth_rows_kernel<MODE, OUT, OWN>;
+        else return orth_thin_kernel<NF, MODE, OUT, OWN>;
     }
     template <int NF> hipError_t thin() {
         const int groups = thin_groups(count, z);
         auto launch = [&](auto kernel, const OrthArgs& g) {
-            const int bytes = (NF == 8 ? 6 * NF : 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF)) * ORTH_BLOCK;
+            const int bytes = ((NF == 8 ? 6 * NF : 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF)) + NF * NF) * ORTH_BLOCK;
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
             if (e != hipSuccess) return e;
             kernel<<<dim3(groups, count), 256, bytes, st>>>(g);
@@ -1043,31 +1121,43 @@ template <bool F32> struct Steps {
         g.matrices = count;
         g.a = w.q, g.b = w.x[0];
         g.steps = z.m / 32;
-        g.part = w.part;
-        hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS>(), g);
+        float *sums = w.part, *next = w.part + part_bytes(count, z) / 8;  // (read and written by one launch)
+        g.part = sums;
+        hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS, false>(), g);
+        // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second parts
+        // are multiplied with each other too, and, up to 64 rows, steps taken one by one (2 x 24 x 24: 1.6e-6 of the norm in pairs without,
+        // 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).  Otherwise pairs, whose products take a launch of their own, where X is long or Q larger.
+        const bool pairs = NF == 8 || (!F32 && groups > 8);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second parts
-            // are multiplied with each other too, and, up to 64 rows, steps taken one by one (2 x 24 x 24: 1.6e-6 of the norm in pairs without,
-            // 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).
-            const int n = (!F32 || NF == 8) && k + 2 <= t.steps ? 2 : 1;
+            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
-            OrthArgs l = {};
-            l.c = w.q;
-            l.part = w.part;
-            e = link<NF>(l, groups, abc, n);
+            g.apart = g.ranges = groups;
+            if (groups > 8) {
+                orth_fold_kernel<<<dim3(NF * NF / 4, count), 256, 0, st>>>(sums, groups, NF * NF);
+                e = hipGetLastError();
+                g.ranges = 1;
+            }
+            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, abc);
             if (e != hipSuccess) break;
+            g.sums = sums, g.part = next;
+            for (int j = 0; j < 3; ++j) g.abc[j] = abc[j];
             g.b = w.x[0], g.c = w.x[1];
             g.alpha = 1.f / Q_SCALE;
+            g.beta = 1.f;
+            constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
-                e = launch(step_kernel<NF, 1, ORTH_BLOCKS>(), g);
+                e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g);
             } else {
                 to_caller(g);
-                e = launch(step_kernel<NF, 2, F32 ? ORTH_F32 : ORTH_BF16>(), g);
+                e = n == 2 ? launch(step_kernel<NF, 2, OUT, false>(), g) : launch(step_kernel<NF, 2, OUT, true>(), g);
             }
             const OrthOperand o = w.x[0];
             w.x[0] = w.x[1];
             w.x[1] = o;
+            float* p = sums;
+            sums = next;
+            next = p;
         }
         return e;
     }
