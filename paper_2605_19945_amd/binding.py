@@ -968,15 +968,24 @@ def moe_residual_norm_backward(dout, y, weight=None, out=None, dh=None, norm=Tru
 
 # ---- orthogonalised updates ----
 @functools.lru_cache(maxsize=64)
-def _coefficients(values, steps):
-    """Host array (bytes) of the coefficients [steps][3], or None."""
+def _packed(triples):
+    return struct.pack(f"={3 * len(triples)}f", *[v for t in triples for v in t])
+
+
+def _coefficients(what, values, steps):
+    """Host array (bytes) of the coefficients [steps][3].  They are turned into numbers before they are looked up: tensors would be found by identity."""
+    if not isinstance(steps, int) or not 1 <= steps <= 64:
+        _refuse(what, "steps has to be an integer from 1 to 64")
     try:
-        rows = [values] * steps if len(values) == 3 and not hasattr(values[0], "__len__") else values
-        if len(rows) != steps or any(len(r) != 3 for r in rows):
-            return None
-        return struct.pack(f"={3 * steps}f", *[float(v) for r in rows for v in r])
-    except (TypeError, ValueError, OverflowError):
-        return None
+        try:
+            triples = (tuple(map(float, values)),) * steps
+        except (TypeError, ValueError, RuntimeError):
+            triples = tuple(tuple(map(float, t)) for t in values)
+        if len(triples) == steps and all(len(t) == 3 for t in triples):
+            return _packed(triples)
+    except (TypeError, ValueError, RuntimeError, OverflowError):
+        pass
+    _refuse(what, "coefficients have to be three numbers, or three for each step")
 
 
 def _stack(what, name, t):
@@ -1000,11 +1009,7 @@ def moe_orthogonalize(g, steps=5, scale=1.0, eps=1e-7, coefficients=(3.4445, -4.
     dtype = dtype or (out.dtype if out is not None else g.dtype)
     if dtype not in (_F32, _BF16):
         _refuse(what, "dtype has to be float32 or bfloat16")
-    if not isinstance(coefficients, tuple):
-        coefficients = tuple(map(tuple, coefficients))
-    abc = _coefficients(coefficients, steps)
-    if abc is None:
-        _refuse(what, "coefficients have to be three numbers, or three for each step")
+    abc = _coefficients(what, coefficients, steps)
     dev = _launch_device(what, g, out)
     x, ostride, ldo = out, rows * cols, cols
     if out is None:

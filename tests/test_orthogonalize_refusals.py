@@ -70,3 +70,20 @@ def test_the_binding_refuses(lib):
     refused(g.clone().requires_grad_())
     for bad in ((1.0, 2.0), ((1.0, 2.0, 3.0),) * 4, (1.0, "x", 2.0), ((1.0, 2.0),) * 5, (1e300, 0.0, 0.0)):
         refused(g, coefficients=bad)
+    for bad in (None, 1.0, [1.0, 2.0], torch.ones(2), ([1.0, 2.0, 3.0],) * 4, [[1.0, 2.0]] * 5, (torch.ones(3), 1.0, 2.0), "abc"):
+        refused(g, coefficients=bad)
+    for steps in (0, -1, 65, 10 ** 9, 5.0, "5", None):
+        refused(g, steps=steps)
+
+
+def test_coefficients_in_any_form():
+    """Lists, tuples, arrays and tensors of numbers; a tensor whose values change is read again."""
+    from paper_2605_19945_amd.binding import _coefficients
+    one = _coefficients("", (3.0, -4.0, 2.0), 2)
+    assert list(memoryview(one).cast("f")) == [3.0, -4.0, 2.0] * 2
+    abc = torch.tensor([3.0, -4.0, 2.0])
+    for same in ([3, -4, 2], abc, tuple(abc), abc.numpy(), [[3.0, -4.0, 2.0]] * 2, ([3.0, -4.0, 2.0], (3.0, -4.0, 2.0)), abc.expand(2, 3)):
+        assert _coefficients("", same, 2) == one
+    parts = tuple(abc)
+    abc[0] = 1.0
+    assert list(memoryview(_coefficients("", parts, 2)).cast("f")) == [1.0, -4.0, 2.0] * 2
