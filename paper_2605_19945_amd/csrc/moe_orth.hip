@@ -1110,8 +1110,8 @@ template <bool F32> struct Steps {
     }
     template <int NF> hipError_t thin() {
         const int groups = thin_groups(count, z);
-        auto launch = [&](auto kernel, const OrthArgs& g) {
-            const int bytes = ((NF == 8 ? 6 * NF : 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF)) + NF * NF) * ORTH_BLOCK;
+        auto launch = [&](auto kernel, const OrthArgs& g, bool own) {
+            const int bytes = ((NF == 8 ? 6 * NF : 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF)) + (own ? NF * NF : 0)) * ORTH_BLOCK;
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
             if (e != hipSuccess) return e;
             kernel<<<dim3(groups, count), 256, bytes, st>>>(g);
@@ -1123,7 +1123,7 @@ template <bool F32> struct Steps {
         g.steps = z.m / 32;
         float *sums = w.part, *next = w.part + part_bytes(count, z) / 8;  // (read and written by one launch)
         g.part = sums;
-        hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS, false>(), g);
+        hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS, false>(), g, false);
         // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second parts
         // are multiplied with each other too, and, up to 64 rows, steps taken one by one (2 x 24 x 24: 1.6e-6 of the norm in pairs without,
         // 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).  Otherwise pairs, whose products take a launch of their own, where X is long or Q larger.
@@ -1147,10 +1147,10 @@ template <bool F32> struct Steps {
             g.beta = 1.f;
             constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
-                e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g);
+                e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g, false) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g, true);
             } else {
                 to_caller(g);
-                e = n == 2 ? launch(step_kernel<NF, 2, OUT, false>(), g) : launch(step_kernel<NF, 2, OUT, true>(), g);
+                e = n == 2 ? launch(step_kernel<NF, 2, OUT, false>(), g, false) : launch(step_kernel<NF, 2, OUT, true>(), g, true);
             }
             const OrthOperand o = w.x[0];
             w.x[0] = w.x[1];
