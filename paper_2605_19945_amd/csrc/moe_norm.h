@@ -119,16 +119,20 @@ template <int W, int N> static __device__ inline void group_sums(float (&v)[N], 
     }
 }
 
-// The layout of a row of d values; calls f(Layout<W, CH>).  Narrow rows a wavefront each, wide ones all eight.
+// The layout of a row of d values; calls f(Layout<W, CH>): a chunk a lane where eight wavefronts or fewer do for that.  More wavefronts than that leave
+// lanes idle (131072 rows of 512, forward and backward: 41 and 80 us by one wavefront a row, 59 and 184 by four), fewer hold more of a row
+// each (32768 rows of 2048: 39 and 88 by four wavefronts, 42 and 109 by one; 32 rows of 1024, join and gradients: 3.1 and 7.2 by two, 3.7
+// and 10.6 by one; 16384 rows of 4096, its gradients: 137 by eight, 185 by four).
 template <int W_, int CH_> struct Layout { static constexpr int W = W_, CH = CH_; };
 template <typename F> static inline hipError_t with_layout(int d, F&& f) {
     if (d <= 512) return f(Layout<1, 1>{});
-    if (d <= 1024) return f(Layout<1, 2>{});
+    if (d <= 1024) return f(Layout<2, 1>{});
     if (d <= 2048) return f(Layout<4, 1>{});
     if (d <= 4096) return f(Layout<8, 1>{});
     if (d <= 8192) return f(Layout<8, 2>{});
     return f(Layout<8, 4>{});
 }
-// Tensors that the last-level cache (256 MB) does not hold until their next use: `bytes` of all that a call reads and writes.
+// Tensors that the last-level cache (256 MB) does not hold until their next use: `bytes` of all that a call reads and writes.  With the hint the join of
+// 65536 rows of 1024 (400 MB) takes 93 us, without 103; the norm of as many (268 MB) 45 with and 41 without.
 static inline bool norm_streams(int64_t bytes) { return bytes > (int64_t)256 << 20; }
-static inline int norm_rows_per_group(int d) { return d <= 1024 ? 8 : d <= 2048 ? 2 : 1; }
+static inline int norm_rows_per_group(int d) { return d <= 512 ? 8 : d <= 1024 ? 4 : d <= 2048 ? 2 : 1; }

@@ -49,7 +49,6 @@ struct NormGradArgs {
     bool x_f32, y_f32, w_f32, norm;
 };
 constexpr int NORM_MAX_WIDTH = 16384;   // a row stays in the registers of 512 lanes
-constexpr int NORM_GRAD_GROUPS = 1024;  // workgroups of a backward launch, at most
 int norm_grad_groups(int rows, int d);
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float* workspace, hipStream_t st);
