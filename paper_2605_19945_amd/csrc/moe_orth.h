@@ -25,8 +25,8 @@ struct OrthOperand {
 
 struct OrthArgs {
     OrthOperand a, b;
-    OrthOperand cin;       // beta times this is added, or (beta + rest of the row) times
-    float* rest;           // what one part leaves of a symmetric result's diagonal: [matrices][its rows]
+    OrthOperand cin;       // beta times this is added, or times the row's of
+    float* own;            // a symmetric result's diagonal: [matrices][its rows]
     OrthOperand c;         // the result
     float alpha, beta;
     float diagonal;        // added to the diagonal of a symmetric result
@@ -83,6 +83,13 @@ static __device__ inline uint32_t pack_f16(float lo, float hi) {
 }
 static __device__ inline float f16_lo(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)w); }
 static __device__ inline float f16_hi(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16)); }
+// Two values' first parts and second ones.  The first are hidden from the compiler before the second are formed: it would make those from another rounding of
+// the values, by an instruction that multiplies, adds and rounds once, which differs in one of some thousand values, by a whole step of the first part.
+static __device__ inline void split_f16(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = pack_f16(x, y);
+    asm("" : "+v"(hi));
+    lo = pack_f16(x - f16_lo(hi), y - f16_hi(hi));
+}
 
 template <int I> struct OrthInt { static constexpr int value = I; };
 template <int N, int I = 0, typename F> static __device__ inline void orth_repeat(F&& f) {  // f(0) .. f(N - 1), each a constant

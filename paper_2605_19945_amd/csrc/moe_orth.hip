@@ -7,11 +7,11 @@
 // each, for the small singular values), so operands are kept in one or two parts of fp16 (moe_orth.h), and X always in two.
 //   fp32 results: all operands of all products have two parts, 22 bits: as far from the exact ones as those of 32-bit products (0.8 to 1.3 times,
 // 1e-6 to 3e-6 of their norm).  Three products of parts for one, so where X is wide two steps are taken at a time through products of squares only.
-//   bf16 results: one part in every product; X's own term a X, the largest, is added from both parts, and so is what one part leaves of the diagonal of
-// b S + c S S.  1e-4 of the norm on the spectra of gradients, 1.3e-3 on flat ones, below the 1.7e-3 of the result's own rounding; with X in one part steep
-// spectra lose 8e-3, with bf16 operands 6e-2.
-// Measured: 8 matrices of 4096 x 14336 in bf16 30.1 ms (1050 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
-// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 30.0 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.4 ms.  One-part
+//   bf16 results: one part in every product; X's second part takes the diagonal of Q = a I + b S + c S S alone, its largest share.  5e-4 of the norm on the
+// spectra of gradients, 1.1e-3 on flat ones, below the 1.7e-3 of the result's own rounding (1.03 to 1.2 times that in all); with X in one part
+// steep spectra lose 8e-3, with bf16 operands 6e-2.
+// Measured: 8 matrices of 4096 x 14336 in bf16 29.8 ms (1060 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
+// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 30.0 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.3 ms.  One-part
 // products wait for their operands on the way from the L2s through LDS (without these loads the first case takes two thirds of its time); short
 // reductions, as 768, for tiles' beginnings and ends.
 #include "moe_orth.h"
@@ -50,7 +50,7 @@ template <bool SYM> static __device__ inline void place(const OrthArgs& g, int t
 }
 
 // The sums of two neighbouring fragments on their way out: a lane has the columns c + 4 q + 0..3 and c + 16 + 4 q + 0..3 of row r + i (i = lane % 16,
-// q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each of its rows (beta + what the diagonal of A has left) times.
+// q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each of its rows beta times A's diagonal.
 // OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any result in blocks; or its type in
 // the caller's rows.  PARTS: of a result in blocks.
 // In a block a lane's 4 values are half a piece, and lanes of neighbouring q change halves for accesses of 16 bytes.
@@ -60,7 +60,7 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
     u *= g.alpha;
     v *= g.alpha;
     if constexpr (CIN > 0) {
-        const float beta = ROWS ? g.beta * (g.diagonal + g.rest[(int64_t)matrix * (g.square) + r + i]) : g.beta;
+        const float beta = ROWS ? g.beta * g.own[(int64_t)matrix * g.square + r + i] : g.beta;
 #pragma unroll
         for (int p = 0; p < CIN; ++p) {
             const u32x4_t w = *(const u32x4_t*)(g.cin.part[p] + matrix * g.cin.matrix + here);
@@ -77,25 +77,20 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
         }
     }
     if constexpr (OUT == ORTH_SQUARE || OUT == ORTH_BLOCKS) {
-        uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+        uint32_t parts[2][4];
+        split_f16(u[0], u[1], parts[0][0], parts[1][0]), split_f16(u[2], u[3], parts[0][1], parts[1][1]);
+        split_f16(v[0], v[1], parts[0][2], parts[1][2]), split_f16(v[2], v[3], parts[0][3], parts[1][3]);
         if constexpr (OUT == ORTH_SQUARE && PARTS == 1) {
-            if (g.rest != nullptr && (r == c || r == c + 16)) {
+            if (g.own != nullptr && (r == c || r == c + 16)) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float x = r == c ? u[j] : v[j];
-                    if (4 * q + j == i) g.rest[(int64_t)matrix * (g.square) + r + i] = (x - (float)(_Float16)x) * (1.f / Q_SCALE);
+                    if (4 * q + j == i) g.own[(int64_t)matrix * g.square + r + i] = (r == c ? u[j] : v[j]) * (1.f / Q_SCALE);
                 }
             }
         }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            if (p == 1) {
-                const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
-                a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
-                a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
-                a[2] = pack_f16(v[0] - f16_lo(h[2]), v[1] - f16_hi(h[2]));
-                a[3] = pack_f16(v[2] - f16_lo(h[3]), v[3] - f16_hi(h[3]));
-            }
+            const uint32_t(&a)[4] = parts[p];
             char* to = g.c.part[p] + matrix * g.c.matrix;
             const auto x = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
             *(u32x4_t*)(to + here) = u32x4_t{x[0], y[0], x[1], y[1]};
@@ -362,9 +357,10 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
     auto put = [&](char* to, int64_t plane, int blocks) {
         each([&](int m, int n) {
             const f32x4_t& x = v[m][n];
-            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
-            *(u32x2_t*)(to + at(m, n, blocks)) = u32x2_t{h0, h1};
-            *(u32x2_t*)(to + plane + at(m, n, blocks)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+            uint32_t hi[2], lo[2];
+            split_f16(x[0], x[1], hi[0], lo[0]), split_f16(x[2], x[3], hi[1], lo[1]);
+            *(u32x2_t*)(to + at(m, n, blocks)) = u32x2_t{hi[0], hi[1]};
+            *(u32x2_t*)(to + plane + at(m, n, blocks)) = u32x2_t{lo[0], lo[1]};
         });
     };
 
@@ -426,16 +422,12 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
 
 // Two neighbouring fragments' values as the pieces of a block that a lane stores, in two parts
 static __device__ inline void pieces_of(const f32x4_t& u, const f32x4_t& v, u32x4_t (&piece)[2]) {
-    uint32_t a[4] = {pack_f16(u[0], u[1]), pack_f16(u[2], u[3]), pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+    uint32_t parts[2][4];
+    split_f16(u[0], u[1], parts[0][0], parts[1][0]), split_f16(u[2], u[3], parts[0][1], parts[1][1]);
+    split_f16(v[0], v[1], parts[0][2], parts[1][2]), split_f16(v[2], v[3], parts[0][3], parts[1][3]);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        if (p == 1) {
-            const uint32_t h[4] = {a[0], a[1], a[2], a[3]};
-            a[0] = pack_f16(u[0] - f16_lo(h[0]), u[1] - f16_hi(h[0]));
-            a[1] = pack_f16(u[2] - f16_lo(h[1]), u[3] - f16_hi(h[1]));
-            a[2] = pack_f16(v[0] - f16_lo(h[2]), v[1] - f16_hi(h[2]));
-            a[3] = pack_f16(v[2] - f16_lo(h[3]), v[3] - f16_hi(h[3]));
-        }
+        const uint32_t(&a)[4] = parts[p];
         const auto x = __builtin_amdgcn_permlane16_swap(a[0], a[2], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[3], false, false);
         piece[p] = u32x4_t{x[0], y[0], x[1], y[1]};
     }
@@ -459,9 +451,10 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
     auto put = [&] {
         each([&](int m, int n) {
             const f32x4_t& x = v[m][n];
-            const uint32_t h0 = pack_f16(x[0], x[1]), h1 = pack_f16(x[2], x[3]);
-            *(u32x2_t*)(s + at(m, n)) = u32x2_t{h0, h1};
-            *(u32x2_t*)(s + PLANE + at(m, n)) = u32x2_t{pack_f16(x[0] - f16_lo(h0), x[1] - f16_hi(h0)), pack_f16(x[2] - f16_lo(h1), x[3] - f16_hi(h1))};
+            uint32_t hi[2], lo[2];
+            split_f16(x[0], x[1], hi[0], lo[0]), split_f16(x[2], x[3], hi[1], lo[1]);
+            *(u32x2_t*)(s + at(m, n)) = u32x2_t{hi[0], hi[1]};
+            *(u32x2_t*)(s + PLANE + at(m, n)) = u32x2_t{lo[0], lo[1]};
         });
     };
     const f32x4_t* part = (const f32x4_t*)g.sums + (int64_t)matrix * g.apart * (NF * NF * 64) + lane;
@@ -876,8 +869,9 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
         u32x4_t hi, lo;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            hi[j] = pack_f16(v[2 * j], v[2 * j + 1]);
-            lo[j] = pack_f16(v[2 * j] - f16_lo(hi[j]), v[2 * j + 1] - f16_hi(hi[j]));
+            uint32_t h, l;
+            split_f16(v[2 * j], v[2 * j + 1], h, l);
+            hi[j] = h, lo[j] = l;
         }
         const int R = (in.tall ? c0 : r0) / 16 + (k >> 7), C = (in.tall ? r0 : c0) / 32 + (k >> 6 & 1);
         if (R >= in.block_rows) continue;
@@ -967,7 +961,7 @@ constexpr int64_t kPartBytes = (int64_t)kUnits * 256 * 256 * 4;
 
 template <int PA, int PB, bool TB, int CIN, bool ROWS, int PARTS, int OUT> hipError_t product(OrthArgs g, int tile, hipStream_t st) {
     constexpr int PLANES = PA + PB, KS = PLANES == 2 ? 2 : 1, STAGES = PLANES == 2 ? 4 : 2;
-    // One-part products with X, whose tiles read X's own term and write X in two parts, are cut to 256 x 128 by four wavefronts, two workgroups a unit, of
+    // One-part products with X, whose tiles read X's second part and write both, are cut to 256 x 128 by four wavefronts, two workgroups a unit, of
     // which one multiplies while the other begins or ends a tile: they load half as much again, and 8 x 4096 x 14336 in bf16 takes 30.3 ms
     // instead of 30.9 all the same, 128 x 768 x 2048 4.53 instead of 4.60.  (The products of squares, which write little, are slower so, by 1 %.)
     constexpr bool FLAT = PLANES == 2 && TB;
@@ -996,7 +990,7 @@ template <int PA, int PB, bool TB, int CIN, bool ROWS, int PARTS, int OUT> hipEr
 
 struct Buffers {
     OrthOperand x[2], s, q, t;
-    float *part, *rest;
+    float *part, *own;
 };
 
 OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
@@ -1043,20 +1037,20 @@ template <bool F32> struct Steps {
         const int size = F32 ? 4 : 2;
         g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
     }
-    // X = q X, into the other buffer or to the caller; where q has one part, X = (a + rest) X + q X of X's first part
-    template <bool TWO> hipError_t apply(const OrthOperand& q, float a, bool last) {
-        constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 2;
+    // X = q X, into the other buffer or to the caller; where q has one part, q of X's first part and, of the second, its diagonal's share alone
+    template <bool TWO> hipError_t apply(const OrthOperand& q, bool last) {
+        constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 1;
         OrthArgs g = {};
         g.matrices = count;
         g.mt = z.n / z.tile, g.nt = z.m / z.tile;
         g.tiles = g.mt * g.nt;
         g.square = z.n;
         g.a = q, g.b = w.x[0], g.c = w.x[1], g.cin = w.x[0];
-        g.rest = w.rest;
+        g.cin.part[0] = w.x[0].part[1];
+        g.own = w.own;
         g.steps = z.n / 32;
         g.alpha = 1.f / Q_SCALE;
         g.beta = 1.f;
-        g.diagonal = a;
         g.part = w.part;
         hipError_t e;
         if (!last) {
@@ -1075,14 +1069,14 @@ template <bool F32> struct Steps {
         constexpr int PARTS = F32 ? 2 : 1;
         return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
     }
-    // to = a I + b S + c S S; in one part without a I, for which it has too few digits, and with what it has too few for on its diagonal aside
+    // to = a I + b S + c S S, and where it has one part its diagonal in 32 bits
     hipError_t polynomial(const OrthOperand& to, const float* abc) const {
         constexpr int PARTS = F32 ? 2 : 1;
         OrthArgs g = square(w.s, w.s, to, abc[2] * Q_SCALE / (S_SCALE * S_SCALE));
         g.cin = w.s;
         g.beta = abc[1] * Q_SCALE / S_SCALE;
-        g.diagonal = F32 ? abc[0] * Q_SCALE : 0.f;
-        g.rest = F32 ? nullptr : w.rest;
+        g.diagonal = abc[0] * Q_SCALE;
+        g.own = F32 ? nullptr : w.own;
         return product<PARTS, PARTS, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
     // to = a q, of matrices that commute
@@ -1092,7 +1086,7 @@ template <bool F32> struct Steps {
     hipError_t one_step(const float* abc, bool last) {
         hipError_t e = gram();
         if (e == hipSuccess) e = polynomial(w.q, abc);
-        if (e == hipSuccess) e = apply<F32>(w.q, abc[0], last);
+        if (e == hipSuccess) e = apply<F32>(w.q, last);
         return e;
     }
     hipError_t two_steps(const float* abc, bool last) {
@@ -1102,7 +1096,7 @@ template <bool F32> struct Steps {
         if (e == hipSuccess) e = times(w.t, w.q, w.s);  // Q S Q = (Q X) (Q X)^T
         if (e == hipSuccess) e = polynomial(w.t, abc + 3);
         if (e == hipSuccess) e = times(w.t, w.q, w.s);
-        if (e == hipSuccess) e = apply<true>(w.s, 0.f, last);
+        if (e == hipSuccess) e = apply<true>(w.s, last);
         return e;
     }
     // Two steps' Q in one launch
@@ -1229,7 +1223,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.ld = t.g_ld;
         in.rows = t.rows;
         in.cols = t.cols;
-        w.rest = (float*)at;
+        w.own = (float*)at;
         in.partials = (double*)(at + (int64_t)z.n * 4 * count);
         in.parts = z.parts;
         in.eps = t.eps;

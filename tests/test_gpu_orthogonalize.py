@@ -5,7 +5,7 @@ steps) and differently for every spectrum, so the bound of a case is found by ca
 product off by a random share, uniform to either side, of what its rounding may be off by (one part of fp16: 2^-11 of the value; two: 2^-22; a
 product's 32-bit sums: 2^-22 of the product of the magnitudes), give a deviation D; |D| is the root of its mean square over a few draws (of small
 matrices more: one draw of a few numbers can come near zero).  The kernel's errors are of the same sizes or smaller.  In the smallest matrices they
-are 15 numbers at least (X, S and P of five steps), each at most 3^1/2 times its root mean square, so by Cauchy and Schwarz together at most 45^1/2 < 8 times
+are 15 numbers at least (X, S and Q of five steps), each at most 3^1/2 times its root mean square, so by Cauchy and Schwarz together at most 45^1/2 < 8 times
 that of their sum; in larger ones there are more of them and they come nearer to it.  So their norm is below 8 |D|; a single value is within 6
 times its share of that (and never past the norm).  Where a few directions u v^T carry the errors, as on steep spectra, the value in row i and column j of each is
 |u_i| |v_j|, so its share is that of row i times that of column j of the whole, not 1 / (n m)^1/2 of it.
@@ -31,7 +31,7 @@ def gradient(shape, seed, dtype, kind="gauss", std=1e-3):
 
 
 def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
-    """64 bits; noise: (parts of S, P and of X where they are formed and multiplied, generator) for the deviated run."""
+    """64 bits; noise: (parts of S, Q and of X where they are formed and multiplied, generator) for the deviated run."""
     tall = G.shape[0] > G.shape[1]
     X = (G.t() if tall else G).double()
     X = X / (X.square().sum().sqrt() + eps)
@@ -55,8 +55,8 @@ def steps_of(G, coefficients, scale=1.0, eps=1e-7, noise=None):
         X = part(X, 2)
         Y = part(X, parts)
         S = part(product(Y, Y.t()), parts)
-        P = part(b * S + c * product(S, S), parts)
-        X = a * X + product(P, Y)
+        Q = part(a * torch.eye(S.shape[0], dtype=F64, device=S.device) + b * S + c * product(S, S), parts)
+        X = product(Q, Y) + Q.diagonal()[:, None] * (X - Y)
     return scale * (X.t() if tall else X)
 
 
