@@ -88,3 +88,42 @@ def test_the_update_of_the_block(step):
                 X = X * 0.2 * max(X.shape) ** 0.5
                 # 1.95 g is rounded to 32 bits before; the steps carry 2^-24 on by at most 3.4445^5 < 2^9, and add as much a few times over
                 assert float((u[e, :, a:b].double() - X).norm()) <= 2.0 ** -12 * float(X.norm())
+
+
+def test_a_captured_step():
+    """The whole step in a graph, replayed over other tokens with eager steps between, gives the eager step's bits."""
+    ex = load()
+    T, d, f, E, k = 96, 256, 128, 4, 2
+    g = torch.Generator().manual_seed(9)
+
+    def normal(*shape, std=1.0, dtype=torch.bfloat16):
+        return (torch.randn(shape, generator=g) * std).to(dtype).cuda()
+
+    x, dout = normal(T, d), normal(T, d)
+    weights, norms = [normal(E, d, 2 * f, std=d ** -0.5), normal(E, f, d, std=f ** -0.5)], [1 + normal(d, std=0.2, dtype=torch.float32) for _ in range(2)]
+    ctx = moe.MoEContext(T, d, f, E, k)
+    router = ctx.moe_pack_router(normal(d, E, std=d ** -0.5, dtype=torch.float32))
+
+    def step():
+        out, kept = ex.block_forward(ctx, x, router, weights, norms)
+        dx, *grads = ex.block_backward(ctx, dout, x, weights, norms, kept)
+        length = moe.moe_clip_grad_norm(grads, 1.0)
+        return [out, dx, length, *grads, *(ex.orthogonal_update(t, torch.zeros_like(t), h) for t, h in zip(grads[:2], (f, 0)))]
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(4):
+        x.copy_(normal(T, d))
+        dout.copy_(normal(T, d))
+        graph.replay()
+        torch.cuda.synchronize()
+        first = [t.clone() for t in held]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, want)) and all(torch.equal(a, b) for a, b in zip(held, want))
+    ctx.close()
