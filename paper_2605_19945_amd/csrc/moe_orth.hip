@@ -333,8 +333,9 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 
 // ---- between S and the next product with X, for matrices of up to 128 rows ----
 // Of two steps' Q = a I + b S + c S S the product, from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
-// of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  All four products
-// of the parts are formed: small matrices have few values to average over (8 x 128 x 256 in fp32: 1.7e-6 of the norm with three, 1.35e-6 with four).
+// of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  Up to 64 rows
+// all four products of the parts are formed: the smallest matrices have few values to average over (4 x 16 x 400 in fp32: 1.5 times the error of 32-bit products with
+// three, 1.2 to 1.3 with four; 8 x 128 x 256: 1.1 and 1.05, but 80 us and 85).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
 // latencies are half of what it takes (8 matrices of 128 rows, two steps: 21 us, 10 of them the products' own; unrolled with all its products 54; only the
 // columns from the diagonal on, half the products, but branches, 28).
@@ -392,7 +393,7 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
             constexpr int k = decltype(block)::value;
             if constexpr (k + 1 < KB) read(k + 1);
             __builtin_amdgcn_sched_barrier(0);
-            orth_repeat<4>([&](auto parts) {
+            orth_repeat<NF == 8 ? 3 : 4>([&](auto parts) {
                 constexpr int p = decltype(parts)::value >> 1, r = decltype(parts)::value & 1;
                 each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k & 1][r][n], a[k & 1][p][m], v[m][n], 0, 0, 0); });
             });
@@ -475,7 +476,7 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
 #pragma unroll
             for (int n = 0; n < NF; ++n) b[p][n] = *(const f16x8_t*)(s + p * PLANE + (n * KB + k) * ORTH_BLOCK + at_row);
         }
-        orth_repeat<4>([&](auto parts) {
+        orth_repeat<NF == 8 ? 3 : 4>([&](auto parts) {
             constexpr int p = decltype(parts)::value >> 1, r = decltype(parts)::value & 1;
             each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p][m], v[m][n], 0, 0, 0); });
         });
@@ -678,7 +679,7 @@ template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1
                         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_turn)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(block + at_next));
                         b[p][j] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                     }
-                orth_repeat<4>([&](auto pair) {
+                orth_repeat<3>([&](auto pair) {
                     constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
 #pragma unroll
                     for (int m = 0; m < FM; ++m)
@@ -720,7 +721,7 @@ template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1
 #pragma unroll
                     for (int w = 1; w < 4; ++w) own[p][m] = wave == w ? x[p][w * FM + m] : own[p][m];
                 }
-            orth_repeat<4>([&](auto pair) {
+            orth_repeat<3>([&](auto pair) {
                 constexpr int p = decltype(pair)::value >> 1, r = decltype(pair)::value & 1;
 #pragma unroll
                 for (int m = 0; m < FM; ++m)
@@ -905,23 +906,33 @@ Cut cut_of(int64_t tiles, int steps, int units) {
     return {(int)tiles, 1};
 }
 
-// Time of one step of E matrices in tiles of this size, roughly, in steps of 32 of the reduction of a tile of 256
-double step_time(int E, int n, int m, int tile) {
-    const int64_t nt = (n + tile - 1) / tile, mt = (m + tile - 1) / tile, half = nt * (nt + 1) / 2;
-    auto product = [&](int64_t tiles, int64_t steps) {
-        tiles *= E;
-        const int units = tile == 256 ? kUnits : 2 * kUnits;
-        const Cut c = cut_of(tiles, (int)steps, units);
-        const int64_t rounds = (c.whole + units - 1) / units;
-        return ((double)rounds * (steps + 8) + (c.splits > 1 ? (double)steps / c.splits + 16 : 0)) * (tile == 256 ? 1.0 : 0.7);
+// Time of a product's tiles, roughly, in blocks of the reduction of a tile of 256 (0.86 us in one part, 2.2 in two): 8 for a tile's beginning and end, 24 for
+// those of a cut one and its sums; a round of small tiles, two a compute unit, 0.6 of one of large ones.
+double product_time(int64_t tiles, int64_t steps, int tile) {
+    const int units = tile == 256 ? kUnits : 2 * kUnits;
+    const Cut c = cut_of(tiles, (int)steps, units);
+    return ((double)((c.whole + units - 1) / units) * (steps + 8) + (c.splits > 1 ? (double)steps / c.splits + 24 : 0)) * (tile == 256 ? 1.0 : 0.6);
+}
+// ... of the products of a step of E matrices: S, its polynomial (any product of squares), the one with X
+struct StepTime { double s, square, x; };
+StepTime step_time(int E, int n, int m, int tile) {
+    const int64_t nt = (n + tile - 1) / tile, mt = (m + tile - 1) / tile, half = nt * (nt + 1) / 2 * E, reduction = nt * tile / 32;
+    return {product_time(half, mt * tile / 32, tile), product_time(half, reduction, tile), product_time(nt * mt * E, reduction, tile)};
+}
+// Large tiles where they take less of that: 128 matrices of 768 x 2048 in bf16 4.3 ms with large ones and 4.8 with small ones, 8 of 1100 x 1300 0.73 and 0.53, one
+// of 2048 x 2048 in fp32 0.82 and 0.68.
+int tile_of(int E, int n, int m) {
+    auto sum = [&](int tile) {
+        const StepTime t = step_time(E, n, m, tile);
+        return t.s + t.square + t.x;
     };
-    return product(half, (int64_t)mt * tile / 32) + product(half, (int64_t)nt * tile / 32) + product(nt * mt, (int64_t)nt * tile / 32);
+    return sum(256) < sum(128) ? 256 : 128;
 }
 
 Size size_of_matrix(int E, int rows, int cols) {
     Size z;
     const int n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    z.tile = n <= 128 ? 0 : step_time(E, n, m, 256) < step_time(E, n, m, 128) ? 256 : 128;
+    z.tile = n <= 128 ? 0 : tile_of(E, n, m);
     z.n = z.tile == 0 ? (n <= 32 ? 32 : n <= 64 ? 64 : 128) : (n + z.tile - 1) / z.tile * z.tile;
     z.m = z.tile == 0 ? (m + 63) / 64 * 64 : (m + z.tile - 1) / z.tile * z.tile;
     z.xb = z.m / 32 + 1, z.sb = z.n / 32 + 1;
@@ -1132,16 +1143,18 @@ template <bool F32> struct Steps {
         float *sums = w.part, *next = w.part + part_bytes(count, z) / 8;  // (read and written by one launch)
         g.part = sums;
         hipError_t e = launch(step_kernel<NF, 0, ORTH_BLOCKS, false>(), g, false);
-        // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those where second parts
-        // are multiplied with each other too, and, up to 64 rows, steps taken one by one (2 x 24 x 24: 1.6e-6 of the norm in pairs without,
-        // 1.4e-6 in pairs, 0.9e-6 so, 0.8e-6 with 32-bit products).  Otherwise pairs, whose products take a launch of their own, where X is long or Q larger.
+        // Small matrices have few values to average over, and 32-bit products lose little on them: fp32 results keep up with those up to 64 rows where steps are
+        // taken one by one (2 x 24 x 24: 1.1 to 1.2 times their error, 1.7 to 1.9 in pairs).  Otherwise pairs, whose products take a launch of their own, where X is long
+        // or Q larger (8 x 16 x 14336 in bf16: 65 us in pairs, 83 one by one; 8 x 128 x 256: 85 and 95).
         const bool pairs = NF == 8 || (!F32 && groups > 8);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
             const int n = pairs && k + 2 <= t.steps ? 2 : 1;
             const float* abc = t.coefficients + 3 * k;
             k += n;
+            // many ranges are added in a launch of their own, from more of the larger sums on (8 x 100 x 500, 8 of them: 100 us with it, 121 without; 64 x 64 x 300,
+            // 3: 84 and 77; 8 x 64 x 2000, 16: 54 and 60)
             g.apart = g.ranges = groups;
-            if (groups > 8) {
+            if (groups > (NF == 8 ? 4 : 8)) {
                 orth_fold_kernel<<<dim3(NF * NF / 4, count), 256, 0, st>>>(sums, groups, NF * NF);
                 e = hipGetLastError();
                 g.ranges = 1;
@@ -1170,10 +1183,10 @@ template <bool F32> struct Steps {
     }
     hipError_t run() {
         if (z.tile == 0) return z.n == 32 ? thin<2>() : z.n == 64 ? thin<4>() : thin<8>();
-        // Two steps at a time take the long products once, S = X X^T and the last one, for three more of the small ones: less work where X is
-        // wide.  (With operands in one part the small ones would need two and cost more than that gains.)
-        const int64_t nt = z.n / z.tile, mt = z.m / z.tile, half = nt * (nt + 1) / 2;
-        const bool pairs = F32 && half * mt + nt * mt * nt > 3 * half * nt;
+        // Two steps at a time take S = X X^T and the product with X once, for three more products of squares: less where X is wide (32 x 7168 x 2048 29.9 ms, one by
+        // one 38.7; 330 x 826 266 and 223 us).  (With operands in one part the squares would need two and cost more than that gains.)
+        const StepTime time = step_time(count, z.n, z.m, z.tile);
+        const bool pairs = F32 && time.s + time.x > 3 * time.square;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
             const int n = pairs && k + 2 <= t.steps ? 2 : 1;
