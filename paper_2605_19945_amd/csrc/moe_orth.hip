@@ -10,8 +10,8 @@
 //   bf16 results: one part in every product; X's second part takes the diagonal of Q = a I + b S + c S S alone, its largest share.  5e-4 of the norm on the
 // spectra of gradients, 1.1e-3 on flat ones, below the 1.7e-3 of the result's own rounding (1.03 to 1.2 times that in all); with X in one part
 // steep spectra lose 8e-3, with bf16 operands 6e-2.
-// Measured: 8 matrices of 4096 x 14336 in bf16 29.8 ms (1060 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
-// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 30.0 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.3 ms.  One-part
+// Measured: 8 matrices of 4096 x 14336 in bf16 29.5 ms (1070 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
+// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 29.9 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.2 ms.  One-part
 // products wait for their operands on the way from the L2s through LDS (without these loads the first case takes two thirds of its time); short
 // reductions, as 768, for tiles' beginnings and ends.
 #include "moe_orth.h"
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 // all four products of the parts are formed: the smallest matrices have few values to average over (4 x 16 x 400 in fp32: 1.5 times the error of 32-bit products with
 // three, 1.2 to 1.3 with four; 8 x 128 x 256: 1.1 and 1.05, but 80 us and 85).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
-// latencies are half of what it takes (8 matrices of 128 rows, two steps: 21 us, 10 of them the products' own; unrolled with all its products 54; only the
+// latencies are half of what it takes (8 matrices of 128 rows, two steps: 19 us, 7 of them the products' own; unrolled with all its products 54; only the
 // columns from the diagonal on, half the products, but branches, 28).
 template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2) {
     extern __shared__ __align__(1024) char lds[];
@@ -498,8 +498,8 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
 
 // ---- matrices of up to 64 rows ----
 // A wavefront takes 32 columns of X at a time, all its rows (16 NF): they are few enough that Q X and the new S = X X^T of these columns are formed
-// one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it (128 x 8004 x 17 in fp32: 390 us, by
-// tiles and products of their own 1900; 24 x 83: 28, of eight launches).  MODE 0: S of X as it is;
+// one after the other, so X is read and written once a step and memory, or for small stacks the launches, bound it (128 x 8004 x 17 in fp32: 382 us, by
+// tiles and products of their own 1310; 24 x 83: 27, of eight launches).  MODE 0: S of X as it is;
 // 1: X = Q X and its S; 2: X = Q X to the caller.  OWN: Q is formed here, from the sums that the launch before has left.
 // The results' lanes have the columns 4 q + 0..3 and 16 + 4 q + 0..3 of row i; after the change of halves that the stores want, lane (i, q) has 8
 // neighbouring columns of row i, in another order of q than an operand's lanes.  S sums over the columns, so any order will do that both of
@@ -613,7 +613,7 @@ template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256,
 
 // ---- matrices of 65 to 128 rows ----
 // The same by four wavefronts together, 32 rows each: X's blocks and the new X's pieces go through LDS to all of them, and each keeps its rows of Q
-// and of S.  The next columns are asked for while these are multiplied.  (1 x 100 x 2000 in fp32: 90 us, by tiles 103; 1 x 128 x 14336 in bf16 122.)
+// and of S.  The next columns are asked for while these are multiplied.  (100 x 2000 in fp32: 81 us, by tiles 133; 128 x 14336 in bf16 119 and 174.)
 template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1 : 2) void orth_rows_kernel(OrthArgs g) {
     constexpr int NF = 8, KB = 4, FM = 2, STAGE = 2 * NF * ORTH_BLOCK;
     extern __shared__ __align__(1024) char lds[];  // two stages of X's blocks [part][row], the new X's [part][row]
