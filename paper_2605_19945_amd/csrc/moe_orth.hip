@@ -896,13 +896,14 @@ struct Size {
 constexpr int kUnits = 256;  // compute units
 
 // How the tiles of a launch take their reductions of `steps` blocks: whole ones in full rounds of the `units` workgroups that run at once (two a compute unit,
-// one of 256 x 256), those of the last round, or of the only one, in ranges for the places that would have none: four blocks a range at least, and ten blocks'
-// time saved at least, about what a second launch and the sums' way to memory and back cost.
+// one of 256 x 256), those of the last round, or of the only one, in ranges for the places that would have none: four blocks a range at least, and the time
+// of 6 saved, about what a second launch costs, and of up to 12 more for the sums' way to memory and back (330 x 826 in fp32, up to 63 ranges that save 8 or more: 187 us,
+// whole 222; 16 x 512 x 512 in bf16, 480 ranges that save 11: 288, whole 204; 2 x 600 x 6000 in fp32, 150 that save 16: 380, whole 422).
 struct Cut { int whole, splits; };
 Cut cut_of(int64_t tiles, int steps, int units) {
     const int rest = (int)(tiles % units), most = steps / 4;
     const int room = rest > 0 ? units / rest : 1, s = room < most ? room : most;
-    if (s > 1 && steps - steps / s >= 10) return {(int)(tiles - rest), s};
+    if (s > 1 && steps - steps / s >= 6 + 12 * rest * s / units) return {(int)(tiles - rest), s};
     return {(int)tiles, 1};
 }
 
@@ -1184,7 +1185,7 @@ template <bool F32> struct Steps {
     hipError_t run() {
         if (z.tile == 0) return z.n == 32 ? thin<2>() : z.n == 64 ? thin<4>() : thin<8>();
         // Two steps at a time take S = X X^T and the product with X once, for three more products of squares: less where X is wide (32 x 7168 x 2048 29.9 ms, one by
-        // one 38.7; 330 x 826 266 and 223 us).  (With operands in one part the squares would need two and cost more than that gains.)
+        // one 38.7; 330 x 826, with its reductions of squares whole, 266 and 223 us).  (With operands in one part the squares would need two and cost more than that gains.)
         const StepTime time = step_time(count, z.n, z.m, z.tile);
         const bool pairs = F32 && time.s + time.x > 3 * time.square;
         hipError_t e = hipSuccess;
