@@ -54,6 +54,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float* workspace, hipStream_t st);
 
 // ---- orthogonalised updates ----
+constexpr int ORTH_MAX_STEPS = 64;
 struct OrthTask {
     const void* g;
     void* out;

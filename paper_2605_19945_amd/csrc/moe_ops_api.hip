@@ -355,7 +355,7 @@ moe_status moe_orthogonalize(const void* g, int32_t type, int64_t stride_g, int6
     if (E < 1 || rows < 1 || cols < 1 || !type_ok(type) || !type_ok(out_type)) return MOE_ERR_INVALID_ARG;
     if (!orth_shape_ok(E, rows, cols)) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (g == nullptr || out == nullptr || !aligned(g, size_of(type)) || !aligned(out, size_of(out_type))) return MOE_ERR_INVALID_ARG;
-    if (coefficients == nullptr || steps < 1 || steps > 64 || !(eps >= 0.f) || eps > 3e38f || !(scale >= -3e38f && scale <= 3e38f)) return MOE_ERR_INVALID_ARG;
+    if (coefficients == nullptr || steps < 1 || steps > ORTH_MAX_STEPS || !(eps >= 0.f) || eps > 3e38f || !(scale >= -3e38f && scale <= 3e38f)) return MOE_ERR_INVALID_ARG;
     for (int32_t i = 0; i < 3 * steps; ++i)
         if (!(coefficients[i] >= -1e6f && coefficients[i] <= 1e6f)) return MOE_ERR_INVALID_ARG;
     const int64_t most = (int64_t)1 << 40;

@@ -16,6 +16,8 @@
 // reductions, as 768, for tiles' beginnings and ends.
 #include "moe_orth.h"
 
+#include <math.h>
+
 #include <initializer_list>
 
 namespace {
@@ -332,14 +334,14 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 }
 
 // ---- between S and the next product with X, for matrices of up to 128 rows ----
-// Of two steps' Q = a I + b S + c S S the product, from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
+// Of two steps' Q = a I + b S + c S S the product, times `joint`, from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
 // of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  Up to 64 rows
 // all four products of the parts are formed: the smallest matrices have few values to average over (4 x 16 x 400 in fp32: 1.5 times the error of 32-bit products with
 // three, 1.2 to 1.3 with four; 8 x 128 x 256: 1.1 and 1.05, but 80 us and 85).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
 // latencies are half of what it takes (8 matrices of 128 rows, two steps: 19 us, 7 of them the products' own; unrolled with all its products 54; only the
 // columns from the diagonal on, half the products, but branches, 28).
-template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2) {
+template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2, float joint) {
     extern __shared__ __align__(1024) char lds[];
     constexpr int KB = NF / 2, FN = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
     char *s = lds, *q = lds + 2 * PLANE;
@@ -399,7 +401,7 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
             });
             __builtin_amdgcn_sched_barrier(0);
         });
-        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : 1.f / Q_SCALE;
+        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : op == last ? joint / (Q_SCALE * Q_SCALE) : 1.f / Q_SCALE;
         each([&](int m, int n) { v[m][n] *= scale; });
         if (sum) {
             const float ca = (op == 0 ? a1 : a2) * Q_SCALE, cb = (op == 0 ? b1 : b2) * (Q_SCALE / S_SCALE);
@@ -882,6 +884,47 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
     }
 }
 
+// ---- ranges of the operands ----
+// The largest power of two up to `most` with which values up to `bound` take half of fp16's range at most.
+float scale_for(double bound, float most) {
+    const double room = 32752.0 / bound;
+    return room >= most ? most : (float)exp2(floor(log2(room)));
+}
+
+// Bounds of a step, from its coefficients and those before it, for any matrix: |G| is at least its largest singular value, so X begins with singular values
+// in [0, 1]; on [0, s] those of Q lie in the range of a + b t + c t^2 for t in [0, s^2], and the next X's in that of their products with s.
+// An entry of a matrix is at most its largest singular value.  Small singular values (and padded rows) take Q's value at 0, which is a.
+struct Bounds {
+    double x;  // singular values of X before the step
+    double q;  // ... of Q
+};
+void bounds_of(const float* coefficients, int steps, Bounds* z) {
+    double x = 1;
+    for (int k = 0; k < steps; ++k) {
+        const double a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2], end = x * x;
+        auto q = [&](double t) { return fabs(a + b * t + c * t * t); };
+        z[k] = {x, fmax(q(0), q(end))};
+        double next = x * q(end);
+        if (c != 0) {
+            const double t = -b / (2 * c);  // where Q's has its extreme
+            if (t > 0 && t < end) z[k].q = fmax(z[k].q, q(t));
+        }
+        // extremes of s q(s^2): a + 3 b t + 5 c t^2 = 0
+        const double d = 9 * b * b - 20 * a * c;
+        for (int i = 0; i < 2; ++i) {
+            const double t = c != 0 ? (d >= 0 ? (-3 * b + (i ? sqrt(d) : -sqrt(d))) / (10 * c) : -1) : b != 0 ? -a / (3 * b) : -1;
+            if (t > 0 && t < end) next = fmax(next, sqrt(t) * q(t));
+        }
+        x = next;
+    }
+}
+// Two steps' Q' Q is kept times this: with entries up to |Q'| |Q| (11.9 of the default coefficients; 34 where the first steps raise small singular values most,
+// which Q_SCALE would take past fp16).  0: they are taken one by one, rather than lose more than 3 bits of the smallest entries.
+float joint_scale(const Bounds& one, const Bounds& two) {
+    const float scale = scale_for(one.q * two.q, Q_SCALE);
+    return scale >= Q_SCALE / 8 ? scale : 0.f;
+}
+
 // ---- plan ----
 struct Size {
     int n, m;        // of X, padded
@@ -1024,6 +1067,10 @@ template <bool F32> struct Steps {
     int count;
     void* out;
     hipStream_t st;
+    const Bounds* bounds;  // of each step
+
+    // Scale of the next two steps' product, 0 where they are taken one by one
+    float pair(int k) const { return k + 2 <= t.steps ? joint_scale(bounds[k], bounds[k + 1]) : 0.f; }
 
     OrthArgs square(const OrthOperand& a, const OrthOperand& b, const OrthOperand& c, float alpha) const {  // c = alpha a b, symmetric
         OrthArgs g = {};
@@ -1049,8 +1096,8 @@ template <bool F32> struct Steps {
         const int size = F32 ? 4 : 2;
         g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
     }
-    // X = q X, into the other buffer or to the caller; where q has one part, q of X's first part and, of the second, its diagonal's share alone
-    template <bool TWO> hipError_t apply(const OrthOperand& q, bool last) {
+    // X = q X, q times `scale`, into the other buffer or to the caller; where q has one part, q of X's first part and, of the second, its diagonal's share alone
+    template <bool TWO> hipError_t apply(const OrthOperand& q, float scale, bool last) {
         constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 1;
         OrthArgs g = {};
         g.matrices = count;
@@ -1061,7 +1108,7 @@ template <bool F32> struct Steps {
         g.cin.part[0] = w.x[0].part[1];
         g.own = w.own;
         g.steps = z.n / 32;
-        g.alpha = 1.f / Q_SCALE;
+        g.alpha = 1.f / scale;
         g.beta = 1.f;
         g.part = w.part;
         hipError_t e;
@@ -1091,28 +1138,28 @@ template <bool F32> struct Steps {
         g.own = F32 ? nullptr : w.own;
         return product<PARTS, PARTS, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
-    // to = a q, of matrices that commute
-    hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to) const {
-        return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, 1.f / Q_SCALE), z.tile, st);
+    // to = a q times alpha, of matrices that commute
+    hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to, float alpha) const {
+        return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, alpha), z.tile, st);
     }
     hipError_t one_step(const float* abc, bool last) {
         hipError_t e = gram();
         if (e == hipSuccess) e = polynomial(w.q, abc);
-        if (e == hipSuccess) e = apply<F32>(w.q, last);
+        if (e == hipSuccess) e = apply<F32>(w.q, Q_SCALE, last);
         return e;
     }
-    hipError_t two_steps(const float* abc, bool last) {
+    hipError_t two_steps(const float* abc, float joint, bool last) {
         hipError_t e = gram();
         if (e == hipSuccess) e = polynomial(w.q, abc);
-        if (e == hipSuccess) e = times(w.s, w.q, w.t);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s);  // Q S Q = (Q X) (Q X)^T
+        if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / Q_SCALE);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / Q_SCALE);  // Q S Q = (Q X) (Q X)^T
         if (e == hipSuccess) e = polynomial(w.t, abc + 3);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s);
-        if (e == hipSuccess) e = apply<true>(w.s, last);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, joint / (Q_SCALE * Q_SCALE));
+        if (e == hipSuccess) e = apply<true>(w.s, joint, last);
         return e;
     }
     // Two steps' Q in one launch
-    template <int NF> hipError_t link(float* sums, const OrthArgs& of, const float* abc) {
+    template <int NF> hipError_t link(float* sums, const OrthArgs& of, const float* abc, float joint) {
         OrthArgs g = {};
         g.part = sums;
         g.c = w.q;
@@ -1120,7 +1167,7 @@ template <bool F32> struct Steps {
         auto kernel = orth_chain_kernel<NF>;
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        kernel<<<count, NF * 64, bytes, st>>>(g, of.apart, of.ranges, abc[0], abc[1], abc[2], abc[3], abc[4], abc[5]);
+        kernel<<<count, NF * 64, bytes, st>>>(g, of.apart, of.ranges, abc[0], abc[1], abc[2], abc[3], abc[4], abc[5], joint);
         return hipGetLastError();
     }
     // Matrices of up to 128 rows (16 NF padded)
@@ -1149,8 +1196,8 @@ template <bool F32> struct Steps {
         // or Q larger (8 x 16 x 14336 in bf16: 65 us in pairs, 83 one by one; 8 x 128 x 256: 85 and 95).
         const bool pairs = NF == 8 || (!F32 && groups > 8);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
-            const float* abc = t.coefficients + 3 * k;
+            const float joint = pairs ? pair(k) : 0.f, *abc = t.coefficients + 3 * k;
+            const int n = joint > 0 ? 2 : 1;
             k += n;
             // many ranges are added in a launch of their own, from more of the larger sums on (8 x 100 x 500, 8 of them: 100 us with it, 121 without; 64 x 64 x 300,
             // 3: 84 and 77; 8 x 64 x 2000, 16: 54 and 60)
@@ -1160,12 +1207,12 @@ template <bool F32> struct Steps {
                 e = hipGetLastError();
                 g.ranges = 1;
             }
-            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, abc);
+            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, abc, joint);
             if (e != hipSuccess) break;
             g.sums = sums, g.part = next;
             for (int j = 0; j < 3; ++j) g.abc[j] = abc[j];
             g.b = w.x[0], g.c = w.x[1];
-            g.alpha = 1.f / Q_SCALE;
+            g.alpha = 1.f / (n == 2 ? joint : Q_SCALE);
             constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
                 e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g, false) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g, true);
@@ -1190,11 +1237,10 @@ template <bool F32> struct Steps {
         const bool pairs = F32 && time.s + time.x > 3 * time.square;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const int n = pairs && k + 2 <= t.steps ? 2 : 1;
-            const float* abc = t.coefficients + 3 * k;
-            k += n;
+            const float joint = pairs ? pair(k) : 0.f, *abc = t.coefficients + 3 * k;
+            k += joint > 0 ? 2 : 1;
             const bool last = k == t.steps;
-            if constexpr (F32) e = n == 2 ? two_steps(abc, last) : one_step(abc, last);
+            if constexpr (F32) e = joint > 0 ? two_steps(abc, joint, last) : one_step(abc, last);
             else e = one_step(abc, last);
         }
         return e;
@@ -1223,6 +1269,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
     const int64_t part = turn < t.E ? kPartBytes : part_bytes(t.E, z);
     const bool tall = t.rows > t.cols;
     const int size_in = t.in_f32 ? 4 : 2, size_out = t.out_f32 ? 4 : 2;
+    Bounds bounds[ORTH_MAX_STEPS];
+    bounds_of(t.coefficients, t.steps, bounds);
     for (int e0 = 0; e0 < t.E; e0 += turn) {
         const int count = t.E - e0 < turn ? t.E - e0 : turn;
         char* at = (char*)workspace;
@@ -1256,7 +1304,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         void* out = (char*)t.out + e0 * t.out_matrix * size_out;
-        e = t.out_f32 ? Steps<true>{t, z, w, count, out, st}.run() : Steps<false>{t, z, w, count, out, st}.run();
+        e = t.out_f32 ? Steps<true>{t, z, w, count, out, st, bounds}.run() : Steps<false>{t, z, w, count, out, st, bounds}.run();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -1,0 +1,46 @@
+"""Orthogonalised updates with other coefficients for each step, against the same steps in 64 bits: bounds as in test_gpu_orthogonalize.
+
+With two steps taken at a time the product of two steps' Q = a I + b S + c S S is formed, whose entries reach a a' along small singular values (and on
+padded rows): 34.0 and 33.0 for the first two triples of these schedules, whose first steps raise small singular values by as much as keeps the largest near 2."""
+import pytest
+import torch
+
+import paper_2605_19945_amd as moe
+from test_gpu_orthogonalize import BF16, F32, check, gradient
+
+pytestmark = pytest.mark.gpu
+
+RAISING = [(8.28721201814563, -23.595886519098837, 17.300387312530933), (4.107059111542203, -2.9478499167379106, 0.5448431082926601),
+           (3.9486908534822946, -2.908902115962949, 0.5518191394370137), (3.3184196573706015, -2.488488024314874, 0.51004894012372),
+           (2.300652019954817, -1.6689039845747493, 0.4188073119525673), (1.891301407787398, -1.2679958271945868, 0.37680408948524835),
+           (1.875, -1.25, 0.375)]
+DAMPED = [(a / 1.01, b / 1.01 ** 3, c / 1.01 ** 5) for a, b, c in RAISING[:-1]] + RAISING[-1:]   # so that rounding does not lead out of their range
+
+
+@pytest.mark.parametrize("E,rows,cols", [(2, 24, 83), (8, 128, 256), (1, 100, 2000), (1, 2000, 100), (1, 16, 14336), (3, 60, 4000), (1, 300, 500), (1, 512, 4096), (8, 1024, 4096),
+                                         (32, 330, 4100)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["gauss", "steep"])
+def test_schedules_against_64_bits(E, rows, cols, dtype, kind):
+    G = gradient((E, rows, cols), E + rows + cols, dtype, kind).cuda()
+    for schedule in (RAISING, DAMPED):
+        for steps in (2, 5, 7):
+            got = moe.moe_orthogonalize(G, steps=steps, coefficients=schedule[:steps])
+            assert torch.isfinite(got).all(), (steps, schedule[0])
+            check(got[:2], G[:2], schedule[:steps])
+
+
+def test_a_schedule_on_a_large_stack():
+    G = gradient((128, 768, 2048), 1, F32, "steep").cuda()
+    got = moe.moe_orthogonalize(G, steps=5, coefficients=DAMPED[:5])
+    assert torch.isfinite(got).all()
+    check(got[126:], G[126:], DAMPED[:5])
+
+
+@pytest.mark.parametrize("rows,cols", [(24, 83), (100, 500), (16, 14336), (300, 4000)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_zeros_stay_zeros(rows, cols, dtype):
+    G = gradient((2, rows, cols), 2, dtype).cuda()
+    G[0] = 0
+    got = moe.moe_orthogonalize(G, steps=6, coefficients=RAISING[:6])
+    assert not got[0].any() and torch.isfinite(got[1]).all()
