@@ -303,9 +303,11 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  *   out = scale X
  * (where rows > cols: the same on the transpose).  coefficients: host, [steps][3], read before the call returns; steps from 1 to 64.
  * Operands of the products are kept in one or two 16-bit parts, sums in 32 bits, |g| in 64: an fp32 result is as far from the exact one
- * as with products in 32 bits, a bf16 result about as far as its own rounding.  Singular values up to 4 and entries of b S + c S S up to 16 are
- * in range on the way (coefficients that keep the singular values below 1.5, as such steps do, stay far below).  A matrix of zeros gives
- * zeros (eps > 0); one that holds a NaN or an infinity gives NaN and spoils no other.
+ * as with products in 32 bits, a bf16 result about as far as its own rounding.  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
+ * from bounds that hold for any matrix: |X| begins at 1, and a s + b s^3 + c s^5 bounds what a step makes of it.  Steps whose bounds of the singular values
+ * before each step stay below 16, and of a + b s^2 + c s^4 below 4000, never leave their range (the usual schedules: 2 and 9); with others a
+ * matrix whose own singular values do gives NaN or infinities.  One that holds a NaN or an infinity gives NaN.  Neither spoils another.  A matrix of
+ * zeros gives zeros (eps > 0).
  * g and out: rows ldg / ldout values apart (at least cols), matrices stride_g / stride_out values apart, pointers aligned to their values; any
  * sizes from 1 to 2^17, rows * cols <= 2^29, E <= 256.  out may be exactly g (of the same type); otherwise they share no byte.
  * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done; about 8 bytes for every

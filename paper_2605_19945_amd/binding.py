@@ -1002,7 +1002,7 @@ def _stack(what, name, t):
 def moe_orthogonalize(g, steps=5, scale=1.0, eps=1e-7, coefficients=(3.4445, -4.7750, 2.0315), out=None, dtype=None):
     """Each matrix of g [rows, cols] or [E, rows, cols] (float32 or bfloat16) near the orthogonal matrix next to it: X = g / (|g| + eps),
     then `steps` times X = a X + (b S + c S S) X with S = X X^T (rows > cols: on the transpose), times scale; of `dtype`, g's by default.
-    coefficients: (a, b, c), or one such triple for each step.  out may be g.  Views whose last dimension is contiguous are taken as they are."""
+    coefficients: (a, b, c), or one such triple for each step; |a| up to 4000.  out may be g.  Views whose last dimension is contiguous are taken as they are."""
     lib, what = _lib or load_library(), "moe_orthogonalize"
     _no_graphs(what, g, out)
     E, rows, cols, stride, ld = _stack(what, "g", g)

@@ -55,6 +55,7 @@ hipError_t launch_norm_backward(NormGradArgs a, float* dw, float* dw_next, float
 
 // ---- orthogonalised updates ----
 constexpr int ORTH_MAX_STEPS = 64;
+constexpr float ORTH_MOST_A = 4000.f;   // what the fp16 parts of a I + b S + c S S hold beside values near 1
 struct OrthTask {
     const void* g;
     void* out;

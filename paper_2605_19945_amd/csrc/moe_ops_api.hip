@@ -357,7 +357,7 @@ moe_status moe_orthogonalize(const void* g, int32_t type, int64_t stride_g, int6
     if (g == nullptr || out == nullptr || !aligned(g, size_of(type)) || !aligned(out, size_of(out_type))) return MOE_ERR_INVALID_ARG;
     if (coefficients == nullptr || steps < 1 || steps > ORTH_MAX_STEPS || !(eps >= 0.f) || eps > 3e38f || !(scale >= -3e38f && scale <= 3e38f)) return MOE_ERR_INVALID_ARG;
     for (int32_t i = 0; i < 3 * steps; ++i)
-        if (!(coefficients[i] >= -1e6f && coefficients[i] <= 1e6f)) return MOE_ERR_INVALID_ARG;
+        if (const float most = i % 3 == 0 ? ORTH_MOST_A : 1e6f; !(coefficients[i] >= -most && coefficients[i] <= most)) return MOE_ERR_INVALID_ARG;
     const int64_t most = (int64_t)1 << 40;
     if (ldg < cols || ldout < cols || ldg > kMaxLd || ldout > kMaxLd) return MOE_ERR_INVALID_ARG;
     // matrices of a stack lie one behind the other, or side by side in the same rows

@@ -30,6 +30,7 @@ struct OrthArgs {
     OrthOperand c;         // the result
     float alpha, beta;
     float diagonal;        // added to the diagonal of a symmetric result
+    float unscale;         // `own` is the diagonal times this
     int square;            // rows of a symmetric operand
     int steps;             // blocks of the reduction
     int whole;             // of all matrices' tiles the first `whole` take their reduction whole; the others' is cut into `splits` ranges, whose
@@ -40,13 +41,18 @@ struct OrthArgs {
     // of matrices of up to 128 rows: S in `ranges` sums, `apart` of them a matrix, of which the coefficients give Q
     const float* sums;
     int ranges, apart;
-    float abc[3];
+    float from, abc[3];    // S = from times the sums; Q = a I + b S + c S S of S and Q as they are kept
     // the last product: results in the caller's rows
     void* out;
     int64_t out_matrix, out_ld;  // values from one matrix, one row to the next
     int rows, cols;              // of C that exist
     int tall;                    // C is the transpose of what the caller has
     int vec;                     // groups of 4 values are aligned
+};
+
+// Two steps at a time, of matrices of up to 128 rows: as from and abc above; S Q's and Q S Q's products times `through`, Q' Q's times `joint`
+struct OrthPair {
+    float from, abc[2][3], through, joint;
 };
 
 enum { ORTH_SQUARE = 0, ORTH_BLOCKS = 1, ORTH_BF16 = 2, ORTH_F32 = 3 };

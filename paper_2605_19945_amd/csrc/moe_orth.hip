@@ -22,9 +22,11 @@
 
 namespace {
 
-// X, S and P are held times these powers of two: in the middle of fp16's range, singular values up to 4 allowed for, so that the
-// second parts are seldom subnormal.
+// X, S and Q = a I + b S + c S S are held times powers of two: in the middle of fp16's range, so that the second parts are seldom subnormal.  These where
+// the coefficients allow them, which the usual ones do (singular values below 2 on the way, Q up to 8); less where they lead further, down to these
+// (singular values of 16, Q of 4094, where the smallest values still have 20 bits).
 constexpr float X_SCALE = 8192.f, S_SCALE = 4096.f, Q_SCALE = 2048.f;
+constexpr float X_LEAST = 1024.f, S_LEAST = 64.f, Q_LEAST = 8.f;
 
 // ---- the products ----
 // Tile t of a symmetric matrix's mt x mt, row by row on and above the diagonal
@@ -86,7 +88,7 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
             if (g.own != nullptr && (r == c || r == c + 16)) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (4 * q + j == i) g.own[(int64_t)matrix * g.square + r + i] = (r == c ? u[j] : v[j]) * (1.f / Q_SCALE);
+                    if (4 * q + j == i) g.own[(int64_t)matrix * g.square + r + i] = (r == c ? u[j] : v[j]) * g.unscale;
                 }
             }
         }
@@ -334,14 +336,14 @@ __global__ __launch_bounds__(256) void orth_fold_kernel(float* part, int splits,
 }
 
 // ---- between S and the next product with X, for matrices of up to 128 rows ----
-// Of two steps' Q = a I + b S + c S S the product, times `joint`, from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
+// Of two steps' Q = a I + b S + c S S the product from S's ranges.  One workgroup of NF wavefronts a matrix, everything in LDS: two matrices
 // of 16 NF rows in two parts, in blocks.  A wavefront has 2 x NF / 2 fragments.  Up to 64 rows
 // all four products of the parts are formed: the smallest matrices have few values to average over (4 x 16 x 400 in fp32: 1.5 times the error of 32-bit products with
 // three, 1.2 to 1.3 with four; 8 x 128 x 256: 1.1 and 1.05, but 80 us and 85).
 // One loop over the products, each with a loop over the reduction, and no branches in them: the code is run from end to end once or a few times, and
 // latencies are half of what it takes (8 matrices of 128 rows, two steps: 19 us, 7 of them the products' own; unrolled with all its products 54; only the
 // columns from the diagonal on, half the products, but branches, 28).
-template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, float a1, float b1, float c1, float a2, float b2, float c2, float joint) {
+template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(OrthArgs g, int apart, int splits, OrthPair pair) {
     extern __shared__ __align__(1024) char lds[];
     constexpr int KB = NF / 2, FN = NF / 2, PLANE = NF * KB * ORTH_BLOCK;
     char *s = lds, *q = lds + 2 * PLANE;
@@ -371,7 +373,7 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
 #pragma unroll 4
     for (int r = 0; r < splits; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + col0 + n) * 64]; });
-    each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
+    each([&](int m, int n) { v[m][n] *= pair.from; });
     put(s, PLANE, KB);
     __syncthreads();
     constexpr int last = 4;  // of the products
@@ -401,10 +403,11 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
             });
             __builtin_amdgcn_sched_barrier(0);
         });
-        const float scale = sum ? (op == 0 ? c1 : c2) * (Q_SCALE / (S_SCALE * S_SCALE)) : op == last ? joint / (Q_SCALE * Q_SCALE) : 1.f / Q_SCALE;
+        const float* abc = pair.abc[op == 0 ? 0 : 1];
+        const float scale = sum ? abc[2] : op == last ? pair.joint : pair.through;
         each([&](int m, int n) { v[m][n] *= scale; });
         if (sum) {
-            const float ca = (op == 0 ? a1 : a2) * Q_SCALE, cb = (op == 0 ? b1 : b2) * (Q_SCALE / S_SCALE);
+            const float ca = abc[0], cb = abc[1];
             each([&](int m, int n) {
                 const u32x2_t hi = *(const u32x2_t*)(s + at(m, n, KB)), lo = *(const u32x2_t*)(s + PLANE + at(m, n, KB));
 #pragma unroll
@@ -464,7 +467,7 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
 #pragma unroll 2
     for (int r = 0; r < g.ranges; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + n) * 64]; });
-    each([&](int m, int n) { v[m][n] *= S_SCALE / (X_SCALE * X_SCALE); });
+    each([&](int m, int n) { v[m][n] *= g.from; });
     if (on) put();
     __syncthreads();
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
@@ -483,7 +486,7 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
             each([&](int m, int n) { v[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[r][n], a[p][m], v[m][n], 0, 0, 0); });
         });
     }
-    const float scale = g.abc[2] * (Q_SCALE / (S_SCALE * S_SCALE)), ca = g.abc[0] * Q_SCALE, cb = g.abc[1] * (Q_SCALE / S_SCALE);
+    const float scale = g.abc[2], ca = g.abc[0], cb = g.abc[1];
     each([&](int m, int n) {
         const u32x2_t hi = *(const u32x2_t*)(s + at(m, n)), lo = *(const u32x2_t*)(s + PLANE + at(m, n));
 #pragma unroll
@@ -885,29 +888,31 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
 }
 
 // ---- ranges of the operands ----
-// The largest power of two up to `most` with which values up to `bound` take half of fp16's range at most.
-float scale_for(double bound, float most) {
+// The largest power of two from `least` to `most` with which values up to `bound` take half of fp16's range at most.
+float scale_for(double bound, float most, float least) {
     const double room = 32752.0 / bound;
-    return room >= most ? most : (float)exp2(floor(log2(room)));
+    return room >= most ? most : fmaxf((float)exp2(floor(log2(room))), least);
 }
 
 // Bounds of a step, from its coefficients and those before it, for any matrix: |G| is at least its largest singular value, so X begins with singular values
 // in [0, 1]; on [0, s] those of Q lie in the range of a + b t + c t^2 for t in [0, s^2], and the next X's in that of their products with s.
 // An entry of a matrix is at most its largest singular value.  Small singular values (and padded rows) take Q's value at 0, which is a.
-struct Bounds {
-    double x;  // singular values of X before the step
-    double q;  // ... of Q
+// (Steps that lead past all range for some matrix may stay in range for others, and are held for those.)
+struct Range {
+    double most;             // the largest of Q's
+    float x, s, q;           // scales of X before the step, of S and Q
+    float from;              // S's over that of X X^T
+    void coefficients(const float* c, float* abc) const { abc[0] = c[0] * q, abc[1] = c[1] * (q / s), abc[2] = c[2] * (q / (s * s)); }  // of products as they are kept
 };
-void bounds_of(const float* coefficients, int steps, Bounds* z) {
+void ranges_of(const float* coefficients, int steps, Range* z) {
     double x = 1;
     for (int k = 0; k < steps; ++k) {
         const double a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2], end = x * x;
         auto q = [&](double t) { return fabs(a + b * t + c * t * t); };
-        z[k] = {x, fmax(q(0), q(end))};
-        double next = x * q(end);
+        double most = fmax(q(0), q(end)), next = x * q(end);
         if (c != 0) {
             const double t = -b / (2 * c);  // where Q's has its extreme
-            if (t > 0 && t < end) z[k].q = fmax(z[k].q, q(t));
+            if (t > 0 && t < end) most = fmax(most, q(t));
         }
         // extremes of s q(s^2): a + 3 b t + 5 c t^2 = 0
         const double d = 9 * b * b - 20 * a * c;
@@ -915,13 +920,15 @@ void bounds_of(const float* coefficients, int steps, Bounds* z) {
             const double t = c != 0 ? (d >= 0 ? (-3 * b + (i ? sqrt(d) : -sqrt(d))) / (10 * c) : -1) : b != 0 ? -a / (3 * b) : -1;
             if (t > 0 && t < end) next = fmax(next, sqrt(t) * q(t));
         }
+        z[k] = {most, scale_for(x, X_SCALE, X_LEAST), scale_for(2 * end, S_SCALE, S_LEAST), scale_for(most, Q_SCALE, Q_LEAST), 0.f};  // (twice its range for X, so four times for S)
+        z[k].from = z[k].s / (z[k].x * z[k].x);
         x = next;
     }
 }
 // Two steps' Q' Q is kept times this: with entries up to |Q'| |Q| (11.9 of the default coefficients; 34 where the first steps raise small singular values most,
 // which Q_SCALE would take past fp16).  0: they are taken one by one, rather than lose more than 3 bits of the smallest entries.
-float joint_scale(const Bounds& one, const Bounds& two) {
-    const float scale = scale_for(one.q * two.q, Q_SCALE);
+float joint_scale(const Range& one, const Range& two) {
+    const float scale = scale_for(one.most * two.most, Q_SCALE, 0.f);
     return scale >= Q_SCALE / 8 ? scale : 0.f;
 }
 
@@ -1067,10 +1074,10 @@ template <bool F32> struct Steps {
     int count;
     void* out;
     hipStream_t st;
-    const Bounds* bounds;  // of each step
+    const Range* ranges;  // of each step
 
     // Scale of the next two steps' product, 0 where they are taken one by one
-    float pair(int k) const { return k + 2 <= t.steps ? joint_scale(bounds[k], bounds[k + 1]) : 0.f; }
+    float pair(int k) const { return k + 2 <= t.steps ? joint_scale(ranges[k], ranges[k + 1]) : 0.f; }
 
     OrthArgs square(const OrthOperand& a, const OrthOperand& b, const OrthOperand& c, float alpha) const {  // c = alpha a b, symmetric
         OrthArgs g = {};
@@ -1084,9 +1091,12 @@ template <bool F32> struct Steps {
         g.square = z.n;
         return g;
     }
+    // q X of the steps before `next`: into X's other buffer, or to the caller
+    void scale(OrthArgs& g, int k, int next, float q) const {
+        g.beta = (next < t.steps ? ranges[next].x : t.scale) / ranges[k].x;
+        g.alpha = g.beta / q;
+    }
     void to_caller(OrthArgs& g) const {
-        g.alpha *= t.scale / X_SCALE;
-        g.beta *= t.scale / X_SCALE;
         g.out = out;
         g.out_matrix = t.out_matrix;
         g.out_ld = t.out_ld;
@@ -1096,8 +1106,8 @@ template <bool F32> struct Steps {
         const int size = F32 ? 4 : 2;
         g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
     }
-    // X = q X, q times `scale`, into the other buffer or to the caller; where q has one part, q of X's first part and, of the second, its diagonal's share alone
-    template <bool TWO> hipError_t apply(const OrthOperand& q, float scale, bool last) {
+    // X = q X of the steps from k to next; where q has one part, q of X's first part and, of the second, its diagonal's share alone
+    template <bool TWO> hipError_t apply(const OrthOperand& q, float q_scale, int k, int next) {
         constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 1;
         OrthArgs g = {};
         g.matrices = count;
@@ -1108,11 +1118,10 @@ template <bool F32> struct Steps {
         g.cin.part[0] = w.x[0].part[1];
         g.own = w.own;
         g.steps = z.n / 32;
-        g.alpha = 1.f / scale;
-        g.beta = 1.f;
+        scale(g, k, next, q_scale);
         g.part = w.part;
         hipError_t e;
-        if (!last) {
+        if (next < t.steps) {
             e = product<PARTS, PARTS, true, CIN, !TWO, 2, ORTH_BLOCKS>(g, z.tile, st);
         } else {
             to_caller(g);
@@ -1124,17 +1133,20 @@ template <bool F32> struct Steps {
         return e;
     }
     // S = X X^T
-    hipError_t gram() const {
+    hipError_t gram(const Range& r) const {
         constexpr int PARTS = F32 ? 2 : 1;
-        return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, S_SCALE / (X_SCALE * X_SCALE)), z.tile, st);
+        return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, r.from), z.tile, st);
     }
     // to = a I + b S + c S S, and where it has one part its diagonal in 32 bits
-    hipError_t polynomial(const OrthOperand& to, const float* abc) const {
+    hipError_t polynomial(const OrthOperand& to, int k, const Range& r) const {
         constexpr int PARTS = F32 ? 2 : 1;
-        OrthArgs g = square(w.s, w.s, to, abc[2] * Q_SCALE / (S_SCALE * S_SCALE));
+        float abc[3];
+        r.coefficients(t.coefficients + 3 * k, abc);
+        OrthArgs g = square(w.s, w.s, to, abc[2]);
         g.cin = w.s;
-        g.beta = abc[1] * Q_SCALE / S_SCALE;
-        g.diagonal = abc[0] * Q_SCALE;
+        g.beta = abc[1];
+        g.diagonal = abc[0];
+        g.unscale = 1.f / r.q;
         g.own = F32 ? nullptr : w.own;
         return product<PARTS, PARTS, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
@@ -1142,32 +1154,47 @@ template <bool F32> struct Steps {
     hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to, float alpha) const {
         return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, alpha), z.tile, st);
     }
-    hipError_t one_step(const float* abc, bool last) {
-        hipError_t e = gram();
-        if (e == hipSuccess) e = polynomial(w.q, abc);
-        if (e == hipSuccess) e = apply<F32>(w.q, Q_SCALE, last);
+    hipError_t one_step(int k) {
+        const Range& r = ranges[k];
+        hipError_t e = gram(r);
+        if (e == hipSuccess) e = polynomial(w.q, k, r);
+        if (e == hipSuccess) e = apply<F32>(w.q, r.q, k, k + 1);
         return e;
     }
-    hipError_t two_steps(const float* abc, float joint, bool last) {
-        hipError_t e = gram();
-        if (e == hipSuccess) e = polynomial(w.q, abc);
-        if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / Q_SCALE);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / Q_SCALE);  // Q S Q = (Q X) (Q X)^T
-        if (e == hipSuccess) e = polynomial(w.t, abc + 3);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s, joint / (Q_SCALE * Q_SCALE));
-        if (e == hipSuccess) e = apply<true>(w.s, joint, last);
+    // S of both steps by the scale that holds both
+    void together(int k, Range& one, Range& two) const {
+        one = ranges[k], two = ranges[k + 1];
+        one.s = two.s = fminf(one.s, two.s);
+        one.from = one.s / (one.x * one.x);
+    }
+    hipError_t two_steps(int k, float joint) {
+        Range one, two;
+        together(k, one, two);
+        hipError_t e = gram(one);
+        if (e == hipSuccess) e = polynomial(w.q, k, one);
+        if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / one.q);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / one.q);  // Q S Q = (Q X) (Q X)^T
+        if (e == hipSuccess) e = polynomial(w.t, k + 1, two);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, joint / (one.q * two.q));
+        if (e == hipSuccess) e = apply<true>(w.s, joint, k, k + 2);
         return e;
     }
     // Two steps' Q in one launch
-    template <int NF> hipError_t link(float* sums, const OrthArgs& of, const float* abc, float joint) {
+    template <int NF> hipError_t link(float* sums, const OrthArgs& of, int k, float joint) {
         OrthArgs g = {};
         g.part = sums;
         g.c = w.q;
+        Range one, two;
+        together(k, one, two);
+        OrthPair p = {};
+        p.from = one.from, p.through = 1.f / one.q, p.joint = joint / (one.q * two.q);
+        one.coefficients(t.coefficients + 3 * k, p.abc[0]);
+        two.coefficients(t.coefficients + 3 * k + 3, p.abc[1]);
         constexpr int bytes = 4 * NF * (NF / 2) * ORTH_BLOCK;
         auto kernel = orth_chain_kernel<NF>;
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
-        kernel<<<count, NF * 64, bytes, st>>>(g, of.apart, of.ranges, abc[0], abc[1], abc[2], abc[3], abc[4], abc[5], joint);
+        kernel<<<count, NF * 64, bytes, st>>>(g, of.apart, of.ranges, p);
         return hipGetLastError();
     }
     // Matrices of up to 128 rows (16 NF padded)
@@ -1196,9 +1223,8 @@ template <bool F32> struct Steps {
         // or Q larger (8 x 16 x 14336 in bf16: 65 us in pairs, 83 one by one; 8 x 128 x 256: 85 and 95).
         const bool pairs = NF == 8 || (!F32 && groups > 8);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const float joint = pairs ? pair(k) : 0.f, *abc = t.coefficients + 3 * k;
+            const float joint = pairs ? pair(k) : 0.f;
             const int n = joint > 0 ? 2 : 1;
-            k += n;
             // many ranges are added in a launch of their own, from more of the larger sums on (8 x 100 x 500, 8 of them: 100 us with it, 121 without; 64 x 64 x 300,
             // 3: 84 and 77; 8 x 64 x 2000, 16: 54 and 60)
             g.apart = g.ranges = groups;
@@ -1207,12 +1233,14 @@ template <bool F32> struct Steps {
                 e = hipGetLastError();
                 g.ranges = 1;
             }
-            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, abc, joint);
+            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, k, joint);
             if (e != hipSuccess) break;
             g.sums = sums, g.part = next;
-            for (int j = 0; j < 3; ++j) g.abc[j] = abc[j];
+            ranges[k].coefficients(t.coefficients + 3 * k, g.abc);
+            g.from = ranges[k].from;
             g.b = w.x[0], g.c = w.x[1];
-            g.alpha = 1.f / (n == 2 ? joint : Q_SCALE);
+            scale(g, k, k + n, n == 2 ? joint : ranges[k].q);
+            k += n;
             constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
                 e = n == 2 ? launch(step_kernel<NF, 1, ORTH_BLOCKS, false>(), g, false) : launch(step_kernel<NF, 1, ORTH_BLOCKS, true>(), g, true);
@@ -1237,11 +1265,10 @@ template <bool F32> struct Steps {
         const bool pairs = F32 && time.s + time.x > 3 * time.square;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const float joint = pairs ? pair(k) : 0.f, *abc = t.coefficients + 3 * k;
+            const float joint = pairs ? pair(k) : 0.f;
+            if constexpr (F32) e = joint > 0 ? two_steps(k, joint) : one_step(k);
+            else e = one_step(k);
             k += joint > 0 ? 2 : 1;
-            const bool last = k == t.steps;
-            if constexpr (F32) e = joint > 0 ? two_steps(abc, joint, last) : one_step(abc, last);
-            else e = one_step(abc, last);
         }
         return e;
     }
@@ -1269,8 +1296,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
     const int64_t part = turn < t.E ? kPartBytes : part_bytes(t.E, z);
     const bool tall = t.rows > t.cols;
     const int size_in = t.in_f32 ? 4 : 2, size_out = t.out_f32 ? 4 : 2;
-    Bounds bounds[ORTH_MAX_STEPS];
-    bounds_of(t.coefficients, t.steps, bounds);
+    Range ranges[ORTH_MAX_STEPS];
+    ranges_of(t.coefficients, t.steps, ranges);
     for (int e0 = 0; e0 < t.E; e0 += turn) {
         const int count = t.E - e0 < turn ? t.E - e0 : turn;
         char* at = (char*)workspace;
@@ -1304,7 +1331,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         void* out = (char*)t.out + e0 * t.out_matrix * size_out;
-        e = t.out_f32 ? Steps<true>{t, z, w, count, out, st, bounds}.run() : Steps<false>{t, z, w, count, out, st, bounds}.run();
+        e = t.out_f32 ? Steps<true>{t, z, w, count, out, st, ranges}.run() : Steps<false>{t, z, w, count, out, st, ranges}.run();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -44,3 +44,16 @@ def test_zeros_stay_zeros(rows, cols, dtype):
     G[0] = 0
     got = moe.moe_orthogonalize(G, steps=6, coefficients=RAISING[:6])
     assert not got[0].any() and torch.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("E,rows,cols", [(2, 24, 83), (2, 100, 500), (1, 16, 14336), (2, 300, 400), (4, 520, 2100)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_coefficients(E, rows, cols, dtype):
+    """Entries of Q past 32, and singular values past 4: the largest of the first schedule is 9.9 after its first step for some matrices; the others' bounds
+    lead past all range, but no singular value of these matrices does."""
+    for steps in ([(33.0, -60.0, 28.0), (0.3, -0.002, 1e-6)], [(31.0, 0.0, 0.0)], [(-33.0, 0.0, 0.0)], [(3000.0, 0.0, 0.0)],
+                  [(33.0, 0.0, 0.0), (0.01, -1e-6, 1e-10)], [(4.0, -3.0, 0.5)] * 2 + [(2.0, -1.5, 0.5)] * 2):
+        G = gradient((E, rows, cols), E + rows, dtype).cuda()
+        got = moe.moe_orthogonalize(G, steps=len(steps), coefficients=steps)
+        assert torch.isfinite(got).all(), steps
+        check(got, G, steps)

@@ -87,3 +87,14 @@ def test_coefficients_in_any_form():
     parts = tuple(abc)
     abc[0] = 1.0
     assert list(memoryview(_coefficients("", parts, 2)).cast("f")) == [1.0, -4.0, 2.0] * 2
+
+
+def test_first_coefficients_that_no_scale_holds(lib):
+    """Small singular values take Q's value at zero, which is the first coefficient."""
+    need = lib.moe_orthogonalize_workspace_bytes(1, 8, 8)
+
+    def call(*abc):
+        return lib.moe_orthogonalize(at(0), 1, 64, 8, 1, 8, 8, (C.c_float * len(abc))(*abc), len(abc) // 3, 1e-7, 1.0, at(1), 1, 64, 8, at(2), need, None)
+
+    for abc in ((4001.0, 0.0, 0.0), (-4001.0, 0.0, 0.0), (1.5, -0.5, 0.0, 1e6, 0.0, 0.0), (1.0, 1.1e6, 0.0), (1.0, 0.0, -1.1e6), (1.0, float("inf"), 0.0)):
+        assert call(*abc) == INVALID, abc
