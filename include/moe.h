@@ -302,8 +302,8 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  *   X = g / (|g| + eps), |g| the root of the sum of its squares;  for (a, b, c) of each step:  S = X X^T,  X = a X + (b S + c S S) X;
  *   out = scale X
  * (where rows > cols: the same on the transpose).  coefficients: host, [steps][3], read before the call returns; steps from 1 to 64.
- * Operands of the products are kept in one or two 16-bit parts, sums in 32 bits, |g| in 64: an fp32 result is as far from the exact one
- * as with products in 32 bits, a bf16 result about as far as its own rounding.  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
+ * Operands of the products are kept in one or two 16-bit parts (22 bits), sums in 32 bits, |g| in 64: an fp32 result is about as far from the exact one
+ * as with products in 32 bits (where |g| is far below eps, and the steps next to a mere factor, 3 10^-7 of its norm), a bf16 result about as far as its own rounding.  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
  * from bounds that hold for any matrix: |X| begins at 1, and a s + b s^3 + c s^5 bounds what a step makes of it.  Steps whose bounds of the singular values
  * before each step stay below 16, and of a + b s^2 + c s^4 below 4000, never leave their range (the usual schedules: 2 and 9); with others a
  * matrix whose own singular values do gives NaN or infinities.  One that holds a NaN or an infinity gives NaN.  Neither spoils another.  A matrix of

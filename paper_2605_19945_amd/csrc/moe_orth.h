@@ -31,6 +31,8 @@ struct OrthArgs {
     float alpha, beta;
     float diagonal;        // added to the diagonal of a symmetric result
     float unscale;         // `own` is the diagonal times this
+    const int* lift;       // of each matrix: X is kept times 2 to this power, less `sunk` (at least 0), on top of its scale; the result less `sunk_after`
+    int lifts, sunk, sunk_after;  // lifts: how many of them the sums have
     int square;            // rows of a symmetric operand
     int steps;             // blocks of the reduction
     int whole;             // of all matrices' tiles the first `whole` take their reduction whole; the others' is cut into `splits` ranges, whose

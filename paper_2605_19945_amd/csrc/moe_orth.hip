@@ -28,6 +28,18 @@ namespace {
 constexpr float X_SCALE = 8192.f, S_SCALE = 4096.f, Q_SCALE = 2048.f;
 constexpr float X_LEAST = 1024.f, S_LEAST = 64.f, Q_LEAST = 8.f;
 
+// Where |G| is far below eps, X is small, and its parts would be subnormal: it is kept another power of two higher, so that its norm begins in [1/2, 1).
+// The steps raise it (all of it by a, as S is next to nothing), so the lift sinks from step to step by what they may have raised it, to nothing.
+// The sums that a step forms of X take the lift out again: S = X X^T twice, the next X, but for the lift that it has.
+constexpr int LIFT_MOST = 96;
+// (by a vector load, which nothing waits for before it is used; a wait for the kernel's arguments would wait for a scalar one too: 2048 x 2048 in bf16 427 and 432 us)
+static __device__ inline int fetch_lift(const OrthArgs& g, int matrix) {
+    asm("" : "+v"(matrix));
+    return g.lift[matrix];
+}
+static __device__ inline int sunk_lift(int lift, int sunk) { return max(lift - sunk, 0); }
+static __device__ inline float unlifted(const OrthArgs& g, int lift) { return ldexpf(1.f, sunk_lift(lift, g.sunk_after) - g.lifts * sunk_lift(lift, g.sunk)); }
+
 // ---- the products ----
 // Tile t of a symmetric matrix's mt x mt, row by row on and above the diagonal
 static __device__ inline void place_symmetric(int t, int mt, int* m, int* n) {
@@ -57,14 +69,15 @@ template <bool SYM> static __device__ inline void place(const OrthArgs& g, int t
 // q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each of its rows beta times A's diagonal.
 // OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any result in blocks; or its type in
 // the caller's rows.  PARTS: of a result in blocks.
+// unlift: what takes the lift of X out of the sums.
 // In a block a lane's 4 values are half a piece, and lanes of neighbouring q change halves for accesses of 16 bytes.
-template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void finish(const OrthArgs& g, f32x4_t u, f32x4_t v, int lane, int matrix, int r, int c, bool both) {
+template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void finish(const OrthArgs& g, float unlift, f32x4_t u, f32x4_t v, int lane, int matrix, int r, int c, bool both) {
     const int i = lane & 15, q = lane >> 4;
     const int64_t here = ((int64_t)(r >> 4) * g.c.blocks + (c >> 5)) * ORTH_BLOCK + orth_piece(i, (q & 1) * 2 + (q >> 1)) * 16;
-    u *= g.alpha;
-    v *= g.alpha;
+    u *= g.alpha * unlift;
+    v *= g.alpha * unlift;
     if constexpr (CIN > 0) {
-        const float beta = ROWS ? g.beta * g.own[(int64_t)matrix * g.square + r + i] : g.beta;
+        const float beta = ROWS ? g.beta * unlift * g.own[(int64_t)matrix * g.square + r + i] : g.beta * unlift;
 #pragma unroll
         for (int p = 0; p < CIN; ++p) {
             const u32x4_t w = *(const u32x4_t*)(g.cin.part[p] + matrix * g.cin.matrix + here);
@@ -159,6 +172,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void orth_product_kernel(OrthArgs g
     const int matrix = item / g.tiles;
     int tm, tn;
     place<SYM>(g, item - matrix * g.tiles, &tm, &tn);
+    const int lift = SYM && CIN > 0 ? 0 : fetch_lift(g, matrix);  // (needed at the end)
 
     // A stage's loads: block row i * WAVES + wave of an operand along its columns; of one along its rows block row i, block column wave.
     const uint32_t panel = (uint32_t)g.a.blocks * ORTH_BLOCK, panel_b = (uint32_t)g.b.blocks * ORTH_BLOCK;
@@ -301,12 +315,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void orth_product_kernel(OrthArgs g
             for (int n = 0; n < FN; ++n) part[((wm * FM + m) * FB + wn * FN + n) * 64] = acc[m][n];
         return;
     }
+    const float unlift = SYM && CIN > 0 ? 1.f : unlifted(g, lift);
     const int row0 = (tm * FA + wm * FM) * 16, col0 = (tn * FB + wn * FN) * 16;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
         if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < FN; n += 2) finish<CIN, ROWS, PARTS, OUT>(g, acc[m][n], acc[m][n + 1], out_lane, matrix, row0 + m * 16, col0 + n * 16, tm != tn);
+        for (int n = 0; n < FN; n += 2) finish<CIN, ROWS, PARTS, OUT>(g, unlift, acc[m][n], acc[m][n + 1], out_lane, matrix, row0 + m * 16, col0 + n * 16, tm != tn);
     }
 }
 
@@ -316,6 +331,7 @@ template <int FA, int FB, int CIN, bool ROWS, int PARTS, int OUT> __global__ __l
     const int f = (int)(pair - item * (FA * FB / 2)) * 2, tile = g.whole + (int)item, matrix = tile / g.tiles, lane = threadIdx.x & 63;
     int tm, tn;
     place<OUT == ORTH_SQUARE>(g, tile - matrix * g.tiles, &tm, &tn);
+    const int lift = OUT == ORTH_SQUARE && CIN > 0 ? 0 : fetch_lift(g, matrix);
     const f32x4_t* part = (const f32x4_t*)g.part + (item * g.splits * (FA * FB) + f) * 64 + lane;
     f32x4_t u = {0.f, 0.f, 0.f, 0.f}, v = u;
 #pragma unroll 4
@@ -323,7 +339,7 @@ template <int FA, int FB, int CIN, bool ROWS, int PARTS, int OUT> __global__ __l
         u += part[(int64_t)s * (FA * FB * 64)];
         v += part[(int64_t)s * (FA * FB * 64) + 64];
     }
-    finish<CIN, ROWS, PARTS, OUT>(g, u, v, lane, matrix, (tm * FA + f / FB) * 16, (tn * FB + f % FB) * 16, tm != tn);
+    finish<CIN, ROWS, PARTS, OUT>(g, OUT == ORTH_SQUARE && CIN > 0 ? 1.f : unlifted(g, lift), u, v, lane, matrix, (tm * FA + f / FB) * 16, (tn * FB + f % FB) * 16, tm != tn);
 }
 
 // ... into the first range's place, where one workgroup alone would be long at it: 4 of F fragments a workgroup
@@ -369,11 +385,13 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
         });
     };
 
+    const int lift = fetch_lift(g, matrix);
     const f32x4_t* part = (const f32x4_t*)g.part + (int64_t)matrix * apart * (NF * NF * 64) + lane;  // (apart: ranges between matrices)
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
 #pragma unroll 4
     for (int r = 0; r < splits; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + col0 + n) * 64]; });
-    each([&](int m, int n) { v[m][n] *= pair.from; });
+    const float from = ldexpf(pair.from, -2 * sunk_lift(lift, g.sunk));
+    each([&](int m, int n) { v[m][n] *= from; });
     put(s, PLANE, KB);
     __syncthreads();
     constexpr int last = 4;  // of the products
@@ -441,7 +459,7 @@ static __device__ inline void pieces_of(const f32x4_t& u, const f32x4_t& v, u32x
 
 // Q = a I + b S + c S S in LDS, in two parts, in blocks, from S's ranges, by four wavefronts: each workgroup that multiplies with Q forms it by itself,
 // which costs less than a launch in between.  NF / 4 rows of fragments a wavefront (one, of fewer wavefronts, where there are two).
-template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* s, int matrix) {
+template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* s, int matrix, int lift) {
     constexpr int KB = NF / 2, PLANE = NF * KB * ORTH_BLOCK, FM = NF == 8 ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q4 = lane >> 4;
     const bool on = wave * FM < NF;
@@ -467,7 +485,8 @@ template <int NF> static __device__ inline void orth_q(const OrthArgs& g, char* 
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
 #pragma unroll 2
     for (int r = 0; r < g.ranges; ++r) each([&](int m, int n) { v[m][n] += part[(r * NF * NF + (row0 + m) * NF + n) * 64]; });
-    each([&](int m, int n) { v[m][n] *= g.from; });
+    const float from = ldexpf(g.from, -2 * sunk_lift(lift, g.sunk));
+    each([&](int m, int n) { v[m][n] *= from; });
     if (on) put();
     __syncthreads();
     each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
@@ -523,9 +542,10 @@ template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256,
 #pragma unroll
     for (int p = 0; p < 2; ++p) desc[p] = orth_desc(g.b.part[p] + matrix * g.b.matrix, (uint32_t)g.b.matrix);
     f16x8_t q[2][NF][KB];
+    const int lift = MODE > 0 ? fetch_lift(g, matrix) : 0;
     if constexpr (MODE > 0) {
         char* own = lds + 4 * (NF * NF > 2 * NF ? NF * NF : 2 * NF) * ORTH_BLOCK;
-        if constexpr (OWN) orth_q<NF>(g, own, matrix);
+        if constexpr (OWN) orth_q<NF>(g, own, matrix, lift);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -535,6 +555,7 @@ template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256,
                     q[p][m][k] = OWN ? *(const f16x8_t*)(own + (p * NF * KB + m * KB + k) * ORTH_BLOCK + at_row)
                                      : *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + (m * g.a.blocks + k) * ORTH_BLOCK + at_row);
     }
+    const float unlift = MODE > 0 ? unlifted(g, lift) : 1.f;
     f32x4_t s[NF][NF];
 #pragma unroll
     for (int m = 0; m < NF; ++m)
@@ -581,10 +602,10 @@ template <int NF, int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256,
 #pragma unroll
             for (int m = 0; m < NF; ++m) {
                 if constexpr (MODE == 2) {
-                    finish<0, false, 0, OUT>(g, v[m][0], v[m][1], lane, matrix, m * 16, c * 32, false);
+                    finish<0, false, 0, OUT>(g, unlift, v[m][0], v[m][1], lane, matrix, m * 16, c * 32, false);
                 } else {
                     u32x4_t piece[2];
-                    pieces_of(v[m][0] * g.alpha, v[m][1] * g.alpha, piece);
+                    pieces_of(v[m][0] * (g.alpha * unlift), v[m][1] * (g.alpha * unlift), piece);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         x[p][m] = __builtin_bit_cast(f16x8_t, piece[p]);
@@ -640,9 +661,10 @@ template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1
     int stage = 0;
     if (MODE > 0 && (int)blockIdx.x < g.steps) issue(blockIdx.x, 0);
     f16x8_t q[2][FM][KB];
+    const int lift = MODE > 0 ? fetch_lift(g, matrix) : 0;
     if constexpr (MODE > 0) {
         char* own = lds + 3 * STAGE;
-        if constexpr (OWN) orth_q<NF>(g, own, matrix);
+        if constexpr (OWN) orth_q<NF>(g, own, matrix, lift);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -652,6 +674,7 @@ template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1
                     q[p][m][k] = OWN ? *(const f16x8_t*)(own + (p * NF * KB + (wave * FM + m) * KB + k) * ORTH_BLOCK + at_row)
                                      : *(const f16x8_t*)(g.a.part[p] + matrix * g.a.matrix + ((wave * FM + m) * g.a.blocks + k) * ORTH_BLOCK + at_row);
     }
+    const float unlift = MODE > 0 ? unlifted(g, lift) : 1.f;
     f32x4_t s[FM][NF];
 #pragma unroll
     for (int m = 0; m < FM; ++m)
@@ -697,10 +720,10 @@ template <int MODE, int OUT, bool OWN> __global__ __launch_bounds__(256, OWN ? 1
             for (int m = 0; m < FM; ++m) {
                 const int row = wave * FM + m;
                 if constexpr (MODE == 2) {
-                    finish<0, false, 0, OUT>(g, v[m][0], v[m][1], lane, matrix, row * 16, c * 32, false);
+                    finish<0, false, 0, OUT>(g, unlift, v[m][0], v[m][1], lane, matrix, row * 16, c * 32, false);
                 } else {
                     u32x4_t piece[2];
-                    pieces_of(v[m][0] * g.alpha, v[m][1] * g.alpha, piece);
+                    pieces_of(v[m][0] * (g.alpha * unlift), v[m][1] * (g.alpha * unlift), piece);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         *(u32x4_t*)(g.c.part[p] + matrix * g.c.matrix + (int64_t)row * line + c * ORTH_BLOCK + orth_piece(i16, (q16 & 1) * 2 + (q16 >> 1)) * 16) = piece[p];
@@ -756,6 +779,7 @@ struct OrthIn {
     float eps;
     int tall;            // G^T is what is put into blocks
     int vec;             // rows begin at multiples of 16 bytes
+    int* lift;           // [matrices], for the steps
     int block_rows;      // of x
     OrthOperand x;
 };
@@ -850,7 +874,15 @@ template <typename T> __global__ __launch_bounds__(kThreads) void orth_blocks_ke
     }
     double s = 0;
     for (int i = threadIdx.x; i < in.parts; i += kThreads) s += in.partials[(int64_t)matrix * in.parts + i];
-    const double scale = (double)X_SCALE / (sqrt(block_sum(s, lds)) + (double)in.eps);
+    const double norm = sqrt(block_sum(s, lds)), least = norm + (double)in.eps;
+    double scale = (double)X_SCALE / least;
+    int lift = 0;
+    if (norm > 0 && norm < (double)in.eps) {
+        (void)frexp(norm / least, &lift);  // (that is below 2^lift)
+        lift = min(-lift, LIFT_MOST);
+        scale = ldexp(scale, lift);
+    }
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) in.lift[matrix] = lift;
     if (whole) {
         const bool live = r0 + row < in.rows;
 #pragma unroll
@@ -898,14 +930,16 @@ float scale_for(double bound, float most, float least) {
 // in [0, 1]; on [0, s] those of Q lie in the range of a + b t + c t^2 for t in [0, s^2], and the next X's in that of their products with s.
 // An entry of a matrix is at most its largest singular value.  Small singular values (and padded rows) take Q's value at 0, which is a.
 // (Steps that lead past all range for some matrix may stay in range for others, and are held for those.)
+constexpr int RAISED_MOST = 1 << 10, RAISED_LEAST = -24;
 struct Range {
     double most;             // the largest of Q's
     float x, s, q;           // scales of X before the step, of S and Q
     float from;              // S's over that of X X^T
+    int raised;              // X has grown by no more than this power of two
     void coefficients(const float* c, float* abc) const { abc[0] = c[0] * q, abc[1] = c[1] * (q / s), abc[2] = c[2] * (q / (s * s)); }  // of products as they are kept
 };
 void ranges_of(const float* coefficients, int steps, Range* z) {
-    double x = 1;
+    double x = 1, raised = 0;
     for (int k = 0; k < steps; ++k) {
         const double a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2], end = x * x;
         auto q = [&](double t) { return fabs(a + b * t + c * t * t); };
@@ -920,9 +954,12 @@ void ranges_of(const float* coefficients, int steps, Range* z) {
             const double t = c != 0 ? (d >= 0 ? (-3 * b + (i ? sqrt(d) : -sqrt(d))) / (10 * c) : -1) : b != 0 ? -a / (3 * b) : -1;
             if (t > 0 && t < end) next = fmax(next, sqrt(t) * q(t));
         }
-        z[k] = {most, scale_for(x, X_SCALE, X_LEAST), scale_for(2 * end, S_SCALE, S_LEAST), scale_for(most, Q_SCALE, Q_LEAST), 0.f};  // (twice its range for X, so four times for S)
+        z[k] = {most, scale_for(x, X_SCALE, X_LEAST), scale_for(2 * end, S_SCALE, S_LEAST), scale_for(most, Q_SCALE, Q_LEAST), 0.f, (int)fmin(ceil(raised), RAISED_MOST)};  // (twice its range for X, so four times for S)
         z[k].from = z[k].s / (z[k].x * z[k].x);
         x = next;
+        raised += log2(most);
+        if (isnan(raised)) raised = INFINITY;
+        if (raised < RAISED_LEAST) raised = RAISED_LEAST;  // (more of a lift is not wanted)
     }
 }
 // Two steps' Q' Q is kept times this: with entries up to |Q'| |Q| (11.9 of the default coefficients; 34 where the first steps raise small singular values most,
@@ -995,8 +1032,8 @@ Size size_of_matrix(int E, int rows, int cols) {
     return z;
 }
 
-// X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares
-int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096; }
+// X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares; the lift
+int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096 + 16; }
 // Workgroups that share the columns of a matrix of up to 128 rows, of which each leaves sums; fewer of the tallest, whose sums are larger
 int thin_groups(int count, const Size& z) {
     const int want = z.n == 128 ? (z.m / 32 + 1) / 2 : (z.m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1, most = z.n == 128 && room > 128 ? 128 : room;
@@ -1053,6 +1090,7 @@ template <int PA, int PB, bool TB, int CIN, bool ROWS, int PARTS, int OUT> hipEr
 struct Buffers {
     OrthOperand x[2], s, q, t;
     float *part, *own;
+    int* lift;
 };
 
 OrthOperand operand(char*& at, int64_t plane, int blocks, int matrices) {
@@ -1089,12 +1127,19 @@ template <bool F32> struct Steps {
         g.alpha = alpha;
         g.part = w.part;
         g.square = z.n;
+        g.lift = w.lift, g.sunk_after = RAISED_MOST;  // (taken out of no sums)
         return g;
     }
     // q X of the steps before `next`: into X's other buffer, or to the caller
     void scale(OrthArgs& g, int k, int next, float q) const {
         g.beta = (next < t.steps ? ranges[next].x : t.scale) / ranges[k].x;
         g.alpha = g.beta / q;
+        lifted(g, 1, k, next);
+    }
+    // sums of the X before step k, so many times over, for what is kept before step `next`
+    void lifted(OrthArgs& g, int lifts, int k, int next) const {
+        g.lift = w.lift, g.lifts = lifts;
+        g.sunk = ranges[k].raised, g.sunk_after = next < t.steps ? ranges[next].raised : RAISED_MOST;
     }
     void to_caller(OrthArgs& g) const {
         g.out = out;
@@ -1133,9 +1178,11 @@ template <bool F32> struct Steps {
         return e;
     }
     // S = X X^T
-    hipError_t gram(const Range& r) const {
+    hipError_t gram(int k, const Range& r) const {
         constexpr int PARTS = F32 ? 2 : 1;
-        return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(square(w.x[0], w.x[0], w.s, r.from), z.tile, st);
+        OrthArgs g = square(w.x[0], w.x[0], w.s, r.from);
+        lifted(g, 2, k, t.steps);
+        return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
     // to = a I + b S + c S S, and where it has one part its diagonal in 32 bits
     hipError_t polynomial(const OrthOperand& to, int k, const Range& r) const {
@@ -1156,7 +1203,7 @@ template <bool F32> struct Steps {
     }
     hipError_t one_step(int k) {
         const Range& r = ranges[k];
-        hipError_t e = gram(r);
+        hipError_t e = gram(k, r);
         if (e == hipSuccess) e = polynomial(w.q, k, r);
         if (e == hipSuccess) e = apply<F32>(w.q, r.q, k, k + 1);
         return e;
@@ -1170,7 +1217,7 @@ template <bool F32> struct Steps {
     hipError_t two_steps(int k, float joint) {
         Range one, two;
         together(k, one, two);
-        hipError_t e = gram(one);
+        hipError_t e = gram(k, one);
         if (e == hipSuccess) e = polynomial(w.q, k, one);
         if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / one.q);
         if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / one.q);  // Q S Q = (Q X) (Q X)^T
@@ -1184,6 +1231,7 @@ template <bool F32> struct Steps {
         OrthArgs g = {};
         g.part = sums;
         g.c = w.q;
+        lifted(g, 2, k, t.steps);
         Range one, two;
         together(k, one, two);
         OrthPair p = {};
@@ -1314,6 +1362,7 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.cols = t.cols;
         w.own = (float*)at;
         in.partials = (double*)(at + (int64_t)z.n * 4 * count);
+        in.lift = w.lift = (int*)(at + (int64_t)(z.n * 4 + 4096) * count);
         in.parts = z.parts;
         in.eps = t.eps;
         in.tall = tall;

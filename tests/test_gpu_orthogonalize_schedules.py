@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2605_19945_amd as moe
-from test_gpu_orthogonalize import BF16, F32, check, gradient
+from test_gpu_orthogonalize import ABC, BF16, F32, check, gradient
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,31 @@ def test_large_coefficients(E, rows, cols, dtype):
         got = moe.moe_orthogonalize(G, steps=len(steps), coefficients=steps)
         assert torch.isfinite(got).all(), steps
         check(got, G, steps)
+
+
+def shares_of(E, rows, cols, dtype, eps, shares):
+    """Matrices whose norm is so many times eps."""
+    G = gradient((E, rows, cols), E + rows, F32).cuda().double()
+    G /= G.square().sum((1, 2), keepdim=True).sqrt()
+    return (G * eps * torch.tensor(shares, dtype=torch.float64, device="cuda")[:, None, None]).to(dtype)
+
+
+@pytest.mark.parametrize("rows,cols", [(24, 83), (60, 4000), (100, 500), (16, 14336), (300, 400), (400, 300), (1024, 2100)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norms_far_below_eps(rows, cols, dtype):
+    """X begins far below 1; matrices of one stack each at another distance."""
+    shares = [1e3, 0.9, 0.1, 1e-2, 1e-4, 1e-6, 1e-12, 1e-25]
+    for eps, coefficients in ((1e-7, (ABC,) * 5), (1e-3, RAISING[:5]), (1e-7, (ABC,)), (1e-7, ((0.5, 0.25, 0.0), ABC)), (1e-7, ((1e-3, 0.0, 0.0), (1e3, 0.0, 0.0), ABC)),
+                              (1e-7, ((0.0, 0.0, 0.0),) * 2)):
+        G = shares_of(len(shares), rows, cols, dtype, eps, shares)
+        got = moe.moe_orthogonalize(G, steps=len(coefficients), coefficients=coefficients, eps=eps)
+        check(got, G, coefficients, eps=eps)
+
+
+@pytest.mark.parametrize("rows,cols", [(24, 83), (100, 500), (300, 400)])
+def test_many_steps_from_far_below_eps(rows, cols):
+    """Singular values come up from 1e-13 to 1 on the way."""
+    G = shares_of(3, rows, cols, F32, 1e-7, [1e-12, 1e-6, 1.0])
+    for steps in (30, 64):
+        got = moe.moe_orthogonalize(G, steps=steps, coefficients=(1.5, -0.5, 0.0))
+        check(got, G, ((1.5, -0.5, 0.0),) * steps)
