@@ -92,7 +92,8 @@ __global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4
             }
         }
         if (NEXT || a.norm) group_sums<W>(s, lds, turn);
-        const float r = rsqrtf(fmaf(s[0], over_d, a.eps)), k = r * r * r * (s[1] * over_d);
+        // o r^2 mean(p o) as (o r) (r mean(p o)), factors of p's size: r^3 leaves the range at rows of 1e-13 and 1e13
+        const float r = rsqrtf(fmaf(s[0], over_d, a.eps)), k = r * (s[1] * over_d);
         const float ry = JOIN && a.norm ? rsqrtf(fmaf(s[2], over_d, a.eps)) : 1.f;
         float u[1] = {0.f};  // sum of g D w y, without the row's gate
         float D[JOIN ? CH : 1][8];
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4
                 f.o[c].open(o), f.dh[c].open(dh);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    out[j] += r * (dh[j] * w[j]) - o[j] * k;
+                    out[j] = fmaf(r, dh[j] * w[j] - o[j] * r * k, out[j]);
                     dnext[c][j] = fmaf(dh[j], o[j] * r, dnext[c][j]);
                 }
             }
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4
             const bool row_gate = a.ldgate == 0 && a.dgate != nullptr;
             if (a.norm || row_gate) group_sums<W>(u, lds, turn);
             if (row_gate && live && lane == 0) ((float*)a.dgate)[row] = u[0] * ry;
-            const float ky = a.norm ? ry * ry * ry * (f.gate * u[0] * over_d) : 0.f;
+            const float ky = a.norm ? ry * (f.gate * u[0] * over_d) : 0.f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (c * 64 * W + lane) * 8;
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float dn = f.gate * g[j] * D[c][j];
-                    out[j] = ry * (dn * w[j]) - y[j] * ky;
+                    out[j] = ry * (dn * w[j] - y[j] * ry * ky);
                     dw[c][j] = fmaf(dn, y[j] * ry, dw[c][j]);
                 }
                 Eight<B>::template store<NT>((B*)a.dy + row * a.lddy + col, out);
