@@ -310,9 +310,11 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  * zeros gives zeros (eps > 0).
  * g and out: rows ldg / ldout values apart (at least cols), matrices stride_g / stride_out values apart, pointers aligned to their values; any
  * sizes from 1 to 2^17, rows * cols <= 2^29, E <= 256.  out may be exactly g (of the same type); otherwise they share no byte.
- * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done; about 8 bytes for every
- * value of the stack and 12 for those of a square of the smaller side, 64 MiB for sums; at most 8 GiB (or what one matrix needs): larger stacks are gone through
- * in turns.  0: sizes that are refused. */
+ * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done.  Matrices are kept padded: the smaller side to
+ * 32, 64 or 128, from 129 on to a multiple of 256 at most; the larger to a multiple of 64, from 129 of the smaller on of 256 at most, and 32 more.  It takes 8 bytes for every
+ * value of these, 12 for those of a square of the smaller side (by itself and 32 more), 4 for each row and 4112 a matrix, and up to 64 MiB for sums: of a
+ * row of 131072 256 bytes a value, of 4096 x 14336 12.  At most 8 GiB (or what one matrix needs): larger stacks are gone through in turns.  0: sizes that are
+ * refused. */
 size_t moe_orthogonalize_workspace_bytes(int32_t E, int32_t rows, int32_t cols);
 moe_status moe_orthogonalize(const void* g, int32_t type, int64_t stride_g, int64_t ldg, int32_t E, int32_t rows, int32_t cols,
                              const float* coefficients /* host */, int32_t steps, float eps, float scale, void* out, int32_t out_type,

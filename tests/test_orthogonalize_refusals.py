@@ -98,3 +98,15 @@ def test_first_coefficients_that_no_scale_holds(lib):
 
     for abc in ((4001.0, 0.0, 0.0), (-4001.0, 0.0, 0.0), (1.5, -0.5, 0.0, 1e6, 0.0, 0.0), (1.0, 1.1e6, 0.0), (1.0, 0.0, -1.1e6), (1.0, float("inf"), 0.0)):
         assert call(*abc) == INVALID, abc
+
+
+def test_workspace_of_padded_sizes(lib):
+    """What the header states, for small sides and stacks; and not less than X in two parts, twice, needs."""
+    for E in (1, 3, 128):
+        for rows, cols in ((1, 1), (1, 9), (1, 131072), (17, 8004), (33, 100), (65, 100), (128, 256), (129, 127), (129, 129), (200, 3000), (330, 826), (1024, 1024)):
+            n, m = min(rows, cols), max(rows, cols)
+            most = next((k for k in (32, 64, 128) if n <= k), -(-n // 256) * 256), (-(-m // 64) * 64 if n <= 128 else -(-m // 256) * 256) + 32
+            bound = E * (8 * most[0] * most[1] + 12 * most[0] * (most[0] + 32) + 4 * most[0] + 4112) + (64 << 20)
+            got = lib.moe_orthogonalize_workspace_bytes(E, rows, cols)
+            assert 8 * E * n * m <= got <= min(bound, 8 << 30), (E, rows, cols)
+            assert lib.moe_orthogonalize_workspace_bytes(E, cols, rows) == got
