@@ -303,7 +303,8 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  *   out = scale X
  * (where rows > cols: the same on the transpose).  coefficients: host, [steps][3], read before the call returns; steps from 1 to 64.
  * Operands of the products are kept in one or two 16-bit parts (22 bits), sums in 32 bits, |g| in 64: an fp32 result is about as far from the exact one
- * as with products in 32 bits (where |g| is far below eps, and the steps next to a mere factor, 3 10^-7 of its norm), a bf16 result about as far as its own rounding.  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
+ * as with products in 32 bits (where |g| is far below eps, and the steps next to a mere factor, 3 10^-7 of its norm), a bf16 result 1 to 1.4 times
+ * as far as its own rounding (2.5 after steps whose slope is large where singular values come to lie: such schedules are better damped).  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
  * from bounds that hold for any matrix: |X| begins at 1, and a s + b s^3 + c s^5 bounds what a step makes of it.  Steps whose bounds of the singular values
  * before each step stay below 16, and of a + b s^2 + c s^4 below 4000, never leave their range (the usual schedules: 2 and 9); with others a
  * matrix whose own singular values do gives NaN or infinities.  One that holds a NaN or an infinity gives NaN.  Neither spoils another.  A matrix of
@@ -312,7 +313,7 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  * sizes from 1 to 2^17, rows * cols <= 2^29, E <= 256.  out may be exactly g (of the same type); otherwise they share no byte.
  * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done.  Matrices are kept padded: the smaller side to
  * 32, 64 or 128, from 129 on to a multiple of 256 at most; the larger to a multiple of 64, from 129 of the smaller on of 256 at most, and 32 more.  It takes 8 bytes for every
- * value of these, 12 for those of a square of the smaller side (by itself and 32 more), 4 for each row and 4112 a matrix, and up to 64 MiB for sums: of a
+ * value of these, 12 for those of a square of the smaller side (by itself and 32 more), 8 for each row and 4112 a matrix, and up to 64 MiB for sums: of a
  * row of 131072 256 bytes a value, of 4096 x 14336 12.  At most 8 GiB (or what one matrix needs): larger stacks are gone through in turns.  0: sizes that are
  * refused. */
 size_t moe_orthogonalize_workspace_bytes(int32_t E, int32_t rows, int32_t cols);

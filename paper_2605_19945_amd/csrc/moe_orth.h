@@ -12,6 +12,7 @@
 #include "moe_ops.h"
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char orth_lds_char;
 
 constexpr int ORTH_BLOCK = 1024;  // bytes of a block of 16 rows by 32 values
@@ -26,11 +27,11 @@ struct OrthOperand {
 struct OrthArgs {
     OrthOperand a, b;
     OrthOperand cin;       // beta times this is added, or times the row's of
-    float* own;            // a symmetric result's diagonal: [matrices][its rows]
+    float* own;            // of a symmetric result in one part: [matrices][its rows][what its diagonal's rounding lost, its diagonal]
     OrthOperand c;         // the result
     float alpha, beta;
     float diagonal;        // added to the diagonal of a symmetric result
-    float unscale;         // `own` is the diagonal times this
+    float unscale;         // ... times this
     const int* lift;       // of each matrix: X is kept times 2 to this power, less `sunk` (at least 0), on top of its scale; the result less `sunk_after`
     int lifts, sunk, sunk_after;  // lifts: how many of them the sums have
     int square;            // rows of a symmetric operand

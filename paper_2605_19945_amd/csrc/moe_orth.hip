@@ -5,12 +5,14 @@
 // Products bound it: of n x m matrices, n <= m, n n m + n n n + 2 n n m operations a step where the two symmetric products are formed on
 // and above the diagonal only.  Matrix instructions take 16-bit operands, and what a step rounds is multiplied by the ones behind it (by a
 // each, for the small singular values), so operands are kept in one or two parts of fp16 (moe_orth.h), and X always in two.
-//   fp32 results: all operands of all products have two parts, 22 bits: as far from the exact ones as those of 32-bit products (0.8 to 1.3 times,
-// 1e-6 to 3e-6 of their norm).  Three products of parts for one, so where X is wide two steps are taken at a time through products of squares only.
-//   bf16 results: one part in every product; X's second part takes the diagonal of Q = a I + b S + c S S alone, its largest share.  5e-4 of the norm on the
-// spectra of gradients, 1.1e-3 on flat ones, below the 1.7e-3 of the result's own rounding (1.03 to 1.2 times that in all); with X in one part
-// steep spectra lose 8e-3, with bf16 operands 6e-2.
-// Measured: 8 matrices of 4096 x 14336 in bf16 29.5 ms (1070 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
+//   fp32 results: all operands of all products have two parts, 22 bits: no further from the exact ones than those of 32-bit products, but for a few small
+// matrices (1e-6 to 1.5e-5 of their norm; 0.2 to 1 times, 1.5 for 100 to 150 rows and steps that raise small values by 8).  Three products of parts for one, so where X is wide two steps are taken at a time through products of squares only.
+//   bf16 results: one part in every product; beside it the diagonal of Q = a I + b S + c S S, its largest share, is kept in 32 bits, for X's second part and
+// for what its own rounding takes from the first.  Of five usual steps 1e-4 of the norm on the spectra of gradients, 8e-4 on flat ones, below the 1.66e-3 of the
+// result's own rounding (1.00 to 1.14 times that in all; without the latter 1.03 to 1.22, and 2.6 for 300 x 400 and the steps of 8; with X in one part steep
+// spectra lose 8e-3, with bf16 operands 6e-2).  More steps carry it further (eight 1.06 to 1.43), and steps whose slope is large where singular values come
+// to lie: 1.0 to 1.8 for the steps of 8, up to 2.5 after four of them; damped by 1 % they stay within 1.24.
+// Measured: 8 matrices of 4096 x 14336 in bf16 29.8 ms (1060 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
 // parts, and 1170 for S), 32 of 7168 x 2048 in fp32 29.9 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.2 ms.  One-part
 // products wait for their operands on the way from the L2s through LDS (without these loads the first case takes two thirds of its time); short
 // reductions, as 768, for tiles' beginnings and ends.
@@ -66,7 +68,7 @@ template <bool SYM> static __device__ inline void place(const OrthArgs& g, int t
 }
 
 // The sums of two neighbouring fragments on their way out: a lane has the columns c + 4 q + 0..3 and c + 16 + 4 q + 0..3 of row r + i (i = lane % 16,
-// q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each of its rows beta times A's diagonal.
+// q = lane / 16).  CIN: parts of another matrix that is added beta times; ROWS: each row of each part beta times its number in `own`.
 // OUT: a symmetric result in blocks, whose tiles above the diagonal (`both`) are written to both sides; any result in blocks; or its type in
 // the caller's rows.  PARTS: of a result in blocks.
 // unlift: what takes the lift of X out of the sums.
@@ -77,9 +79,11 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
     u *= g.alpha * unlift;
     v *= g.alpha * unlift;
     if constexpr (CIN > 0) {
-        const float beta = ROWS ? g.beta * unlift * g.own[(int64_t)matrix * g.square + r + i] : g.beta * unlift;
+        f32x2_t betas = {g.beta * unlift, g.beta * unlift};
+        if (ROWS) betas *= *(const f32x2_t*)(g.own + ((int64_t)matrix * g.square + r + i) * 2);
 #pragma unroll
         for (int p = 0; p < CIN; ++p) {
+            const float beta = betas[p];
             const u32x4_t w = *(const u32x4_t*)(g.cin.part[p] + matrix * g.cin.matrix + here);
             const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane16_swap(w[1], w[3], false, false);
             u[0] = fmaf(beta, f16_lo(x[0]), u[0]), u[1] = fmaf(beta, f16_hi(x[0]), u[1]), u[2] = fmaf(beta, f16_lo(y[0]), u[2]), u[3] = fmaf(beta, f16_hi(y[0]), u[3]);
@@ -101,7 +105,9 @@ template <int CIN, bool ROWS, int PARTS, int OUT> static __device__ inline void 
             if (g.own != nullptr && (r == c || r == c + 16)) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (4 * q + j == i) g.own[(int64_t)matrix * g.square + r + i] = (r == c ? u[j] : v[j]) * g.unscale;
+                    const uint32_t word = parts[0][(r == c ? 0 : 2) + j / 2];
+                    const float x = r == c ? u[j] : v[j], kept = j % 2 == 0 ? f16_lo(word) : f16_hi(word);
+                    if (4 * q + j == i) *(f32x2_t*)(g.own + ((int64_t)matrix * g.square + r + i) * 2) = f32x2_t{(x - kept) * g.unscale, x * g.unscale};
                 }
             }
         }
@@ -1033,7 +1039,7 @@ Size size_of_matrix(int E, int rows, int cols) {
 }
 
 // X in two parts, twice (one is read while the next is written); S, Q and T in two parts; the partial sums of the squares; the lift
-int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 4 + 4096 + 16; }
+int64_t matrix_bytes(const Size& z) { return 4 * z.x + 6 * z.s + z.n * 8 + 4096 + 16; }
 // Workgroups that share the columns of a matrix of up to 128 rows, of which each leaves sums; fewer of the tallest, whose sums are larger
 int thin_groups(int count, const Size& z) {
     const int want = z.n == 128 ? (z.m / 32 + 1) / 2 : (z.m / 32 + 3) / 4, room = 2 * kUnits / count > 1 ? 2 * kUnits / count : 1, most = z.n == 128 && room > 128 ? 128 : room;
@@ -1151,16 +1157,15 @@ template <bool F32> struct Steps {
         const int size = F32 ? 4 : 2;
         g.vec = ((uintptr_t)out & (4 * size - 1)) == 0 && t.out_ld % 4 == 0 && (count == 1 || t.out_matrix % 4 == 0);
     }
-    // X = q X of the steps from k to next; where q has one part, q of X's first part and, of the second, its diagonal's share alone
+    // X = q X of the steps from k to next; where q has one part, q of X's first part, what the diagonal's rounding lost of that, and the diagonal's share of X's second
     template <bool TWO> hipError_t apply(const OrthOperand& q, float q_scale, int k, int next) {
-        constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 1;
+        constexpr int PARTS = TWO ? 2 : 1, CIN = TWO ? 0 : 2;
         OrthArgs g = {};
         g.matrices = count;
         g.mt = z.n / z.tile, g.nt = z.m / z.tile;
         g.tiles = g.mt * g.nt;
         g.square = z.n;
         g.a = q, g.b = w.x[0], g.c = w.x[1], g.cin = w.x[0];
-        g.cin.part[0] = w.x[0].part[1];
         g.own = w.own;
         g.steps = z.n / 32;
         scale(g, k, next, q_scale);
@@ -1184,7 +1189,7 @@ template <bool F32> struct Steps {
         lifted(g, 2, k, t.steps);
         return product<PARTS, PARTS, false, 0, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
-    // to = a I + b S + c S S, and where it has one part its diagonal in 32 bits
+    // to = a I + b S + c S S, and where it has one part its diagonal in 32 bits and what it lost
     hipError_t polynomial(const OrthOperand& to, int k, const Range& r) const {
         constexpr int PARTS = F32 ? 2 : 1;
         float abc[3];
@@ -1361,8 +1366,8 @@ hipError_t launch_orth(const OrthTask& t, void* workspace, hipStream_t st) {
         in.rows = t.rows;
         in.cols = t.cols;
         w.own = (float*)at;
-        in.partials = (double*)(at + (int64_t)z.n * 4 * count);
-        in.lift = w.lift = (int*)(at + (int64_t)(z.n * 4 + 4096) * count);
+        in.partials = (double*)(at + (int64_t)z.n * 8 * count);
+        in.lift = w.lift = (int*)(at + (int64_t)(z.n * 8 + 4096) * count);
         in.parts = z.parts;
         in.eps = t.eps;
         in.tall = tall;

@@ -106,7 +106,7 @@ def test_workspace_of_padded_sizes(lib):
         for rows, cols in ((1, 1), (1, 9), (1, 131072), (17, 8004), (33, 100), (65, 100), (128, 256), (129, 127), (129, 129), (200, 3000), (330, 826), (1024, 1024)):
             n, m = min(rows, cols), max(rows, cols)
             most = next((k for k in (32, 64, 128) if n <= k), -(-n // 256) * 256), (-(-m // 64) * 64 if n <= 128 else -(-m // 256) * 256) + 32
-            bound = E * (8 * most[0] * most[1] + 12 * most[0] * (most[0] + 32) + 4 * most[0] + 4112) + (64 << 20)
+            bound = E * (8 * most[0] * most[1] + 12 * most[0] * (most[0] + 32) + 8 * most[0] + 4112) + (64 << 20)
             got = lib.moe_orthogonalize_workspace_bytes(E, rows, cols)
             assert 8 * E * n * m <= got <= min(bound, 8 << 30), (E, rows, cols)
             assert lib.moe_orthogonalize_workspace_bytes(E, cols, rows) == got
