@@ -939,6 +939,7 @@ float scale_for(double bound, float most, float least) {
 constexpr int RAISED_MOST = 1 << 10, RAISED_LEAST = -24;
 struct Range {
     double most;             // the largest of Q's
+    double bound, slope;     // of X before the step; of the slope of a + b t + c t^2
     float x, s, q;           // scales of X before the step, of S and Q
     float from;              // S's over that of X X^T
     int raised;              // X has grown by no more than this power of two
@@ -960,7 +961,7 @@ void ranges_of(const float* coefficients, int steps, Range* z) {
             const double t = c != 0 ? (d >= 0 ? (-3 * b + (i ? sqrt(d) : -sqrt(d))) / (10 * c) : -1) : b != 0 ? -a / (3 * b) : -1;
             if (t > 0 && t < end) next = fmax(next, sqrt(t) * q(t));
         }
-        z[k] = {most, scale_for(x, X_SCALE, X_LEAST), scale_for(2 * end, S_SCALE, S_LEAST), scale_for(most, Q_SCALE, Q_LEAST), 0.f, (int)fmin(ceil(raised), RAISED_MOST)};  // (twice its range for X, so four times for S)
+        z[k] = {most, x, fmax(fabs(b), fabs(b + 2 * c * end)), scale_for(x, X_SCALE, X_LEAST), scale_for(2 * end, S_SCALE, S_LEAST), scale_for(most, Q_SCALE, Q_LEAST), 0.f, (int)fmin(ceil(raised), RAISED_MOST)};  // (twice its range for X, so four times for S)
         z[k].from = z[k].s / (z[k].x * z[k].x);
         x = next;
         raised += log2(most);
@@ -968,11 +969,14 @@ void ranges_of(const float* coefficients, int steps, Range* z) {
         if (raised < RAISED_LEAST) raised = RAISED_LEAST;  // (more of a lift is not wanted)
     }
 }
-// Two steps' Q' Q is kept times this: with entries up to |Q'| |Q| (11.9 of the default coefficients; 34 where the first steps raise small singular values most,
-// which Q_SCALE would take past fp16).  0: they are taken one by one, rather than lose more than 3 bits of the smallest entries.
-float joint_scale(const Range& one, const Range& two) {
-    const float scale = scale_for(one.most * two.most, Q_SCALE, 0.f);
-    return scale >= Q_SCALE / 8 ? scale : 0.f;
+// May two steps be taken at a time?  Q' Q is kept times Q_SCALE, and its entries reach |Q'| |Q| (11.9 of the default coefficients, 34 where the first steps raise
+// small singular values most).  And S' = Q S Q is off by a share of |Q|^2 |S|, where the S' of a step by itself is off by one of |S'|; Q' takes that times its
+// slope, and the next X times s' more: 68 and 98 roundings with the default coefficients, 280 to 403 in the first steps of schedules that raise small ones by 8 and
+// keep the largest near 2.  In pairs from the first on (times less, for the range) five of those are 4.8 times as far off as with 32-bit products for 8 x 128 x 256 in
+// fp32, by this rule 1.3 (81 and 86 us); 8 x 129 x 9000 2.6 and 0.96 (357 and 379).
+bool together(const Range& one, const Range& two) {
+    const double q = one.most * one.bound;
+    return one.most * two.most * Q_SCALE <= 32752.0 && q * q * two.slope * two.bound <= 128;
 }
 
 // ---- plan ----
@@ -1120,8 +1124,8 @@ template <bool F32> struct Steps {
     hipStream_t st;
     const Range* ranges;  // of each step
 
-    // Scale of the next two steps' product, 0 where they are taken one by one
-    float pair(int k) const { return k + 2 <= t.steps ? joint_scale(ranges[k], ranges[k + 1]) : 0.f; }
+    // Steps from k on that are taken at a time where pairs are
+    int at_a_time(int k, bool pairs) const { return pairs && k + 2 <= t.steps && together(ranges[k], ranges[k + 1]) ? 2 : 1; }
 
     OrthArgs square(const OrthOperand& a, const OrthOperand& b, const OrthOperand& c, float alpha) const {  // c = alpha a b, symmetric
         OrthArgs g = {};
@@ -1214,33 +1218,33 @@ template <bool F32> struct Steps {
         return e;
     }
     // S of both steps by the scale that holds both
-    void together(int k, Range& one, Range& two) const {
+    void pair(int k, Range& one, Range& two) const {
         one = ranges[k], two = ranges[k + 1];
         one.s = two.s = fminf(one.s, two.s);
         one.from = one.s / (one.x * one.x);
     }
-    hipError_t two_steps(int k, float joint) {
+    hipError_t two_steps(int k) {
         Range one, two;
-        together(k, one, two);
+        pair(k, one, two);
         hipError_t e = gram(k, one);
         if (e == hipSuccess) e = polynomial(w.q, k, one);
         if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / one.q);
         if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / one.q);  // Q S Q = (Q X) (Q X)^T
         if (e == hipSuccess) e = polynomial(w.t, k + 1, two);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s, joint / (one.q * two.q));
-        if (e == hipSuccess) e = apply<true>(w.s, joint, k, k + 2);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, Q_SCALE / (one.q * two.q));
+        if (e == hipSuccess) e = apply<true>(w.s, Q_SCALE, k, k + 2);
         return e;
     }
     // Two steps' Q in one launch
-    template <int NF> hipError_t link(float* sums, const OrthArgs& of, int k, float joint) {
+    template <int NF> hipError_t link(float* sums, const OrthArgs& of, int k) {
         OrthArgs g = {};
         g.part = sums;
         g.c = w.q;
         lifted(g, 2, k, t.steps);
         Range one, two;
-        together(k, one, two);
+        pair(k, one, two);
         OrthPair p = {};
-        p.from = one.from, p.through = 1.f / one.q, p.joint = joint / (one.q * two.q);
+        p.from = one.from, p.through = 1.f / one.q, p.joint = Q_SCALE / (one.q * two.q);
         one.coefficients(t.coefficients + 3 * k, p.abc[0]);
         two.coefficients(t.coefficients + 3 * k + 3, p.abc[1]);
         constexpr int bytes = 4 * NF * (NF / 2) * ORTH_BLOCK;
@@ -1276,8 +1280,7 @@ template <bool F32> struct Steps {
         // or Q larger (8 x 16 x 14336 in bf16: 65 us in pairs, 83 one by one; 8 x 128 x 256: 85 and 95).
         const bool pairs = NF == 8 || (!F32 && groups > 8);
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const float joint = pairs ? pair(k) : 0.f;
-            const int n = joint > 0 ? 2 : 1;
+            const int n = at_a_time(k, pairs);
             // many ranges are added in a launch of their own, from more of the larger sums on (8 x 100 x 500, 8 of them: 100 us with it, 121 without; 64 x 64 x 300,
             // 3: 84 and 77; 8 x 64 x 2000, 16: 54 and 60)
             g.apart = g.ranges = groups;
@@ -1286,13 +1289,13 @@ template <bool F32> struct Steps {
                 e = hipGetLastError();
                 g.ranges = 1;
             }
-            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, k, joint);
+            if (n == 2 && e == hipSuccess) e = link<NF>(sums, g, k);
             if (e != hipSuccess) break;
             g.sums = sums, g.part = next;
             ranges[k].coefficients(t.coefficients + 3 * k, g.abc);
             g.from = ranges[k].from;
             g.b = w.x[0], g.c = w.x[1];
-            scale(g, k, k + n, n == 2 ? joint : ranges[k].q);
+            scale(g, k, k + n, n == 2 ? Q_SCALE : ranges[k].q);
             k += n;
             constexpr int OUT = F32 ? ORTH_F32 : ORTH_BF16;
             if (k < t.steps) {
@@ -1318,10 +1321,10 @@ template <bool F32> struct Steps {
         const bool pairs = F32 && time.s + time.x > 3 * time.square;
         hipError_t e = hipSuccess;
         for (int k = 0; k < t.steps && e == hipSuccess;) {
-            const float joint = pairs ? pair(k) : 0.f;
-            if constexpr (F32) e = joint > 0 ? two_steps(k, joint) : one_step(k);
+            const int n = at_a_time(k, pairs);
+            if constexpr (F32) e = n == 2 ? two_steps(k) : one_step(k);
             else e = one_step(k);
-            k += joint > 0 ? 2 : 1;
+            k += n;
         }
         return e;
     }

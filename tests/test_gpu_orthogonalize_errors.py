@@ -35,7 +35,7 @@ def errors(G, coefficients):
 
 
 @pytest.mark.parametrize("rows,cols", [(64, 300), (100, 2000), (128, 256), (300, 400), (768, 2048), (2048, 512), (1024, 1024), (1100, 1300), (2048, 4096)])
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("kind", ["gauss", "steep"])
 def test_errors_beside_32_bit_products(rows, cols, dtype, kind):
     G = gradient((rows, cols), rows + cols, dtype, kind).cuda()
