@@ -403,15 +403,15 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
     constexpr int last = 4;  // of the products
 #pragma unroll 1
     for (int op = 0; op <= last; ++op) {
-        const bool sum = op == 0 || op == 3;  // of s: a I + b s + c s s; the others: s q
-        const char* y = sum ? s : q;
+        const bool sum = op == 0 || op == 3;  // of s: a I + b s + c s s; the others: q s (1), s q (2, 4)
+        const char *x = op == 1 ? q : s, *y = sum || op == 1 ? s : q;
         each([&](int m, int n) { v[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
         f16x8_t a[2][2][2], b[2][2][FN];  // the next block's are read while this one's are multiplied
         auto read = [&](int k) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) a[k & 1][p][m] = *(const f16x8_t*)(s + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
+                for (int m = 0; m < 2; ++m) a[k & 1][p][m] = *(const f16x8_t*)(x + p * PLANE + ((row0 + m) * KB + k) * ORTH_BLOCK + at_row);
 #pragma unroll
                 for (int n = 0; n < FN; ++n) b[k & 1][p][n] = *(const f16x8_t*)(y + p * PLANE + ((col0 + n) * KB + k) * ORTH_BLOCK + at_row);
             }
@@ -443,7 +443,7 @@ template <int NF> __global__ __launch_bounds__(NF * 64) void orth_chain_kernel(O
             });
         }
         __syncthreads();
-        // op 1 and 2: s = q s q = (q x) (q x)^T: they commute
+        // op 1 and 2: s = q s q = (q x) (q x)^T
         if (op == last) put(g.c.part[0] + matrix * g.c.matrix, g.c.part[1] - g.c.part[0], g.c.blocks);
         else put(op == 0 ? q : s, PLANE, KB);
         __syncthreads();
@@ -1206,9 +1206,9 @@ template <bool F32> struct Steps {
         g.own = F32 ? nullptr : w.own;
         return product<PARTS, PARTS, false, PARTS, false, PARTS, ORTH_SQUARE>(g, z.tile, st);
     }
-    // to = a q times alpha, of matrices that commute
-    hipError_t times(const OrthOperand& a, const OrthOperand& q, const OrthOperand& to, float alpha) const {
-        return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, q, to, alpha), z.tile, st);
+    // to = a b times alpha, of matrices that commute but for rounding
+    hipError_t times(const OrthOperand& a, const OrthOperand& b, const OrthOperand& to, float alpha) const {
+        return product<2, 2, false, 0, false, 2, ORTH_SQUARE>(square(a, b, to, alpha), z.tile, st);
     }
     hipError_t one_step(int k) {
         const Range& r = ranges[k];
@@ -1228,8 +1228,10 @@ template <bool F32> struct Steps {
         pair(k, one, two);
         hipError_t e = gram(k, one);
         if (e == hipSuccess) e = polynomial(w.q, k, one);
-        if (e == hipSuccess) e = times(w.s, w.q, w.t, 1.f / one.q);
-        if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / one.q);  // Q S Q = (Q X) (Q X)^T
+        // (Q X) (Q X)^T = Q S Q in this order: Q's own rounding does not commute with S, and S Q Q is further from it (steps 4 and 5 of those that raise by 8, 768 x
+        // 2048: 1.2e-5 off, so 5e-6)
+        if (e == hipSuccess) e = times(w.q, w.s, w.t, 1.f / one.q);
+        if (e == hipSuccess) e = times(w.t, w.q, w.s, 1.f / one.q);
         if (e == hipSuccess) e = polynomial(w.t, k + 1, two);
         if (e == hipSuccess) e = times(w.t, w.q, w.s, Q_SCALE / (one.q * two.q));
         if (e == hipSuccess) e = apply<true>(w.s, Q_SCALE, k, k + 2);

@@ -52,3 +52,13 @@ def test_errors_far_below_eps(rows, cols):
         G = (G / G.norm() * (share * 1e-7)).float()
         ours, _ = errors(G, (ABC,) * 5)
         assert ours <= 2 * 12 ** 0.5 * 2.0 ** -22
+
+
+def test_errors_of_a_stack_in_pairs():
+    """Steps in pairs with a pair at the end: its Q S Q is the last S there is."""
+    G = gradient((128, 768, 2048), 768 + 2048, F32).cuda()
+    for coefficients in (RAISING[:5], DAMPED[:5], RAISING[:6]):
+        ref = steps_of(G[0], coefficients)
+        got = moe.moe_orthogonalize(G, steps=len(coefficients), coefficients=coefficients)[0]
+        ours, theirs = (float((t.double() - ref).norm() / ref.norm()) for t in (got, plain(G[0], coefficients)))
+        assert ours <= 2 * theirs, (ours, theirs)
