@@ -12,8 +12,8 @@
 // result's own rounding (1.00 to 1.14 times that in all; without the latter 1.03 to 1.22, and 2.6 for 300 x 400 and the steps of 8; with X in one part steep
 // spectra lose 8e-3, with bf16 operands 6e-2).  More steps carry it further (eight 1.06 to 1.43), and steps whose slope is large where singular values come
 // to lie: 1.0 to 1.8 for the steps of 8, up to 2.5 after four of them; damped by 1 % they stay within 1.24.
-// Measured: 8 matrices of 4096 x 14336 in bf16 29.8 ms (1060 TFLOP/s of the operations above; single products 1100 with X, whose tiles read and write X's
-// parts, and 1170 for S), 32 of 7168 x 2048 in fp32 29.9 ms (1170 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.2 ms.  One-part
+// Measured: 8 matrices of 4096 x 14336 in bf16 30.8 ms (1025 TFLOP/s of the operations above; single products 1070 with X, whose tiles read and write X's
+// parts, and 1130 for S), 32 of 7168 x 2048 in fp32 30.6 ms (1145 TFLOP/s of the products of parts), 128 of 768 x 2048 in bf16 4.4 ms.  One-part
 // products wait for their operands on the way from the L2s through LDS (without these loads the first case takes two thirds of its time); short
 // reductions, as 768, for tiles' beginnings and ends.
 #include "moe_orth.h"
@@ -25,8 +25,8 @@
 namespace {
 
 // X, S and Q = a I + b S + c S S are held times powers of two: in the middle of fp16's range, so that the second parts are seldom subnormal.  These where
-// the coefficients allow them, which the usual ones do (singular values below 2 on the way, Q up to 8); less where they lead further, down to these
-// (singular values of 16, Q of 4094, where the smallest values still have 20 bits).
+// the coefficients allow them, which the usual ones do (singular values below 2 on the way, Q below 16); less where they lead further, down to these
+// (singular values of 16, Q of 4094).
 constexpr float X_SCALE = 8192.f, S_SCALE = 4096.f, Q_SCALE = 2048.f;
 constexpr float X_LEAST = 1024.f, S_LEAST = 64.f, Q_LEAST = 8.f;
 
