@@ -151,7 +151,7 @@ __global__ __launch_bounds__(NORM_THREADS, CH * (sizeof(S) + sizeof(B)) <= 6 ? 4
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float dn = f.gate * g[j] * D[c][j];
-                    out[j] = ry * (dn * w[j] - y[j] * ry * ky);
+                    out[j] = a.norm ? ry * (dn * w[j] - y[j] * ry * ky) : dn * w[j];  // (without a norm y has no part in it, an infinite one neither)
                     dw[c][j] = fmaf(dn, y[j] * ry, dw[c][j]);
                 }
                 Eight<B>::template store<NT>((B*)a.dy + row * a.lddy + col, out);

@@ -65,3 +65,17 @@ def test_gradients_of_rows_of_zeros(d):
         got = moe.moe_residual_norm_backward(dev(dh), dev(x), dev(w), eps=eps)
         close(got[1], ref, ref.abs(), TWICE)
         assert not got[2].any()
+
+
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("d", [64, 2048, 16384])
+@pytest.mark.parametrize("B", [BF16, F32])
+def test_infinite_outputs_of_a_block_without_a_norm(d, B, gate):
+    """dy = gate dout w holds no y."""
+    y, dout, w = normal((4, d), 1).to(B), normal((4, d), 2), 1 + normal((d,), 3, 0.2)
+    g = normal((4,), 4) if gate else None
+    y[1, d // 3], y[2, 0] = float("inf"), float("nan")
+    got = moe.moe_residual_norm_backward(dev(dout), dev(y), dev(w), norm=False, gate=None if g is None else dev(g))
+    ref = dout.double() * w.double() * (1 if g is None else g.double()[:, None])
+    close(got[1], ref, ref.abs(), ONCE)
+    assert torch.equal(got[0].cpu(), dout)
