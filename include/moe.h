@@ -302,13 +302,13 @@ moe_status moe_residual_norm_backward(const void* dout, int64_t lddout, const vo
  *   X = g / (|g| + eps), |g| the root of the sum of its squares;  for (a, b, c) of each step:  S = X X^T,  X = a X + (b S + c S S) X;
  *   out = scale X
  * (where rows > cols: the same on the transpose).  coefficients: host, [steps][3], read before the call returns; steps from 1 to 64.
- * Operands of the products are kept in one or two 16-bit parts (22 bits), sums in 32 bits, |g| in 64: an fp32 result is about as far from the exact one
- * as with products in 32 bits (where |g| is far below eps, and the steps next to a mere factor, 3 10^-7 of its norm), a bf16 result 1 to 1.4 times
- * as far as its own rounding (2.5 after steps whose slope is large where singular values come to lie: such schedules are better damped).  |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow
- * from bounds that hold for any matrix: |X| begins at 1, and a s + b s^3 + c s^5 bounds what a step makes of it.  Steps whose bounds of the singular values
- * before each step stay below 16, and of a + b s^2 + c s^4 below 4000, never leave their range (the usual schedules: 2 and 9); with others a
- * matrix whose own singular values do gives NaN or infinities.  One that holds a NaN or an infinity gives NaN.  Neither spoils another.  A matrix of
- * zeros gives zeros (eps > 0).
+ * Operands of the products are kept in one or two 16-bit parts (22 bits), sums in 32 bits, |g| in 64.  With a not far below b and c an fp32 result is about as
+ * far from the exact one as with products in 32 bits (where |g| is far below eps, and the steps next to a mere factor, 6 10^-7 of its norm at most), a bf16 result
+ * 1 to 1.4 times as far as its own rounding (up to 2.5 after steps whose slope is large where singular values come to lie: such schedules are better damped).
+ * |a| is at most 4000, |b| and |c| 10^6.  The parts' scales follow from bounds that hold for any matrix: |X| begins at 1, and a s + b s^3 + c s^5 bounds what a
+ * step makes of it.  Steps whose bounds of the singular values before each step stay below 16, and of a + b s^2 + c s^4 below 4000, never leave their range
+ * (the usual schedules: 2 and 9); with others a matrix whose own singular values do gives NaN or infinities.  One that holds a NaN or an infinity gives NaN.
+ * Neither spoils another.  A matrix of zeros gives zeros (eps > 0).
  * g and out: rows ldg / ldout values apart (at least cols), matrices stride_g / stride_out values apart, pointers aligned to their values; any
  * sizes from 1 to 2^17, rows * cols <= 2^29, E <= 256.  out may be exactly g (of the same type); otherwise they share no byte.
  * workspace: moe_orthogonalize_workspace_bytes bytes, 256-byte aligned, used until the call's work is done.  Matrices are kept padded: the smaller side to
